@@ -440,6 +440,128 @@ int dels_prior_estimate(const int32_t* tokens, const uint8_t* loss_mask, int64_t
                         float* out_log_prior, uint64_t* out_counts, uint64_t* out_tally, void* workspace,
                         size_t workspace_bytes, dels_stream_t stream);
 
+/* ---- scoring and distillation of vocabulary rows -------------------------- */
+
+/*
+ * Rows of fused logits (Section 4.3), as both operations below read them:
+ *   l[r, v] = (long[r, v] + alpha[r mod n_weights] * short[r, v])
+ *             - beta[r mod n_weights] * log_prior[v],
+ * float32, rounded after every operation; z = l / temperature. A term whose
+ * pointer is NULL is absent, and NULL weights are 1. Rows of B blocks of n
+ * positions in order take per-position weights with n_weights = n. (Position 0
+ * has no head and no prior: give it rows of its own, or weights of 0.)
+ * Unlike the drafting calls these take rows of any alignment and pitch, and the
+ * weights from the device, where they are learned.
+ */
+typedef struct {
+  const void* long_logits;       /* [device] [rows, V], or NULL */
+  const void* short_logits;      /* [device] [rows, V], or NULL; not both NULL */
+  dels_dtype dtype;              /* of both */
+  long long long_stride;         /* elements from one row to the next, >= V; 0: V */
+  long long short_stride;
+  const float* log_prior;        /* [device] [V] finite, or NULL */
+  const float* alpha;            /* [device] [n_weights], or NULL */
+  const float* beta;             /* [device] [n_weights], or NULL */
+  int n_weights;
+  float temperature;             /* finite, > 0 */
+} dels_rows;
+
+/*
+ * Scores rows: with q = softmax(z) of each row,
+ *   out_logprob[r] = log q[tokens[r]],
+ *   out_entropy[r] = -sum_v q_v log q_v (nats),
+ *   out_top_ids[r, k], out_top_logprob[r, k], k < top_k: the most likely entries
+ *     and their log q, largest l first, the lower index first among equal l.
+ * tokens [device] [rows] int32 or NULL (then out_logprob must be NULL). A row
+ * whose token is -1 is left out: it is not read; its log-probability and entropy
+ * are 0, its ids -1 and their log-probabilities -inf. Entries of -inf (masked) are
+ * no alternatives: where a row has fewer than top_k others, the missing ids are -1
+ * and their log-probabilities -inf, which is how dels_distill_* leaves entries out.
+ * A token outside [0, V) other than -1 sets DELS_STATUS_BAD_TOKEN and gives a
+ * log-probability of NaN; a row with NaN or +inf, or of -inf alone, sets
+ * DELS_STATUS_NONFINITE and gives NaN (ids -1).
+ * out_logprob, out_entropy [device] [rows] float32, each may be NULL;
+ * out_top_ids int32 and out_top_logprob float32 [device] [rows, top_k], not read
+ * for top_k = 0. One pass over the rows; every sum is taken in a fixed order, so
+ * that equal calls give equal bits.
+ * Limits: 0 <= rows <= 2^27, 1 <= V <= 2^30, 0 <= top_k <= 256; pointers aligned
+ * to their elements (rows that start on 16 bytes are fastest).
+ */
+size_t dels_score_workspace_bytes(int rows, int V);
+int dels_score_rows(const dels_rows* x, int rows, int V, const int32_t* tokens, int top_k, float* out_logprob,
+                    float* out_entropy, int32_t* out_top_ids, float* out_top_logprob, void* workspace,
+                    size_t workspace_bytes, dels_stream_t stream);
+
+/*
+ * A teacher's most likely entries of each row, as dels_score_rows writes them. An
+ * entry with a negative id or a logprob of -inf is left out (rows may have fewer
+ * than k); an id >= V is left out too and sets DELS_STATUS_BAD_TOKEN. An id listed
+ * more than once counts with the sum of its probabilities in the gradient and
+ * term by term in the loss.
+ *   tail = 0: p_k = softmax over the listed entries of logprob_k / temperature;
+ *   tail = 1: p_k = exp(logprob_k), the student's temperature already in them, and
+ *     what they leave of 1, p_t = max(0, 1 - sum_k p_k), is one more entry: the ids
+ *     that are not listed, all together. It is left out where the student gives
+ *     those ids no probability at all.
+ * row_weight scales a row's loss and gradients; a row of weight 0, and one without
+ * entries, is left out: loss and gradients 0, its logits not read.
+ */
+typedef struct {
+  const int32_t* ids;            /* [device] [rows, k] */
+  const float* logprob;          /* [device] [rows, k] */
+  int k;                         /* 1 .. 256 */
+  int tail;
+  const float* row_weight;       /* [device] [rows] float32, or NULL: 1 */
+} dels_teacher;
+
+/*
+ * Distils the local head (its logits short_logits) from a teacher through the
+ * fusion. Per row, with the student's q = softmax(z) and q_t its sum over the ids
+ * that are not listed:
+ *   loss = row_weight * ( sum_k p_k (log p_k - log q[ids_k])
+ *                         + p_t (log p_t - log q_t) )            (last term: tail = 1)
+ * and the gradients of sum_r grad_loss[r] loss[r]:
+ *   grad_short = alpha * d/dl,
+ *   d/dl_v = grad_loss row_weight / temperature * (M q_v - p_v)          v listed,
+ *            grad_loss row_weight / temperature * (M - p_t / q_t) q_v    other v,
+ *   M = sum_k p_k + p_t (1 without a tail);
+ *   grad_alpha[j] = sum over the rows of weight j and v of short_v d/dl_v,
+ *   grad_beta[j]  = minus the sum of log_prior_v d/dl_v.
+ * (Section 4.2 trains the head by next-token NLL, which is k = 1, logprob 0, tail
+ * = 0; Appendix C learns the weights.)
+ *
+ * dels_distill_loss  the losses, and `state` for dels_distill_grad;
+ * dels_distill_grad  the gradients for given grad_loss [device] [rows] (NULL: 1);
+ *                    the other arguments are those of the dels_distill_loss call;
+ * dels_distill_step  both at once with grad_loss = 1, what a training step calls.
+ *   out_loss   [device] [rows] float32;
+ *   state      [device] >= dels_distill_state_bytes(rows), 16-byte aligned, contents
+ *              private to the library;
+ *   grad_short [device] [rows, V] of the rows' dtype, grad_stride elements from one
+ *              row to the next (0: V); it may be short_logits itself with the same
+ *              stride (then overwritten);
+ *   grad_alpha, grad_beta [device] [n_weights] float32, overwritten, each may be
+ *              NULL; they need alpha, and beta and log_prior.
+ * A row with NaN or +inf logits, or of -inf alone, or with a teacher logprob of NaN
+ * or +inf sets DELS_STATUS_NONFINITE; its loss and gradients are NaN. Sums are
+ * float32 in a fixed order: equal calls give equal bits.
+ * Limits: 0 <= rows <= 2^27, 1 <= V <= 2^22; short_logits is required; pointers
+ * aligned to their elements (rows that start on 16 bytes are fastest). The status
+ * word is in the workspace of dels_distill_loss and dels_distill_step;
+ * dels_distill_grad raises none. dels_distill_loss needs 256 bytes of workspace,
+ * dels_distill_step dels_distill_workspace_bytes.
+ */
+size_t dels_distill_state_bytes(int rows);
+size_t dels_distill_workspace_bytes(int rows, int V);
+int dels_distill_loss(const dels_rows* x, int rows, int V, const dels_teacher* teacher, float* out_loss, void* state,
+                      size_t state_bytes, void* workspace, size_t workspace_bytes, dels_stream_t stream);
+int dels_distill_grad(const dels_rows* x, int rows, int V, const dels_teacher* teacher, const float* grad_loss,
+                      const void* state, size_t state_bytes, void* grad_short, long long grad_stride,
+                      float* grad_alpha, float* grad_beta, dels_stream_t stream);
+int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* teacher, float* out_loss,
+                      void* grad_short, long long grad_stride, float* grad_alpha, float* grad_beta, void* workspace,
+                      size_t workspace_bytes, dels_stream_t stream);
+
 /* ---- instrumentation (not part of the method) ---------------------------- */
 
 /* Kernel classes timed by the optional per-kernel profiler. */
@@ -453,7 +575,9 @@ enum {
   DELS_KCLASS_COMBINE = 6,       /* dels_combine_argmax                                   */
   DELS_KCLASS_DRAFT_BLOCK = 7,   /* persistent per-block drafting kernel (whole block)    */
   DELS_KCLASS_PRIOR = 8,         /* unigram prior estimation (count, sum, log)            */
-  DELS_KCLASS_COUNT = 9
+  DELS_KCLASS_SCORE = 9,         /* scoring of rows                                       */
+  DELS_KCLASS_DISTILL = 10,      /* distillation loss and gradients                       */
+  DELS_KCLASS_COUNT = 11
 };
 
 /*

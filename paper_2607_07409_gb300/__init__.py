@@ -34,6 +34,9 @@ __all__ = [
     "dels_selftest_timeout_bytes", "dels_selftest_timeout", "dels_selftest_gumbel",
     "dels_prior_workspace_bytes", "dels_prior_count", "dels_prior_log", "dels_prior_estimate", "estimate_prior",
     "make_head", "Drafter", "dtype_code",
+    "Rows", "Teacher", "dels_score_workspace_bytes", "dels_score_rows",
+    "dels_distill_state_bytes", "dels_distill_workspace_bytes", "dels_distill_loss", "dels_distill_grad",
+    "dels_distill_step", "rows_of", "teacher_of", "TokenScorer", "Distiller", "distill_loss",
 ]
 
 DELS_OK = 0
@@ -63,6 +66,28 @@ class LocalHead(ctypes.Structure):
     ]
 
 
+class Rows(ctypes.Structure):
+    """Mirror of ``dels_rows``."""
+
+    _fields_ = [
+        ("long_logits", ctypes.c_void_p), ("short_logits", ctypes.c_void_p), ("dtype", ctypes.c_int),
+        ("long_stride", ctypes.c_longlong), ("short_stride", ctypes.c_longlong),
+        ("log_prior", ctypes.c_void_p), ("alpha", ctypes.c_void_p), ("beta", ctypes.c_void_p),
+        ("n_weights", ctypes.c_int), ("temperature", ctypes.c_float),
+    ]
+
+
+class Teacher(ctypes.Structure):
+    """Mirror of ``dels_teacher``."""
+
+    _fields_ = [
+        ("ids", ctypes.c_void_p), ("logprob", ctypes.c_void_p), ("k", ctypes.c_int), ("tail", ctypes.c_int),
+        ("row_weight", ctypes.c_void_p),
+    ]
+
+
+_ROWS, _TEACHER, _ll = ctypes.POINTER(Rows), ctypes.POINTER(Teacher), ctypes.c_longlong
+
 _SIGS = {
     "dels_selftest_timeout_bytes": (_sz, []),
     "dels_selftest_timeout": (_i, [_vp, _sz, _vp]),
@@ -91,6 +116,13 @@ _SIGS = {
     "dels_prior_count": (_i, [_vp, _vp, ctypes.c_int64, _i, _vp, _vp, _vp, _sz, _vp]),
     "dels_prior_log": (_i, [_vp, _i, _d, _vp, _vp, _sz, _vp]),
     "dels_prior_estimate": (_i, [_vp, _vp, ctypes.c_int64, _i, _d, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dels_score_workspace_bytes": (_sz, [_i, _i]),
+    "dels_score_rows": (_i, [_ROWS, _i, _i, _vp, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dels_distill_state_bytes": (_sz, [_i]),
+    "dels_distill_workspace_bytes": (_sz, [_i, _i]),
+    "dels_distill_loss": (_i, [_ROWS, _i, _i, _TEACHER, _vp, _vp, _sz, _vp, _sz, _vp]),
+    "dels_distill_grad": (_i, [_ROWS, _i, _i, _TEACHER, _vp, _vp, _sz, _vp, _ll, _vp, _vp, _vp]),
+    "dels_distill_step": (_i, [_ROWS, _i, _i, _TEACHER, _vp, _vp, _ll, _vp, _vp, _vp, _sz, _vp]),
     "dels_status_string": (ctypes.c_char_p, [_i]),
     "dels_version": (_i, []),
     "dels_profile_enable": (_i, [_i]),
@@ -100,7 +132,7 @@ _SIGS = {
 
 # kernel classes of the optional profiler
 KCLASS = {"vocab_combine": 0, "head_gemm": 1, "head_misc": 2, "merge": 3, "pos0": 4, "verify": 5, "combine": 6,
-          "draft_block": 7, "prior": 8}
+          "draft_block": 7, "prior": 8, "score": 9, "distill": 10}
 
 
 def exported_symbols():
@@ -386,6 +418,46 @@ def estimate_prior(tokens: torch.Tensor, loss_mask: torch.Tensor, V: int, lam: f
     return out, counts, tally
 
 
+def dels_score_workspace_bytes(rows: int, V: int) -> int:
+    return lib().dels_score_workspace_bytes(rows, V)
+
+
+def dels_score_rows(x: Rows, rows: int, V: int, tokens, top_k: int, out_logprob, out_entropy, out_top_ids,
+                    out_top_logprob, workspace, workspace_bytes: int, stream=None) -> int:
+    return lib().dels_score_rows(ctypes.byref(x), rows, V, _ptr(tokens), top_k, _ptr(out_logprob), _ptr(out_entropy),
+                                 _ptr(out_top_ids), _ptr(out_top_logprob), _ptr(workspace), workspace_bytes,
+                                 _stream(stream))
+
+
+def dels_distill_state_bytes(rows: int) -> int:
+    return lib().dels_distill_state_bytes(rows)
+
+
+def dels_distill_workspace_bytes(rows: int, V: int) -> int:
+    return lib().dels_distill_workspace_bytes(rows, V)
+
+
+def dels_distill_loss(x: Rows, rows: int, V: int, teacher: Teacher, out_loss, state, state_bytes: int, workspace,
+                      workspace_bytes: int, stream=None) -> int:
+    return lib().dels_distill_loss(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(out_loss), _ptr(state),
+                                   state_bytes, _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def dels_distill_grad(x: Rows, rows: int, V: int, teacher: Teacher, grad_loss, state, state_bytes: int, grad_short,
+                      grad_stride: int, grad_alpha, grad_beta, stream=None) -> int:
+    """``grad_short``: a tensor whose rows may be strided, or an address (``grad_stride`` elements a row)."""
+    return lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(grad_loss), _ptr(state),
+                                   state_bytes, _row_ptr(grad_short), grad_stride, _ptr(grad_alpha), _ptr(grad_beta),
+                                   _stream(stream))
+
+
+def dels_distill_step(x: Rows, rows: int, V: int, teacher: Teacher, out_loss, grad_short, grad_stride: int,
+                      grad_alpha, grad_beta, workspace, workspace_bytes: int, stream=None) -> int:
+    return lib().dels_distill_step(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(out_loss),
+                                   _row_ptr(grad_short), grad_stride, _ptr(grad_alpha), _ptr(grad_beta),
+                                   _ptr(workspace), workspace_bytes, _stream(stream))
+
+
 def dels_profile_enable(on: bool) -> None:
     _check(lib().dels_profile_enable(1 if on else 0), "dels_profile_enable")
 
@@ -476,3 +548,215 @@ class Drafter:
 
     def status(self, stream=None) -> int:
         return dels_read_status(self.workspace, stream)
+
+
+# ----------------------------------------------------------------------------- scoring and distillation
+
+def _row_ptr(x) -> Optional[int]:
+    """Device address of [rows, V] logits whose rows may be strided."""
+    if not isinstance(x, torch.Tensor):
+        return _ptr(x)
+    if not x.is_cuda:
+        raise ValueError("expected a CUDA tensor: the library's entry points take device pointers")
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("expected [rows, V] logits whose rows are dense")
+    return x.data_ptr()
+
+
+def _row_stride(x: torch.Tensor, what: str) -> int:
+    """Elements from one row to the next (a single row's own length: its stride may be anything)."""
+    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        raise ValueError(f"{what}: rows overlap")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _of(t, dtype, shape, device, what) -> Optional[int]:
+    """Device address of a dense tensor of this dtype and shape on this device."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device:
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on {device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+    return _ptr(t)
+
+
+def _logits(x, rows: int, V: int, dtype, device, what) -> torch.Tensor:
+    if tuple(x.shape) != (rows, V) or x.dtype != dtype or x.device != device:
+        raise ValueError(f"{what} must be {dtype} [{rows}, {V}] on {device}, got {x.dtype} {list(x.shape)} on {x.device}")
+    return x
+
+
+def rows_of(rows: int, V: int, long=None, short=None, log_prior=None, alpha=None, beta=None,
+            temperature: float = 1.0) -> Rows:
+    """``dels_rows`` of [rows, V] logit tensors (one dtype, rows may be strided), a
+    [V] prior and [n_weights] fusion weights. The caller keeps the tensors alive."""
+    one = long if long is not None else short
+    if one is None:
+        raise ValueError("rows need long or short logits")
+    x = Rows()
+    x.dtype = dtype_code(one)
+    for t, name in ((long, "long"), (short, "short")):
+        if t is not None:
+            _logits(t, rows, V, one.dtype, one.device, name)
+            setattr(x, name + "_logits", _row_ptr(t))
+            setattr(x, name + "_stride", _row_stride(t, name))
+    x.log_prior = _of(log_prior, torch.float32, (V,), one.device, "log_prior")
+    n = [w.numel() for w in (alpha, beta) if w is not None]
+    if len(set(n)) > 1:
+        raise ValueError("alpha and beta must have the same length")
+    x.n_weights = n[0] if n else 0
+    x.alpha = _of(alpha, torch.float32, (x.n_weights,), one.device, "alpha")
+    x.beta = _of(beta, torch.float32, (x.n_weights,), one.device, "beta")
+    x.temperature = float(temperature)
+    return x
+
+
+def teacher_of(rows: int, ids: torch.Tensor, logprob: torch.Tensor, row_weight=None, tail: bool = False) -> Teacher:
+    """``dels_teacher`` of [rows, k] ids and log-probabilities. The caller keeps the tensors alive."""
+    if ids.dim() != 2:
+        raise ValueError("ids must be [rows, k]")
+    t = Teacher()
+    t.k, t.tail = ids.shape[1], int(bool(tail))
+    t.ids = _of(ids, torch.int32, (rows, t.k), ids.device, "ids")
+    t.logprob = _of(logprob, torch.float32, (rows, t.k), ids.device, "logprob")
+    t.row_weight = _of(row_weight, torch.float32, (rows,), ids.device, "row_weight")
+    return t
+
+
+class TokenScorer:
+    """Log-probabilities of given tokens, entropies and the ``top_k`` most likely
+    entries of [rows, V] logits, plain or fused: outputs and a workspace for
+    repeated ``dels_score_rows`` calls."""
+
+    def __init__(self, rows: int, V: int, top_k: int = 0, device=None):
+        self.rows, self.V, self.top_k = rows, V, top_k
+        self.device = torch.device(device or "cuda")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.ws_bytes = dels_score_workspace_bytes(rows, V)
+        if self.ws_bytes == 0:
+            raise DelsError(DELS_ERR_BAD_SHAPE, "dels_score_workspace_bytes")
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self.logprob = torch.empty(rows, dtype=torch.float32, device=self.device)
+        self.entropy = torch.empty(rows, dtype=torch.float32, device=self.device)
+        self.top_ids = torch.empty(rows, top_k, dtype=torch.int32, device=self.device) if top_k else None
+        self.top_logprob = torch.empty(rows, top_k, dtype=torch.float32, device=self.device) if top_k else None
+
+    def __call__(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, short=None, log_prior=None,
+                 alpha=None, beta=None, temperature: float = 1.0, stream=None):
+        """(log-probabilities or None without tokens, entropies, top ids, top log-probabilities)."""
+        x = rows_of(self.rows, self.V, logits, short, log_prior, alpha, beta, temperature)
+        _logits(logits, self.rows, self.V, logits.dtype, self.device, "logits")
+        tok = _of(tokens, torch.int32, (self.rows,), self.device, "tokens")
+        lp = self.logprob if tokens is not None else None
+        _check(dels_score_rows(x, self.rows, self.V, tok, self.top_k, lp, self.entropy, self.top_ids,
+                               self.top_logprob, self.workspace, self.ws_bytes, stream), "dels_score_rows")
+        return lp, self.entropy, self.top_ids, self.top_logprob
+
+    def status(self, stream=None) -> int:
+        return dels_read_status(self.workspace, stream)
+
+
+class Distiller:
+    """Distillation of a local head's [rows, V] logits from ``k`` teacher entries a
+    row: outputs, state and a workspace for repeated calls. ``n_weights``: fusion
+    weights of the calls' alpha and beta."""
+
+    def __init__(self, rows: int, V: int, k: int, dtype: torch.dtype, n_weights: int = 1, tail: bool = False,
+                 temperature: float = 1.0, device=None):
+        self.rows, self.V, self.k, self.dtype, self.n_weights = rows, V, k, dtype, n_weights
+        self.tail, self.temperature = tail, temperature
+        dtype_code(dtype)
+        self.device = torch.device(device or "cuda")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.ws_bytes = dels_distill_workspace_bytes(rows, V)
+        if self.ws_bytes == 0:
+            raise DelsError(DELS_ERR_BAD_SHAPE, "dels_distill_workspace_bytes")
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self._loss = torch.empty(rows, dtype=torch.float32, device=self.device)
+        self._grad = self._state = None
+        self._grad_w = torch.empty(2, n_weights, dtype=torch.float32, device=self.device)
+
+    def _args(self, short, ids, logprob, long, log_prior, alpha, beta, row_weight):
+        _logits(short, self.rows, self.V, self.dtype, self.device, "short")
+        x = rows_of(self.rows, self.V, long, short, log_prior, alpha, beta, self.temperature)
+        if x.n_weights not in (0, self.n_weights):
+            raise ValueError(f"alpha and beta must have {self.n_weights} entries")
+        t = teacher_of(self.rows, ids, logprob, row_weight, self.tail)
+        if t.k != self.k or ids.device != self.device:
+            raise ValueError(f"ids must be [{self.rows}, {self.k}] on {self.device}")
+        return x, t
+
+    def loss(self, short, ids, logprob, *, long=None, log_prior=None, alpha=None, beta=None, row_weight=None,
+             stream=None) -> torch.Tensor:
+        """The rows' losses, float32 [rows]."""
+        x, t = self._args(short, ids, logprob, long, log_prior, alpha, beta, row_weight)
+        if self._state is None:
+            self._state = torch.empty(dels_distill_state_bytes(self.rows), dtype=torch.uint8, device=self.device)
+        _check(dels_distill_loss(x, self.rows, self.V, t, self._loss, self._state, self._state.numel(),
+                                 self.workspace, self.ws_bytes, stream), "dels_distill_loss")
+        return self._loss
+
+    def step(self, short, ids, logprob, *, long=None, log_prior=None, alpha=None, beta=None, row_weight=None,
+             out=None, stream=None):
+        """(losses, gradient of ``short``, of alpha, of beta) of the sum of the losses;
+        the weights' are None where the call has none (beta's too without a prior).
+        ``out``: where the gradient goes ([rows, V], ``short`` itself for in place)."""
+        x, t = self._args(short, ids, logprob, long, log_prior, alpha, beta, row_weight)
+        if out is None:
+            if self._grad is None:
+                self._grad = torch.empty(self.rows, self.V, dtype=self.dtype, device=self.device)
+            out = self._grad
+        _logits(out, self.rows, self.V, self.dtype, self.device, "out")
+        ga = self._grad_w[0] if alpha is not None else None
+        gb = self._grad_w[1] if beta is not None and log_prior is not None else None
+        _check(dels_distill_step(x, self.rows, self.V, t, self._loss, out, _row_stride(out, "out"), ga, gb, self.workspace,
+                                 self.ws_bytes, stream), "dels_distill_step")
+        return self._loss, out, ga, gb
+
+    def status(self, stream=None) -> int:
+        return dels_read_status(self.workspace, stream)
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature):
+        if short.dim() != 2:
+            raise ValueError("short must be [rows, V]")
+        rows, V = short.shape
+        dev = short.device
+        if ids.device != dev:
+            raise ValueError(f"ids must be on {dev}")
+        x = rows_of(rows, V, long, short, log_prior, alpha, beta, temperature)
+        t = teacher_of(rows, ids, logprob, row_weight, tail)
+        loss = torch.empty(rows, dtype=torch.float32, device=dev)
+        state = torch.empty(dels_distill_state_bytes(rows), dtype=torch.uint8, device=dev)
+        ws = torch.empty(256, dtype=torch.uint8, device=dev)   # its status word is not read: flagged rows are NaN
+        _check(dels_distill_loss(x, rows, V, t, loss, state, state.numel(), ws, 256), "dels_distill_loss")
+        ctx.save_for_backward(short, alpha, beta, long, log_prior, ids, logprob, row_weight, state)
+        ctx.tail, ctx.temperature = tail, temperature
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        short, alpha, beta, long, log_prior, ids, logprob, row_weight, state = ctx.saved_tensors
+        rows, V = short.shape
+        x = rows_of(rows, V, long, short, log_prior, alpha, beta, ctx.temperature)
+        t = teacher_of(rows, ids, logprob, row_weight, ctx.tail)
+        grad = torch.empty(rows, V, dtype=short.dtype, device=short.device)
+        ga = torch.empty_like(alpha) if alpha is not None and ctx.needs_input_grad[1] else None
+        gb = (torch.empty_like(beta) if beta is not None and log_prior is not None and ctx.needs_input_grad[2]
+              else None)
+        up = grad_loss.to(torch.float32).contiguous()
+        _check(dels_distill_grad(x, rows, V, t, up, state, state.numel(), grad, V, ga, gb), "dels_distill_grad")
+        return (grad, ga, gb) + (None,) * 7
+
+
+def distill_loss(short, ids, logprob, *, long=None, log_prior=None, alpha=None, beta=None, row_weight=None,
+                 tail: bool = False, temperature: float = 1.0) -> torch.Tensor:
+    """Distillation losses [rows] of a local head's logits, differentiable in
+    ``short``, ``alpha`` and ``beta``, on the current stream. Rows flagged as
+    non-finite have a loss of NaN."""
+    return _DistillLoss.apply(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature)

@@ -2082,3 +2082,229 @@ int dels_draft_block_weighted(const dels_local_head* head, const void* long_logi
 }
 
 }  // extern "C"
+
+// ------------------------------------------- scoring and distillation of rows
+
+namespace {
+
+// A call's rows: its checks, and the kernels' view of them.
+struct RowsCall {
+  StreamRows in{};
+  bool fused = false;   // more than one term, or weights
+  bool vec = false;     // every row starts on a 16-byte boundary
+};
+
+int rows_call(const dels_rows* x, int rows, int V, int max_v, RowsCall* out) {
+  if (!x) return DELS_ERR_NULL_POINTER;
+  if (x->dtype != DELS_F32 && x->dtype != DELS_BF16) return DELS_ERR_BAD_DTYPE;
+  if (rows < 0 || rows > (1 << 27) || V < 1 || V > max_v) return DELS_ERR_BAD_SHAPE;
+  if (!(x->temperature > 0.f) || !std::isfinite(x->temperature) || !std::isfinite(1.f / x->temperature))
+    return DELS_ERR_BAD_SHAPE;
+  const bool has_long = x->long_logits != nullptr, has_short = x->short_logits != nullptr;
+  if (x->n_weights < 0 || ((x->alpha || x->beta) && x->n_weights < 1)) return DELS_ERR_BAD_SHAPE;
+  const long long ld_long = x->long_stride ? x->long_stride : V, ld_short = x->short_stride ? x->short_stride : V;
+  if ((has_long && ld_long < V) || (has_short && ld_short < V)) return DELS_ERR_BAD_SHAPE;
+  if (rows > 0 && !has_long && !has_short) return DELS_ERR_NULL_POINTER;
+  const uintptr_t es = x->dtype == DELS_F32 ? 4 : 2;
+  const auto off = [](const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; };
+  if (off(x->long_logits, es) || off(x->short_logits, es) || off(x->log_prior, 4) || off(x->alpha, 4) ||
+      off(x->beta, 4))
+    return DELS_ERR_ALIGNMENT;
+  StreamRows& in = out->in;
+  in.longp = x->long_logits;
+  in.shortp = x->short_logits;
+  in.prior = x->log_prior;
+  in.alpha = x->alpha;
+  in.beta = x->beta;
+  in.ld_long = ld_long;
+  in.ld_short = ld_short;
+  in.n_weights = std::max(1, x->n_weights);
+  in.rows = rows;
+  in.V = V;
+  in.inv_t = 1.f / x->temperature;
+  in.scale = (float)(1.4426950408889634 / (double)x->temperature);
+  out->fused = in.prior || (has_long && has_short) || (has_short && in.alpha);
+  out->vec = !off(in.longp, 16) && !off(in.shortp, 16) && !off(in.prior, 16) &&
+             (!has_long || ld_long * (long long)es % 16 == 0) && (!has_short || ld_short * (long long)es % 16 == 0);
+  if (!out->fused && !has_long) {      // the student's logits alone: read as the one term
+    in.longp = in.shortp;
+    in.ld_long = in.ld_short;
+    in.shortp = nullptr;
+  }
+  return DELS_OK;
+}
+
+// CTAs per row: as many as bring four per SM into flight, at slices of 4096
+// columns and more, a power of two up to 8; at least `least`.
+void plan_cluster(StreamRows& in, int sms, int least) {
+  int c = 1;
+  while (c < 8 && (c < least || ((long long)in.rows * c < 4LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
+  in.cluster = c;
+  in.slice_cols = (int)round_up((size_t)(in.V + c - 1) / c, 8);
+}
+
+int distill_call(const dels_rows* x, int rows, int V, const dels_teacher* t, RowsCall* call, DistillArgs* a) {
+  const int rc = rows_call(x, rows, V, kMaxDistillV, call);
+  if (rc != DELS_OK) return rc;
+  if (!t) return DELS_ERR_NULL_POINTER;
+  if (t->k < 1 || t->k > kMaxTopK) return DELS_ERR_BAD_SHAPE;
+  if (rows > 0 && (!x->short_logits || !t->ids || !t->logprob)) return DELS_ERR_NULL_POINTER;
+  const auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
+  if (off4(t->ids) || off4(t->logprob) || off4(t->row_weight)) return DELS_ERR_ALIGNMENT;
+  a->in = call->in;
+  a->ids = t->ids;
+  a->teacher = t->logprob;
+  a->K = t->k;
+  a->tail = t->tail != 0;
+  a->row_weight = t->row_weight;
+  return DELS_OK;
+}
+
+bool plan_distill(DistillArgs* a) {
+  const int sms = device_sm_count();
+  if (sms <= 0) return false;
+  plan_cluster(a->in, sms, (a->in.V + (1 << 19) - 1) >> 19);     // a slice's bitmap: at most 64 KB
+  return true;
+}
+
+// The gradient's side of a call.
+int distill_grad_call(const dels_rows* x, int rows, int V, void* grad_short, long long grad_stride, float* grad_alpha,
+                      float* grad_beta, RowsCall* call, DistillArgs* a) {
+  if ((rows > 0 && !grad_short) || (grad_alpha && !x->alpha) || (grad_beta && (!x->beta || !x->log_prior)))
+    return DELS_ERR_NULL_POINTER;
+  const long long ld = grad_stride ? grad_stride : V;
+  if (ld < V) return DELS_ERR_BAD_SHAPE;
+  const uintptr_t es = x->dtype == DELS_F32 ? 4 : 2, at = reinterpret_cast<uintptr_t>(grad_short);
+  if ((at & (es - 1)) || (reinterpret_cast<uintptr_t>(grad_alpha) & 3u) || (reinterpret_cast<uintptr_t>(grad_beta) & 3u))
+    return DELS_ERR_ALIGNMENT;
+  call->vec = call->vec && (at & 15u) == 0 && ld * (long long)es % 16 == 0;
+  a->grad = grad_short;
+  a->ld_grad = ld;
+  a->grad_alpha = grad_alpha;
+  a->grad_beta = grad_beta;
+  return DELS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dels_score_workspace_bytes(int rows, int V) {
+  return rows < 0 || V < 1 || V > kMaxScoreV ? 0 : (size_t)kHeaderBytes;
+}
+
+int dels_score_rows(const dels_rows* x, int rows, int V, const int32_t* tokens, int top_k, float* out_logprob,
+                    float* out_entropy, int32_t* out_top_ids, float* out_top_logprob, void* workspace,
+                    size_t workspace_bytes, dels_stream_t stream) {
+  RowsCall call;
+  const int rc = rows_call(x, rows, V, kMaxScoreV, &call);
+  if (rc != DELS_OK) return rc;
+  if (top_k < 0 || top_k > kMaxTopK) return DELS_ERR_BAD_SHAPE;
+  if (!workspace || workspace_bytes < (size_t)kHeaderBytes) return DELS_ERR_WORKSPACE;
+  if (rows == 0) return DELS_OK;
+  if ((out_logprob && !tokens) || (top_k > 0 && (!out_top_ids || !out_top_logprob))) return DELS_ERR_NULL_POINTER;
+  const auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
+  if (!aligned16(workspace) || off4(tokens) || off4(out_logprob) || off4(out_entropy) || off4(out_top_ids) ||
+      off4(out_top_logprob))
+    return DELS_ERR_ALIGNMENT;
+  const int sms = device_sm_count();
+  if (sms <= 0) return DELS_ERR_CUDA;
+  plan_cluster(call.in, sms, 1);
+  ScoreArgs a{};
+  a.in = call.in;
+  a.tokens = tokens;
+  a.top_k = top_k;
+  a.out_lp = out_logprob;
+  a.out_entropy = out_entropy;
+  a.out_ids = out_top_ids;
+  a.out_top_lp = out_top_logprob;
+  a.status = at<int>(workspace, 0);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  PROF(DELS_KCLASS_SCORE);
+  if (launch_score_rows(a, x->dtype == DELS_F32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+size_t dels_distill_state_bytes(int rows) { return rows < 0 ? 0 : (size_t)rows * sizeof(DistillState); }
+
+size_t dels_distill_workspace_bytes(int rows, int V) {
+  if (rows < 0 || V < 1 || V > kMaxDistillV) return 0;
+  return (size_t)kHeaderBytes + dels_distill_state_bytes(rows);
+}
+
+int dels_distill_loss(const dels_rows* x, int rows, int V, const dels_teacher* teacher, float* out_loss, void* state,
+                      size_t state_bytes, void* workspace, size_t workspace_bytes, dels_stream_t stream) {
+  RowsCall call;
+  DistillArgs a{};
+  const int rc = distill_call(x, rows, V, teacher, &call, &a);
+  if (rc != DELS_OK) return rc;
+  if (!workspace || workspace_bytes < (size_t)kHeaderBytes) return DELS_ERR_WORKSPACE;
+  if (rows == 0) return DELS_OK;
+  if (!out_loss || !state) return DELS_ERR_NULL_POINTER;
+  if (state_bytes < dels_distill_state_bytes(rows)) return DELS_ERR_WORKSPACE;
+  if (!aligned16(workspace) || !aligned16(state) || (reinterpret_cast<uintptr_t>(out_loss) & 3u))
+    return DELS_ERR_ALIGNMENT;
+  if (!plan_distill(&a)) return DELS_ERR_CUDA;
+  a.out_loss = out_loss;
+  a.state = static_cast<DistillState*>(state);
+  a.status = at<int>(workspace, 0);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  PROF(DELS_KCLASS_DISTILL);
+  if (launch_distill_loss(a, x->dtype == DELS_F32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+int dels_distill_grad(const dels_rows* x, int rows, int V, const dels_teacher* teacher, const float* grad_loss,
+                      const void* state, size_t state_bytes, void* grad_short, long long grad_stride,
+                      float* grad_alpha, float* grad_beta, dels_stream_t stream) {
+  RowsCall call;
+  DistillArgs a{};
+  int rc = distill_call(x, rows, V, teacher, &call, &a);
+  if (rc != DELS_OK) return rc;
+  rc = distill_grad_call(x, rows, V, grad_short, grad_stride, grad_alpha, grad_beta, &call, &a);
+  if (rc != DELS_OK) return rc;
+  if (rows > 0) {
+    if (!state) return DELS_ERR_NULL_POINTER;
+    if (state_bytes < dels_distill_state_bytes(rows)) return DELS_ERR_WORKSPACE;
+    if (!aligned16(state) || (reinterpret_cast<uintptr_t>(grad_loss) & 3u)) return DELS_ERR_ALIGNMENT;
+  }
+  if (!plan_distill(&a)) return DELS_ERR_CUDA;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  a.state = static_cast<DistillState*>(const_cast<void*>(state));
+  a.grad_loss = grad_loss;
+  PROF(DELS_KCLASS_DISTILL);
+  if (rows > 0 && launch_distill_grad(a, x->dtype == DELS_F32, call.fused, call.vec, s) != cudaSuccess)
+    return DELS_ERR_CUDA;
+  if ((grad_alpha || grad_beta) && launch_weight_grads(a, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* teacher, float* out_loss,
+                      void* grad_short, long long grad_stride, float* grad_alpha, float* grad_beta, void* workspace,
+                      size_t workspace_bytes, dels_stream_t stream) {
+  RowsCall call;
+  DistillArgs a{};
+  int rc = distill_call(x, rows, V, teacher, &call, &a);
+  if (rc != DELS_OK) return rc;
+  if (!workspace || workspace_bytes < dels_distill_workspace_bytes(rows, V)) return DELS_ERR_WORKSPACE;
+  const bool loss_vec = call.vec;
+  rc = distill_grad_call(x, rows, V, grad_short, grad_stride, grad_alpha, grad_beta, &call, &a);
+  if (rc != DELS_OK) return rc;
+  if (rows > 0 && !out_loss) return DELS_ERR_NULL_POINTER;
+  if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(out_loss) & 3u)) return DELS_ERR_ALIGNMENT;
+  if (!plan_distill(&a)) return DELS_ERR_CUDA;
+  a.out_loss = out_loss;
+  a.state = at<DistillState>(workspace, kHeaderBytes);
+  a.status = at<int>(workspace, 0);
+  const bool f32 = x->dtype == DELS_F32;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  PROF(DELS_KCLASS_DISTILL);
+  if (rows > 0) {
+    if (launch_distill_loss(a, f32, call.fused, loss_vec, s) != cudaSuccess) return DELS_ERR_CUDA;
+    if (launch_distill_grad(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
+  }
+  if ((grad_alpha || grad_beta) && launch_weight_grads(a, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+}  // extern "C"

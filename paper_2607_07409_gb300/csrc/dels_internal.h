@@ -106,6 +106,77 @@ struct CombineLayout {
 };
 CombineLayout combine_layout(int rows, int V, dels_dtype dtype, int sms);
 
+// ---- scoring and distillation of vocabulary rows ---------------------------
+// Rows l = (l_L + alpha l_S) - beta l_P over temperature T; weight r % n_weights
+// of row r (null: 1). A plain row has longp alone.
+struct StreamRows {
+  const void* longp;
+  const void* shortp;
+  const float* prior;
+  const float* alpha;            // [device] [n_weights]
+  const float* beta;
+  long long ld_long, ld_short;   // elements from one row to the next
+  int n_weights;
+  int rows, V;
+  float inv_t;                   // 1 / T
+  float scale;                   // log2(e) / T
+  int cluster;                   // CTAs per row
+  int slice_cols;                // columns per CTA (a multiple of 8)
+};
+
+constexpr int kMaxTopK = 256;
+constexpr int kMaxScoreV = 1 << 30;      // columns: offsets inside a row stay below 2^31
+constexpr int kMaxDistillV = 1 << 22;    // a slice's bitmap of listed ids fits a CTA's shared memory
+
+struct ScoreArgs {
+  StreamRows in;
+  const int32_t* tokens;         // [rows] or null
+  int top_k;
+  float* out_lp;                 // [rows] or null
+  float* out_entropy;            // [rows] or null
+  int32_t* out_ids;              // [rows, top_k]
+  float* out_top_lp;             // [rows, top_k]
+  int* status;
+};
+cudaError_t launch_score_rows(const ScoreArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
+
+// Statistics of one row, written by the loss kernel and read by the gradient's.
+struct DistillState {
+  float m;          // largest student entry
+  float inv_s;      // 1 / S, S = sum exp((l - m) / T)
+  float ln_s;       // ln S
+  float coef_n;     // dL/dl of an id that is not listed: q coef_n / T
+  float mass;       // of a listed one: (q mass - p) / T
+  float t_max;      // teacher: ln p = (t - t_max) t_scale - log_norm
+  float t_scale;
+  float log_norm;
+  float weight;     // the row's weight; 0: left out
+  float d_alpha;    // dL/d alpha, dL/d beta (weight included)
+  float d_beta;
+  float pad[5];
+};
+static_assert(sizeof(DistillState) == 64, "one 64-byte record per row");
+
+struct DistillArgs {
+  StreamRows in;                 // shortp: the student's logits
+  const int32_t* ids;            // [rows, K]
+  const float* teacher;          // [rows, K]
+  int K, tail;
+  const float* row_weight;       // [rows] or null
+  float* out_loss;               // [rows] or null
+  DistillState* state;           // [rows]
+  // gradient
+  const float* grad_loss;        // [rows] or null
+  void* grad;                    // [rows, V] of the logits' type
+  long long ld_grad;
+  float* grad_alpha;             // [n_weights] or null
+  float* grad_beta;
+  int* status;
+};
+cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
+cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
+cudaError_t launch_weight_grads(const DistillArgs& a, cudaStream_t s);
+
 // ---- draft merge + gather of the next local-head input ----------------------
 // Temperature-1 drafting (on = 0: temperature 0). The uniforms of (request
 // b, position j, stream, vocabulary index) come from Philox4x32-10 keyed by
