@@ -2122,10 +2122,15 @@ int rows_call(const dels_rows* x, int rows, int V, int max_v, RowsCall* out) {
   in.rows = rows;
   in.V = V;
   in.inv_t = 1.f / x->temperature;
+  in.minus_zero = -0.f;
   in.scale = (float)(1.4426950408889634 / (double)x->temperature);
   out->fused = in.prior || (has_long && has_short) || (has_short && in.alpha);
-  out->vec = !off(in.longp, 16) && !off(in.shortp, 16) && !off(in.prior, 16) &&
-             (!has_long || ld_long * (long long)es % 16 == 0) && (!has_short || ld_short * (long long)es % 16 == 0);
+  // all rows' terms alike against 16-byte boundaries: the same place at the first
+  // row, and pitches that keep it so
+  out->vec = !off(in.prior, 16);
+  if (has_long && has_short)
+    out->vec = out->vec && ((reinterpret_cast<uintptr_t>(in.longp) ^ reinterpret_cast<uintptr_t>(in.shortp)) & 15u) == 0 &&
+               (rows == 1 || (ld_long - ld_short) * (long long)es % 16 == 0);
   if (!out->fused && !has_long) {      // the student's logits alone: read as the one term
     in.longp = in.shortp;
     in.ld_long = in.ld_short;
@@ -2140,7 +2145,8 @@ void plan_cluster(StreamRows& in, int sms, int least) {
   int c = 1;
   while (c < 8 && (c < least || ((long long)in.rows * c < 4LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
   in.cluster = c;
-  in.slice_cols = (int)round_up((size_t)(in.V + c - 1) / c, 8);
+  // (positions: a row may start up to 7 columns past a 16-byte boundary)
+  in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, 8);
 }
 
 int distill_call(const dels_rows* x, int rows, int V, const dels_teacher* t, RowsCall* call, DistillArgs* a) {
@@ -2160,16 +2166,19 @@ int distill_call(const dels_rows* x, int rows, int V, const dels_teacher* t, Row
   return DELS_OK;
 }
 
-bool plan_distill(DistillArgs* a) {
+// `step`: slices whose values leave room for a second CTA on the SM, where 8 CTAs
+// per row reach that.
+bool plan_distill(DistillArgs* a, bool step) {
   const int sms = device_sm_count();
   if (sms <= 0) return false;
-  plan_cluster(a->in, sms, (a->in.V + (1 << 19) - 1) >> 19);     // a slice's bitmap: at most 64 KB
+  const int slice = step ? 5 * 4096 : 1 << 19;                  // (a slice's bitmap: at most 64 KB)
+  plan_cluster(a->in, sms, (a->in.V + 7 + slice - 1) / slice);
   return true;
 }
 
 // The gradient's side of a call.
 int distill_grad_call(const dels_rows* x, int rows, int V, void* grad_short, long long grad_stride, float* grad_alpha,
-                      float* grad_beta, RowsCall* call, DistillArgs* a) {
+                      float* grad_beta, const RowsCall* call, DistillArgs* a) {
   if ((rows > 0 && !grad_short) || (grad_alpha && !x->alpha) || (grad_beta && (!x->beta || !x->log_prior)))
     return DELS_ERR_NULL_POINTER;
   const long long ld = grad_stride ? grad_stride : V;
@@ -2177,7 +2186,10 @@ int distill_grad_call(const dels_rows* x, int rows, int V, void* grad_short, lon
   const uintptr_t es = x->dtype == DELS_F32 ? 4 : 2, at = reinterpret_cast<uintptr_t>(grad_short);
   if ((at & (es - 1)) || (reinterpret_cast<uintptr_t>(grad_alpha) & 3u) || (reinterpret_cast<uintptr_t>(grad_beta) & 3u))
     return DELS_ERR_ALIGNMENT;
-  call->vec = call->vec && (at & 15u) == 0 && ld * (long long)es % 16 == 0;
+  const StreamRows& in = call->in;       // one of its terms: the others lie like it
+  const uintptr_t like = reinterpret_cast<uintptr_t>(in.longp ? in.longp : in.shortp);
+  const long long ld_like = in.longp ? in.ld_long : in.ld_short;
+  a->grad_vec = ((at ^ like) & 15u) == 0 && (in.rows == 1 || (ld - ld_like) * (long long)es % 16 == 0);
   a->grad = grad_short;
   a->ld_grad = ld;
   a->grad_alpha = grad_alpha;
@@ -2244,7 +2256,7 @@ int dels_distill_loss(const dels_rows* x, int rows, int V, const dels_teacher* t
   if (state_bytes < dels_distill_state_bytes(rows)) return DELS_ERR_WORKSPACE;
   if (!aligned16(workspace) || !aligned16(state) || (reinterpret_cast<uintptr_t>(out_loss) & 3u))
     return DELS_ERR_ALIGNMENT;
-  if (!plan_distill(&a)) return DELS_ERR_CUDA;
+  if (!plan_distill(&a, false)) return DELS_ERR_CUDA;
   a.out_loss = out_loss;
   a.state = static_cast<DistillState*>(state);
   a.status = at<int>(workspace, 0);
@@ -2268,7 +2280,7 @@ int dels_distill_grad(const dels_rows* x, int rows, int V, const dels_teacher* t
     if (state_bytes < dels_distill_state_bytes(rows)) return DELS_ERR_WORKSPACE;
     if (!aligned16(state) || (reinterpret_cast<uintptr_t>(grad_loss) & 3u)) return DELS_ERR_ALIGNMENT;
   }
-  if (!plan_distill(&a)) return DELS_ERR_CUDA;
+  if (!plan_distill(&a, false)) return DELS_ERR_CUDA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   a.state = static_cast<DistillState*>(const_cast<void*>(state));
   a.grad_loss = grad_loss;
@@ -2287,20 +2299,23 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
   int rc = distill_call(x, rows, V, teacher, &call, &a);
   if (rc != DELS_OK) return rc;
   if (!workspace || workspace_bytes < dels_distill_workspace_bytes(rows, V)) return DELS_ERR_WORKSPACE;
-  const bool loss_vec = call.vec;
   rc = distill_grad_call(x, rows, V, grad_short, grad_stride, grad_alpha, grad_beta, &call, &a);
   if (rc != DELS_OK) return rc;
   if (rows > 0 && !out_loss) return DELS_ERR_NULL_POINTER;
   if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(out_loss) & 3u)) return DELS_ERR_ALIGNMENT;
-  if (!plan_distill(&a)) return DELS_ERR_CUDA;
+  if (!plan_distill(&a, true)) return DELS_ERR_CUDA;
   a.out_loss = out_loss;
+  a.ticket = at<int>(workspace, 64);
   a.state = at<DistillState>(workspace, kHeaderBytes);
   a.status = at<int>(workspace, 0);
   const bool f32 = x->dtype == DELS_F32;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_DISTILL);
+  if (rows > 0 && distill_step_fits(a))
+    return launch_distill_step(a, f32, call.fused, call.vec, s) == cudaSuccess ? DELS_OK : DELS_ERR_CUDA;
   if (rows > 0) {
-    if (launch_distill_loss(a, f32, call.fused, loss_vec, s) != cudaSuccess) return DELS_ERR_CUDA;
+    if (!plan_distill(&a, false)) return DELS_ERR_CUDA;
+    if (launch_distill_loss(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
     if (launch_distill_grad(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
   }
   if ((grad_alpha || grad_beta) && launch_weight_grads(a, s) != cudaSuccess) return DELS_ERR_CUDA;

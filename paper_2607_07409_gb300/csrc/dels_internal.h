@@ -120,6 +120,7 @@ struct StreamRows {
   int rows, V;
   float inv_t;                   // 1 / T
   float scale;                   // log2(e) / T
+  float minus_zero;              // -0.f
   int cluster;                   // CTAs per row
   int slice_cols;                // columns per CTA (a multiple of 8)
 };
@@ -151,9 +152,10 @@ struct DistillState {
   float t_scale;
   float log_norm;
   float weight;     // the row's weight; 0: left out
+  float pad0;
   float d_alpha;    // dL/d alpha, dL/d beta (weight included)
   float d_beta;
-  float pad[5];
+  float pad[4];
 };
 static_assert(sizeof(DistillState) == 64, "one 64-byte record per row");
 
@@ -169,11 +171,17 @@ struct DistillArgs {
   const float* grad_loss;        // [rows] or null
   void* grad;                    // [rows, V] of the logits' type
   long long ld_grad;
+  int grad_vec;                  // its rows lie like the logits' against 16-byte boundaries
   float* grad_alpha;             // [n_weights] or null
   float* grad_beta;
+  int* ticket;                   // step: rows done, zero between calls
   int* status;
 };
 cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
+// Loss and gradient at once: a slice's values stay in shared memory.
+constexpr int kStepSmemBytes = 200 * 1024;
+bool distill_step_fits(const DistillArgs& a);
+cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_weight_grads(const DistillArgs& a, cudaStream_t s);
 

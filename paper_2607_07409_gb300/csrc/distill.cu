@@ -26,22 +26,138 @@ namespace {
 
 enum { kFlagAny = 1, kFlagBadId = 2, kFlagBadLogit = 4, kFlagTwice = 8 };
 
-// Sums of the columns that are not listed, relative to m: `rest` without one entry
-// that attains m, s = sum 2^t l_S and p = sum 2^t (l_P - ref) over all of them.
+// Sums of the columns that are not listed relative to m, an entry among them or one
+// before them: sum 2^t, sum 2^t l_S and sum 2^t (l_P - ref), t = (l - m) log2(e) / T.
 struct TailRec {
-  float m, rest, s, p;
+  float m, sum, s, p;
 };
-__device__ __forceinline__ void tail_add(TailRec& r, const TailRec& b, float c, bool stays_out) {
-  const float f = b.m == -INFINITY ? (b.rest != b.rest ? NAN : 0.f) : ex2_approx((b.m - r.m) * c);
-  r.rest += f * b.rest + (b.m == -INFINITY || stays_out ? 0.f : f);
-  r.s += f * b.s;
-  r.p += f * b.p;
-}
-__device__ __forceinline__ TailRec tail_merge(const TailRec& a, const TailRec& b, float c) {
-  TailRec r{fmaxf(a.m, b.m), 0.f, 0.f, 0.f};
-  tail_add(r, a, c, a.m >= b.m);
-  tail_add(r, b, c, a.m < b.m);
+// Those of the listed: m the largest, `rest` without one that attains it (the
+// student's whole mass may be there: ln(1 + rest) keeps its digits).
+struct ListRec {
+  float m, rest;
+};
+// Record i of `tails` in lanes 0 .. 7 (i + 8: the same; all lanes converged)
+// merged into every lane, in a fixed order.
+__device__ __forceinline__ TailRec tail_merge8(const TailRec& b, float c) {
+  TailRec r;
+  r.m = warp_max(b.m);
+  const float f = b.m == -INFINITY ? (b.sum != b.sum ? NAN : 0.f) : ex2_approx((b.m - r.m) * c);
+  r.sum = f * b.sum;
+  r.s = f * b.s;
+  r.p = f * b.p;
+#pragma unroll
+  for (int d = 4; d > 0; d >>= 1) {
+    r.sum += __shfl_xor_sync(0xFFFFFFFFu, r.sum, d);
+    r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, d);
+    r.p += __shfl_xor_sync(0xFFFFFFFFu, r.p, d);
+  }
   return r;
+}
+__device__ __forceinline__ ListRec list_merge8(const ListRec& b, float c) {
+  ListRec r;
+  r.m = warp_max(b.m);
+  const unsigned who = __ballot_sync(0xFFFFFFFFu, b.m == r.m);
+  const float f = b.m == -INFINITY ? (b.rest != b.rest ? NAN : 0.f) : ex2_approx((b.m - r.m) * c);
+  const bool out = b.m == -INFINITY || (threadIdx.x & 7) == (unsigned)(__ffs(who) - 1);
+  r.rest = f * b.rest + (out ? 0.f : f);
+#pragma unroll
+  for (int d = 4; d > 0; d >>= 1) r.rest += __shfl_xor_sync(0xFFFFFFFFu, r.rest, d);
+  return r;
+}
+
+// One lane's sums over the columns that are not listed. The reference of a warp's
+// exponentials is an entry that it has met: the largest of its first item, and
+// another only when one 2^20 times as likely comes (each is in float32's range and
+// the sums' digits do not depend on it; the largest entry so far would change about
+// ln n times, and a slice has few items).
+constexpr float kFarAbove = 20.f;
+template <bool FUSED>
+struct WarpTail {
+  float ref, limit, off;   // the same in every lane; off = ref, or 0 while ref is -inf
+  f32x2 sum, s, p;
+  __device__ __forceinline__ void init() {
+    ref = limit = -INFINITY;
+    off = 0.f;
+    sum = s = p = 0ull;
+  }
+  // One item's values, all lanes converged.
+  __device__ __forceinline__ void push(const float (&x)[8], const float (&sv)[8], const float (&pv)[8], float c,
+                                       float p_ref) {
+    const float vm = max8(x);
+    if (__any_sync(0xFFFFFFFFu, vm > limit)) {
+      const float top = warp_max(vm);
+      const f32x2 f = both2(ref == -INFINITY ? (sum2(sum) != sum2(sum) ? NAN : 0.f) : ex2_approx((ref - top) * c));
+      sum = mul2(f, sum);
+      s = mul2(f, s);
+      p = mul2(f, p);
+      ref = off = top;
+      limit = top + kFarAbove / c;
+    }
+    const f32x2 no = both2(-off), c2 = both2(c), np = both2(-p_ref);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float t0, t1;
+      split2(mul2(add2(pair2(x[i], x[i + 1]), no), c2), t0, t1);
+      const f32x2 e = pair2(ex2_approx(t0), ex2_approx(t1));
+      sum = add2(sum, e);
+      if constexpr (FUSED) {
+        s = fma2(e, pair2(fmaxf(sv[i], -FLT_MAX), fmaxf(sv[i + 1], -FLT_MAX)), s);     // a masked entry: 0
+        p = fma2(e, add2(pair2(pv[i], pv[i + 1]), np), p);
+      }
+    }
+  }
+  __device__ __forceinline__ TailRec record() const {
+    TailRec r{ref, sum2(sum), sum2(s), sum2(p)};
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+      r.sum += __shfl_xor_sync(0xFFFFFFFFu, r.sum, d);
+      if constexpr (FUSED) {
+        r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, d);
+        r.p += __shfl_xor_sync(0xFFFFFFFFu, r.p, d);
+      }
+    }
+    return r;
+  }
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  uint32_t w;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  return w;
+}
+__device__ __forceinline__ void grad_elem(float* g, long long i, float v) { g[i] = v; }
+__device__ __forceinline__ void grad_elem(uint16_t* g, long long i, float v) { g[i] = (uint16_t)bf16_pair(v, 0.f); }
+__device__ __forceinline__ void grad_vec(float* g, const float (&v)[8]) {
+  __stcs(reinterpret_cast<float4*>(g), make_float4(v[0], v[1], v[2], v[3]));
+  __stcs(reinterpret_cast<float4*>(g) + 1, make_float4(v[4], v[5], v[6], v[7]));
+}
+__device__ __forceinline__ void grad_vec(uint16_t* g, const float (&v)[8]) {
+  __stcs(reinterpret_cast<uint4*>(g),
+         make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])));
+}
+// An item's gradient at position k of a row whose position 0 is at g; vec: the
+// gradient's rows lie like the logits' against 16-byte boundaries.
+template <typename T, bool VEC>
+__device__ __forceinline__ void grad_item(T* g, int k, int begin, int stop, bool vec, const float (&v)[8]) {
+  if (VEC && vec && k >= begin && k + 8 <= stop) {
+    grad_vec(g + k, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int q = elem_pos<VEC>(k, i);
+    if (q >= begin && q < stop) grad_elem(g, q, v[i]);
+  }
+}
+// g = f 2^((x - m) c) of 8 values.
+__device__ __forceinline__ void unlisted_grad(const float (&x)[8], float m, float c, float f, float (&g)[8]) {
+  const f32x2 nm = both2(-m), c2 = both2(c), f2 = both2(f);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    float t0, t1;
+    split2(mul2(add2(pair2(x[i], x[i + 1]), nm), c2), t0, t1);
+    split2(mul2(f2, pair2(ex2_approx(t0), ex2_approx(t1))), g[i], g[i + 1]);
+  }
 }
 
 // The teacher's side of a row.
@@ -52,8 +168,8 @@ struct Teacher {
 
 struct LossShared {
   TailRec warps[kStreamWarps];
-  float members[kStreamWarps][2];   // largest listed entry, sum of the listed without one that attains it
-  float ctas[kMaxCluster][8];       // TailRec, then the listed pair
+  ListRec listed[kStreamWarps];
+  float ctas[kMaxCluster][8];       // TailRec, then ListRec
   float sums[kStreamWarps][4];
   float last[kMaxCluster][4];
   float logit[kMaxTopK];            // the teacher's as stored; -inf: left out
@@ -103,9 +219,85 @@ __device__ __forceinline__ float listed_grad(float lq, float lp, float mass) {
   return d < 1.f ? p * expm1f(d) + expf(lq) * (mass - 1.f) : expf(lq) * mass - p;
 }
 
-template <typename T, bool FUSED, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs a) {
-  extern __shared__ unsigned bitmap[];             // one bit per column of the slice: listed
+// Sums over the rows of each weight, in a fixed order, by a whole CTA of NT threads
+// (the rows' records past L1: other CTAs of the grid may have written them).
+template <int NT>
+__device__ void weight_grads(const DistillArgs& a, int j, float (*red)[2]) {
+  const int n = a.in.n_weights;
+  float da = 0.f, db = 0.f;
+  for (long long r = j + (long long)threadIdx.x * n; r < a.in.rows; r += (long long)NT * n) {
+    const float g = a.grad_loss ? a.grad_loss[r] : 1.f;
+    const float2 d = __ldcg(reinterpret_cast<const float2*>(&a.state[r].d_alpha));
+    if (__ldcg(&a.state[r].weight) != 0.f) {
+      da += g * d.x;
+      db += g * d.y;
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    da += __shfl_xor_sync(0xFFFFFFFFu, da, d);
+    db += __shfl_xor_sync(0xFFFFFFFFu, db, d);
+  }
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) {
+    red[threadIdx.x >> 5][0] = da;
+    red[threadIdx.x >> 5][1] = db;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    da = db = 0.f;
+    for (int k = 0; k < NT / 32; ++k) {
+      da += red[k][0];
+      db += red[k][1];
+    }
+    if (a.grad_alpha) a.grad_alpha[j] = da;
+    if (a.grad_beta) a.grad_beta[j] = db;
+  }
+}
+
+// The first CTA of a row's cluster, when the row is done: the last row of the grid
+// sums the weights' gradients (its count starts the next call at zero).
+__device__ __forceinline__ void finish_rows(const DistillArgs& a, LossShared& sh) {
+  if (!a.grad_alpha && !a.grad_beta) return;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    sh.flags = atomicAdd(a.ticket, 1) == a.in.rows - 1;
+  }
+  __syncthreads();
+  if (!sh.flags) return;
+  __threadfence();
+  for (int j = 0; j < a.in.n_weights; ++j)
+    weight_grads<kStreamThreads>(a, j, reinterpret_cast<float(*)[2]>(sh.sums));
+  if (threadIdx.x == 0) *a.ticket = 0;
+}
+
+// Gradients of listed ids where some are listed twice (all threads): an id's last
+// entry writes the sum of all its entries', in their order. `g`: of the calling
+// thread's entry.
+template <typename T>
+__device__ void twice_grads(const DistillArgs& a, LossShared& sh, long long r, bool mine, int id, float g, T* out) {
+  __syncthreads();
+  if (threadIdx.x < kMaxTopK) sh.logit[threadIdx.x] = g;     // (the teacher's are not needed any more)
+  __syncthreads();
+  if (!mine) return;
+  float sum = 0.f;
+  for (int k = 0; k < a.K; ++k) {
+    if (__ldg(a.ids + r * a.K + k) != id || __ldg(a.teacher + r * a.K + k) == -INFINITY) continue;
+    if (k > (int)threadIdx.x) return;
+    sum += sh.logit[k];
+  }
+  grad_elem(out, 0, sum);
+}
+
+// Loss and statistics of the rows, a cluster per row, a slice per CTA; GRAD: and
+// the gradient of l_S. The slice's fused values then stay in shared memory between
+// the pass that sums them and the one that writes their gradient, so that the rows
+// are read once: 3 s V bytes a row instead of 5 s V. Each thread reads back what it
+// wrote itself.
+template <typename T, bool FUSED, bool VEC, bool GRAD>
+__global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(DistillArgs a) {
+  extern __shared__ __align__(16) unsigned bitmap[];   // one bit per position of the slice: listed
   __shared__ LossShared sh;
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
@@ -115,8 +307,12 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
   const long long r = blockIdx.x / C;
   const float c = a.in.scale, inv_t = a.in.inv_t;
   const float weight = a.row_weight ? __ldg(a.row_weight + r) : 1.f;
+  const FusedRow<T, FUSED, VEC> row(a.in, r);
   const long long first = (long long)rank * a.in.slice_cols;
-  const int c0 = (int)min(first, (long long)V), c1 = (int)min(first + a.in.slice_cols, (long long)V);
+  const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
+  float4* kept = reinterpret_cast<float4*>(bitmap + (a.in.slice_cols + 127) / 128 * 4);
+  T* out = nullptr;                                // the row's gradient at position 0
+  if constexpr (GRAD) out = static_cast<T*>(a.grad) + r * a.ld_grad - row.sh;
 
   for (int i = tid; i < (a.in.slice_cols + 31) / 32; i += kStreamThreads) bitmap[i] = 0u;
   if (tid == 0) sh.flags = 0;
@@ -137,11 +333,12 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
     }
     sh.logit[tid] = logit;
   }
-  const bool mine = id >= c0 && id < c1 && id >= 0;
+  const int at = id + row.sh - k0;                 // its place in the slice
+  const bool mine = id >= 0 && at >= 0 && at < k1 - k0;
   __syncthreads();
   if (mine) {
-    const unsigned bit = 1u << ((id - c0) & 31);
-    if (atomicOr(&bitmap[(id - c0) >> 5], bit) & bit) flags |= kFlagTwice;
+    const unsigned bit = 1u << (at & 31);
+    if (atomicOr(&bitmap[at >> 5], bit) & bit) flags |= kFlagTwice;
   }
   if (tid < kMaxTopK) {
     flags = __reduce_or_sync(0xFFFFFFFFu, flags);
@@ -149,80 +346,69 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
   }
   __syncthreads();
   flags = (unsigned)sh.flags;
+  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
   if (weight == 0.f || !(flags & (kFlagAny | kFlagBadLogit))) {     // left out: the logits are not read
+    if constexpr (GRAD) {
+      const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
+    }
     if (rank == 0 && tid == 0) {
       if (weight != 0.f && (flags & kFlagBadId)) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
       if (a.out_loss) a.out_loss[r] = 0.f;
       a.state[r] = DistillState{};
     }
+    if constexpr (GRAD) {
+      if (rank == 0) finish_rows(a, sh);
+    }
     return;
   }
-  const FusedRow<T, FUSED> row(a.in, r);
   // a constant in the prior drops out of the gradient's sum with it: taken out first
-  const float p_ref = FUSED ? row.p_at(V / 2) : 0.f;
+  const float p_ref = FUSED ? row.p_at(row.sh + V / 2) : 0.f;
   float x_k = -INFINITY, s_k = 0.f, p_k = 0.f;
   if (mine) {
-    x_k = row.at(id);
-    s_k = fmaxf(row.s_at(id), -FLT_MAX);
-    p_k = row.p_at(id) - p_ref;
+    x_k = row.at(k0 + at);
+    s_k = fmaxf(row.s_at(k0 + at), -FLT_MAX);
+    p_k = row.p_at(k0 + at) - p_ref;
   }
 
   // the columns that are not listed
-  TailRec st{-INFINITY, 0.f, 0.f, 0.f};
-  float off = 0.f;
-  bool holds = false;
-  const int items = (c1 - c0 + kStreamStep - 1) / kStreamStep;
-  for (int it = 0; it < items; ++it) {
-    const int col = item_col<VEC>(c0, it, tid);
-    float l[8], s[8], p[8], x[8];
-    row.template load<VEC, true>(col, c1, l, s, p);
+  WarpTail<FUSED> st;
+  st.init();
+  constexpr int U = GRAD ? (sizeof(T) == 2 ? 4 : 2) : 2;
+  float4* keep = kept + tid;
+  stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] = row.combine(l[i], s[i], p[i]);
-      const int k = elem_col<VEC>(col, i) - c0;
-      if (k < c1 - c0 && (bitmap[k >> 5] >> (k & 31) & 1u)) x[i] = -INFINITY;
-    }
-    const float vm = max8(x);
-    if (__any_sync(0xFFFFFFFFu, vm > st.m)) {
-      const float nt = warp_max(vm);
-      const float f = st.m == -INFINITY ? (st.rest != st.rest ? NAN : 0.f) : ex2_approx((st.m - nt) * c);
-      st.rest = st.rest * f + (holds ? f : 0.f);
-      st.s *= f;
-      st.p *= f;
-      st.m = off = nt;
-      const unsigned who = __ballot_sync(0xFFFFFFFFu, vm == nt);
-      holds = lane == __ffs(who) - 1;
-      if (holds) {
-        bool kept = false;
+    for (int u = 0; u < U; ++u) {
+      float x[8], s[8], p[8];
+      v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
+      if constexpr (VEC) {
+        const int b = v[u].k - k0;
+        const unsigned bits = !decltype(checked)::value || b < k1 - k0
+                                  ? reinterpret_cast<const unsigned char*>(bitmap)[b >> 3] : 0u;
+        if (bits) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (!kept && x[i] == nt) {
-            kept = true;
-            x[i] = -INFINITY;
-            if constexpr (FUSED) {
-              st.s += s[i];
-              st.p += p[i] - p_ref;
-            }
-          }
+          for (int i = 0; i < 8; ++i)
+            if (bits >> i & 1u) x[i] = -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int b = elem_pos<VEC>(v[u].k, i) - k0;
+          if ((!decltype(checked)::value || b < k1 - k0) && (bitmap[b >> 5] >> (b & 31) & 1u)) x[i] = -INFINITY;
+        }
       }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float e = ex2_approx((x[i] - off) * c);
-      st.rest += e;
-      if constexpr (FUSED) {
-        st.s += e * fmaxf(s[i], -FLT_MAX);         // a masked entry: 0
-        st.p += e * (p[i] - p_ref);
+      if constexpr (GRAD) {
+        if (!decltype(checked)::value || v[u].k < k1) {
+          keep[0] = make_float4(x[0], x[1], x[2], x[3]);
+          keep[kStreamThreads] = make_float4(x[4], x[5], x[6], x[7]);
+        }
+        keep += 2 * kStreamThreads;
       }
+      st.push(x, s, p, c, p_ref);
     }
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    st.rest += __shfl_xor_sync(0xFFFFFFFFu, st.rest, d);
-    st.s += __shfl_xor_sync(0xFFFFFFFFu, st.s, d);
-    st.p += __shfl_xor_sync(0xFFFFFFFFu, st.p, d);
-  }
-  if (lane == 0) sh.warps[warp] = st;
+  });
+  const TailRec wr = st.record();
+  if (lane == 0) sh.warps[warp] = wr;
 
   // the listed columns of this slice; an id listed twice counts once in the student's sums
   bool once = mine;
@@ -237,47 +423,57 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
     if (once && x_k != x_k) e = NAN;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) e += __shfl_xor_sync(0xFFFFFFFFu, e, d);
-    if (lane == 0) {
-      sh.members[warp][0] = m_k;
-      sh.members[warp][1] = e;
-    }
+    if (lane == 0) sh.listed[warp] = ListRec{m_k, e};
   }
   if (warp == kStreamWarps - 1) teacher_side(sh, K, a.tail != 0, inv_t);
   __syncthreads();
-  TailRec tail = sh.warps[0];
-  TailRec listed{sh.members[0][0], sh.members[0][1], 0.f, 0.f};
-  for (int k = 1; k < kStreamWarps; ++k) {
-    tail = tail_merge(tail, sh.warps[k], c);
-    listed = tail_merge(listed, TailRec{sh.members[k][0], sh.members[k][1], 0.f, 0.f}, c);
-  }
+  TailRec tail = tail_merge8(sh.warps[lane & 7], c);
+  ListRec listed = list_merge8(sh.listed[lane & 7], c);
   if (C > 1) {
     cluster_sync_all();            // every CTA of the cluster runs before its shared memory is written
     if (tid < C) {
       const uint32_t to = cluster_map(smem_u32(&sh.ctas[rank][0]), (uint32_t)tid);
-      st_cluster_v4(to, tail.m, tail.rest, tail.s, tail.p);
+      st_cluster_v4(to, tail.m, tail.sum, tail.s, tail.p);
       st_cluster_v4(to + 16, listed.m, listed.rest, 0.f, 0.f);
     }
     cluster_sync_all();
-    tail = TailRec{sh.ctas[0][0], sh.ctas[0][1], sh.ctas[0][2], sh.ctas[0][3]};
-    listed = TailRec{sh.ctas[0][4], sh.ctas[0][5], 0.f, 0.f};
-    for (int k = 1; k < C; ++k) {
-      tail = tail_merge(tail, TailRec{sh.ctas[k][0], sh.ctas[k][1], sh.ctas[k][2], sh.ctas[k][3]}, c);
-      listed = tail_merge(listed, TailRec{sh.ctas[k][4], sh.ctas[k][5], 0.f, 0.f}, c);
-    }
+    const float* rec = sh.ctas[lane & 7];
+    const bool in = (lane & 7) < C;
+    tail = tail_merge8(in ? TailRec{rec[0], rec[1], rec[2], rec[3]} : TailRec{-INFINITY, 0.f, 0.f, 0.f}, c);
+    listed = list_merge8(in ? ListRec{rec[4], rec[5]} : ListRec{-INFINITY, 0.f}, c);
   }
-  const TailRec all = tail_merge(tail, listed, c);        // its s and p: the unlisted columns' alone
-  const float m = all.m, S = 1.f + all.rest, inv_s = 1.f / S, ln_s = log1pf(all.rest);
-  const bool ok = m > -INFINITY && m < INFINITY && all.rest >= 0.f && all.rest < INFINITY && !(flags & kFlagBadLogit);
+  // S = sum over all columns, relative to the larger reference; rest = S - 1 where
+  // that is a listed entry of the largest value
+  const float m = fmaxf(tail.m, listed.m);
+  const float f_tail = tail.m == -INFINITY ? (tail.sum != tail.sum ? NAN : 0.f) : ex2_approx((tail.m - m) * c);
+  const float f_list = listed.m == -INFINITY ? (listed.rest != listed.rest ? NAN : 0.f) : ex2_approx((listed.m - m) * c);
+  const float tail_sum = f_tail * tail.sum;
+  const float list_sum = listed.m == -INFINITY ? f_list : f_list * (1.f + listed.rest);
+  const float rest = listed.m == m ? listed.rest + tail_sum : tail_sum - 1.f + list_sum;
+  const float S = 1.f + rest, inv_s = 1.f / S, ln_s = log1pf(rest);
+  const bool ok = m > -INFINITY && m < INFINITY && S > 0.f && S < INFINITY && !(flags & kFlagBadLogit);
   const Teacher te = sh.teacher;
-  // q_t = tail_sum / S, from the unlisted columns' own sum; ln q_t = -ln(1 + listed_sum / tail_sum)
-  const float f_tail = tail.m == -INFINITY ? 0.f : ex2_approx((tail.m - m) * c);
-  const float f_list = listed.m == -INFINITY ? 0.f : ex2_approx((listed.m - m) * c);
-  const float tail_sum = f_tail * (1.f + tail.rest), list_sum = f_list * (1.f + listed.rest);
+  // q_t = tail_sum / S; ln q_t = -ln(1 + list_sum / tail_sum)
   const bool has_tail = a.tail && te.rest > 0.f && tail_sum > 0.f;
   const float mass = has_tail ? 1.f : te.sum;
   const float coef_n = has_tail ? mass - te.rest * (S / tail_sum) : mass;
 
+  const float up = weight * inv_t * (FUSED ? row.a : 1.f);   // dL/dl -> what the gradient holds
+  if constexpr (GRAD) {
+    const float f = ok ? up * coef_n * inv_s : NAN;
+    const float4* got = kept + tid;
+    for (int it = 0; it < items; ++it, got += 2 * kStreamThreads) {
+      const int k = item_pos<VEC>(k0, it, tid);
+      if (k >= k1) break;
+      const float4 u = got[0], w = got[kStreamThreads];
+      const float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+      float g[8];
+      unlisted_grad(x, m, c, f, g);
+      grad_item<T, VEC>(out, k, row.sh, k1, a.grad_vec, g);
+    }
+  }
   float v[3] = {0.f, 0.f, 0.f};
+  float g_k = 0.f;
   if (mine) {
     const float lp = (logit - te.t_max) * te.t_scale - te.log_norm, p = expf(lp);
     const float lq = (x_k - m) * inv_t - ln_s;
@@ -285,6 +481,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
     v[0] = p > 0.f ? p * (lp - lq) : 0.f;
     v[1] = g * s_k;
     v[2] = g * p_k;
+    g_k = up * g;
   }
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
@@ -292,7 +489,11 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
     for (int d = 16; d > 0; d >>= 1) v[j] += __shfl_xor_sync(0xFFFFFFFFu, v[j], d);
     if (lane == 0) sh.sums[warp][j] = v[j];
   }
-  __syncthreads();
+  __syncthreads();                                 // (and the unlisted columns' gradients are written)
+  if constexpr (GRAD) {
+    if (flags & kFlagTwice) twice_grads(a, sh, r, mine, id, ok ? g_k : NAN, out + k0 + at);
+    else if (mine) grad_elem(out, k0 + at, ok ? g_k : NAN);
+  }
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
     v[j] = 0.f;
@@ -308,7 +509,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
       for (int k = 0; k < C; ++k) v[j] += sh.last[k][j];
     }
   }
-  if (tid != 0) return;
+  if (tid == 0) {
   if (!ok) raise_status(a.status, DELS_STATUS_NONFINITE);
   if (flags & kFlagBadId) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
   float loss = v[0];
@@ -327,57 +528,48 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_loss(DistillArgs 
   o.t_scale = te.t_scale;
   o.log_norm = te.log_norm;
   o.weight = weight;
-  o.d_alpha = ok ? weight * inv_t * (coef_n * inv_s * all.s + v[1]) : NAN;
-  o.d_beta = ok ? -weight * inv_t * (coef_n * inv_s * all.p + v[2]) : NAN;
+  o.d_alpha = ok ? weight * inv_t * (coef_n * inv_s * (f_tail * tail.s) + v[1]) : NAN;
+  o.d_beta = ok ? -weight * inv_t * (coef_n * inv_s * (f_tail * tail.p) + v[2]) : NAN;
   a.state[r] = o;
-}
-
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
-  uint32_t w;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
-  return w;
-}
-__device__ __forceinline__ void grad_elem(float* g, long long i, float v) { g[i] = v; }
-__device__ __forceinline__ void grad_elem(uint16_t* g, long long i, float v) { g[i] = (uint16_t)bf16_pair(v, 0.f); }
-__device__ __forceinline__ void grad_vec(float* g, const float (&v)[8]) {
-  __stcs(reinterpret_cast<float4*>(g), make_float4(v[0], v[1], v[2], v[3]));
-  __stcs(reinterpret_cast<float4*>(g) + 1, make_float4(v[4], v[5], v[6], v[7]));
-}
-__device__ __forceinline__ void grad_vec(uint16_t* g, const float (&v)[8]) {
-  __stcs(reinterpret_cast<uint4*>(g),
-         make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])));
+  }
+  if constexpr (GRAD) finish_rows(a, sh);
 }
 
 // The gradient of l_S from the statistics: every column as one that is not listed,
 // then the listed ones over it. The rows' own logits may be the output (each column
 // is read before it is written).
 template <typename T, bool FUSED, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, 2) k_distill_grad(DistillArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, 4) k_distill_grad(DistillArgs a) {
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
   const int tid = threadIdx.x;
-  const int C = a.in.cluster, K = a.K, V = a.in.V;
+  const int C = a.in.cluster, K = a.K;
   const int rank = (int)(blockIdx.x % C);
   const long long r = blockIdx.x / C;
   const long long first = (long long)rank * a.in.slice_cols;
-  const int c0 = (int)min(first, (long long)V), c1 = (int)min(first + a.in.slice_cols, (long long)V);
+  const FusedRow<T, FUSED, VEC> row(a.in, r);
+  const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
   const DistillState st = a.state[r];
   const float up = a.grad_loss ? __ldg(a.grad_loss + r) : 1.f;
-  const FusedRow<T, FUSED> row(a.in, r);
-  T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
-  const bool left_out = st.weight == 0.f;
+  T* out = static_cast<T*>(a.grad) + r * a.ld_grad - row.sh;
+  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
+  if (st.weight == 0.f) {                          // left out
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
+    return;
+  }
   const float g0 = up * st.weight * a.in.inv_t * (FUSED ? row.a : 1.f);
   const float c = a.in.scale;
 
   int id = -1;
   float g_k = 0.f;
-  if (tid < K && !left_out) {
+  if (tid < K) {
     id = __ldg(a.ids + r * K + tid);
     const float t = __ldg(a.teacher + r * K + tid);
-    if (id < c0 || id >= c1 || t == -INFINITY) id = -1;
+    if (id < 0 || id + row.sh < k0 || id + row.sh >= k1 || t == -INFINITY) id = -1;
     if (id >= 0) {
       // every entry with this id, in their order; the last of them writes
-      const float lp = (t - st.t_max) * st.t_scale - st.log_norm, x = row.at(id);
+      const float lp = (t - st.t_max) * st.t_scale - st.log_norm, x = row.at(id + row.sh);
       float before = 0.f;
       for (int k = 0; k < K; ++k) {
         if (k == tid || __ldg(a.ids + r * K + k) != id) continue;
@@ -393,93 +585,65 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_distill_grad(DistillArgs 
       g_k = g0 * (listed_grad(lq, lp, st.mass) - before);
     }
   }
-  __syncthreads();
+  __syncthreads();                                 // the output may be l_S itself
   const float f = g0 * st.coef_n * st.inv_s;
-  const int items = (c1 - c0 + kStreamStep - 1) / kStreamStep;
-  for (int it = 0; it < items; ++it) {
-    const int col = item_col<VEC>(c0, it, tid);
-    float g[8];
-    if (left_out) {
+  constexpr int U = 2;
+  stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = 0.f;
-    } else {
-      float l[8], s[8], p[8];
-      row.template load<VEC, true>(col, c1, l, s, p);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = f * ex2_approx((row.combine(l[i], s[i], p[i]) - st.m) * c);
+    for (int u = 0; u < U; ++u) {
+      float x[8], s[8], p[8], g[8];
+      v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
+      unlisted_grad(x, st.m, c, f, g);
+      grad_item<T, VEC>(out, v[u].k, row.sh, k1, a.grad_vec, g);
     }
-    if (VEC && col + 8 <= c1) {
-      grad_vec(out + col, g);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int k = elem_col<VEC>(col, i);
-        if (k < c1) grad_elem(out, k, g[i]);
-      }
-    }
-  }
+  });
   __syncthreads();
-  if (id >= 0) grad_elem(out, id, g_k);
+  if (id >= 0) grad_elem(out, id + row.sh, g_k);
 }
 
-// Sums over the rows of each weight, in a fixed order: one CTA per weight.
 __global__ void __launch_bounds__(256) k_weight_grads(DistillArgs a) {
+  __shared__ float red[8][2];
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
-  __shared__ float red[8][2];
-  const int j = blockIdx.x, n = a.in.n_weights;
-  float da = 0.f, db = 0.f;
-  for (long long r = j + (long long)threadIdx.x * n; r < a.in.rows; r += 256LL * n) {
-    const float g = a.grad_loss ? a.grad_loss[r] : 1.f;
-    if (a.state[r].weight != 0.f) {
-      da += g * a.state[r].d_alpha;
-      db += g * a.state[r].d_beta;
-    }
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    da += __shfl_xor_sync(0xFFFFFFFFu, da, d);
-    db += __shfl_xor_sync(0xFFFFFFFFu, db, d);
-  }
-  if ((threadIdx.x & 31) == 0) {
-    red[threadIdx.x >> 5][0] = da;
-    red[threadIdx.x >> 5][1] = db;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    da = db = 0.f;
-    for (int k = 0; k < 8; ++k) {
-      da += red[k][0];
-      db += red[k][1];
-    }
-    if (a.grad_alpha) a.grad_alpha[j] = da;
-    if (a.grad_beta) a.grad_beta[j] = db;
-  }
+  weight_grads<256>(a, blockIdx.x, red);
 }
 
-template <typename T>
-cudaError_t launch_t(const DistillArgs& a, bool grad, bool fused, bool vec, cudaStream_t s) {
+// Shared memory of the loss kernel: the bitmap, and with GRAD the slice's values.
+size_t loss_smem(const StreamRows& in, bool grad) {
+  const size_t items = ((size_t)in.slice_cols + kStreamStep - 1) / kStreamStep;
+  return ((size_t)in.slice_cols + 127) / 128 * 16 + (grad ? items * kStreamStep * 4 : 0);
+}
+
+template <typename T, bool GRAD>
+cudaError_t launch_loss_t(const DistillArgs& a, bool fused, bool vec, cudaStream_t s) {
   const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
-  if (grad) {
-    auto k = fused ? (vec ? k_distill_grad<T, true, true> : k_distill_grad<T, true, false>)
-                   : (vec ? k_distill_grad<T, false, true> : k_distill_grad<T, false, false>);
-    return launch_pdl(k, grid, block, 0, s, a);
-  }
-  auto k = fused ? (vec ? k_distill_loss<T, true, true> : k_distill_loss<T, true, false>)
-                 : (vec ? k_distill_loss<T, false, true> : k_distill_loss<T, false, false>);
-  const size_t bytes = (size_t)(a.in.slice_cols + 31) / 32 * 4;
+  auto k = fused ? (vec ? k_distill_loss<T, true, true, GRAD> : k_distill_loss<T, true, false, GRAD>)
+                 : (vec ? k_distill_loss<T, false, true, GRAD> : k_distill_loss<T, false, false, GRAD>);
+  const size_t bytes = loss_smem(a.in, GRAD);
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
   if (e != cudaSuccess) return e;
   return launch_pdl_cluster(k, grid, block, bytes, s, a.in.cluster, a);
 }
 
+template <typename T>
+cudaError_t launch_grad_t(const DistillArgs& a, bool fused, bool vec, cudaStream_t s) {
+  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
+  auto k = fused ? (vec ? k_distill_grad<T, true, true> : k_distill_grad<T, true, false>)
+                 : (vec ? k_distill_grad<T, false, true> : k_distill_grad<T, false, false>);
+  return launch_pdl(k, grid, block, 0, s, a);
+}
+
 }  // namespace
 
 cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
-  return f32 ? launch_t<float>(a, false, fused, vec, s) : launch_t<uint16_t>(a, false, fused, vec, s);
+  return f32 ? launch_loss_t<float, false>(a, fused, vec, s) : launch_loss_t<uint16_t, false>(a, fused, vec, s);
+}
+bool distill_step_fits(const DistillArgs& a) { return loss_smem(a.in, true) <= (size_t)kStepSmemBytes; }
+cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
+  return f32 ? launch_loss_t<float, true>(a, fused, vec, s) : launch_loss_t<uint16_t, true>(a, fused, vec, s);
 }
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
-  return f32 ? launch_t<float>(a, true, fused, vec, s) : launch_t<uint16_t>(a, true, fused, vec, s);
+  return f32 ? launch_grad_t<float>(a, fused, vec, s) : launch_grad_t<uint16_t>(a, fused, vec, s);
 }
 cudaError_t launch_weight_grads(const DistillArgs& a, cudaStream_t s) {
   return launch_pdl(k_weight_grads, dim3((unsigned)a.in.n_weights), dim3(256), 0, s, a);

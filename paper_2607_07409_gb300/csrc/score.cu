@@ -40,82 +40,95 @@ struct ScoreShared {
   int ncand, ngroups;
 };
 
-// The K largest of cand[0 .. n) to best[] in order (all threads; n <= kCandidates).
+// The K largest of cand[0 .. n) to best[] in order (all threads; n <= kCandidates):
+// a warp counts what is above one candidate, 32 at a time.
 __device__ void sort_best(ScoreShared& sh, int n, int K) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int k = threadIdx.x; k < K; k += kStreamThreads) sh.best[k] = 0ull;
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kStreamThreads) {
+  for (int i = warp; i < n; i += kStreamWarps) {
     const unsigned long long x = sh.cand[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += sh.cand[j] > x;
-    if (rank < K && x) sh.best[rank] = x;
+    for (int j = lane; j < n; j += 32) rank += sh.cand[j] > x;
+    rank = __reduce_add_sync(0xFFFFFFFFu, rank);
+    if (lane == 0 && rank < K && x) sh.best[rank] = x;
   }
   __syncthreads();
+}
+
+// The entries of an item that reach `floor_key`, into cand[] as far as it has room.
+template <typename T, bool FUSED, bool VEC>
+__device__ __forceinline__ void keep_entries(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, int pos, int k1,
+                                             unsigned long long floor_key) {
+  Item<T, FUSED, VEC> v;
+  v.load(row, pos, k1);
+  float x[8], s[8], p[8];
+  v.template values<true>(row, k1, x, s, p);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (!(x[i] > -INFINITY)) continue;
+    const unsigned long long e = entry_key(x[i], elem_pos<VEC>(pos, i) - row.sh);
+    if (e < floor_key) continue;
+    const int at = atomicAdd(&sh.ncand, 1);
+    if (at < kCandidates) sh.cand[at] = e;
+  }
 }
 
 // This CTA's K largest entries of its slice into sh.best. `top`: the largest
 // entry of the calling thread.
 template <typename T, bool FUSED, bool VEC>
-__device__ void slice_top(ScoreShared& sh, const FusedRow<T, FUSED>& row, int c0, int c1, int K, float top) {
+__device__ void slice_top(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, int k0, int k1, int K, float top) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // The K-th largest thread maximum, from its highest bit down; -inf where fewer
-  // than K threads have an entry.
+  // About the K-th largest thread maximum, from its highest bit down; 0 where
+  // fewer than K threads have an entry.
   const unsigned key = top > -INFINITY ? order_u32(top) : 0u;
   unsigned tau = 0u;
+  if (tid == 0) sh.ncand = sh.ngroups = 0;
   if (__syncthreads_count(key > 0u) >= K) {
     for (int bit = 31; bit >= 0; --bit) {
       const unsigned t = tau | (1u << bit);
       const int n = __syncthreads_count(key >= t);
       if (n >= K) tau = t;
-      if (n == K) break;
+      if (n >= K && n <= K + 8) break;
     }
   }
-  if (tid == 0) sh.ncand = sh.ngroups = 0;
-  __syncthreads();
   if (key > 0u && key >= tau) sh.groups[atomicAdd(&sh.ngroups, 1)] = tid;
   __syncthreads();
-  const int items = (c1 - c0 + kStreamStep - 1) / kStreamStep;      // per thread
+  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;      // per thread
   const int parts = (items + 31) / 32;                              // a warp's rounds for one thread's items
   const int jobs = sh.ngroups * parts;
-  unsigned long long floor_key = (unsigned long long)tau << 32;     // what an entry has to exceed or equal
-  for (int j0 = 0; j0 < jobs; j0 += kStreamWarps) {
-    if (j0 > 0) {
-      __syncthreads();
+  unsigned long long floor_key = (unsigned long long)tau << 32;     // what an entry has to reach
+  for (int j = warp; j < jobs; j += kStreamWarps) {
+    const int it = (j % parts) * 32 + lane;
+    if (it < items) keep_entries(sh, row, item_pos<VEC>(k0, it, sh.groups[j / parts]), k1, floor_key);
+  }
+  __syncthreads();
+  if (sh.ncand > kCandidates) {
+    // more entries than there is room for: a round of items at a time, the best
+    // of them kept as soon as the next round might not fit
+    __syncthreads();
+    if (tid == 0) sh.ncand = 0;
+    __syncthreads();
+    for (int j0 = 0; j0 < jobs; j0 += kStreamWarps) {
       const int n = sh.ncand;
       __syncthreads();
-      if (n > kCandidates - kStreamWarps * 256) {                   // room for one more round
+      if (n > kCandidates - kStreamWarps * 256) {
         sort_best(sh, n, K);
         for (int k = tid; k < K; k += kStreamThreads) sh.cand[k] = sh.best[k];
-        if (sh.best[K - 1]) floor_key = sh.best[K - 1];
+        floor_key = sh.best[K - 1];                                 // n > K: there are K
         if (tid == 0) sh.ncand = K;
         __syncthreads();
       }
-    }
-    const int j = j0 + warp;
-    if (j < jobs) {
-      const int g = sh.groups[j / parts], it = (j % parts) * 32 + lane;
-      const int c = item_col<VEC>(c0, it, g);
-      if (it < items && c < c1) {
-        float l[8], s[8], p[8];
-        row.template load<VEC, true>(c, c1, l, s, p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int col = elem_col<VEC>(c, i);
-          const float x = row.combine(l[i], s[i], p[i]);
-          if (col < c1 && x > -INFINITY) {
-            const unsigned long long e = entry_key(x, col);
-            if (e >= floor_key) sh.cand[atomicAdd(&sh.ncand, 1)] = e;
-          }
-        }
-      }
+      const int j = j0 + warp, it = (j % parts) * 32 + lane;
+      if (j < jobs && it < items) keep_entries(sh, row, item_pos<VEC>(k0, it, sh.groups[j / parts]), k1, floor_key);
+      __syncthreads();
     }
   }
-  __syncthreads();
   sort_best(sh, sh.ncand, K);
 }
 
 template <typename T, bool FUSED, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, 2) k_score_rows(ScoreArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, 4) k_score_rows(ScoreArgs a) {
   __shared__ ScoreShared sh;
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
@@ -139,55 +152,34 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_score_rows(ScoreArgs a) {
     }
     return;
   }
-  const FusedRow<T, FUSED> row(a.in, r);
+  const FusedRow<T, FUSED, VEC> row(a.in, r);
   const bool tok_ok = tok >= 0 && tok < V;
   float x_tok = 0.f;
-  if (rank == 0 && tid == 0 && a.tokens && tok_ok) x_tok = row.at(tok);
+  if (rank == 0 && tid == 0 && a.tokens && tok_ok) x_tok = row.at(tok + row.sh);
   const long long first = (long long)rank * a.in.slice_cols;
-  const int c0 = (int)min(first, (long long)V), c1 = (int)min(first + a.in.slice_cols, (long long)V);
+  const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
 
+  // items in flight per thread: 64 bytes of bf16 rows, 64 to 128 of the others
+  constexpr int U = FUSED ? 2 : sizeof(T) == 2 ? 4 : 2;
   WarpSoft st;
   st.init();
   float top = -INFINITY;
-  const int items = (c1 - c0 + kStreamStep - 1) / kStreamStep;
-  for (int it = 0; it < items; ++it) {
-    const int col = item_col<VEC>(c0, it, tid);
-    float l[8], s[8], p[8], x[8];
-    row.template load<VEC, true>(col, c1, l, s, p);
+  stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
+    float x[U][8], s[8], p[8], vm = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = row.combine(l[i], s[i], p[i]);
-    const float vm = max8(x);
+    for (int u = 0; u < U; ++u) {
+      v[u].template values<decltype(checked)::value>(row, k1, x[u], s, p);
+      vm = fmaxf(vm, max8(x[u]));
+    }
     top = fmaxf(top, vm);
-    if (__any_sync(0xFFFFFFFFu, vm > st.ref)) {
-      const float nt = warp_max(vm);
-      st.move(nt, c);
-      const unsigned who = __ballot_sync(0xFFFFFFFFu, vm == nt);
-      if (lane == __ffs(who) - 1) {
-        bool kept = false;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (!kept && x[i] == nt) {
-            kept = true;
-            x[i] = -INFINITY;
-          }
-        st.holds = true;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = (x[i] - st.off) * c;
-      const float e = ex2_approx(t);
-      st.rest += e;
-      st.w += e * fmaxf(t, kLowT);
-    }
-  }
+    st.push(x, vm, c);
+  });
   const SoftRec wr = st.record();
   if (lane == 0) sh.warps[warp] = wr;
   __syncthreads();
-  SoftRec cta = sh.warps[0];
-  for (int k = 1; k < kStreamWarps; ++k) cta = softrec_merge(cta, sh.warps[k], c);
+  const SoftRec cta = softrec_merge8(sh.warps[lane & 7], c);
 
-  if (K > 0) slice_top<T, FUSED, VEC>(sh, row, c0, c1, K, top);
+  if (K > 0) slice_top(sh, row, k0, k1, K, top);
   SoftRec all = cta;
   if (C > 1) {
     cluster_sync_all();            // every CTA of the cluster runs before its shared memory is written
@@ -206,8 +198,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) k_score_rows(ScoreArgs a) {
     }
     cluster_sync_all();
     if (rank != 0) return;
-    all = sh.ctas[0];
-    for (int k = 1; k < C; ++k) all = softrec_merge(all, sh.ctas[k], c);
+    all = softrec_merge8((lane & 7) < C ? sh.ctas[lane & 7] : softrec_init(), c);
     if (K > 0) sort_best(sh, C * K, K);
   }
   const bool ok = softrec_valid(all);

@@ -145,6 +145,14 @@ def test_score_matches_float64(rows, V, K, offset, pitch, fused, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [30000, 30001])
+def test_score_rounds_fused_values_step_by_step(V, dtype):
+    """Enough fused entries that neighbours in the order differ in their last bits:
+    a contracted product would exchange some."""
+    assert check_score(Case(48, V, dtype, 77, True, n=5), 256)[-1] == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("V,offset", [(9000, 0), (9001, 0), (131072, 0), (131073, 0)])
 def test_score_orders_ties_and_crowded_threads(V, offset, dtype):
     """Rows whose alternatives meet in few threads, more entries above the
