@@ -187,6 +187,8 @@ def _ptr(x) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        if torch.cuda.is_initialized():       # the current device's current stream, without the object around it
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
@@ -563,27 +565,35 @@ def _row_ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
-def _row_stride(x: torch.Tensor, what: str) -> int:
+def _row_stride(x: torch.Tensor, shape, what: str) -> int:
     """Elements from one row to the next (a single row's own length: its stride may be anything)."""
-    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+    rows, V = shape
+    step, one = x.stride()
+    if V > 1 and one != 1:
+        raise ValueError(f"{what}: expected [rows, V] logits whose rows are dense")
+    if rows <= 1:
+        return V
+    if step < V:
         raise ValueError(f"{what}: rows overlap")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return step
 
 
-def _of(t, dtype, shape, device, what) -> Optional[int]:
+def _of(t, dtype, shape, device: int, what) -> Optional[int]:
     """Device address of a dense tensor of this dtype and shape on this device."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device:
-        raise ValueError(f"{what} must be {dtype} {list(shape)} on {device}, "
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous {dtype} {list(shape)} on cuda:{device}, "
                          f"got {t.dtype} {list(t.shape)} on {t.device}")
-    return _ptr(t)
+    return t.data_ptr()
 
 
-def _logits(x, rows: int, V: int, dtype, device, what) -> torch.Tensor:
-    if tuple(x.shape) != (rows, V) or x.dtype != dtype or x.device != device:
-        raise ValueError(f"{what} must be {dtype} [{rows}, {V}] on {device}, got {x.dtype} {list(x.shape)} on {x.device}")
-    return x
+def _logits(t, shape, dtype, device: int, what) -> int:
+    """Device address of [rows, V] logits (their rows may be strided)."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on cuda:{device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def rows_of(rows: int, V: int, long=None, short=None, log_prior=None, alpha=None, beta=None,
@@ -593,21 +603,29 @@ def rows_of(rows: int, V: int, long=None, short=None, log_prior=None, alpha=None
     one = long if long is not None else short
     if one is None:
         raise ValueError("rows need long or short logits")
+    if not one.is_cuda:
+        raise ValueError("expected a CUDA tensor: the library's entry points take device pointers")
+    shape, dev, dtype = (rows, V), one.get_device(), one.dtype
     x = Rows()
-    x.dtype = dtype_code(one)
-    for t, name in ((long, "long"), (short, "short")):
-        if t is not None:
-            _logits(t, rows, V, one.dtype, one.device, name)
-            setattr(x, name + "_logits", _row_ptr(t))
-            setattr(x, name + "_stride", _row_stride(t, name))
-    x.log_prior = _of(log_prior, torch.float32, (V,), one.device, "log_prior")
-    n = [w.numel() for w in (alpha, beta) if w is not None]
-    if len(set(n)) > 1:
-        raise ValueError("alpha and beta must have the same length")
-    x.n_weights = n[0] if n else 0
-    x.alpha = _of(alpha, torch.float32, (x.n_weights,), one.device, "alpha")
-    x.beta = _of(beta, torch.float32, (x.n_weights,), one.device, "beta")
-    x.temperature = float(temperature)
+    x.dtype = dtype_code(dtype)
+    if long is not None:
+        x.long_logits = _logits(long, shape, dtype, dev, "long")
+        x.long_stride = _row_stride(long, shape, "long")
+    if short is not None:
+        x.short_logits = _logits(short, shape, dtype, dev, "short")
+        x.short_stride = _row_stride(short, shape, "short")
+    if log_prior is not None:
+        x.log_prior = _of(log_prior, torch.float32, (V,), dev, "log_prior")
+    if alpha is not None:
+        x.n_weights = alpha.numel()
+        x.alpha = _of(alpha, torch.float32, (x.n_weights,), dev, "alpha")
+    if beta is not None:
+        n = beta.numel()
+        if alpha is not None and n != x.n_weights:
+            raise ValueError("alpha and beta must have the same length")
+        x.n_weights = n
+        x.beta = _of(beta, torch.float32, (n,), dev, "beta")
+    x.temperature = temperature
     return x
 
 
@@ -615,12 +633,18 @@ def teacher_of(rows: int, ids: torch.Tensor, logprob: torch.Tensor, row_weight=N
     """``dels_teacher`` of [rows, k] ids and log-probabilities. The caller keeps the tensors alive."""
     if ids.dim() != 2:
         raise ValueError("ids must be [rows, k]")
-    t = Teacher()
-    t.k, t.tail = ids.shape[1], int(bool(tail))
-    t.ids = _of(ids, torch.int32, (rows, t.k), ids.device, "ids")
-    t.logprob = _of(logprob, torch.float32, (rows, t.k), ids.device, "logprob")
-    t.row_weight = _of(row_weight, torch.float32, (rows,), ids.device, "row_weight")
-    return t
+    if not ids.is_cuda:
+        raise ValueError("expected a CUDA tensor: the library's entry points take device pointers")
+    k, dev = ids.shape[1], ids.get_device()
+    return Teacher(_of(ids, torch.int32, (rows, k), dev, "ids"), _of(logprob, torch.float32, (rows, k), dev, "logprob"),
+                   k, 1 if tail else 0, _of(row_weight, torch.float32, (rows,), dev, "row_weight"))
+
+
+def _device_index(device) -> int:
+    device = torch.device(device or "cuda")
+    if device.type != "cuda":
+        raise ValueError("expected a CUDA device: the library's entry points take device pointers")
+    return torch.cuda.current_device() if device.index is None else device.index
 
 
 class TokenScorer:
@@ -630,9 +654,8 @@ class TokenScorer:
 
     def __init__(self, rows: int, V: int, top_k: int = 0, device=None):
         self.rows, self.V, self.top_k = rows, V, top_k
-        self.device = torch.device(device or "cuda")
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._dev = _device_index(device)
+        self.device = torch.device("cuda", self._dev)
         self.ws_bytes = dels_score_workspace_bytes(rows, V)
         if self.ws_bytes == 0:
             raise DelsError(DELS_ERR_BAD_SHAPE, "dels_score_workspace_bytes")
@@ -641,17 +664,22 @@ class TokenScorer:
         self.entropy = torch.empty(rows, dtype=torch.float32, device=self.device)
         self.top_ids = torch.empty(rows, top_k, dtype=torch.int32, device=self.device) if top_k else None
         self.top_logprob = torch.empty(rows, top_k, dtype=torch.float32, device=self.device) if top_k else None
+        self._call = lib().dels_score_rows
+        self._own = [_ptr(t) for t in (self.logprob, self.entropy, self.top_ids, self.top_logprob, self.workspace)]
 
     def __call__(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, short=None, log_prior=None,
                  alpha=None, beta=None, temperature: float = 1.0, stream=None):
         """(log-probabilities or None without tokens, entropies, top ids, top log-probabilities)."""
         x = rows_of(self.rows, self.V, logits, short, log_prior, alpha, beta, temperature)
-        _logits(logits, self.rows, self.V, logits.dtype, self.device, "logits")
-        tok = _of(tokens, torch.int32, (self.rows,), self.device, "tokens")
-        lp = self.logprob if tokens is not None else None
-        _check(dels_score_rows(x, self.rows, self.V, tok, self.top_k, lp, self.entropy, self.top_ids,
-                               self.top_logprob, self.workspace, self.ws_bytes, stream), "dels_score_rows")
-        return lp, self.entropy, self.top_ids, self.top_logprob
+        if logits.get_device() != self._dev:
+            raise ValueError(f"logits must be on {self.device}")
+        tok = _of(tokens, torch.int32, (self.rows,), self._dev, "tokens")
+        lp, ent, ids, tlp, ws = self._own
+        r = self._call(ctypes.byref(x), self.rows, self.V, tok, self.top_k, lp if tok else None, ent, ids, tlp, ws,
+                       self.ws_bytes, _stream(stream))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_score_rows")
+        return self.logprob if tokens is not None else None, self.entropy, self.top_ids, self.top_logprob
 
     def status(self, stream=None) -> int:
         return dels_read_status(self.workspace, stream)
@@ -667,25 +695,27 @@ class Distiller:
         self.rows, self.V, self.k, self.dtype, self.n_weights = rows, V, k, dtype, n_weights
         self.tail, self.temperature = tail, temperature
         dtype_code(dtype)
-        self.device = torch.device(device or "cuda")
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._dev = _device_index(device)
+        self.device = torch.device("cuda", self._dev)
         self.ws_bytes = dels_distill_workspace_bytes(rows, V)
         if self.ws_bytes == 0:
             raise DelsError(DELS_ERR_BAD_SHAPE, "dels_distill_workspace_bytes")
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
         self._loss = torch.empty(rows, dtype=torch.float32, device=self.device)
         self._grad = self._state = None
-        self._grad_w = torch.empty(2, n_weights, dtype=torch.float32, device=self.device)
+        self._grad_w = torch.empty(2, n_weights, dtype=torch.float32, device=self.device).unbind()
+        self._own = [_ptr(t) for t in (self._loss, *self._grad_w, self.workspace)]
+        self._call = lib().dels_distill_step
 
     def _args(self, short, ids, logprob, long, log_prior, alpha, beta, row_weight):
-        _logits(short, self.rows, self.V, self.dtype, self.device, "short")
+        if short.dtype is not self.dtype or short.get_device() != self._dev or ids.get_device() != self._dev:
+            raise ValueError(f"short must be {self.dtype} and all tensors on {self.device}")
         x = rows_of(self.rows, self.V, long, short, log_prior, alpha, beta, self.temperature)
         if x.n_weights not in (0, self.n_weights):
             raise ValueError(f"alpha and beta must have {self.n_weights} entries")
         t = teacher_of(self.rows, ids, logprob, row_weight, self.tail)
-        if t.k != self.k or ids.device != self.device:
-            raise ValueError(f"ids must be [{self.rows}, {self.k}] on {self.device}")
+        if t.k != self.k:
+            raise ValueError(f"ids must be [{self.rows}, {self.k}]")
         return x, t
 
     def loss(self, short, ids, logprob, *, long=None, log_prior=None, alpha=None, beta=None, row_weight=None,
@@ -694,8 +724,11 @@ class Distiller:
         x, t = self._args(short, ids, logprob, long, log_prior, alpha, beta, row_weight)
         if self._state is None:
             self._state = torch.empty(dels_distill_state_bytes(self.rows), dtype=torch.uint8, device=self.device)
-        _check(dels_distill_loss(x, self.rows, self.V, t, self._loss, self._state, self._state.numel(),
-                                 self.workspace, self.ws_bytes, stream), "dels_distill_loss")
+        r = lib().dels_distill_loss(ctypes.byref(x), self.rows, self.V, ctypes.byref(t), self._own[0],
+                                    self._state.data_ptr(), self._state.numel(), self._own[3], self.ws_bytes,
+                                    _stream(stream))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_distill_loss")
         return self._loss
 
     def step(self, short, ids, logprob, *, long=None, log_prior=None, alpha=None, beta=None, row_weight=None,
@@ -708,12 +741,15 @@ class Distiller:
             if self._grad is None:
                 self._grad = torch.empty(self.rows, self.V, dtype=self.dtype, device=self.device)
             out = self._grad
-        _logits(out, self.rows, self.V, self.dtype, self.device, "out")
-        ga = self._grad_w[0] if alpha is not None else None
-        gb = self._grad_w[1] if beta is not None and log_prior is not None else None
-        _check(dels_distill_step(x, self.rows, self.V, t, self._loss, out, _row_stride(out, "out"), ga, gb, self.workspace,
-                                 self.ws_bytes, stream), "dels_distill_step")
-        return self._loss, out, ga, gb
+        shape = (self.rows, self.V)
+        to = _logits(out, shape, self.dtype, self._dev, "out")
+        loss, ga, gb, ws = self._own
+        has_a, has_b = alpha is not None, beta is not None and log_prior is not None
+        r = self._call(ctypes.byref(x), self.rows, self.V, ctypes.byref(t), loss, to, _row_stride(out, shape, "out"),
+                       ga if has_a else None, gb if has_b else None, ws, self.ws_bytes, _stream(stream))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_distill_step")
+        return self._loss, out, self._grad_w[0] if has_a else None, self._grad_w[1] if has_b else None
 
     def status(self, stream=None) -> int:
         return dels_read_status(self.workspace, stream)
@@ -726,37 +762,46 @@ class _DistillLoss(torch.autograd.Function):
             raise ValueError("short must be [rows, V]")
         rows, V = short.shape
         dev = short.device
-        if ids.device != dev:
+        if ids.get_device() != short.get_device():
             raise ValueError(f"ids must be on {dev}")
         x = rows_of(rows, V, long, short, log_prior, alpha, beta, temperature)
         t = teacher_of(rows, ids, logprob, row_weight, tail)
         loss = torch.empty(rows, dtype=torch.float32, device=dev)
-        state = torch.empty(dels_distill_state_bytes(rows), dtype=torch.uint8, device=dev)
-        ws = torch.empty(256, dtype=torch.uint8, device=dev)   # its status word is not read: flagged rows are NaN
-        _check(dels_distill_loss(x, rows, V, t, loss, state, state.numel(), ws, 256), "dels_distill_loss")
+        # the state, and a workspace whose status word is not read (flagged rows are NaN)
+        nbytes = dels_distill_state_bytes(rows)
+        state = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
+        r = lib().dels_distill_loss(ctypes.byref(x), rows, V, ctypes.byref(t), loss.data_ptr(), state.data_ptr(),
+                                    nbytes, state.data_ptr() + nbytes, 256, _stream(None))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_distill_loss")
+        # the tensors themselves are saved, so that backward() sees whether they were changed since
         ctx.save_for_backward(short, alpha, beta, long, log_prior, ids, logprob, row_weight, state)
-        ctx.tail, ctx.temperature = tail, temperature
+        ctx.call = x, t, nbytes, beta is not None and log_prior is not None
         return loss
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
-        short, alpha, beta, long, log_prior, ids, logprob, row_weight, state = ctx.saved_tensors
+        if torch.is_grad_enabled():
+            raise RuntimeError("distill_loss is differentiable once")
+        short, alpha, beta, _, _, _, _, _, state = ctx.saved_tensors
+        x, t, nbytes, has_prior = ctx.call
         rows, V = short.shape
-        x = rows_of(rows, V, long, short, log_prior, alpha, beta, ctx.temperature)
-        t = teacher_of(rows, ids, logprob, row_weight, ctx.tail)
         grad = torch.empty(rows, V, dtype=short.dtype, device=short.device)
         ga = torch.empty_like(alpha) if alpha is not None and ctx.needs_input_grad[1] else None
-        gb = (torch.empty_like(beta) if beta is not None and log_prior is not None and ctx.needs_input_grad[2]
-              else None)
-        up = grad_loss.to(torch.float32).contiguous()
-        _check(dels_distill_grad(x, rows, V, t, up, state, state.numel(), grad, V, ga, gb), "dels_distill_grad")
-        return (grad, ga, gb) + (None,) * 7
+        gb = torch.empty_like(beta) if has_prior and ctx.needs_input_grad[2] else None
+        if grad_loss.dtype is not torch.float32 or not grad_loss.is_contiguous():
+            grad_loss = grad_loss.to(torch.float32).contiguous()
+        r = lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(t), grad_loss.data_ptr(), state.data_ptr(),
+                                    nbytes, grad.data_ptr(), V, None if ga is None else ga.data_ptr(),
+                                    None if gb is None else gb.data_ptr(), _stream(None))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_distill_grad")
+        return grad, ga, gb, None, None, None, None, None, None, None
 
 
 def distill_loss(short, ids, logprob, *, long=None, log_prior=None, alpha=None, beta=None, row_weight=None,
                  tail: bool = False, temperature: float = 1.0) -> torch.Tensor:
-    """Distillation losses [rows] of a local head's logits, differentiable in
+    """Distillation losses [rows] of a local head's logits, differentiable (once) in
     ``short``, ``alpha`` and ``beta``, on the current stream. Rows flagged as
     non-finite have a loss of NaN."""
     return _DistillLoss.apply(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature)
