@@ -2145,8 +2145,9 @@ void plan_cluster(StreamRows& in, int sms, int least) {
   int c = 1;
   while (c < 8 && (c < least || ((long long)in.rows * c < 4LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
   in.cluster = c;
-  // (positions: a row may start up to 7 columns past a 16-byte boundary)
-  in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, 8);
+  // whole items of every thread (positions: a row may start up to 7 columns past a
+  // 16-byte boundary)
+  in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, c > 1 ? 2048 : 8);
 }
 
 int distill_call(const dels_rows* x, int rows, int V, const dels_teacher* t, RowsCall* call, DistillArgs* a) {

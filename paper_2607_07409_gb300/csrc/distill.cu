@@ -362,6 +362,8 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
     }
     return;
   }
+  if (C > 1) cluster_arrive_relaxed();
+  if (warp == kStreamWarps - 1) teacher_side(sh, K, a.tail != 0, inv_t);
   // a constant in the prior drops out of the gradient's sum with it: taken out first
   const float p_ref = FUSED ? row.p_at(row.sh + V / 2) : 0.f;
   float x_k = -INFINITY, s_k = 0.f, p_k = 0.f;
@@ -378,7 +380,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
   float4* keep = kept + tid;
   stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < (int)(sizeof(v) / sizeof(v[0])); ++u) {
       float x[8], s[8], p[8];
       v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
       if constexpr (VEC) {
@@ -425,12 +427,11 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
     for (int d = 16; d > 0; d >>= 1) e += __shfl_xor_sync(0xFFFFFFFFu, e, d);
     if (lane == 0) sh.listed[warp] = ListRec{m_k, e};
   }
-  if (warp == kStreamWarps - 1) teacher_side(sh, K, a.tail != 0, inv_t);
   __syncthreads();
   TailRec tail = tail_merge8(sh.warps[lane & 7], c);
   ListRec listed = list_merge8(sh.listed[lane & 7], c);
   if (C > 1) {
-    cluster_sync_all();            // every CTA of the cluster runs before its shared memory is written
+    cluster_wait();                // every CTA of the cluster runs before its shared memory is written
     if (tid < C) {
       const uint32_t to = cluster_map(smem_u32(&sh.ctas[rank][0]), (uint32_t)tid);
       st_cluster_v4(to, tail.m, tail.sum, tail.s, tail.p);
@@ -501,8 +502,9 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
   }
   if (C > 1) {
     if (tid == 0) st_cluster_v4(cluster_map(smem_u32(&sh.last[rank][0]), 0), v[0], v[1], v[2], 0.f);
-    cluster_sync_all();
+    cluster_arrive();
     if (rank != 0) return;
+    cluster_wait();
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
       v[j] = 0.f;
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_distill_grad(DistillArgs 
   constexpr int U = 2;
   stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < (int)(sizeof(v) / sizeof(v[0])); ++u) {
       float x[8], s[8], p[8], g[8];
       v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
       unlisted_grad(x, st.m, c, f, g);

@@ -370,30 +370,39 @@ struct WarpSoft {
 
 // The items of a thread in positions k0 .. k1 - 1 of a row (a slice, at most the
 // row's end), U at a time: f(items, checked) with checked = std::false_type where
-// all of them are whole for every thread. U loads are in flight at once.
+// all of them are whole for every thread. U loads are in flight at once; what U
+// leaves over, and a row's ends, go one by one.
 template <int U, typename T, bool FUSED, bool VEC, typename F>
 __device__ __forceinline__ void stream_items(const FusedRow<T, FUSED, VEC>& row, int k0, int k1, F&& f) {
   const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
-  const int whole = k0 >= row.sh ? (k1 - k0) / kStreamStep : 0;    // a row's first items may not be
+  const int whole = (k1 - k0) / kStreamStep;
   int it = 0;
+  if (k0 < row.sh && items > 0) {                  // a row's first item may not be whole
+    Item<T, FUSED, VEC> v[1];
+    v[0].load(row, item_pos<VEC>(k0, 0, threadIdx.x), k1);
+    f(v, std::true_type{});
+    it = 1;
+  }
   for (; it + U <= whole; it += U) {
     Item<T, FUSED, VEC> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u].load_whole(row, item_pos<VEC>(k0, it + u, threadIdx.x));
     f(v, std::false_type{});
   }
-  for (; it < items; it += U) {
-    Item<T, FUSED, VEC> v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u].load(row, item_pos<VEC>(k0, it + u, threadIdx.x), k1);
+  for (; it < items; ++it) {
+    const int pos = item_pos<VEC>(k0, it, threadIdx.x);
+    if (!__any_sync(0xFFFFFFFFu, pos < k1)) break;
+    Item<T, FUSED, VEC> v[1];
+    v[0].load(row, pos, k1);
     f(v, std::true_type{});
   }
 }
 
-// Cluster barrier of C CTAs; one CTA alone takes its own barrier.
-__device__ __forceinline__ void cluster_or_cta_sync(int C) {
-  if (C > 1) cluster_sync_all();
-  else __syncthreads();
+// The two halves of a cluster barrier (all threads of all its CTAs).
+__device__ __forceinline__ void cluster_arrive_relaxed() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 }  // namespace dels

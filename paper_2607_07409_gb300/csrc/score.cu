@@ -34,22 +34,23 @@ constexpr int kCandidates = kStreamWarps * 256 + 4 * kMaxTopK;   // one round of
 struct ScoreShared {
   unsigned long long cand[kCandidates];
   unsigned long long best[kMaxTopK];       // this CTA's entries in order, 0 where there are none
+  unsigned long long slices[kMaxCluster * kMaxTopK];   // first CTA: all slices' entries
   int groups[kStreamThreads];
   SoftRec warps[kStreamWarps];
   SoftRec ctas[kMaxCluster];
   int ncand, ngroups;
 };
 
-// The K largest of cand[0 .. n) to best[] in order (all threads; n <= kCandidates):
-// a warp counts what is above one candidate, 32 at a time.
-__device__ void sort_best(ScoreShared& sh, int n, int K) {
+// The K largest of cand[0 .. n) to best[] in order (all threads): a warp counts
+// what is above one candidate, 32 at a time.
+__device__ void sort_best(ScoreShared& sh, const unsigned long long* cand, int n, int K) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int k = threadIdx.x; k < K; k += kStreamThreads) sh.best[k] = 0ull;
   __syncthreads();
   for (int i = warp; i < n; i += kStreamWarps) {
-    const unsigned long long x = sh.cand[i];
+    const unsigned long long x = cand[i];
     int rank = 0;
-    for (int j = lane; j < n; j += 32) rank += sh.cand[j] > x;
+    for (int j = lane; j < n; j += 32) rank += cand[j] > x;
     rank = __reduce_add_sync(0xFFFFFFFFu, rank);
     if (lane == 0 && rank < K && x) sh.best[rank] = x;
   }
@@ -64,9 +65,11 @@ __device__ __forceinline__ void keep_entries(ScoreShared& sh, const FusedRow<T, 
   v.load(row, pos, k1);
   float x[8], s[8], p[8];
   v.template values<true>(row, k1, x, s, p);
+  const float least = from_order_u32((unsigned)(floor_key >> 32));
+  if (!(max8(x) >= least)) return;                 // most items: nothing
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (!(x[i] > -INFINITY)) continue;
+    if (!(x[i] >= least && x[i] > -INFINITY)) continue;
     const unsigned long long e = entry_key(x[i], elem_pos<VEC>(pos, i) - row.sh);
     if (e < floor_key) continue;
     const int at = atomicAdd(&sh.ncand, 1);
@@ -97,6 +100,7 @@ __device__ void slice_top(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, i
   const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;      // per thread
   const int parts = (items + 31) / 32;                              // a warp's rounds for one thread's items
   const int jobs = sh.ngroups * parts;
+  if (tau == 0u) tau = order_u32(-INFINITY);
   unsigned long long floor_key = (unsigned long long)tau << 32;     // what an entry has to reach
   for (int j = warp; j < jobs; j += kStreamWarps) {
     const int it = (j % parts) * 32 + lane;
@@ -113,7 +117,7 @@ __device__ void slice_top(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, i
       const int n = sh.ncand;
       __syncthreads();
       if (n > kCandidates - kStreamWarps * 256) {
-        sort_best(sh, n, K);
+        sort_best(sh, sh.cand, n, K);
         for (int k = tid; k < K; k += kStreamThreads) sh.cand[k] = sh.best[k];
         floor_key = sh.best[K - 1];                                 // n > K: there are K
         if (tid == 0) sh.ncand = K;
@@ -124,7 +128,7 @@ __device__ void slice_top(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, i
       __syncthreads();
     }
   }
-  sort_best(sh, sh.ncand, K);
+  sort_best(sh, sh.cand, sh.ncand, K);
 }
 
 template <typename T, bool FUSED, bool VEC>
@@ -152,6 +156,7 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_score_rows(ScoreArgs a) {
     }
     return;
   }
+  if (C > 1) cluster_arrive_relaxed();
   const FusedRow<T, FUSED, VEC> row(a.in, r);
   const bool tok_ok = tok >= 0 && tok < V;
   float x_tok = 0.f;
@@ -160,14 +165,15 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_score_rows(ScoreArgs a) {
   const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
 
   // items in flight per thread: 64 bytes of bf16 rows, 64 to 128 of the others
-  constexpr int U = FUSED ? 2 : sizeof(T) == 2 ? 4 : 2;
+  constexpr int U = sizeof(T) == 2 ? (FUSED ? 2 : 4) : (FUSED ? 1 : 2);
   WarpSoft st;
   st.init();
   float top = -INFINITY;
   stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
-    float x[U][8], s[8], p[8], vm = -INFINITY;
+    constexpr int N = sizeof(v) / sizeof(v[0]);
+    float x[N][8], s[8], p[8], vm = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < N; ++u) {
       v[u].template values<decltype(checked)::value>(row, k1, x[u], s, p);
       vm = fmaxf(vm, max8(x[u]));
     }
@@ -182,24 +188,24 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_score_rows(ScoreArgs a) {
   if (K > 0) slice_top(sh, row, k0, k1, K, top);
   SoftRec all = cta;
   if (C > 1) {
-    cluster_sync_all();            // every CTA of the cluster runs before its shared memory is written
+    cluster_wait();                // every CTA of the cluster runs before its shared memory is written
     if (tid < 3) {
       const float v = tid == 0 ? cta.m : tid == 1 ? cta.rest : cta.w;
       st_cluster_f32(cluster_map(smem_u32(&sh.ctas[rank]), 0) + 4 * tid, v);
     }
-    // the slices' entries into the first CTA's candidates (its own are free again)
     if (K > 0) {
-      const uint32_t to = cluster_map(smem_u32(&sh.cand[(size_t)rank * K]), 0);
+      const uint32_t to = cluster_map(smem_u32(&sh.slices[(size_t)rank * K]), 0);
       for (int k = tid; k < K; k += kStreamThreads) {
         const unsigned long long e = sh.best[k];
         st_cluster_f32(to + 8 * k, __uint_as_float((unsigned)e));
         st_cluster_f32(to + 8 * k + 4, __uint_as_float((unsigned)(e >> 32)));
       }
     }
-    cluster_sync_all();
+    cluster_arrive();
     if (rank != 0) return;
+    cluster_wait();
     all = softrec_merge8((lane & 7) < C ? sh.ctas[lane & 7] : softrec_init(), c);
-    if (K > 0) sort_best(sh, C * K, K);
+    if (K > 0) sort_best(sh, sh.slices, C * K, K);
   }
   const bool ok = softrec_valid(all);
   const float ln_s = log1pf(all.rest), inv_t = a.in.inv_t;
