@@ -463,7 +463,7 @@ typedef struct {
   const float* alpha;            /* [device] [n_weights], or NULL */
   const float* beta;             /* [device] [n_weights], or NULL */
   int n_weights;
-  float temperature;             /* finite, > 0 */
+  float temperature;             /* 1e-30 .. 1e30 */
 } dels_rows;
 
 /*

@@ -2098,8 +2098,7 @@ int rows_call(const dels_rows* x, int rows, int V, int max_v, RowsCall* out) {
   if (!x) return DELS_ERR_NULL_POINTER;
   if (x->dtype != DELS_F32 && x->dtype != DELS_BF16) return DELS_ERR_BAD_DTYPE;
   if (rows < 0 || rows > (1 << 27) || V < 1 || V > max_v) return DELS_ERR_BAD_SHAPE;
-  if (!(x->temperature > 0.f) || !std::isfinite(x->temperature) || !std::isfinite(1.f / x->temperature))
-    return DELS_ERR_BAD_SHAPE;
+  if (!(x->temperature >= 1e-30f && x->temperature <= 1e30f)) return DELS_ERR_BAD_SHAPE;
   const bool has_long = x->long_logits != nullptr, has_short = x->short_logits != nullptr;
   if (x->n_weights < 0 || ((x->alpha || x->beta) && x->n_weights < 1)) return DELS_ERR_BAD_SHAPE;
   const long long ld_long = x->long_stride ? x->long_stride : V, ld_short = x->short_stride ? x->short_stride : V;
@@ -2227,6 +2226,9 @@ int dels_score_rows(const dels_rows* x, int rows, int V, const int32_t* tokens, 
   a.in = call.in;
   a.tokens = tokens;
   a.top_k = top_k;
+  // finite after the scaling too (a zero times it stays one), and far below any entry
+  // that has weight beside a reference of at most kMaxRef / scale
+  a.low = -std::min(3.3e38f, 1e37f / call.in.scale);
   a.out_lp = out_logprob;
   a.out_entropy = out_entropy;
   a.out_ids = out_top_ids;
@@ -2312,7 +2314,7 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
   const bool f32 = x->dtype == DELS_F32;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_DISTILL);
-  if (rows > 0 && distill_step_fits(a))
+  if (rows > 0 && distill_step_fits(a, f32, call.fused, call.vec))
     return launch_distill_step(a, f32, call.fused, call.vec, s) == cudaSuccess ? DELS_OK : DELS_ERR_CUDA;
   if (rows > 0) {
     if (!plan_distill(&a, false)) return DELS_ERR_CUDA;

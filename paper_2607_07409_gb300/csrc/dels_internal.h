@@ -133,6 +133,7 @@ struct ScoreArgs {
   StreamRows in;
   const int32_t* tokens;         // [rows] or null
   int top_k;
+  float low;                     // bf16: entries below it, relative to a reference, count as it
   float* out_lp;                 // [rows] or null
   float* out_entropy;            // [rows] or null
   int32_t* out_ids;              // [rows, top_k]
@@ -143,16 +144,15 @@ cudaError_t launch_score_rows(const ScoreArgs& a, bool f32, bool fused, bool vec
 
 // Statistics of one row, written by the loss kernel and read by the gradient's.
 struct DistillState {
-  float m;          // largest student entry
-  float inv_s;      // 1 / S, S = sum exp((l - m) / T)
-  float ln_s;       // ln S
-  float coef_n;     // dL/dl of an id that is not listed: q coef_n / T
-  float mass;       // of a listed one: (q mass - p) / T
+  float f_off, f_r; // reference of the exponentials: z = (l - f_off) c - f_r
+  float factor;     // dL/dl of an id that is not listed: factor 2^z / T
+  float base;       // ln q = (l - base) / T - base_ln
+  float base_ln;
+  float mass;       // dL/dl of a listed one: (q mass - p) / T
   float t_max;      // teacher: ln p = (t - t_max) t_scale - log_norm
   float t_scale;
   float log_norm;
   float weight;     // the row's weight; 0: left out
-  float pad0;
   float d_alpha;    // dL/d alpha, dL/d beta (weight included)
   float d_beta;
   float pad[4];
@@ -180,7 +180,7 @@ struct DistillArgs {
 cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 // Loss and gradient at once: a slice's values stay in shared memory.
 constexpr int kStepSmemBytes = 200 * 1024;
-bool distill_step_fits(const DistillArgs& a);
+bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec);
 cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_weight_grads(const DistillArgs& a, cudaStream_t s);

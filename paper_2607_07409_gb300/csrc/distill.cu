@@ -26,22 +26,28 @@ namespace {
 
 enum { kFlagAny = 1, kFlagBadId = 2, kFlagBadLogit = 4, kFlagTwice = 8 };
 
-// Sums of the columns that are not listed relative to m, an entry among them or one
-// before them: sum 2^t, sum 2^t l_S and sum 2^t (l_P - ref), t = (l - m) log2(e) / T.
+// Sums of the columns that are not listed, relative to f, the reference of m, an entry
+// among them: sum 2^z, sum 2^z l_S and sum 2^z (l_P - ref).
 struct TailRec {
-  float m, sum, s, p;
+  float m;
+  Ref f;
+  float sum, s, p;
 };
-// Those of the listed: m the largest, `rest` without one that attains it (the
-// student's whole mass may be there: ln(1 + rest) keeps its digits).
+// Those of the listed: m the largest, rest = sum 2^((l - m) c) without one that
+// attains it (the student's whole mass may be there: ln(1 + rest) keeps its digits).
 struct ListRec {
   float m, rest;
 };
-// Record i of `tails` in lanes 0 .. 7 (i + 8: the same; all lanes converged)
-// merged into every lane, in a fixed order.
+__device__ __forceinline__ TailRec tail_init() { return TailRec{-INFINITY, Ref{0.f, 0.f}, 0.f, 0.f, 0.f}; }
+// The records of lanes 0 .. 7 (i + 8: the same; all lanes converged) merged into
+// every lane, in a fixed order.
 __device__ __forceinline__ TailRec tail_merge8(const TailRec& b, float c) {
   TailRec r;
   r.m = warp_max(b.m);
-  const float f = b.m == -INFINITY ? (b.sum != b.sum ? NAN : 0.f) : ex2_approx((b.m - r.m) * c);
+  const int top = __ffs(__ballot_sync(0xFFFFFFFFu, b.m == r.m)) - 1;
+  r.f.off = __shfl_sync(0xFFFFFFFFu, b.f.off, top);
+  r.f.r = __shfl_sync(0xFFFFFFFFu, b.f.r, top);
+  const float f = b.m == -INFINITY ? 1.f : ex2_approx(ref_shift(b.f, r.f, c));   // (none: 0, or NaN, stays)
   r.sum = f * b.sum;
   r.s = f * b.s;
   r.p = f * b.p;
@@ -66,39 +72,47 @@ __device__ __forceinline__ ListRec list_merge8(const ListRec& b, float c) {
 }
 
 // One lane's sums over the columns that are not listed. The reference of a warp's
-// exponentials is an entry that it has met: the largest of its first item, and
+// exponentials is that of an entry it has met: the largest of its first item, and
 // another only when one 2^20 times as likely comes (each is in float32's range and
 // the sums' digits do not depend on it; the largest entry so far would change about
 // ln n times, and a slice has few items).
 constexpr float kFarAbove = 20.f;
 template <bool FUSED>
 struct WarpTail {
-  float ref, limit, off;   // the same in every lane; off = ref, or 0 while ref is -inf
+  float m, limit;      // the same in every lane, as f
+  Ref f;
   f32x2 sum, s, p;
   __device__ __forceinline__ void init() {
-    ref = limit = -INFINITY;
-    off = 0.f;
+    m = limit = -INFINITY;
+    f = Ref{0.f, 0.f};
     sum = s = p = 0ull;
   }
   // One item's values, all lanes converged.
-  __device__ __forceinline__ void push(const float (&x)[8], const float (&sv)[8], const float (&pv)[8], float c,
-                                       float p_ref) {
+  __device__ __forceinline__ void push(float (&x)[8], const float (&sv)[8], const float (&pv)[8], float c, float p_ref) {
     const float vm = max8(x);
     if (__any_sync(0xFFFFFFFFu, vm > limit)) {
       const float top = warp_max(vm);
-      const f32x2 f = both2(ref == -INFINITY ? (sum2(sum) != sum2(sum) ? NAN : 0.f) : ex2_approx((ref - top) * c));
-      sum = mul2(f, sum);
-      s = mul2(f, s);
-      p = mul2(f, p);
-      ref = off = top;
+      const Ref to = make_ref(top, c);
+      if (m > -INFINITY) {
+        const f32x2 k = both2(ex2_approx(ref_shift(f, to, c)));
+        sum = mul2(k, sum);
+        s = mul2(k, s);
+        p = mul2(k, p);
+      }
+      f = to;
+      m = top;
       limit = top + kFarAbove / c;
     }
-    const f32x2 no = both2(-off), c2 = both2(c), np = both2(-p_ref);
+    if (f.off != 0.f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] -= f.off;
+    }
+    const f32x2 c2 = both2(c), nr = both2(-f.r), np = both2(-p_ref);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      float t0, t1;
-      split2(mul2(add2(pair2(x[i], x[i + 1]), no), c2), t0, t1);
-      const f32x2 e = pair2(ex2_approx(t0), ex2_approx(t1));
+      float z0, z1;
+      split2(fma2(pair2(x[i], x[i + 1]), c2, nr), z0, z1);
+      const f32x2 e = pair2(ex2_approx(z0), ex2_approx(z1));
       sum = add2(sum, e);
       if constexpr (FUSED) {
         s = fma2(e, pair2(fmaxf(sv[i], -FLT_MAX), fmaxf(sv[i + 1], -FLT_MAX)), s);     // a masked entry: 0
@@ -107,7 +121,7 @@ struct WarpTail {
     }
   }
   __device__ __forceinline__ TailRec record() const {
-    TailRec r{ref, sum2(sum), sum2(s), sum2(p)};
+    TailRec r{m, f, sum2(sum), sum2(s), sum2(p)};
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
       r.sum += __shfl_xor_sync(0xFFFFFFFFu, r.sum, d);
@@ -120,6 +134,15 @@ struct WarpTail {
   }
 };
 
+// Copies ahead of the loss and gradient kernels, and of the step's, whose items stay
+// (beside 10 items of 8 KB its ring is to leave room for a second CTA on the SM).
+template <typename T, bool FUSED>
+using LossCopies = Copies<T, FUSED, 1, FUSED ? (sizeof(T) == 2 ? 3 : 2) : 4>;
+template <typename T, bool FUSED>
+using StepCopies = Copies<T, FUSED, 1, 3, 8>;
+template <typename T, bool FUSED, bool GRAD>
+using RowCopies = std::conditional_t<GRAD, StepCopies<T, FUSED>, LossCopies<T, FUSED>>;
+
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   uint32_t w;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
@@ -129,7 +152,7 @@ __device__ __forceinline__ void grad_elem(float* g, long long i, float v) { g[i]
 __device__ __forceinline__ void grad_elem(uint16_t* g, long long i, float v) { g[i] = (uint16_t)bf16_pair(v, 0.f); }
 __device__ __forceinline__ void grad_vec(float* g, const float (&v)[8]) {
   __stcs(reinterpret_cast<float4*>(g), make_float4(v[0], v[1], v[2], v[3]));
-  __stcs(reinterpret_cast<float4*>(g) + 1, make_float4(v[4], v[5], v[6], v[7]));
+  __stcs(reinterpret_cast<float4*>(g + kHalf<float>), make_float4(v[4], v[5], v[6], v[7]));
 }
 __device__ __forceinline__ void grad_vec(uint16_t* g, const float (&v)[8]) {
   __stcs(reinterpret_cast<uint4*>(g),
@@ -139,24 +162,28 @@ __device__ __forceinline__ void grad_vec(uint16_t* g, const float (&v)[8]) {
 // gradient's rows lie like the logits' against 16-byte boundaries.
 template <typename T, bool VEC>
 __device__ __forceinline__ void grad_item(T* g, int k, int begin, int stop, bool vec, const float (&v)[8]) {
-  if (VEC && vec && k >= begin && k + 8 <= stop) {
+  if (VEC && vec && k >= begin && k + kHalf<T> + 4 <= stop) {
     grad_vec(g + k, v);
     return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int q = elem_pos<VEC>(k, i);
+    const int q = elem_pos<T, VEC>(k, i);
     if (q >= begin && q < stop) grad_elem(g, q, v[i]);
   }
 }
-// g = f 2^((x - m) c) of 8 values.
-__device__ __forceinline__ void unlisted_grad(const float (&x)[8], float m, float c, float f, float (&g)[8]) {
-  const f32x2 nm = both2(-m), c2 = both2(c), f2 = both2(f);
+// g = k 2^z of 8 values.
+__device__ __forceinline__ void unlisted_grad(float (&x)[8], const Ref& f, float c, float k, float (&g)[8]) {
+  if (f.off != 0.f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] -= f.off;
+  }
+  const f32x2 c2 = both2(c), nr = both2(-f.r), k2 = both2(k);
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
-    float t0, t1;
-    split2(mul2(add2(pair2(x[i], x[i + 1]), nm), c2), t0, t1);
-    split2(mul2(f2, pair2(ex2_approx(t0), ex2_approx(t1))), g[i], g[i + 1]);
+    float z0, z1;
+    split2(fma2(pair2(x[i], x[i + 1]), c2, nr), z0, z1);
+    split2(mul2(k2, pair2(ex2_approx(z0), ex2_approx(z1))), g[i], g[i + 1]);
   }
 }
 
@@ -169,7 +196,7 @@ struct Teacher {
 struct LossShared {
   TailRec warps[kStreamWarps];
   ListRec listed[kStreamWarps];
-  float ctas[kMaxCluster][8];       // TailRec, then ListRec
+  float ctas[kMaxCluster][8];       // TailRec, ListRec
   float sums[kStreamWarps][4];
   float last[kMaxCluster][4];
   float logit[kMaxTopK];            // the teacher's as stored; -inf: left out
@@ -296,7 +323,7 @@ __device__ void twice_grads(const DistillArgs& a, LossShared& sh, long long r, b
 // are read once: 3 s V bytes a row instead of 5 s V. Each thread reads back what it
 // wrote itself.
 template <typename T, bool FUSED, bool VEC, bool GRAD>
-__global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(DistillArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(DistillArgs a) {
   extern __shared__ __align__(16) unsigned bitmap[];   // one bit per position of the slice: listed
   __shared__ LossShared sh;
   pdl_wait();
@@ -310,7 +337,9 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
   const FusedRow<T, FUSED, VEC> row(a.in, r);
   const long long first = (long long)rank * a.in.slice_cols;
   const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
-  float4* kept = reinterpret_cast<float4*>(bitmap + (a.in.slice_cols + 127) / 128 * 4);
+  using Cp = RowCopies<T, FUSED, GRAD>;
+  uint8_t* ring = reinterpret_cast<uint8_t*>(bitmap + (a.in.slice_cols + 127) / 128 * 4);
+  uint8_t* kept = ring + (VEC ? Cp::kRingBytes : 0);           // GRAD: the slice's values, 32 bytes an item
   T* out = nullptr;                                // the row's gradient at position 0
   if constexpr (GRAD) out = static_cast<T*>(a.grad) + r * a.ld_grad - row.sh;
 
@@ -350,7 +379,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
   if (weight == 0.f || !(flags & (kFlagAny | kFlagBadLogit))) {     // left out: the logits are not read
     if constexpr (GRAD) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
+      for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
     }
     if (rank == 0 && tid == 0) {
       if (weight != 0.f && (flags & kFlagBadId)) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
@@ -376,17 +405,21 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
   // the columns that are not listed
   WarpTail<FUSED> st;
   st.init();
-  constexpr int U = GRAD ? (sizeof(T) == 2 ? 4 : 2) : 2;
-  float4* keep = kept + tid;
-  stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
-#pragma unroll
-    for (int u = 0; u < (int)(sizeof(v) / sizeof(v[0])); ++u) {
+  stream_items<Cp>(row, k0, k1, ring, kept, [&](auto& v, auto checked, int call) {
+    {
+      constexpr int u = 0;         // (one item a call)
       float x[8], s[8], p[8];
       v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
       if constexpr (VEC) {
         const int b = v[u].k - k0;
-        const unsigned bits = !decltype(checked)::value || b < k1 - k0
-                                  ? reinterpret_cast<const unsigned char*>(bitmap)[b >> 3] : 0u;
+        unsigned bits = 0u;        // of the item's 8 positions
+        if constexpr (sizeof(T) == 2) {
+          if (!decltype(checked)::value || b < k1 - k0) bits = reinterpret_cast<const unsigned char*>(bitmap)[b >> 3];
+        } else {
+          if (!decltype(checked)::value || b < k1 - k0) bits = bitmap[b >> 5] >> (b & 31) & 15u;
+          if (!decltype(checked)::value || b + kHalf<T> < k1 - k0)
+            bits |= (bitmap[(b + kHalf<T>) >> 5] >> (b & 31) & 15u) << 4;
+        }
         if (bits) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -395,16 +428,14 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int b = elem_pos<VEC>(v[u].k, i) - k0;
+          const int b = elem_pos<T, VEC>(v[u].k, i) - k0;
           if ((!decltype(checked)::value || b < k1 - k0) && (bitmap[b >> 5] >> (b & 31) & 1u)) x[i] = -INFINITY;
         }
       }
       if constexpr (GRAD) {
-        if (!decltype(checked)::value || v[u].k < k1) {
-          keep[0] = make_float4(x[0], x[1], x[2], x[3]);
-          keep[kStreamThreads] = make_float4(x[4], x[5], x[6], x[7]);
-        }
-        keep += 2 * kStreamThreads;
+        float4* keep = reinterpret_cast<float4*>(kept) + call * 2 * kStreamThreads + tid;
+        keep[0] = make_float4(x[0], x[1], x[2], x[3]);
+        keep[kStreamThreads] = make_float4(x[4], x[5], x[6], x[7]);
       }
       st.push(x, s, p, c, p_ref);
     }
@@ -434,42 +465,47 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
     cluster_wait();                // every CTA of the cluster runs before its shared memory is written
     if (tid < C) {
       const uint32_t to = cluster_map(smem_u32(&sh.ctas[rank][0]), (uint32_t)tid);
-      st_cluster_v4(to, tail.m, tail.sum, tail.s, tail.p);
-      st_cluster_v4(to + 16, listed.m, listed.rest, 0.f, 0.f);
+      st_cluster_v4(to, tail.m, tail.f.off, tail.f.r, tail.sum);
+      st_cluster_v4(to + 16, tail.s, tail.p, listed.m, listed.rest);
     }
     cluster_sync_all();
     const float* rec = sh.ctas[lane & 7];
     const bool in = (lane & 7) < C;
-    tail = tail_merge8(in ? TailRec{rec[0], rec[1], rec[2], rec[3]} : TailRec{-INFINITY, 0.f, 0.f, 0.f}, c);
-    listed = list_merge8(in ? ListRec{rec[4], rec[5]} : ListRec{-INFINITY, 0.f}, c);
+    tail = tail_merge8(in ? TailRec{rec[0], Ref{rec[1], rec[2]}, rec[3], rec[4], rec[5]} : tail_init(), c);
+    listed = list_merge8(in ? ListRec{rec[6], rec[7]} : ListRec{-INFINITY, 0.f}, c);
   }
-  // S = sum over all columns, relative to the larger reference; rest = S - 1 where
-  // that is a listed entry of the largest value
-  const float m = fmaxf(tail.m, listed.m);
-  const float f_tail = tail.m == -INFINITY ? (tail.sum != tail.sum ? NAN : 0.f) : ex2_approx((tail.m - m) * c);
-  const float f_list = listed.m == -INFINITY ? (listed.rest != listed.rest ? NAN : 0.f) : ex2_approx((listed.m - m) * c);
-  const float tail_sum = f_tail * tail.sum;
-  const float list_sum = listed.m == -INFINITY ? f_list : f_list * (1.f + listed.rest);
-  const float rest = listed.m == m ? listed.rest + tail_sum : tail_sum - 1.f + list_sum;
-  const float S = 1.f + rest, inv_s = 1.f / S, ln_s = log1pf(rest);
-  const bool ok = m > -INFINITY && m < INFINITY && S > 0.f && S < INFINITY && !(flags & kFlagBadLogit);
+  // S = sum over all columns = listed + not listed, in units of the reference f of
+  // those that are not listed (of the largest listed where there are none).
+  const bool none_listed = listed.m == -INFINITY, none_else = tail.m == -INFINITY;
+  const Ref f = none_else ? make_ref(listed.m, c) : tail.f;
+  const float z_l = none_listed ? -INFINITY : ref_z(listed.m, f, c);
+  const float list_sum = none_listed ? listed.rest : (1.f + listed.rest) * ex2_approx(z_l);   // may be infinite
+  const float inv_s = 1.f / (tail.sum + list_sum);
+  // ln q = (l - base) / T - base_ln: from the largest listed entry, whose digits that
+  // keeps, unless the others are far above it
+  const bool from_list = !none_listed && z_l >= -20.f;
+  const float base = from_list ? listed.m : f.off;
+  const float base_ln = from_list ? log1pf(listed.rest + tail.sum * ex2_approx(-z_l))
+                                  : f.r * kLn2 + logf(tail.sum + list_sum);
+  const float top = fmaxf(tail.m, listed.m);
+  const bool ok = top > -INFINITY && top < INFINITY && tail.sum >= 0.f && tail.sum < INFINITY && listed.rest >= 0.f &&
+                  listed.rest < INFINITY && !(flags & kFlagBadLogit);
   const Teacher te = sh.teacher;
-  // q_t = tail_sum / S; ln q_t = -ln(1 + list_sum / tail_sum)
-  const bool has_tail = a.tail && te.rest > 0.f && tail_sum > 0.f;
+  // the tail: q_t = tail.sum / S; dL/dl of one of it (M - p_t / q_t) q = (M / S - p_t / tail.sum) 2^z
+  const bool has_tail = a.tail && te.rest > 0.f && tail.sum > 0.f;
   const float mass = has_tail ? 1.f : te.sum;
-  const float coef_n = has_tail ? mass - te.rest * (S / tail_sum) : mass;
+  const float factor = mass * inv_s - (has_tail ? te.rest / tail.sum : 0.f);
 
   const float up = weight * inv_t * (FUSED ? row.a : 1.f);   // dL/dl -> what the gradient holds
   if constexpr (GRAD) {
-    const float f = ok ? up * coef_n * inv_s : NAN;
-    const float4* got = kept + tid;
+    const float k2 = ok ? up * factor : NAN;
+    const float4* got = reinterpret_cast<const float4*>(kept) + tid;
     for (int it = 0; it < items; ++it, got += 2 * kStreamThreads) {
-      const int k = item_pos<VEC>(k0, it, tid);
+      const int k = item_pos<T, VEC>(k0, it, tid);
       if (k >= k1) break;
       const float4 u = got[0], w = got[kStreamThreads];
-      const float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
-      float g[8];
-      unlisted_grad(x, m, c, f, g);
+      float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w}, g[8];
+      unlisted_grad(x, f, c, k2, g);
       grad_item<T, VEC>(out, k, row.sh, k1, a.grad_vec, g);
     }
   }
@@ -477,7 +513,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
   float g_k = 0.f;
   if (mine) {
     const float lp = (logit - te.t_max) * te.t_scale - te.log_norm, p = expf(lp);
-    const float lq = (x_k - m) * inv_t - ln_s;
+    const float lq = (x_k - base) * inv_t - base_ln;
     const float g = once ? listed_grad(lq, lp, mass) : -p;
     v[0] = p > 0.f ? p * (lp - lq) : 0.f;
     v[1] = g * s_k;
@@ -517,21 +553,24 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
   float loss = v[0];
   if (has_tail) {
     const float log_rest = te.rest > 0.5f ? log1pf(-te.sum) : logf(te.rest);
-    loss += te.rest * (log_rest + log1pf(list_sum / tail_sum));
+    // -ln q_t = ln(1 + list_sum / tail.sum)
+    const float more = z_l > 60.f ? z_l * kLn2 + logf((1.f + listed.rest) / tail.sum) : log1pf(list_sum / tail.sum);
+    loss += te.rest * (log_rest + more);
   }
   if (a.out_loss) a.out_loss[r] = ok ? weight * loss : NAN;
   DistillState o{};
-  o.m = m;
-  o.inv_s = inv_s;
-  o.ln_s = ln_s;
-  o.coef_n = ok ? coef_n : NAN;
+  o.f_off = f.off;
+  o.f_r = f.r;
+  o.factor = ok ? factor : NAN;
+  o.base = base;
+  o.base_ln = base_ln;
   o.mass = ok ? mass : NAN;
   o.t_max = te.t_max;
   o.t_scale = te.t_scale;
   o.log_norm = te.log_norm;
   o.weight = weight;
-  o.d_alpha = ok ? weight * inv_t * (coef_n * inv_s * (f_tail * tail.s) + v[1]) : NAN;
-  o.d_beta = ok ? -weight * inv_t * (coef_n * inv_s * (f_tail * tail.p) + v[2]) : NAN;
+  o.d_alpha = ok ? weight * inv_t * (factor * tail.s + v[1]) : NAN;
+  o.d_beta = ok ? -weight * inv_t * (factor * tail.p + v[2]) : NAN;
   a.state[r] = o;
   }
   if constexpr (GRAD) finish_rows(a, sh);
@@ -541,7 +580,8 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 4) k_distill_loss(D
 // then the listed ones over it. The rows' own logits may be the output (each column
 // is read before it is written).
 template <typename T, bool FUSED, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, 4) k_distill_grad(DistillArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs a) {
+  extern __shared__ __align__(16) uint8_t ring[];
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
   const int tid = threadIdx.x;
@@ -557,7 +597,7 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_distill_grad(DistillArgs 
   const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
   if (st.weight == 0.f) {                          // left out
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
+    for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
     return;
   }
   const float g0 = up * st.weight * a.in.inv_t * (FUSED ? row.a : 1.f);
@@ -583,21 +623,18 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_distill_grad(DistillArgs 
         }
         before += expf((tk - st.t_max) * st.t_scale - st.log_norm);
       }
-      const float lq = (x - st.m) * a.in.inv_t - st.ln_s;
+      const float lq = (x - st.base) * a.in.inv_t - st.base_ln;
       g_k = g0 * (listed_grad(lq, lp, st.mass) - before);
     }
   }
   __syncthreads();                                 // the output may be l_S itself
-  const float f = g0 * st.coef_n * st.inv_s;
-  constexpr int U = 2;
-  stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
-#pragma unroll
-    for (int u = 0; u < (int)(sizeof(v) / sizeof(v[0])); ++u) {
-      float x[8], s[8], p[8], g[8];
-      v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
-      unlisted_grad(x, st.m, c, f, g);
-      grad_item<T, VEC>(out, v[u].k, row.sh, k1, a.grad_vec, g);
-    }
+  const float k2 = g0 * st.factor;
+  const Ref f{st.f_off, st.f_r};
+  stream_items<LossCopies<T, FUSED>>(row, k0, k1, ring, nullptr, [&](auto& v, auto checked, int) {
+    float x[8], s[8], p[8], g[8];
+    v[0].template values<decltype(checked)::value>(row, k1, x, s, p);
+    unlisted_grad(x, f, c, k2, g);
+    grad_item<T, VEC>(out, v[0].k, row.sh, k1, a.grad_vec, g);
   });
   __syncthreads();
   if (id >= 0) grad_elem(out, id + row.sh, g_k);
@@ -610,10 +647,17 @@ __global__ void __launch_bounds__(256) k_weight_grads(DistillArgs a) {
   weight_grads<256>(a, blockIdx.x, red);
 }
 
-// Shared memory of the loss kernel: the bitmap, and with GRAD the slice's values.
-size_t loss_smem(const StreamRows& in, bool grad) {
+// Shared memory of the loss kernel: the bitmap, the ring, and with GRAD the slice's
+// values.
+template <typename T, bool FUSED, bool GRAD>
+constexpr size_t ring_bytes(bool vec) {
+  return vec ? RowCopies<T, FUSED, GRAD>::kRingBytes : 0;
+}
+template <typename T, bool GRAD>
+size_t loss_smem(const StreamRows& in, bool fused, bool vec) {
   const size_t items = ((size_t)in.slice_cols + kStreamStep - 1) / kStreamStep;
-  return ((size_t)in.slice_cols + 127) / 128 * 16 + (grad ? items * kStreamStep * 4 : 0);
+  return ((size_t)in.slice_cols + 127) / 128 * 16 + (GRAD ? items * kStreamStep * 4 : 0) +
+         (fused ? ring_bytes<T, true, GRAD>(vec) : ring_bytes<T, false, GRAD>(vec));
 }
 
 template <typename T, bool GRAD>
@@ -621,7 +665,7 @@ cudaError_t launch_loss_t(const DistillArgs& a, bool fused, bool vec, cudaStream
   const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
   auto k = fused ? (vec ? k_distill_loss<T, true, true, GRAD> : k_distill_loss<T, true, false, GRAD>)
                  : (vec ? k_distill_loss<T, false, true, GRAD> : k_distill_loss<T, false, false, GRAD>);
-  const size_t bytes = loss_smem(a.in, GRAD);
+  const size_t bytes = loss_smem<T, GRAD>(a.in, fused, vec);
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
   if (e != cudaSuccess) return e;
   return launch_pdl_cluster(k, grid, block, bytes, s, a.in.cluster, a);
@@ -632,7 +676,10 @@ cudaError_t launch_grad_t(const DistillArgs& a, bool fused, bool vec, cudaStream
   const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
   auto k = fused ? (vec ? k_distill_grad<T, true, true> : k_distill_grad<T, true, false>)
                  : (vec ? k_distill_grad<T, false, true> : k_distill_grad<T, false, false>);
-  return launch_pdl(k, grid, block, 0, s, a);
+  const size_t bytes = fused ? ring_bytes<T, true, false>(vec) : ring_bytes<T, false, false>(vec);
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(k, grid, block, bytes, s, a);
 }
 
 }  // namespace
@@ -640,7 +687,10 @@ cudaError_t launch_grad_t(const DistillArgs& a, bool fused, bool vec, cudaStream
 cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
   return f32 ? launch_loss_t<float, false>(a, fused, vec, s) : launch_loss_t<uint16_t, false>(a, fused, vec, s);
 }
-bool distill_step_fits(const DistillArgs& a) { return loss_smem(a.in, true) <= (size_t)kStepSmemBytes; }
+bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec) {
+  return (f32 ? loss_smem<float, true>(a.in, fused, vec) : loss_smem<uint16_t, true>(a.in, fused, vec)) <=
+         (size_t)kStepSmemBytes;
+}
 cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
   return f32 ? launch_loss_t<float, true>(a, fused, vec, s) : launch_loss_t<uint16_t, true>(a, fused, vec, s);
 }

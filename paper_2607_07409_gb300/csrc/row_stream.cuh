@@ -58,9 +58,9 @@ template <typename T>
 struct Raw8 {
   static constexpr int W = sizeof(T) / 2;
   uint4 w[W];
-  __device__ __forceinline__ void load(const T* p) {
+  __device__ __forceinline__ void load(const T* p, int half) {      // half: elements between the words
 #pragma unroll
-    for (int k = 0; k < W; ++k) w[k] = __ldcs(reinterpret_cast<const uint4*>(p) + k);
+    for (int k = 0; k < W; ++k) w[k] = __ldcs(reinterpret_cast<const uint4*>(p + k * half));
   }
   __device__ __forceinline__ void fill(float x) {
     const uint32_t b = __float_as_uint(x);         // 0 or -inf: exact in bf16
@@ -94,8 +94,9 @@ struct Raw8 {
 // operation, so that equal inputs order equally wherever they are evaluated; an
 // absent term counts as zero. FUSED = false: l = l_L as stored.
 //
-// A thread takes items of 8 columns. VEC: the row's terms lie alike against
-// 16-byte boundaries (rows of an odd vocabulary do, and lie differently from row
+// A thread takes items of 8 columns: consecutive ones of bf16 rows, two times four of
+// float32 rows, 4 kStreamThreads apart (a warp's 16-byte loads are side by side
+// either way). VEC: the row's terms lie alike against 16-byte boundaries (rows of an odd vocabulary do, and lie differently from row
 // to row): items are counted from the boundary at or before the row's start,
 // `sh` elements before it, so that whole items are vector loads and only a row's
 // first and last are not. Otherwise an item's columns are kStreamThreads apart (a
@@ -145,47 +146,67 @@ struct FusedRow {
   __device__ __forceinline__ float at(int k) const { return combine(l_at(k), s_at(k), p_at(k)); }
 };
 
+// Distance from an item's first four positions to its other four.
+template <typename T>
+constexpr int kHalf = sizeof(T) == 4 ? 4 * kStreamThreads : 4;
 // First position of item `it` of thread t in a slice that starts at k0; position i of an item.
-template <bool VEC>
+template <typename T, bool VEC>
 __device__ __forceinline__ int item_pos(int k0, int it, int t) {
-  return k0 + it * kStreamStep + (VEC ? t * 8 : t);
+  return k0 + it * kStreamStep + (VEC ? t * (sizeof(T) == 4 ? 4 : 8) : t);
 }
-template <bool VEC>
-__device__ __forceinline__ int elem_pos(int k, int i) { return VEC ? k + i : k + i * kStreamThreads; }
+template <typename T, bool VEC>
+__device__ __forceinline__ int elem_pos(int k, int i) {
+  return VEC ? k + (i < 4 ? i : kHalf<T> + i - 4) : k + i * kStreamThreads;
+}
+// Four floats of the prior, `o` past a 16-byte boundary.
+__device__ __forceinline__ void prior4(const float* p, int o, float* x) {
+  if (o == 0) {
+    const float4 u = __ldg(reinterpret_cast<const float4*>(p));
+    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+  } else if (o == 2) {
+    const float2 u = __ldg(reinterpret_cast<const float2*>(p)), v = __ldg(reinterpret_cast<const float2*>(p + 2));
+    x[0] = u.x; x[1] = u.y; x[2] = v.x; x[3] = v.y;
+  } else {
+    const float2 u = __ldg(reinterpret_cast<const float2*>(p + 1));
+    x[0] = __ldg(p); x[1] = u.x; x[2] = u.y; x[3] = __ldg(p + 3);
+  }
+}
 
 // One item's terms as loaded.
 template <typename T, bool FUSED, bool VEC>
 struct Item {
   Raw8<T> l;
   Raw8<T> s;           // FUSED only
-  int k;               // its first position; -1: past the slice
+  int k;               // its first position
+  const uint8_t* ring_prior = nullptr;   // l_P in shared memory, if it was copied there
 
   __device__ __forceinline__ void load_whole(const FusedRow<T, FUSED, VEC>& row, int pos) {
     k = pos;
     if constexpr (VEC) {
-      if (!FUSED || row.L) l.load(row.L + pos);
+      if (!FUSED || row.L) l.load(row.L + pos, kHalf<T>);
       else l.fill(0.f);
       if constexpr (FUSED) {
-        if (row.S) s.load(row.S + pos);
+        if (row.S) s.load(row.S + pos, kHalf<T>);
         else s.fill(0.f);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        l.set(i, row.l_at(elem_pos<VEC>(pos, i)));
-        if constexpr (FUSED) s.set(i, row.s_at(elem_pos<VEC>(pos, i)));
+        l.set(i, row.l_at(elem_pos<T, VEC>(pos, i)));
+        if constexpr (FUSED) s.set(i, row.s_at(elem_pos<T, VEC>(pos, i)));
       }
     }
   }
   // As far as its positions are in the row and before `stop`: -inf (l_S: 0) elsewhere.
   __device__ __forceinline__ void load(const FusedRow<T, FUSED, VEC>& row, int pos, int stop) {
-    if (VEC && pos >= row.sh && pos + 8 <= stop) return load_whole(row, pos);
+    if (VEC && pos >= row.sh && pos + kHalf<T> + 4 <= stop) return load_whole(row, pos);
     k = pos;
     l.fill(-INFINITY);
     if constexpr (FUSED) s.fill(0.f);
+    if (pos >= stop) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int q = elem_pos<VEC>(pos, i);
+      const int q = elem_pos<T, VEC>(pos, i);
       if (q >= row.sh && q < stop) {
         l.set(i, row.l_at(q));
         if constexpr (FUSED) s.set(i, row.s_at(q));
@@ -202,43 +223,26 @@ struct Item {
       return;
     }
     if constexpr (!VEC || CHECK) {
-      if (!VEC || k < row.sh || k + 8 > stop) {
+      if (!VEC || k < row.sh || k + kHalf<T> + 4 > stop) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int q = elem_pos<VEC>(k, i);
+          const int q = elem_pos<T, VEC>(k, i);
           p[i] = !CHECK || (q >= row.sh && q < stop) ? row.p_at(q) : 0.f;
         }
         return;
       }
     }
-    if constexpr (VEC) {
-      const int o = row.sh & 3;                    // the prior's own place against 16 bytes is -sh
-      const float* base = row.P + k;
-      if (o == 0) {
-        const float4 u = __ldg(reinterpret_cast<const float4*>(base));
-        const float4 v = __ldg(reinterpret_cast<const float4*>(base) + 1);
+    if constexpr (VEC && !CHECK) {
+      if (ring_prior) {
+        const float4 u = *reinterpret_cast<const float4*>(ring_prior);
+        const float4 v = *reinterpret_cast<const float4*>(ring_prior + kStreamThreads * 16);
         p[0] = u.x; p[1] = u.y; p[2] = u.z; p[3] = u.w; p[4] = v.x; p[5] = v.y; p[6] = v.z; p[7] = v.w;
         return;
       }
-      // the widest aligned loads of each place
-      if (o == 2) {
-        const float2 u = __ldg(reinterpret_cast<const float2*>(base));
-        const float4 v = __ldg(reinterpret_cast<const float4*>(base + 2));
-        const float2 w = __ldg(reinterpret_cast<const float2*>(base + 6));
-        p[0] = u.x; p[1] = u.y; p[2] = v.x; p[3] = v.y; p[4] = v.z; p[5] = v.w; p[6] = w.x; p[7] = w.y;
-      } else if (o == 1) {
-        const float u = __ldg(base);
-        const float4 v = __ldg(reinterpret_cast<const float4*>(base + 1));
-        const float2 w = __ldg(reinterpret_cast<const float2*>(base + 5));
-        const float z = __ldg(base + 7);
-        p[0] = u; p[1] = v.x; p[2] = v.y; p[3] = v.z; p[4] = v.w; p[5] = w.x; p[6] = w.y; p[7] = z;
-      } else {
-        const float u = __ldg(base);
-        const float2 v = __ldg(reinterpret_cast<const float2*>(base + 1));
-        const float4 w = __ldg(reinterpret_cast<const float4*>(base + 3));
-        const float z = __ldg(base + 7);
-        p[0] = u; p[1] = v.x; p[2] = v.y; p[3] = w.x; p[4] = w.y; p[5] = w.z; p[6] = w.w; p[7] = z;
-      }
+    }
+    if constexpr (VEC) {                           // (the prior's own place against 16 bytes is -sh)
+      prior4(row.P + k, -row.sh & 3, p);
+      prior4(row.P + k + kHalf<T>, -row.sh & 3, p + 4);
     }
   }
   // Values of the 8 positions, and the l_S and l_P in them. The products are packed
@@ -263,38 +267,64 @@ struct Item {
   }
 };
 
-// ---------------------------------------------------------------------------
-// Running softmax sums. With t = (x - m) log2(e) / T, m the largest entry so far:
-//   rest = sum 2^t without one entry that attains m (it is 1: held out, so that
-//          ln(1 + rest) keeps its digits where one entry has nearly all mass),
-//   w    = sum 2^t t over the same entries (both of one sign: the entropy
-//          ln S - ln2 w / S has no cancellation).
-// ---------------------------------------------------------------------------
-struct SoftRec {
-  float m, rest, w;
-};
-constexpr float kLowT = -1e30f;   // 2^t t is 0 from here on, -inf included
-
-__device__ __forceinline__ SoftRec softrec_init() { return SoftRec{-INFINITY, 0.f, 0.f}; }
-
-// b's sums relative to M >= b.m, its held-out entry among them unless it stays out.
-__device__ __forceinline__ void softrec_add(SoftRec& r, const SoftRec& b, float M, float c, bool stays_out) {
-  const float d = b.m == -INFINITY ? 0.f : fmaxf((b.m - M) * c, kLowT);
-  const float f = b.m == -INFINITY ? (b.rest != b.rest ? NAN : 0.f) : ex2_approx(d);
-  const float out = b.m == -INFINITY || stays_out ? 0.f : f;
-  r.rest += f * b.rest + out;
-  r.w += f * (b.w + d * b.rest) + out * d;
+// Largest of 8 values (NaN ignored).
+__device__ __forceinline__ float max8(const float (&x)[8]) {
+  return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
 }
+
+// ---------------------------------------------------------------------------
+// Running softmax sums: exponentials as 2^z, z = (x - off) c - r, c = log2(e) / T.
+// The reference is off = 0 with a whole number r near m c, m an entry met: z is
+// then one fma, exact but for its own rounding (m c itself would be rounded, a
+// common factor of 2^(|m c| 2^-24) in all of them), and a change of r scales sums by
+// a power of two. Past kMaxRef, where a whole row is masked by values such as -1e9
+// or the type's lowest, off = m and r = 0.
+// ---------------------------------------------------------------------------
+struct Ref {
+  float off, r;
+};
+__device__ __forceinline__ Ref make_ref(float m, float c) {
+  const float s = m * c;
+  return past_ref_bound(s) ? Ref{m, 0.f} : Ref{0.f, rintf(s)};
+}
+__device__ __forceinline__ float ref_z(float x, const Ref& f, float c) { return fmaf(x - f.off, c, -f.r); }
+constexpr float kLowT = -1e30f;   // 2^z z is 0 from here on, -inf included
+// What sums relative to `from` are multiplied by, as a power of two, for `to`.
+__device__ __forceinline__ float ref_shift(const Ref& from, const Ref& to, float c) {
+  return fmaxf((from.off - to.off) * c + (from.r - to.r), kLowT);
+}
+
+// m: the largest entry; rest = sum 2^z without one entry that attains m (held out, so
+// that ln S = z_m ln 2 + ln(1 + rest / 2^z_m) keeps its digits where one entry has
+// nearly all mass); w = sum 2^z z over the same.
+struct SoftRec {
+  float m;
+  Ref f;
+  float rest, w;
+};
+__device__ __forceinline__ SoftRec softrec_init() { return SoftRec{-INFINITY, Ref{0.f, 0.f}, 0.f, 0.f}; }
+
 // The records of lanes 0 .. 7 of a warp merged (all lanes converged; lane i + 8 has
 // lane i's), in every lane, in a fixed order.
 __device__ __forceinline__ SoftRec softrec_merge8(const SoftRec& b, float c) {
-  SoftRec r{warp_max(b.m), 0.f, 0.f};
-  const unsigned who = __ballot_sync(0xFFFFFFFFu, b.m == r.m);
-  softrec_add(r, b, r.m, c, (threadIdx.x & 7) == (unsigned)(__ffs(who) - 1));
+  SoftRec r;
+  r.m = warp_max(b.m);
+  const int top = __ffs(__ballot_sync(0xFFFFFFFFu, b.m == r.m)) - 1;
+  r.f.off = __shfl_sync(0xFFFFFFFFu, b.f.off, top);
+  r.f.r = __shfl_sync(0xFFFFFFFFu, b.f.r, top);
+  const bool none = b.m == -INFINITY;              // (its rest is 0, or NaN where it met one)
+  const float d = none ? 0.f : ref_shift(b.f, r.f, c), f = none ? 1.f : ex2_approx(d);
+  r.rest = f * b.rest;
+  r.w = f * (b.w + d * b.rest);
+  if (!none && (int)(threadIdx.x & 7) != top) {      // another's largest goes in
+    const float z = fmaxf(ref_z(b.m, r.f, c), kLowT), e = ex2_approx(z);
+    r.rest += e;
+    r.w += e * z;
+  }
 #pragma unroll
-  for (int d = 4; d > 0; d >>= 1) {
-    r.rest += __shfl_xor_sync(0xFFFFFFFFu, r.rest, d);
-    r.w += __shfl_xor_sync(0xFFFFFFFFu, r.w, d);
+  for (int d2 = 4; d2 > 0; d2 >>= 1) {
+    r.rest += __shfl_xor_sync(0xFFFFFFFFu, r.rest, d2);
+    r.w += __shfl_xor_sync(0xFFFFFFFFu, r.w, d2);
   }
   return r;
 }
@@ -303,62 +333,61 @@ __device__ __forceinline__ bool softrec_valid(const SoftRec& r) {
   return r.m > -INFINITY && r.m < INFINITY && r.rest >= 0.f && r.rest < INFINITY;
 }
 
-// Largest of 8 values (NaN ignored).
-__device__ __forceinline__ float max8(const float (&x)[8]) {
-  return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-}
-
-// One lane's sums under its warp's reference (the warp's largest entry so far),
-// in which the lane that holds an entry equal to it keeps that entry out. The sums
-// are pairs: even and odd elements apart.
+// One lane's sums under its warp's reference; `m` is the warp's largest entry so
+// far, and the lane that met it first keeps it out of its sums. The sums are pairs:
+// even and odd elements apart.
 struct WarpSoft {
-  float ref, off;      // the same in every lane; off = ref, or 0 while ref is -inf
+  float m;             // the same in every lane, as f
+  Ref f;
   f32x2 rest, w;
   bool holds;
   __device__ __forceinline__ void init() {
-    ref = -INFINITY;
-    off = 0.f;
+    m = -INFINITY;
+    f = Ref{0.f, 0.f};
     rest = w = 0ull;
     holds = false;
   }
-  // U items' values, all lanes converged; `vm`: the largest of the lane's.
-  template <int U>
-  __device__ __forceinline__ void push(float (&x)[U][8], float vm, float c) {
-    if (__any_sync(0xFFFFFFFFu, vm > ref)) {
-      const float top = warp_max(vm);
-      const float d = ref == -INFINITY ? 0.f : fmaxf((ref - top) * c, kLowT);
-      const float r1 = sum2(rest);
-      const float f = ref == -INFINITY ? (r1 != r1 ? NAN : 0.f) : ex2_approx(d);
-      w = pair2(f * (sum2(w) + d * r1) + (holds ? f * d : 0.f), 0.f);
-      rest = pair2(f * r1 + (holds ? f : 0.f), 0.f);
-      ref = off = top;
-      const unsigned who = __ballot_sync(0xFFFFFFFFu, vm == top);
-      holds = (int)(threadIdx.x & 31) == __ffs(who) - 1;
-      bool out = holds;
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (out && x[u][i] == top) {
-            out = false;
-            x[u][i] = -INFINITY;
-          }
+  // A new largest entry `top` > m (all lanes converged): the one held so far goes
+  // into the sums; whether this lane holds the new one (`vm`: its largest).
+  __device__ __forceinline__ bool raise(float top, float vm, float c) {
+    float r1 = sum2(rest), w1 = sum2(w);
+    if (holds) {
+      const float z = ref_z(m, f, c), e = ex2_approx(z);
+      r1 += e;
+      w1 += e * z;
     }
-    const f32x2 no = both2(-off), c2 = both2(c);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        float t0, t1;
-        split2(mul2(add2(pair2(x[u][i], x[u][i + 1]), no), c2), t0, t1);
-        const f32x2 e = pair2(ex2_approx(t0), ex2_approx(t1));
-        rest = add2(rest, e);
-        w = fma2(e, pair2(fmaxf(t0, kLowT), fmaxf(t1, kLowT)), w);
+    if (m == -INFINITY || past_ref_bound(top * c) || f.off != 0.f || fmaf(top, c, -f.r) > 1.f) {
+      const Ref to = make_ref(top, c);
+      if (m > -INFINITY) {
+        const float d = ref_shift(f, to, c), s = ex2_approx(d);
+        w1 = s * (w1 + d * r1);
+        r1 *= s;
       }
+      f = to;
+    }
+    rest = pair2(r1, 0.f);
+    w = pair2(w1, 0.f);
+    m = top;
+    const unsigned who = __ballot_sync(0xFFFFFFFFu, vm == top);
+    return holds = (int)(threadIdx.x & 31) == __ffs(who) - 1;
+  }
+  // CLAMPED: no x is so low that 2^z z is not a number (x relative to f.off).
+  template <bool CLAMPED>
+  __device__ __forceinline__ void add(const float (&x)[8], float c) {
+    const f32x2 c2 = both2(c), nr = both2(-f.r);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const f32x2 z = fma2(pair2(x[i], x[i + 1]), c2, nr);
+      float z0, z1;
+      split2(z, z0, z1);
+      const f32x2 e = pair2(ex2_approx(z0), ex2_approx(z1));
+      rest = add2(rest, e);
+      w = fma2(e, CLAMPED ? z : pair2(fmaxf(z0, kLowT), fmaxf(z1, kLowT)), w);
+    }
   }
   // The warp's record (all lanes converged), in every lane.
   __device__ __forceinline__ SoftRec record() const {
-    SoftRec r{ref, sum2(rest), sum2(w)};
+    SoftRec r{m, f, sum2(rest), sum2(w)};
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
       r.rest += __shfl_xor_sync(0xFFFFFFFFu, r.rest, d);
@@ -368,34 +397,160 @@ struct WarpSoft {
   }
 };
 
+// 16 bytes from global to shared memory without a register between.
+__device__ __forceinline__ void copy16(uint32_t smem, const void* gmem) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
+}
+__device__ __forceinline__ void copy16_l1(uint32_t smem, const void* gmem) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Shared memory that whole items are copied to ahead of their use, in 16-byte pieces:
+// 8 logits are W of them, a fused item l_L's, l_S's and two of l_P. A piece belongs
+// to one thread, which copies it, waits for it and reads it: no barrier. A warp's
+// copies of a piece are 512 bytes side by side.
+//
+// A ring of D groups of U items; with R > 0 (U = 1) the first two pieces of every
+// item have a place of their own that stays (32 bytes: the item's 8 values as
+// float32 later), copied R items ahead, and the ring has the others.
+template <typename T, bool FUSED, int U_, int D_, int R_ = 0>
+struct Copies {
+  static constexpr int U = U_, D = D_, R = R_;
+  static constexpr int W = Raw8<T>::W;
+  static constexpr bool kPrior = FUSED && !(R > 0 && W == 2);    // l_P too (else: loaded where it is used)
+  static constexpr int kPieces = FUSED ? 2 * W + (kPrior ? 2 : 0) : W;
+  static constexpr int kStay = R > 0 ? 2 : 0;
+  static constexpr int kRing = kPieces > kStay ? kPieces - kStay : 0;
+  static constexpr int kPiece = 16 * kStreamThreads;             // one piece of all threads
+  static constexpr int kRingBytes = D * U * kRing * kPiece;
+  static constexpr int kItemBytes = kStay * kPiece;              // per item that stays
+};
+
 // The items of a thread in positions k0 .. k1 - 1 of a row (a slice, at most the
-// row's end), U at a time: f(items, checked) with checked = std::false_type where
-// all of them are whole for every thread. U loads are in flight at once; what U
-// leaves over, and a row's ends, go one by one.
-template <int U, typename T, bool FUSED, bool VEC, typename F>
-__device__ __forceinline__ void stream_items(const FusedRow<T, FUSED, VEC>& row, int k0, int k1, F&& f) {
-  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
-  const int whole = (k1 - k0) / kStreamStep;
-  int it = 0;
-  if (k0 < row.sh && items > 0) {                  // a row's first item may not be whole
-    Item<T, FUSED, VEC> v[1];
-    v[0].load(row, item_pos<VEC>(k0, 0, threadIdx.x), k1);
-    f(v, std::true_type{});
-    it = 1;
+// row's end): f(items, checked, call), checked = std::false_type where all of them are
+// whole for every thread, `call` counting the calls. With VEC whole items come U at
+// a time, D - 1 such groups ahead in flight; what U leaves over, and a row's ends, go
+// one by one. (`ring`, `stay`: the thread block's.)
+struct StreamPlan {
+  int head;            // calls of the row's first item, which may not be whole: 0 or 1
+  int groups;          // calls of U whole items
+  int items;           // of a thread
+  template <int U>
+  __device__ __forceinline__ static StreamPlan of(int k0, int k1, int sh, bool vec) {
+    StreamPlan p;
+    p.items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
+    p.head = p.items > 0 && k0 < sh;
+    p.groups = vec ? max(0, (k1 - k0) / kStreamStep - p.head) / U : 0;
+    return p;
   }
-  for (; it + U <= whole; it += U) {
-    Item<T, FUSED, VEC> v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u].load_whole(row, item_pos<VEC>(k0, it + u, threadIdx.x));
-    f(v, std::false_type{});
+  template <int U>
+  __device__ __forceinline__ int calls() const { return head + groups + items - head - groups * U; }
+  // First item of a call.
+  template <int U>
+  __device__ __forceinline__ int first(int call) const {
+    const int g = call - head;
+    return g <= 0 ? call : g < groups ? head + g * U : head + groups * U + (g - groups);
   }
-  for (; it < items; ++it) {
-    const int pos = item_pos<VEC>(k0, it, threadIdx.x);
-    if (!__any_sync(0xFFFFFFFFu, pos < k1)) break;
+};
+template <typename Cp, typename T, bool FUSED, bool VEC, typename F>
+__device__ __forceinline__ void stream_items(const FusedRow<T, FUSED, VEC>& row, int k0, int k1, uint8_t* ring,
+                                             uint8_t* stay, F&& f) {
+  constexpr int U = Cp::U, D = Cp::D, R = Cp::R, W = Cp::W, PC = Cp::kPiece;
+  const StreamPlan p = StreamPlan::of<U>(k0, k1, row.sh, VEC);
+  int it = 0, call = 0;
+  auto one = [&]() {
+    const int pos = item_pos<T, VEC>(k0, it, threadIdx.x);
     Item<T, FUSED, VEC> v[1];
     v[0].load(row, pos, k1);
-    f(v, std::true_type{});
+    f(v, std::true_type{}, call);
+    ++it;
+    ++call;
+  };
+  if constexpr (VEC) {
+    const bool prior = Cp::kPrior && row.P && (row.sh & 3) == 0;   // (its own place against 16 bytes is -sh)
+    // Place of piece k of item i of the groups, which is in place `q` of the ring.
+    auto place = [&](uint8_t* rg, uint8_t* st, int k, int i, int q) -> uint8_t* {
+      return k < Cp::kStay ? st + (size_t)(p.head + i) * Cp::kItemBytes + k * PC
+                           : rg + (q * Cp::kRing + k - Cp::kStay) * PC;
+    };
+    ring += threadIdx.x * 16;
+    stay += threadIdx.x * 16;
+    // pieces [from, to) of item i
+    auto copy = [&](int i, int q, int from, int to) {
+      const int at = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
+#pragma unroll
+      for (int k = 0; k < Cp::kPieces; ++k) {
+        if (k < from || k >= to) continue;
+        const uint32_t dst = smem_u32(place(ring, stay, k, i, q));
+        if (k < W) {
+          if (!FUSED || row.L) copy16(dst, row.L + at + k * kHalf<T>);
+        } else if (k < 2 * W) {
+          if (row.S) copy16(dst, row.S + at + (k - W) * kHalf<T>);
+        } else if (prior) {
+          copy16_l1(dst, row.P + at + (k - 2 * W) * kHalf<T>);   // (bf16: a 32-byte sector in two halves)
+        }
+      }
+    };
+    // What is copied when call g begins: group g + D - 1 (its ring pieces), and item
+    // g + R - 1 (those that stay); one commit a call, empty at the end, so that at
+    // most D - 1 later ones are in flight when group g is waited for.
+    int slot_in = 0;
+    auto issue = [&](int g) {
+      if (g < p.groups) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) copy(g * U + u, slot_in * U + u, Cp::kStay, Cp::kPieces);
+        slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
+      }
+    };
+    auto issue_stay = [&](int i) {
+      if (R > 0 && i < p.groups) copy(i, 0, 0, Cp::kStay);
+    };
+#pragma unroll 1
+    for (int i = 0; i < R - 1; ++i) issue_stay(i);
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d) {
+      issue(d);
+      copies_commit();
+    }
+    if (p.head) one();
+    int slot = 0;
+#pragma unroll 1
+    for (int g = 0; g < p.groups; ++g) {
+      issue(g + D - 1);
+      issue_stay(g + R - 1);
+      copies_commit();
+      copies_wait<D - 1>();
+      Item<T, FUSED, VEC> v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = g * U + u, q = slot * U + u;
+        v[u].k = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          if (!FUSED || row.L) v[u].l.w[k] = *reinterpret_cast<const uint4*>(place(ring, stay, k, i, q));
+          if constexpr (FUSED) {
+            if (row.S) v[u].s.w[k] = *reinterpret_cast<const uint4*>(place(ring, stay, W + k, i, q));
+          }
+        }
+        if (FUSED && !row.L) v[u].l.fill(0.f);
+        if constexpr (FUSED) {
+          if (!row.S) v[u].s.fill(0.f);
+        }
+        v[u].ring_prior = prior ? place(ring, stay, 2 * W, i, q) : nullptr;
+      }
+      f(v, std::false_type{}, call);
+      it += U;
+      ++call;
+      slot = slot + 1 == D ? 0 : slot + 1;
+    }
+    copies_wait<0>();
   }
+  while (it < p.items) one();
 }
 
 // The two halves of a cluster barrier (all threads of all its CTAs).

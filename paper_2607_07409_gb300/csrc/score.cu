@@ -5,10 +5,10 @@
 //   H       = ln S - (1 / S) sum_v exp((l_v - m) / T) (l_v - m) / T
 //
 // What bounds it: the read of the logits. The alternatives cost no second read of
-// the row: every thread keeps the largest of its own entries, the K-th largest of
-// those is at most the K-th largest entry of the slice, and only the items of the
-// few threads above that threshold are read again (out of L2) for their entries.
-#include <climits>
+// the row: every thread keeps the largest entry of each of its blocks of a few
+// items; the K-th largest thread maximum is at most the K-th largest entry of the
+// slice, and only the blocks that reach it are read again for their entries.
+#include <cuda_bf16.h>
 
 #include "row_stream.cuh"
 
@@ -29,16 +29,20 @@ __device__ __forceinline__ unsigned long long entry_key(float x, int col) {
   return ((unsigned long long)order_u32(x) << 32) | (0xFFFFFFFFu - (unsigned)col);
 }
 
-constexpr int kCandidates = kStreamWarps * 256 + 4 * kMaxTopK;   // one round of rescanned items, and what was kept
+constexpr int kJobs = 2048;          // blocks read again
+constexpr int kCandidates = 2048;    // their entries that are kept
+constexpr int kSlots = 20;           // block maxima per thread: 20 KB of float
 
-struct ScoreShared {
+// What the selection needs once the ring is done with (in its place).
+struct SelectShared {
   unsigned long long cand[kCandidates];
+  int jobs[kJobs];
+};
+struct ScoreShared {
   unsigned long long best[kMaxTopK];       // this CTA's entries in order, 0 where there are none
-  unsigned long long slices[kMaxCluster * kMaxTopK];   // first CTA: all slices' entries
-  int groups[kStreamThreads];
   SoftRec warps[kStreamWarps];
   SoftRec ctas[kMaxCluster];
-  int ncand, ngroups;
+  int ncand, njobs;
 };
 
 // The K largest of cand[0 .. n) to best[] in order (all threads): a warp counts
@@ -59,34 +63,38 @@ __device__ void sort_best(ScoreShared& sh, const unsigned long long* cand, int n
 
 // The entries of an item that reach `floor_key`, into cand[] as far as it has room.
 template <typename T, bool FUSED, bool VEC>
-__device__ __forceinline__ void keep_entries(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, int pos, int k1,
-                                             unsigned long long floor_key) {
+__device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel, const FusedRow<T, FUSED, VEC>& row,
+                                             int pos, int k1, unsigned long long floor_key) {
   Item<T, FUSED, VEC> v;
   v.load(row, pos, k1);
   float x[8], s[8], p[8];
   v.template values<true>(row, k1, x, s, p);
   const float least = from_order_u32((unsigned)(floor_key >> 32));
-  if (!(max8(x) >= least)) return;                 // most items: nothing
+  if (!(max8(x) >= least)) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (!(x[i] >= least && x[i] > -INFINITY)) continue;
-    const unsigned long long e = entry_key(x[i], elem_pos<VEC>(pos, i) - row.sh);
+    const unsigned long long e = entry_key(x[i], elem_pos<T, VEC>(pos, i) - row.sh);
     if (e < floor_key) continue;
     const int at = atomicAdd(&sh.ncand, 1);
-    if (at < kCandidates) sh.cand[at] = e;
+    if (at < kCandidates) sel.cand[at] = e;
   }
 }
 
 // This CTA's K largest entries of its slice into sh.best. `top`: the largest
-// entry of the calling thread.
-template <typename T, bool FUSED, bool VEC>
-__device__ void slice_top(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, int k0, int k1, int K, float top) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // About the K-th largest thread maximum, from its highest bit down; 0 where
+// entry of the calling thread; bmax: [slot][thread] the largest of a thread's calls
+// slot << shift .. of the stream.
+template <int U, typename T, bool FUSED, bool VEC>
+__device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax, int shift,
+                          const FusedRow<T, FUSED, VEC>& row, int k0, int k1, int K, float top) {
+  const int tid = threadIdx.x;
+  const StreamPlan p = StreamPlan::of<U>(k0, k1, row.sh, VEC);
+  const int calls = p.template calls<U>(), slots = (calls + (1 << shift) - 1) >> shift;
+  // About the K-th largest thread maximum, from its highest bit down; -inf where
   // fewer than K threads have an entry.
   const unsigned key = top > -INFINITY ? order_u32(top) : 0u;
   unsigned tau = 0u;
-  if (tid == 0) sh.ncand = sh.ngroups = 0;
+  if (tid == 0) sh.ncand = sh.njobs = 0;
   if (__syncthreads_count(key > 0u) >= K) {
     for (int bit = 31; bit >= 0; --bit) {
       const unsigned t = tau | (1u << bit);
@@ -94,45 +102,84 @@ __device__ void slice_top(ScoreShared& sh, const FusedRow<T, FUSED, VEC>& row, i
       if (n >= K) tau = t;
       if (n >= K && n <= K + 8) break;
     }
+  } else {
+    tau = order_u32(-INFINITY);
   }
-  if (key > 0u && key >= tau) sh.groups[atomicAdd(&sh.ngroups, 1)] = tid;
-  __syncthreads();
-  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;      // per thread
-  const int parts = (items + 31) / 32;                              // a warp's rounds for one thread's items
-  const int jobs = sh.ngroups * parts;
-  if (tau == 0u) tau = order_u32(-INFINITY);
+  const float least = from_order_u32(tau);
   unsigned long long floor_key = (unsigned long long)tau << 32;     // what an entry has to reach
-  for (int j = warp; j < jobs; j += kStreamWarps) {
-    const int it = (j % parts) * 32 + lane;
-    if (it < items) keep_entries(sh, row, item_pos<VEC>(k0, it, sh.groups[j / parts]), k1, floor_key);
+  if (top >= least && top > -INFINITY) {
+    for (int b = 0; b < slots; ++b)
+      if (bmax[b * kStreamThreads + tid] >= least) {
+        const int at = atomicAdd(&sh.njobs, 1);
+        if (at < kJobs) sel.jobs[at] = b * kStreamThreads + tid;
+      }
   }
   __syncthreads();
-  if (sh.ncand > kCandidates) {
-    // more entries than there is room for: a round of items at a time, the best
-    // of them kept as soon as the next round might not fit
+  if (sh.njobs <= kJobs) {
+    // a lane per item of a job
+    const int per = U << shift, n = sh.njobs * per;
+    for (int i = tid; i < n; i += kStreamThreads) {
+      const int job = sel.jobs[i / per], o = i % per;
+      const int call0 = (job / kStreamThreads) << shift;
+      const int it = p.template first<U>(call0) + o;
+      const int end = p.template first<U>(min(call0 + (1 << shift), calls));
+      if (it >= end || it >= p.items) continue;
+      keep_entries(sh, sel, row, item_pos<T, VEC>(k0, it, job % kStreamThreads), k1, floor_key);
+    }
+  }
+  __syncthreads();
+  if (sh.njobs > kJobs || sh.ncand > kCandidates) {
+    // more than there is room for: the slice again, 128 items at a time, the best of
+    // them kept as soon as the next might not fit
     __syncthreads();
     if (tid == 0) sh.ncand = 0;
     __syncthreads();
-    for (int j0 = 0; j0 < jobs; j0 += kStreamWarps) {
+    for (int j = 0; j < 2 * p.items; ++j) {
       const int n = sh.ncand;
       __syncthreads();
-      if (n > kCandidates - kStreamWarps * 256) {
-        sort_best(sh, sh.cand, n, K);
-        for (int k = tid; k < K; k += kStreamThreads) sh.cand[k] = sh.best[k];
+      if (n > kCandidates - 128 * 8) {
+        sort_best(sh, sel.cand, n, K);
+        for (int k = tid; k < K; k += kStreamThreads) sel.cand[k] = sh.best[k];
         floor_key = sh.best[K - 1];                                 // n > K: there are K
         if (tid == 0) sh.ncand = K;
         __syncthreads();
       }
-      const int j = j0 + warp, it = (j % parts) * 32 + lane;
-      if (j < jobs && it < items) keep_entries(sh, row, item_pos<VEC>(k0, it, sh.groups[j / parts]), k1, floor_key);
+      if ((tid >> 7) == (j & 1)) keep_entries(sh, sel, row, item_pos<T, VEC>(k0, j >> 1, tid), k1, floor_key);
       __syncthreads();
     }
   }
-  sort_best(sh, sh.cand, sh.ncand, K);
+  sort_best(sh, sel.cand, sh.ncand, K);
+}
+
+// Packed maximum of 8 bf16 (NaN ignored), and every one raised to at least `low`
+// (NaN stays).
+__device__ __forceinline__ float max8_bf16(const uint4& w) {
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
+  const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ void raise8_bf16(uint4& w, __nv_bfloat162 low) {
+  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __hmax2_nan(h[i], low);
+}
+
+// Copies ahead: 32 KB of plain rows (four CTAs on an SM), 48 KB of two rows and the
+// prior (three).
+template <typename T, bool FUSED>
+using ScoreCopies = Copies<T, FUSED, sizeof(T) == 2 && !FUSED ? 2 : 1, FUSED ? (sizeof(T) == 2 ? 3 : 2) : 4>;
+
+// Dynamic shared memory: the ring (later SelectShared), the block maxima, and for a
+// cluster the entries of all slices.
+template <typename T, bool FUSED, bool VEC>
+constexpr size_t ring_bytes() {
+  const size_t ring = VEC ? ScoreCopies<T, FUSED>::kRingBytes : 0;
+  return ring > sizeof(SelectShared) ? ring : sizeof(SelectShared);
 }
 
 template <typename T, bool FUSED, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, 4) k_score_rows(ScoreArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, FUSED ? 3 : 4) k_score_rows(ScoreArgs a) {
+  extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ ScoreShared sh;
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
@@ -164,37 +211,104 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_score_rows(ScoreArgs a) {
   const long long first = (long long)rank * a.in.slice_cols;
   const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
 
-  // items in flight per thread: 64 bytes of bf16 rows, 64 to 128 of the others
-  constexpr int U = sizeof(T) == 2 ? (FUSED ? 2 : 4) : (FUSED ? 1 : 2);
+  using Cp = ScoreCopies<T, FUSED>;
+  constexpr int U = Cp::U;
+  float* bmax = reinterpret_cast<float*>(dyn + ring_bytes<T, FUSED, VEC>());
+  unsigned long long* slices = reinterpret_cast<unsigned long long*>(bmax + (K > 0 ? kSlots * kStreamThreads : 0));
+  int shift = 0;                   // calls per block maximum: 1 << shift
+  while (((StreamPlan::of<U>(k0, k1, row.sh, VEC).template calls<U>() - 1) >> shift) >= kSlots) ++shift;
+
   WarpSoft st;
   st.init();
-  float top = -INFINITY;
-  stream_items<U>(row, k0, k1, [&](auto& v, auto checked) {
+  float top = -INFINITY, block = -INFINITY;
+  const __nv_bfloat162 low2 = __float2bfloat162_rn(a.low);
+  stream_items<Cp>(row, k0, k1, dyn, nullptr, [&](auto& v, auto checked, int call) {
     constexpr int N = sizeof(v) / sizeof(v[0]);
-    float x[N][8], s[8], p[8], vm = -INFINITY;
+    float vm = -INFINITY;
+    if constexpr (sizeof(T) == 2 && !FUSED) {
+      // bf16 as stored: the maximum and the clamp of masked entries on pairs
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      v[u].template values<decltype(checked)::value>(row, k1, x[u], s, p);
-      vm = fmaxf(vm, max8(x[u]));
+      for (int u = 0; u < N; ++u) vm = fmaxf(vm, max8_bf16(v[u].l.w[0]));
+      if (__any_sync(0xFFFFFFFFu, vm > st.m)) {
+        const float nt = warp_max(vm);
+        bool out = st.raise(nt, vm, c);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          float x[8];
+          v[u].l.unpack(x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (out && x[i] == nt) {
+              out = false;
+              v[u].l.set(i, -INFINITY);
+            }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        float x[8];
+        if (st.f.off == 0.f) {
+          raise8_bf16(v[u].l.w[0], low2);
+          v[u].l.unpack(x);
+        } else {                   // all so far masked by huge values: their differences
+          v[u].l.unpack(x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[i] -= st.f.off;
+            if (x[i] < a.low) x[i] = a.low;
+          }
+        }
+        st.template add<true>(x, c);
+      }
+    } else {
+      float x[N][8], s[8], p[8];
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        v[u].template values<decltype(checked)::value>(row, k1, x[u], s, p);
+        vm = fmaxf(vm, max8(x[u]));
+      }
+      if (__any_sync(0xFFFFFFFFu, vm > st.m)) {
+        const float nt = warp_max(vm);
+        bool out = st.raise(nt, vm, c);
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (out && x[u][i] == nt) {
+              out = false;
+              x[u][i] = -INFINITY;
+            }
+      }
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        if (st.f.off != 0.f) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[u][i] -= st.f.off;
+        }
+        st.template add<false>(x[u], c);
+      }
     }
-    top = fmaxf(top, vm);
-    st.push(x, vm, c);
+    if (K > 0) {
+      top = fmaxf(top, vm);
+      block = (call & ((1 << shift) - 1)) == 0 ? vm : fmaxf(block, vm);
+      bmax[(call >> shift) * kStreamThreads + tid] = block;
+    }
   });
   const SoftRec wr = st.record();
   if (lane == 0) sh.warps[warp] = wr;
   __syncthreads();
   const SoftRec cta = softrec_merge8(sh.warps[lane & 7], c);
 
-  if (K > 0) slice_top(sh, row, k0, k1, K, top);
+  if (K > 0) slice_top<U>(sh, *reinterpret_cast<SelectShared*>(dyn), bmax, shift, row, k0, k1, K, top);
   SoftRec all = cta;
   if (C > 1) {
     cluster_wait();                // every CTA of the cluster runs before its shared memory is written
-    if (tid < 3) {
-      const float v = tid == 0 ? cta.m : tid == 1 ? cta.rest : cta.w;
+    if (tid < 5) {
+      const float v = tid == 0 ? cta.m : tid == 1 ? cta.f.off : tid == 2 ? cta.f.r : tid == 3 ? cta.rest : cta.w;
       st_cluster_f32(cluster_map(smem_u32(&sh.ctas[rank]), 0) + 4 * tid, v);
     }
     if (K > 0) {
-      const uint32_t to = cluster_map(smem_u32(&sh.slices[(size_t)rank * K]), 0);
+      const uint32_t to = cluster_map(smem_u32(slices + (size_t)rank * K), 0);
       for (int k = tid; k < K; k += kStreamThreads) {
         const unsigned long long e = sh.best[k];
         st_cluster_f32(to + 8 * k, __uint_as_float((unsigned)e));
@@ -205,15 +319,16 @@ __global__ void __launch_bounds__(kStreamThreads, 4) k_score_rows(ScoreArgs a) {
     if (rank != 0) return;
     cluster_wait();
     all = softrec_merge8((lane & 7) < C ? sh.ctas[lane & 7] : softrec_init(), c);
-    if (K > 0) sort_best(sh, sh.slices, C * K, K);
+    if (K > 0) sort_best(sh, slices, C * K, K);
   }
   const bool ok = softrec_valid(all);
-  const float ln_s = log1pf(all.rest), inv_t = a.in.inv_t;
+  const float z_m = ref_z(all.m, all.f, c), e_m = ex2_approx(z_m);
+  const float ln_s = log1pf(all.rest / e_m), inv_t = a.in.inv_t;
   if (tid == 0) {
     if (!ok) raise_status(a.status, DELS_STATUS_NONFINITE);
     if (a.tokens && !tok_ok) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
     if (a.out_lp) a.out_lp[r] = ok && tok_ok ? (x_tok - all.m) * inv_t - ln_s : NAN;
-    if (a.out_entropy) a.out_entropy[r] = ok ? ln_s - kLn2 * (all.w / (1.f + all.rest)) : NAN;
+    if (a.out_entropy) a.out_entropy[r] = ok ? ln_s - kLn2 * ((all.w - z_m * all.rest) / (e_m + all.rest)) : NAN;
   }
   for (int k = tid; k < K; k += kStreamThreads) {
     const unsigned long long e = sh.best[k];
@@ -228,7 +343,13 @@ cudaError_t launch_score_t(const ScoreArgs& a, bool fused, bool vec, cudaStream_
   const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
   auto k = fused ? (vec ? k_score_rows<T, true, true> : k_score_rows<T, true, false>)
                  : (vec ? k_score_rows<T, false, true> : k_score_rows<T, false, false>);
-  return launch_pdl_cluster(k, grid, block, 0, s, a.in.cluster, a);
+  const size_t ring = fused ? (vec ? ring_bytes<T, true, true>() : ring_bytes<T, true, false>())
+                            : (vec ? ring_bytes<T, false, true>() : ring_bytes<T, false, false>());
+  const size_t bytes = ring + (a.top_k > 0 ? (size_t)kSlots * kStreamThreads * 4 : 0) +
+                       (a.in.cluster > 1 ? (size_t)a.in.cluster * a.top_k * 8 : 0);
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
+  if (e != cudaSuccess) return e;
+  return launch_pdl_cluster(k, grid, block, bytes, s, a.in.cluster, a);
 }
 
 }  // namespace
