@@ -38,37 +38,50 @@ struct TailRec {
 struct ListRec {
   float m, rest;
 };
-__device__ __forceinline__ TailRec tail_init() { return TailRec{-INFINITY, Ref{0.f, 0.f}, 0.f, 0.f, 0.f}; }
-// The records of lanes 0 .. 7 (i + 8: the same; all lanes converged) merged into
+// What a warp has of a row.
+struct __align__(16) WarpRec {
+  TailRec t;
+  ListRec l;
+};
+static_assert(sizeof(WarpRec) == 32, "two 16-byte words");
+
+// `n` records (at most 64) merged by a warp (all lanes converged), the result in
 // every lane, in a fixed order.
-__device__ __forceinline__ TailRec tail_merge8(const TailRec& b, float c) {
-  TailRec r;
-  r.m = warp_max(b.m);
-  const int top = __ffs(__ballot_sync(0xFFFFFFFFu, b.m == r.m)) - 1;
-  r.f.off = __shfl_sync(0xFFFFFFFFu, b.f.off, top);
-  r.f.r = __shfl_sync(0xFFFFFFFFu, b.f.r, top);
-  const float f = b.m == -INFINITY ? 1.f : ex2_approx(ref_shift(b.f, r.f, c));   // (none: 0, or NaN, stays)
-  r.sum = f * b.sum;
-  r.s = f * b.s;
-  r.p = f * b.p;
+__device__ __forceinline__ void merge_records(const WarpRec* recs, int n, float c, TailRec& t, ListRec& l) {
+  const int lane = threadIdx.x & 31;
+  const WarpRec none{TailRec{-INFINITY, Ref{0.f, 0.f}, 0.f, 0.f, 0.f}, ListRec{-INFINITY, 0.f}};
+  const WarpRec a = lane < n ? recs[lane] : none;
+  WarpRec b = none;
+  if (n > 32) b = lane + 32 < n ? recs[lane + 32] : none;
+  // not listed: the reference of the largest
+  const bool second = b.t.m > a.t.m;
+  const float m = second ? b.t.m : a.t.m;
+  const Ref f = second ? b.t.f : a.t.f;
+  t.m = warp_max(m);
+  const int who = __ffs(__ballot_sync(0xFFFFFFFFu, m == t.m)) - 1;
+  t.f.off = __shfl_sync(0xFFFFFFFFu, f.off, who);
+  t.f.r = __shfl_sync(0xFFFFFFFFu, f.r, who);
+  const float ka = a.t.m == -INFINITY ? 1.f : ex2_approx(ref_shift(a.t.f, t.f, c));   // (none: 0, or NaN, stays)
+  const float kb = b.t.m == -INFINITY ? 1.f : ex2_approx(ref_shift(b.t.f, t.f, c));
+  t.sum = ka * a.t.sum + kb * b.t.sum;
+  t.s = ka * a.t.s + kb * b.t.s;
+  t.p = ka * a.t.p + kb * b.t.p;
+  // listed: one entry of the largest value stays out
+  l.m = warp_max(fmaxf(a.l.m, b.l.m));
+  const bool has = l.m > -INFINITY;
+  const unsigned at_a = __ballot_sync(0xFFFFFFFFu, a.l.m == l.m), at_b = __ballot_sync(0xFFFFFFFFu, b.l.m == l.m);
+  const bool out_a = lane == __ffs(at_a) - 1, out_b = at_a == 0u && lane == __ffs(at_b) - 1;
+  const float la = a.l.m == -INFINITY ? 0.f : ex2_approx((a.l.m - l.m) * c);
+  const float lb = b.l.m == -INFINITY ? 0.f : ex2_approx((b.l.m - l.m) * c);
+  l.rest = (a.l.m == -INFINITY ? a.l.rest : la * a.l.rest) + (b.l.m == -INFINITY ? b.l.rest : lb * b.l.rest);
+  if (has) l.rest += (out_a ? 0.f : la) + (out_b ? 0.f : lb);
 #pragma unroll
-  for (int d = 4; d > 0; d >>= 1) {
-    r.sum += __shfl_xor_sync(0xFFFFFFFFu, r.sum, d);
-    r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, d);
-    r.p += __shfl_xor_sync(0xFFFFFFFFu, r.p, d);
+  for (int d = 16; d > 0; d >>= 1) {
+    t.sum += __shfl_xor_sync(0xFFFFFFFFu, t.sum, d);
+    t.s += __shfl_xor_sync(0xFFFFFFFFu, t.s, d);
+    t.p += __shfl_xor_sync(0xFFFFFFFFu, t.p, d);
+    l.rest += __shfl_xor_sync(0xFFFFFFFFu, l.rest, d);
   }
-  return r;
-}
-__device__ __forceinline__ ListRec list_merge8(const ListRec& b, float c) {
-  ListRec r;
-  r.m = warp_max(b.m);
-  const unsigned who = __ballot_sync(0xFFFFFFFFu, b.m == r.m);
-  const float f = b.m == -INFINITY ? (b.rest != b.rest ? NAN : 0.f) : ex2_approx((b.m - r.m) * c);
-  const bool out = b.m == -INFINITY || (threadIdx.x & 7) == (unsigned)(__ffs(who) - 1);
-  r.rest = f * b.rest + (out ? 0.f : f);
-#pragma unroll
-  for (int d = 4; d > 0; d >>= 1) r.rest += __shfl_xor_sync(0xFFFFFFFFu, r.rest, d);
-  return r;
 }
 
 // One lane's sums over the columns that are not listed. The reference of a warp's
@@ -87,9 +100,13 @@ struct WarpTail {
     f = Ref{0.f, 0.f};
     sum = s = p = 0ull;
   }
-  // One item's values, all lanes converged.
-  __device__ __forceinline__ void push(float (&x)[8], const float (&sv)[8], const float (&pv)[8], float c, float p_ref) {
-    const float vm = max8(x);
+  // N items' values, all lanes converged.
+  template <int N>
+  __device__ __forceinline__ void push(float (&x)[N][8], const float (&sv)[N][8], const float (&pv)[N][8], float c,
+                                       float p_ref) {
+    float vm = max8(x[0]);
+#pragma unroll
+    for (int u = 1; u < N; ++u) vm = fmaxf(vm, max8(x[u]));
     if (__any_sync(0xFFFFFFFFu, vm > limit)) {
       const float top = warp_max(vm);
       const Ref to = make_ref(top, c);
@@ -105,20 +122,24 @@ struct WarpTail {
     }
     if (f.off != 0.f) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] -= f.off;
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[u][i] -= f.off;
     }
     const f32x2 c2 = both2(c), nr = both2(-f.r), np = both2(-p_ref);
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      float z0, z1;
-      split2(fma2(pair2(x[i], x[i + 1]), c2, nr), z0, z1);
-      const f32x2 e = pair2(ex2_approx(z0), ex2_approx(z1));
-      sum = add2(sum, e);
-      if constexpr (FUSED) {
-        s = fma2(e, pair2(fmaxf(sv[i], -FLT_MAX), fmaxf(sv[i + 1], -FLT_MAX)), s);     // a masked entry: 0
-        p = fma2(e, add2(pair2(pv[i], pv[i + 1]), np), p);
+    for (int i = 0; i < 8; i += 2)
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        float z0, z1;
+        split2(fma2(pair2(x[u][i], x[u][i + 1]), c2, nr), z0, z1);
+        const f32x2 e = pair2(ex2_approx(z0), ex2_approx(z1));
+        sum = add2(sum, e);
+        if constexpr (FUSED) {
+          s = fma2(e, pair2(fmaxf(sv[u][i], -FLT_MAX), fmaxf(sv[u][i + 1], -FLT_MAX)), s);   // a masked entry: 0
+          p = fma2(e, add2(pair2(pv[u][i], pv[u][i + 1]), np), p);
+        }
       }
-    }
   }
   __device__ __forceinline__ TailRec record() const {
     TailRec r{m, f, sum2(sum), sum2(s), sum2(p)};
@@ -137,9 +158,9 @@ struct WarpTail {
 // Copies ahead of the loss and gradient kernels, and of the step's, whose items stay
 // (beside 10 items of 8 KB its ring is to leave room for a second CTA on the SM).
 template <typename T, bool FUSED>
-using LossCopies = Copies<T, FUSED, 1, FUSED ? (sizeof(T) == 2 ? 3 : 2) : 4>;
+using LossCopies = Copies<T, FUSED, sizeof(T) == 2 && !FUSED ? 2 : 1, FUSED && sizeof(T) == 4 ? 3 : 4>;
 template <typename T, bool FUSED>
-using StepCopies = Copies<T, FUSED, 1, 3, 8>;
+using StepCopies = std::conditional_t<sizeof(T) == 2, Copies<T, FUSED, 2, 4, 4>, Copies<T, FUSED, 1, FUSED ? 3 : 8, 8>>;
 template <typename T, bool FUSED, bool GRAD>
 using RowCopies = std::conditional_t<GRAD, StepCopies<T, FUSED>, LossCopies<T, FUSED>>;
 
@@ -194,11 +215,9 @@ struct Teacher {
 };
 
 struct LossShared {
-  TailRec warps[kStreamWarps];
-  ListRec listed[kStreamWarps];
-  float ctas[kMaxCluster][8];       // TailRec, ListRec
-  float sums[kStreamWarps][4];
-  float last[kMaxCluster][4];
+  WarpRec recs[kMaxCluster * kStreamWarps];        // every warp's of the cluster
+  float4 sums[kMaxCluster * kStreamWarps];         // first CTA: their shares of the row's loss and weights' gradients
+  float2 red[kStreamWarps];
   float logit[kMaxTopK];            // the teacher's as stored; -inf: left out
   Teacher teacher;
   int flags;
@@ -208,25 +227,19 @@ struct LossShared {
 // the largest entry leaves of 1 (-expm1): its digits outlast a sum next to 1.
 __device__ __forceinline__ void teacher_side(LossShared& sh, int K, bool tail, float inv_t) {
   const int lane = threadIdx.x & 31;
-  constexpr int N = kMaxTopK / 32;
-  float t[N], top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int k = i * 32 + lane;
-    t[i] = k < K ? sh.logit[k] : -INFINITY;
-    top = fmaxf(top, t[i]);
-  }
+  float top = -INFINITY;
+  for (int k = lane; k < K; k += 32) top = fmaxf(top, sh.logit[k]);
   top = warp_max(top);
   int first = kMaxTopK;
-#pragma unroll
-  for (int i = N - 1; i >= 0; --i)
-    if (t[i] == top) first = i * 32 + lane;
+  for (int k = lane; k < K; k += 32)
+    if (sh.logit[k] == top) first = min(first, k);
   first = __reduce_min_sync(0xFFFFFFFFu, first);
   const float shift = tail ? 0.f : top, scale = tail ? 1.f : inv_t;
   float others = 0.f;                              // without the first of the largest
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (t[i] > -INFINITY && i * 32 + lane != first) others += expf((t[i] - shift) * scale);
+  for (int k = lane; k < K; k += 32) {
+    const float t = sh.logit[k];
+    if (t > -INFINITY && k != first) others += expf((t - shift) * scale);
+  }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) others += __shfl_xor_sync(0xFFFFFFFFu, others, d);
   if (lane == 0) {
@@ -249,7 +262,7 @@ __device__ __forceinline__ float listed_grad(float lq, float lp, float mass) {
 // Sums over the rows of each weight, in a fixed order, by a whole CTA of NT threads
 // (the rows' records past L1: other CTAs of the grid may have written them).
 template <int NT>
-__device__ void weight_grads(const DistillArgs& a, int j, float (*red)[2]) {
+__device__ void weight_grads(const DistillArgs& a, int j, float2* red) {
   const int n = a.in.n_weights;
   float da = 0.f, db = 0.f;
   for (long long r = j + (long long)threadIdx.x * n; r < a.in.rows; r += (long long)NT * n) {
@@ -267,15 +280,14 @@ __device__ void weight_grads(const DistillArgs& a, int j, float (*red)[2]) {
   }
   __syncthreads();
   if ((threadIdx.x & 31) == 0) {
-    red[threadIdx.x >> 5][0] = da;
-    red[threadIdx.x >> 5][1] = db;
+    red[threadIdx.x >> 5] = make_float2(da, db);
   }
   __syncthreads();
   if (threadIdx.x == 0) {
     da = db = 0.f;
     for (int k = 0; k < NT / 32; ++k) {
-      da += red[k][0];
-      db += red[k][1];
+      da += red[k].x;
+      db += red[k].y;
     }
     if (a.grad_alpha) a.grad_alpha[j] = da;
     if (a.grad_beta) a.grad_beta[j] = db;
@@ -295,7 +307,7 @@ __device__ __forceinline__ void finish_rows(const DistillArgs& a, LossShared& sh
   if (!sh.flags) return;
   __threadfence();
   for (int j = 0; j < a.in.n_weights; ++j)
-    weight_grads<kStreamThreads>(a, j, reinterpret_cast<float(*)[2]>(sh.sums));
+    weight_grads<kStreamThreads>(a, j, sh.red);
   if (threadIdx.x == 0) *a.ticket = 0;
 }
 
@@ -330,11 +342,19 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   if (threadIdx.x == 0) pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = a.in.cluster, K = a.K, V = a.in.V;
-  const int rank = (int)(blockIdx.x % C);
-  const long long r = blockIdx.x / C;
+  const int rank = (int)(blockIdx.x & (C - 1));
+  const long long r = blockIdx.x / (unsigned)C;
   const float c = a.in.scale, inv_t = a.in.inv_t;
   const float weight = a.row_weight ? __ldg(a.row_weight + r) : 1.f;
+  // thread k has entry k (kMaxTopK <= kStreamThreads)
+  int id = -1;
+  float logit = -INFINITY;
+  if (tid < K) {
+    id = __ldg(a.ids + r * K + tid);
+    logit = __ldg(a.teacher + r * K + tid);
+  }
   const FusedRow<T, FUSED, VEC> row(a.in, r);
+  const float p_ref = FUSED ? row.p_at(row.sh + V / 2) : 0.f;
   const long long first = (long long)rank * a.in.slice_cols;
   const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
   using Cp = RowCopies<T, FUSED, GRAD>;
@@ -342,16 +362,14 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   uint8_t* kept = ring + (VEC ? Cp::kRingBytes : 0);           // GRAD: the slice's values, 32 bytes an item
   T* out = nullptr;                                // the row's gradient at position 0
   if constexpr (GRAD) out = static_cast<T*>(a.grad) + r * a.ld_grad - row.sh;
+  RowStream<Cp, T, FUSED, VEC> stream(row, k0, k1, ring, kept);
+  if (weight != 0.f) stream.begin();
 
-  for (int i = tid; i < (a.in.slice_cols + 31) / 32; i += kStreamThreads) bitmap[i] = 0u;
+  for (int i = tid; i < (a.in.slice_cols + 127) / 128; i += kStreamThreads)
+    reinterpret_cast<uint4*>(bitmap)[i] = make_uint4(0u, 0u, 0u, 0u);
   if (tid == 0) sh.flags = 0;
-  // thread k has entry k (kMaxTopK <= kStreamThreads)
-  int id = -1;
-  float logit = -INFINITY;
   unsigned flags = 0u;
   if (tid < K) {
-    id = __ldg(a.ids + r * K + tid);
-    logit = __ldg(a.teacher + r * K + tid);
     if (id >= V) flags |= kFlagBadId;
     else if (id >= 0 && !(logit < INFINITY)) flags |= kFlagBadLogit;
     if (id < 0 || id >= V || logit == -INFINITY) {
@@ -369,14 +387,15 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
     const unsigned bit = 1u << (at & 31);
     if (atomicOr(&bitmap[at >> 5], bit) & bit) flags |= kFlagTwice;
   }
-  if (tid < kMaxTopK) {
+  if (warp * 32 < K) {
     flags = __reduce_or_sync(0xFFFFFFFFu, flags);
     if (lane == 0 && flags) atomicOr(&sh.flags, (int)flags);
   }
   __syncthreads();
   flags = (unsigned)sh.flags;
   const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
-  if (weight == 0.f || !(flags & (kFlagAny | kFlagBadLogit))) {     // left out: the logits are not read
+  if (weight == 0.f || !(flags & (kFlagAny | kFlagBadLogit))) {     // left out
+    stream.drain();
     if constexpr (GRAD) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
@@ -392,88 +411,88 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
     return;
   }
   if (C > 1) cluster_arrive_relaxed();
-  if (warp == kStreamWarps - 1) teacher_side(sh, K, a.tail != 0, inv_t);
-  // a constant in the prior drops out of the gradient's sum with it: taken out first
-  const float p_ref = FUSED ? row.p_at(row.sh + V / 2) : 0.f;
-  float x_k = -INFINITY, s_k = 0.f, p_k = 0.f;
+  float l_k = -INFINITY, s_k = 0.f, p_k = 0.f;     // the listed column's terms
   if (mine) {
-    x_k = row.at(k0 + at);
-    s_k = fmaxf(row.s_at(k0 + at), -FLT_MAX);
-    p_k = row.p_at(k0 + at) - p_ref;
+    l_k = row.l_at(k0 + at);
+    s_k = row.s_at(k0 + at);
+    p_k = row.p_at(k0 + at);
   }
+  if (warp == kStreamWarps - 1) teacher_side(sh, K, a.tail != 0, inv_t);
 
   // the columns that are not listed
   WarpTail<FUSED> st;
   st.init();
-  stream_items<Cp>(row, k0, k1, ring, kept, [&](auto& v, auto checked, int call) {
-    {
-      constexpr int u = 0;         // (one item a call)
-      float x[8], s[8], p[8];
-      v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
+  stream.run([&](auto& v, auto checked, int, int it) {
+    constexpr int N = sizeof(v) / sizeof(v[0]);
+    constexpr bool kChecked = decltype(checked)::value;
+    float x[N][8], s[N][8], p[N][8];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      v[u].template values<kChecked>(row, k1, x[u], s[u], p[u]);
       if constexpr (VEC) {
         const int b = v[u].k - k0;
         unsigned bits = 0u;        // of the item's 8 positions
         if constexpr (sizeof(T) == 2) {
-          if (!decltype(checked)::value || b < k1 - k0) bits = reinterpret_cast<const unsigned char*>(bitmap)[b >> 3];
+          if (!kChecked || b < k1 - k0) bits = reinterpret_cast<const unsigned char*>(bitmap)[b >> 3];
         } else {
-          if (!decltype(checked)::value || b < k1 - k0) bits = bitmap[b >> 5] >> (b & 31) & 15u;
-          if (!decltype(checked)::value || b + kHalf<T> < k1 - k0)
-            bits |= (bitmap[(b + kHalf<T>) >> 5] >> (b & 31) & 15u) << 4;
+          if (!kChecked || b < k1 - k0) bits = bitmap[b >> 5] >> (b & 31) & 15u;
+          if (!kChecked || b + kHalf<T> < k1 - k0) bits |= (bitmap[(b + kHalf<T>) >> 5] >> (b & 31) & 15u) << 4;
         }
         if (bits) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (bits >> i & 1u) x[i] = -INFINITY;
+            if (bits >> i & 1u) x[u][i] = -INFINITY;
         }
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int b = elem_pos<T, VEC>(v[u].k, i) - k0;
-          if ((!decltype(checked)::value || b < k1 - k0) && (bitmap[b >> 5] >> (b & 31) & 1u)) x[i] = -INFINITY;
+          if ((!kChecked || b < k1 - k0) && (bitmap[b >> 5] >> (b & 31) & 1u)) x[u][i] = -INFINITY;
         }
       }
       if constexpr (GRAD) {
-        float4* keep = reinterpret_cast<float4*>(kept) + call * 2 * kStreamThreads + tid;
-        keep[0] = make_float4(x[0], x[1], x[2], x[3]);
-        keep[kStreamThreads] = make_float4(x[4], x[5], x[6], x[7]);
+        float4* keep = reinterpret_cast<float4*>(kept) + (it + u) * 2 * kStreamThreads + tid;
+        keep[0] = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
+        keep[kStreamThreads] = make_float4(x[u][4], x[u][5], x[u][6], x[u][7]);
       }
-      st.push(x, s, p, c, p_ref);
     }
+    st.push(x, s, p, c, p_ref);
   });
-  const TailRec wr = st.record();
-  if (lane == 0) sh.warps[warp] = wr;
+  WarpRec rec{st.record(), ListRec{-INFINITY, 0.f}};
 
   // the listed columns of this slice; an id listed twice counts once in the student's sums
   bool once = mine;
-  if (mine && (flags & kFlagTwice))
-    for (int k = 0; k < tid; ++k)
-      if (sh.logit[k] > -INFINITY && __ldg(a.ids + r * K + k) == id) once = false;
-  const float m_k = warp_max(once && x_k == x_k ? x_k : -INFINITY);
-  {
-    const unsigned who = __ballot_sync(0xFFFFFFFFu, once && x_k == m_k && m_k > -INFINITY);
+  const float x_k = mine ? row.combine(l_k, s_k, p_k) : -INFINITY;
+  if (__any_sync(0xFFFFFFFFu, mine)) {
+    if (mine && (flags & kFlagTwice))
+      for (int k = 0; k < tid; ++k)
+        if (sh.logit[k] > -INFINITY && __ldg(a.ids + r * K + k) == id) once = false;
+    rec.l.m = warp_max(once && x_k == x_k ? x_k : -INFINITY);
+    const unsigned who = __ballot_sync(0xFFFFFFFFu, once && x_k == rec.l.m && rec.l.m > -INFINITY);
     float e = 0.f;
-    if (once && x_k != -INFINITY && lane != __ffs(who) - 1) e = ex2_approx((x_k - m_k) * c);
+    if (once && x_k != -INFINITY && lane != __ffs(who) - 1) e = ex2_approx((x_k - rec.l.m) * c);
     if (once && x_k != x_k) e = NAN;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) e += __shfl_xor_sync(0xFFFFFFFFu, e, d);
-    if (lane == 0) sh.listed[warp] = ListRec{m_k, e};
+    rec.l.rest = e;
   }
-  __syncthreads();
-  TailRec tail = tail_merge8(sh.warps[lane & 7], c);
-  ListRec listed = list_merge8(sh.listed[lane & 7], c);
+  // every warp's record to every CTA of the cluster
   if (C > 1) {
     cluster_wait();                // every CTA of the cluster runs before its shared memory is written
-    if (tid < C) {
-      const uint32_t to = cluster_map(smem_u32(&sh.ctas[rank][0]), (uint32_t)tid);
-      st_cluster_v4(to, tail.m, tail.f.off, tail.f.r, tail.sum);
-      st_cluster_v4(to + 16, tail.s, tail.p, listed.m, listed.rest);
+    if (lane < C) {
+      const uint32_t to = cluster_map(smem_u32(&sh.recs[rank * kStreamWarps + warp]), (uint32_t)lane);
+      st_cluster_v4(to, rec.t.m, rec.t.f.off, rec.t.f.r, rec.t.sum);
+      st_cluster_v4(to + 16, rec.t.s, rec.t.p, rec.l.m, rec.l.rest);
     }
+    __syncwarp();
     cluster_sync_all();
-    const float* rec = sh.ctas[lane & 7];
-    const bool in = (lane & 7) < C;
-    tail = tail_merge8(in ? TailRec{rec[0], Ref{rec[1], rec[2]}, rec[3], rec[4], rec[5]} : tail_init(), c);
-    listed = list_merge8(in ? ListRec{rec[6], rec[7]} : ListRec{-INFINITY, 0.f}, c);
+  } else {
+    if (lane == 0) sh.recs[warp] = rec;
+    __syncthreads();
   }
+  TailRec tail;
+  ListRec listed;
+  merge_records(sh.recs, C * kStreamWarps, c, tail, listed);
   // S = sum over all columns = listed + not listed, in units of the reference f of
   // those that are not listed (of the largest listed where there are none).
   const bool none_listed = listed.m == -INFINITY, none_else = tail.m == -INFINITY;
@@ -495,83 +514,92 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   const bool has_tail = a.tail && te.rest > 0.f && tail.sum > 0.f;
   const float mass = has_tail ? 1.f : te.sum;
   const float factor = mass * inv_s - (has_tail ? te.rest / tail.sum : 0.f);
-
   const float up = weight * inv_t * (FUSED ? row.a : 1.f);   // dL/dl -> what the gradient holds
+
+  // the listed columns' share of the loss and of the weights' gradients, to the first CTA
+  float g_k = 0.f;
+  if (warp * 32 < K) {
+    float v[3] = {0.f, 0.f, 0.f};
+    if (mine) {
+      const float lp = (logit - te.t_max) * te.t_scale - te.log_norm, p = expf(lp);
+      const float lq = (x_k - base) * inv_t - base_ln;
+      const float g = once ? listed_grad(lq, lp, mass) : -p;
+      v[0] = p > 0.f ? p * (lp - lq) : 0.f;
+      v[1] = g * fmaxf(s_k, -FLT_MAX);
+      v[2] = g * (p_k - p_ref);
+      g_k = up * g;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) v[j] += __shfl_xor_sync(0xFFFFFFFFu, v[j], d);
+    if (lane == 0) {
+      float4* to = &sh.sums[rank * kStreamWarps + warp];
+      if (C > 1) st_cluster_v4(cluster_map(smem_u32(to), 0), v[0], v[1], v[2], 0.f);
+      else *to = make_float4(v[0], v[1], v[2], 0.f);
+    }
+  }
+  __syncwarp();
+  if (C > 1) cluster_arrive();
+
   if constexpr (GRAD) {
     const float k2 = ok ? up * factor : NAN;
     const float4* got = reinterpret_cast<const float4*>(kept) + tid;
-    for (int it = 0; it < items; ++it, got += 2 * kStreamThreads) {
+#pragma unroll 2
+    for (int it = 0; it < items; ++it) {
       const int k = item_pos<T, VEC>(k0, it, tid);
-      if (k >= k1) break;
-      const float4 u = got[0], w = got[kStreamThreads];
+      const float4 u = got[it * 2 * kStreamThreads], w = got[(it * 2 + 1) * kStreamThreads];
       float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w}, g[8];
       unlisted_grad(x, f, c, k2, g);
       grad_item<T, VEC>(out, k, row.sh, k1, a.grad_vec, g);
     }
-  }
-  float v[3] = {0.f, 0.f, 0.f};
-  float g_k = 0.f;
-  if (mine) {
-    const float lp = (logit - te.t_max) * te.t_scale - te.log_norm, p = expf(lp);
-    const float lq = (x_k - base) * inv_t - base_ln;
-    const float g = once ? listed_grad(lq, lp, mass) : -p;
-    v[0] = p > 0.f ? p * (lp - lq) : 0.f;
-    v[1] = g * s_k;
-    v[2] = g * p_k;
-    g_k = up * g;
-  }
-#pragma unroll
-  for (int j = 0; j < 3; ++j) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v[j] += __shfl_xor_sync(0xFFFFFFFFu, v[j], d);
-    if (lane == 0) sh.sums[warp][j] = v[j];
-  }
-  __syncthreads();                                 // (and the unlisted columns' gradients are written)
-  if constexpr (GRAD) {
+    __syncthreads();               // the unlisted columns' gradients are written
     if (flags & kFlagTwice) twice_grads(a, sh, r, mine, id, ok ? g_k : NAN, out + k0 + at);
     else if (mine) grad_elem(out, k0 + at, ok ? g_k : NAN);
+  } else if (C == 1) {
+    __syncthreads();
   }
-#pragma unroll
-  for (int j = 0; j < 3; ++j) {
-    v[j] = 0.f;
-    for (int k = 0; k < kStreamWarps; ++k) v[j] += sh.sums[k][j];
-  }
-  if (C > 1) {
-    if (tid == 0) st_cluster_v4(cluster_map(smem_u32(&sh.last[rank][0]), 0), v[0], v[1], v[2], 0.f);
-    cluster_arrive();
-    if (rank != 0) return;
-    cluster_wait();
-#pragma unroll
-    for (int j = 0; j < 3; ++j) {
-      v[j] = 0.f;
-      for (int k = 0; k < C; ++k) v[j] += sh.last[k][j];
+  if (rank != 0) return;
+  if (C > 1) cluster_wait();
+  if (warp == 0) {
+    float v[3] = {0.f, 0.f, 0.f};
+    for (int i = lane; i < C * kStreamWarps; i += 32) {
+      if ((i & (kStreamWarps - 1)) * 32 >= K) continue;
+      const float4 q = sh.sums[i];
+      v[0] += q.x;
+      v[1] += q.y;
+      v[2] += q.z;
     }
-  }
-  if (tid == 0) {
-  if (!ok) raise_status(a.status, DELS_STATUS_NONFINITE);
-  if (flags & kFlagBadId) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
-  float loss = v[0];
-  if (has_tail) {
-    const float log_rest = te.rest > 0.5f ? log1pf(-te.sum) : logf(te.rest);
-    // -ln q_t = ln(1 + list_sum / tail.sum)
-    const float more = z_l > 60.f ? z_l * kLn2 + logf((1.f + listed.rest) / tail.sum) : log1pf(list_sum / tail.sum);
-    loss += te.rest * (log_rest + more);
-  }
-  if (a.out_loss) a.out_loss[r] = ok ? weight * loss : NAN;
-  DistillState o{};
-  o.f_off = f.off;
-  o.f_r = f.r;
-  o.factor = ok ? factor : NAN;
-  o.base = base;
-  o.base_ln = base_ln;
-  o.mass = ok ? mass : NAN;
-  o.t_max = te.t_max;
-  o.t_scale = te.t_scale;
-  o.log_norm = te.log_norm;
-  o.weight = weight;
-  o.d_alpha = ok ? weight * inv_t * (factor * tail.s + v[1]) : NAN;
-  o.d_beta = ok ? -weight * inv_t * (factor * tail.p + v[2]) : NAN;
-  a.state[r] = o;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) v[j] += __shfl_xor_sync(0xFFFFFFFFu, v[j], d);
+    if (lane == 0) {
+      if (!ok) raise_status(a.status, DELS_STATUS_NONFINITE);
+      if (flags & kFlagBadId) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
+      float loss = v[0];
+      if (has_tail) {
+        const float log_rest = te.rest > 0.5f ? log1pf(-te.sum) : logf(te.rest);
+        // -ln q_t = ln(1 + list_sum / tail.sum)
+        const float more = z_l > 60.f ? z_l * kLn2 + logf((1.f + listed.rest) / tail.sum) : log1pf(list_sum / tail.sum);
+        loss += te.rest * (log_rest + more);
+      }
+      if (a.out_loss) a.out_loss[r] = ok ? weight * loss : NAN;
+      DistillState o{};
+      o.f_off = f.off;
+      o.f_r = f.r;
+      o.factor = ok ? factor : NAN;
+      o.base = base;
+      o.base_ln = base_ln;
+      o.mass = ok ? mass : NAN;
+      o.t_max = te.t_max;
+      o.t_scale = te.t_scale;
+      o.log_norm = te.log_norm;
+      o.weight = weight;
+      o.d_alpha = ok ? weight * inv_t * (factor * tail.s + v[1]) : NAN;
+      o.d_beta = ok ? -weight * inv_t * (factor * tail.p + v[2]) : NAN;
+      a.state[r] = o;
+    }
   }
   if constexpr (GRAD) finish_rows(a, sh);
 }
@@ -602,6 +630,8 @@ __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs 
   }
   const float g0 = up * st.weight * a.in.inv_t * (FUSED ? row.a : 1.f);
   const float c = a.in.scale;
+  RowStream<LossCopies<T, FUSED>, T, FUSED, VEC> stream(row, k0, k1, ring, nullptr);
+  stream.begin();
 
   int id = -1;
   float g_k = 0.f;
@@ -630,18 +660,21 @@ __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs 
   __syncthreads();                                 // the output may be l_S itself
   const float k2 = g0 * st.factor;
   const Ref f{st.f_off, st.f_r};
-  stream_items<LossCopies<T, FUSED>>(row, k0, k1, ring, nullptr, [&](auto& v, auto checked, int) {
-    float x[8], s[8], p[8], g[8];
-    v[0].template values<decltype(checked)::value>(row, k1, x, s, p);
-    unlisted_grad(x, f, c, k2, g);
-    grad_item<T, VEC>(out, v[0].k, row.sh, k1, a.grad_vec, g);
+  stream.run([&](auto& v, auto checked, int, int) {
+#pragma unroll
+    for (int u = 0; u < (int)(sizeof(v) / sizeof(v[0])); ++u) {
+      float x[8], s[8], p[8], g[8];
+      v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
+      unlisted_grad(x, f, c, k2, g);
+      grad_item<T, VEC>(out, v[u].k, row.sh, k1, a.grad_vec, g);
+    }
   });
   __syncthreads();
   if (id >= 0) grad_elem(out, id + row.sh, g_k);
 }
 
 __global__ void __launch_bounds__(256) k_weight_grads(DistillArgs a) {
-  __shared__ float red[8][2];
+  __shared__ float2 red[8];
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
   weight_grads<256>(a, blockIdx.x, red);

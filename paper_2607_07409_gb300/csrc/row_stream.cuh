@@ -117,7 +117,7 @@ struct FusedRow {
     a = b = 1.f;
     minus_zero = in.minus_zero;
     if constexpr (FUSED) {
-      const int j = (int)(row % in.n_weights);
+      const unsigned j = (unsigned)row % (unsigned)in.n_weights;
       if (in.shortp) {
         S = static_cast<const T*>(in.shortp) + row * in.ld_short;
         if (in.alpha) a = __ldg(in.alpha + j);
@@ -178,7 +178,7 @@ struct Item {
   Raw8<T> l;
   Raw8<T> s;           // FUSED only
   int k;               // its first position
-  const uint8_t* ring_prior = nullptr;   // l_P in shared memory, if it was copied there
+  float pr[8];         // its l_P, where the stream has loaded it (whole items of FUSED rows)
 
   __device__ __forceinline__ void load_whole(const FusedRow<T, FUSED, VEC>& row, int pos) {
     k = pos;
@@ -213,7 +213,7 @@ struct Item {
       }
     }
   }
-  // The prior of its positions (CHECK: 0 outside the row and from `stop` on).
+  // The prior of the positions of an item at k (CHECK: 0 outside the row and from `stop` on).
   template <bool CHECK>
   __device__ __forceinline__ void prior(const FusedRow<T, FUSED, VEC>& row, int stop, float (&p)[8]) const {
     if constexpr (!FUSED) return;
@@ -232,14 +232,6 @@ struct Item {
         return;
       }
     }
-    if constexpr (VEC && !CHECK) {
-      if (ring_prior) {
-        const float4 u = *reinterpret_cast<const float4*>(ring_prior);
-        const float4 v = *reinterpret_cast<const float4*>(ring_prior + kStreamThreads * 16);
-        p[0] = u.x; p[1] = u.y; p[2] = u.z; p[3] = u.w; p[4] = v.x; p[5] = v.y; p[6] = v.z; p[7] = v.w;
-        return;
-      }
-    }
     if constexpr (VEC) {                           // (the prior's own place against 16 bytes is -sh)
       prior4(row.P + k, -row.sh & 3, p);
       prior4(row.P + k + kHalf<T>, -row.sh & 3, p + 4);
@@ -255,7 +247,12 @@ struct Item {
     l.unpack(x);
     if constexpr (!FUSED) return;
     s.unpack(sv);
-    prior<CHECK>(row, stop, p);
+    if constexpr (VEC && !CHECK) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = pr[i];
+    } else {
+      prior<CHECK>(row, stop, p);
+    }
     const f32x2 a2 = both2(row.a), b2 = both2(-row.b);       // x - b p = x + (-b) p, both rounded alike
     const f32x2 z2 = both2(row.minus_zero);
 #pragma unroll
@@ -411,19 +408,18 @@ __device__ __forceinline__ void copies_wait() {
 }
 
 // Shared memory that whole items are copied to ahead of their use, in 16-byte pieces:
-// 8 logits are W of them, a fused item l_L's, l_S's and two of l_P. A piece belongs
-// to one thread, which copies it, waits for it and reads it: no barrier. A warp's
-// copies of a piece are 512 bytes side by side.
+// 8 logits are W of them, a fused item l_L's and l_S's. A piece belongs to one
+// thread, which copies it, waits for it and reads it: no barrier. A warp's copies of a
+// piece are 512 bytes side by side.
 //
-// A ring of D groups of U items; with R > 0 (U = 1) the first two pieces of every
-// item have a place of their own that stays (32 bytes: the item's 8 values as
-// float32 later), copied R items ahead, and the ring has the others.
+// Items come in groups of U; a ring has D groups. With R > 0 the first two pieces of
+// every item have a place of their own that stays (32 bytes: the item's 8 values as
+// float32 later), copied R groups ahead, and the ring has the others.
 template <typename T, bool FUSED, int U_, int D_, int R_ = 0>
 struct Copies {
   static constexpr int U = U_, D = D_, R = R_;
   static constexpr int W = Raw8<T>::W;
-  static constexpr bool kPrior = FUSED && !(R > 0 && W == 2);    // l_P too (else: loaded where it is used)
-  static constexpr int kPieces = FUSED ? 2 * W + (kPrior ? 2 : 0) : W;
+  static constexpr int kPieces = FUSED ? 2 * W : W;
   static constexpr int kStay = R > 0 ? 2 : 0;
   static constexpr int kRing = kPieces > kStay ? kPieces - kStay : 0;
   static constexpr int kPiece = 16 * kStreamThreads;             // one piece of all threads
@@ -431,11 +427,6 @@ struct Copies {
   static constexpr int kItemBytes = kStay * kPiece;              // per item that stays
 };
 
-// The items of a thread in positions k0 .. k1 - 1 of a row (a slice, at most the
-// row's end): f(items, checked, call), checked = std::false_type where all of them are
-// whole for every thread, `call` counting the calls. With VEC whole items come U at
-// a time, D - 1 such groups ahead in flight; what U leaves over, and a row's ends, go
-// one by one. (`ring`, `stay`: the thread block's.)
 struct StreamPlan {
   int head;            // calls of the row's first item, which may not be whole: 0 or 1
   int groups;          // calls of U whole items
@@ -457,101 +448,140 @@ struct StreamPlan {
     return g <= 0 ? call : g < groups ? head + g * U : head + groups * U + (g - groups);
   }
 };
-template <typename Cp, typename T, bool FUSED, bool VEC, typename F>
-__device__ __forceinline__ void stream_items(const FusedRow<T, FUSED, VEC>& row, int k0, int k1, uint8_t* ring,
-                                             uint8_t* stay, F&& f) {
-  constexpr int U = Cp::U, D = Cp::D, R = Cp::R, W = Cp::W, PC = Cp::kPiece;
-  const StreamPlan p = StreamPlan::of<U>(k0, k1, row.sh, VEC);
-  int it = 0, call = 0;
-  auto one = [&]() {
-    const int pos = item_pos<T, VEC>(k0, it, threadIdx.x);
-    Item<T, FUSED, VEC> v[1];
-    v[0].load(row, pos, k1);
-    f(v, std::true_type{}, call);
-    ++it;
-    ++call;
-  };
-  if constexpr (VEC) {
-    const bool prior = Cp::kPrior && row.P && (row.sh & 3) == 0;   // (its own place against 16 bytes is -sh)
-    // Place of piece k of item i of the groups, which is in place `q` of the ring.
-    auto place = [&](uint8_t* rg, uint8_t* st, int k, int i, int q) -> uint8_t* {
-      return k < Cp::kStay ? st + (size_t)(p.head + i) * Cp::kItemBytes + k * PC
-                           : rg + (q * Cp::kRing + k - Cp::kStay) * PC;
-    };
-    ring += threadIdx.x * 16;
-    stay += threadIdx.x * 16;
-    // pieces [from, to) of item i
-    auto copy = [&](int i, int q, int from, int to) {
-      const int at = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
+// The items of a thread in positions k0 .. k1 - 1 of a row (a slice, at most the
+// row's end). run() calls f(items, checked, call, it): checked = std::false_type where
+// all of them are whole for every thread, `call` the number of the call, `it` the
+// first one's number. With VEC whole items come U at a time, D - 1 such groups ahead in
+// flight and the prior one group ahead in registers; what U leaves over, and a row's
+// ends, go one by one. begin() starts the first copies; one that is not run is
+// drained.
+template <typename Cp, typename T, bool FUSED, bool VEC>
+struct RowStream {
+  static constexpr int U = Cp::U, D = Cp::D, R = Cp::R, W = Cp::W, PC = Cp::kPiece;
+  const FusedRow<T, FUSED, VEC>& row;
+  int k0, k1;
+  uint8_t *ring, *stay;    // the calling thread's
+  StreamPlan p;
+  int slot_in = 0;
+
+  __device__ __forceinline__ RowStream(const FusedRow<T, FUSED, VEC>& r, int from, int to, uint8_t* ring_, uint8_t* stay_)
+      : row(r), k0(from), k1(to), ring(ring_ + threadIdx.x * 16), stay(stay_ + threadIdx.x * 16),
+        p(StreamPlan::of<U>(from, to, r.sh, VEC)) {}
+  // Piece k of item i of the groups, which is in place q of the ring.
+  __device__ __forceinline__ uint8_t* place(int k, int i, int q) const {
+    return k < Cp::kStay ? stay + (size_t)(p.head + i) * Cp::kItemBytes + k * PC
+                         : ring + (q * Cp::kRing + k - Cp::kStay) * PC;
+  }
+  __device__ __forceinline__ void copy(int i, int q, int from, int to) const {
+    const int at = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
 #pragma unroll
-      for (int k = 0; k < Cp::kPieces; ++k) {
-        if (k < from || k >= to) continue;
-        const uint32_t dst = smem_u32(place(ring, stay, k, i, q));
-        if (k < W) {
-          if (!FUSED || row.L) copy16(dst, row.L + at + k * kHalf<T>);
-        } else if (k < 2 * W) {
-          if (row.S) copy16(dst, row.S + at + (k - W) * kHalf<T>);
-        } else if (prior) {
-          copy16_l1(dst, row.P + at + (k - 2 * W) * kHalf<T>);   // (bf16: a 32-byte sector in two halves)
-        }
+    for (int k = 0; k < Cp::kPieces; ++k) {
+      if (k < from || k >= to) continue;
+      const uint32_t dst = smem_u32(place(k, i, q));
+      if (k < W) {
+        if (!FUSED || row.L) copy16(dst, row.L + at + k * kHalf<T>);
+      } else {
+        if (row.S) copy16(dst, row.S + at + (k - W) * kHalf<T>);
       }
-    };
-    // What is copied when call g begins: group g + D - 1 (its ring pieces), and item
-    // g + R - 1 (those that stay); one commit a call, empty at the end, so that at
-    // most D - 1 later ones are in flight when group g is waited for.
-    int slot_in = 0;
-    auto issue = [&](int g) {
-      if (g < p.groups) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) copy(g * U + u, slot_in * U + u, Cp::kStay, Cp::kPieces);
-        slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
-      }
-    };
-    auto issue_stay = [&](int i) {
-      if (R > 0 && i < p.groups) copy(i, 0, 0, Cp::kStay);
-    };
-#pragma unroll 1
-    for (int i = 0; i < R - 1; ++i) issue_stay(i);
-#pragma unroll
-    for (int d = 0; d < D - 1; ++d) {
-      issue(d);
-      copies_commit();
     }
-    if (p.head) one();
-    int slot = 0;
+  }
+  // What is copied when call g begins: the ring pieces of group g + D - 1 and those that
+  // stay of group g + R - 1; one commit a call, empty at the end, so that at most
+  // D - 1 later ones are in flight when group g is waited for.
+  __device__ __forceinline__ void issue(int g) {
+    if (Cp::kRing > 0 && g < p.groups) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) copy(g * U + u, slot_in * U + u, Cp::kStay, Cp::kPieces);
+      slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
+    }
+  }
+  __device__ __forceinline__ void issue_stay(int g) const {
+    if (R > 0 && g < p.groups) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) copy(g * U + u, 0, 0, Cp::kStay);
+    }
+  }
+  __device__ __forceinline__ void begin() {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int d = 0; d < D - 1; ++d) {
+        issue(d);
+        if (d < R - 1) issue_stay(d);
+        copies_commit();
+      }
 #pragma unroll 1
-    for (int g = 0; g < p.groups; ++g) {
-      issue(g + D - 1);
-      issue_stay(g + R - 1);
-      copies_commit();
-      copies_wait<D - 1>();
-      Item<T, FUSED, VEC> v[U];
+      for (int g = D - 1; g < R - 1; ++g) issue_stay(g);
+    }
+  }
+  __device__ __forceinline__ void drain() const {
+    if constexpr (VEC) copies_wait<0>();
+  }
+  __device__ __forceinline__ void prior_of(int g, float (&x)[U][8]) const {
+    if constexpr (FUSED && VEC) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int i = g * U + u, q = slot * U + u;
-        v[u].k = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
+        if (row.P && g < p.groups) {
+          const int at = item_pos<T, VEC>(k0, p.head + g * U + u, threadIdx.x);
+          prior4(row.P + at, -row.sh & 3, x[u]);             // (its own place against 16 bytes is -sh)
+          prior4(row.P + at + kHalf<T>, -row.sh & 3, x[u] + 4);
+        } else {
 #pragma unroll
-        for (int k = 0; k < W; ++k) {
-          if (!FUSED || row.L) v[u].l.w[k] = *reinterpret_cast<const uint4*>(place(ring, stay, k, i, q));
+          for (int i = 0; i < 8; ++i) x[u][i] = 0.f;
+        }
+      }
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void run(F&& f) {
+    int it = 0, call = 0;
+    auto one = [&]() {
+      Item<T, FUSED, VEC> v[1];
+      v[0].load(row, item_pos<T, VEC>(k0, it, threadIdx.x), k1);
+      f(v, std::true_type{}, call, it);
+      ++it;
+      ++call;
+    };
+    if constexpr (VEC) {
+      float pn[U][8];
+      prior_of(0, pn);
+      if (p.head) one();
+      int slot = 0;
+#pragma unroll 1
+      for (int g = 0; g < p.groups; ++g) {
+        issue(g + D - 1);
+        issue_stay(g + R - 1);
+        copies_commit();
+        copies_wait<D - 1>();
+        Item<T, FUSED, VEC> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = g * U + u, q = slot * U + u;
+          v[u].k = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
+#pragma unroll
+          for (int k = 0; k < W; ++k) {
+            if (!FUSED || row.L) v[u].l.w[k] = *reinterpret_cast<const uint4*>(place(k, i, q));
+            if constexpr (FUSED) {
+              if (row.S) v[u].s.w[k] = *reinterpret_cast<const uint4*>(place(W + k, i, q));
+            }
+          }
+          if (FUSED && !row.L) v[u].l.fill(0.f);
           if constexpr (FUSED) {
-            if (row.S) v[u].s.w[k] = *reinterpret_cast<const uint4*>(place(ring, stay, W + k, i, q));
+            if (!row.S) v[u].s.fill(0.f);
+#pragma unroll
+            for (int i2 = 0; i2 < 8; ++i2) v[u].pr[i2] = pn[u][i2];
           }
         }
-        if (FUSED && !row.L) v[u].l.fill(0.f);
-        if constexpr (FUSED) {
-          if (!row.S) v[u].s.fill(0.f);
-        }
-        v[u].ring_prior = prior ? place(ring, stay, 2 * W, i, q) : nullptr;
+        prior_of(g + 1, pn);
+        f(v, std::false_type{}, call, it);
+        it += U;
+        ++call;
+        slot = slot + 1 == D ? 0 : slot + 1;
       }
-      f(v, std::false_type{}, call);
-      it += U;
-      ++call;
-      slot = slot + 1 == D ? 0 : slot + 1;
+      copies_wait<0>();
     }
-    copies_wait<0>();
+    while (it < p.items) one();
   }
-  while (it < p.items) one();
-}
+};
 
 // The two halves of a cluster barrier (all threads of all its CTAs).
 __device__ __forceinline__ void cluster_arrive_relaxed() {

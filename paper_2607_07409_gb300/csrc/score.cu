@@ -164,10 +164,9 @@ __device__ __forceinline__ void raise8_bf16(uint4& w, __nv_bfloat162 low) {
   for (int i = 0; i < 4; ++i) h[i] = __hmax2_nan(h[i], low);
 }
 
-// Copies ahead: 32 KB of plain rows (four CTAs on an SM), 48 KB of two rows and the
-// prior (three).
+// Copies ahead: 32 KB of plain rows (four CTAs on an SM), 48 KB of two rows (three).
 template <typename T, bool FUSED>
-using ScoreCopies = Copies<T, FUSED, sizeof(T) == 2 && !FUSED ? 2 : 1, FUSED ? (sizeof(T) == 2 ? 3 : 2) : 4>;
+using ScoreCopies = Copies<T, FUSED, sizeof(T) == 2 ? 2 : 1, FUSED ? 3 : 4>;
 
 // Dynamic shared memory: the ring (later SelectShared), the block maxima, and for a
 // cluster the entries of all slices.
@@ -218,11 +217,13 @@ __global__ void __launch_bounds__(kStreamThreads, FUSED ? 3 : 4) k_score_rows(Sc
   int shift = 0;                   // calls per block maximum: 1 << shift
   while (((StreamPlan::of<U>(k0, k1, row.sh, VEC).template calls<U>() - 1) >> shift) >= kSlots) ++shift;
 
+  RowStream<Cp, T, FUSED, VEC> stream(row, k0, k1, dyn, nullptr);
+  stream.begin();
   WarpSoft st;
   st.init();
   float top = -INFINITY, block = -INFINITY;
   const __nv_bfloat162 low2 = __float2bfloat162_rn(a.low);
-  stream_items<Cp>(row, k0, k1, dyn, nullptr, [&](auto& v, auto checked, int call) {
+  stream.run([&](auto& v, auto checked, int call, int) {
     constexpr int N = sizeof(v) / sizeof(v[0]);
     float vm = -INFINITY;
     if constexpr (sizeof(T) == 2 && !FUSED) {
