@@ -2146,7 +2146,7 @@ void plan_cluster(StreamRows& in, int sms, int least) {
   in.cluster = c;
   // whole items of every thread (positions: a row may start up to 7 columns past a
   // 16-byte boundary)
-  in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, c > 1 ? 2048 : 8);
+  in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, c > 1 ? 4096 : 8);
 }
 
 int distill_call(const dels_rows* x, int rows, int V, const dels_teacher* t, RowsCall* call, DistillArgs* a) {

@@ -84,41 +84,31 @@ __device__ __forceinline__ void merge_records(const WarpRec* recs, int n, float 
   }
 }
 
-// One lane's sums over the columns that are not listed. The reference of a warp's
-// exponentials is that of an entry it has met: the largest of its first item, and
-// another only when one 2^20 times as likely comes (each is in float32's range and
-// the sums' digits do not depend on it; the largest entry so far would change about
-// ln n times, and a slice has few items).
-constexpr float kFarAbove = 20.f;
+// One lane's sums over the columns that are not listed, under its warp's reference:
+// that of the largest entry of the warp's first items. Nothing else is compared: the
+// sums' digits do not depend on the reference, and an entry 2^100 times as likely as
+// those (or one that is not a number) shows in sums that are not finite, which are
+// then taken again (redo). A running maximum took 10 instructions of an item's 100.
 template <bool FUSED>
 struct WarpTail {
-  float m, limit;      // the same in every lane, as f
+  float m;             // the same in every lane, as f
   Ref f;
   f32x2 sum, s, p;
   __device__ __forceinline__ void init() {
-    m = limit = -INFINITY;
+    m = -INFINITY;
     f = Ref{0.f, 0.f};
     sum = s = p = 0ull;
   }
-  // N items' values, all lanes converged.
-  template <int N>
-  __device__ __forceinline__ void push(float (&x)[N][8], const float (&sv)[N][8], const float (&pv)[N][8], float c,
+  // N items' values, all lanes converged: x becomes 2^z.
+  template <int N, typename It>
+  __device__ __forceinline__ void push(float (&x)[N][8], const float (&sv)[N][8], const It (&v)[N], float c,
                                        float p_ref) {
-    float vm = max8(x[0]);
+    if (m == -INFINITY) {
+      float vm = max8(x[0]);
 #pragma unroll
-    for (int u = 1; u < N; ++u) vm = fmaxf(vm, max8(x[u]));
-    if (__any_sync(0xFFFFFFFFu, vm > limit)) {
-      const float top = warp_max(vm);
-      const Ref to = make_ref(top, c);
-      if (m > -INFINITY) {
-        const f32x2 k = both2(ex2_approx(ref_shift(f, to, c)));
-        sum = mul2(k, sum);
-        s = mul2(k, s);
-        p = mul2(k, p);
-      }
-      f = to;
-      m = top;
-      limit = top + kFarAbove / c;
+      for (int u = 1; u < N; ++u) vm = fmaxf(vm, max8(x[u]));
+      m = warp_max(vm);
+      if (m > -INFINITY) f = make_ref(m, c);
     }
     if (f.off != 0.f) {
 #pragma unroll
@@ -133,11 +123,13 @@ struct WarpTail {
       for (int u = 0; u < N; ++u) {
         float z0, z1;
         split2(fma2(pair2(x[u][i], x[u][i + 1]), c2, nr), z0, z1);
-        const f32x2 e = pair2(ex2_approx(z0), ex2_approx(z1));
+        x[u][i] = ex2_approx(z0);
+        x[u][i + 1] = ex2_approx(z1);
+        const f32x2 e = pair2(x[u][i], x[u][i + 1]);
         sum = add2(sum, e);
         if constexpr (FUSED) {
-          s = fma2(e, pair2(fmaxf(sv[u][i], -FLT_MAX), fmaxf(sv[u][i + 1], -FLT_MAX)), s);   // a masked entry: 0
-          p = fma2(e, add2(pair2(pv[u][i], pv[u][i + 1]), np), p);
+          s = fma2(e, pair2(sv[u][i], sv[u][i + 1]), s);
+          p = fma2(e, add2(pair2(v[u].pr[i], v[u].pr[i + 1]), np), p);
         }
       }
   }
@@ -154,15 +146,50 @@ struct WarpTail {
     return r;
   }
 };
+// Where those are not finite (a later entry far above the first ones, a masked l_S of
+// -inf, an entry that is not a number): the warp's items again, element by element, the
+// largest entry first. `kept`: the step's place of 2^z, or null.
+template <typename T, int F, bool VEC>
+__device__ __noinline__ TailRec redo_tail(const FusedRow<T, F, VEC>& row, int k0, int k1, const unsigned* bitmap,
+                                          float* kept, float c, float p_ref) {
+  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep, tid = threadIdx.x;
+  auto value = [&](int it, int i, int& q) {
+    q = elem_pos<T, VEC>(item_pos<T, VEC>(k0, it, tid), i);
+    const bool in = q >= row.sh && q < k1 && !(bitmap[(q - k0) >> 5] >> ((q - k0) & 31) & 1u);
+    return in ? row.contracted(row.l_at(q), row.s_at(q), row.p_at(q)) : -INFINITY;
+  };
+  int q;
+  float m = -INFINITY;
+  for (int it = 0; it < items; ++it)
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, value(it, i, q));
+  TailRec r{warp_max(m), Ref{0.f, 0.f}, 0.f, 0.f, 0.f};
+  if (r.m > -INFINITY) r.f = make_ref(r.m, c);
+  for (int it = 0; it < items; ++it)
+    for (int i = 0; i < 8; ++i) {
+      const float x = value(it, i, q), e = ex2_approx(ref_z(x, r.f, c));
+      r.sum += e;
+      if (F && e != 0.f) {                     // (masked: neither l_S nor l_P counts)
+        r.s += e * row.s_at(q);
+        r.p += e * (row.p_at(q) - p_ref);
+      }
+      if (kept) kept[((it * 2 + (i >> 2)) * kStreamThreads + tid) * 4 + (i & 3)] = e;
+    }
+  for (int d = 16; d > 0; d >>= 1) {
+    r.sum += __shfl_xor_sync(0xFFFFFFFFu, r.sum, d);
+    r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, d);
+    r.p += __shfl_xor_sync(0xFFFFFFFFu, r.p, d);
+  }
+  return r;
+}
 
 // Copies ahead of the loss and gradient kernels, and of the step's, whose items stay
 // (beside 10 items of 8 KB its ring is to leave room for a second CTA on the SM).
-template <typename T, bool FUSED>
-using LossCopies = Copies<T, FUSED, sizeof(T) == 2 && !FUSED ? 2 : 1, FUSED && sizeof(T) == 4 ? 3 : 4>;
-template <typename T, bool FUSED>
-using StepCopies = std::conditional_t<sizeof(T) == 2, Copies<T, FUSED, 2, 4, 4>, Copies<T, FUSED, 1, FUSED ? 3 : 8, 8>>;
-template <typename T, bool FUSED, bool GRAD>
-using RowCopies = std::conditional_t<GRAD, StepCopies<T, FUSED>, LossCopies<T, FUSED>>;
+template <typename T, int F>
+using LossCopies = Copies<T, F, sizeof(T) == 2 && !F ? 2 : 1, F && sizeof(T) == 4 ? 3 : 4>;
+template <typename T, int F>
+using StepCopies = Copies<T, F, sizeof(T) == 2 ? 2 : 1, sizeof(T) == 2 ? 4 : F ? 3 : 6, true>;
+template <typename T, int F, bool GRAD>
+using RowCopies = std::conditional_t<GRAD, StepCopies<T, F>, LossCopies<T, F>>;
 
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   uint32_t w;
@@ -252,6 +279,43 @@ __device__ __forceinline__ void teacher_side(LossShared& sh, int K, bool tail, f
   }
 }
 
+// The student's sums of a row: S = sum over all columns = listed + not listed, in units
+// of the reference f of those that are not listed (of the largest listed where there
+// are none), and with the teacher's side dL/dl of a column that is not listed:
+//   (M - p_t / q_t) q = (M / S - p_t / sum) 2^z = factor 2^z,   q_t = sum / S.
+struct RowSums {
+  Ref f;
+  float z_l;        // of the largest listed; -inf: none
+  float list_sum;   // the listed ones' (may be infinite: the others then have nothing)
+  float factor, mass;
+  bool has_tail, ok;
+  __device__ __forceinline__ RowSums(const TailRec& t, const ListRec& l, const Teacher& te, bool tail, float c) {
+    f = t.m == -INFINITY ? make_ref(l.m, c) : t.f;
+    const bool none = l.m == -INFINITY;
+    z_l = none ? -INFINITY : ref_z(l.m, f, c);
+    list_sum = none ? l.rest : (1.f + l.rest) * ex2_approx(z_l);
+    has_tail = tail && te.rest > 0.f && t.sum > 0.f;
+    mass = has_tail ? 1.f : te.sum;
+    factor = __fdividef(mass, t.sum + list_sum) - (has_tail ? __fdividef(te.rest, t.sum) : 0.f);
+    const float top = fmaxf(t.m, l.m);
+    ok = top > -INFINITY && top < INFINITY && t.sum >= 0.f && t.sum < INFINITY && l.rest >= 0.f && l.rest < INFINITY;
+  }
+};
+// And its logarithms: ln q = (l - base) / T - base_ln, from the largest listed entry,
+// whose digits that keeps, unless the others are far above it.
+struct RowLogs {
+  float base, base_ln;
+  __device__ __forceinline__ RowLogs(const TailRec& t, const ListRec& l, const RowSums& s) {
+    const bool from_list = l.m > -INFINITY && s.z_l >= -20.f;
+    base = from_list ? l.m : s.f.off;
+    base_ln = from_list ? log1pf(l.rest + t.sum * ex2_approx(-s.z_l)) : s.f.r * kLn2 + logf(t.sum + s.list_sum);
+  }
+};
+// ln q_t = -ln(1 + list_sum / sum)
+__device__ __forceinline__ float tail_ln(const TailRec& t, const ListRec& l, const RowSums& s) {
+  return s.z_l > 60.f ? -(s.z_l * kLn2 + logf((1.f + l.rest) / t.sum)) : -log1pf(s.list_sum / t.sum);
+}
+
 // q M - p of a listed id from its logarithms: where p and q are next to 1 and to
 // each other their difference keeps its digits.
 __device__ __forceinline__ float listed_grad(float lq, float lp, float mass) {
@@ -306,8 +370,7 @@ __device__ __forceinline__ void finish_rows(const DistillArgs& a, LossShared& sh
   __syncthreads();
   if (!sh.flags) return;
   __threadfence();
-  for (int j = 0; j < a.in.n_weights; ++j)
-    weight_grads<kStreamThreads>(a, j, sh.red);
+  for (int j = 0; j < a.in.n_weights; ++j) weight_grads<kStreamThreads>(a, j, sh.red);
   if (threadIdx.x == 0) *a.ticket = 0;
 }
 
@@ -330,11 +393,10 @@ __device__ void twice_grads(const DistillArgs& a, LossShared& sh, long long r, b
 }
 
 // Loss and statistics of the rows, a cluster per row, a slice per CTA; GRAD: and
-// the gradient of l_S. The slice's fused values then stay in shared memory between
-// the pass that sums them and the one that writes their gradient, so that the rows
-// are read once: 3 s V bytes a row instead of 5 s V. Each thread reads back what it
-// wrote itself.
-template <typename T, bool FUSED, bool VEC, bool GRAD>
+// the gradient of l_S. The slice's 2^z then stay in shared memory between the pass that
+// sums them and the one that scales them, so that the rows are read once: 3 s V bytes
+// a row instead of 5 s V. Each thread reads back what it wrote itself.
+template <typename T, int F, bool VEC, bool GRAD>
 __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(DistillArgs a) {
   extern __shared__ __align__(16) unsigned bitmap[];   // one bit per position of the slice: listed
   __shared__ LossShared sh;
@@ -353,20 +415,19 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
     id = __ldg(a.ids + r * K + tid);
     logit = __ldg(a.teacher + r * K + tid);
   }
-  const FusedRow<T, FUSED, VEC> row(a.in, r);
-  const float p_ref = FUSED ? row.p_at(row.sh + V / 2) : 0.f;
-  const long long first = (long long)rank * a.in.slice_cols;
-  const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
-  using Cp = RowCopies<T, FUSED, GRAD>;
-  uint8_t* ring = reinterpret_cast<uint8_t*>(bitmap + (a.in.slice_cols + 127) / 128 * 4);
+  using Cp = RowCopies<T, F, GRAD>;
+  const int words = (a.in.slice_cols + Cp::U * kStreamStep - 1) / (Cp::U * kStreamStep) * (Cp::U * kStreamStep / 128);
+  uint8_t* ring = reinterpret_cast<uint8_t*>(bitmap + words * 4);
   uint8_t* kept = ring + (VEC ? Cp::kRingBytes : 0);           // GRAD: the slice's values, 32 bytes an item
+  RowStream<Cp, T, F, VEC> stream(a.in, r, rank, ring, kept);
+  const FusedRow<T, F, VEC>& row = stream.row;
+  const int k0 = stream.k0, k1 = stream.k1;
+  const float p_ref = F ? row.p_at(row.sh + V / 2) : 0.f;
+  if (weight != 0.f) stream.begin();
   T* out = nullptr;                                // the row's gradient at position 0
   if constexpr (GRAD) out = static_cast<T*>(a.grad) + r * a.ld_grad - row.sh;
-  RowStream<Cp, T, FUSED, VEC> stream(row, k0, k1, ring, kept);
-  if (weight != 0.f) stream.begin();
 
-  for (int i = tid; i < (a.in.slice_cols + 127) / 128; i += kStreamThreads)
-    reinterpret_cast<uint4*>(bitmap)[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = tid; i < words; i += kStreamThreads) reinterpret_cast<uint4*>(bitmap)[i] = make_uint4(0u, 0u, 0u, 0u);
   if (tid == 0) sh.flags = 0;
   unsigned flags = 0u;
   if (tid < K) {
@@ -393,12 +454,12 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   }
   __syncthreads();
   flags = (unsigned)sh.flags;
-  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
   if (weight == 0.f || !(flags & (kFlagAny | kFlagBadLogit))) {     // left out
     stream.drain();
     if constexpr (GRAD) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
+      for (int it = 0; it < stream.items; ++it)
+        grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
     }
     if (rank == 0 && tid == 0) {
       if (weight != 0.f && (flags & kFlagBadId)) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
@@ -420,23 +481,22 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   if (warp == kStreamWarps - 1) teacher_side(sh, K, a.tail != 0, inv_t);
 
   // the columns that are not listed
-  WarpTail<FUSED> st;
+  WarpTail<F != kPlain> st;
   st.init();
-  stream.run([&](auto& v, auto checked, int, int it) {
-    constexpr int N = sizeof(v) / sizeof(v[0]);
-    constexpr bool kChecked = decltype(checked)::value;
-    float x[N][8], s[N][8], p[N][8];
+  stream.run([&](auto& v, int g) {
+    constexpr int N = Cp::U;
+    float x[N][8], s[N][8];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      v[u].template values<kChecked>(row, k1, x[u], s[u], p[u]);
+      v[u].template values<true>(row, x[u], s[u]);
       if constexpr (VEC) {
+        // the item's 8 bits (positions past the slice are -inf already, their bits 0)
         const int b = v[u].k - k0;
-        unsigned bits = 0u;        // of the item's 8 positions
+        unsigned bits;
         if constexpr (sizeof(T) == 2) {
-          if (!kChecked || b < k1 - k0) bits = reinterpret_cast<const unsigned char*>(bitmap)[b >> 3];
+          bits = reinterpret_cast<const unsigned char*>(bitmap)[b >> 3];
         } else {
-          if (!kChecked || b < k1 - k0) bits = bitmap[b >> 5] >> (b & 31) & 15u;
-          if (!kChecked || b + kHalf<T> < k1 - k0) bits |= (bitmap[(b + kHalf<T>) >> 5] >> (b & 31) & 15u) << 4;
+          bits = (bitmap[b >> 5] >> (b & 31) & 15u) | (bitmap[(b + kHalf<T>) >> 5] >> (b & 31) & 15u) << 4;
         }
         if (bits) {
 #pragma unroll
@@ -447,22 +507,27 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int b = elem_pos<T, VEC>(v[u].k, i) - k0;
-          if ((!kChecked || b < k1 - k0) && (bitmap[b >> 5] >> (b & 31) & 1u)) x[u][i] = -INFINITY;
+          if (bitmap[b >> 5] >> (b & 31) & 1u) x[u][i] = -INFINITY;
         }
       }
-      if constexpr (GRAD) {
-        float4* keep = reinterpret_cast<float4*>(kept) + (it + u) * 2 * kStreamThreads + tid;
-        keep[0] = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
-        keep[kStreamThreads] = make_float4(x[u][4], x[u][5], x[u][6], x[u][7]);
+    }
+    st.push(x, s, v, c, p_ref);
+    if constexpr (GRAD) {
+      float4* keep = reinterpret_cast<float4*>(kept) + g * (N * 2 * kStreamThreads) + tid;
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        keep[u * 2 * kStreamThreads] = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
+        keep[(u * 2 + 1) * kStreamThreads] = make_float4(x[u][4], x[u][5], x[u][6], x[u][7]);
       }
     }
-    st.push(x, s, p, c, p_ref);
   });
   WarpRec rec{st.record(), ListRec{-INFINITY, 0.f}};
+  if (!(fabsf(rec.t.sum) + fabsf(rec.t.s) + fabsf(rec.t.p) < INFINITY))
+    rec.t = redo_tail<T, F, VEC>(row, k0, k1, bitmap, GRAD ? reinterpret_cast<float*>(kept) : nullptr, c, p_ref);
 
   // the listed columns of this slice; an id listed twice counts once in the student's sums
   bool once = mine;
-  const float x_k = mine ? row.combine(l_k, s_k, p_k) : -INFINITY;
+  const float x_k = mine ? row.contracted(l_k, s_k, p_k) : -INFINITY;
   if (__any_sync(0xFFFFFFFFu, mine)) {
     if (mine && (flags & kFlagTwice))
       for (int k = 0; k < tid; ++k)
@@ -493,46 +558,47 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   TailRec tail;
   ListRec listed;
   merge_records(sh.recs, C * kStreamWarps, c, tail, listed);
-  // S = sum over all columns = listed + not listed, in units of the reference f of
-  // those that are not listed (of the largest listed where there are none).
-  const bool none_listed = listed.m == -INFINITY, none_else = tail.m == -INFINITY;
-  const Ref f = none_else ? make_ref(listed.m, c) : tail.f;
-  const float z_l = none_listed ? -INFINITY : ref_z(listed.m, f, c);
-  const float list_sum = none_listed ? listed.rest : (1.f + listed.rest) * ex2_approx(z_l);   // may be infinite
-  const float inv_s = 1.f / (tail.sum + list_sum);
-  // ln q = (l - base) / T - base_ln: from the largest listed entry, whose digits that
-  // keeps, unless the others are far above it
-  const bool from_list = !none_listed && z_l >= -20.f;
-  const float base = from_list ? listed.m : f.off;
-  const float base_ln = from_list ? log1pf(listed.rest + tail.sum * ex2_approx(-z_l))
-                                  : f.r * kLn2 + logf(tail.sum + list_sum);
-  const float top = fmaxf(tail.m, listed.m);
-  const bool ok = top > -INFINITY && top < INFINITY && tail.sum >= 0.f && tail.sum < INFINITY && listed.rest >= 0.f &&
-                  listed.rest < INFINITY && !(flags & kFlagBadLogit);
   const Teacher te = sh.teacher;
-  // the tail: q_t = tail.sum / S; dL/dl of one of it (M - p_t / q_t) q = (M / S - p_t / tail.sum) 2^z
-  const bool has_tail = a.tail && te.rest > 0.f && tail.sum > 0.f;
-  const float mass = has_tail ? 1.f : te.sum;
-  const float factor = mass * inv_s - (has_tail ? te.rest / tail.sum : 0.f);
-  const float up = weight * inv_t * (FUSED ? row.a : 1.f);   // dL/dl -> what the gradient holds
+  const RowSums sums(tail, listed, te, a.tail != 0, c);
+  const bool ok = sums.ok && !(flags & kFlagBadLogit);
+  const float up = weight * inv_t * (F ? row.a : 1.f);   // dL/dl -> what the gradient holds
+  if constexpr (GRAD) {
+    // this warp's 2^z are relative to its own reference
+    const float k2 = ok ? up * sums.factor * (rec.t.m > -INFINITY ? ex2_approx(ref_shift(rec.t.f, sums.f, c)) : 0.f) : NAN;
+    const f32x2 kk = both2(k2);
+    const float4* got = reinterpret_cast<const float4*>(kept) + tid;
+#pragma unroll 2
+    for (int it = 0; it < stream.items; ++it) {
+      const float4 y = got[it * 2 * kStreamThreads], w = got[(it * 2 + 1) * kStreamThreads];
+      float gr[8];
+      split2(mul2(kk, pair2(y.x, y.y)), gr[0], gr[1]);
+      split2(mul2(kk, pair2(y.z, y.w)), gr[2], gr[3]);
+      split2(mul2(kk, pair2(w.x, w.y)), gr[4], gr[5]);
+      split2(mul2(kk, pair2(w.z, w.w)), gr[6], gr[7]);
+      grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, gr);
+    }
+  }
 
   // the listed columns' share of the loss and of the weights' gradients, to the first CTA
   float g_k = 0.f;
   if (warp * 32 < K) {
     float v[3] = {0.f, 0.f, 0.f};
-    if (mine) {
-      const float lp = (logit - te.t_max) * te.t_scale - te.log_norm, p = expf(lp);
-      const float lq = (x_k - base) * inv_t - base_ln;
-      const float g = once ? listed_grad(lq, lp, mass) : -p;
-      v[0] = p > 0.f ? p * (lp - lq) : 0.f;
-      v[1] = g * fmaxf(s_k, -FLT_MAX);
-      v[2] = g * (p_k - p_ref);
-      g_k = up * g;
+    if (__any_sync(0xFFFFFFFFu, mine)) {
+      const RowLogs logs(tail, listed, sums);
+      if (mine) {
+        const float lp = (logit - te.t_max) * te.t_scale - te.log_norm, p = expf(lp);
+        const float lq = (x_k - logs.base) * inv_t - logs.base_ln;
+        const float g = once ? listed_grad(lq, lp, sums.mass) : -p;
+        v[0] = p > 0.f ? p * (lp - lq) : 0.f;
+        v[1] = g * fmaxf(s_k, -FLT_MAX);
+        v[2] = g * (p_k - p_ref);
+        g_k = ok ? up * g : NAN;
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+        for (int j = 0; j < 3; ++j) v[j] += __shfl_xor_sync(0xFFFFFFFFu, v[j], d);
     }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-      for (int j = 0; j < 3; ++j) v[j] += __shfl_xor_sync(0xFFFFFFFFu, v[j], d);
     if (lane == 0) {
       float4* to = &sh.sums[rank * kStreamWarps + warp];
       if (C > 1) st_cluster_v4(cluster_map(smem_u32(to), 0), v[0], v[1], v[2], 0.f);
@@ -541,23 +607,10 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   }
   __syncwarp();
   if (C > 1) cluster_arrive();
-
+  if (GRAD || C == 1) __syncthreads();             // the unlisted columns' gradients are written
   if constexpr (GRAD) {
-    const float k2 = ok ? up * factor : NAN;
-    const float4* got = reinterpret_cast<const float4*>(kept) + tid;
-#pragma unroll 2
-    for (int it = 0; it < items; ++it) {
-      const int k = item_pos<T, VEC>(k0, it, tid);
-      const float4 u = got[it * 2 * kStreamThreads], w = got[(it * 2 + 1) * kStreamThreads];
-      float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w}, g[8];
-      unlisted_grad(x, f, c, k2, g);
-      grad_item<T, VEC>(out, k, row.sh, k1, a.grad_vec, g);
-    }
-    __syncthreads();               // the unlisted columns' gradients are written
-    if (flags & kFlagTwice) twice_grads(a, sh, r, mine, id, ok ? g_k : NAN, out + k0 + at);
-    else if (mine) grad_elem(out, k0 + at, ok ? g_k : NAN);
-  } else if (C == 1) {
-    __syncthreads();
+    if (flags & kFlagTwice) twice_grads(a, sh, r, mine, id, g_k, out + k0 + at);
+    else if (mine) grad_elem(out, k0 + at, g_k);
   }
   if (rank != 0) return;
   if (C > 1) cluster_wait();
@@ -577,27 +630,24 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
     if (lane == 0) {
       if (!ok) raise_status(a.status, DELS_STATUS_NONFINITE);
       if (flags & kFlagBadId) raise_status(a.status, DELS_STATUS_BAD_TOKEN);
+      const RowLogs logs(tail, listed, sums);
       float loss = v[0];
-      if (has_tail) {
-        const float log_rest = te.rest > 0.5f ? log1pf(-te.sum) : logf(te.rest);
-        // -ln q_t = ln(1 + list_sum / tail.sum)
-        const float more = z_l > 60.f ? z_l * kLn2 + logf((1.f + listed.rest) / tail.sum) : log1pf(list_sum / tail.sum);
-        loss += te.rest * (log_rest + more);
-      }
+      if (sums.has_tail)
+        loss += te.rest * ((te.rest > 0.5f ? log1pf(-te.sum) : logf(te.rest)) - tail_ln(tail, listed, sums));
       if (a.out_loss) a.out_loss[r] = ok ? weight * loss : NAN;
       DistillState o{};
-      o.f_off = f.off;
-      o.f_r = f.r;
-      o.factor = ok ? factor : NAN;
-      o.base = base;
-      o.base_ln = base_ln;
-      o.mass = ok ? mass : NAN;
+      o.f_off = sums.f.off;
+      o.f_r = sums.f.r;
+      o.factor = ok ? sums.factor : NAN;
+      o.base = logs.base;
+      o.base_ln = logs.base_ln;
+      o.mass = ok ? sums.mass : NAN;
       o.t_max = te.t_max;
       o.t_scale = te.t_scale;
       o.log_norm = te.log_norm;
       o.weight = weight;
-      o.d_alpha = ok ? weight * inv_t * (factor * tail.s + v[1]) : NAN;
-      o.d_beta = ok ? -weight * inv_t * (factor * tail.p + v[2]) : NAN;
+      o.d_alpha = ok ? weight * inv_t * (sums.factor * tail.s + v[1]) : NAN;
+      o.d_beta = ok ? -weight * inv_t * (sums.factor * tail.p + v[2]) : NAN;
       a.state[r] = o;
     }
   }
@@ -607,30 +657,28 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
 // The gradient of l_S from the statistics: every column as one that is not listed,
 // then the listed ones over it. The rows' own logits may be the output (each column
 // is read before it is written).
-template <typename T, bool FUSED, bool VEC>
+template <typename T, int F, bool VEC>
 __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs a) {
   extern __shared__ __align__(16) uint8_t ring[];
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
   const int tid = threadIdx.x;
   const int C = a.in.cluster, K = a.K;
-  const int rank = (int)(blockIdx.x % C);
-  const long long r = blockIdx.x / C;
-  const long long first = (long long)rank * a.in.slice_cols;
-  const FusedRow<T, FUSED, VEC> row(a.in, r);
-  const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
+  const int rank = (int)(blockIdx.x & (C - 1));
+  const long long r = blockIdx.x / (unsigned)C;
+  RowStream<LossCopies<T, F>, T, F, VEC> stream(a.in, r, rank, ring, nullptr);
+  const FusedRow<T, F, VEC>& row = stream.row;
+  const int k0 = stream.k0, k1 = stream.k1, items = stream.items;
   const DistillState st = a.state[r];
   const float up = a.grad_loss ? __ldg(a.grad_loss + r) : 1.f;
   T* out = static_cast<T*>(a.grad) + r * a.ld_grad - row.sh;
-  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
   if (st.weight == 0.f) {                          // left out
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
     return;
   }
-  const float g0 = up * st.weight * a.in.inv_t * (FUSED ? row.a : 1.f);
+  const float g0 = up * st.weight * a.in.inv_t * (F ? row.a : 1.f);
   const float c = a.in.scale;
-  RowStream<LossCopies<T, FUSED>, T, FUSED, VEC> stream(row, k0, k1, ring, nullptr);
   stream.begin();
 
   int id = -1;
@@ -641,7 +689,8 @@ __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs 
     if (id < 0 || id + row.sh < k0 || id + row.sh >= k1 || t == -INFINITY) id = -1;
     if (id >= 0) {
       // every entry with this id, in their order; the last of them writes
-      const float lp = (t - st.t_max) * st.t_scale - st.log_norm, x = row.at(id + row.sh);
+      const float lp = (t - st.t_max) * st.t_scale - st.log_norm;
+      const float x = row.contracted(row.l_at(id + row.sh), row.s_at(id + row.sh), row.p_at(id + row.sh));
       float before = 0.f;
       for (int k = 0; k < K; ++k) {
         if (k == tid || __ldg(a.ids + r * K + k) != id) continue;
@@ -660,11 +709,11 @@ __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs 
   __syncthreads();                                 // the output may be l_S itself
   const float k2 = g0 * st.factor;
   const Ref f{st.f_off, st.f_r};
-  stream.run([&](auto& v, auto checked, int, int) {
+  stream.run([&](auto& v, int) {
 #pragma unroll
-    for (int u = 0; u < (int)(sizeof(v) / sizeof(v[0])); ++u) {
-      float x[8], s[8], p[8], g[8];
-      v[u].template values<decltype(checked)::value>(row, k1, x, s, p);
+    for (int u = 0; u < LossCopies<T, F>::U; ++u) {
+      float x[8], s[8], g[8];
+      v[u].template values<true>(row, x, s);
       unlisted_grad(x, f, c, k2, g);
       grad_item<T, VEC>(out, v[u].k, row.sh, k1, a.grad_vec, g);
     }
@@ -680,55 +729,63 @@ __global__ void __launch_bounds__(256) k_weight_grads(DistillArgs a) {
   weight_grads<256>(a, blockIdx.x, red);
 }
 
-// Shared memory of the loss kernel: the bitmap, the ring, and with GRAD the slice's
-// values.
-template <typename T, bool FUSED, bool GRAD>
-constexpr size_t ring_bytes(bool vec) {
-  return vec ? RowCopies<T, FUSED, GRAD>::kRingBytes : 0;
+// Shared memory of the loss kernel: the bitmap (of whole groups of items), the ring,
+// and with GRAD the slice's values.
+template <typename Cp>
+size_t loss_items(const StreamRows& in) {
+  return ((size_t)in.slice_cols + Cp::U * kStreamStep - 1) / (Cp::U * kStreamStep) * Cp::U;
 }
-template <typename T, bool GRAD>
-size_t loss_smem(const StreamRows& in, bool fused, bool vec) {
-  const size_t items = ((size_t)in.slice_cols + kStreamStep - 1) / kStreamStep;
-  return ((size_t)in.slice_cols + 127) / 128 * 16 + (GRAD ? items * kStreamStep * 4 : 0) +
-         (fused ? ring_bytes<T, true, GRAD>(vec) : ring_bytes<T, false, GRAD>(vec));
-}
-
-template <typename T, bool GRAD>
-cudaError_t launch_loss_t(const DistillArgs& a, bool fused, bool vec, cudaStream_t s) {
-  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
-  auto k = fused ? (vec ? k_distill_loss<T, true, true, GRAD> : k_distill_loss<T, true, false, GRAD>)
-                 : (vec ? k_distill_loss<T, false, true, GRAD> : k_distill_loss<T, false, false, GRAD>);
-  const size_t bytes = loss_smem<T, GRAD>(a.in, fused, vec);
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
-  if (e != cudaSuccess) return e;
-  return launch_pdl_cluster(k, grid, block, bytes, s, a.in.cluster, a);
+template <typename T, int F, bool VEC, bool GRAD>
+size_t loss_smem(const StreamRows& in) {
+  using Cp = RowCopies<T, F, GRAD>;
+  const size_t items = loss_items<Cp>(in);
+  return items * (kStreamStep / 8) + (VEC ? Cp::kRingBytes : 0) + (GRAD ? items * kStreamStep * 4 : 0);
 }
 
-template <typename T>
-cudaError_t launch_grad_t(const DistillArgs& a, bool fused, bool vec, cudaStream_t s) {
-  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
-  auto k = fused ? (vec ? k_distill_grad<T, true, true> : k_distill_grad<T, true, false>)
-                 : (vec ? k_distill_grad<T, false, true> : k_distill_grad<T, false, false>);
-  const size_t bytes = fused ? ring_bytes<T, true, false>(vec) : ring_bytes<T, false, false>(vec);
+template <typename T, int F, bool VEC, bool GRAD>
+cudaError_t launch_loss_t(const DistillArgs& a, cudaStream_t s) {
+  const auto k = k_distill_loss<T, F, VEC, GRAD>;
+  const size_t bytes = loss_smem<T, F, VEC, GRAD>(a.in);
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
   if (e != cudaSuccess) return e;
-  return launch_pdl(k, grid, block, bytes, s, a);
+  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster));
+  return launch_pdl_cluster(k, grid, dim3(kStreamThreads), bytes, s, a.in.cluster, a);
+}
+
+template <typename T, int F, bool VEC>
+cudaError_t launch_grad_t(const DistillArgs& a, cudaStream_t s) {
+  const auto k = k_distill_grad<T, F, VEC>;
+  const size_t bytes = VEC ? LossCopies<T, F>::kRingBytes : 0;
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
+  if (e != cudaSuccess) return e;
+  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster));
+  return launch_pdl(k, grid, dim3(kStreamThreads), bytes, s, a);
 }
 
 }  // namespace
 
 cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
-  return f32 ? launch_loss_t<float, false>(a, fused, vec, s) : launch_loss_t<uint16_t, false>(a, fused, vec, s);
-}
-bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec) {
-  return (f32 ? loss_smem<float, true>(a.in, fused, vec) : loss_smem<uint16_t, true>(a.in, fused, vec)) <=
-         (size_t)kStepSmemBytes;
+  return dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
+    return launch_loss_t<typename decltype(t)::type, decltype(f)::value, decltype(v)::value, false>(a, s);
+  });
 }
 cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
-  return f32 ? launch_loss_t<float, true>(a, fused, vec, s) : launch_loss_t<uint16_t, true>(a, fused, vec, s);
+  return dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
+    return launch_loss_t<typename decltype(t)::type, decltype(f)::value, decltype(v)::value, true>(a, s);
+  });
+}
+bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec) {
+  size_t bytes = 0;
+  dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
+    bytes = loss_smem<typename decltype(t)::type, decltype(f)::value, decltype(v)::value, true>(a.in);
+    return cudaSuccess;
+  });
+  return bytes <= (size_t)kStepSmemBytes;
 }
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
-  return f32 ? launch_grad_t<float>(a, fused, vec, s) : launch_grad_t<uint16_t>(a, fused, vec, s);
+  return dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
+    return launch_grad_t<typename decltype(t)::type, decltype(f)::value, decltype(v)::value>(a, s);
+  });
 }
 cudaError_t launch_weight_grads(const DistillArgs& a, cudaStream_t s) {
   return launch_pdl(k_weight_grads, dim3((unsigned)a.in.n_weights), dim3(256), 0, s, a);

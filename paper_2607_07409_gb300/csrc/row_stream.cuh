@@ -90,9 +90,12 @@ struct Raw8 {
   }
 };
 
+// What a row has: l_L as stored; any of the fusion's terms (an absent one counts as
+// zero); all of them.
+enum { kPlain = 0, kSome = 1, kFull = 2 };
+
 // One row of l = (l_L + alpha l_S) - beta l_P, rounded to float32 after every
-// operation, so that equal inputs order equally wherever they are evaluated; an
-// absent term counts as zero. FUSED = false: l = l_L as stored.
+// operation, so that equal inputs order equally wherever they are evaluated.
 //
 // A thread takes items of 8 columns: consecutive ones of bf16 rows, two times four of
 // float32 rows, 4 kStreamThreads apart (a warp's 16-byte loads are side by side
@@ -101,48 +104,55 @@ struct Raw8 {
 // `sh` elements before it, so that whole items are vector loads and only a row's
 // first and last are not. Otherwise an item's columns are kStreamThreads apart (a
 // warp's lanes side by side) and sh = 0. Positions below are columns + sh.
-template <typename T, bool FUSED, bool VEC>
+template <typename T, int F, bool VEC>
 struct FusedRow {
-  const T* L;          // at position 0; FUSED: may be null
-  const T* S;          // FUSED only, may be null
-  const float* P;      // FUSED only, may be null
+  const T* L;          // at position 0; kSome: may be null
+  const T* S;          // F != kPlain; kSome: may be null
+  const float* P;
   float a, b;
   float minus_zero;    // -0, from the launch: see values()
   int sh, end;         // positions sh .. end - 1 are the row
 
   __device__ __forceinline__ FusedRow(const StreamRows& in, long long row) {
-    L = in.longp ? static_cast<const T*>(in.longp) + row * in.ld_long : nullptr;
+    L = F != kSome || in.longp ? static_cast<const T*>(in.longp) + row * in.ld_long : nullptr;
     S = nullptr;
     P = nullptr;
     a = b = 1.f;
     minus_zero = in.minus_zero;
-    if constexpr (FUSED) {
+    if constexpr (F != kPlain) {
       const unsigned j = (unsigned)row % (unsigned)in.n_weights;
-      if (in.shortp) {
+      if (F == kFull || in.shortp) {
         S = static_cast<const T*>(in.shortp) + row * in.ld_short;
         if (in.alpha) a = __ldg(in.alpha + j);
       }
-      if (in.prior) {
+      if (F == kFull || in.prior) {
         P = in.prior;
         if (in.beta) b = __ldg(in.beta + j);
       }
     }
     sh = 0;
     if constexpr (VEC) {
-      sh = (int)((reinterpret_cast<uintptr_t>(!FUSED || L ? L : S) & 15u) / sizeof(T));
-      if (!FUSED || L) L -= sh;
-      if (FUSED && S) S -= sh;
-      if (FUSED && P) P -= sh;
+      sh = (int)((reinterpret_cast<uintptr_t>(has_l() ? L : S) & 15u) / sizeof(T));
+      if (has_l()) L -= sh;
+      if (has_s()) S -= sh;
+      if (has_p()) P -= sh;
     }
     end = sh + in.V;
   }
+  __device__ __forceinline__ bool has_l() const { return F != kSome || L; }
+  __device__ __forceinline__ bool has_s() const { return F == kFull || (F == kSome && S); }
+  __device__ __forceinline__ bool has_p() const { return F == kFull || (F == kSome && P); }
   __device__ __forceinline__ float combine(float l, float s, float p) const {
-    return FUSED ? __fsub_rn(__fadd_rn(l, __fmul_rn(a, s)), __fmul_rn(b, p)) : l;
+    return F ? __fsub_rn(__fadd_rn(l, __fmul_rn(a, s)), __fmul_rn(b, p)) : l;
+  }
+  // The same in two fmas, where no order of entries hangs on the last bit.
+  __device__ __forceinline__ float contracted(float l, float s, float p) const {
+    return F ? fmaf(-b, p, fmaf(a, s, l)) : l;
   }
   // by position
-  __device__ __forceinline__ float l_at(int k) const { return !FUSED || L ? row_elem(L, k) : 0.f; }
-  __device__ __forceinline__ float s_at(int k) const { return FUSED && S ? row_elem(S, k) : 0.f; }
-  __device__ __forceinline__ float p_at(int k) const { return FUSED && P ? __ldg(P + k) : 0.f; }
+  __device__ __forceinline__ float l_at(int k) const { return has_l() ? row_elem(L, k) : 0.f; }
+  __device__ __forceinline__ float s_at(int k) const { return has_s() ? row_elem(S, k) : 0.f; }
+  __device__ __forceinline__ float p_at(int k) const { return has_p() ? __ldg(P + k) : 0.f; }
   __device__ __forceinline__ float at(int k) const { return combine(l_at(k), s_at(k), p_at(k)); }
 };
 
@@ -173,93 +183,54 @@ __device__ __forceinline__ void prior4(const float* p, int o, float* x) {
 }
 
 // One item's terms as loaded.
-template <typename T, bool FUSED, bool VEC>
+template <typename T, int F, bool VEC>
 struct Item {
   Raw8<T> l;
-  Raw8<T> s;           // FUSED only
+  Raw8<T> s;           // F != kPlain, as pr
+  float pr[8];
   int k;               // its first position
-  float pr[8];         // its l_P, where the stream has loaded it (whole items of FUSED rows)
 
-  __device__ __forceinline__ void load_whole(const FusedRow<T, FUSED, VEC>& row, int pos) {
-    k = pos;
-    if constexpr (VEC) {
-      if (!FUSED || row.L) l.load(row.L + pos, kHalf<T>);
-      else l.fill(0.f);
-      if constexpr (FUSED) {
-        if (row.S) s.load(row.S + pos, kHalf<T>);
-        else s.fill(0.f);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        l.set(i, row.l_at(elem_pos<T, VEC>(pos, i)));
-        if constexpr (FUSED) s.set(i, row.s_at(elem_pos<T, VEC>(pos, i)));
-      }
-    }
-  }
-  // As far as its positions are in the row and before `stop`: -inf (l_S: 0) elsewhere.
-  __device__ __forceinline__ void load(const FusedRow<T, FUSED, VEC>& row, int pos, int stop) {
-    if (VEC && pos >= row.sh && pos + kHalf<T> + 4 <= stop) return load_whole(row, pos);
+  // As far as its positions are in the row and before `stop`: l = -inf (l_S, l_P: 0)
+  // elsewhere.
+  __device__ __forceinline__ void load(const FusedRow<T, F, VEC>& row, int pos, int stop) {
     k = pos;
     l.fill(-INFINITY);
-    if constexpr (FUSED) s.fill(0.f);
+    if constexpr (F != kPlain) {
+      s.fill(0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pr[i] = 0.f;
+    }
     if (pos >= stop) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int q = elem_pos<T, VEC>(pos, i);
       if (q >= row.sh && q < stop) {
         l.set(i, row.l_at(q));
-        if constexpr (FUSED) s.set(i, row.s_at(q));
-      }
-    }
-  }
-  // The prior of the positions of an item at k (CHECK: 0 outside the row and from `stop` on).
-  template <bool CHECK>
-  __device__ __forceinline__ void prior(const FusedRow<T, FUSED, VEC>& row, int stop, float (&p)[8]) const {
-    if constexpr (!FUSED) return;
-    if (!row.P) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = 0.f;
-      return;
-    }
-    if constexpr (!VEC || CHECK) {
-      if (!VEC || k < row.sh || k + kHalf<T> + 4 > stop) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int q = elem_pos<T, VEC>(k, i);
-          p[i] = !CHECK || (q >= row.sh && q < stop) ? row.p_at(q) : 0.f;
+        if constexpr (F != kPlain) {
+          s.set(i, row.s_at(q));
+          pr[i] = row.p_at(q);
         }
-        return;
       }
     }
-    if constexpr (VEC) {                           // (the prior's own place against 16 bytes is -sh)
-      prior4(row.P + k, -row.sh & 3, p);
-      prior4(row.P + k + kHalf<T>, -row.sh & 3, p + 4);
-    }
   }
-  // Values of the 8 positions, and the l_S and l_P in them. The products are packed
-  // fmas with an addend of -0 that only the launch knows: a packed product that
-  // feeds a packed sum is contracted whatever its rounding modifier and the
-  // compiler's flags (seen by comparing bits), and so is one with a constant -0.
-  template <bool CHECK>
-  __device__ __forceinline__ void values(const FusedRow<T, FUSED, VEC>& row, int stop, float (&x)[8], float (&sv)[8],
-                                         float (&p)[8]) const {
+  // Values of the 8 positions, and the l_S in them. Where they are rounded after every
+  // operation the products are packed fmas with an addend of -0 that only the launch
+  // knows: a packed product that feeds a packed sum is contracted whatever its rounding
+  // modifier and the compiler's flags (seen by comparing bits), and so is one with a
+  // constant -0.
+  template <bool CONTRACT>
+  __device__ __forceinline__ void values(const FusedRow<T, F, VEC>& row, float (&x)[8], float (&sv)[8]) const {
     l.unpack(x);
-    if constexpr (!FUSED) return;
-    s.unpack(sv);
-    if constexpr (VEC && !CHECK) {
+    if constexpr (F != kPlain) {
+      s.unpack(sv);
+      const f32x2 a2 = both2(row.a), b2 = both2(-row.b);     // x - b p = x + (-b) p, both rounded alike
+      const f32x2 z2 = both2(row.minus_zero);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = pr[i];
-    } else {
-      prior<CHECK>(row, stop, p);
-    }
-    const f32x2 a2 = both2(row.a), b2 = both2(-row.b);       // x - b p = x + (-b) p, both rounded alike
-    const f32x2 z2 = both2(row.minus_zero);
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const f32x2 v = add2(add2(pair2(x[i], x[i + 1]), fma2(a2, pair2(sv[i], sv[i + 1]), z2)),
-                           fma2(b2, pair2(p[i], p[i + 1]), z2));
-      split2(v, x[i], x[i + 1]);
+      for (int i = 0; i < 8; i += 2) {
+        const f32x2 lv = pair2(x[i], x[i + 1]), s2 = pair2(sv[i], sv[i + 1]), p2 = pair2(pr[i], pr[i + 1]);
+        split2(CONTRACT ? fma2(b2, p2, fma2(a2, s2, lv)) : add2(add2(lv, fma2(a2, s2, z2)), fma2(b2, p2, z2)), x[i],
+               x[i + 1]);
+      }
     }
   }
 };
@@ -412,174 +383,162 @@ __device__ __forceinline__ void copies_wait() {
 // thread, which copies it, waits for it and reads it: no barrier. A warp's copies of a
 // piece are 512 bytes side by side.
 //
-// Items come in groups of U; a ring has D groups. With R > 0 the first two pieces of
-// every item have a place of their own that stays (32 bytes: the item's 8 values as
-// float32 later), copied R groups ahead, and the ring has the others.
-template <typename T, bool FUSED, int U_, int D_, int R_ = 0>
+// Items come in groups of U, D groups ahead, in a ring of D groups. With STAY the first
+// two pieces of every item have a place of their own (32 bytes: what 8 values take as
+// float32 later), and the ring has the others.
+template <typename T, int F, int U_, int D_, bool STAY_ = false>
 struct Copies {
-  static constexpr int U = U_, D = D_, R = R_;
+  static constexpr int U = U_, D = D_;
+  static constexpr bool STAY = STAY_;
   static constexpr int W = Raw8<T>::W;
-  static constexpr int kPieces = FUSED ? 2 * W : W;
-  static constexpr int kStay = R > 0 ? 2 : 0;
+  static constexpr int kPieces = F ? 2 * W : W;
+  static constexpr int kStay = STAY ? 2 : 0;
   static constexpr int kRing = kPieces > kStay ? kPieces - kStay : 0;
   static constexpr int kPiece = 16 * kStreamThreads;             // one piece of all threads
   static constexpr int kRingBytes = D * U * kRing * kPiece;
   static constexpr int kItemBytes = kStay * kPiece;              // per item that stays
 };
 
-struct StreamPlan {
-  int head;            // calls of the row's first item, which may not be whole: 0 or 1
-  int groups;          // calls of U whole items
-  int items;           // of a thread
-  template <int U>
-  __device__ __forceinline__ static StreamPlan of(int k0, int k1, int sh, bool vec) {
-    StreamPlan p;
-    p.items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
-    p.head = p.items > 0 && k0 < sh;
-    p.groups = vec ? max(0, (k1 - k0) / kStreamStep - p.head) / U : 0;
-    return p;
-  }
-  template <int U>
-  __device__ __forceinline__ int calls() const { return head + groups + items - head - groups * U; }
-  // First item of a call.
-  template <int U>
-  __device__ __forceinline__ int first(int call) const {
-    const int g = call - head;
-    return g <= 0 ? call : g < groups ? head + g * U : head + groups * U + (g - groups);
-  }
-};
 // The items of a thread in positions k0 .. k1 - 1 of a row (a slice, at most the
-// row's end). run() calls f(items, checked, call, it): checked = std::false_type where
-// all of them are whole for every thread, `call` the number of the call, `it` the
-// first one's number. With VEC whole items come U at a time, D - 1 such groups ahead in
-// flight and the prior one group ahead in registers; what U leaves over, and a row's
-// ends, go one by one. begin() starts the first copies; one that is not run is
-// drained.
-template <typename Cp, typename T, bool FUSED, bool VEC>
+// row's end), in groups of U. begin() starts the first copies; run() calls
+// f(items, group). Items that are not whole (at a row's ends; all without VEC) are
+// loaded where they are used.
+template <typename Cp, typename T, int F, bool VEC>
 struct RowStream {
-  static constexpr int U = Cp::U, D = Cp::D, R = Cp::R, W = Cp::W, PC = Cp::kPiece;
-  const FusedRow<T, FUSED, VEC>& row;
-  int k0, k1;
+  static constexpr int U = Cp::U, D = Cp::D, W = Cp::W, PC = Cp::kPiece;
+  FusedRow<T, F, VEC> row;
+  int k0, k1, items, groups;
   uint8_t *ring, *stay;    // the calling thread's
-  StreamPlan p;
-  int slot_in = 0;
+  const T *next_l, *next_s;// its first item of the next group to copy
+  int next_group = 0;
+  int in = 0;              // the ring's place for it, in bytes
+  int in_stay = 0;
 
-  __device__ __forceinline__ RowStream(const FusedRow<T, FUSED, VEC>& r, int from, int to, uint8_t* ring_, uint8_t* stay_)
-      : row(r), k0(from), k1(to), ring(ring_ + threadIdx.x * 16), stay(stay_ + threadIdx.x * 16),
-        p(StreamPlan::of<U>(from, to, r.sh, VEC)) {}
-  // Piece k of item i of the groups, which is in place q of the ring.
-  __device__ __forceinline__ uint8_t* place(int k, int i, int q) const {
-    return k < Cp::kStay ? stay + (size_t)(p.head + i) * Cp::kItemBytes + k * PC
-                         : ring + (q * Cp::kRing + k - Cp::kStay) * PC;
+  __device__ __forceinline__ RowStream(const StreamRows& rows, long long r, int rank, uint8_t* ring_, uint8_t* stay_)
+      : row(rows, r), ring(ring_ + threadIdx.x * 16), stay(stay_ + threadIdx.x * 16) {
+    const long long first = (long long)rank * rows.slice_cols;
+    k0 = (int)min(first, (long long)row.end);
+    k1 = (int)min(first + rows.slice_cols, (long long)row.end);
+    items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
+    groups = (items + U - 1) / U;
+    next_l = row.L + item_pos<T, VEC>(k0, 0, threadIdx.x);
+    next_s = row.S + item_pos<T, VEC>(k0, 0, threadIdx.x);
   }
-  __device__ __forceinline__ void copy(int i, int q, int from, int to) const {
-    const int at = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
+  __device__ __forceinline__ bool whole(int pos) const { return VEC && pos >= row.sh && pos + kHalf<T> + 4 <= k1; }
+  // Whether some thread's item of group g is not whole.
+  __device__ __forceinline__ bool ragged(int g) const {
+    return !VEC || (g == 0 && k0 < row.sh) || k0 + (g + 1) * U * kStreamStep > k1;
+  }
+  // Piece k of item u of a group at `rg` in the ring, `st` among those that stay.
+  __device__ __forceinline__ uint8_t* place(int k, int u, int rg, int st) const {
+    return k < Cp::kStay ? stay + st + u * Cp::kItemBytes + k * PC : ring + rg + (u * Cp::kRing + k - Cp::kStay) * PC;
+  }
+  __device__ __forceinline__ void copy(int u) const {
 #pragma unroll
     for (int k = 0; k < Cp::kPieces; ++k) {
-      if (k < from || k >= to) continue;
-      const uint32_t dst = smem_u32(place(k, i, q));
+      const uint32_t dst = smem_u32(place(k, u, in, in_stay));
       if (k < W) {
-        if (!FUSED || row.L) copy16(dst, row.L + at + k * kHalf<T>);
+        if (row.has_l()) copy16(dst, next_l + u * kStreamStep + k * kHalf<T>);
       } else {
-        if (row.S) copy16(dst, row.S + at + (k - W) * kHalf<T>);
+        if (row.has_s()) copy16(dst, next_s + u * kStreamStep + (k - W) * kHalf<T>);
       }
     }
   }
-  // What is copied when call g begins: the ring pieces of group g + D - 1 and those that
-  // stay of group g + R - 1; one commit a call, empty at the end, so that at most
-  // D - 1 later ones are in flight when group g is waited for.
-  __device__ __forceinline__ void issue(int g) {
-    if (Cp::kRing > 0 && g < p.groups) {
+  // The next group's copies, one commit (empty past the last).
+  __device__ __forceinline__ void fetch() {
+    if (next_group < groups) {
+      if (!ragged(next_group)) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) copy(g * U + u, slot_in * U + u, Cp::kStay, Cp::kPieces);
-      slot_in = slot_in + 1 == D ? 0 : slot_in + 1;
-    }
-  }
-  __device__ __forceinline__ void issue_stay(int g) const {
-    if (R > 0 && g < p.groups) {
+        for (int u = 0; u < U; ++u) copy(u);
+      } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) copy(g * U + u, 0, 0, Cp::kStay);
+        for (int u = 0; u < U; ++u)
+          if (whole(item_pos<T, VEC>(k0, next_group * U + u, threadIdx.x))) copy(u);
+      }
+      ++next_group;
+      next_l += U * kStreamStep;
+      next_s += U * kStreamStep;
+      in = in == (D - 1) * U * Cp::kRing * PC ? 0 : in + U * Cp::kRing * PC;
+      in_stay += U * Cp::kItemBytes;
     }
+    copies_commit();
   }
   __device__ __forceinline__ void begin() {
     if constexpr (VEC) {
-#pragma unroll
-      for (int d = 0; d < D - 1; ++d) {
-        issue(d);
-        if (d < R - 1) issue_stay(d);
-        copies_commit();
-      }
 #pragma unroll 1
-      for (int g = D - 1; g < R - 1; ++g) issue_stay(g);
+      for (int d = 0; d < D; ++d) fetch();
     }
   }
   __device__ __forceinline__ void drain() const {
     if constexpr (VEC) copies_wait<0>();
   }
-  __device__ __forceinline__ void prior_of(int g, float (&x)[U][8]) const {
-    if constexpr (FUSED && VEC) {
+  __device__ __forceinline__ void take(Item<T, F, VEC>& v, int u, int out, int out_stay) const {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (row.P && g < p.groups) {
-          const int at = item_pos<T, VEC>(k0, p.head + g * U + u, threadIdx.x);
-          prior4(row.P + at, -row.sh & 3, x[u]);             // (its own place against 16 bytes is -sh)
-          prior4(row.P + at + kHalf<T>, -row.sh & 3, x[u] + 4);
+    for (int k = 0; k < W; ++k) {
+      if (row.has_l()) v.l.w[k] = *reinterpret_cast<const uint4*>(place(k, u, out, out_stay));
+      if constexpr (F != kPlain) {
+        if (row.has_s()) v.s.w[k] = *reinterpret_cast<const uint4*>(place(W + k, u, out, out_stay));
+      }
+    }
+    if (!row.has_l()) v.l.fill(0.f);
+    if constexpr (F != kPlain) {
+      if (!row.has_s()) v.s.fill(0.f);
+    }
+  }
+  __device__ __forceinline__ void take_prior(Item<T, F, VEC>& v, int pos) const {
+    if constexpr (F != kPlain) {
+      if (row.has_p()) {
+        const int o = -row.sh & 3;                 // (its own place against 16 bytes is -sh)
+        if (o == 0) {
+          const float4 x = __ldg(reinterpret_cast<const float4*>(row.P + pos));
+          const float4 y = __ldg(reinterpret_cast<const float4*>(row.P + pos + kHalf<T>));
+          v.pr[0] = x.x; v.pr[1] = x.y; v.pr[2] = x.z; v.pr[3] = x.w;
+          v.pr[4] = y.x; v.pr[5] = y.y; v.pr[6] = y.z; v.pr[7] = y.w;
         } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[u][i] = 0.f;
+          prior4(row.P + pos, o, v.pr);
+          prior4(row.P + pos + kHalf<T>, o, v.pr + 4);
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v.pr[j] = 0.f;
       }
     }
   }
-  template <typename F>
-  __device__ __forceinline__ void run(F&& f) {
-    int it = 0, call = 0;
-    auto one = [&]() {
-      Item<T, FUSED, VEC> v[1];
-      v[0].load(row, item_pos<T, VEC>(k0, it, threadIdx.x), k1);
-      f(v, std::true_type{}, call, it);
-      ++it;
-      ++call;
-    };
-    if constexpr (VEC) {
-      float pn[U][8];
-      prior_of(0, pn);
-      if (p.head) one();
-      int slot = 0;
+  template <typename Fn>
+  __device__ __forceinline__ void run(Fn&& f) {
+    int out = 0, out_stay = 0, pos = item_pos<T, VEC>(k0, 0, threadIdx.x);
 #pragma unroll 1
-      for (int g = 0; g < p.groups; ++g) {
-        issue(g + D - 1);
-        issue_stay(g + R - 1);
-        copies_commit();
-        copies_wait<D - 1>();
-        Item<T, FUSED, VEC> v[U];
+    for (int g = 0; g < groups; ++g) {
+      Item<T, F, VEC> v[U];
+      if (!ragged(g)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int i = g * U + u, q = slot * U + u;
-          v[u].k = item_pos<T, VEC>(k0, p.head + i, threadIdx.x);
+          v[u].k = pos + u * kStreamStep;
+          take_prior(v[u], pos + u * kStreamStep);
+        }
+        copies_wait<D - 1>();
 #pragma unroll
-          for (int k = 0; k < W; ++k) {
-            if (!FUSED || row.L) v[u].l.w[k] = *reinterpret_cast<const uint4*>(place(k, i, q));
-            if constexpr (FUSED) {
-              if (row.S) v[u].s.w[k] = *reinterpret_cast<const uint4*>(place(W + k, i, q));
-            }
-          }
-          if (FUSED && !row.L) v[u].l.fill(0.f);
-          if constexpr (FUSED) {
-            if (!row.S) v[u].s.fill(0.f);
+        for (int u = 0; u < U; ++u) take(v[u], u, out, out_stay);
+      } else {
+        copies_wait<D - 1>();
 #pragma unroll
-            for (int i2 = 0; i2 < 8; ++i2) v[u].pr[i2] = pn[u][i2];
+        for (int u = 0; u < U; ++u) {
+          if (whole(pos + u * kStreamStep)) {
+            v[u].k = pos + u * kStreamStep;
+            take_prior(v[u], pos + u * kStreamStep);
+            take(v[u], u, out, out_stay);
+          } else {
+            v[u].load(row, pos + u * kStreamStep, k1);
           }
         }
-        prior_of(g + 1, pn);
-        f(v, std::false_type{}, call, it);
-        it += U;
-        ++call;
-        slot = slot + 1 == D ? 0 : slot + 1;
       }
-      copies_wait<0>();
+      f(v, g);
+      if constexpr (VEC) fetch();
+      pos += U * kStreamStep;
+      out = out == (D - 1) * U * Cp::kRing * PC ? 0 : out + U * Cp::kRing * PC;
+      out_stay += U * Cp::kItemBytes;
     }
-    while (it < p.items) one();
+    drain();
   }
 };
 
@@ -589,5 +548,26 @@ __device__ __forceinline__ void cluster_arrive_relaxed() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// The kernel of a call: its logits' type, its rows' terms, and whether they lie alike
+// against 16-byte boundaries. launch(type, terms, vec) takes them as types.
+template <typename T>
+struct TypeOf {
+  using type = T;
+};
+template <typename Launch>
+cudaError_t dispatch_rows(const StreamRows& in, bool f32, bool fused, bool vec, Launch&& launch) {
+  const bool full = in.longp && in.shortp && in.prior;
+  const auto with_terms = [&](auto type) {
+    using std::integral_constant;
+    if (!fused)
+      return vec ? launch(type, integral_constant<int, kPlain>{}, std::true_type{})
+                 : launch(type, integral_constant<int, kPlain>{}, std::false_type{});
+    if (full && vec) return launch(type, integral_constant<int, kFull>{}, std::true_type{});
+    return vec ? launch(type, integral_constant<int, kSome>{}, std::true_type{})
+               : launch(type, integral_constant<int, kSome>{}, std::false_type{});
+  };
+  return f32 ? with_terms(TypeOf<float>{}) : with_terms(TypeOf<uint16_t>{});
+}
 
 }  // namespace dels

@@ -62,13 +62,15 @@ __device__ void sort_best(ScoreShared& sh, const unsigned long long* cand, int n
 }
 
 // The entries of an item that reach `floor_key`, into cand[] as far as it has room.
-template <typename T, bool FUSED, bool VEC>
-__device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel, const FusedRow<T, FUSED, VEC>& row,
+template <typename T, int F, bool VEC>
+__device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel, const FusedRow<T, F, VEC>& row,
                                              int pos, int k1, unsigned long long floor_key) {
-  Item<T, FUSED, VEC> v;
-  v.load(row, pos, k1);
-  float x[8], s[8], p[8];
-  v.template values<true>(row, k1, x, s, p);
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int q = elem_pos<T, VEC>(pos, i);
+    x[i] = q >= row.sh && q < k1 ? row.at(q) : -INFINITY;
+  }
   const float least = from_order_u32((unsigned)(floor_key >> 32));
   if (!(max8(x) >= least)) return;
 #pragma unroll
@@ -82,14 +84,14 @@ __device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel,
 }
 
 // This CTA's K largest entries of its slice into sh.best. `top`: the largest
-// entry of the calling thread; bmax: [slot][thread] the largest of a thread's calls
+// entry of the calling thread; bmax: [slot][thread] the largest of a thread's groups
 // slot << shift .. of the stream.
-template <int U, typename T, bool FUSED, bool VEC>
+template <int U, typename T, int F, bool VEC>
 __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax, int shift,
-                          const FusedRow<T, FUSED, VEC>& row, int k0, int k1, int K, float top) {
+                          const FusedRow<T, F, VEC>& row, int k0, int k1, int K, float top) {
   const int tid = threadIdx.x;
-  const StreamPlan p = StreamPlan::of<U>(k0, k1, row.sh, VEC);
-  const int calls = p.template calls<U>(), slots = (calls + (1 << shift) - 1) >> shift;
+  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep, groups = (items + U - 1) / U;
+  const int slots = (groups + (1 << shift) - 1) >> shift;
   // About the K-th largest thread maximum, from its highest bit down; -inf where
   // fewer than K threads have an entry.
   const unsigned key = top > -INFINITY ? order_u32(top) : 0u;
@@ -120,10 +122,8 @@ __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax,
     const int per = U << shift, n = sh.njobs * per;
     for (int i = tid; i < n; i += kStreamThreads) {
       const int job = sel.jobs[i / per], o = i % per;
-      const int call0 = (job / kStreamThreads) << shift;
-      const int it = p.template first<U>(call0) + o;
-      const int end = p.template first<U>(min(call0 + (1 << shift), calls));
-      if (it >= end || it >= p.items) continue;
+      const int it = (job / kStreamThreads) * per + o;
+      if (it >= items) continue;
       keep_entries(sh, sel, row, item_pos<T, VEC>(k0, it, job % kStreamThreads), k1, floor_key);
     }
   }
@@ -134,7 +134,7 @@ __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax,
     __syncthreads();
     if (tid == 0) sh.ncand = 0;
     __syncthreads();
-    for (int j = 0; j < 2 * p.items; ++j) {
+    for (int j = 0; j < 2 * items; ++j) {
       const int n = sh.ncand;
       __syncthreads();
       if (n > kCandidates - 128 * 8) {
@@ -165,27 +165,27 @@ __device__ __forceinline__ void raise8_bf16(uint4& w, __nv_bfloat162 low) {
 }
 
 // Copies ahead: 32 KB of plain rows (four CTAs on an SM), 48 KB of two rows (three).
-template <typename T, bool FUSED>
-using ScoreCopies = Copies<T, FUSED, sizeof(T) == 2 ? 2 : 1, FUSED ? 3 : 4>;
+template <typename T, int F>
+using ScoreCopies = Copies<T, F, sizeof(T) == 2 ? 2 : 1, F ? 3 : 4>;
 
 // Dynamic shared memory: the ring (later SelectShared), the block maxima, and for a
 // cluster the entries of all slices.
-template <typename T, bool FUSED, bool VEC>
+template <typename T, int F, bool VEC>
 constexpr size_t ring_bytes() {
-  const size_t ring = VEC ? ScoreCopies<T, FUSED>::kRingBytes : 0;
+  const size_t ring = VEC ? ScoreCopies<T, F>::kRingBytes : 0;
   return ring > sizeof(SelectShared) ? ring : sizeof(SelectShared);
 }
 
-template <typename T, bool FUSED, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, FUSED ? 3 : 4) k_score_rows(ScoreArgs a) {
+template <typename T, int F, bool VEC>
+__global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreArgs a) {
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ ScoreShared sh;
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = a.in.cluster, K = a.top_k;
-  const int rank = (int)(blockIdx.x % C);
-  const long long r = blockIdx.x / C;
+  const int rank = (int)(blockIdx.x & (C - 1));
+  const long long r = blockIdx.x / (unsigned)C;
   const int V = a.in.V;
   const float c = a.in.scale;
   const int tok = a.tokens ? __ldg(a.tokens + r) : 0;
@@ -203,30 +203,29 @@ __global__ void __launch_bounds__(kStreamThreads, FUSED ? 3 : 4) k_score_rows(Sc
     return;
   }
   if (C > 1) cluster_arrive_relaxed();
-  const FusedRow<T, FUSED, VEC> row(a.in, r);
+  using Cp = ScoreCopies<T, F>;
+  RowStream<Cp, T, F, VEC> stream(a.in, r, rank, dyn, nullptr);
+  stream.begin();
+  const FusedRow<T, F, VEC>& row = stream.row;
+  const int k0 = stream.k0, k1 = stream.k1;
   const bool tok_ok = tok >= 0 && tok < V;
   float x_tok = 0.f;
   if (rank == 0 && tid == 0 && a.tokens && tok_ok) x_tok = row.at(tok + row.sh);
-  const long long first = (long long)rank * a.in.slice_cols;
-  const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
 
-  using Cp = ScoreCopies<T, FUSED>;
   constexpr int U = Cp::U;
-  float* bmax = reinterpret_cast<float*>(dyn + ring_bytes<T, FUSED, VEC>());
+  float* bmax = reinterpret_cast<float*>(dyn + ring_bytes<T, F, VEC>());
   unsigned long long* slices = reinterpret_cast<unsigned long long*>(bmax + (K > 0 ? kSlots * kStreamThreads : 0));
-  int shift = 0;                   // calls per block maximum: 1 << shift
-  while (((StreamPlan::of<U>(k0, k1, row.sh, VEC).template calls<U>() - 1) >> shift) >= kSlots) ++shift;
+  int shift = 0;                   // groups per block maximum: 1 << shift
+  while (((stream.groups - 1) >> shift) >= kSlots) ++shift;
 
-  RowStream<Cp, T, FUSED, VEC> stream(row, k0, k1, dyn, nullptr);
-  stream.begin();
   WarpSoft st;
   st.init();
   float top = -INFINITY, block = -INFINITY;
   const __nv_bfloat162 low2 = __float2bfloat162_rn(a.low);
-  stream.run([&](auto& v, auto checked, int call, int) {
-    constexpr int N = sizeof(v) / sizeof(v[0]);
+  stream.run([&](auto& v, int g) {
+    constexpr int N = U;
     float vm = -INFINITY;
-    if constexpr (sizeof(T) == 2 && !FUSED) {
+    if constexpr (sizeof(T) == 2 && F == kPlain) {
       // bf16 as stored: the maximum and the clamp of masked entries on pairs
 #pragma unroll
       for (int u = 0; u < N; ++u) vm = fmaxf(vm, max8_bf16(v[u].l.w[0]));
@@ -262,10 +261,10 @@ __global__ void __launch_bounds__(kStreamThreads, FUSED ? 3 : 4) k_score_rows(Sc
         st.template add<true>(x, c);
       }
     } else {
-      float x[N][8], s[8], p[8];
+      float x[N][8], s[8];
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        v[u].template values<decltype(checked)::value>(row, k1, x[u], s, p);
+        v[u].template values<false>(row, x[u], s);
         vm = fmaxf(vm, max8(x[u]));
       }
       if (__any_sync(0xFFFFFFFFu, vm > st.m)) {
@@ -291,8 +290,8 @@ __global__ void __launch_bounds__(kStreamThreads, FUSED ? 3 : 4) k_score_rows(Sc
     }
     if (K > 0) {
       top = fmaxf(top, vm);
-      block = (call & ((1 << shift) - 1)) == 0 ? vm : fmaxf(block, vm);
-      bmax[(call >> shift) * kStreamThreads + tid] = block;
+      block = (g & ((1 << shift) - 1)) == 0 ? vm : fmaxf(block, vm);
+      bmax[(g >> shift) * kStreamThreads + tid] = block;
     }
   });
   const SoftRec wr = st.record();
@@ -339,24 +338,23 @@ __global__ void __launch_bounds__(kStreamThreads, FUSED ? 3 : 4) k_score_rows(Sc
   }
 }
 
-template <typename T>
-cudaError_t launch_score_t(const ScoreArgs& a, bool fused, bool vec, cudaStream_t s) {
-  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster)), block(kStreamThreads);
-  auto k = fused ? (vec ? k_score_rows<T, true, true> : k_score_rows<T, true, false>)
-                 : (vec ? k_score_rows<T, false, true> : k_score_rows<T, false, false>);
-  const size_t ring = fused ? (vec ? ring_bytes<T, true, true>() : ring_bytes<T, true, false>())
-                            : (vec ? ring_bytes<T, false, true>() : ring_bytes<T, false, false>());
-  const size_t bytes = ring + (a.top_k > 0 ? (size_t)kSlots * kStreamThreads * 4 : 0) +
+template <typename T, int F, bool VEC>
+cudaError_t launch_score_t(const ScoreArgs& a, cudaStream_t s) {
+  const auto k = k_score_rows<T, F, VEC>;
+  const size_t bytes = ring_bytes<T, F, VEC>() + (a.top_k > 0 ? (size_t)kSlots * kStreamThreads * 4 : 0) +
                        (a.in.cluster > 1 ? (size_t)a.in.cluster * a.top_k * 8 : 0);
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
   if (e != cudaSuccess) return e;
-  return launch_pdl_cluster(k, grid, block, bytes, s, a.in.cluster, a);
+  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster));
+  return launch_pdl_cluster(k, grid, dim3(kStreamThreads), bytes, s, a.in.cluster, a);
 }
 
 }  // namespace
 
 cudaError_t launch_score_rows(const ScoreArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
-  return f32 ? launch_score_t<float>(a, fused, vec, s) : launch_score_t<uint16_t>(a, fused, vec, s);
+  return dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
+    return launch_score_t<typename decltype(t)::type, decltype(f)::value, decltype(v)::value>(a, s);
+  });
 }
 
 }  // namespace dels
