@@ -100,8 +100,8 @@ struct WarpTail {
     sum = s = p = 0ull;
   }
   // N items' values, all lanes converged: x becomes 2^z.
-  template <int N, typename It>
-  __device__ __forceinline__ void push(float (&x)[N][8], const float (&sv)[N][8], const It (&v)[N], float c,
+  template <int N>
+  __device__ __forceinline__ void push(float (&x)[N][8], const float (&sv)[N][8], const float (&pr)[N][8], float c,
                                        float p_ref) {
     if (m == -INFINITY) {
       float vm = max8(x[0]);
@@ -129,7 +129,7 @@ struct WarpTail {
         sum = add2(sum, e);
         if constexpr (FUSED) {
           s = fma2(e, pair2(sv[u][i], sv[u][i + 1]), s);
-          p = fma2(e, add2(pair2(v[u].pr[i], v[u].pr[i + 1]), np), p);
+          p = fma2(e, add2(pair2(pr[u][i], pr[u][i + 1]), np), p);
         }
       }
   }
@@ -483,12 +483,12 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   // the columns that are not listed
   WarpTail<F != kPlain> st;
   st.init();
-  stream.run([&](auto& v, int g) {
+  stream.run([&](auto& v, auto& pr, int g) {
     constexpr int N = Cp::U;
     float x[N][8], s[N][8];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      v[u].template values<true>(row, x[u], s[u]);
+      v[u].template values<true>(row, pr[u], x[u], s[u]);
       if constexpr (VEC) {
         // the item's 8 bits (positions past the slice are -inf already, their bits 0)
         const int b = v[u].k - k0;
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
         }
       }
     }
-    st.push(x, s, v, c, p_ref);
+    st.push(x, s, pr, c, p_ref);
     if constexpr (GRAD) {
       float4* keep = reinterpret_cast<float4*>(kept) + g * (N * 2 * kStreamThreads) + tid;
 #pragma unroll
@@ -709,11 +709,11 @@ __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs 
   __syncthreads();                                 // the output may be l_S itself
   const float k2 = g0 * st.factor;
   const Ref f{st.f_off, st.f_r};
-  stream.run([&](auto& v, int) {
+  stream.run([&](auto& v, auto& pr, int) {
 #pragma unroll
     for (int u = 0; u < LossCopies<T, F>::U; ++u) {
       float x[8], s[8], g[8];
-      v[u].template values<true>(row, x, s);
+      v[u].template values<true>(row, pr[u], x, s);
       unlisted_grad(x, f, c, k2, g);
       grad_item<T, VEC>(out, v[u].k, row.sh, k1, a.grad_vec, g);
     }

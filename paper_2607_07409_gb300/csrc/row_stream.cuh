@@ -186,13 +186,12 @@ __device__ __forceinline__ void prior4(const float* p, int o, float* x) {
 template <typename T, int F, bool VEC>
 struct Item {
   Raw8<T> l;
-  Raw8<T> s;           // F != kPlain, as pr
-  float pr[8];
+  Raw8<T> s;           // F != kPlain
   int k;               // its first position
 
   // As far as its positions are in the row and before `stop`: l = -inf (l_S, l_P: 0)
   // elsewhere.
-  __device__ __forceinline__ void load(const FusedRow<T, F, VEC>& row, int pos, int stop) {
+  __device__ __forceinline__ void load(const FusedRow<T, F, VEC>& row, int pos, int stop, float (&pr)[8]) {
     k = pos;
     l.fill(-INFINITY);
     if constexpr (F != kPlain) {
@@ -219,7 +218,8 @@ struct Item {
   // modifier and the compiler's flags (seen by comparing bits), and so is one with a
   // constant -0.
   template <bool CONTRACT>
-  __device__ __forceinline__ void values(const FusedRow<T, F, VEC>& row, float (&x)[8], float (&sv)[8]) const {
+  __device__ __forceinline__ void values(const FusedRow<T, F, VEC>& row, const float (&pr)[8], float (&x)[8],
+                                         float (&sv)[8]) const {
     l.unpack(x);
     if constexpr (F != kPlain) {
       s.unpack(sv);
@@ -401,8 +401,10 @@ struct Copies {
 
 // The items of a thread in positions k0 .. k1 - 1 of a row (a slice, at most the
 // row's end), in groups of U. begin() starts the first copies; run() calls
-// f(items, group). Items that are not whole (at a row's ends; all without VEC) are
-// loaded where they are used.
+// f(items, l_P, group). Items that are not whole (at a row's ends; all without VEC) are
+// loaded where they are used. The prior comes out of L2 into registers a group ahead:
+// two sets of them, one for each of two bodies of the loop (copies between them took 8
+// instructions an item, and loads without a group between 700 cycles a group).
 template <typename Cp, typename T, int F, bool VEC>
 struct RowStream {
   static constexpr int U = Cp::U, D = Cp::D, W = Cp::W, PC = Cp::kPiece;
@@ -485,58 +487,72 @@ struct RowStream {
       if (!row.has_s()) v.s.fill(0.f);
     }
   }
-  __device__ __forceinline__ void take_prior(Item<T, F, VEC>& v, int pos) const {
+  // l_P of group g, whose first item of the thread is at pos (0 for what is not whole).
+  __device__ __forceinline__ void take_prior(float (&pr)[U][8], int g, int pos) const {
     if constexpr (F != kPlain) {
-      if (row.has_p()) {
-        const int o = -row.sh & 3;                 // (its own place against 16 bytes is -sh)
-        if (o == 0) {
-          const float4 x = __ldg(reinterpret_cast<const float4*>(row.P + pos));
-          const float4 y = __ldg(reinterpret_cast<const float4*>(row.P + pos + kHalf<T>));
-          v.pr[0] = x.x; v.pr[1] = x.y; v.pr[2] = x.z; v.pr[3] = x.w;
-          v.pr[4] = y.x; v.pr[5] = y.y; v.pr[6] = y.z; v.pr[7] = y.w;
-        } else {
-          prior4(row.P + pos, o, v.pr);
-          prior4(row.P + pos + kHalf<T>, o, v.pr + 4);
-        }
-      } else {
+      if (g >= groups) return;
+      const int o = -row.sh & 3;                   // (its own place against 16 bytes is -sh)
+      const float* p = row.P + pos;
+      if (row.has_p() && o == 0 && !ragged(g)) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.pr[j] = 0.f;
+        for (int u = 0; u < U; ++u) {
+          const float4 x = __ldg(reinterpret_cast<const float4*>(p + u * kStreamStep));
+          const float4 y = __ldg(reinterpret_cast<const float4*>(p + u * kStreamStep + kHalf<T>));
+          pr[u][0] = x.x; pr[u][1] = x.y; pr[u][2] = x.z; pr[u][3] = x.w;
+          pr[u][4] = y.x; pr[u][5] = y.y; pr[u][6] = y.z; pr[u][7] = y.w;
+        }
+        return;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (row.has_p() && whole(pos + u * kStreamStep)) {
+          prior4(p + u * kStreamStep, o, pr[u]);
+          prior4(p + u * kStreamStep + kHalf<T>, o, pr[u] + 4);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) pr[u][j] = 0.f;
+        }
       }
     }
   }
   template <typename Fn>
   __device__ __forceinline__ void run(Fn&& f) {
     int out = 0, out_stay = 0, pos = item_pos<T, VEC>(k0, 0, threadIdx.x);
-#pragma unroll 1
-    for (int g = 0; g < groups; ++g) {
+    float pa[U][8], pb[U][8];
+    take_prior(pa, 0, pos);
+    auto body = [&](int g, float (&pr)[U][8], float (&ahead)[U][8]) {
       Item<T, F, VEC> v[U];
+      take_prior(ahead, g + 1, pos + U * kStreamStep);
+      copies_wait<D - 1>();
       if (!ragged(g)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           v[u].k = pos + u * kStreamStep;
-          take_prior(v[u], pos + u * kStreamStep);
+          take(v[u], u, out, out_stay);
         }
-        copies_wait<D - 1>();
-#pragma unroll
-        for (int u = 0; u < U; ++u) take(v[u], u, out, out_stay);
       } else {
-        copies_wait<D - 1>();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          if (whole(pos + u * kStreamStep)) {
-            v[u].k = pos + u * kStreamStep;
-            take_prior(v[u], pos + u * kStreamStep);
-            take(v[u], u, out, out_stay);
-          } else {
-            v[u].load(row, pos + u * kStreamStep, k1);
-          }
+          v[u].k = pos + u * kStreamStep;
+          if (whole(pos + u * kStreamStep)) take(v[u], u, out, out_stay);
+          else v[u].load(row, pos + u * kStreamStep, k1, pr[u]);
         }
       }
-      f(v, g);
+      f(v, pr, g);
       if constexpr (VEC) fetch();
       pos += U * kStreamStep;
       out = out == (D - 1) * U * Cp::kRing * PC ? 0 : out + U * Cp::kRing * PC;
       out_stay += U * Cp::kItemBytes;
+    };
+    if constexpr (F == kPlain) {
+#pragma unroll 1
+      for (int g = 0; g < groups; ++g) body(g, pa, pa);
+    } else {
+#pragma unroll 1
+      for (int g = 0; g < groups; g += 2) {
+        body(g, pa, pb);
+        if (g + 1 < groups) body(g + 1, pb, pa);
+      }
     }
     drain();
   }

@@ -166,7 +166,7 @@ __device__ __forceinline__ void raise8_bf16(uint4& w, __nv_bfloat162 low) {
 
 // Copies ahead: 32 KB of plain rows (four CTAs on an SM), 48 KB of two rows (three).
 template <typename T, int F>
-using ScoreCopies = Copies<T, F, sizeof(T) == 2 ? 2 : 1, F ? 3 : 4>;
+using ScoreCopies = Copies<T, F, sizeof(T) == 2 && !F ? 2 : 1, sizeof(T) == 2 && F ? 6 : F ? 3 : 4>;
 
 // Dynamic shared memory: the ring (later SelectShared), the block maxima, and for a
 // cluster the entries of all slices.
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
   st.init();
   float top = -INFINITY, block = -INFINITY;
   const __nv_bfloat162 low2 = __float2bfloat162_rn(a.low);
-  stream.run([&](auto& v, int g) {
+  stream.run([&](auto& v, auto& pr, int g) {
     constexpr int N = U;
     float vm = -INFINITY;
     if constexpr (sizeof(T) == 2 && F == kPlain) {
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
       float x[N][8], s[8];
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        v[u].template values<false>(row, x[u], s);
+        v[u].template values<false>(row, pr[u], x[u], s);
         vm = fmaxf(vm, max8(x[u]));
       }
       if (__any_sync(0xFFFFFFFFu, vm > st.m)) {
