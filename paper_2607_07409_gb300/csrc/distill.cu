@@ -562,23 +562,6 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   const RowSums sums(tail, listed, te, a.tail != 0, c);
   const bool ok = sums.ok && !(flags & kFlagBadLogit);
   const float up = weight * inv_t * (F ? row.a : 1.f);   // dL/dl -> what the gradient holds
-  if constexpr (GRAD) {
-    // this warp's 2^z are relative to its own reference
-    const float k2 = ok ? up * sums.factor * (rec.t.m > -INFINITY ? ex2_approx(ref_shift(rec.t.f, sums.f, c)) : 0.f) : NAN;
-    const f32x2 kk = both2(k2);
-    const float4* got = reinterpret_cast<const float4*>(kept) + tid;
-#pragma unroll 2
-    for (int it = 0; it < stream.items; ++it) {
-      const float4 y = got[it * 2 * kStreamThreads], w = got[(it * 2 + 1) * kStreamThreads];
-      float gr[8];
-      split2(mul2(kk, pair2(y.x, y.y)), gr[0], gr[1]);
-      split2(mul2(kk, pair2(y.z, y.w)), gr[2], gr[3]);
-      split2(mul2(kk, pair2(w.x, w.y)), gr[4], gr[5]);
-      split2(mul2(kk, pair2(w.z, w.w)), gr[6], gr[7]);
-      grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, gr);
-    }
-  }
-
   // the listed columns' share of the loss and of the weights' gradients, to the first CTA
   float g_k = 0.f;
   if (warp * 32 < K) {
@@ -606,7 +589,25 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
     }
   }
   __syncwarp();
+  // (before the gradient is written: the arrival waits for every store before it)
   if (C > 1) cluster_arrive();
+  if constexpr (GRAD) {
+    // this warp's 2^z are relative to its own reference
+    const float k2 = ok ? up * sums.factor * (rec.t.m > -INFINITY ? ex2_approx(ref_shift(rec.t.f, sums.f, c)) : 0.f) : NAN;
+    const f32x2 kk = both2(k2);
+    const float4* got = reinterpret_cast<const float4*>(kept) + tid;
+#pragma unroll 2
+    for (int it = 0; it < stream.items; ++it) {
+      const float4 y = got[it * 2 * kStreamThreads], w = got[(it * 2 + 1) * kStreamThreads];
+      float gr[8];
+      split2(mul2(kk, pair2(y.x, y.y)), gr[0], gr[1]);
+      split2(mul2(kk, pair2(y.z, y.w)), gr[2], gr[3]);
+      split2(mul2(kk, pair2(w.x, w.y)), gr[4], gr[5]);
+      split2(mul2(kk, pair2(w.z, w.w)), gr[6], gr[7]);
+      grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, gr);
+    }
+  }
+
   if (GRAD || C == 1) __syncthreads();             // the unlisted columns' gradients are written
   if constexpr (GRAD) {
     if (flags & kFlagTwice) twice_grads(a, sh, r, mine, id, g_k, out + k0 + at);
