@@ -99,39 +99,30 @@ struct WarpTail {
     f = Ref{0.f, 0.f};
     sum = s = p = 0ull;
   }
-  // N items' values, all lanes converged: x becomes 2^z.
-  template <int N>
-  __device__ __forceinline__ void push(float (&x)[N][8], const float (&sv)[N][8], const float (&pr)[N][8], float c,
-                                       float p_ref) {
+  // One item's values, all lanes converged: x becomes 2^z.
+  __device__ __forceinline__ void push(float (&x)[8], const float (&sv)[8], const float (&pr)[8], float c, float p_ref) {
     if (m == -INFINITY) {
-      float vm = max8(x[0]);
-#pragma unroll
-      for (int u = 1; u < N; ++u) vm = fmaxf(vm, max8(x[u]));
-      m = warp_max(vm);
+      m = warp_max(max8(x));
       if (m > -INFINITY) f = make_ref(m, c);
     }
     if (f.off != 0.f) {
 #pragma unroll
-      for (int u = 0; u < N; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[u][i] -= f.off;
+      for (int i = 0; i < 8; ++i) x[i] -= f.off;
     }
     const f32x2 c2 = both2(c), nr = both2(-f.r), np = both2(-p_ref);
 #pragma unroll
-    for (int i = 0; i < 8; i += 2)
-#pragma unroll
-      for (int u = 0; u < N; ++u) {
-        float z0, z1;
-        split2(fma2(pair2(x[u][i], x[u][i + 1]), c2, nr), z0, z1);
-        x[u][i] = ex2_approx(z0);
-        x[u][i + 1] = ex2_approx(z1);
-        const f32x2 e = pair2(x[u][i], x[u][i + 1]);
-        sum = add2(sum, e);
-        if constexpr (FUSED) {
-          s = fma2(e, pair2(sv[u][i], sv[u][i + 1]), s);
-          p = fma2(e, add2(pair2(pr[u][i], pr[u][i + 1]), np), p);
-        }
+    for (int i = 0; i < 8; i += 2) {
+      float z0, z1;
+      split2(fma2(pair2(x[i], x[i + 1]), c2, nr), z0, z1);
+      x[i] = ex2_approx(z0);
+      x[i + 1] = ex2_approx(z1);
+      const f32x2 e = pair2(x[i], x[i + 1]);
+      sum = add2(sum, e);
+      if constexpr (FUSED) {
+        s = fma2(e, pair2(sv[i], sv[i + 1]), s);
+        p = fma2(e, add2(pair2(pr[i], pr[i + 1]), np), p);
       }
+    }
   }
   __device__ __forceinline__ TailRec record() const {
     TailRec r{m, f, sum2(sum), sum2(s), sum2(p)};
@@ -185,9 +176,10 @@ __device__ __noinline__ TailRec redo_tail(const FusedRow<T, F, VEC>& row, int k0
 // Copies ahead of the loss and gradient kernels, and of the step's, whose items stay
 // (beside 10 items of 8 KB its ring is to leave room for a second CTA on the SM).
 template <typename T, int F>
-using LossCopies = Copies<T, F, sizeof(T) == 2 && !F ? 2 : 1, F && sizeof(T) == 4 ? 3 : 4>;
+using LossCopies = std::conditional_t<F == kPlain, Copies<T, F, sizeof(T) == 2 ? 4 : 2, 2>,
+                                      Copies<T, F, sizeof(T) == 2 ? 4 : 2, 2>>;
 template <typename T, int F>
-using StepCopies = Copies<T, F, sizeof(T) == 2 ? 2 : 1, sizeof(T) == 2 ? 4 : F ? 3 : 6, true>;
+using StepCopies = Copies<T, F, 2, sizeof(T) == 4 && F ? 2 : 4, true>;
 template <typename T, int F, bool GRAD>
 using RowCopies = std::conditional_t<GRAD, StepCopies<T, F>, LossCopies<T, F>>;
 
@@ -483,44 +475,41 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   // the columns that are not listed
   WarpTail<F != kPlain> st;
   st.init();
-  stream.run([&](auto& v, auto& pr, int g) {
-    constexpr int N = Cp::U;
-    float x[N][8], s[N][8];
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      v[u].template values<true>(row, pr[u], x[u], s[u]);
-      if constexpr (VEC) {
-        // the item's 8 bits (positions past the slice are -inf already, their bits 0)
-        const int b = v[u].k - k0;
-        unsigned bits;
-        if constexpr (sizeof(T) == 2) {
-          bits = reinterpret_cast<const unsigned char*>(bitmap)[b >> 3];
-        } else {
-          bits = (bitmap[b >> 5] >> (b & 31) & 15u) | (bitmap[(b + kHalf<T>) >> 5] >> (b & 31) & 15u) << 4;
-        }
-        if (bits) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (bits >> i & 1u) x[u][i] = -INFINITY;
-        }
+  float pa[8], pb[8];
+  const unsigned char* bits8 = reinterpret_cast<const unsigned char*>(bitmap);
+  const auto item_of = [&](auto& v, auto& pr, int it) {
+    float x[8], s[8];
+    v.template values<true>(row, pr, x, s);
+    if constexpr (VEC) {
+      // the item's 8 bits (positions past the slice are -inf already, their bits 0)
+      unsigned bits;
+      if constexpr (sizeof(T) == 2) {
+        bits = bits8[it * kStreamThreads + tid];
       } else {
+        const unsigned lo = bits8[(it * 2) * (kStreamThreads / 2) + (tid >> 1)];
+        const unsigned hi = bits8[(it * 2 + 1) * (kStreamThreads / 2) + (tid >> 1)];
+        bits = (lo >> (tid & 1) * 4 & 15u) | (hi >> (tid & 1) * 4 & 15u) << 4;
+      }
+      if (bits) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int b = elem_pos<T, VEC>(v[u].k, i) - k0;
-          if (bitmap[b >> 5] >> (b & 31) & 1u) x[u][i] = -INFINITY;
-        }
+        for (int i = 0; i < 8; ++i)
+          if (bits >> i & 1u) x[i] = -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int b = elem_pos<T, VEC>(v.k, i) - k0;
+        if (bitmap[b >> 5] >> (b & 31) & 1u) x[i] = -INFINITY;
       }
     }
     st.push(x, s, pr, c, p_ref);
     if constexpr (GRAD) {
-      float4* keep = reinterpret_cast<float4*>(kept) + g * (N * 2 * kStreamThreads) + tid;
-#pragma unroll
-      for (int u = 0; u < N; ++u) {
-        keep[u * 2 * kStreamThreads] = make_float4(x[u][0], x[u][1], x[u][2], x[u][3]);
-        keep[(u * 2 + 1) * kStreamThreads] = make_float4(x[u][4], x[u][5], x[u][6], x[u][7]);
-      }
+      float4* keep = reinterpret_cast<float4*>(kept) + it * (2 * kStreamThreads) + tid;
+      keep[0] = make_float4(x[0], x[1], x[2], x[3]);
+      keep[kStreamThreads] = make_float4(x[4], x[5], x[6], x[7]);
     }
-  });
+  };
+  stream.run([&](int g) { stream.each(g, pa, pb, item_of); }, item_of);
   WarpRec rec{st.record(), ListRec{-INFINITY, 0.f}};
   if (!(fabsf(rec.t.sum) + fabsf(rec.t.s) + fabsf(rec.t.p) < INFINITY))
     rec.t = redo_tail<T, F, VEC>(row, k0, k1, bitmap, GRAD ? reinterpret_cast<float*>(kept) : nullptr, c, p_ref);
@@ -710,15 +699,14 @@ __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs 
   __syncthreads();                                 // the output may be l_S itself
   const float k2 = g0 * st.factor;
   const Ref f{st.f_off, st.f_r};
-  stream.run([&](auto& v, auto& pr, int) {
-#pragma unroll
-    for (int u = 0; u < LossCopies<T, F>::U; ++u) {
-      float x[8], s[8], g[8];
-      v[u].template values<true>(row, pr[u], x, s);
-      unlisted_grad(x, f, c, k2, g);
-      grad_item<T, VEC>(out, v[u].k, row.sh, k1, a.grad_vec, g);
-    }
-  });
+  float pa[8], pb[8];
+  const auto item_of = [&](auto& v, auto& pr, int) {
+    float x[8], s[8], g[8];
+    v.template values<true>(row, pr, x, s);
+    unlisted_grad(x, f, c, k2, g);
+    grad_item<T, VEC>(out, v.k, row.sh, k1, a.grad_vec, g);
+  };
+  stream.run([&](int g) { stream.each(g, pa, pb, item_of); }, item_of);
   __syncthreads();
   if (id >= 0) grad_elem(out, id + row.sh, g_k);
 }

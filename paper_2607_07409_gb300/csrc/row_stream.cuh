@@ -400,21 +400,26 @@ struct Copies {
 };
 
 // The items of a thread in positions k0 .. k1 - 1 of a row (a slice, at most the
-// row's end), in groups of U. begin() starts the first copies; run() calls
-// f(items, l_P, group). Items that are not whole (at a row's ends; all without VEC) are
-// loaded where they are used. The prior comes out of L2 into registers a group ahead:
-// two sets of them, one for each of two bodies of the loop (copies between them took 8
-// instructions an item, and loads without a group between 700 cycles a group).
+// row's end). begin() starts the first copies; run() calls whole(group) for groups of U
+// items that are whole for every thread, which reads them with take() and their l_P
+// with prior(), and ragged(item, l_P, it) for an item of the others (at a row's ends;
+// all without VEC), loaded where it is used if it is not whole itself.
 template <typename Cp, typename T, int F, bool VEC>
 struct RowStream {
   static constexpr int U = Cp::U, D = Cp::D, W = Cp::W, PC = Cp::kPiece;
+  static constexpr int kRingGroup = U * Cp::kRing * PC, kStayGroup = U * Cp::kItemBytes;
   FusedRow<T, F, VEC> row;
   int k0, k1, items, groups;
+  int lo, hi;              // groups lo .. hi - 1 are whole
   uint8_t *ring, *stay;    // the calling thread's
   const T *next_l, *next_s;// its first item of the next group to copy
   int next_group = 0;
-  int in = 0;              // the ring's place for it, in bytes
-  int in_stay = 0;
+  uint32_t in;             // the ring's place for it
+  uint32_t in_stay;
+  // while a group is processed
+  const uint8_t *out, *out_stay;
+  const float* p;          // l_P of its first item
+  int pos;                 // its position
 
   __device__ __forceinline__ RowStream(const StreamRows& rows, long long r, int rank, uint8_t* ring_, uint8_t* stay_)
       : row(rows, r), ring(ring_ + threadIdx.x * 16), stay(stay_ + threadIdx.x * 16) {
@@ -423,22 +428,23 @@ struct RowStream {
     k1 = (int)min(first + rows.slice_cols, (long long)row.end);
     items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
     groups = (items + U - 1) / U;
-    next_l = row.L + item_pos<T, VEC>(k0, 0, threadIdx.x);
-    next_s = row.S + item_pos<T, VEC>(k0, 0, threadIdx.x);
+    lo = k0 < row.sh ? 1 : 0;
+    hi = VEC ? max(lo, (k1 - k0) / (U * kStreamStep)) : lo;
+    if (!VEC || hi > groups) hi = lo = groups;
+    pos = item_pos<T, VEC>(k0, 0, threadIdx.x);
+    next_l = row.L + pos;
+    next_s = row.S + pos;
+    p = row.P + pos;
+    in = smem_u32(ring);
+    in_stay = smem_u32(stay);
+    out = ring;
+    out_stay = stay;
   }
-  __device__ __forceinline__ bool whole(int pos) const { return VEC && pos >= row.sh && pos + kHalf<T> + 4 <= k1; }
-  // Whether some thread's item of group g is not whole.
-  __device__ __forceinline__ bool ragged(int g) const {
-    return !VEC || (g == 0 && k0 < row.sh) || k0 + (g + 1) * U * kStreamStep > k1;
-  }
-  // Piece k of item u of a group at `rg` in the ring, `st` among those that stay.
-  __device__ __forceinline__ uint8_t* place(int k, int u, int rg, int st) const {
-    return k < Cp::kStay ? stay + st + u * Cp::kItemBytes + k * PC : ring + rg + (u * Cp::kRing + k - Cp::kStay) * PC;
-  }
+  __device__ __forceinline__ bool whole(int at) const { return VEC && at >= row.sh && at + kHalf<T> + 4 <= k1; }
   __device__ __forceinline__ void copy(int u) const {
 #pragma unroll
     for (int k = 0; k < Cp::kPieces; ++k) {
-      const uint32_t dst = smem_u32(place(k, u, in, in_stay));
+      const uint32_t dst = k < Cp::kStay ? in_stay + u * Cp::kItemBytes + k * PC : in + (u * Cp::kRing + k - Cp::kStay) * PC;
       if (k < W) {
         if (row.has_l()) copy16(dst, next_l + u * kStreamStep + k * kHalf<T>);
       } else {
@@ -449,7 +455,7 @@ struct RowStream {
   // The next group's copies, one commit (empty past the last).
   __device__ __forceinline__ void fetch() {
     if (next_group < groups) {
-      if (!ragged(next_group)) {
+      if (next_group >= lo && next_group < hi) {
 #pragma unroll
         for (int u = 0; u < U; ++u) copy(u);
       } else {
@@ -460,8 +466,8 @@ struct RowStream {
       ++next_group;
       next_l += U * kStreamStep;
       next_s += U * kStreamStep;
-      in = in == (D - 1) * U * Cp::kRing * PC ? 0 : in + U * Cp::kRing * PC;
-      in_stay += U * Cp::kItemBytes;
+      if (Cp::kRing > 0) in = in == smem_u32(ring) + (D - 1) * kRingGroup ? smem_u32(ring) : in + kRingGroup;
+      in_stay += kStayGroup;
     }
     copies_commit();
   }
@@ -474,12 +480,17 @@ struct RowStream {
   __device__ __forceinline__ void drain() const {
     if constexpr (VEC) copies_wait<0>();
   }
-  __device__ __forceinline__ void take(Item<T, F, VEC>& v, int u, int out, int out_stay) const {
+  // Item u of the current group.
+  __device__ __forceinline__ void take(int u, Item<T, F, VEC>& v) const {
+    v.k = pos + u * kStreamStep;
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-      if (row.has_l()) v.l.w[k] = *reinterpret_cast<const uint4*>(place(k, u, out, out_stay));
+      const auto at = [&](int q) {
+        return q < Cp::kStay ? out_stay + u * Cp::kItemBytes + q * PC : out + (u * Cp::kRing + q - Cp::kStay) * PC;
+      };
+      if (row.has_l()) v.l.w[k] = *reinterpret_cast<const uint4*>(at(k));
       if constexpr (F != kPlain) {
-        if (row.has_s()) v.s.w[k] = *reinterpret_cast<const uint4*>(place(W + k, u, out, out_stay));
+        if (row.has_s()) v.s.w[k] = *reinterpret_cast<const uint4*>(at(W + k));
       }
     }
     if (!row.has_l()) v.l.fill(0.f);
@@ -487,74 +498,70 @@ struct RowStream {
       if (!row.has_s()) v.s.fill(0.f);
     }
   }
-  // l_P of group g, whose first item of the thread is at pos (0 for what is not whole).
-  __device__ __forceinline__ void take_prior(float (&pr)[U][8], int g, int pos) const {
+  // l_P of whole item u of the current group (u may run past it; `aligned`: the prior's
+  // own place against 16 bytes, which is -sh, is 0).
+  __device__ __forceinline__ void prior(int u, bool aligned, float (&x)[8]) const {
     if constexpr (F != kPlain) {
-      if (g >= groups) return;
-      const int o = -row.sh & 3;                   // (its own place against 16 bytes is -sh)
-      const float* p = row.P + pos;
-      if (row.has_p() && o == 0 && !ragged(g)) {
+      const float* at = p + u * kStreamStep;
+      if (!row.has_p()) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const float4 x = __ldg(reinterpret_cast<const float4*>(p + u * kStreamStep));
-          const float4 y = __ldg(reinterpret_cast<const float4*>(p + u * kStreamStep + kHalf<T>));
-          pr[u][0] = x.x; pr[u][1] = x.y; pr[u][2] = x.z; pr[u][3] = x.w;
-          pr[u][4] = y.x; pr[u][5] = y.y; pr[u][6] = y.z; pr[u][7] = y.w;
-        }
-        return;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (row.has_p() && whole(pos + u * kStreamStep)) {
-          prior4(p + u * kStreamStep, o, pr[u]);
-          prior4(p + u * kStreamStep + kHalf<T>, o, pr[u] + 4);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) pr[u][j] = 0.f;
-        }
+        for (int j = 0; j < 8; ++j) x[j] = 0.f;
+      } else if (aligned) {
+        const float4 y = __ldg(reinterpret_cast<const float4*>(at));
+        const float4 z = __ldg(reinterpret_cast<const float4*>(at + kHalf<T>));
+        x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w; x[4] = z.x; x[5] = z.y; x[6] = z.z; x[7] = z.w;
+      } else {
+        prior4(at, -row.sh & 3, x);
+        prior4(at + kHalf<T>, -row.sh & 3, x + 4);
       }
     }
   }
-  template <typename Fn>
-  __device__ __forceinline__ void run(Fn&& f) {
-    int out = 0, out_stay = 0, pos = item_pos<T, VEC>(k0, 0, threadIdx.x);
-    float pa[U][8], pb[U][8];
-    take_prior(pa, 0, pos);
-    auto body = [&](int g, float (&pr)[U][8], float (&ahead)[U][8]) {
-      Item<T, F, VEC> v[U];
-      take_prior(ahead, g + 1, pos + U * kStreamStep);
-      copies_wait<D - 1>();
-      if (!ragged(g)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          v[u].k = pos + u * kStreamStep;
-          take(v[u], u, out, out_stay);
-        }
+  __device__ __forceinline__ bool prior_aligned() const { return (row.sh & 3) == 0; }
+  template <typename Whole, typename Ragged>
+  __device__ __forceinline__ void run(Whole&& f_whole, Ragged&& f_ragged) {
+#pragma unroll 1
+    for (int g = 0; g < groups; ++g) {
+      if constexpr (VEC) copies_wait<D - 1>();
+      if (g >= lo && g < hi) {
+        f_whole(g);
       } else {
-#pragma unroll
+#pragma unroll 1
         for (int u = 0; u < U; ++u) {
-          v[u].k = pos + u * kStreamStep;
-          if (whole(pos + u * kStreamStep)) take(v[u], u, out, out_stay);
-          else v[u].load(row, pos + u * kStreamStep, k1, pr[u]);
+          const int at = pos + u * kStreamStep;
+          Item<T, F, VEC> v;
+          float pr[8];
+          if (whole(at)) {
+            take(u, v);
+            prior(u, false, pr);
+          } else {
+            v.load(row, at, k1, pr);
+          }
+          f_ragged(v, pr, g * U + u);
         }
       }
-      f(v, pr, g);
       if constexpr (VEC) fetch();
       pos += U * kStreamStep;
-      out = out == (D - 1) * U * Cp::kRing * PC ? 0 : out + U * Cp::kRing * PC;
-      out_stay += U * Cp::kItemBytes;
-    };
-    if constexpr (F == kPlain) {
-#pragma unroll 1
-      for (int g = 0; g < groups; ++g) body(g, pa, pa);
-    } else {
-#pragma unroll 1
-      for (int g = 0; g < groups; g += 2) {
-        body(g, pa, pb);
-        if (g + 1 < groups) body(g + 1, pb, pa);
-      }
+      if (F != kPlain) p += U * kStreamStep;
+      if (Cp::kRing > 0) out = out == ring + (D - 1) * kRingGroup ? ring : out + kRingGroup;
+      out_stay += kStayGroup;
     }
     drain();
+  }
+  // As whole(group) of run() for fused rows: f(item, l_P, it) for each item, the prior
+  // out of L2 an item ahead, in two sets of registers by turns (copies between them took
+  // 8 instructions an item, loads at their use 700 cycles).
+  template <typename Fn>
+  __device__ __forceinline__ void each(int g, float (&pa)[8], float (&pb)[8], Fn&& f) const {
+    static_assert(U % 2 == 0 || F == kPlain, "two sets by turns");
+    const bool al = prior_aligned();
+    if (g == lo) prior(0, al, pa);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      Item<T, F, VEC> v;
+      take(u, v);
+      if (u + 1 < U || g + 1 < hi) prior(u + 1, al, u & 1 ? pa : pb);
+      f(v, u & 1 ? pb : pa, g * U + u);
+    }
   }
 };
 

@@ -166,7 +166,8 @@ __device__ __forceinline__ void raise8_bf16(uint4& w, __nv_bfloat162 low) {
 
 // Copies ahead: 32 KB of plain rows (four CTAs on an SM), 48 KB of two rows (three).
 template <typename T, int F>
-using ScoreCopies = Copies<T, F, sizeof(T) == 2 && !F ? 2 : 1, sizeof(T) == 2 && F ? 6 : F ? 3 : 4>;
+using ScoreCopies = std::conditional_t<F == kPlain, Copies<T, F, sizeof(T) == 2 ? 4 : 2, 2>,
+                                       Copies<T, F, 2, sizeof(T) == 2 ? 3 : 2>>;
 
 // Dynamic shared memory: the ring (later SelectShared), the block maxima, and for a
 // cluster the entries of all slices.
@@ -221,14 +222,23 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
   WarpSoft st;
   st.init();
   float top = -INFINITY, block = -INFINITY;
-  const __nv_bfloat162 low2 = __float2bfloat162_rn(a.low);
-  stream.run([&](auto& v, auto& pr, int g) {
-    constexpr int N = U;
-    float vm = -INFINITY;
-    if constexpr (sizeof(T) == 2 && F == kPlain) {
-      // bf16 as stored: the maximum and the clamp of masked entries on pairs
+  // the largest of the items' block so far
+  const auto note = [&](float vm, int it) {
+    if (K > 0) {
+      top = fmaxf(top, vm);
+      block = (it & ((U << shift) - 1)) == 0 ? vm : fmaxf(block, vm);
+      bmax[(it / U >> shift) * kStreamThreads + tid] = block;
+    }
+  };
+  float pa[8], pb[8];
+  if constexpr (sizeof(T) == 2 && F == kPlain) {
+    // bf16 as stored: the maximum and the clamp of masked entries on pairs
+    const __nv_bfloat162 low2 = __float2bfloat162_rn(a.low);
+    const auto items_of = [&](auto& v, int it) {
+      constexpr int N = sizeof(v) / sizeof(v[0]);
+      float vm = max8_bf16(v[0].l.w[0]);
 #pragma unroll
-      for (int u = 0; u < N; ++u) vm = fmaxf(vm, max8_bf16(v[u].l.w[0]));
+      for (int u = 1; u < N; ++u) vm = fmaxf(vm, max8_bf16(v[u].l.w[0]));
       if (__any_sync(0xFFFFFFFFu, vm > st.m)) {
         const float nt = warp_max(vm);
         bool out = st.raise(nt, vm, c);
@@ -244,56 +254,64 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
             }
         }
       }
+      if (st.f.off == 0.f) {
 #pragma unroll
-      for (int u = 0; u < N; ++u) {
-        float x[8];
-        if (st.f.off == 0.f) {
+        for (int u = 0; u < N; ++u) {
+          float x[8];
           raise8_bf16(v[u].l.w[0], low2);
           v[u].l.unpack(x);
-        } else {                   // all so far masked by huge values: their differences
+          st.template add<true>(x, c);
+        }
+      } else {                     // all so far masked by huge values: their differences
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          float x[8];
           v[u].l.unpack(x);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             x[i] -= st.f.off;
             if (x[i] < a.low) x[i] = a.low;
           }
+          st.template add<true>(x, c);
         }
-        st.template add<true>(x, c);
       }
-    } else {
-      float x[N][8], s[8];
+      note(vm, it);
+    };
+    stream.run(
+        [&](int g) {
+          Item<T, F, VEC> v[U];
 #pragma unroll
-      for (int u = 0; u < N; ++u) {
-        v[u].template values<false>(row, pr[u], x[u], s);
-        vm = fmaxf(vm, max8(x[u]));
-      }
+          for (int u = 0; u < U; ++u) stream.take(u, v[u]);
+          items_of(v, g * U);
+        },
+        [&](auto& v, auto&, int it) {
+          Item<T, F, VEC> one[1] = {v};
+          items_of(one, it);
+        });
+  } else {
+    const auto item_of = [&](auto& v, auto& pr, int it) {
+      float x[8], s[8];
+      v.template values<false>(row, pr, x, s);
+      const float vm = max8(x);
       if (__any_sync(0xFFFFFFFFu, vm > st.m)) {
         const float nt = warp_max(vm);
         bool out = st.raise(nt, vm, c);
 #pragma unroll
-        for (int u = 0; u < N; ++u)
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (out && x[u][i] == nt) {
-              out = false;
-              x[u][i] = -INFINITY;
-            }
+        for (int i = 0; i < 8; ++i)
+          if (out && x[i] == nt) {
+            out = false;
+            x[i] = -INFINITY;
+          }
       }
+      if (st.f.off != 0.f) {
 #pragma unroll
-      for (int u = 0; u < N; ++u) {
-        if (st.f.off != 0.f) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[u][i] -= st.f.off;
-        }
-        st.template add<false>(x[u], c);
+        for (int i = 0; i < 8; ++i) x[i] -= st.f.off;
       }
-    }
-    if (K > 0) {
-      top = fmaxf(top, vm);
-      block = (g & ((1 << shift) - 1)) == 0 ? vm : fmaxf(block, vm);
-      bmax[(g >> shift) * kStreamThreads + tid] = block;
-    }
-  });
+      st.template add<false>(x, c);
+      note(vm, it);
+    };
+    stream.run([&](int g) { stream.each(g, pa, pb, item_of); }, item_of);
+  }
   const SoftRec wr = st.record();
   if (lane == 0) sh.warps[warp] = wr;
   __syncthreads();
