@@ -2138,11 +2138,12 @@ int rows_call(const dels_rows* x, int rows, int V, int max_v, RowsCall* out) {
   return DELS_OK;
 }
 
-// CTAs per row: as many as bring four per SM into flight, at slices of 4096
-// columns and more, a power of two up to 8; at least `least`.
+// CTAs per row: as many as bring 1.6 per SM into flight, at slices of 4096 columns and
+// more, a power of two up to 8; at least `least`. (A CTA's start, its records and their
+// exchange cost it 3 to 8 us whatever its slice: see the launches' comments.)
 void plan_cluster(StreamRows& in, int sms, int least) {
   int c = 1;
-  while (c < 8 && (c < least || ((long long)in.rows * c < 4LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
+  while (c < 8 && (c < least || ((long long)in.rows * c * 5 < 8LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
   in.cluster = c;
   // whole items of every thread (positions: a row may start up to 7 columns past a
   // 16-byte boundary)

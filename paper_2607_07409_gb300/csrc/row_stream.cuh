@@ -212,6 +212,18 @@ struct Item {
       }
     }
   }
+  // A whole item, straight from memory.
+  __device__ __forceinline__ void load_whole(const FusedRow<T, F, VEC>& row, int pos, float (&pr)[8]) {
+    k = pos;
+    if (row.has_l()) l.load(row.L + pos, kHalf<T>);
+    else l.fill(0.f);
+    if constexpr (F != kPlain) {
+      if (row.has_s()) s.load(row.S + pos, kHalf<T>);
+      else s.fill(0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pr[i] = row.p_at(elem_pos<T, VEC>(pos, i));
+    }
+  }
   // Values of the 8 positions, and the l_S in them. Where they are rounded after every
   // operation the products are packed fmas with an addend of -0 that only the launch
   // knows: a packed product that feeds a packed sum is contracted whatever its rounding

@@ -6,8 +6,8 @@
 //
 // What bounds it: the read of the logits. The alternatives cost no second read of
 // the row: every thread keeps the largest entry of each of its blocks of a few
-// items; the K-th largest thread maximum is at most the K-th largest entry of the
-// slice, and only the blocks that reach it are read again for their entries.
+// items; a value that K threads' largest reach is at most the K-th largest entry of
+// the slice, and only the blocks that reach it are read again for their entries.
 #include <cuda_bf16.h>
 
 #include "row_stream.cuh"
@@ -42,44 +42,143 @@ struct ScoreShared {
   unsigned long long best[kMaxTopK];       // this CTA's entries in order, 0 where there are none
   SoftRec warps[kStreamWarps];
   SoftRec ctas[kMaxCluster];
+  float lanes[kStreamWarps][32];           // each warp's thread maxima in order, and how many there are
+  int counts[kStreamWarps];
   int ncand, njobs;
 };
 
-// The K largest of cand[0 .. n) to best[] in order (all threads): a warp counts
-// what is above one candidate, 32 at a time.
-__device__ void sort_best(ScoreShared& sh, const unsigned long long* cand, int n, int K) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int k = threadIdx.x; k < K; k += kStreamThreads) sh.best[k] = 0ull;
+// The K largest of cand[0 .. n) to best[] in order (all threads). Up to 512 are sorted
+// by a bitonic network, E a thread: exchanges inside a warp by shuffles, six to nine of
+// them through shared memory; of more (a row of ties) each one's place is counted.
+template <int E>
+__device__ __forceinline__ void sort_network(ScoreShared& sh, SelectShared& sel, int n, int K) {
+  const int tid = threadIdx.x;
+  unsigned long long x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = e * kStreamThreads + tid < n ? sel.cand[e * kStreamThreads + tid] : 0ull;
+  int size = 32;
+  while (size < n) size *= 2;
+  for (int k = 2; k <= size; k *= 2)
+    for (int d = k >> 1; d > 0; d >>= 1) {
+      if (d >= kStreamThreads) {                             // between a thread's own
+        if constexpr (E == 2) {
+          if (x[0] < x[1]) {
+            const unsigned long long t = x[0];
+            x[0] = x[1];
+            x[1] = t;
+          }
+        }
+        continue;
+      }
+      if (d >= 32) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) sel.cand[e * kStreamThreads + tid] = x[e];
+        __syncthreads();
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = e * kStreamThreads + tid;
+        const unsigned long long o =
+            d >= 32 ? sel.cand[i ^ d] : __shfl_xor_sync(0xFFFFFFFFu, x[e], d);
+        const bool larger = ((i & k) == 0) == ((i & d) == 0);
+        x[e] = larger == (o > x[e]) ? o : x[e];
+      }
+    }
   __syncthreads();
-  for (int i = warp; i < n; i += kStreamWarps) {
-    const unsigned long long x = cand[i];
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (e * kStreamThreads + tid < K) sh.best[e * kStreamThreads + tid] = x[e];
+  __syncthreads();
+}
+__device__ void sort_best(ScoreShared& sh, SelectShared& sel, int n, int K) {
+  if (n <= kStreamThreads) return sort_network<1>(sh, sel, n, K);
+  if (n <= 2 * kStreamThreads) return sort_network<2>(sh, sel, n, K);
+  for (int i = threadIdx.x; i < n; i += kStreamThreads) {
+    const unsigned long long x = sel.cand[i];
     int rank = 0;
-    for (int j = lane; j < n; j += 32) rank += cand[j] > x;
-    rank = __reduce_add_sync(0xFFFFFFFFu, rank);
-    if (lane == 0 && rank < K && x) sh.best[rank] = x;
+    for (int j = 0; j < n; ++j) rank += sel.cand[j] > x;
+    if (rank < K) sh.best[rank] = x;
   }
   __syncthreads();
 }
 
-// The entries of an item that reach `floor_key`, into cand[] as far as it has room.
-template <typename T, int F, bool VEC>
-__device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel, const FusedRow<T, F, VEC>& row,
-                                             int pos, int k1, unsigned long long floor_key) {
-  float x[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int q = elem_pos<T, VEC>(pos, i);
-    x[i] = q >= row.sh && q < k1 ? row.at(q) : -INFINITY;
+// Lists of K entries in order (0 past their ends), C of them, to the K largest of all in
+// best[]: an entry's place is its own plus what is above it in the other lists.
+__device__ void merge_best(ScoreShared& sh, const unsigned long long* lists, int C, int K) {
+  const int tid = threadIdx.x;
+  for (int k = tid; k < K; k += kStreamThreads) sh.best[k] = 0ull;
+  __syncthreads();
+  for (int i = tid; i < C * K; i += kStreamThreads) {
+    const unsigned long long x = lists[i];
+    const int own = i / K;
+    int rank = i - own * K;
+    if (!x) continue;
+    for (int l = 0; l < C && rank < K; ++l) {
+      if (l == own) continue;
+      int lo = 0, hi = K;                                    // entries before lo are above x, from hi on are not
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (lists[l * K + mid] > x) lo = mid + 1;
+        else hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank < K) sh.best[rank] = x;
   }
+  __syncthreads();
+}
+
+// The values of an item at `pos`, -inf outside the row (not in a stream's turn).
+template <typename T, int F, bool VEC>
+__device__ __forceinline__ void item_values(const FusedRow<T, F, VEC>& row, int pos, int k1, float (&x)[8]) {
+  Item<T, F, VEC> v;
+  float pr[8], s[8];
+  if (VEC && pos >= row.sh && pos + kHalf<T> + 4 <= k1) {
+    v.load_whole(row, pos, pr);
+  } else {
+    v.load(row, pos, k1, pr);
+  }
+  v.template values<false>(row, pr, x, s);
+}
+
+// Where this lane's `n` things go in a list that `count` counts: one addition a warp
+// (all lanes converged).
+__device__ __forceinline__ int reserve(int* count, int n) {
+  const int lane = threadIdx.x & 31;
+  int up = n;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(0xFFFFFFFFu, up, d);
+    if (lane >= d) up += o;
+  }
+  int base = 0;
+  if (lane == 31 && up > 0) base = atomicAdd(count, up);
+  return __shfl_sync(0xFFFFFFFFu, base, 31) + up - n;
+}
+
+// The entries among x[8] of an item at `pos` that reach `floor_key`, into cand[] as far
+// as it has room (all lanes converged; of no thread's item: x = -inf).
+template <typename T, int F, bool VEC>
+__device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel, const FusedRow<T, F, VEC>& row, int pos,
+                                             const float (&x)[8], unsigned long long floor_key) {
   const float least = from_order_u32((unsigned)(floor_key >> 32));
-  if (!(max8(x) >= least)) return;
+  unsigned hits = 0u;
+  if (max8(x) >= least) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (x[i] >= least && x[i] > -INFINITY &&
+          entry_key(x[i], elem_pos<T, VEC>(pos, i) - row.sh) >= floor_key)
+        hits |= 1u << i;
+  }
+  if (!__any_sync(0xFFFFFFFFu, hits != 0u)) return;
+  int at = reserve(&sh.ncand, __popc(hits));
+  if (!hits) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (!(x[i] >= least && x[i] > -INFINITY)) continue;
-    const unsigned long long e = entry_key(x[i], elem_pos<T, VEC>(pos, i) - row.sh);
-    if (e < floor_key) continue;
-    const int at = atomicAdd(&sh.ncand, 1);
-    if (at < kCandidates) sel.cand[at] = e;
+    if (!(hits >> i & 1u)) continue;
+    if (at < kCandidates) sel.cand[at] = entry_key(x[i], elem_pos<T, VEC>(pos, i) - row.sh);
+    ++at;
   }
 }
 
@@ -89,42 +188,66 @@ __device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel,
 template <int U, typename T, int F, bool VEC>
 __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax, int shift,
                           const FusedRow<T, F, VEC>& row, int k0, int k1, int K, float top) {
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep, groups = (items + U - 1) / U;
   const int slots = (groups + (1 << shift) - 1) >> shift;
-  // About the K-th largest thread maximum, from its highest bit down; -inf where
-  // fewer than K threads have an entry.
-  const unsigned key = top > -INFINITY ? order_u32(top) : 0u;
-  unsigned tau = 0u;
-  if (tid == 0) sh.ncand = sh.njobs = 0;
-  if (__syncthreads_count(key > 0u) >= K) {
-    for (int bit = 31; bit >= 0; --bit) {
-      const unsigned t = tau | (1u << bit);
-      const int n = __syncthreads_count(key >= t);
-      if (n >= K) tau = t;
-      if (n >= K && n <= K + 8) break;
+  // What at least K entries reach: the warps' thread maxima in order, and of them either
+  // K divided among the warps (the least of those), or all K of one warp (the largest of
+  // those); both count entries of K threads or more.
+  float t = top;
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int d = k >> 1; d > 0; d >>= 1) {
+      const float o = __shfl_xor_sync(0xFFFFFFFFu, t, d);
+      t = ((lane & k) == 0) == ((lane & d) == 0) ? fmaxf(t, o) : fminf(t, o);
     }
-  } else {
-    tau = order_u32(-INFINITY);
+  sh.lanes[warp][lane] = t;
+  const int have = __popc(__ballot_sync(0xFFFFFFFFu, top > -INFINITY));
+  if (lane == 0) sh.counts[warp] = have;
+  if (tid == 0) sh.ncand = sh.njobs = 0;
+  __syncthreads();
+  unsigned tau;
+  {
+    const int w = lane & (kStreamWarps - 1), cnt = sh.counts[w];
+    const int live = __popc(__ballot_sync(0xFFFFFFFFu, cnt > 0)) / (32 / kStreamWarps);
+    const int each = live ? (K + live - 1) / live : K;
+    const bool fair = __all_sync(0xFFFFFFFFu, cnt == 0 || cnt >= each) && live;
+    float least_of = cnt > 0 && cnt >= each ? sh.lanes[w][each - 1] : INFINITY;
+    least_of = -warp_max(-least_of);
+    const float one = warp_max(K <= cnt ? sh.lanes[w][K - 1] : -INFINITY);
+    tau = order_u32(fmaxf(fair ? least_of : -INFINITY, one));
   }
   const float least = from_order_u32(tau);
   unsigned long long floor_key = (unsigned long long)tau << 32;     // what an entry has to reach
+  unsigned hits = 0u;                                               // (kSlots bits)
   if (top >= least && top > -INFINITY) {
-    for (int b = 0; b < slots; ++b)
-      if (bmax[b * kStreamThreads + tid] >= least) {
-        const int at = atomicAdd(&sh.njobs, 1);
-        if (at < kJobs) sel.jobs[at] = b * kStreamThreads + tid;
-      }
+    for (int b = 0; b < slots; ++b) hits |= bmax[b * kStreamThreads + tid] >= least ? 1u << b : 0u;
   }
+  for (int j = reserve(&sh.njobs, __popc(hits)); hits; hits &= hits - 1, ++j)
+    if (j < kJobs) sel.jobs[j] = (__ffs(hits) - 1) * kStreamThreads + tid;
   __syncthreads();
   if (sh.njobs <= kJobs) {
-    // a lane per item of a job
+    // a lane per item of a job, two of them at a time
     const int per = U << shift, n = sh.njobs * per;
-    for (int i = tid; i < n; i += kStreamThreads) {
-      const int job = sel.jobs[i / per], o = i % per;
-      const int it = (job / kStreamThreads) * per + o;
-      if (it >= items) continue;
-      keep_entries(sh, sel, row, item_pos<T, VEC>(k0, it, job % kStreamThreads), k1, floor_key);
+    for (int i0 = warp * 32; i0 < n; i0 += 2 * kStreamThreads) {
+      float x[2][8];
+      int pos[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int i = i0 + h * kStreamThreads + lane;
+        int it = items;
+        if (i < n) it = (sel.jobs[i / per] / kStreamThreads) * per + i % per;
+        pos[h] = it < items ? item_pos<T, VEC>(k0, it, sel.jobs[i / per] % kStreamThreads) : k1;
+        if (pos[h] < k1) {
+          item_values(row, pos[h], k1, x[h]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[h][e] = -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) keep_entries(sh, sel, row, pos[h], x[h], floor_key);
     }
   }
   __syncthreads();
@@ -138,17 +261,22 @@ __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax,
       const int n = sh.ncand;
       __syncthreads();
       if (n > kCandidates - 128 * 8) {
-        sort_best(sh, sel.cand, n, K);
+        sort_best(sh, sel, n, K);
         for (int k = tid; k < K; k += kStreamThreads) sel.cand[k] = sh.best[k];
         floor_key = sh.best[K - 1];                                 // n > K: there are K
         if (tid == 0) sh.ncand = K;
         __syncthreads();
       }
-      if ((tid >> 7) == (j & 1)) keep_entries(sh, sel, row, item_pos<T, VEC>(k0, j >> 1, tid), k1, floor_key);
+      if ((tid >> 7) == (j & 1)) {
+        const int pos = item_pos<T, VEC>(k0, j >> 1, tid);
+        float x[8];
+        item_values(row, pos, k1, x);
+        keep_entries(sh, sel, row, pos, x, floor_key);
+      }
       __syncthreads();
     }
   }
-  sort_best(sh, sel.cand, sh.ncand, K);
+  sort_best(sh, sel, sh.ncand, K);
 }
 
 // Packed maximum of 8 bf16 (NaN ignored), and every one raised to at least `low`
@@ -337,7 +465,7 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
     if (rank != 0) return;
     cluster_wait();
     all = softrec_merge8((lane & 7) < C ? sh.ctas[lane & 7] : softrec_init(), c);
-    if (K > 0) sort_best(sh, slices, C * K, K);
+    if (K > 0) merge_best(sh, slices, C, K);
   }
   const bool ok = softrec_valid(all);
   const float z_m = ref_z(all.m, all.f, c), e_m = ex2_approx(z_m);
