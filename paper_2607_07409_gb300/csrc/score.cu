@@ -47,9 +47,11 @@ struct ScoreShared {
   int ncand, njobs;
 };
 
-// The K largest of cand[0 .. n) to best[] in order (all threads). Up to 512 are sorted
-// by a bitonic network, E a thread: exchanges inside a warp by shuffles, six to nine of
-// them through shared memory; of more (a row of ties) each one's place is counted.
+// The K largest of cand[0 .. n) to best[] in order (all threads). Up to 128: each one's
+// place is the number above it, counted by the threads that share it. Up to 1024: a
+// bitonic network, E a thread, exchanges inside a warp by shuffles. (Cycles of 36, 95
+// and 220: 1300, 2700 and 9000 counted, 3500, 5000 and 6500 by the network.) More
+// (rows of ties): counted by a thread each.
 template <int E>
 __device__ __forceinline__ void sort_network(ScoreShared& sh, SelectShared& sel, int n, int K) {
   const int tid = threadIdx.x;
@@ -61,11 +63,16 @@ __device__ __forceinline__ void sort_network(ScoreShared& sh, SelectShared& sel,
   for (int k = 2; k <= size; k *= 2)
     for (int d = k >> 1; d > 0; d >>= 1) {
       if (d >= kStreamThreads) {                             // between a thread's own
-        if constexpr (E == 2) {
-          if (x[0] < x[1]) {
-            const unsigned long long t = x[0];
-            x[0] = x[1];
-            x[1] = t;
+#pragma unroll
+        for (int m = 1; m < E; m *= 2) {
+          if (d != m * kStreamThreads) continue;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            if (e & m) continue;
+            const bool down = ((e * kStreamThreads + tid) & k) == 0;
+            const unsigned long long lo = x[e], hi = x[e | m];
+            x[e] = down == (lo > hi) ? lo : hi;
+            x[e | m] = down == (lo > hi) ? hi : lo;
           }
         }
         continue;
@@ -92,39 +99,22 @@ __device__ __forceinline__ void sort_network(ScoreShared& sh, SelectShared& sel,
   __syncthreads();
 }
 __device__ void sort_best(ScoreShared& sh, SelectShared& sel, int n, int K) {
-  if (n <= kStreamThreads) return sort_network<1>(sh, sel, n, K);
-  if (n <= 2 * kStreamThreads) return sort_network<2>(sh, sel, n, K);
-  for (int i = threadIdx.x; i < n; i += kStreamThreads) {
-    const unsigned long long x = sel.cand[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += sel.cand[j] > x;
-    if (rank < K) sh.best[rank] = x;
-  }
-  __syncthreads();
-}
-
-// Lists of K entries in order (0 past their ends), C of them, to the K largest of all in
-// best[]: an entry's place is its own plus what is above it in the other lists.
-__device__ void merge_best(ScoreShared& sh, const unsigned long long* lists, int C, int K) {
   const int tid = threadIdx.x;
+  if (n > 128 && n <= kStreamThreads) return sort_network<1>(sh, sel, n, K);
+  if (n > 128 && n <= 2 * kStreamThreads) return sort_network<2>(sh, sel, n, K);
+  if (n > 128 && n <= 4 * kStreamThreads) return sort_network<4>(sh, sel, n, K);
   for (int k = tid; k < K; k += kStreamThreads) sh.best[k] = 0ull;
   __syncthreads();
-  for (int i = tid; i < C * K; i += kStreamThreads) {
-    const unsigned long long x = lists[i];
-    const int own = i / K;
-    int rank = i - own * K;
-    if (!x) continue;
-    for (int l = 0; l < C && rank < K; ++l) {
-      if (l == own) continue;
-      int lo = 0, hi = K;                                    // entries before lo are above x, from hi on are not
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (lists[l * K + mid] > x) lo = mid + 1;
-        else hi = mid;
-      }
-      rank += lo;
-    }
-    if (rank < K) sh.best[rank] = x;
+  int log_share = 0;               // 2^log_share threads a candidate
+  while (log_share < 5 && n << (log_share + 1) <= kStreamThreads) ++log_share;
+  const int share = 1 << log_share, part = tid & (share - 1);
+  for (int i = tid >> log_share; i - (tid >> log_share) < n; i += kStreamThreads >> log_share) {
+    const unsigned long long x = i < n ? sel.cand[i] : 0ull;
+    int rank = 0;
+#pragma unroll 4
+    for (int j = part; j < n; j += share) rank += sel.cand[j] > x;
+    for (int d = share >> 1; d > 0; d >>= 1) rank += __shfl_xor_sync(0xFFFFFFFFu, rank, d);
+    if (part == 0 && x && rank < K) sh.best[rank] = x;
   }
   __syncthreads();
 }
@@ -164,22 +154,43 @@ __device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel,
                                              const float (&x)[8], unsigned long long floor_key) {
   const float least = from_order_u32((unsigned)(floor_key >> 32));
   unsigned hits = 0u;
-  if (max8(x) >= least) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (x[i] >= least && x[i] > -INFINITY &&
-          entry_key(x[i], elem_pos<T, VEC>(pos, i) - row.sh) >= floor_key)
-        hits |= 1u << i;
-  }
+  for (int i = 0; i < 8; ++i) hits |= x[i] >= least && x[i] > -INFINITY ? 1u << i : 0u;
   if (!__any_sync(0xFFFFFFFFu, hits != 0u)) return;
-  int at = reserve(&sh.ncand, __popc(hits));
-  if (!hits) return;
+  for (int at = reserve(&sh.ncand, __popc(hits)); hits; hits &= hits - 1, ++at) {
+    const int i = __ffs(hits) - 1;
+    float v = x[0];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (!(hits >> i & 1u)) continue;
-    if (at < kCandidates) sel.cand[at] = entry_key(x[i], elem_pos<T, VEC>(pos, i) - row.sh);
-    ++at;
+    for (int j = 1; j < 8; ++j) v = i == j ? x[j] : v;
+    const unsigned long long e = entry_key(v, elem_pos<T, VEC>(pos, i) - row.sh);
+    if (at < kCandidates) sel.cand[at] = e >= floor_key ? e : 0ull;   // (of a tie past the floor: none)
   }
+}
+
+// The K largest of C lists of K entries in order (0 past their ends) to best[]: those
+// that reach what K of them do, either K divided among the lists (the least of those) or
+// all of one list (the largest of those).
+__device__ void merge_best(ScoreShared& sh, SelectShared& sel, const unsigned long long* lists, int C, int K) {
+  const int tid = threadIdx.x, lane = tid & 31, each = (K + C - 1) / C;
+  if (tid == 0) sh.ncand = 0;
+  unsigned long long fair = lane < C ? lists[lane * K + each - 1] : ~0ull, one = lane < C ? lists[lane * K + K - 1] : 0ull;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    const unsigned long long f = __shfl_xor_sync(0xFFFFFFFFu, fair, d), o = __shfl_xor_sync(0xFFFFFFFFu, one, d);
+    fair = f < fair ? f : fair;
+    one = o > one ? o : one;
+  }
+  const unsigned long long least = fair > one ? fair : one;
+  __syncthreads();
+  for (int i0 = tid - lane; i0 < C * K; i0 += kStreamThreads) {
+    const int i = i0 + lane;
+    const unsigned long long e = i < C * K ? lists[i] : 0ull;
+    const bool in = e && e >= least;
+    const int at = reserve(&sh.ncand, in ? 1 : 0);
+    if (in) sel.cand[at] = e;
+  }
+  __syncthreads();
+  sort_best(sh, sel, sh.ncand, K);
 }
 
 // This CTA's K largest entries of its slice into sh.best. `top`: the largest
@@ -229,16 +240,21 @@ __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax,
   __syncthreads();
   if (sh.njobs <= kJobs) {
     // a lane per item of a job, two of them at a time
-    const int per = U << shift, n = sh.njobs * per;
+    constexpr int kLogU = U == 4 ? 2 : U == 2 ? 1 : 0;
+    static_assert(U == 1 << kLogU, "a power of two");
+    const int log_per = kLogU + shift, n = sh.njobs << log_per;
     for (int i0 = warp * 32; i0 < n; i0 += 2 * kStreamThreads) {
       float x[2][8];
       int pos[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int i = i0 + h * kStreamThreads + lane;
-        int it = items;
-        if (i < n) it = (sel.jobs[i / per] / kStreamThreads) * per + i % per;
-        pos[h] = it < items ? item_pos<T, VEC>(k0, it, sel.jobs[i / per] % kStreamThreads) : k1;
+        pos[h] = k1;
+        if (i < n) {
+          const unsigned job = (unsigned)sel.jobs[i >> log_per];
+          const int it = ((int)(job / kStreamThreads) << log_per) + (i & ((1 << log_per) - 1));
+          if (it < items) pos[h] = item_pos<T, VEC>(k0, it, (int)(job % kStreamThreads));
+        }
         if (pos[h] < k1) {
           item_values(row, pos[h], k1, x[h]);
         } else {
@@ -246,8 +262,8 @@ __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax,
           for (int e = 0; e < 8; ++e) x[h][e] = -INFINITY;
         }
       }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) keep_entries(sh, sel, row, pos[h], x[h], floor_key);
+      keep_entries(sh, sel, row, pos[0], x[0], floor_key);
+      if (i0 + kStreamThreads < n) keep_entries(sh, sel, row, pos[1], x[1], floor_key);
     }
   }
   __syncthreads();
@@ -465,7 +481,7 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
     if (rank != 0) return;
     cluster_wait();
     all = softrec_merge8((lane & 7) < C ? sh.ctas[lane & 7] : softrec_init(), c);
-    if (K > 0) merge_best(sh, slices, C, K);
+    if (K > 0) merge_best(sh, *reinterpret_cast<SelectShared*>(dyn), slices, C, K);
   }
   const bool ok = softrec_valid(all);
   const float z_m = ref_z(all.m, all.f, c), e_m = ex2_approx(z_m);

@@ -133,6 +133,8 @@ SCORE_SIZES = [
     (4, 1000, 7, 1, None), (3, 1000, 7, 0, 1003), (4, 1001, 7, 0, 1008), (3, 5000, 16, 8, 5008), (3, 4099, 5, 3, 4101),
     # many rows: one CTA a row
     (700, 1030, 4, 0, None), (640, 9001, 2, 0, None),
+    # few entries a thread and many asked for: more candidates than are sorted at once
+    (2, 1024, 128, 0, None), (2, 2048, 256, 0, None), (300, 3000, 200, 0, None),
 ]
 
 
