@@ -99,15 +99,20 @@ struct WarpTail {
     f = Ref{0.f, 0.f};
     sum = s = p = 0ull;
   }
+  // Whether there is a reference, and it is a whole number.
+  __device__ __forceinline__ bool settled() const { return m > -INFINITY && f.off == 0.f; }
   // One item's values, all lanes converged: x becomes 2^z.
+  template <bool SETTLED>
   __device__ __forceinline__ void push(float (&x)[8], const float (&sv)[8], const float (&pr)[8], float c, float p_ref) {
-    if (m == -INFINITY) {
-      m = warp_max(max8(x));
-      if (m > -INFINITY) f = make_ref(m, c);
-    }
-    if (f.off != 0.f) {
+    if (!SETTLED) {
+      if (m == -INFINITY) {
+        m = warp_max(max8(x));
+        if (m > -INFINITY) f = make_ref(m, c);
+      }
+      if (f.off != 0.f) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] -= f.off;
+        for (int i = 0; i < 8; ++i) x[i] -= f.off;
+      }
     }
     const f32x2 c2 = both2(c), nr = both2(-f.r), np = both2(-p_ref);
 #pragma unroll
@@ -177,7 +182,7 @@ __device__ __noinline__ TailRec redo_tail(const FusedRow<T, F, VEC>& row, int k0
 // (beside 10 items of 8 KB its ring is to leave room for a second CTA on the SM).
 template <typename T, int F>
 using LossCopies = std::conditional_t<F == kPlain, Copies<T, F, sizeof(T) == 2 ? 4 : 2, 2>,
-                                      Copies<T, F, sizeof(T) == 2 ? 4 : 2, 2>>;
+                                      Copies<T, F, 2, sizeof(T) == 2 ? 3 : 2>>;
 template <typename T, int F>
 using StepCopies = Copies<T, F, 2, sizeof(T) == 4 && F ? 2 : 4, true>;
 template <typename T, int F, bool GRAD>
@@ -477,7 +482,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
   st.init();
   float pa[8], pb[8];
   const unsigned char* bits8 = reinterpret_cast<const unsigned char*>(bitmap);
-  const auto item_of = [&](auto& v, auto& pr, int it) {
+  const auto item_of = [&](auto& v, auto& pr, int it, auto settled) {
     float x[8], s[8];
     v.template values<true>(row, pr, x, s);
     if constexpr (VEC) {
@@ -502,17 +507,26 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
         if (bitmap[b >> 5] >> (b & 31) & 1u) x[i] = -INFINITY;
       }
     }
-    st.push(x, s, pr, c, p_ref);
+    st.template push<decltype(settled)::value>(x, s, pr, c, p_ref);
     if constexpr (GRAD) {
       float4* keep = reinterpret_cast<float4*>(kept) + it * (2 * kStreamThreads) + tid;
       keep[0] = make_float4(x[0], x[1], x[2], x[3]);
       keep[kStreamThreads] = make_float4(x[4], x[5], x[6], x[7]);
     }
   };
-  stream.run([&](int g) { stream.each(g, pa, pb, item_of); }, item_of);
+  const auto any_of = [&](auto& v, auto& pr, int it) { item_of(v, pr, it, std::false_type{}); };
+  const auto settled_of = [&](auto& v, auto& pr, int it) { item_of(v, pr, it, std::true_type{}); };
+  stream.run(
+      [&](int g) {
+        if (st.settled()) stream.each(g, pa, pb, settled_of);
+        else stream.each(g, pa, pb, any_of);
+      },
+      any_of);
   WarpRec rec{st.record(), ListRec{-INFINITY, 0.f}};
-  if (!(fabsf(rec.t.sum) + fabsf(rec.t.s) + fabsf(rec.t.p) < INFINITY))
-    rec.t = redo_tail<T, F, VEC>(row, k0, k1, bitmap, GRAD ? reinterpret_cast<float*>(kept) : nullptr, c, p_ref);
+  if (!(fabsf(rec.t.sum) + fabsf(rec.t.s) + fabsf(rec.t.p) < INFINITY)) {
+    const FusedRow<T, F, VEC> its = row;     // (a copy has the address that the call takes: the stream's stays in registers)
+    rec.t = redo_tail<T, F, VEC>(its, k0, k1, bitmap, GRAD ? reinterpret_cast<float*>(kept) : nullptr, c, p_ref);
+  }
 
   // the listed columns of this slice; an id listed twice counts once in the student's sums
   bool once = mine;

@@ -510,15 +510,16 @@ struct RowStream {
       if (!row.has_s()) v.s.fill(0.f);
     }
   }
-  // l_P of whole item u of the current group (u may run past it; `aligned`: the prior's
-  // own place against 16 bytes, which is -sh, is 0).
-  __device__ __forceinline__ void prior(int u, bool aligned, float (&x)[8]) const {
+  // l_P of whole item u of the current group (u may run past it). ALIGNED: the prior's
+  // own place against 16 bytes, which is -sh, is 0.
+  template <bool ALIGNED>
+  __device__ __forceinline__ void prior(int u, float (&x)[8]) const {
     if constexpr (F != kPlain) {
       const float* at = p + u * kStreamStep;
       if (!row.has_p()) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = 0.f;
-      } else if (aligned) {
+      } else if (ALIGNED) {
         const float4 y = __ldg(reinterpret_cast<const float4*>(at));
         const float4 z = __ldg(reinterpret_cast<const float4*>(at + kHalf<T>));
         x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w; x[4] = z.x; x[5] = z.y; x[6] = z.z; x[7] = z.w;
@@ -544,7 +545,7 @@ struct RowStream {
           float pr[8];
           if (whole(at)) {
             take(u, v);
-            prior(u, false, pr);
+            prior<false>(u, pr);
           } else {
             v.load(row, at, k1, pr);
           }
@@ -559,21 +560,25 @@ struct RowStream {
     }
     drain();
   }
-  // As whole(group) of run() for fused rows: f(item, l_P, it) for each item, the prior
-  // out of L2 an item ahead, in two sets of registers by turns (copies between them took
-  // 8 instructions an item, loads at their use 700 cycles).
-  template <typename Fn>
-  __device__ __forceinline__ void each(int g, float (&pa)[8], float (&pb)[8], Fn&& f) const {
+  // As whole(group) of run(): f(item, l_P, it) for each item, the prior out of L2 an
+  // item ahead, in two sets of registers by turns (copies between them took 8
+  // instructions an item, loads at their use 700 cycles).
+  template <bool ALIGNED, typename Fn>
+  __device__ __forceinline__ void each_of(int g, float (&pa)[8], float (&pb)[8], Fn&& f) const {
     static_assert(U % 2 == 0 || F == kPlain, "two sets by turns");
-    const bool al = prior_aligned();
-    if (g == lo) prior(0, al, pa);
+    if (g == lo) prior<ALIGNED>(0, pa);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       Item<T, F, VEC> v;
       take(u, v);
-      if (u + 1 < U || g + 1 < hi) prior(u + 1, al, u & 1 ? pa : pb);
+      if (u + 1 < U || g + 1 < hi) prior<ALIGNED>(u + 1, u & 1 ? pa : pb);
       f(v, u & 1 ? pb : pa, g * U + u);
     }
+  }
+  template <typename Fn>
+  __device__ __forceinline__ void each(int g, float (&pa)[8], float (&pb)[8], Fn&& f) const {
+    if (F == kPlain || prior_aligned()) each_of<true>(g, pa, pb, f);
+    else each_of<false>(g, pa, pb, f);
   }
 };
 
