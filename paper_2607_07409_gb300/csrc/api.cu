@@ -2315,7 +2315,7 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
   const bool f32 = x->dtype == DELS_F32;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_DISTILL);
-  if (rows > 0 && distill_step_fits(a, f32, call.fused, call.vec))
+  if (rows > 0 && distill_step_fits(a, f32, call.fused, call.vec, device_sm_count()))
     return launch_distill_step(a, f32, call.fused, call.vec, s) == cudaSuccess ? DELS_OK : DELS_ERR_CUDA;
   if (rows > 0) {
     if (!plan_distill(&a, false)) return DELS_ERR_CUDA;

@@ -180,7 +180,7 @@ struct DistillArgs {
 cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 // Loss and gradient at once: a slice's values stay in shared memory.
 constexpr int kStepSmemBytes = 200 * 1024;
-bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec);
+bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec, int sms);
 cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_weight_grads(const DistillArgs& a, cudaStream_t s);

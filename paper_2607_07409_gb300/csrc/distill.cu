@@ -16,6 +16,7 @@
 // where the listed ids have nearly all mass), and the weights' gradients come from
 // sums taken along with the softmax's: no pass over the rows is added for them.
 // What bounds it: the rows' bytes (read both, write the gradient).
+#include <algorithm>
 #include <cfloat>
 
 #include "row_stream.cuh"
@@ -777,13 +778,26 @@ cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool
     return launch_loss_t<typename decltype(t)::type, decltype(f)::value, decltype(v)::value, true>(a, s);
   });
 }
-bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec) {
+// Whether the step reads its rows once (k_distill_loss with GRAD, a launch less) or
+// twice (k_distill_loss, then k_distill_grad). Once needs room for the slice's 2^z
+// beside the ring, and with it few CTAs share an SM: 1 to 3, which hide less of a CTA's
+// start and exchange than the 3 to 6 of the two launches. us, once against twice:
+//   one round of CTAs     24 bf16 rows of 151936: 19.5, 23.0 fused; 9.0, 18.0 plain
+//   more, fused bf16      40: 28.3, 25.8; 160: 68.1, 62.6; 1024: 321, 320
+//   up to two, plain bf16 76: 22.6, 24.3; more: 160: 39.6, 36.9; 600: 135, 108
+//   float32, two on an SM 160 of 100003: 74.5, 85.0 fused; 600: 117, 141 plain
+//   float32, one on an SM 256 of 151936 fused: 188, 144
+bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec, int sms) {
   size_t bytes = 0;
   dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
     bytes = loss_smem<typename decltype(t)::type, decltype(f)::value, decltype(v)::value, true>(a.in);
     return cudaSuccess;
   });
-  return bytes <= (size_t)kStepSmemBytes;
+  if (bytes > (size_t)kStepSmemBytes) return false;
+  const int per_sm = std::min(fused ? 2 : 3, (int)((228u << 10) / (bytes + 1024)));
+  if (f32 && per_sm >= 2) return true;
+  const long long ctas = (long long)a.in.rows * a.in.cluster, round = (long long)sms * per_sm;
+  return fused ? ctas * 5 <= round * 4 : ctas <= round * 2;
 }
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
   return dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
