@@ -88,8 +88,9 @@ __device__ __forceinline__ void merge_records(const WarpRec* recs, int n, float 
 // One lane's sums over the columns that are not listed, under its warp's reference:
 // that of the largest entry of the warp's first items. Nothing else is compared: the
 // sums' digits do not depend on the reference, and an entry 2^100 times as likely as
-// those (or one that is not a number) shows in sums that are not finite, which are
-// then taken again (redo). A running maximum took 10 instructions of an item's 100.
+// those (or one that is not a number) shows in sums that are not below 2^100, which are
+// then taken again (redo; the sums of a row's 64 warps together stay below 2^107). A
+// running maximum took 10 instructions of an item's 100.
 template <bool FUSED>
 struct WarpTail {
   float m;             // the same in every lane, as f
@@ -524,7 +525,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
       },
       any_of);
   WarpRec rec{st.record(), ListRec{-INFINITY, 0.f}};
-  if (!(fabsf(rec.t.sum) + fabsf(rec.t.s) + fabsf(rec.t.p) < INFINITY)) {
+  if (!(fabsf(rec.t.sum) + fabsf(rec.t.s) + fabsf(rec.t.p) < 0x1p100f)) {
     const FusedRow<T, F, VEC> its = row;     // (a copy has the address that the call takes: the stream's stays in registers)
     rec.t = redo_tail<T, F, VEC>(its, k0, k1, bitmap, GRAD ? reinterpret_cast<float*>(kept) : nullptr, c, p_ref);
   }

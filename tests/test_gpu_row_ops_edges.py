@@ -1,0 +1,217 @@
+"""Scoring and distillation of vocabulary rows where the kernels change their way of
+working: entries far above a row's first ones, masks in the local head's logits, terms
+that are absent or lie differently against 16-byte boundaries, slices that leave room
+for one CTA on an SM or none, the largest vocabularies. Bounds as in test_gpu_row_ops."""
+import math
+
+import pytest
+import torch
+
+import paper_2607_07409_gb300 as dels
+from test_gpu_row_ops import DEV, INF, LOW, Case, check_distill, check_score, eps_sum, gen, put, teacher
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+TAIL = pytest.mark.parametrize("tail", [False, True], ids=["renormalised", "tail"])
+VIA = pytest.mark.parametrize("via", ["step", "autograd"])
+
+
+class Placed(Case):
+    """A Case whose tensors on the device differ from the ones it computes with: `absent` ones are not passed
+    (they are zero on the host), `offsets` of their own, `masked` columns of the local head at -inf (on the host
+    the drafter's are, and the local head's are 0 there: the same rows, and sums without 0 * inf)."""
+
+    def __init__(self, *args, absent=(), offsets=None, **kw):
+        super().__init__(*args, **kw)
+        self.absent, self.offsets, self.masked = absent, offsets or {}, None
+        for name in absent:
+            getattr(self, name).zero_()
+
+    def mask(self, columns):
+        self.masked = columns
+        self.long[:, columns] = -INF
+        self.short[:, columns] = 0.0
+        self.plain_long = torch.zeros_like(self.long)
+
+    def dev(self, name):
+        if name in self.absent:
+            return None
+        t = getattr(self, name)
+        if self.masked is not None and name in ("long", "short"):
+            t = t.clone()
+            t[:, self.masked] = -INF if name == "short" else 1.0
+        if name == "prior":
+            t = put(t[None], self.offsets.get(name, 0))[0]
+            return t
+        return put(t, self.offsets.get(name, self.offset), self.pitch) if t.dim() == 2 else t.to(DEV)
+
+
+@DTYPES
+@TAIL
+@VIA
+@pytest.mark.parametrize("fused", [False, True], ids=["plain", "fused"])
+def test_distill_entries_far_above_the_first(fused, via, tail, dtype):
+    """Unlisted entries up to e^10000 times as likely as those that a row begins with, and rows that begin with such."""
+    V, rows = 20000, 8
+    c = Case(rows, V, dtype, 101, fused, n=3)
+    ids, t = teacher(c, 9, 3, tail, 1.0, missing=False)
+    free = [v for v in range(V - 1, 0, -1) if not (ids == v).any()]
+    for r, far in enumerate((75.0, 90.0, 200.0, 1e4)):
+        c.long[r, free[r]] = far
+    c.long[4, free[4]] = c.long[4, free[5]] = 150.0
+    first = [v for v in reversed(free) if v < 2000][:20]
+    c.long[5, first] = 500.0                       # the rest has nothing beside these
+    c.long[6, :16000] = torch.where(torch.arange(16000) % 2 == 0, -INF, c.long[6, :16000].float()).to(dtype)
+    c.long[6, ids[6].long()] = 1.0
+    c.long[7, :17000] = -INF                       # nothing in the first items of any lane
+    c.long[7, ids[7].long()] = 2.0
+    check_distill(c, 9, tail, ids_t=(ids, t), via=via)
+
+
+@DTYPES
+@VIA
+@pytest.mark.parametrize("fused", [False, True], ids=["plain", "fused"])
+def test_distill_entries_that_pass_the_range_together(fused, via, dtype):
+    """Sums of warps that are finite each, and not together: 2^126.96 sixty-four times, and other sizes near it."""
+    V, rows = 20000, 6
+    c = Case(rows, V, dtype, 109, fused, n=2, scale=0.0)
+    if fused:
+        c.short *= 0.01
+        c.prior *= 0.01
+    ids = torch.tensor([[3, 9, 12345]] * rows, dtype=torch.int32)
+    t = torch.log_softmax(torch.tensor([1.0, 0.5, 0.25, 0.0]), 0)[:3].expand(rows, 3).clone()
+    for r, far in enumerate((88.0, 87.0, 86.0, 84.0, 70.0, 60.0)):
+        c.long[r, 4000::250] = far
+    check_distill(c, 3, True, ids_t=(ids, t), via=via)
+
+
+@DTYPES
+@pytest.mark.parametrize("V", [3001, 20000])
+def test_row_ops_that_begin_with_the_lowest_value(V, dtype):
+    """Rows whose first part is masked by the type's lowest value, in one term and in all that have it."""
+    for fused in (False, True):
+        c = Case(5, V, dtype, 110, fused, n=5)
+        ids, t = teacher(c, 8, 3, True, 1.0, missing=False)
+        for r in range(4):
+            c.long[r, :V * (r + 1) // 5] = LOW[dtype]
+            c.long[r, ids[r].long()] = 1.0
+        c.size = lambda: torch.full((5,), 40.0).double()
+        check_distill(c, 8, True, ids_t=(ids, t))
+        check_distill(c, 8, False, ids_t=(ids, t), via="autograd")
+        assert check_score(c, 64)[-1] == 0
+
+
+@DTYPES
+@TAIL
+@VIA
+def test_distill_masks_in_the_local_head(via, tail, dtype):
+    """-inf among the local head's logits, listed ones too: no weight, no gradient, no NaN in the weights' gradients."""
+    c = Placed(6, 9000, dtype, 102, fused=True, n=2)
+    ids, t = teacher(c, 7, 3, tail, 1.0, missing=False)
+    listed = set(ids.flatten().tolist())
+    c.mask([v for v in range(0, 9000, 3) if v not in listed] + [8999 - v for v in range(40) if 8999 - v not in listed])
+    _, g, ga, gb, _ = check_distill(c, 7, tail, ids_t=(ids, t), via=via)
+    assert (g[:, c.masked] == 0).all() and torch.isfinite(ga).all() and torch.isfinite(gb).all()
+
+
+@DTYPES
+@VIA
+@pytest.mark.parametrize("absent", [("long",), ("prior",), ("long", "prior")], ids="-".join)
+@pytest.mark.parametrize("V", [777, 12000])
+def test_distill_terms_may_be_absent(V, absent, via, dtype):
+    """The prior's weight has no gradient without a prior."""
+    c = Placed(5, V, dtype, 103, fused=True, n=3, absent=absent)
+    ids, t = teacher(c, 6, 3, True, 1.0)
+    kw = dict(long=c.dev("long"), log_prior=c.dev("prior"), alpha=c.dev("alpha"))
+    if "prior" not in absent:
+        check_distill(c, 6, True, ids_t=(ids, t), via=via)
+        return
+    # (the reference with a prior of zeros; its beta's gradient is zero)
+    c2 = Case(5, V, dtype, 103, True, n=3)
+    c2.long, c2.prior = c.long, c.prior
+    loss, g, ga, _, _ = check_distill(c2, 6, True, ids_t=(ids, t), via=via)
+    weight = (torch.rand(5, generator=gen(3)) + 0.5).to(DEV)
+    short = c.dev("short")
+    if via == "step":
+        d = dels.Distiller(5, V, 6, dtype, n_weights=3, tail=True, device=DEV)
+        loss1, g1, ga1, gb1 = d.step(short, ids.to(DEV), t.to(DEV), row_weight=weight, **kw)
+        assert gb1 is None
+    else:
+        up = torch.rand(5, generator=gen(4)) + 0.5
+        short, al = short.requires_grad_(), kw.pop("alpha").requires_grad_()
+        loss1 = dels.distill_loss(short, ids.to(DEV), t.to(DEV), alpha=al, row_weight=weight, tail=True, **kw)
+        g1, ga1 = torch.autograd.grad(loss1, (short, al), up.to(DEV))
+    # the same numbers but for the order of their sums: twice the bounds that c2 holds
+    e = 2 * (16 * 2.0 ** -24 * c2.size() + eps_sum(V) + 2.0 ** -18).to(DEV)
+    assert ((loss1 - loss).abs().double() <= e * (2 + loss.abs().double() + math.log(V) + 20)).all()
+    unit = 2.0 ** -7 if dtype is torch.bfloat16 else 2.0 ** -18
+    assert ((g1 - g).double().norm(dim=-1) <= (unit + 8 * e) * g.double().norm(dim=-1)).all()
+    assert ((ga1 - ga).abs().double() <= 8 * float(e.max()) * 5 * float(c2.short.abs().max())).all()
+
+
+@DTYPES
+@TAIL
+@pytest.mark.parametrize("V", [1000, 5003, 30000])
+@pytest.mark.parametrize("offsets", [dict(long=1), dict(short=3), dict(prior=1), dict(long=5, short=2, prior=3)],
+                         ids=["long", "short", "prior", "all"])
+def test_row_ops_terms_that_lie_differently(offsets, V, tail, dtype):
+    """Terms whose rows begin at different places against 16-byte boundaries."""
+    c = Placed(4, V, dtype, 104, fused=True, n=4, offsets=offsets)
+    check_distill(c, 11, tail)
+    if tail:
+        assert check_score(c, 20)[-1] == 0
+    else:
+        check_distill(c, 11, tail, via="autograd")
+
+
+@DTYPES
+@pytest.mark.parametrize("fused", [False, True], ids=["plain", "fused"])
+@pytest.mark.parametrize("rows,V,K", [(20, 151936, 16), (1000, 300, 4), (1, 420001, 9), (2, 1 << 22, 12)])
+def test_distill_step_by_one_launch_or_two(rows, V, K, fused, dtype):
+    """Sizes on both sides of the step's choice; in place, as the second launch reads what it overwrites."""
+    c = Case(rows, V, dtype, 105, fused, n=4)
+    a = [None if x is None else x.clone() for x in check_distill(c, K, True)[:4]]
+    b = check_distill(c, K, True, in_place=True)
+    for u, v in zip(a, b):
+        assert u is None or torch.equal(u, v)
+
+
+def test_distill_is_differentiable_once():
+    c = Case(3, 200, torch.float32, 106, False)
+    ids, t = teacher(c, 4, 1, False, 1.0)
+    short = c.dev("long").requires_grad_()
+    loss = dels.distill_loss(short, ids.to(DEV), t.to(DEV)).sum()
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(loss, short, create_graph=True)
+    loss = dels.distill_loss(short, ids.to(DEV), t.to(DEV)).sum()
+    with torch.no_grad():
+        short.add_(1.0)                            # what the gradient reads has changed
+    with pytest.raises(RuntimeError):
+        loss.backward()
+
+
+@pytest.mark.parametrize("V", [150_000_001, 40_000_000])
+def test_score_very_long_rows(V):
+    """Alternatives and the token among hundreds of millions of columns, the first and the last of them too."""
+    x = torch.empty(1, V, dtype=torch.bfloat16, device=DEV)
+    x.normal_(generator=torch.Generator(DEV).manual_seed(107))
+    at = torch.randperm(V // 1000, generator=gen(108))[:64] * 1000
+    at[0], at[1] = 0, V - 1
+    top = torch.arange(64, 0, -1).float() + 16.0
+    x[0, at.to(DEV)] = top.to(torch.bfloat16).to(DEV)
+    token = torch.tensor([V - 1], dtype=torch.int32, device=DEV)
+    sc = dels.TokenScorer(1, V, 64, device=DEV)
+    lp, ent, ids, tlp = sc(x, token)
+    assert sc.status() == 0
+    assert torch.equal(ids[0].cpu().long(), at)
+    m, total, weighted = float(top[0]), 0.0, 0.0
+    for part in x[0].split(1 << 24):
+        z = part.double() - m
+        total += float(z.exp().sum())
+        weighted += float((z.exp() * z).sum())
+    ln = math.log(total)
+    tol = 2 * 8 * 2.0 ** -24 * m + eps_sum(V)
+    assert ((tlp[0].cpu().double() - (top.double() - m - ln)).abs() <= tol).all()
+    assert abs(float(lp[0]) - (float(top[1]) - m - ln)) <= tol
+    assert abs(float(ent[0]) - (ln - weighted / total)) <= tol * (math.log(V) + 3)
