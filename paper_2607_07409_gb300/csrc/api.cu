@@ -156,6 +156,18 @@ struct Scope {
 
 #define PROF(cls) prof::Scope prof_scope_(cls, s)
 
+// (A CTA's start, its records and their exchange cost it 3 to 8 us whatever its slice:
+// 1024 rows of 151936, 1, 2 and 4 CTAs a row: scoring with 64 alternatives 78, 109,
+// 158 us, the loss of fused rows 134, 129, 152.)
+void plan_cluster(StreamRows& in, int count, int sms, int least) {
+  int c = 1;
+  while (c < 8 && (c < least || ((long long)count * c * 5 < 8LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
+  in.cluster = c;
+  // whole items of every thread (positions: a row may start up to 7 columns past a
+  // 16-byte boundary)
+  in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, c > 1 ? 4096 : 8);
+}
+
 namespace {
 
 // ------------------------------------------------------------- tcgen05 plans
@@ -2118,7 +2130,8 @@ int rows_call(const dels_rows* x, int rows, int V, int max_v, RowsCall* out) {
   in.ld_long = ld_long;
   in.ld_short = ld_short;
   in.n_weights = std::max(1, x->n_weights);
-  in.rows = rows;
+  in.rows = in.count = rows;
+  in.first = in.beside = 0;
   in.V = V;
   in.inv_t = 1.f / x->temperature;
   in.minus_zero = -0.f;
@@ -2136,18 +2149,6 @@ int rows_call(const dels_rows* x, int rows, int V, int max_v, RowsCall* out) {
     in.shortp = nullptr;
   }
   return DELS_OK;
-}
-
-// CTAs per row: as many as bring 1.6 per SM into flight, at slices of 4096 columns and
-// more, a power of two up to 8; at least `least`. (A CTA's start, its records and their
-// exchange cost it 3 to 8 us whatever its slice: see the launches' comments.)
-void plan_cluster(StreamRows& in, int sms, int least) {
-  int c = 1;
-  while (c < 8 && (c < least || ((long long)in.rows * c * 5 < 8LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
-  in.cluster = c;
-  // whole items of every thread (positions: a row may start up to 7 columns past a
-  // 16-byte boundary)
-  in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, c > 1 ? 4096 : 8);
 }
 
 int distill_call(const dels_rows* x, int rows, int V, const dels_teacher* t, RowsCall* call, DistillArgs* a) {
@@ -2173,7 +2174,7 @@ bool plan_distill(DistillArgs* a, bool step) {
   const int sms = device_sm_count();
   if (sms <= 0) return false;
   const int slice = step ? 5 * 4096 : 1 << 19;                  // (a slice's bitmap: at most 64 KB)
-  plan_cluster(a->in, sms, (a->in.V + 7 + slice - 1) / slice);
+  plan_cluster(a->in, a->in.rows, sms, (a->in.V + 7 + slice - 1) / slice);
   return true;
 }
 
@@ -2222,7 +2223,7 @@ int dels_score_rows(const dels_rows* x, int rows, int V, const int32_t* tokens, 
     return DELS_ERR_ALIGNMENT;
   const int sms = device_sm_count();
   if (sms <= 0) return DELS_ERR_CUDA;
-  plan_cluster(call.in, sms, 1);
+  plan_cluster(call.in, rows, sms, 1);
   ScoreArgs a{};
   a.in = call.in;
   a.tokens = tokens;

@@ -123,7 +123,12 @@ struct StreamRows {
   float minus_zero;              // -0.f
   int cluster;                   // CTAs per row
   int slice_cols;                // columns per CTA (a multiple of 8)
+  int first, count;              // the rows of this launch
+  int beside;                    // it runs beside the one before it, which has other rows: see launch_rows()
 };
+// CTAs per row of a launch over `count` rows: as many as bring 1.6 per SM into flight,
+// at slices of 4096 columns and more, a power of two up to 8; at least `least`.
+void plan_cluster(StreamRows& in, int count, int sms, int least);
 
 constexpr int kMaxTopK = 256;
 constexpr int kMaxScoreV = 1 << 30;      // columns: offsets inside a row stay below 2^31

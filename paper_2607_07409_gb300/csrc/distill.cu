@@ -399,12 +399,11 @@ template <typename T, int F, bool VEC, bool GRAD>
 __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(DistillArgs a) {
   extern __shared__ __align__(16) unsigned bitmap[];   // one bit per position of the slice: listed
   __shared__ LossShared sh;
-  pdl_wait();
-  if (threadIdx.x == 0) pdl_trigger();
+  const long long r = begin_row(a.in);
+  if (r == a.in.rows) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = a.in.cluster, K = a.K, V = a.in.V;
   const int rank = (int)(blockIdx.x & (C - 1));
-  const long long r = blockIdx.x / (unsigned)C;
   const float c = a.in.scale, inv_t = a.in.inv_t;
   const float weight = a.row_weight ? __ldg(a.row_weight + r) : 1.f;
   // thread k has entry k (kMaxTopK <= kStreamThreads)
@@ -526,7 +525,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
       any_of);
   WarpRec rec{st.record(), ListRec{-INFINITY, 0.f}};
   if (!(fabsf(rec.t.sum) + fabsf(rec.t.s) + fabsf(rec.t.p) < 0x1p100f)) {
-    const FusedRow<T, F, VEC> its = row;     // (a copy has the address that the call takes: the stream's stays in registers)
+    const FusedRow<T, F, VEC> its = stream.anew();   // (the call takes its address: the stream's stays in registers)
     rec.t = redo_tail<T, F, VEC>(its, k0, k1, bitmap, GRAD ? reinterpret_cast<float*>(kept) : nullptr, c, p_ref);
   }
 
@@ -666,12 +665,11 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
 template <typename T, int F, bool VEC>
 __global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs a) {
   extern __shared__ __align__(16) uint8_t ring[];
-  pdl_wait();
-  if (threadIdx.x == 0) pdl_trigger();
+  const long long r = begin_row(a.in);
+  if (r == a.in.rows) return;
   const int tid = threadIdx.x;
   const int C = a.in.cluster, K = a.K;
   const int rank = (int)(blockIdx.x & (C - 1));
-  const long long r = blockIdx.x / (unsigned)C;
   RowStream<LossCopies<T, F>, T, F, VEC> stream(a.in, r, rank, ring, nullptr);
   const FusedRow<T, F, VEC>& row = stream.row;
   const int k0 = stream.k0, k1 = stream.k1, items = stream.items;
@@ -747,24 +745,24 @@ size_t loss_smem(const StreamRows& in) {
   return items * (kStreamStep / 8) + (VEC ? Cp::kRingBytes : 0) + (GRAD ? items * kStreamStep * 4 : 0);
 }
 
+// Rows from which a round of CTAs that is not full is split (launch_rows), us without
+// and with: 608 rows of 256 KB (65536 fused bf16) 40.6, 37.4 and the gradient 57.6,
+// 53.1; of 128 KB (the same alone) 16.9, 17.3. The loss of float32 rows is not: its
+// reads fill the time as they are (500 fused of 151936: 109, 119; their gradient 170, 145).
+constexpr int kSplitBytes = 1 << 18;
+
 template <typename T, int F, bool VEC, bool GRAD>
 cudaError_t launch_loss_t(const DistillArgs& a, cudaStream_t s) {
   const auto k = k_distill_loss<T, F, VEC, GRAD>;
-  const size_t bytes = loss_smem<T, F, VEC, GRAD>(a.in);
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
-  if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster));
-  return launch_pdl_cluster(k, grid, dim3(kStreamThreads), bytes, s, a.in.cluster, a);
+  const bool split = sizeof(T) == 2 && row_bytes<T, F>(a.in) >= kSplitBytes;
+  return launch_rows(k, a, true, split, loss_smem<T, F, VEC, GRAD>, s);
 }
 
 template <typename T, int F, bool VEC>
 cudaError_t launch_grad_t(const DistillArgs& a, cudaStream_t s) {
   const auto k = k_distill_grad<T, F, VEC>;
   const size_t bytes = VEC ? LossCopies<T, F>::kRingBytes : 0;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
-  if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster));
-  return launch_pdl(k, grid, dim3(kStreamThreads), bytes, s, a);
+  return launch_rows(k, a, false, row_bytes<T, F>(a.in) >= kSplitBytes, [&](const StreamRows&) { return bytes; }, s);
 }
 
 }  // namespace

@@ -421,6 +421,8 @@ struct RowStream {
   static constexpr int U = Cp::U, D = Cp::D, W = Cp::W, PC = Cp::kPiece;
   static constexpr int kRingGroup = U * Cp::kRing * PC, kStayGroup = U * Cp::kItemBytes;
   FusedRow<T, F, VEC> row;
+  const StreamRows& rows;  // to make `row` anew where it is rarely used: its pointers then take no registers on the way
+  unsigned r;
   int k0, k1, items, groups;
   int lo, hi;              // groups lo .. hi - 1 are whole
   uint8_t *ring, *stay;    // the calling thread's
@@ -433,8 +435,8 @@ struct RowStream {
   const float* p;          // l_P of its first item
   int pos;                 // its position
 
-  __device__ __forceinline__ RowStream(const StreamRows& rows, long long r, int rank, uint8_t* ring_, uint8_t* stay_)
-      : row(rows, r), ring(ring_ + threadIdx.x * 16), stay(stay_ + threadIdx.x * 16) {
+  __device__ __forceinline__ RowStream(const StreamRows& rows_, unsigned r_, int rank, uint8_t* ring_, uint8_t* stay_)
+      : row(rows_, r_), rows(rows_), r(r_), ring(ring_ + threadIdx.x * 16), stay(stay_ + threadIdx.x * 16) {
     const long long first = (long long)rank * rows.slice_cols;
     k0 = (int)min(first, (long long)row.end);
     k1 = (int)min(first + rows.slice_cols, (long long)row.end);
@@ -452,6 +454,7 @@ struct RowStream {
     out = ring;
     out_stay = stay;
   }
+  __device__ __forceinline__ FusedRow<T, F, VEC> anew() const { return FusedRow<T, F, VEC>(rows, r); }
   __device__ __forceinline__ bool whole(int at) const { return VEC && at >= row.sh && at + kHalf<T> + 4 <= k1; }
   __device__ __forceinline__ void copy(int u) const {
 #pragma unroll
@@ -547,7 +550,7 @@ struct RowStream {
             take(u, v);
             prior<false>(u, pr);
           } else {
-            v.load(row, at, k1, pr);
+            v.load(anew(), at, k1, pr);
           }
           f_ragged(v, pr, g * U + u);
         }
@@ -588,6 +591,62 @@ __device__ __forceinline__ void cluster_arrive_relaxed() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A row kernel's launch over the rows of `a`, of `smem(in)` dynamic bytes a CTA.
+//
+// `split`: where a CTA has a row, the rows past the last whole round of CTAs would leave most
+// of the device idle for a round. They get a launch of their own with more CTAs a row,
+// which starts as soon as those of the first have (programmatic launch) and fills
+// the places that they leave. It does not wait for the first launch, whose rows are
+// others (what is before both has ended: every CTA of the first has waited for it);
+// but what comes after must, so one more cluster of it does nothing but that wait.
+// Fused bf16 rows of 151936, one launch and two, us: 1024 rows the loss 133, 127, the
+// gradient 178, 162, scoring 166, 159; 500 rows 85, 74, 106, 84, 105, 84. Short rows
+// lose by it (1024 of 16384: 23.0, 27.0; 32.5, 32.4; 32.4, 39.8): see the callers' bounds.
+template <typename Args, typename Smem>
+cudaError_t launch_rows(void (*k)(Args), const Args& a, bool clusters, bool split, Smem&& smem, cudaStream_t s) {
+  const auto launch = [&](const Args& part) {
+    const size_t bytes = smem(part.in);
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)((long long)(part.in.count + part.in.beside) * part.in.cluster));
+    return launch_pdl_cluster(k, grid, dim3(kStreamThreads), bytes, s, clusters ? part.in.cluster : 1, part);
+  };
+  const int sms = device_sm_count();
+  if (split && a.in.cluster == 1 && a.in.count > sms) {
+    int per_sm = 0;
+    const size_t bytes = smem(a.in);
+    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, kStreamThreads, bytes);
+    if (e != cudaSuccess) return e;
+    const int round = per_sm * sms, rest = round > 0 ? a.in.count % round : 0;
+    Args tail = a;
+    plan_cluster(tail.in, rest, sms, 1);
+    if (rest > 0 && rest < a.in.count && tail.in.cluster > 1) {
+      Args whole = a;
+      whole.in.count = a.in.count - rest;
+      e = launch(whole);
+      if (e != cudaSuccess) return e;
+      tail.in.first = whole.in.count;
+      tail.in.count = rest;
+      tail.in.beside = 1;
+      return launch(tail);
+    }
+  }
+  return launch(a);
+}
+// Bytes of a row's logits.
+template <typename T, int F>
+long long row_bytes(const StreamRows& in) {
+  return (long long)in.V * (int)sizeof(T) * (F ? 2 : 1);
+}
+// The row of a CTA, once it may begin; in.rows: the cluster that waits (and has).
+__device__ __forceinline__ unsigned begin_row(const StreamRows& in) {
+  const unsigned r = (unsigned)in.first + blockIdx.x / (unsigned)in.cluster;
+  if (!in.beside || r == (unsigned)in.rows) pdl_wait();
+  if (threadIdx.x == 0) pdl_trigger();
+  return r;
+}
 
 // The kernel of a call: its logits' type, its rows' terms, and whether they lie alike
 // against 16-byte boundaries. launch(type, terms, vec) takes them as types.

@@ -325,12 +325,11 @@ template <typename T, int F, bool VEC>
 __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreArgs a) {
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ ScoreShared sh;
-  pdl_wait();
-  if (threadIdx.x == 0) pdl_trigger();
+  const long long r = begin_row(a.in);
+  if (r == a.in.rows) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = a.in.cluster, K = a.top_k;
   const int rank = (int)(blockIdx.x & (C - 1));
-  const long long r = blockIdx.x / (unsigned)C;
   const int V = a.in.V;
   const float c = a.in.scale;
   const int tok = a.tokens ? __ldg(a.tokens + r) : 0;
@@ -461,7 +460,7 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
   __syncthreads();
   const SoftRec cta = softrec_merge8(sh.warps[lane & 7], c);
 
-  if (K > 0) slice_top<U>(sh, *reinterpret_cast<SelectShared*>(dyn), bmax, shift, row, k0, k1, K, top);
+  if (K > 0) slice_top<U>(sh, *reinterpret_cast<SelectShared*>(dyn), bmax, shift, stream.anew(), k0, k1, K, top);
   SoftRec all = cta;
   if (C > 1) {
     cluster_wait();                // every CTA of the cluster runs before its shared memory is written
@@ -503,12 +502,15 @@ __global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreA
 template <typename T, int F, bool VEC>
 cudaError_t launch_score_t(const ScoreArgs& a, cudaStream_t s) {
   const auto k = k_score_rows<T, F, VEC>;
-  const size_t bytes = ring_bytes<T, F, VEC>() + (a.top_k > 0 ? (size_t)kSlots * kStreamThreads * 4 : 0) +
-                       (a.in.cluster > 1 ? (size_t)a.in.cluster * a.top_k * 8 : 0);
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), bytes);
-  if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)((long long)a.in.rows * a.in.cluster));
-  return launch_pdl_cluster(k, grid, dim3(kStreamThreads), bytes, s, a.in.cluster, a);
+  // the split: 1024, 608 and 500 bf16 rows of 608 KB gain 4 to 20 %, 1024 of 256 KB lose
+  // 3; float32 rows, whose reads fill the time as they are, lose too (500: 134, 143 us)
+  return launch_rows(
+      k, a, true, sizeof(T) == 2 && row_bytes<T, F>(a.in) > 1 << 19,
+      [&](const StreamRows& in) {
+        return ring_bytes<T, F, VEC>() + (a.top_k > 0 ? (size_t)kSlots * kStreamThreads * 4 : 0) +
+               (in.cluster > 1 ? (size_t)in.cluster * a.top_k * 8 : 0);
+      },
+      s);
 }
 
 }  // namespace

@@ -177,6 +177,56 @@ def test_distill_step_by_one_launch_or_two(rows, V, K, fused, dtype):
         assert u is None or torch.equal(u, v)
 
 
+@DTYPES
+def test_rows_past_the_last_whole_round(dtype):
+    """More rows than the device takes at once, in two launches side by side: the rows of the second against the
+    same rows alone, among them ones that are left out, and what the next call on the stream reads and overwrites."""
+    V, rows, n = 151936, 152 * 4 + 40, 3
+    g = torch.Generator(DEV).manual_seed(111)
+    long = torch.empty(rows, V, dtype=dtype, device=DEV).normal_(0, 3, generator=g)
+    short = torch.empty(rows, V, dtype=dtype, device=DEV).normal_(generator=g)
+    prior = torch.log_softmax(torch.randn(V, device=DEV, generator=g), 0)
+    alpha, beta = torch.tensor([0.5, 0.7, 0.2], device=DEV), torch.tensor([0.3, 0.1, 0.2], device=DEV)
+    kw = dict(log_prior=prior, alpha=alpha, beta=beta)
+    token = torch.randint(0, V, (rows,), device=DEV, generator=g, dtype=torch.int32)
+    weight = torch.rand(rows, device=DEV, generator=g)
+    token[-3], weight[-3] = -1, 0.0
+    sc = dels.TokenScorer(rows, V, 8, device=DEV)
+    d = dels.Distiller(rows, V, 8, dtype, n_weights=n, tail=True, device=DEV)
+    for _ in range(2):
+        score = sc(long, token, short=short, **kw)
+        _, _, ids, lp = score
+        target = lp - 0.1
+        out = d.step(short, ids, target, long=long, row_weight=weight, **kw)
+        copy = [x.clone() for x in score + out]                    # right behind them on the stream
+    assert sc.status() == 0 and d.status() == 0
+    for a, b in zip(copy, score + out):
+        assert torch.equal(a, b)
+    loss = dels.distill_loss(short, ids, target, long=long, row_weight=weight, tail=True, **kw)
+    assert torch.equal(loss, out[0]) or (loss - out[0]).abs().max() <= 1e-4
+    some = list(range(0, rows, 97)) + list(range(rows - 41, rows))
+    first = torch.tensor([r for r in some if r % n == 0], device=DEV)
+    kw1 = dict(log_prior=prior, alpha=alpha[:1], beta=beta[:1])
+    alone = dels.TokenScorer(len(first), V, 8, device=DEV)(long[first], token[first], short=short[first], **kw1)
+    assert torch.equal(alone[2], ids[first])
+    for k in (0, 1, 3):
+        assert torch.allclose(alone[k], score[k][first], rtol=0, atol=1e-4)
+    d1 = dels.Distiller(len(first), V, 8, dtype, tail=True, device=DEV)
+    alone = d1.step(short[first], ids[first], target[first], long=long[first], row_weight=weight[first], **kw1)
+    assert torch.allclose(alone[0], out[0][first], rtol=0, atol=1e-4)
+    # the order of sums differs: 2^-12 of a row's largest, and bf16's last place
+    close = 2.0 ** -12 + (2.0 ** -7 if dtype is torch.bfloat16 else 0.0)
+    a, b = alone[1].float(), out[1][first].float()
+    assert ((a - b).abs() <= close * b.abs() + 2.0 ** -16 * b.abs().amax(-1, keepdim=True)).all()
+    # the weights' gradients are the rows': each alone
+    ga = torch.zeros(n, device=DEV, dtype=torch.float64)
+    dl = dels.Distiller(rows, V, 8, dtype, n_weights=rows, tail=True, device=DEV)
+    each = dl.step(short, ids, target, long=long, row_weight=weight, log_prior=prior, alpha=alpha.repeat(rows)[:rows],
+                   beta=beta.repeat(rows)[:rows])
+    ga.index_add_(0, torch.arange(rows, device=DEV) % n, each[2].double())
+    assert ((ga - out[2]).abs() <= 1e-5 * each[2].double().abs().sum()).all()
+
+
 def test_distill_is_differentiable_once():
     c = Case(3, 200, torch.float32, 106, False)
     ids, t = teacher(c, 4, 1, False, 1.0)
