@@ -396,7 +396,7 @@ __device__ void twice_grads(const DistillArgs& a, LossShared& sh, long long r, b
 // sums them and the one that scales them, so that the rows are read once: 3 s V bytes
 // a row instead of 5 s V. Each thread reads back what it wrote itself.
 template <typename T, int F, bool VEC, bool GRAD>
-__global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(DistillArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, (GRAD ? 2 : 3) - kFewer<T, F>) k_distill_loss(DistillArgs a) {
   extern __shared__ __align__(16) unsigned bitmap[];   // one bit per position of the slice: listed
   __shared__ LossShared sh;
   const long long r = begin_row(a.in);
@@ -663,7 +663,7 @@ __global__ void __launch_bounds__(kStreamThreads, GRAD ? 2 : 3) k_distill_loss(D
 // then the listed ones over it. The rows' own logits may be the output (each column
 // is read before it is written).
 template <typename T, int F, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, 3) k_distill_grad(DistillArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, 3 - kFewer<T, F>) k_distill_grad(DistillArgs a) {
   extern __shared__ __align__(16) uint8_t ring[];
   const long long r = begin_row(a.in);
   if (r == a.in.rows) return;
@@ -788,12 +788,15 @@ cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool
 //   float32, one on an SM 256 of 151936 fused: 188, 144
 bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec, int sms) {
   size_t bytes = 0;
+  int per_sm = 0;
   dispatch_rows(a.in, f32, fused, vec, [&](auto t, auto f, auto v) {
-    bytes = loss_smem<typename decltype(t)::type, decltype(f)::value, decltype(v)::value, true>(a.in);
+    using T = typename decltype(t)::type;
+    constexpr int F = decltype(f)::value;
+    bytes = loss_smem<T, F, decltype(v)::value, true>(a.in);
+    per_sm = std::min((F ? 2 : 3) - kFewer<T, F>, (int)((228u << 10) / (bytes + 1024)));
     return cudaSuccess;
   });
   if (bytes > (size_t)kStepSmemBytes) return false;
-  const int per_sm = std::min(fused ? 2 : 3, (int)((228u << 10) / (bytes + 1024)));
   if (f32 && per_sm >= 2) return true;
   const long long ctas = (long long)a.in.rows * a.in.cluster, round = (long long)sms * per_sm;
   return fused ? ctas * 5 <= round * 4 : ctas <= round * 2;

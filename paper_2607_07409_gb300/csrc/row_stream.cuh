@@ -93,6 +93,11 @@ struct Raw8 {
 // What a row has: l_L as stored; any of the fusion's terms (an absent one counts as
 // zero); all of them.
 enum { kPlain = 0, kSome = 1, kFull = 2 };
+// Kernels of float32 rows with some of the terms, which test for each where it is used:
+// one CTA less on an SM than the others, for the registers that this takes (with as
+// many, spills in the stream: 304 rows of 151936, l_L and l_S, loss 148, 105 us).
+template <typename T, int F>
+constexpr int kFewer = F == kSome && sizeof(T) == 4 ? 1 : 0;
 
 // One row of l = (l_L + alpha l_S) - beta l_P, rounded to float32 after every
 // operation, so that equal inputs order equally wherever they are evaluated.

@@ -322,7 +322,7 @@ constexpr size_t ring_bytes() {
 }
 
 template <typename T, int F, bool VEC>
-__global__ void __launch_bounds__(kStreamThreads, F ? 3 : 4) k_score_rows(ScoreArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, (F ? 3 : 4) - kFewer<T, F>) k_score_rows(ScoreArgs a) {
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ ScoreShared sh;
   const long long r = begin_row(a.in);
