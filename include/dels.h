@@ -446,8 +446,10 @@ int dels_prior_estimate(const int32_t* tokens, const uint8_t* loss_mask, int64_t
  * Rows of fused logits (Section 4.3), as both operations below read them:
  *   l[r, v] = (long[r, v] + alpha[r mod n_weights] * short[r, v])
  *             - beta[r mod n_weights] * log_prior[v],
- * float32, rounded after every operation; z = l / temperature. A term whose
- * pointer is NULL is absent, and NULL weights are 1. Rows of B blocks of n
+ * z = l / temperature, in float32: dels_score_rows rounds l after every operation
+ * (equal terms give equal values, whatever the alignment), dels_distill_* once per
+ * term (two fused multiply-adds). A term whose pointer is NULL is absent, and NULL
+ * weights are 1. Rows of B blocks of n
  * positions in order take per-position weights with n_weights = n. (Position 0
  * has no head and no prior: give it rows of its own, or weights of 0.)
  * Unlike the drafting calls these take rows of any alignment and pitch, and the

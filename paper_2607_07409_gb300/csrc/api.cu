@@ -802,7 +802,7 @@ using namespace dels;
 
 extern "C" {
 
-int dels_version(void) { return 100; }
+int dels_version(void) { return 200; }
 
 int dels_profile_enable(int on) {
   prof::on = on != 0;

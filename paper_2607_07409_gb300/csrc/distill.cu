@@ -15,7 +15,12 @@
 // apart, so that q_t is a sum of its own terms (1 - sum q_ik would lose its digits
 // where the listed ids have nearly all mass), and the weights' gradients come from
 // sums taken along with the softmax's: no pass over the rows is added for them.
-// What bounds it: the rows' bytes (read both, write the gradient).
+//
+// What bounds it, on fused rows of 151936: 1024 bf16 rows' loss takes 128 us (4.9 TB/s:
+// instructions, see row_stream.cuh), their gradient 162 us (5.8 TB/s: the bytes), both as
+// one step 293 us, 64 rows 32 us; 256 float32 rows 55, 84 and 143 us (5.7 and 5.6 TB/s).
+// A row's bytes in one pass would be 3 s V: the step that reads once (GRAD below) is the
+// faster one for few rows only, as distill_step_fits() says.
 #include <algorithm>
 #include <cfloat>
 
@@ -597,7 +602,8 @@ __global__ void __launch_bounds__(kStreamThreads, (GRAD ? 2 : 3) - kFewer<T, F>)
   if (C > 1) cluster_arrive();
   if constexpr (GRAD) {
     // this warp's 2^z are relative to its own reference
-    const float k2 = ok ? up * sums.factor * (rec.t.m > -INFINITY ? ex2_approx(ref_shift(rec.t.f, sums.f, c)) : 0.f) : NAN;
+    const float unit = rec.t.m > -INFINITY ? ex2_approx(ref_shift(rec.t.f, sums.f, c)) : 0.f;
+    const float k2 = ok ? up * sums.factor * unit : NAN;
     const f32x2 kk = both2(k2);
     const float4* got = reinterpret_cast<const float4*>(kept) + tid;
 #pragma unroll 2
@@ -678,37 +684,29 @@ __global__ void __launch_bounds__(kStreamThreads, 3 - kFewer<T, F>) k_distill_gr
   T* out = static_cast<T*>(a.grad) + r * a.ld_grad - row.sh;
   if (st.weight == 0.f) {                          // left out
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int it = 0; it < items; ++it) grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
+    for (int it = 0; it < items; ++it)
+      grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, zero);
     return;
   }
   const float g0 = up * st.weight * a.in.inv_t * (F ? row.a : 1.f);
   const float c = a.in.scale;
   stream.begin();
 
+  // thread k has entry k: its logit is read before it may be written over
+  __shared__ int ids[kMaxTopK];                    // -1: none of this slice
+  __shared__ float probs[kMaxTopK];
   int id = -1;
-  float g_k = 0.f;
+  float lp = 0.f, x_k = 0.f;
   if (tid < K) {
     id = __ldg(a.ids + r * K + tid);
     const float t = __ldg(a.teacher + r * K + tid);
     if (id < 0 || id + row.sh < k0 || id + row.sh >= k1 || t == -INFINITY) id = -1;
     if (id >= 0) {
-      // every entry with this id, in their order; the last of them writes
-      const float lp = (t - st.t_max) * st.t_scale - st.log_norm;
-      const float x = row.contracted(row.l_at(id + row.sh), row.s_at(id + row.sh), row.p_at(id + row.sh));
-      float before = 0.f;
-      for (int k = 0; k < K; ++k) {
-        if (k == tid || __ldg(a.ids + r * K + k) != id) continue;
-        const float tk = __ldg(a.teacher + r * K + k);
-        if (tk == -INFINITY) continue;
-        if (k > tid) {
-          id = -1;
-          break;
-        }
-        before += expf((tk - st.t_max) * st.t_scale - st.log_norm);
-      }
-      const float lq = (x - st.base) * a.in.inv_t - st.base_ln;
-      g_k = g0 * (listed_grad(lq, lp, st.mass) - before);
+      lp = (t - st.t_max) * st.t_scale - st.log_norm;
+      x_k = row.contracted(row.l_at(id + row.sh), row.s_at(id + row.sh), row.p_at(id + row.sh));
+      probs[tid] = expf(lp);
     }
+    ids[tid] = id;
   }
   __syncthreads();                                 // the output may be l_S itself
   const float k2 = g0 * st.factor;
@@ -721,8 +719,17 @@ __global__ void __launch_bounds__(kStreamThreads, 3 - kFewer<T, F>) k_distill_gr
     grad_item<T, VEC>(out, v.k, row.sh, k1, a.grad_vec, g);
   };
   stream.run([&](int g) { stream.each(g, pa, pb, item_of); }, item_of);
-  __syncthreads();
-  if (id >= 0) grad_elem(out, id + row.sh, g_k);
+  __syncthreads();                                 // the columns as ones that are not listed are written
+  if (id < 0) return;
+  // every entry with this id, in their order; the last of them writes
+  float before = 0.f;
+  for (int k = 0; k < K; ++k) {
+    if (ids[k] != id || k == tid) continue;
+    if (k > tid) return;
+    before += probs[k];
+  }
+  const float lq = (x_k - st.base) * a.in.inv_t - st.base_ln;
+  grad_elem(out, id + row.sh, g0 * (listed_grad(lq, lp, st.mass) - before));
 }
 
 __global__ void __launch_bounds__(256) k_weight_grads(DistillArgs a) {

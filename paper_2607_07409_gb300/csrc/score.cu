@@ -4,10 +4,18 @@
 //   log q_v = (l_v - m) / T - ln S,   S = sum_v exp((l_v - m) / T)
 //   H       = ln S - (1 / S) sum_v exp((l_v - m) / T) (l_v - m) / T
 //
-// What bounds it: the read of the logits. The alternatives cost no second read of
-// the row: every thread keeps the largest entry of each of its blocks of a few
-// items; a value that K threads' largest reach is at most the K-th largest entry of
-// the slice, and only the blocks that reach it are read again for their entries.
+// The alternatives cost no second read of the row: every thread keeps the largest entry
+// of each of its blocks of a few items; a value that K threads' largest reach is at most
+// the K-th largest entry of the slice, and only the blocks that reach it are read again
+// for their entries.
+//
+// What bounds it, on rows of 151936: without alternatives 1024 bf16 rows take 58 us
+// (5.4 TB/s), the stream's instructions beside the reads. 64 alternatives make them 78 us
+// (4.0 TB/s): lists, gathers and sorts are some 13,000 cycles of latency for each CTA
+// that other CTAs' streams only partly hide, which is why few CTAs share a row. 128
+// fused float32 rows with 8 take 37 us (4.3 TB/s), 1024 fused bf16 rows with 20 157 us
+// (4.0 TB/s: 21 instructions a column, as every operation of the fused value is rounded).
+// One row is 10 us, the latency of one slice's stream, selection and merge.
 #include <cuda_bf16.h>
 
 #include "row_stream.cuh"
@@ -173,7 +181,8 @@ __device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel,
 __device__ void merge_best(ScoreShared& sh, SelectShared& sel, const unsigned long long* lists, int C, int K) {
   const int tid = threadIdx.x, lane = tid & 31, each = (K + C - 1) / C;
   if (tid == 0) sh.ncand = 0;
-  unsigned long long fair = lane < C ? lists[lane * K + each - 1] : ~0ull, one = lane < C ? lists[lane * K + K - 1] : 0ull;
+  unsigned long long fair = lane < C ? lists[lane * K + each - 1] : ~0ull;
+  unsigned long long one = lane < C ? lists[lane * K + K - 1] : 0ull;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) {
     const unsigned long long f = __shfl_xor_sync(0xFFFFFFFFu, fair, d), o = __shfl_xor_sync(0xFFFFFFFFu, one, d);
