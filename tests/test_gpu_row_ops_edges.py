@@ -265,3 +265,35 @@ def test_score_very_long_rows(V):
     assert ((tlp[0].cpu().double() - (top.double() - m - ln)).abs() <= tol).all()
     assert abs(float(lp[0]) - (float(top[1]) - m - ln)) <= tol
     assert abs(float(ent[0]) - (ln - weighted / total)) <= tol * (math.log(V) + 3)
+
+
+def test_rows_past_the_last_whole_round_under_a_graph():
+    """The two launches side by side captured, between calls of their own kind, and replayed on new inputs."""
+    V, rows = 151936, 152 * 3 + 50
+    long, short = (torch.empty(rows, V, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    alpha, prior = torch.ones(1, device=DEV), torch.full((V,), -math.log(V), device=DEV)
+    sc = dels.TokenScorer(rows, V, 4, device=DEV)
+    d = dels.Distiller(rows, V, 4, torch.bfloat16, tail=True, device=DEV)
+
+    def calls():
+        first = [x.clone() for x in sc(long, short=short, log_prior=prior, alpha=alpha)[1:]]
+        return first + list(d.step(short, first[1], first[2] - 0.5, long=long, log_prior=prior, alpha=alpha)[:3])
+
+    long.normal_(0, 2)
+    short.normal_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = calls()
+    for seed in (1, 2, 3):
+        torch.manual_seed(seed)
+        long.normal_(0, 2)
+        short.normal_()
+        g.replay()
+        got = [x.clone() for x in out]
+        for a, b in zip(got, calls()):
+            assert torch.equal(a, b)
