@@ -156,16 +156,39 @@ struct Scope {
 
 #define PROF(cls) prof::Scope prof_scope_(cls, s)
 
-// (A CTA's start, its records and their exchange cost it 3 to 8 us whatever its slice:
-// 1024 rows of 151936, 1, 2 and 4 CTAs a row: scoring with 64 alternatives 78, 109,
-// 158 us, the loss of fused rows 134, 129, 152.)
-void plan_cluster(StreamRows& in, int count, int sms, int least) {
-  int c = 1;
-  while (c < 8 && (c < least || ((long long)count * c * 5 < 8LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
+static void set_cluster(StreamRows& in, int c) {
   in.cluster = c;
   // whole items of every thread (positions: a row may start up to 7 columns past a
   // 16-byte boundary)
   in.slice_cols = (int)round_up((size_t)(in.V + 7 + c - 1) / c, c > 1 ? 4096 : 8);
+}
+
+// (A CTA's start, its records and their exchange cost it 3 to 8 us whatever its slice:
+// the loss of 1024 fused bf16 rows of 151936 by 1, 2 and 4 CTAs a row: 134, 129, 152 us.)
+void plan_cluster(StreamRows& in, int count, int sms, int least) {
+  int c = 1;
+  while (c < 8 && (c < least || ((long long)count * c * 5 < 8LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
+  set_cluster(in, c);
+}
+
+// Scoring's CTAs per row: one an SM, two where the rows are long, at slices worth a
+// selection and a place in the merge; with many alternatives, which both grow with,
+// longer ones. us by 1, 2, 4 and 8 CTAs a row:
+//   8 bf16 rows of 151936    16.2, 14.3, 11.0, 10.2; 64 alternatives 19.1, 18.0, 14.5, 15.4
+//   64                       17.0, 14.7, 13.1, 16.4;                  19.8, 18.4, 20.0, 30.4
+//   152                      18.1, 18.1, 23.6, 33.3;                  20.2, 26.6, 33.1, 49.2
+//   152 of 32768             9.1, 11.5, 17.5, 22.8;                   12.2, 18.0, 26.4, 38.7
+//   152 fused f32 of 151936  51.2, 40.4, 60.3, 68.3;                  57.7, 47.4, 68.9, 87.5
+void plan_score(StreamRows& in, long long row_bytes, int top_k, int sms) {
+  const bool many = top_k >= 32;
+  const int least = top_k > 128 ? 1 << 18 : many ? 1 << 16 : 1 << 15;    // bytes of a slice
+  int c = 1;
+  while (c < 8 && row_bytes >= 1 << 17 && row_bytes / (2 * c) >= least) {
+    const int ctas = c < 4 && row_bytes > (many ? 3 << 18 : 1 << 18) ? 2 * sms : sms;
+    if ((long long)in.rows * 2 * c > ctas) break;
+    c *= 2;
+  }
+  set_cluster(in, c);
 }
 
 namespace {
@@ -2223,7 +2246,8 @@ int dels_score_rows(const dels_rows* x, int rows, int V, const int32_t* tokens, 
     return DELS_ERR_ALIGNMENT;
   const int sms = device_sm_count();
   if (sms <= 0) return DELS_ERR_CUDA;
-  plan_cluster(call.in, rows, sms, 1);
+  const int terms = call.in.longp && call.in.shortp ? 2 : 1;
+  plan_score(call.in, (long long)V * (x->dtype == DELS_F32 ? 4 : 2) * terms, top_k, sms);
   ScoreArgs a{};
   a.in = call.in;
   a.tokens = tokens;

@@ -56,10 +56,9 @@ struct ScoreShared {
 };
 
 // The K largest of cand[0 .. n) to best[] in order (all threads). Up to 128: each one's
-// place is the number above it, counted by the threads that share it. Up to 1024: a
-// bitonic network, E a thread, exchanges inside a warp by shuffles. (Cycles of 36, 95
-// and 220: 1300, 2700 and 9000 counted, 3500, 5000 and 6500 by the network.) More
-// (rows of ties): counted by a thread each.
+// place is the number above it, counted by the threads that share it. More: a bitonic
+// network, E a thread, exchanges inside a warp by shuffles. (Cycles of 36, 95 and 220:
+// 1300, 2700 and 9000 counted, 3500, 5000 and 6500 by the network.)
 template <int E>
 __device__ __forceinline__ void sort_network(ScoreShared& sh, SelectShared& sel, int n, int K) {
   const int tid = threadIdx.x;
@@ -111,6 +110,8 @@ __device__ void sort_best(ScoreShared& sh, SelectShared& sel, int n, int K) {
   if (n > 128 && n <= kStreamThreads) return sort_network<1>(sh, sel, n, K);
   if (n > 128 && n <= 2 * kStreamThreads) return sort_network<2>(sh, sel, n, K);
   if (n > 128 && n <= 4 * kStreamThreads) return sort_network<4>(sh, sel, n, K);
+  if (n > 128) return sort_network<8>(sh, sel, n, K);
+  static_assert(kCandidates <= 8 * kStreamThreads, "eight a thread at most");
   for (int k = tid; k < K; k += kStreamThreads) sh.best[k] = 0ull;
   __syncthreads();
   int log_share = 0;               // 2^log_share threads a candidate
@@ -202,6 +203,40 @@ __device__ void merge_best(ScoreShared& sh, SelectShared& sel, const unsigned lo
   sort_best(sh, sel, sh.ncand, K);
 }
 
+// What at least K entries of the slice reach, as order_u32, for more than 128 entries
+// (all threads): four lists a warp of 32 maxima in order, each of every fourth block of
+// its threads, and of each list its share of K. From the threads' maxima alone 256 entries
+// are the least of all of them, which thousands reach (one row: 200 us, from these 33).
+__device__ __noinline__ unsigned reached_by_blocks(SelectShared& sel, const float* bmax, int slots, int K) {
+  constexpr int kPer = 4;
+  static_assert(kStreamWarps * kPer == 32, "a lane for every list");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  float* lists = reinterpret_cast<float*>(sel.cand);
+  int* counts = sel.jobs;
+  for (int j = 0; j < kPer; ++j) {
+    float t = -INFINITY;
+    for (int b = j; b < slots; b += kPer) t = fmaxf(t, bmax[b * kStreamThreads + tid]);
+    const int have = __popc(__ballot_sync(0xFFFFFFFFu, t > -INFINITY));
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+      for (int d = k >> 1; d > 0; d >>= 1) {
+        const float o = __shfl_xor_sync(0xFFFFFFFFu, t, d);
+        t = ((lane & k) == 0) == ((lane & d) == 0) ? fmaxf(t, o) : fminf(t, o);
+      }
+    lists[(warp * kPer + j) * 32 + lane] = t;
+    if (lane == 0) counts[warp * kPer + j] = have;
+  }
+  __syncthreads();
+  const int cnt = counts[lane];
+  const int live = __popc(__ballot_sync(0xFFFFFFFFu, cnt > 0));
+  const int each = live ? (K + live - 1) / live : K;
+  const bool fair = __all_sync(0xFFFFFFFFu, cnt == 0 || cnt >= each) && live;
+  const float least = -warp_max(cnt > 0 && cnt >= each ? -lists[lane * 32 + each - 1] : -INFINITY);
+  __syncthreads();                 // (the lists' place is the jobs' and the entries')
+  return order_u32(fair ? least : -INFINITY);
+}
+
 // This CTA's K largest entries of its slice into sh.best. `top`: the largest
 // entry of the calling thread; bmax: [slot][thread] the largest of a thread's groups
 // slot << shift .. of the stream.
@@ -238,6 +273,7 @@ __device__ void slice_top(ScoreShared& sh, SelectShared& sel, const float* bmax,
     const float one = warp_max(K <= cnt ? sh.lanes[w][K - 1] : -INFINITY);
     tau = order_u32(fmaxf(fair ? least_of : -INFINITY, one));
   }
+  if (K > 128) tau = reached_by_blocks(sel, bmax, slots, K);
   const float least = from_order_u32(tau);
   unsigned long long floor_key = (unsigned long long)tau << 32;     // what an entry has to reach
   unsigned hits = 0u;                                               // (kSlots bits)
