@@ -171,15 +171,18 @@ void plan_cluster(StreamRows& in, int count, int sms, int least) {
   set_cluster(in, c);
 }
 
-// Scoring's CTAs per row: one an SM, two where the rows are long, at slices worth a
-// selection and a place in the merge; with many alternatives, which both grow with,
-// longer ones. us by 1, 2, 4 and 8 CTAs a row:
+// A call's CTAs per row: one an SM, two where the rows are long, at slices worth a CTA's
+// start, records and exchange; with many alternatives (scoring), which a selection and
+// its place in the merge grow with, longer ones. us by 1, 2, 4 and 8 CTAs a row, scoring:
 //   8 bf16 rows of 151936    16.2, 14.3, 11.0, 10.2; 64 alternatives 19.1, 18.0, 14.5, 15.4
 //   64                       17.0, 14.7, 13.1, 16.4;                  19.8, 18.4, 20.0, 30.4
 //   152                      18.1, 18.1, 23.6, 33.3;                  20.2, 26.6, 33.1, 49.2
 //   152 of 32768             9.1, 11.5, 17.5, 22.8;                   12.2, 18.0, 26.4, 38.7
 //   152 fused f32 of 151936  51.2, 40.4, 60.3, 68.3;                  57.7, 47.4, 68.9, 87.5
-void plan_score(StreamRows& in, long long row_bytes, int top_k, int sms) {
+// loss of fused bf16 rows:
+//   38, 96, 240 of 32768     9.3, 8.2, 7.5, 8.4;  7.9, 9.1, 11.8, 19.0;  14.3, 17.3, 22.3, 34.0
+//   240 of 8192              7.6, 12.8, 16.3, 27.9
+static void plan_rows(StreamRows& in, long long row_bytes, int top_k, int sms) {
   const bool many = top_k >= 32;
   const int least = top_k > 128 ? 1 << 18 : many ? 1 << 16 : 1 << 15;    // bytes of a slice
   int c = 1;
@@ -2191,14 +2194,34 @@ int distill_call(const dels_rows* x, int rows, int V, const dels_teacher* t, Row
   return DELS_OK;
 }
 
-// `step`: slices whose values leave room for a second CTA on the SM, where 8 CTAs
-// per row reach that.
-bool plan_distill(DistillArgs* a, bool step) {
+// CTAs per row of the loss and of the gradient (a slice's bitmap: at most 64 KB).
+bool plan_distill(DistillArgs* a, bool f32) {
   const int sms = device_sm_count();
   if (sms <= 0) return false;
-  const int slice = step ? 5 * 4096 : 1 << 19;                  // (a slice's bitmap: at most 64 KB)
-  plan_cluster(a->in, a->in.rows, sms, (a->in.V + 7 + slice - 1) / slice);
+  StreamRows& in = a->in;
+  const long long row_bytes = (long long)in.V * (f32 ? 4 : 2) * (in.longp && in.shortp ? 2 : 1);
+  // long rows gain by more CTAs than one or two an SM: 96 and 200 fused bf16 rows of
+  // 151936 with plan_rows' 2 and 1 CTAs a row 20.8 and 39.8 us, with 4 and 2 17.5 and 29.9
+  if (row_bytes > 1 << 18) plan_cluster(in, in.rows, sms, 1);
+  else plan_rows(in, row_bytes, 0, sms);
+  int c = in.cluster;
+  while (c < 8 && in.V / c >= 1 << 19) c *= 2;
+  set_cluster(in, c);
   return true;
+}
+// Whether the step reads its rows once: with these CTAs a row, with half as many (the
+// launch may then be one round), or with as many as leave room for a second CTA on an SM.
+bool plan_step(DistillArgs* a, bool f32, bool fused, bool vec) {
+  const int sms = device_sm_count(), c = a->in.cluster;
+  int wide = 1;
+  while (wide < 8 && (a->in.V + 7) / wide > 5 * 4096) wide *= 2;
+  for (const int t : {c, c / 2, std::max(c, wide)}) {
+    if (t < 1) continue;
+    set_cluster(a->in, t);
+    if (distill_step_fits(*a, f32, fused, vec, sms)) return true;
+  }
+  set_cluster(a->in, c);
+  return false;
 }
 
 // The gradient's side of a call.
@@ -2247,7 +2270,7 @@ int dels_score_rows(const dels_rows* x, int rows, int V, const int32_t* tokens, 
   const int sms = device_sm_count();
   if (sms <= 0) return DELS_ERR_CUDA;
   const int terms = call.in.longp && call.in.shortp ? 2 : 1;
-  plan_score(call.in, (long long)V * (x->dtype == DELS_F32 ? 4 : 2) * terms, top_k, sms);
+  plan_rows(call.in, (long long)V * (x->dtype == DELS_F32 ? 4 : 2) * terms, top_k, sms);
   ScoreArgs a{};
   a.in = call.in;
   a.tokens = tokens;
@@ -2285,7 +2308,7 @@ int dels_distill_loss(const dels_rows* x, int rows, int V, const dels_teacher* t
   if (state_bytes < dels_distill_state_bytes(rows)) return DELS_ERR_WORKSPACE;
   if (!aligned16(workspace) || !aligned16(state) || (reinterpret_cast<uintptr_t>(out_loss) & 3u))
     return DELS_ERR_ALIGNMENT;
-  if (!plan_distill(&a, false)) return DELS_ERR_CUDA;
+  if (!plan_distill(&a, x->dtype == DELS_F32)) return DELS_ERR_CUDA;
   a.out_loss = out_loss;
   a.state = static_cast<DistillState*>(state);
   a.status = at<int>(workspace, 0);
@@ -2309,7 +2332,7 @@ int dels_distill_grad(const dels_rows* x, int rows, int V, const dels_teacher* t
     if (state_bytes < dels_distill_state_bytes(rows)) return DELS_ERR_WORKSPACE;
     if (!aligned16(state) || (reinterpret_cast<uintptr_t>(grad_loss) & 3u)) return DELS_ERR_ALIGNMENT;
   }
-  if (!plan_distill(&a, false)) return DELS_ERR_CUDA;
+  if (!plan_distill(&a, x->dtype == DELS_F32)) return DELS_ERR_CUDA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   a.state = static_cast<DistillState*>(const_cast<void*>(state));
   a.grad_loss = grad_loss;
@@ -2332,7 +2355,7 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
   if (rc != DELS_OK) return rc;
   if (rows > 0 && !out_loss) return DELS_ERR_NULL_POINTER;
   if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(out_loss) & 3u)) return DELS_ERR_ALIGNMENT;
-  if (!plan_distill(&a, true)) return DELS_ERR_CUDA;
+  if (!plan_distill(&a, x->dtype == DELS_F32)) return DELS_ERR_CUDA;
   a.out_loss = out_loss;
   a.ticket = at<int>(workspace, 64);
   a.state = at<DistillState>(workspace, kHeaderBytes);
@@ -2340,10 +2363,9 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
   const bool f32 = x->dtype == DELS_F32;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_DISTILL);
-  if (rows > 0 && distill_step_fits(a, f32, call.fused, call.vec, device_sm_count()))
+  if (rows > 0 && plan_step(&a, f32, call.fused, call.vec))
     return launch_distill_step(a, f32, call.fused, call.vec, s) == cudaSuccess ? DELS_OK : DELS_ERR_CUDA;
   if (rows > 0) {
-    if (!plan_distill(&a, false)) return DELS_ERR_CUDA;
     if (launch_distill_loss(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
     if (launch_distill_grad(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
   }
