@@ -165,9 +165,9 @@ static void set_cluster(StreamRows& in, int c) {
 
 // (A CTA's start, its records and their exchange cost it 3 to 8 us whatever its slice:
 // the loss of 1024 fused bf16 rows of 151936 by 1, 2 and 4 CTAs a row: 134, 129, 152 us.)
-void plan_cluster(StreamRows& in, int count, int sms, int least) {
+void plan_cluster(StreamRows& in, int count, int sms) {
   int c = 1;
-  while (c < 8 && (c < least || ((long long)count * c * 5 < 8LL * sms && in.V / (2 * c) >= 4096))) c *= 2;
+  while (c < 8 && (long long)count * c * 5 < 8LL * sms && in.V / (2 * c) >= 4096) c *= 2;
   set_cluster(in, c);
 }
 
@@ -180,7 +180,7 @@ void plan_cluster(StreamRows& in, int count, int sms, int least) {
 //   152 of 32768             9.1, 11.5, 17.5, 22.8;                   12.2, 18.0, 26.4, 38.7
 //   152 fused f32 of 151936  51.2, 40.4, 60.3, 68.3;                  57.7, 47.4, 68.9, 87.5
 // loss of fused bf16 rows:
-//   38, 96, 240 of 32768     9.3, 8.2, 7.5, 8.4;  7.9, 9.1, 11.8, 19.0;  14.3, 17.3, 22.3, 34.0
+//   38, 96, 240 of 32768     9.3, 8.2, 7.5, 8.4;  9.4, 9.6, 9.7, 15.3;  14.3, 17.3, 22.3, 34.0
 //   240 of 8192              7.6, 12.8, 16.3, 27.9
 static void plan_rows(StreamRows& in, long long row_bytes, int top_k, int sms) {
   const bool many = top_k >= 32;
@@ -2202,7 +2202,7 @@ bool plan_distill(DistillArgs* a, bool f32) {
   const long long row_bytes = (long long)in.V * (f32 ? 4 : 2) * (in.longp && in.shortp ? 2 : 1);
   // long rows gain by more CTAs than one or two an SM: 96 and 200 fused bf16 rows of
   // 151936 with plan_rows' 2 and 1 CTAs a row 20.8 and 39.8 us, with 4 and 2 17.5 and 29.9
-  if (row_bytes > 1 << 18) plan_cluster(in, in.rows, sms, 1);
+  if (row_bytes > 1 << 18) plan_cluster(in, in.rows, sms);
   else plan_rows(in, row_bytes, 0, sms);
   int c = in.cluster;
   while (c < 8 && in.V / c >= 1 << 19) c *= 2;

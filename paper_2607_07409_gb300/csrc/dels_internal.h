@@ -127,8 +127,8 @@ struct StreamRows {
   int beside;                    // it runs beside the one before it, which has other rows: see launch_rows()
 };
 // CTAs per row of a launch over `count` rows: as many as bring 1.6 per SM into flight,
-// at slices of 4096 columns and more, a power of two up to 8; at least `least`.
-void plan_cluster(StreamRows& in, int count, int sms, int least);
+// at slices of 4096 columns and more, a power of two up to 8.
+void plan_cluster(StreamRows& in, int count, int sms);
 
 constexpr int kMaxTopK = 256;
 constexpr int kMaxScoreV = 1 << 30;      // columns: offsets inside a row stay below 2^31

@@ -110,7 +110,8 @@ struct WarpTail {
   __device__ __forceinline__ bool settled() const { return m > -INFINITY && f.off == 0.f; }
   // One item's values, all lanes converged: x becomes 2^z.
   template <bool SETTLED>
-  __device__ __forceinline__ void push(float (&x)[8], const float (&sv)[8], const float (&pr)[8], float c, float p_ref) {
+  __device__ __forceinline__ void push(float (&x)[8], const float (&sv)[8], const float (&pr)[8], float c,
+                                       float p_ref) {
     if (!SETTLED) {
       if (m == -INFINITY) {
         m = warp_max(max8(x));

@@ -635,7 +635,7 @@ cudaError_t launch_rows(void (*k)(Args), const Args& a, bool clusters, bool spli
     if (e != cudaSuccess) return e;
     const int round = per_sm * sms, rest = round > 0 ? a.in.count % round : 0;
     Args tail = a;
-    plan_cluster(tail.in, rest, sms, 1);
+    plan_cluster(tail.in, rest, sms);
     if (rest > 0 && rest < a.in.count && tail.in.cluster > 1) {
       Args whole = a;
       whole.in.count = a.in.count - rest;

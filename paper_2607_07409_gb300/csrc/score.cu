@@ -159,8 +159,8 @@ __device__ __forceinline__ int reserve(int* count, int n) {
 // The entries among x[8] of an item at `pos` that reach `floor_key`, into cand[] as far
 // as it has room (all lanes converged; of no thread's item: x = -inf).
 template <typename T, int F, bool VEC>
-__device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel, const FusedRow<T, F, VEC>& row, int pos,
-                                             const float (&x)[8], unsigned long long floor_key) {
+__device__ __forceinline__ void keep_entries(ScoreShared& sh, SelectShared& sel, const FusedRow<T, F, VEC>& row,
+                                             int pos, const float (&x)[8], unsigned long long floor_key) {
   const float least = from_order_u32((unsigned)(floor_key >> 32));
   unsigned hits = 0u;
 #pragma unroll
@@ -540,7 +540,8 @@ __global__ void __launch_bounds__(kStreamThreads, (F ? 3 : 4) - kFewer<T, F>) k_
     const unsigned long long e = sh.best[k];
     const bool has = ok && e != 0ull;
     a.out_ids[r * K + k] = has ? (int)(0xFFFFFFFFu - (unsigned)e) : -1;
-    a.out_top_lp[r * K + k] = !ok ? NAN : has ? (from_order_u32((unsigned)(e >> 32)) - all.m) * inv_t - ln_s : -INFINITY;
+    const float lq = (from_order_u32((unsigned)(e >> 32)) - all.m) * inv_t - ln_s;
+    a.out_top_lp[r * K + k] = !ok ? NAN : has ? lq : -INFINITY;
   }
 }
 
