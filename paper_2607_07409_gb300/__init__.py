@@ -755,17 +755,23 @@ class Distiller:
         return dels_read_status(self.workspace, stream)
 
 
+def _distill_structs(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature):
+    """``dels_rows`` and ``dels_teacher`` of a distillation's tensors, on one device."""
+    if short.dim() != 2:
+        raise ValueError("short must be [rows, V]")
+    rows, V = short.shape
+    if ids.get_device() != short.get_device():
+        raise ValueError(f"ids must be on {short.device}")
+    return (rows_of(rows, V, long, short, log_prior, alpha, beta, temperature),
+            teacher_of(rows, ids, logprob, row_weight, tail))
+
+
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature):
-        if short.dim() != 2:
-            raise ValueError("short must be [rows, V]")
+        x, t = _distill_structs(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature)
         rows, V = short.shape
         dev = short.device
-        if ids.get_device() != short.get_device():
-            raise ValueError(f"ids must be on {dev}")
-        x = rows_of(rows, V, long, short, log_prior, alpha, beta, temperature)
-        t = teacher_of(rows, ids, logprob, row_weight, tail)
         loss = torch.empty(rows, dtype=torch.float32, device=dev)
         # the state, and a workspace whose status word is not read (flagged rows are NaN)
         nbytes = dels_distill_state_bytes(rows)
@@ -774,24 +780,28 @@ class _DistillLoss(torch.autograd.Function):
                                     nbytes, state.data_ptr() + nbytes, 256, _stream(None))
         if r != DELS_OK:
             raise DelsError(r, "dels_distill_loss")
-        # the tensors themselves are saved, so that backward() sees whether they were changed since
+        # the tensors, not their addresses: backward() sees whether they were changed since, and takes what
+        # saved-tensor hooks give back in their place (checkpointing: rows made again, the first ones freed)
         ctx.save_for_backward(short, alpha, beta, long, log_prior, ids, logprob, row_weight, state)
-        ctx.call = x, t, nbytes, beta is not None and log_prior is not None
+        ctx.how = tail, temperature
         return loss
 
     @staticmethod
     def backward(ctx, grad_loss):
         if torch.is_grad_enabled():
             raise RuntimeError("distill_loss is differentiable once")
-        short, alpha, beta, _, _, _, _, _, state = ctx.saved_tensors
-        x, t, nbytes, has_prior = ctx.call
+        *tensors, state = ctx.saved_tensors
+        x, t = _distill_structs(*tensors, *ctx.how)
+        short, alpha, beta, _, log_prior = tensors[:5]
         rows, V = short.shape
+        nbytes = dels_distill_state_bytes(rows)
+        at_state = _of(state, torch.uint8, (nbytes + 256,), short.get_device(), "the saved state")
         grad = torch.empty(rows, V, dtype=short.dtype, device=short.device)
         ga = torch.empty_like(alpha) if alpha is not None and ctx.needs_input_grad[1] else None
-        gb = torch.empty_like(beta) if has_prior and ctx.needs_input_grad[2] else None
+        gb = torch.empty_like(beta) if beta is not None and log_prior is not None and ctx.needs_input_grad[2] else None
         if grad_loss.dtype is not torch.float32 or not grad_loss.is_contiguous():
             grad_loss = grad_loss.to(torch.float32).contiguous()
-        r = lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(t), grad_loss.data_ptr(), state.data_ptr(),
+        r = lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(t), grad_loss.data_ptr(), at_state,
                                     nbytes, grad.data_ptr(), V, None if ga is None else ga.data_ptr(),
                                     None if gb is None else gb.data_ptr(), _stream(None))
         if r != DELS_OK:
