@@ -766,6 +766,19 @@ def _distill_structs(short, alpha, beta, long, log_prior, ids, logprob, row_weig
             teacher_of(rows, ids, logprob, row_weight, tail))
 
 
+def _address(t) -> Optional[int]:
+    return None if t is None else t.data_ptr() or None      # (ctypes gives an address of 0 back as None)
+
+
+def _holds(x: Rows, t: Teacher, shape, short, alpha, beta, long, log_prior, ids, logprob, row_weight) -> bool:
+    """Whether the structures are those of these tensors: their addresses, the rows' type, shape and pitches."""
+    return (short.shape == shape and x.dtype == dtype_code(short.dtype)
+            and x.short_logits == _address(short) and x.short_stride == _row_stride(short, shape, "short")
+            and x.long_logits == _address(long) and (long is None or x.long_stride == _row_stride(long, shape, "long"))
+            and x.log_prior == _address(log_prior) and x.alpha == _address(alpha) and x.beta == _address(beta)
+            and t.ids == _address(ids) and t.logprob == _address(logprob) and t.row_weight == _address(row_weight))
+
+
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature):
@@ -783,7 +796,7 @@ class _DistillLoss(torch.autograd.Function):
         # the tensors, not their addresses: backward() sees whether they were changed since, and takes what
         # saved-tensor hooks give back in their place (checkpointing: rows made again, the first ones freed)
         ctx.save_for_backward(short, alpha, beta, long, log_prior, ids, logprob, row_weight, state)
-        ctx.how = tail, temperature
+        ctx.call = x, t, (rows, V), tail, temperature
         return loss
 
     @staticmethod
@@ -791,11 +804,12 @@ class _DistillLoss(torch.autograd.Function):
         if torch.is_grad_enabled():
             raise RuntimeError("distill_loss is differentiable once")
         *tensors, state = ctx.saved_tensors
-        x, t = _distill_structs(*tensors, *ctx.how)
+        x, t, (rows, V), tail, temperature = ctx.call
+        if not _holds(x, t, (rows, V), *tensors):
+            x, t = _distill_structs(*tensors, tail, temperature)
         short, alpha, beta, _, log_prior = tensors[:5]
-        rows, V = short.shape
-        nbytes = dels_distill_state_bytes(rows)
-        at_state = _of(state, torch.uint8, (nbytes + 256,), short.get_device(), "the saved state")
+        nbytes = state.numel() - 256
+        at_state = _of(state, torch.uint8, state.shape, short.get_device(), "the saved state")
         grad = torch.empty(rows, V, dtype=short.dtype, device=short.device)
         ga = torch.empty_like(alpha) if alpha is not None and ctx.needs_input_grad[1] else None
         gb = torch.empty_like(beta) if beta is not None and log_prior is not None and ctx.needs_input_grad[2] else None
