@@ -51,6 +51,20 @@ struct __align__(16) WarpRec {
 };
 static_assert(sizeof(WarpRec) == 32, "two 16-byte words");
 
+// A row's sums in units in which that of the columns that are not listed is from 1 to 2:
+// the reference came from some of a row's first columns, 2^100 below others perhaps. What is
+// asked of the sums (how far the listed ones are above them, 1 / (sum + listed)) is then
+// asked of the sums and not of the reference. Scaled by powers of two: no digit changes.
+__device__ __forceinline__ void settle(TailRec& t) {
+  if (!(t.sum >= 2.f && t.sum < INFINITY)) return;        // 0: none; NaN: flagged later
+  const int k = (int)(__float_as_uint(t.sum) >> 23) - 127;
+  const float by = __uint_as_float((unsigned)(127 - k) << 23);
+  t.f.r += (float)k;
+  t.sum *= by;
+  t.s *= by;
+  t.p *= by;
+}
+
 // `n` records (at most 64) merged by a warp (all lanes converged), the result in
 // every lane, in a fixed order.
 __device__ __forceinline__ void merge_records(const WarpRec* recs, int n, float c, TailRec& t, ListRec& l) {
@@ -88,6 +102,7 @@ __device__ __forceinline__ void merge_records(const WarpRec* recs, int n, float 
     t.p += __shfl_xor_sync(0xFFFFFFFFu, t.p, d);
     l.rest += __shfl_xor_sync(0xFFFFFFFFu, l.rest, d);
   }
+  settle(t);
 }
 
 // One lane's sums over the columns that are not listed, under its warp's reference:
