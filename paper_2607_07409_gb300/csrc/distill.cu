@@ -617,19 +617,20 @@ __global__ void __launch_bounds__(kStreamThreads, (GRAD ? 2 : 3) - kFewer<T, F>)
   // (before the gradient is written: the arrival waits for every store before it)
   if (C > 1) cluster_arrive();
   if constexpr (GRAD) {
-    // this warp's 2^z are relative to its own reference
-    const float unit = rec.t.m > -INFINITY ? ex2_approx(ref_shift(rec.t.f, sums.f, c)) : 0.f;
-    const float k2 = ok ? up * sums.factor * unit : NAN;
-    const f32x2 kk = both2(k2);
+    // this warp's 2^z are relative to its own reference, perhaps far below the row's: brought to
+    // the row's first, where at most 1 is left of them, then multiplied (their factors' product alone
+    // may leave the range)
+    const float d = rec.t.m > -INFINITY ? ref_shift(rec.t.f, sums.f, c) : 0.f, d1 = fmaxf(d, -100.f);
+    const f32x2 unit = both2(ex2_approx(d1)), kk = both2(ok ? up * sums.factor * ex2_approx(d - d1) : NAN);
     const float4* got = reinterpret_cast<const float4*>(kept) + tid;
 #pragma unroll 2
     for (int it = 0; it < stream.items; ++it) {
       const float4 y = got[it * 2 * kStreamThreads], w = got[(it * 2 + 1) * kStreamThreads];
       float gr[8];
-      split2(mul2(kk, pair2(y.x, y.y)), gr[0], gr[1]);
-      split2(mul2(kk, pair2(y.z, y.w)), gr[2], gr[3]);
-      split2(mul2(kk, pair2(w.x, w.y)), gr[4], gr[5]);
-      split2(mul2(kk, pair2(w.z, w.w)), gr[6], gr[7]);
+      split2(mul2(kk, mul2(unit, pair2(y.x, y.y))), gr[0], gr[1]);
+      split2(mul2(kk, mul2(unit, pair2(y.z, y.w))), gr[2], gr[3]);
+      split2(mul2(kk, mul2(unit, pair2(w.x, w.y))), gr[4], gr[5]);
+      split2(mul2(kk, mul2(unit, pair2(w.z, w.w))), gr[6], gr[7]);
       grad_item<T, VEC>(out, item_pos<T, VEC>(k0, it, tid), row.sh, k1, a.grad_vec, gr);
     }
   }

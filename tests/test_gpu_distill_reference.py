@@ -39,3 +39,16 @@ def test_tail_next_to_listed_ids_far_above_the_first_columns(low, T, fused, via,
                           [0.1 * T, 0.0, -0.2 * T])
     for tail in (True, False):
         check_distill(c, 3, tail, T, ids_t=(ids, t), via=via)
+
+
+@DTYPES
+@VIA
+@pytest.mark.parametrize("fused", [False, True], ids=["plain", "fused"])
+def test_entries_that_are_not_listed_beside_listed_ones_past_the_range(fused, via, dtype):
+    """Listed entries 2^120 to 2^140 times as likely as the first columns, others 2^20 to 2^40 times less than they:
+    their gradients, of 1e-12 to 1e-6, hold to their own digits."""
+    c, ids, t = low_first(5, dtype, fused, 302, -84.0, [-14.0, -18.0, -20.0, -25.0, -28.0], [4.0, 1.0, 0.0])
+    for r, up in enumerate((0.0, 3.0, 4.0, 6.0, 9.0)):
+        c.long[r, ids[r].long()] += up
+    check_distill(c, 3, False, ids_t=(ids, t), via=via)
+    check_distill(c, 3, True, ids_t=(ids, t), via=via)
