@@ -11,6 +11,7 @@ built, every call raises ``RuntimeError``.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Dict, Optional
 
@@ -426,9 +427,12 @@ def dels_score_workspace_bytes(rows: int, V: int) -> int:
 
 def dels_score_rows(x: Rows, rows: int, V: int, tokens, top_k: int, out_logprob, out_entropy, out_top_ids,
                     out_top_logprob, workspace, workspace_bytes: int, stream=None) -> int:
-    return lib().dels_score_rows(ctypes.byref(x), rows, V, _ptr(tokens), top_k, _ptr(out_logprob), _ptr(out_entropy),
-                                 _ptr(out_top_ids), _ptr(out_top_logprob), _ptr(workspace), workspace_bytes,
-                                 _stream(stream))
+    r = lib().dels_score_rows(ctypes.byref(x), rows, V, _ptr(tokens), top_k, _ptr(out_logprob), _ptr(out_entropy),
+                              _ptr(out_top_ids), _ptr(out_top_logprob), _ptr(workspace), workspace_bytes,
+                              _stream(stream))
+    if r == DELS_OK:
+        _written(out_logprob, out_entropy, out_top_ids, out_top_logprob)
+    return r
 
 
 def dels_distill_state_bytes(rows: int) -> int:
@@ -441,23 +445,32 @@ def dels_distill_workspace_bytes(rows: int, V: int) -> int:
 
 def dels_distill_loss(x: Rows, rows: int, V: int, teacher: Teacher, out_loss, state, state_bytes: int, workspace,
                       workspace_bytes: int, stream=None) -> int:
-    return lib().dels_distill_loss(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(out_loss), _ptr(state),
-                                   state_bytes, _ptr(workspace), workspace_bytes, _stream(stream))
+    r = lib().dels_distill_loss(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(out_loss), _ptr(state),
+                                state_bytes, _ptr(workspace), workspace_bytes, _stream(stream))
+    if r == DELS_OK:
+        _written(out_loss, state)
+    return r
 
 
 def dels_distill_grad(x: Rows, rows: int, V: int, teacher: Teacher, grad_loss, state, state_bytes: int, grad_short,
                       grad_stride: int, grad_alpha, grad_beta, stream=None) -> int:
     """``grad_short``: a tensor whose rows may be strided, or an address (``grad_stride`` elements a row)."""
-    return lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(grad_loss), _ptr(state),
-                                   state_bytes, _row_ptr(grad_short), grad_stride, _ptr(grad_alpha), _ptr(grad_beta),
-                                   _stream(stream))
+    r = lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(grad_loss), _ptr(state),
+                                state_bytes, _row_ptr(grad_short), grad_stride, _ptr(grad_alpha), _ptr(grad_beta),
+                                _stream(stream))
+    if r == DELS_OK:
+        _written(grad_short, grad_alpha, grad_beta)
+    return r
 
 
 def dels_distill_step(x: Rows, rows: int, V: int, teacher: Teacher, out_loss, grad_short, grad_stride: int,
                       grad_alpha, grad_beta, workspace, workspace_bytes: int, stream=None) -> int:
-    return lib().dels_distill_step(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(out_loss),
-                                   _row_ptr(grad_short), grad_stride, _ptr(grad_alpha), _ptr(grad_beta),
-                                   _ptr(workspace), workspace_bytes, _stream(stream))
+    r = lib().dels_distill_step(ctypes.byref(x), rows, V, ctypes.byref(teacher), _ptr(out_loss),
+                                _row_ptr(grad_short), grad_stride, _ptr(grad_alpha), _ptr(grad_beta),
+                                _ptr(workspace), workspace_bytes, _stream(stream))
+    if r == DELS_OK:
+        _written(out_loss, grad_short, grad_alpha, grad_beta)
+    return r
 
 
 def dels_profile_enable(on: bool) -> None:
@@ -596,6 +609,26 @@ def _logits(t, shape, dtype, device: int, what) -> int:
     return t.data_ptr()
 
 
+_increment_version = torch._C._increment_version      # of an iterable of tensors
+
+
+def _written(*tensors) -> None:
+    """Tells the autograd engine that the library has written these (None, or an address: not known to it): a graph
+    that still needs what they held then refuses its backward pass instead of taking what they hold now."""
+    _increment_version([t for t in tensors if isinstance(t, torch.Tensor)])
+
+
+def _outputs(device, *shapes):
+    """Float32 outputs of these shapes in one buffer, and the buffer: its version, which is theirs too, is moved by
+    every call that writes them."""
+    sizes = [math.prod(shape) for shape in shapes]
+    starts = [0]
+    for n in sizes:
+        starts.append(starts[-1] + (n + 63) // 64 * 64)
+    buf = torch.empty(starts[-1], dtype=torch.float32, device=device)
+    return [buf[i:i + n].view(shape) for i, n, shape in zip(starts, sizes, shapes)], buf
+
+
 def rows_of(rows: int, V: int, long=None, short=None, log_prior=None, alpha=None, beta=None,
             temperature: float = 1.0) -> Rows:
     """``dels_rows`` of [rows, V] logit tensors (one dtype, rows may be strided), a
@@ -660,10 +693,14 @@ class TokenScorer:
         if self.ws_bytes == 0:
             raise DelsError(DELS_ERR_BAD_SHAPE, "dels_score_workspace_bytes")
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
-        self.logprob = torch.empty(rows, dtype=torch.float32, device=self.device)
-        self.entropy = torch.empty(rows, dtype=torch.float32, device=self.device)
-        self.top_ids = torch.empty(rows, top_k, dtype=torch.int32, device=self.device) if top_k else None
-        self.top_logprob = torch.empty(rows, top_k, dtype=torch.float32, device=self.device) if top_k else None
+        self.top_ids = self.top_logprob = None
+        if top_k > 0:
+            out, buf = _outputs(self.device, (rows,), (rows,), (rows, top_k), (rows, top_k))
+            self.top_ids, self.top_logprob = out[2].view(torch.int32), out[3]
+        else:
+            out, buf = _outputs(self.device, (rows,), (rows,))
+        self.logprob, self.entropy = out[:2]
+        self._writes = (buf,)
         self._call = lib().dels_score_rows
         self._own = [_ptr(t) for t in (self.logprob, self.entropy, self.top_ids, self.top_logprob, self.workspace)]
 
@@ -679,6 +716,7 @@ class TokenScorer:
                        self.ws_bytes, _stream(stream))
         if r != DELS_OK:
             raise DelsError(r, "dels_score_rows")
+        _increment_version(self._writes)
         return self.logprob if tokens is not None else None, self.entropy, self.top_ids, self.top_logprob
 
     def status(self, stream=None) -> int:
@@ -701,9 +739,8 @@ class Distiller:
         if self.ws_bytes == 0:
             raise DelsError(DELS_ERR_BAD_SHAPE, "dels_distill_workspace_bytes")
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
-        self._loss = torch.empty(rows, dtype=torch.float32, device=self.device)
+        (self._loss, *self._grad_w), self._buf = _outputs(self.device, (rows,), (n_weights,), (n_weights,))
         self._grad = self._state = None
-        self._grad_w = torch.empty(2, n_weights, dtype=torch.float32, device=self.device).unbind()
         self._own = [_ptr(t) for t in (self._loss, *self._grad_w, self.workspace)]
         self._call = lib().dels_distill_step
 
@@ -729,6 +766,7 @@ class Distiller:
                                     _stream(stream))
         if r != DELS_OK:
             raise DelsError(r, "dels_distill_loss")
+        _increment_version((self._buf,))
         return self._loss
 
     def step(self, short, ids, logprob, *, long=None, log_prior=None, alpha=None, beta=None, row_weight=None,
@@ -749,6 +787,7 @@ class Distiller:
                        ga if has_a else None, gb if has_b else None, ws, self.ws_bytes, _stream(stream))
         if r != DELS_OK:
             raise DelsError(r, "dels_distill_step")
+        _increment_version((self._buf, out))
         return self._loss, out, self._grad_w[0] if has_a else None, self._grad_w[1] if has_b else None
 
     def status(self, stream=None) -> int:

@@ -75,3 +75,91 @@ def test_gradients_of_rows_that_come_back_with_another_pitch():
         later = grads()
     for a, b in zip(plain, later()):
         assert torch.allclose(a, b, rtol=1e-5, atol=1e-7)      # (other alignments: the same sums in another order)
+
+
+def two_batches(rows=6, V=3001):
+    g = torch.Generator(DEV).manual_seed(204)
+    return [torch.randn(rows, V, generator=g, device=DEV) * 3 for _ in range(2)]
+
+
+def test_a_table_that_was_scored_over_is_refused():
+    """The scorer's own table of one batch in a loss, and the next batch scored before the first one's backward."""
+    first, second = two_batches()
+    rows, V = first.shape
+    sc = dels.TokenScorer(rows, V, 8, device=DEV)
+    short = torch.randn(rows, V, device=DEV).requires_grad_()
+    _, _, ids, lp = sc(first)
+    loss = dels.distill_loss(short, ids, lp, tail=True)
+    want = torch.autograd.grad(dels.distill_loss(short, ids.clone(), lp.clone(), tail=True).sum(), short)[0]
+    assert torch.equal(torch.autograd.grad(loss.sum(), short, retain_graph=True)[0], want)
+    kept = dels.distill_loss(short, ids.clone(), lp.clone(), tail=True)
+    sc(second)
+    with pytest.raises(RuntimeError):
+        loss.sum().backward()
+    assert torch.equal(torch.autograd.grad(kept.sum(), short)[0], want)      # a copy of the table outlasts it
+
+
+def test_logits_that_a_step_wrote_over_are_refused():
+    first, second = two_batches()
+    rows, V = first.shape
+    ids = torch.arange(rows * 4, dtype=torch.int32, device=DEV).view(rows, 4)
+    lp = torch.full((rows, 4), -2.0, device=DEV)
+    short = first.clone().requires_grad_()
+    loss = dels.distill_loss(short, ids, lp)
+    d = dels.Distiller(rows, V, 4, torch.float32, device=DEV)
+    d.step(short, ids, lp)
+    loss.sum().backward(retain_graph=True)                                   # another place: nothing has changed
+    d.step(short, ids, lp, out=short)
+    with pytest.raises(RuntimeError):
+        loss.sum().backward()
+
+
+def test_what_the_library_writes_is_marked_as_written():
+    first, _ = two_batches()
+    rows, V = first.shape
+    ids = torch.arange(rows * 4, dtype=torch.int32, device=DEV).view(rows, 4)
+    lp = torch.full((rows, 4), -2.0, device=DEV)
+    w, prior = torch.ones(2, device=DEV), torch.zeros(V, device=DEV)
+    tok = torch.zeros(rows, dtype=torch.int32, device=DEV)
+
+    def moved(call, *written):
+        before = [t._version for t in written]
+        call()
+        return all(t._version > b for t, b in zip(written, before))
+
+    sc = dels.TokenScorer(rows, V, 4, device=DEV)
+    assert moved(lambda: sc(first, tok), sc.logprob, sc.entropy, sc.top_ids, sc.top_logprob)
+    d = dels.Distiller(rows, V, 4, torch.float32, n_weights=2, device=DEV)
+    loss = d.loss(first, ids, lp)
+    assert moved(lambda: d.loss(first, ids, lp), loss)
+    kw = dict(long=first, log_prior=prior, alpha=w, beta=w)
+    out = d.step(first, ids, lp, **kw)
+    assert moved(lambda: d.step(first, ids, lp, **kw), *out)
+    read = [first, ids, lp, w, prior]
+    before = [t._version for t in read]
+    d.step(first, ids, lp, **kw)
+    assert [t._version for t in read] == before
+    # the calls by their C names, tensors or addresses
+    x, t = dels.rows_of(rows, V, first, first, prior, w, w), dels.teacher_of(rows, ids, lp)
+    ws = torch.zeros(dels.dels_distill_workspace_bytes(rows, V), dtype=torch.uint8, device=DEV)
+    state = torch.zeros(dels.dels_distill_state_bytes(rows), dtype=torch.uint8, device=DEV)
+    los, g, ga, gb = torch.empty(rows, device=DEV), torch.empty_like(first), torch.empty_like(w), torch.empty_like(w)
+    assert moved(lambda: dels.dels_distill_loss(x, rows, V, t, los, state, state.numel(), ws, ws.numel()), los, state)
+    assert moved(lambda: dels.dels_distill_grad(x, rows, V, t, None, state, state.numel(), g, V, ga, gb), g, ga, gb)
+    assert moved(lambda: dels.dels_distill_step(x, rows, V, t, los, g, V, ga, gb, ws, ws.numel()), los, g, ga, gb)
+    ent, top, tlp = torch.empty(rows, device=DEV), torch.empty_like(ids), torch.empty_like(lp)
+    assert moved(lambda: dels.dels_score_rows(x, rows, V, tok, 4, los, ent, top, tlp, ws, 256), los, ent, top, tlp)
+    assert not moved(lambda: dels.dels_score_rows(x, rows, V, tok, 999, los, ent, top, tlp, ws, 256), los)   # refused
+    assert dels.dels_score_rows(x, rows, V, tok, 4, los.data_ptr(), ent, top, tlp, ws, 256) == 0
+
+
+def test_handles_under_inference_mode():
+    first, _ = two_batches()
+    rows, V = first.shape
+    want = [t.clone() for t in dels.TokenScorer(rows, V, 4, device=DEV)(first)[1:]]
+    with torch.inference_mode():
+        sc = dels.TokenScorer(rows, V, 4, device=DEV)
+        for a, b in zip(sc(first)[1:], want):
+            assert torch.equal(a, b)
+    for a, b in zip(sc(first)[1:], want):
+        assert torch.equal(a, b)
