@@ -805,17 +805,17 @@ def _distill_structs(short, alpha, beta, long, log_prior, ids, logprob, row_weig
             teacher_of(rows, ids, logprob, row_weight, tail))
 
 
-def _address(t) -> Optional[int]:
-    return None if t is None else t.data_ptr() or None      # (ctypes gives an address of 0 back as None)
+def _lies_at(x: Rows, t: Teacher, short, alpha, beta, long, log_prior, ids, logprob, row_weight) -> bool:
+    """Whether the structures' addresses are those of these tensors."""
+    return (short.data_ptr() == x.short_logits and ids.data_ptr() == t.ids and logprob.data_ptr() == t.logprob
+            and (long is None or long.data_ptr() == x.long_logits)
+            and (log_prior is None or log_prior.data_ptr() == x.log_prior)
+            and (alpha is None or alpha.data_ptr() == x.alpha) and (beta is None or beta.data_ptr() == x.beta)
+            and (row_weight is None or row_weight.data_ptr() == t.row_weight))
 
 
-def _holds(x: Rows, t: Teacher, shape, short, alpha, beta, long, log_prior, ids, logprob, row_weight) -> bool:
-    """Whether the structures are those of these tensors: their addresses, the rows' type, shape and pitches."""
-    return (short.shape == shape and x.dtype == dtype_code(short.dtype)
-            and x.short_logits == _address(short) and x.short_stride == _row_stride(short, shape, "short")
-            and x.long_logits == _address(long) and (long is None or x.long_stride == _row_stride(long, shape, "long"))
-            and x.log_prior == _address(log_prior) and x.alpha == _address(alpha) and x.beta == _address(beta)
-            and t.ids == _address(ids) and t.logprob == _address(logprob) and t.row_weight == _address(row_weight))
+def _layout(short, long):
+    return short.dtype, short.shape, short.stride(), None if long is None else long.stride()
 
 
 class _DistillLoss(torch.autograd.Function):
@@ -826,36 +826,38 @@ class _DistillLoss(torch.autograd.Function):
         dev = short.device
         loss = torch.empty(rows, dtype=torch.float32, device=dev)
         # the state, and a workspace whose status word is not read (flagged rows are NaN)
-        nbytes = dels_distill_state_bytes(rows)
+        call = lib()
+        nbytes = call.dels_distill_state_bytes(rows)
         state = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
-        r = lib().dels_distill_loss(ctypes.byref(x), rows, V, ctypes.byref(t), loss.data_ptr(), state.data_ptr(),
-                                    nbytes, state.data_ptr() + nbytes, 256, _stream(None))
+        at = state.data_ptr()
+        r = call.dels_distill_loss(ctypes.byref(x), rows, V, ctypes.byref(t), loss.data_ptr(), at, nbytes, at + nbytes,
+                                   256, _stream(None))
         if r != DELS_OK:
             raise DelsError(r, "dels_distill_loss")
         # the tensors, not their addresses: backward() sees whether they were changed since, and takes what
         # saved-tensor hooks give back in their place (checkpointing: rows made again, the first ones freed)
         ctx.save_for_backward(short, alpha, beta, long, log_prior, ids, logprob, row_weight, state)
-        ctx.call = x, t, (rows, V), tail, temperature
+        ctx.call = x, t, at, nbytes, _layout(short, long), tail, temperature
         return loss
 
     @staticmethod
     def backward(ctx, grad_loss):
         if torch.is_grad_enabled():
             raise RuntimeError("distill_loss is differentiable once")
-        *tensors, state = ctx.saved_tensors
-        x, t, (rows, V), tail, temperature = ctx.call
-        if not _holds(x, t, (rows, V), *tensors):
-            x, t = _distill_structs(*tensors, tail, temperature)
-        short, alpha, beta, _, log_prior = tensors[:5]
-        nbytes = state.numel() - 256
-        at_state = _of(state, torch.uint8, state.shape, short.get_device(), "the saved state")
+        short, alpha, beta, long, log_prior, ids, logprob, row_weight, state = ctx.saved_tensors
+        x, t, at, nbytes, layout, tail, temperature = ctx.call
+        if not (state.data_ptr() == at and _layout(short, long) == layout
+                and _lies_at(x, t, short, alpha, beta, long, log_prior, ids, logprob, row_weight)):
+            x, t = _distill_structs(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature)
+            at = _of(state, torch.uint8, (nbytes + 256,), short.get_device(), "the saved state")
+        rows, V = short.shape
         grad = torch.empty(rows, V, dtype=short.dtype, device=short.device)
         ga = torch.empty_like(alpha) if alpha is not None and ctx.needs_input_grad[1] else None
         gb = torch.empty_like(beta) if beta is not None and log_prior is not None and ctx.needs_input_grad[2] else None
         if grad_loss.dtype is not torch.float32 or not grad_loss.is_contiguous():
             grad_loss = grad_loss.to(torch.float32).contiguous()
-        r = lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(t), grad_loss.data_ptr(), at_state,
-                                    nbytes, grad.data_ptr(), V, None if ga is None else ga.data_ptr(),
+        r = lib().dels_distill_grad(ctypes.byref(x), rows, V, ctypes.byref(t), grad_loss.data_ptr(), at, nbytes,
+                                    grad.data_ptr(), V, None if ga is None else ga.data_ptr(),
                                     None if gb is None else gb.data_ptr(), _stream(None))
         if r != DELS_OK:
             raise DelsError(r, "dels_distill_grad")
