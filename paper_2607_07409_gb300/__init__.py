@@ -868,5 +868,10 @@ def distill_loss(short, ids, logprob, *, long=None, log_prior=None, alpha=None, 
                  tail: bool = False, temperature: float = 1.0) -> torch.Tensor:
     """Distillation losses [rows] of a local head's logits, differentiable (once) in
     ``short``, ``alpha`` and ``beta``, on the current stream. Rows flagged as
-    non-finite have a loss of NaN."""
+    non-finite have a loss of NaN. The other tensors have no gradient here: where the engine
+    records, none of them may require one (``detach()`` them)."""
+    if torch.is_grad_enabled():
+        for name, t in (("logprob", logprob), ("long", long), ("log_prior", log_prior), ("row_weight", row_weight)):
+            if t is not None and t.requires_grad:
+                raise ValueError(f"distill_loss has no gradient of {name}: detach it")
     return _DistillLoss.apply(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature)

@@ -125,3 +125,17 @@ def test_backward_under_checkpoint_takes_the_rows_made_again(stub):
     assert [kind for kind, *_ in stub.seen] == ["loss", "loss", "grad"] and len(made) == 2
     assert stub.seen[0][1].short_logits == made[0].data_ptr()
     assert stub.seen[2][1].short_logits == made[1].data_ptr() != made[0].data_ptr()
+
+
+@pytest.mark.parametrize("name", ["long", "log_prior", "logprob", "row_weight"])
+def test_tensors_without_a_gradient_may_not_require_one(stub, name):
+    v = inputs()
+    v["short"].requires_grad_()
+    v[name].requires_grad_()
+    with pytest.raises(ValueError, match=name):
+        loss_of(v)
+    assert not stub.seen
+    with torch.no_grad():                                     # nothing is recorded: nothing is lost
+        loss_of(v)
+    loss_of(dict(v, **{name: v[name].detach()})).sum().backward()
+    assert [kind for kind, *_ in stub.seen] == ["loss", "loss", "grad"] and v["short"].grad is not None
