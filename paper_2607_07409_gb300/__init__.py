@@ -680,6 +680,17 @@ def _device_index(device) -> int:
     return torch.cuda.current_device() if device.index is None else device.index
 
 
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _need_current(device: int) -> None:
+    """The library launches on the current device: tensors of another one are refused before it sees them."""
+    if _current_device() != device:
+        raise ValueError(f"the tensors are on cuda:{device}, and the current device is cuda:{_current_device()}: "
+                         f"call under torch.cuda.device({device})")
+
+
 class TokenScorer:
     """Log-probabilities of given tokens, entropies and the ``top_k`` most likely
     entries of [rows, V] logits, plain or fused: outputs and a workspace for
@@ -707,6 +718,7 @@ class TokenScorer:
     def __call__(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, short=None, log_prior=None,
                  alpha=None, beta=None, temperature: float = 1.0, stream=None):
         """(log-probabilities or None without tokens, entropies, top ids, top log-probabilities)."""
+        _need_current(self._dev)
         x = rows_of(self.rows, self.V, logits, short, log_prior, alpha, beta, temperature)
         if logits.get_device() != self._dev:
             raise ValueError(f"logits must be on {self.device}")
@@ -745,6 +757,7 @@ class Distiller:
         self._call = lib().dels_distill_step
 
     def _args(self, short, ids, logprob, long, log_prior, alpha, beta, row_weight):
+        _need_current(self._dev)
         if short.dtype is not self.dtype or short.get_device() != self._dev or ids.get_device() != self._dev:
             raise ValueError(f"short must be {self.dtype} and all tensors on {self.device}")
         x = rows_of(self.rows, self.V, long, short, log_prior, alpha, beta, self.temperature)
@@ -801,6 +814,7 @@ def _distill_structs(short, alpha, beta, long, log_prior, ids, logprob, row_weig
     rows, V = short.shape
     if ids.get_device() != short.get_device():
         raise ValueError(f"ids must be on {short.device}")
+    _need_current(short.get_device())
     return (rows_of(rows, V, long, short, log_prior, alpha, beta, temperature),
             teacher_of(rows, ids, logprob, row_weight, tail))
 

@@ -58,6 +58,7 @@ def stub(monkeypatch):
     monkeypatch.setattr(dels, "rows_of", host_rows)
     monkeypatch.setattr(dels, "teacher_of", host_teacher)
     monkeypatch.setattr(dels, "_stream", lambda stream: None)
+    monkeypatch.setattr(dels, "_current_device", lambda: -1, raising=False)    # a host tensor's get_device()
     return s
 
 
@@ -139,3 +140,29 @@ def test_tensors_without_a_gradient_may_not_require_one(stub, name):
         loss_of(v)
     loss_of(dict(v, **{name: v[name].detach()})).sum().backward()
     assert [kind for kind, *_ in stub.seen] == ["loss", "loss", "grad"] and v["short"].grad is not None
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(stub, monkeypatch):
+    """The library launches on the current device, on its stream."""
+    v = inputs()
+    loss_of(dict(v, short=v["short"].requires_grad_()))
+    calls = len(stub.seen)
+    sc = dels.TokenScorer.__new__(dels.TokenScorer)
+    sc.rows, sc.V, sc.top_k, sc._dev = ROWS, V, 0, -1
+    d = dels.Distiller.__new__(dels.Distiller)
+    d.rows, d.V, d.k, d.dtype, d.n_weights, d.tail, d.temperature, d._dev = ROWS, V, K, torch.float32, 2, False, 1.0, -1
+    for o in (sc, d):
+        o._own, o._call = [0] * 5, lambda *a: pytest.fail("the library was called")
+    d._loss, d._grad_w, d._state, d._grad, d.ws_bytes = v["long"], (), v["long"], v["long"], 0
+    monkeypatch.setattr(dels, "_current_device", lambda: 0)
+    for call in (lambda: loss_of(v), lambda: sc(v["long"]), lambda: d.step(v["short"], v["ids"], v["logprob"]),
+                 lambda: d.loss(v["short"], v["ids"], v["logprob"])):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    assert len(stub.seen) == calls
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t.clone(), lambda t: t):
+        monkeypatch.setattr(dels, "_current_device", lambda: -1)
+        loss = loss_of(v)
+    monkeypatch.setattr(dels, "_current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device"):
+        loss.sum().backward()
