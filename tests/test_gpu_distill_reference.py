@@ -3,7 +3,8 @@ are relative to then lie far below them. Bounds as in test_gpu_row_ops."""
 import pytest
 import torch
 
-from test_gpu_row_ops import Case, check_distill, gen
+import paper_2607_07409_gb300 as dels
+from test_gpu_row_ops import DEV, INF, Case, check_distill, eps_sum, gen, reference, teacher
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,48 @@ def test_entries_that_are_not_listed_beside_listed_ones_past_the_range(fused, vi
         c.long[r, ids[r].long()] += up
     check_distill(c, 3, False, ids_t=(ids, t), via=via)
     check_distill(c, 3, True, ids_t=(ids, t), via=via)
+
+
+def weight_grads_of(c, ids, t, via, w):
+    """The weights' gradients by the step or by the engine."""
+    kw = dict(long=c.dev("long"), row_weight=w.to(DEV), **c.kwargs())
+    short, ids, t = c.dev("short"), ids.to(DEV), t.to(DEV)
+    if via == "step":
+        d = dels.Distiller(c.rows, c.V, ids.shape[1], c.dtype, n_weights=c.alpha.numel(), tail=True, device=DEV)
+        return [g.cpu().double() for g in d.step(short, ids, t, **kw)[2:]]
+    leaves = [kw["alpha"].requires_grad_(), kw["beta"].requires_grad_()]
+    loss = dels.distill_loss(short, ids, t, tail=True, **kw)
+    return [g.cpu().double() for g in torch.autograd.grad(loss.sum(), leaves)]
+
+
+def centred_bound(c, ids, t, w, lq, terms, around):
+    """The bound of a sum over the columns of gradient entries times what `terms` have beside `around`, one of them:
+    the entries' own bounds (as in check_distill, the fused value's size being that of its last operations, since a
+    product is not rounded before it is added), and 2^-20 of the sum of the products."""
+    size = (c.long.double() + c.at(c.alpha).double() * c.short.double()).abs().amax(-1) \
+        + (c.at(c.beta).double() * c.prior.double()).abs().amax(-1)
+    e = (2 * 8 * 2.0 ** -24 * size + eps_sum(c.V) + 2.0 ** -23 * float(t[t > -INF].abs().max()) + 2.0 ** -20)[:, None]
+    q, p = lq.exp(), torch.zeros_like(lq)
+    p.scatter_add_(1, ids.long(), t.double().exp())
+    rest = (1 - p.sum(-1, keepdim=True)).clamp(min=0.0)
+    q_t = q.masked_fill(p > 0, 0.0).sum(-1, keepdim=True)
+    per = 2 * e * (q + p) + q * (2.0 ** -21 + 2 * e * rest) / q_t + 2.0 ** -20 * (q + p * (1 + rest / q_t))
+    far = (terms.double() - around).abs()
+    far = far + torch.where(far < 1e3, far, torch.zeros_like(far)).amax(-1, keepdim=True)   # (the reference is one of them)
+    return (w.double()[:, None] * per * far).sum(-1)
+
+
+@VIA
+@pytest.mark.parametrize("V", [3001, 20000])
+def test_the_gradient_of_alpha_where_the_heads_logits_share_an_offset(V, via):
+    """A row's gradient sums to zero: an offset of 2^14 in l_S, which l_L takes away again, changes no gradient. (The
+    sums of products with the logits themselves would be off by some 2^-22 of it.)"""
+    c = Case(6, V, torch.float32, 303, True, n=6)
+    ids, t = teacher(c, 7, 3, True, 1.0, missing=False)
+    c.short = c.short + 16384.0
+    c.long = (c.long.double() - c.at(c.alpha).double() * 16384.0).float()
+    w = torch.rand(6, generator=gen(3)) + 0.5
+    ref = reference(c, ids, t, True, 1.0, w.double(), torch.ones(6).double())
+    got = weight_grads_of(c, ids, t, via, w)
+    bound = centred_bound(c, ids, t, w, ref[4], c.short, 16384.0)
+    assert ((got[0] - ref[2]).abs() <= bound).all(), ((got[0] - ref[2]).abs() / bound).max()
