@@ -449,15 +449,15 @@ __global__ void __launch_bounds__(kStreamThreads, (GRAD ? 2 : 3) - kFewer<T, F>)
   RowStream<Cp, T, F, VEC> stream(a.in, r, rank, ring, kept);
   const FusedRow<T, F, VEC>& row = stream.row;
   const int k0 = stream.k0, k1 = stream.k1;
-  const float p_ref = F ? row.p_at(row.sh + V / 2) : 0.f;
   // (looked at when the copies are under way: before them their latency came on top, 64 bf16 rows 18.9, 18.5 us)
-  float s_some[3] = {0.f, 0.f, 0.f};
+  float s_some[3] = {0.f, 0.f, 0.f}, p_some[3] = {0.f, 0.f, 0.f};
   if (weight != 0.f) {
     if constexpr (F != kPlain) {
 #pragma unroll
       for (int i = 0; i < 3; ++i) {
         const int at = row.sh + (i == 0 ? V / 4 : i == 1 ? V / 2 : V - 1 - V / 4);
         s_some[i] = row.s_at(at);
+        p_some[i] = row.p_at(at);
       }
     }
     stream.begin();
@@ -519,6 +519,7 @@ __global__ void __launch_bounds__(kStreamThreads, (GRAD ? 2 : 3) - kFewer<T, F>)
   if (warp == kStreamWarps - 1) teacher_side(sh, K, a.tail != 0, inv_t);
 
   const float s_ref = middle(s_some[0], s_some[1], s_some[2]);
+  const float p_ref = middle(p_some[0], p_some[1], p_some[2]);
   // the columns that are not listed
   WarpTail<F != kPlain> st;
   st.init();

@@ -98,3 +98,27 @@ def test_the_gradient_of_alpha_where_the_heads_logits_share_an_offset(V, via):
     got = weight_grads_of(c, ids, t, via, w)
     bound = centred_bound(c, ids, t, w, ref[4], c.short, 16384.0)
     assert ((got[0] - ref[2]).abs() <= bound).all(), ((got[0] - ref[2]).abs() / bound).max()
+
+
+@VIA
+@pytest.mark.parametrize("V", [3001, 20000])
+@pytest.mark.parametrize("far", [-1e6, -1e9])
+def test_the_gradient_of_beta_where_the_prior_has_values_far_below(far, V, via):
+    """Some of the prior's values far below the others (columns that l_L masks, the middle one and every 7th): they
+    have no part in a gradient, and take no digits from it."""
+    c = Case(6, V, torch.float32, 304, True, n=6)
+    ids, t = teacher(c, 7, 3, True, 1.0, missing=False)
+    listed = set(ids.flatten().tolist())
+    gone = [v for v in sorted({V // 2, *range(0, V, 7)} - {V // 4, V - 1 - V // 4}) if v not in listed]
+    c.long[:, gone] = -INF
+    c.prior[gone] = 0.0                                       # (the reference's rows: the same columns without weight)
+    w = torch.rand(6, generator=gen(3)) + 0.5
+    ref = reference(c, ids, t, True, 1.0, w.double(), torch.ones(6).double())
+    # (the others' largest sets the bound: columns of no weight take no part in it)
+    c.long[:, gone] = 0.0
+    bound = centred_bound(c, ids, t, w, ref[4], c.prior, float(c.prior[c.prior != 0].median()))
+    c.long[:, gone] = -INF
+    c.prior[gone] = far
+    got = weight_grads_of(c, ids, t, via, w)
+    assert ((got[1] - ref[3]).abs() <= bound).all(), ((got[1] - ref[3]).abs() / bound).max()
+    assert ((got[0] - ref[2]).abs() <= 16 * bound).all()
