@@ -2363,9 +2363,14 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
   const bool f32 = x->dtype == DELS_F32;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_DISTILL);
-  if (rows > 0 && plan_step(&a, f32, call.fused, call.vec))
-    return launch_distill_step(a, f32, call.fused, call.vec, s) == cudaSuccess ? DELS_OK : DELS_ERR_CUDA;
-  if (rows > 0) {
+  if (rows > 0 && plan_step(&a, f32, call.fused, call.vec)) {
+    const bool here = a.in.n_weights <= kTicketWeights;
+    if (!here) a.grad_alpha = a.grad_beta = nullptr;
+    if (launch_distill_step(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
+    if (here) return DELS_OK;
+    a.grad_alpha = grad_alpha;
+    a.grad_beta = grad_beta;
+  } else if (rows > 0) {
     if (launch_distill_loss(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
     if (launch_distill_grad(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
   }

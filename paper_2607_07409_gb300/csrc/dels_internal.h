@@ -185,6 +185,12 @@ struct DistillArgs {
 cudaError_t launch_distill_loss(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 // Loss and gradient at once: a slice's values stay in shared memory.
 constexpr int kStepSmemBytes = 200 * 1024;
+// Weights up to which its last row sums their gradients, one after another; more take a launch of
+// their own, a CTA each. us, by the last row against by a launch: 16 fused bf16 rows of 151936 with
+// 1, 8, 16, 64, 512 weights 12.4, 15.2, 18.4, 28.3, 121 against 12.2 for all; 297 float32 rows of
+// 32003 31.5, 34.9, 38.8, 61, 200 against 30; the launch is 1.4 us more for the host where that is
+// behind (8 float32 rows of 1024 with 8: 12.8 against 14.2).
+constexpr int kTicketWeights = 8;
 bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec, int sms);
 cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);

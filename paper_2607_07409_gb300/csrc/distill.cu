@@ -387,7 +387,7 @@ __device__ void weight_grads(const DistillArgs& a, int j, float2* red) {
 }
 
 // The first CTA of a row's cluster, when the row is done: the last row of the grid
-// sums the weights' gradients (its count starts the next call at zero).
+// sums the gradients of up to kTicketWeights weights (its count starts the next call at zero).
 __device__ __forceinline__ void finish_rows(const DistillArgs& a, LossShared& sh) {
   if (!a.grad_alpha && !a.grad_beta) return;
   __syncthreads();

@@ -163,3 +163,44 @@ def test_handles_under_inference_mode():
             assert torch.equal(a, b)
     for a, b in zip(sc(first)[1:], want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [7, 8, 9, 40])
+def test_weights_gradients_by_the_steps_last_row_or_by_a_launch(n):
+    """Both sides of the step's choice, and the engine's, which is always the launch: the same sums in the same order."""
+    c = Case(12, 3001, torch.float32, 205, True, n=n)
+    ids, t = teacher(c, 9, 3, True, 1.0)
+    short, long, kw = c.dev("short"), c.dev("long"), c.kwargs()
+    ids, t = ids.to(DEV), t.to(DEV)
+    d = dels.Distiller(12, 3001, 9, torch.float32, n_weights=n, tail=True, device=DEV)
+    for _ in range(3):                                        # (the count of the rows starts anew)
+        _, _, ga, gb = d.step(short, ids, t, long=long, **kw)
+        leaves = [kw["alpha"].requires_grad_(), kw["beta"].requires_grad_()]
+        loss = dels.distill_loss(short, ids, t, long=long, tail=True, **kw)
+        want = torch.autograd.grad(loss.sum(), leaves)
+        kw = {k: v.detach() for k, v in kw.items()}
+        assert torch.equal(ga, want[0]) and torch.equal(gb, want[1])
+
+
+def test_a_step_with_many_weights_takes_no_serial_time():
+    """The gradients of 20000 weights, one after another by one CTA, take some 40 ms; with a CTA each, microseconds."""
+    rows, V, n = 16, 4096, 20000
+    long, short = torch.randn(rows, V, device=DEV), torch.randn(rows, V, device=DEV)
+    ids = torch.arange(rows * 4, dtype=torch.int32, device=DEV).view(rows, 4)
+    lp = torch.full((rows, 4), -2.0, device=DEV)
+    prior = torch.zeros(V, device=DEV)
+    d = dels.Distiller(rows, V, 4, torch.float32, n_weights=n, tail=True, device=DEV)
+    w = torch.ones(n, device=DEV)
+    kw = dict(long=long, log_prior=prior, alpha=w, beta=w)
+    for _ in range(3):
+        _, _, ga, gb = d.step(short, ids, lp, **kw)
+    assert (ga[rows:] == 0).all() and (gb[rows:] == 0).all() and (ga[:rows] != 0).any()
+    ms = []
+    for _ in range(5):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        d.step(short, ids, lp, **kw)
+        b.record()
+        torch.cuda.synchronize()
+        ms.append(a.elapsed_time(b))
+    assert min(ms) < 4.0, ms
