@@ -505,8 +505,8 @@ int dels_score_rows(const dels_rows* x, int rows, int V, const int32_t* tokens, 
  *     what they leave of 1, p_t = max(0, 1 - sum_k p_k), is one more entry: the ids
  *     that are not listed, all together. It is left out where the student gives
  *     those ids no probability at all.
- * row_weight scales a row's loss and gradients; a row of weight 0, and one without
- * entries, is left out: loss and gradients 0, its logits not read.
+ * row_weight scales a row's loss and gradients; a row of weight 0 (its logits are not
+ * read), and one without entries, is left out: loss and gradients 0, whatever its logits.
  */
 typedef struct {
   const int32_t* ids;            /* [device] [rows, k] */
@@ -544,6 +544,10 @@ typedef struct {
  *              stride (then overwritten);
  *   grad_alpha, grad_beta [device] [n_weights] float32, overwritten, each may be
  *              NULL; they need alpha, and beta and log_prior.
+ * Masked logits are -inf or the type's lowest value; of short_logits the lowest value is
+ * the faster one (-inf there has the part of the row that meets it read again, see
+ * csrc/distill.cu). grad_alpha and grad_beta are of the terms beside a value that they
+ * have in common: an offset of short_logits or of log_prior takes no digits from them.
  * A row with NaN or +inf logits, or of -inf alone, or with a teacher logprob of NaN
  * or +inf sets DELS_STATUS_NONFINITE; its loss and gradients are NaN. Sums are
  * float32 in a fixed order: equal calls give equal bits.

@@ -17,8 +17,8 @@
 // sums taken along with the softmax's: no pass over the rows is added for them.
 //
 // What bounds it, on fused rows of 151936: 1024 bf16 rows' loss takes 128 us (4.9 TB/s:
-// instructions, see row_stream.cuh), their gradient 162 us (5.8 TB/s: the bytes), both as
-// one step 293 us, 64 rows 32 us; 256 float32 rows 55, 84 and 143 us (5.7 and 5.6 TB/s).
+// instructions, see row_stream.cuh), their gradient 158 us (5.9 TB/s: the bytes), both as
+// one step 287 us, 64 rows 31 to 34 us; 256 float32 rows 55, 81 and 142 us (5.7 and 5.8 TB/s).
 // A row's bytes in one pass would be 3 s V: the step that reads once (GRAD below) is the
 // faster one for few rows only, as distill_step_fits() says.
 #include <algorithm>
@@ -176,6 +176,16 @@ struct WarpTail {
 // Where those are not finite (a later entry far above the first ones, a masked l_S of
 // -inf, an entry that is not a number): the warp's items again, element by element, the
 // largest entry first. `kept`: the step's place of 2^z, or null.
+//
+// This is slow, without copies ahead and twice over. Loss of fused rows of 151936, us:
+//                                               1024 bf16   64 bf16   256 float32
+//   none of it                                     128         17          54
+//   256 padded columns of -inf in l_S (a warp)    1090         63         360
+//   3 % of l_S at -inf (all warps)                2440        184         612
+//   the first 256 columns masked by -1e4           805         72          55
+//   the first 2048 so                             2410        178         610
+//   a temperature of 0.1                           396         67         300
+// (Columns masked by -inf in l_L alone, or by the lowest finite value in l_S, cost nothing.)
 template <typename T, int F, bool VEC>
 __device__ __noinline__ TailRec redo_tail(const FusedRow<T, F, VEC>& row, int k0, int k1, const unsigned* bitmap,
                                           float* kept, float c, float s_ref, float p_ref) {
@@ -209,8 +219,9 @@ __device__ __noinline__ TailRec redo_tail(const FusedRow<T, F, VEC>& row, int k0
   return r;
 }
 
-// Copies ahead of the loss and gradient kernels, and of the step's, whose items stay
-// (beside 10 items of 8 KB its ring is to leave room for a second CTA on the SM).
+// Copies ahead of the loss and gradient kernels, and of the step's, whose items stay: only
+// fused float32 rows have a ring beside them, of 32 KB, which with 8 items (66 KB) leaves
+// room for a second CTA on the SM and with 10 does not.
 template <typename T, int F>
 using LossCopies = std::conditional_t<F == kPlain, Copies<T, F, sizeof(T) == 2 ? 4 : 2, 2>,
                                       Copies<T, F, 2, sizeof(T) == 2 ? 3 : 2>>;
@@ -825,12 +836,14 @@ cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool
 // Whether the step reads its rows once (k_distill_loss with GRAD, a launch less) or
 // twice (k_distill_loss, then k_distill_grad). Once needs room for the slice's 2^z
 // beside the ring, and with it few CTAs share an SM: 1 to 3, which hide less of a CTA's
-// start and exchange than the 3 to 6 of the two launches. us, once against twice:
-//   one round of CTAs     24 bf16 rows of 151936: 19.5, 23.0 fused; 9.0, 18.0 plain
-//   more, fused bf16      40: 28.3, 25.8; 160: 68.1, 62.6; 1024: 321, 320
-//   up to two, plain bf16 76: 22.6, 24.3; more: 160: 39.6, 36.9; 600: 135, 108
-//   float32, two on an SM 160 of 100003: 74.5, 85.0 fused; 600: 117, 141 plain
-//   float32, one on an SM 256 of 151936 fused: 188, 144
+// start and exchange than the 3 to 6 of the two launches. us, once against twice, the
+// gradients of 16 weights among them:
+//   one round of CTAs     24 bf16 rows of 151936: 12.6, 19.5 fused; 8.8, 14.8 plain
+//   more, fused bf16      40: 22.7, 23.1; 160: 59.8, 58.7; 1024: 327, 279
+//   up to two, plain bf16 57: 15.5, 22.5; 100 of 100003: 18.5, 27.9 (but 76 of 151936, 24.4,
+//                         19.8); more: 160: 37.3, 34.0; 600: 129, 98
+//   float32, two on an SM 160 of 100003: 64, 80 fused; 600: 115, 139 plain
+//   float32, one on an SM 256 of 151936 fused: 174, 141
 bool distill_step_fits(const DistillArgs& a, bool f32, bool fused, bool vec, int sms) {
   size_t bytes = 0;
   int per_sm = 0;

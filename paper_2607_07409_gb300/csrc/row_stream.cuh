@@ -4,9 +4,9 @@
 // shared memory, so that a pass over the rows needs no scratch in memory and no second
 // launch to join them.
 //
-// What bounds the stream: of float32 rows the bytes (5.6 TB/s of a copy's 6.8); of bf16
-// rows the instructions of a column beside the latency that 24 warps an SM hide: 18.7
-// of the fused loss, 8.5 of plain scoring, 20.8 of fused scoring, at 55 to 65 % of the
+// What bounds the stream: of float32 rows the bytes (5.7 TB/s of a copy's 6.8); of bf16
+// rows the instructions of a column beside the latency that 24 warps an SM hide: 19.2
+// of the fused loss, 8.5 of plain scoring, 20.8 of fused scoring, at 58 to 67 % of the
 // issue slots. Hence packed pairs, whole items without tests, one reference for a warp,
 // and copies that pass through shared memory without a register or a barrier.
 #pragma once
@@ -102,7 +102,8 @@ struct Raw8 {
 enum { kPlain = 0, kSome = 1, kFull = 2 };
 // Kernels of float32 rows with some of the terms, which test for each where it is used:
 // one CTA less on an SM than the others, for the registers that this takes (with as
-// many, spills in the stream: 304 rows of 151936, l_L and l_S, loss 148, 105 us).
+// many 1740 bytes of spills, now 320 and in the loss alone: 304 rows of 151936, l_L and
+// l_S, loss 148, 92 us).
 template <typename T, int F>
 constexpr int kFewer = F == kSome && sizeof(T) == 4 ? 1 : 0;
 
