@@ -73,7 +73,8 @@ enum {
   /* detected on the device; bits of the workspace status word */
   DELS_STATUS_NONFINITE = 1,       /* NaN or +inf logit, or a row that is all -inf */
   DELS_STATUS_TIMEOUT = 2,         /* a bounded device-side wait expired */
-  DELS_STATUS_BAD_TOKEN = 4        /* a draft or loss-masked corpus token outside [0, V) */
+  DELS_STATUS_BAD_TOKEN = 4,       /* a draft or loss-masked corpus token outside [0, V) */
+  DELS_STATUS_BAD_VALUE = 8        /* a given uniform, length, code or zero point outside its range */
 };
 
 typedef enum { DELS_F32 = 0, DELS_BF16 = 1 } dels_dtype;
@@ -568,6 +569,99 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
                       void* grad_short, long long grad_stride, float* grad_alpha, float* grad_beta, void* workspace,
                       size_t workspace_bytes, dels_stream_t stream);
 
+/* ---- probabilities of rows, and verification from given numbers ----------- */
+
+/*
+ * out[r, v] = softmax(z)_v for the rows that dels_score_rows reads (plain or fused,
+ * z = l / temperature; two fused multiply-adds a value): a drafter's or a target's
+ * distributions as dels_verify_given reads them. Entries of -inf have probability 0.
+ * A row with NaN or +inf, or of -inf alone, sets DELS_STATUS_NONFINITE and gives NaN.
+ * out [device] [rows, V] of out_dtype, out_stride elements from one row to the next
+ * (0: V); it may be none of the inputs. Sums are float32 in a fixed order: equal
+ * calls give equal bits. Limits: 0 <= rows <= 2^27, 1 <= V <= 2^30; pointers aligned
+ * to their elements (rows that start on 16 bytes are fastest).
+ */
+size_t dels_row_probs_workspace_bytes(int rows, int V);
+int dels_row_probs(const dels_rows* x, int rows, int V, void* out, dels_dtype out_dtype, long long out_stride,
+                   void* workspace, size_t workspace_bytes, dels_stream_t stream);
+
+/* Probabilities [B, rows, V]: element (b, j, v) at b * batch_stride + j * row_stride + v. */
+typedef struct {
+  const void* data;              /* [device] */
+  dels_dtype dtype;
+  long long batch_stride;        /* elements; 0: rows * row_stride */
+  long long row_stride;          /* elements, >= V; 0: V */
+} dels_probs;
+
+/*
+ * Speculative sampling of drafted blocks with the caller's own random numbers
+ * (dels_verify_block_sampled draws its numbers itself and rebuilds the draft's rows).
+ * Of request b, the drafted token x_j, j < lengths[b], is kept while
+ *   u[b, j] q_j(x_j) < p_j(x_j);
+ * a = the number kept. The bonus token is drawn from w = max(0, p_a - q_a) at a
+ * rejection (from p_a where that is 0 everywhere), from w = p_a where a = lengths[b]:
+ * the lowest v with w_0 + .. + w_v > u[b, n] (w_0 + .. + w_{V-1}).
+ *   tokens   [device] [B, n] int32; lengths [device] [B] int32 of 0 .. n, or NULL: n;
+ *   target   p: n + 1 rows a request, of which the first lengths[b] + 1 are read;
+ *   draft    q: n rows a request, or NULL: probability 1 for every drafted token (a
+ *            greedy drafter's);
+ *   uniforms [device] [B, n + 1] float32 of [0, 1);
+ *   out_accept_len, out_bonus [device] [B] int32.
+ * n = 0 draws a token of each row (tokens and draft are not read). Comparisons are
+ * exact; sums are as good as float64's. Probabilities need no sum of 1. A drafted
+ * token outside [0, V), a uniform outside [0, 1) or a length outside 0 .. n sets
+ * DELS_STATUS_BAD_TOKEN or DELS_STATUS_BAD_VALUE; a probability that is negative, NaN
+ * or infinite where it is read, or a row of p whose sum is 0
+ * or above float32's range, DELS_STATUS_NONFINITE: the
+ * request's bonus is then -1, its length the tokens kept before that was met. What
+ * lies behind the token that decides is not looked at.
+ * Limits: 0 <= B <= 2^20, 0 <= n <= 1024, 1 <= V <= 2^30; pointers aligned to their
+ * elements (rows that start on 16 bytes are fastest).
+ */
+size_t dels_verify_given_workspace_bytes(int B, int n, int V);
+int dels_verify_given(const int32_t* tokens, const dels_probs* target, const dels_probs* draft, const float* uniforms,
+                      const int32_t* lengths, int B, int n, int V, int32_t* out_accept_len, int32_t* out_bonus,
+                      void* workspace, size_t workspace_bytes, dels_stream_t stream);
+
+/* ---- products with 4-bit weights ------------------------------------------ */
+
+/*
+ * A matrix [V, K] of 4-bit codes with a scale for each group of `group` inputs of a
+ * row (and a zero point, or 8):  w[v, k] = scale[v, k / group] (code[v, k] - zero[v, k / group]).
+ * `data` [device] is what dels_w4_pack wrote, 16-byte aligned.
+ */
+typedef struct {
+  const void* data;
+  int V, K;
+  int group;                     /* 32, 64 or 128 */
+  int zeros;                     /* 1: zero points of its own; 0: 8 throughout */
+} dels_w4;
+
+/*
+ * Lays a matrix out for the products, once per set of weights.
+ * codes [device] [V, K] uint8 of 0 .. 15; scales [device] [V, ceil(K / group)] bf16;
+ * zeros [device] [V, ceil(K / group)] uint8 of 0 .. 15, or NULL. packed [device] >=
+ * dels_w4_bytes(V, K, group, zeros != NULL), 16-byte aligned. A code or zero point
+ * above 15 sets DELS_STATUS_BAD_VALUE in the workspace (256 bytes) and loses its
+ * higher bits. dels_w4_bytes is 0 for sizes that are not supported.
+ * Limits: 1 <= V <= 2^27, 1 <= K <= 65536.
+ */
+size_t dels_w4_bytes(int V, int K, int group, int zeros);
+int dels_w4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros, int V, int K, int group, void* packed,
+                 size_t packed_bytes, void* workspace, size_t workspace_bytes, dels_stream_t stream);
+
+/*
+ * out[b, v] = sum_k w[v, k] x[b, k].  x [device] [B, K] of x_dtype, x_stride elements
+ * from one row to the next (0: K); out [device] [B, V] of out_dtype, out_stride (0: V).
+ * Products and sums are float32 (x to its last bit: float32 features as three exact
+ * bf16 terms), each group's sum times its scale; equal calls give equal bits.
+ * workspace >= 256 bytes. Limits: 0 <= B <= 65535; pointers aligned to their elements.
+ */
+size_t dels_w4_project_workspace_bytes(const dels_w4* w, int B);
+int dels_w4_project(const dels_w4* w, const void* x, dels_dtype x_dtype, long long x_stride, int B, void* out,
+                    dels_dtype out_dtype, long long out_stride, void* workspace, size_t workspace_bytes,
+                    dels_stream_t stream);
+
 /* ---- instrumentation (not part of the method) ---------------------------- */
 
 /* Kernel classes timed by the optional per-kernel profiler. */
@@ -583,7 +677,9 @@ enum {
   DELS_KCLASS_PRIOR = 8,         /* unigram prior estimation (count, sum, log)            */
   DELS_KCLASS_SCORE = 9,         /* scoring of rows                                       */
   DELS_KCLASS_DISTILL = 10,      /* distillation loss and gradients                       */
-  DELS_KCLASS_COUNT = 11
+  DELS_KCLASS_PROBS = 11,        /* probabilities of rows                                 */
+  DELS_KCLASS_W4 = 12,           /* 4-bit matrices: layout and products                   */
+  DELS_KCLASS_COUNT = 13
 };
 
 /*

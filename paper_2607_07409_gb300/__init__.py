@@ -20,7 +20,7 @@ import torch
 __all__ = [
     "DELS_OK", "DELS_F32", "DELS_BF16",
     "DELS_HEAD_GRU", "DELS_HEAD_MLP", "DELS_HEAD_XFMR", "DELS_HEAD_MARKOV",
-    "DELS_STATUS_NONFINITE", "DELS_STATUS_TIMEOUT", "DELS_STATUS_BAD_TOKEN",
+    "DELS_STATUS_NONFINITE", "DELS_STATUS_TIMEOUT", "DELS_STATUS_BAD_TOKEN", "DELS_STATUS_BAD_VALUE",
     "DELS_ERR_NULL_POINTER", "DELS_ERR_BAD_SHAPE", "DELS_ERR_BAD_DTYPE", "DELS_ERR_ALIGNMENT",
     "DELS_ERR_WORKSPACE", "DELS_ERR_UNSUPPORTED", "DELS_ERR_CUDA", "DELS_ERR_TOO_LARGE",
     "DelsError", "LocalHead", "lib", "library_path", "exported_symbols",
@@ -38,12 +38,15 @@ __all__ = [
     "Rows", "Teacher", "dels_score_workspace_bytes", "dels_score_rows",
     "dels_distill_state_bytes", "dels_distill_workspace_bytes", "dels_distill_loss", "dels_distill_grad",
     "dels_distill_step", "rows_of", "teacher_of", "TokenScorer", "Distiller", "distill_loss",
+    "Probs", "dels_row_probs_workspace_bytes", "dels_row_probs", "dels_verify_given_workspace_bytes",
+    "dels_verify_given", "RowProbs", "BlockVerifier",
+    "W4", "dels_w4_bytes", "dels_w4_pack", "dels_w4_project_workspace_bytes", "dels_w4_project", "pack_w4", "W4Matrix",
 ]
 
 DELS_OK = 0
 DELS_F32, DELS_BF16 = 0, 1
 DELS_HEAD_GRU, DELS_HEAD_MLP, DELS_HEAD_XFMR, DELS_HEAD_MARKOV = 0, 1, 2, 3
-DELS_STATUS_NONFINITE, DELS_STATUS_TIMEOUT, DELS_STATUS_BAD_TOKEN = 1, 2, 4
+DELS_STATUS_NONFINITE, DELS_STATUS_TIMEOUT, DELS_STATUS_BAD_TOKEN, DELS_STATUS_BAD_VALUE = 1, 2, 4, 8
 (DELS_ERR_NULL_POINTER, DELS_ERR_BAD_SHAPE, DELS_ERR_BAD_DTYPE, DELS_ERR_ALIGNMENT, DELS_ERR_WORKSPACE,
  DELS_ERR_UNSUPPORTED, DELS_ERR_CUDA, DELS_ERR_TOO_LARGE) = -1, -2, -3, -4, -5, -6, -7, -8
 
@@ -87,7 +90,26 @@ class Teacher(ctypes.Structure):
     ]
 
 
+class Probs(ctypes.Structure):
+    """Mirror of ``dels_probs``."""
+
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("batch_stride", ctypes.c_longlong),
+        ("row_stride", ctypes.c_longlong),
+    ]
+
+
+class W4(ctypes.Structure):
+    """Mirror of ``dels_w4``."""
+
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("V", ctypes.c_int), ("K", ctypes.c_int), ("group", ctypes.c_int),
+        ("zeros", ctypes.c_int),
+    ]
+
+
 _ROWS, _TEACHER, _ll = ctypes.POINTER(Rows), ctypes.POINTER(Teacher), ctypes.c_longlong
+_PROBS, _W4 = ctypes.POINTER(Probs), ctypes.POINTER(W4)
 
 _SIGS = {
     "dels_selftest_timeout_bytes": (_sz, []),
@@ -124,6 +146,14 @@ _SIGS = {
     "dels_distill_loss": (_i, [_ROWS, _i, _i, _TEACHER, _vp, _vp, _sz, _vp, _sz, _vp]),
     "dels_distill_grad": (_i, [_ROWS, _i, _i, _TEACHER, _vp, _vp, _sz, _vp, _ll, _vp, _vp, _vp]),
     "dels_distill_step": (_i, [_ROWS, _i, _i, _TEACHER, _vp, _vp, _ll, _vp, _vp, _vp, _sz, _vp]),
+    "dels_row_probs_workspace_bytes": (_sz, [_i, _i]),
+    "dels_row_probs": (_i, [_ROWS, _i, _i, _vp, _i, _ll, _vp, _sz, _vp]),
+    "dels_verify_given_workspace_bytes": (_sz, [_i, _i, _i]),
+    "dels_verify_given": (_i, [_vp, _PROBS, _PROBS, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "dels_w4_bytes": (_sz, [_i, _i, _i, _i]),
+    "dels_w4_pack": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _sz, _vp, _sz, _vp]),
+    "dels_w4_project_workspace_bytes": (_sz, [_W4, _i]),
+    "dels_w4_project": (_i, [_W4, _vp, _i, _ll, _i, _vp, _i, _ll, _vp, _sz, _vp]),
     "dels_status_string": (ctypes.c_char_p, [_i]),
     "dels_version": (_i, []),
     "dels_profile_enable": (_i, [_i]),
@@ -133,7 +163,7 @@ _SIGS = {
 
 # kernel classes of the optional profiler
 KCLASS = {"vocab_combine": 0, "head_gemm": 1, "head_misc": 2, "merge": 3, "pos0": 4, "verify": 5, "combine": 6,
-          "draft_block": 7, "prior": 8, "score": 9, "distill": 10}
+          "draft_block": 7, "prior": 8, "score": 9, "distill": 10, "probs": 11, "w4": 12}
 
 
 def exported_symbols():
@@ -470,6 +500,61 @@ def dels_distill_step(x: Rows, rows: int, V: int, teacher: Teacher, out_loss, gr
                                 _ptr(workspace), workspace_bytes, _stream(stream))
     if r == DELS_OK:
         _written(out_loss, grad_short, grad_alpha, grad_beta)
+    return r
+
+
+def dels_row_probs_workspace_bytes(rows: int, V: int) -> int:
+    return lib().dels_row_probs_workspace_bytes(rows, V)
+
+
+def dels_row_probs(x: Rows, rows: int, V: int, out, out_dtype: int, out_stride: int, workspace, workspace_bytes: int,
+                   stream=None) -> int:
+    """``out``: a tensor whose rows may be strided, or an address (``out_stride`` elements a row)."""
+    r = lib().dels_row_probs(ctypes.byref(x), rows, V, _row_ptr(out), out_dtype, out_stride, _ptr(workspace),
+                             workspace_bytes, _stream(stream))
+    if r == DELS_OK:
+        _written(out)
+    return r
+
+
+def dels_verify_given_workspace_bytes(B: int, n: int, V: int) -> int:
+    return lib().dels_verify_given_workspace_bytes(B, n, V)
+
+
+def dels_verify_given(tokens, target: Probs, draft: Optional[Probs], uniforms, lengths, B: int, n: int, V: int,
+                      out_accept_len, out_bonus, workspace, workspace_bytes: int, stream=None) -> int:
+    r = lib().dels_verify_given(_ptr(tokens), ctypes.byref(target), None if draft is None else ctypes.byref(draft),
+                                _ptr(uniforms), _ptr(lengths), B, n, V, _ptr(out_accept_len), _ptr(out_bonus),
+                                _ptr(workspace), workspace_bytes, _stream(stream))
+    if r == DELS_OK:
+        _written(out_accept_len, out_bonus)
+    return r
+
+
+def dels_w4_bytes(V: int, K: int, group: int, zeros: bool) -> int:
+    return lib().dels_w4_bytes(V, K, group, 1 if zeros else 0)
+
+
+def dels_w4_pack(codes, scales, zeros, V: int, K: int, group: int, packed, packed_bytes: int, workspace,
+                 workspace_bytes: int, stream=None) -> int:
+    r = lib().dels_w4_pack(_ptr(codes), _ptr(scales), _ptr(zeros), V, K, group, _ptr(packed), packed_bytes,
+                           _ptr(workspace), workspace_bytes, _stream(stream))
+    if r == DELS_OK:
+        _written(packed)
+    return r
+
+
+def dels_w4_project_workspace_bytes(w: W4, B: int) -> int:
+    return lib().dels_w4_project_workspace_bytes(ctypes.byref(w), B)
+
+
+def dels_w4_project(w: W4, x, x_dtype: int, x_stride: int, B: int, out, out_dtype: int, out_stride: int, workspace,
+                    workspace_bytes: int, stream=None) -> int:
+    """``x``, ``out``: tensors whose rows may be strided, or addresses (with their strides in elements)."""
+    r = lib().dels_w4_project(ctypes.byref(w), _row_ptr(x), x_dtype, x_stride, B, _row_ptr(out), out_dtype, out_stride,
+                              _ptr(workspace), workspace_bytes, _stream(stream))
+    if r == DELS_OK:
+        _written(out)
     return r
 
 
@@ -889,3 +974,171 @@ def distill_loss(short, ids, logprob, *, long=None, log_prior=None, alpha=None, 
             if t is not None and t.requires_grad:
                 raise ValueError(f"distill_loss has no gradient of {name}: detach it")
     return _DistillLoss.apply(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature)
+
+
+# ----------------------------------------------------------------------------- probabilities, given numbers, 4-bit weights
+
+class RowProbs:
+    """Probabilities of [rows, V] logits, plain or fused, as float32 or bfloat16: output and a workspace for
+    repeated ``dels_row_probs`` calls."""
+
+    def __init__(self, rows: int, V: int, dtype: torch.dtype = torch.float32, device=None):
+        self.rows, self.V, self.dtype = rows, V, dtype
+        self._code = dtype_code(dtype)
+        self._dev = _device_index(device)
+        self.device = torch.device("cuda", self._dev)
+        self.ws_bytes = dels_row_probs_workspace_bytes(rows, V)
+        if self.ws_bytes == 0:
+            raise DelsError(DELS_ERR_BAD_SHAPE, "dels_row_probs_workspace_bytes")
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self._ws = self.workspace.data_ptr()
+        self._out = None
+        self._call = lib().dels_row_probs
+
+    def __call__(self, logits: torch.Tensor, *, short=None, log_prior=None, alpha=None, beta=None,
+                 temperature: float = 1.0, out=None, stream=None) -> torch.Tensor:
+        """Probabilities [rows, V]; ``out``: where they go (rows may be strided), else the handle's own tensor,
+        which its next call overwrites."""
+        _need_current(self._dev)
+        x = rows_of(self.rows, self.V, logits, short, log_prior, alpha, beta, temperature)
+        if logits.get_device() != self._dev:
+            raise ValueError(f"logits must be on {self.device}")
+        if out is None:
+            if self._out is None:
+                self._out = torch.empty(self.rows, self.V, dtype=self.dtype, device=self.device)
+            out = self._out
+        shape = (self.rows, self.V)
+        to = _logits(out, shape, self.dtype, self._dev, "out")
+        r = self._call(ctypes.byref(x), self.rows, self.V, to, self._code, _row_stride(out, shape, "out"), self._ws,
+                       self.ws_bytes, _stream(stream))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_row_probs")
+        _increment_version((out,))
+        return out
+
+    def status(self, stream=None) -> int:
+        return dels_read_status(self.workspace, stream)
+
+
+def _probs_of(t: torch.Tensor, B: int, rows: int, V: int, device: int, what: str) -> Probs:
+    """``dels_probs`` of a [B, rows, V] tensor (requests and rows may be strided). The caller keeps it alive."""
+    if t.shape != (B, rows, V) or t.get_device() != device:
+        raise ValueError(f"{what} must be [{B}, {rows}, {V}] on cuda:{device}, got {list(t.shape)} on {t.device}")
+    sb, sr, one = t.stride()
+    if rows == 1:
+        sr = V
+    if B <= 1:
+        sb = rows * sr
+    if (V > 1 and one != 1) or sr < V or sb < (rows - 1) * sr + V:
+        raise ValueError(f"{what}: expected [B, rows, V] probabilities whose rows are dense and apart")
+    return Probs(t.data_ptr(), dtype_code(t.dtype), sb, sr)
+
+
+class BlockVerifier:
+    """Speculative sampling of drafted blocks from given probabilities and uniforms (``n = 0``: a token of each
+    row): outputs and a workspace for repeated ``dels_verify_given`` calls."""
+
+    def __init__(self, B: int, n: int, V: int, device=None):
+        self.B, self.n, self.V = B, n, V
+        self._dev = _device_index(device)
+        self.device = torch.device("cuda", self._dev)
+        self.ws_bytes = dels_verify_given_workspace_bytes(B, n, V)
+        if self.ws_bytes == 0:
+            raise DelsError(DELS_ERR_BAD_SHAPE, "dels_verify_given_workspace_bytes")
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self.accept_len, self.bonus = torch.empty(2, B, dtype=torch.int32, device=self.device).unbind(0)
+        self._own = [t.data_ptr() for t in (self.accept_len, self.bonus, self.workspace)]
+        self._call = lib().dels_verify_given
+
+    def __call__(self, tokens, target: torch.Tensor, uniforms: torch.Tensor, *, draft=None, lengths=None, stream=None):
+        """(tokens kept of each request, the token after them), int32 [B] each, which the next call overwrites.
+        ``tokens`` [B, n] (None for n = 0), ``target`` [B, n + 1, V] and ``draft`` [B, n, V] probabilities,
+        ``uniforms`` [B, n + 1], ``lengths`` [B]."""
+        _need_current(self._dev)
+        B, n, V, dev = self.B, self.n, self.V, self._dev
+        p = _probs_of(target, B, n + 1, V, dev, "target")
+        q = None if draft is None or n == 0 else _probs_of(draft, B, n, V, dev, "draft")
+        if tokens is None and n > 0:
+            raise ValueError(f"tokens must be [{B}, {n}]")
+        tok = _of(tokens, torch.int32, (B, n), dev, "tokens")
+        u = _of(uniforms, torch.float32, (B, n + 1), dev, "uniforms")
+        if u is None:
+            raise ValueError(f"uniforms must be [{B}, {n + 1}]")
+        acc, bonus, ws = self._own
+        r = self._call(tok, ctypes.byref(p), None if q is None else ctypes.byref(q), u,
+                       _of(lengths, torch.int32, (B,), dev, "lengths"), B, n, V, acc, bonus, ws, self.ws_bytes,
+                       _stream(stream))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_verify_given")
+        _increment_version((self.accept_len, self.bonus))
+        return self.accept_len, self.bonus
+
+    def status(self, stream=None) -> int:
+        return dels_read_status(self.workspace, stream)
+
+
+class W4Matrix:
+    """A [V, K] matrix of 4-bit codes with a bf16 scale (and zero point) per group of inputs, laid out for
+    ``project``. ``pack_w4`` makes one."""
+
+    def __init__(self, data: torch.Tensor, V: int, K: int, group: int, zeros: bool):
+        if data.data_ptr() % 16 or data.numel() < dels_w4_bytes(V, K, group, zeros):
+            raise ValueError("data must be what dels_w4_pack wrote")
+        self.data, self.V, self.K, self.group, self.zeros = data, V, K, group, zeros
+        self._dev = data.get_device()
+        self.device = data.device
+        self.struct = W4(data.data_ptr(), V, K, group, 1 if zeros else 0)
+        self.ws_bytes = dels_w4_project_workspace_bytes(self.struct, 1)
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self._ws = self.workspace.data_ptr()
+        self._call = lib().dels_w4_project
+
+    def project(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32,
+                stream=None) -> torch.Tensor:
+        """[B, V] = x W^T of features [B, K] (float32 or bfloat16; rows may be strided), in a new tensor of
+        ``dtype`` or in ``out`` (float32 or bfloat16; rows may be strided; no part of ``x``)."""
+        _need_current(self._dev)
+        if x.dim() != 2:
+            raise ValueError(f"x must be [B, {self.K}]")
+        B = x.shape[0]
+        if out is None:
+            out = torch.empty(B, self.V, dtype=dtype, device=self.device)
+        xs, os_ = (B, self.K), (B, self.V)
+        xp = _logits(x, xs, x.dtype, self._dev, "x")
+        op = _logits(out, os_, out.dtype, self._dev, "out")
+        r = self._call(ctypes.byref(self.struct), xp, dtype_code(x.dtype), _row_stride(x, xs, "x"), B, op,
+                       dtype_code(out.dtype), _row_stride(out, os_, "out"), self._ws, self.ws_bytes, _stream(stream))
+        if r != DELS_OK:
+            raise DelsError(r, "dels_w4_project")
+        _increment_version((out,))
+        return out
+
+    def status(self, stream=None) -> int:
+        return dels_read_status(self.workspace, stream)
+
+
+def pack_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, *, group: int,
+            stream=None) -> W4Matrix:
+    """A ``W4Matrix`` of codes [V, K] uint8 of 0 .. 15, scales [V, ceil(K / group)] bfloat16 and zero points of the
+    same shape, uint8 of 0 .. 15 (None: 8). ``group``: 32, 64 or 128. Waits for the device, which checks them."""
+    if codes.dim() != 2:
+        raise ValueError("codes must be [V, K]")
+    if not codes.is_cuda:
+        raise ValueError("expected a CUDA tensor: the library's entry points take device pointers")
+    (V, K), dev = codes.shape, codes.get_device()
+    _need_current(dev)
+    nbytes = dels_w4_bytes(V, K, group, zeros is not None)
+    if nbytes == 0:
+        raise DelsError(DELS_ERR_BAD_SHAPE, "dels_w4_bytes")
+    groups = (V, -(-K // group))
+    data = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+    if scales is None:
+        raise ValueError("a matrix needs scales")
+    w = W4Matrix(data, V, K, group, zeros is not None)
+    _check(lib().dels_w4_pack(_of(codes, torch.uint8, (V, K), dev, "codes"),
+                              _of(scales, torch.bfloat16, groups, dev, "scales"),
+                              _of(zeros, torch.uint8, groups, dev, "zeros"), V, K, group, data.data_ptr(), nbytes,
+                              w._ws, w.ws_bytes, _stream(stream)), "dels_w4_pack")
+    if w.status(stream) != 0:
+        raise ValueError("codes and zero points must be 0 .. 15")
+    return w

@@ -878,6 +878,7 @@ const char* dels_status_string(int code) {
     case DELS_STATUS_NONFINITE: return "device: non-finite logits";
     case DELS_STATUS_TIMEOUT: return "device: bounded wait expired";
     case DELS_STATUS_BAD_TOKEN: return "device: draft token out of range";
+    case DELS_STATUS_BAD_VALUE: return "device: given value out of range";
     default: return "unknown status";
   }
 }
@@ -2375,6 +2376,170 @@ int dels_distill_step(const dels_rows* x, int rows, int V, const dels_teacher* t
     if (launch_distill_grad(a, f32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
   }
   if ((grad_alpha || grad_beta) && launch_weight_grads(a, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+// ------------------------------ probabilities of rows, verification from given numbers
+
+size_t dels_row_probs_workspace_bytes(int rows, int V) {
+  return rows < 0 || rows > (1 << 27) || V < 1 || V > kMaxScoreV ? 0 : (size_t)kHeaderBytes;
+}
+
+int dels_row_probs(const dels_rows* x, int rows, int V, void* out, dels_dtype out_dtype, long long out_stride,
+                   void* workspace, size_t workspace_bytes, dels_stream_t stream) {
+  RowsCall call;
+  const int rc = rows_call(x, rows, V, kMaxScoreV, &call);
+  if (rc != DELS_OK) return rc;
+  if (out_dtype != DELS_F32 && out_dtype != DELS_BF16) return DELS_ERR_BAD_DTYPE;
+  const long long ld = out_stride ? out_stride : V;
+  if (ld < V) return DELS_ERR_BAD_SHAPE;
+  if (!workspace || workspace_bytes < (size_t)kHeaderBytes) return DELS_ERR_WORKSPACE;
+  if (rows == 0) return DELS_OK;
+  if (!out) return DELS_ERR_NULL_POINTER;
+  const uintptr_t es = out_dtype == DELS_F32 ? 4 : 2;
+  if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(out) & (es - 1))) return DELS_ERR_ALIGNMENT;
+  ProbsArgs a{};
+  a.in = call.in;
+  a.out = out;
+  a.out_f32 = out_dtype == DELS_F32;
+  a.ld_out = ld;
+  a.status = at<int>(workspace, 0);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  PROF(DELS_KCLASS_PROBS);
+  if (launch_row_probs(a, x->dtype == DELS_F32, call.fused, call.vec, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+static bool given_ok(int B, int n, int V) {
+  return B >= 0 && B <= (1 << 20) && n >= 0 && n <= kMaxVerifyBlock && V >= 1 && V <= kMaxScoreV;
+}
+
+// [B, rows, V] probabilities of a call.
+static int given_rows(const dels_probs* x, int rows, int V, GivenRows* out) {
+  if (x->dtype != DELS_F32 && x->dtype != DELS_BF16) return DELS_ERR_BAD_DTYPE;
+  out->p = x->data;
+  out->f32 = x->dtype == DELS_F32;
+  out->ld = x->row_stride ? x->row_stride : V;
+  if (out->ld < V || out->ld > (1ll << 40)) return DELS_ERR_BAD_SHAPE;
+  out->ld_b = x->batch_stride ? x->batch_stride : rows * out->ld;
+  if (out->ld_b < (rows - 1) * out->ld + V) return DELS_ERR_BAD_SHAPE;
+  if (reinterpret_cast<uintptr_t>(x->data) & (out->f32 ? 3u : 1u)) return DELS_ERR_ALIGNMENT;
+  return DELS_OK;
+}
+
+size_t dels_verify_given_workspace_bytes(int B, int n, int V) { return given_ok(B, n, V) ? (size_t)kHeaderBytes : 0; }
+
+int dels_verify_given(const int32_t* tokens, const dels_probs* target, const dels_probs* draft, const float* uniforms,
+                      const int32_t* lengths, int B, int n, int V, int32_t* out_accept_len, int32_t* out_bonus,
+                      void* workspace, size_t workspace_bytes, dels_stream_t stream) {
+  if (!given_ok(B, n, V)) return DELS_ERR_BAD_SHAPE;
+  if (!target) return DELS_ERR_NULL_POINTER;
+  VerifyGivenArgs a{};
+  int rc = given_rows(target, n + 1, V, &a.target);
+  if (rc == DELS_OK && draft && n > 0) rc = given_rows(draft, n, V, &a.draft);
+  if (rc != DELS_OK) return rc;
+  if (!workspace || workspace_bytes < (size_t)kHeaderBytes) return DELS_ERR_WORKSPACE;
+  if (B == 0) return DELS_OK;
+  if (!target->data || !uniforms || !out_accept_len || !out_bonus || (n > 0 && (!tokens || (draft && !draft->data))))
+    return DELS_ERR_NULL_POINTER;
+  const auto off4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
+  if (!aligned16(workspace) || off4(tokens) || off4(uniforms) || off4(lengths) || off4(out_accept_len) ||
+      off4(out_bonus))
+    return DELS_ERR_ALIGNMENT;
+  a.tokens = tokens;
+  a.uniforms = uniforms;
+  a.lengths = lengths;
+  a.B = B;
+  a.n = n;
+  a.V = V;
+  a.out_accept = out_accept_len;
+  a.out_bonus = out_bonus;
+  a.status = at<int>(workspace, 0);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  PROF(DELS_KCLASS_VERIFY);
+  if (launch_verify_given(a, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+// --------------------------------------------------- products with 4-bit weights
+
+static bool w4_ok(int V, int K, int group) {
+  return V >= 1 && V <= (1 << 27) && K >= 1 && K <= 65536 && (group == 32 || group == 64 || group == 128);
+}
+
+static int w4_matrix(const dels_w4* w) {
+  if (!w || !w->data) return DELS_ERR_NULL_POINTER;
+  if (!w4_ok(w->V, w->K, w->group)) return DELS_ERR_BAD_SHAPE;
+  return aligned16(w->data) ? DELS_OK : DELS_ERR_ALIGNMENT;
+}
+
+size_t dels_w4_bytes(int V, int K, int group, int zeros) {
+  if (!w4_ok(V, K, group)) return 0;
+  const W4Layout L = w4_layout(V, K, group, zeros != 0);
+  return (size_t)L.tile_bytes * (size_t)L.tiles;
+}
+
+int dels_w4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros, int V, int K, int group, void* packed,
+                 size_t packed_bytes, void* workspace, size_t workspace_bytes, dels_stream_t stream) {
+  if (!w4_ok(V, K, group)) return DELS_ERR_BAD_SHAPE;
+  if (!codes || !scales || !packed) return DELS_ERR_NULL_POINTER;
+  if (!workspace || workspace_bytes < (size_t)kHeaderBytes || packed_bytes < dels_w4_bytes(V, K, group, zeros != nullptr))
+    return DELS_ERR_WORKSPACE;
+  if (!aligned16(packed) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(scales) & 1u))
+    return DELS_ERR_ALIGNMENT;
+  W4PackArgs a{};
+  a.codes = codes;
+  a.scales = static_cast<const uint16_t*>(scales);
+  a.zeros = zeros;
+  a.V = V;
+  a.K = K;
+  a.group = group;
+  a.lay = w4_layout(V, K, group, zeros != nullptr);
+  a.packed = static_cast<uint8_t*>(packed);
+  a.status = at<int>(workspace, 0);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  PROF(DELS_KCLASS_W4);
+  if (launch_w4_pack(a, s) != cudaSuccess) return DELS_ERR_CUDA;
+  return DELS_OK;
+}
+
+size_t dels_w4_project_workspace_bytes(const dels_w4* w, int B) {
+  return !w || !w4_ok(w->V, w->K, w->group) || B < 0 || B > 65535 ? 0 : (size_t)kHeaderBytes;
+}
+
+int dels_w4_project(const dels_w4* w, const void* x, dels_dtype x_dtype, long long x_stride, int B, void* out,
+                    dels_dtype out_dtype, long long out_stride, void* workspace, size_t workspace_bytes,
+                    dels_stream_t stream) {
+  const int rc = w4_matrix(w);
+  if (rc != DELS_OK) return rc;
+  if ((x_dtype != DELS_F32 && x_dtype != DELS_BF16) || (out_dtype != DELS_F32 && out_dtype != DELS_BF16))
+    return DELS_ERR_BAD_DTYPE;
+  const long long ld_x = x_stride ? x_stride : w->K, ld_out = out_stride ? out_stride : w->V;
+  if (B < 0 || B > 65535 || ld_x < w->K || ld_out < w->V) return DELS_ERR_BAD_SHAPE;
+  if (!workspace || workspace_bytes < (size_t)kHeaderBytes) return DELS_ERR_WORKSPACE;
+  if (B == 0) return DELS_OK;
+  if (!x || !out) return DELS_ERR_NULL_POINTER;
+  if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(x) & (x_dtype == DELS_F32 ? 3u : 1u)) ||
+      (reinterpret_cast<uintptr_t>(out) & (out_dtype == DELS_F32 ? 3u : 1u)))
+    return DELS_ERR_ALIGNMENT;
+  W4Args a{};
+  a.packed = static_cast<const uint8_t*>(w->data);
+  a.V = w->V;
+  a.K = w->K;
+  a.group = w->group;
+  a.zeros = w->zeros != 0;
+  a.lay = w4_layout(w->V, w->K, w->group, a.zeros);
+  a.x = x;
+  a.x_f32 = x_dtype == DELS_F32;
+  a.ld_x = ld_x;
+  a.B = B;
+  a.out = out;
+  a.out_f32 = out_dtype == DELS_F32;
+  a.ld_out = ld_out;
+  a.status = at<int>(workspace, 0);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  PROF(DELS_KCLASS_W4);
+  if (launch_w4_project(a, s) != cudaSuccess) return DELS_ERR_CUDA;
   return DELS_OK;
 }
 

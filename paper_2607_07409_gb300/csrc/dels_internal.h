@@ -196,6 +196,88 @@ cudaError_t launch_distill_step(const DistillArgs& a, bool f32, bool fused, bool
 cudaError_t launch_distill_grad(const DistillArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
 cudaError_t launch_weight_grads(const DistillArgs& a, cudaStream_t s);
 
+// ---- probabilities of rows, verification from given numbers -------------------
+struct ProbsArgs {
+  StreamRows in;
+  void* out;                     // [rows, V]
+  int out_f32;
+  long long ld_out;              // elements
+  int* status;
+};
+cudaError_t launch_row_probs(const ProbsArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
+
+struct GivenRows {
+  const void* p;
+  int f32;
+  long long ld_b, ld;            // elements from one request, one row to the next
+};
+struct VerifyGivenArgs {
+  const int32_t* tokens;         // [B, n]
+  GivenRows target, draft;       // draft.p null: probability 1 for the drafted token
+  const float* uniforms;         // [B, n + 1]
+  const int32_t* lengths;        // [B] or null
+  int B, n, V;
+  int32_t* out_accept;
+  int32_t* out_bonus;
+  int* status;
+};
+cudaError_t launch_verify_given(const VerifyGivenArgs& a, cudaStream_t s);
+
+// ---- products with 4-bit weights ---------------------------------------------
+// The packed matrix: for every 32 rows, blocks of 128 inputs (the last one of as many
+// whole 32s as there are), each with its codes, its groups' scales and zero points.
+// * codes: 512 bytes for 32 rows x 32 inputs ("unit"), 16 for each lane of a warp. Lane
+//   4 g + t has rows g + 8 i (i < 4) and inputs 8 t .. 8 t + 7, as word 2 (i / 2) + s for the
+//   inputs 8 t + 4 s .. + 3: its nibble q and q + 4 are row i % 2 = q % 2, inputs 2 (q / 2)
+//   and 2 (q / 2) + 1 of the four. A word and a mask then give the four registers of an
+//   mma.m16n8k16 operand: (w >> 4 q) & 0x000F000F is register q.
+// * scales: 64 bytes a group, bf16 of rows g, g + 8, g + 16, g + 24 for each g of 0 .. 7
+// * zero points: 16 bytes a group, four nibbles of the same rows for each g
+constexpr int kW4Rows = 32, kW4Block = 128, kW4Unit = 32;
+struct W4Layout {
+  int units, blocks;             // of 32 and 128 inputs
+  int block_bytes;               // of a whole block
+  long long tile_bytes;          // of 32 rows
+  long long tiles;
+};
+inline __host__ __device__ int w4_part_bytes(int units, int group, int zeros) {   // of a block's first units
+  return units * 512 + (units * kW4Unit + group - 1) / group * (zeros ? 80 : 64);
+}
+inline W4Layout w4_layout(int V, int K, int group, int zeros) {
+  W4Layout L;
+  L.units = (K + kW4Unit - 1) / kW4Unit;
+  L.blocks = (L.units + 3) / 4;
+  L.block_bytes = w4_part_bytes(4, group, zeros);
+  L.tile_bytes = (long long)(L.blocks - 1) * L.block_bytes + w4_part_bytes(L.units - 4 * (L.blocks - 1), group, zeros);
+  L.tiles = ((long long)V + kW4Rows - 1) / kW4Rows;
+  return L;
+}
+struct W4PackArgs {
+  const uint8_t* codes;
+  const uint16_t* scales;
+  const uint8_t* zeros;          // or null
+  int V, K, group;
+  W4Layout lay;
+  uint8_t* packed;
+  int* status;
+};
+cudaError_t launch_w4_pack(const W4PackArgs& a, cudaStream_t s);
+
+struct W4Args {
+  const uint8_t* packed;
+  int V, K, group, zeros;
+  W4Layout lay;
+  const void* x;                 // [B, K]
+  int x_f32;
+  long long ld_x;                // elements
+  int B;
+  void* out;                     // [B, V]
+  int out_f32;
+  long long ld_out;
+  int* status;
+};
+cudaError_t launch_w4_project(const W4Args& a, cudaStream_t s);
+
 // ---- draft merge + gather of the next local-head input ----------------------
 // Temperature-1 drafting (on = 0: temperature 0). The uniforms of (request
 // b, position j, stream, vocabulary index) come from Philox4x32-10 keyed by
