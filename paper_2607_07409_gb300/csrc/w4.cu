@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "dels_device.cuh"
 
@@ -67,13 +68,19 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// y = W x on the tensor cores' register path (mma.m16n8k16, bf16 in, float32 out).
+// y = W x on the tensor cores' register path (mma.m16n8k16, float32 sums).
 //
-// A code minus its zero point is a whole number of -15 .. 15, exact in bf16, so that the
-// products with a bf16 feature are exact too; a group's sum is scaled in float32. Float32
-// features are three bf16 terms by truncation, again exact. The codes of a word become an
-// operand's registers by a mask each: the 4 bits over bf16's 0x4300 are 128 + c, minus
-// 128 + z the weight.
+// A code minus its zero point is a whole number of -15 .. 15, and a bf16 feature has 8
+// significant bits: the products are exact, and a group's sum is scaled in float32.
+// * HALF, few requests: fp16 operands. Its 10 bits of mantissa hold a code where it lies in
+//   a byte, low or high, so that a word of 8 codes takes 4 masks and one shift (a bf16 operand 4
+//   and 3, and these are what bounds few requests: the ALU pipe issues every other cycle).
+//   (w & 0x000F000F) | 0x6400 is 1024 + c and the high ones' 1024 + 16 c; an fma takes the zero
+//   point off. A request's features are scaled by a power of two to at most 2^15: fp16 then
+//   holds bf16 features exactly down to 2^-32 of the request's largest, and what is
+//   smaller to 2^-40 of that. Float32 features are three fp16 terms, to the same 2^-40.
+// * else bf16 operands, the features as they are or in three bf16 terms by truncation, exactly:
+//   (w & 0x000F000F) | 0x4300 is 128 + c, minus 128 + z the weight.
 //
 // The codes stream through a ring in shared memory (bulk copies by one thread, a stage at a
 // time), so that a warp's arithmetic never waits for memory itself; the features, a few KB,
@@ -86,37 +93,62 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                "l"(src), "r"(bytes), "r"(smem_u32(bar))
                : "memory");
 }
-__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+template <bool HALF>
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (HALF)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Weights of register q of a word: codes of nibbles q and q + 4, minus zero points; base: 128 + z twice.
-__device__ __forceinline__ uint32_t weights_of(uint32_t word, int q, uint32_t base) {
-  const uint32_t c = ((word >> (4 * q)) & 0x000F000Fu) | 0x43004300u;
-  uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(c), "r"(base));
-  return r;
+// Zero points of rows g, g + 8, g + 16, g + 24 as weights_of() takes them; z: four nibbles.
+template <bool HALF>
+struct ZeroPoints {
+  uint32_t low[4], high[HALF ? 4 : 1];
+  __device__ __forceinline__ void set(uint32_t z) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t d = ((z >> (4 * i)) & 15u) * 0x00010001u;
+      if constexpr (HALF) {
+        low[i] = 0x64006400u + d;                // 1024 + z
+        high[i] = 0xD400D400u + (d << 4);        // -(64 + z)
+      } else {
+        low[i] = 0x43004300u + d;                // 128 + z
+      }
+    }
+  }
+};
+// The four registers of a word's weights: codes of nibbles q and q + 4, rows `half` and half + 1 of the lane's.
+template <bool HALF>
+__device__ __forceinline__ void weights_of(uint32_t word, const ZeroPoints<HALF>& z, int half, uint32_t (&m)[4]) {
+  if constexpr (HALF) {
+    const uint32_t next = word >> 8;
+    const uint32_t c[4] = {(word & 0x000F000Fu) | 0x64006400u, (word & 0x00F000F0u) | 0x64006400u,
+                           (next & 0x000F000Fu) | 0x64006400u, (next & 0x00F000F0u) | 0x64006400u};
+#pragma unroll
+    for (int q = 0; q < 4; q += 2) {
+      asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(m[q]) : "r"(c[q]), "r"(z.low[half]));
+      asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(m[q + 1]) : "r"(c[q + 1]), "r"(0x2C002C00u), "r"(z.high[half + 1]));
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t c = ((word >> (4 * q)) & 0x000F000Fu) | 0x43004300u;
+      asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(m[q]) : "r"(c), "r"(z.low[half + (q & 1)]));
+    }
+  }
 }
 
-// 8 features of a row from column k on (0 past K), as TERMS bf16 terms.
-template <int TERMS>
-__device__ __forceinline__ void load_features(const W4Args& a, int b, int k, uint4 (&out)[TERMS]) {
+// 8 features of a row from column k on (0 past K, and past the last row).
+__device__ __forceinline__ void load_features(const W4Args& a, int b, int k, float (&f)[8]) {
   const int n = b < a.B ? min(8, a.K - k) : 0;
-  if constexpr (TERMS == 1) {
-    uint32_t h[8];
-    const uint16_t* x = static_cast<const uint16_t*>(a.x) + b * a.ld_x + k;
-    if (n == 8 && (reinterpret_cast<uintptr_t>(x) & 15u) == 0) {
-      out[0] = __ldg(reinterpret_cast<const uint4*>(x));
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = i < n ? __ldg(x + i) : 0u;
-    out[0] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-  } else {
+  if (a.x_f32) {
     const float* x = static_cast<const float*>(a.x) + b * a.ld_x + k;
-    float f[8];
     if (n == 8 && (reinterpret_cast<uintptr_t>(x) & 15u) == 0) {
       const float4 u = __ldg(reinterpret_cast<const float4*>(x)), v = __ldg(reinterpret_cast<const float4*>(x) + 1);
       f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = v.x; f[5] = v.y; f[6] = v.z; f[7] = v.w;
@@ -124,24 +156,16 @@ __device__ __forceinline__ void load_features(const W4Args& a, int b, int k, uin
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = i < n ? __ldg(x + i) : 0.f;
     }
-    uint32_t t[TERMS][8];
+  } else {
+    const uint16_t* x = static_cast<const uint16_t*>(a.x) + b * a.ld_x + k;
+    if (n == 8 && (reinterpret_cast<uintptr_t>(x) & 15u) == 0) {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(x));
+      f[0] = bf16lo(u.x); f[1] = bf16hi(u.x); f[2] = bf16lo(u.y); f[3] = bf16hi(u.y);
+      f[4] = bf16lo(u.z); f[5] = bf16hi(u.z); f[6] = bf16lo(u.w); f[7] = bf16hi(u.w);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float r = f[i];
-#pragma unroll
-      for (int j = 0; j < TERMS; ++j) {
-        // truncated, 8 significant bits each: no term overflows, and three of them hold 24 bits.
-        // Infinities and NaN (whose bits may all be in the lower half) stay in the first.
-        const float h = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
-        const bool finite = fabsf(f[i]) < INFINITY;
-        t[j][i] = finite ? __float_as_uint(h) >> 16 : j ? 0u : f[i] != f[i] ? 0x7FC0u : __float_as_uint(f[i]) >> 16;
-        r = finite ? r - h : 0.f;
-      }
+      for (int i = 0; i < 8; ++i) f[i] = i < n ? bf16_to_f(__ldg(x + i)) : 0.f;
     }
-#pragma unroll
-    for (int j = 0; j < TERMS; ++j)
-      out[j] = make_uint4(t[j][0] | t[j][1] << 16, t[j][2] | t[j][3] << 16, t[j][4] | t[j][5] << 16,
-                          t[j][6] | t[j][7] << 16);
   }
 }
 
@@ -151,24 +175,130 @@ constexpr int kW4Producers = 96;         // threads that stage features where th
 template <int NT>
 constexpr int kW4Warps = NT <= 2 ? 16 : 8;      // warps that multiply, at most
 
+// A request's power of two: its features' largest, m, comes to 2^14 .. 2^15. 0 where there
+// is an infinity or NaN: its outputs are those of these alone, and the others count as 0.
+__device__ __forceinline__ int feature_shift(float m) {
+  return m > 0.f ? 14 - ilogbf(m) : 0;
+}
+constexpr int kNotFinite = 1 << 20;
+__device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }    // -126 .. 127
+
 // Fragments of a block's features: [4 units][TERMS][NT][32 lanes] of 16 bytes; lane 4 g + t
-// has request 8 j + g, inputs 8 t .. 8 t + 7 of the unit's 32.
-template <int NT, int TERMS>
-__device__ __forceinline__ void stage_features(const W4Args& a, int b0, int unit, int j, uint4* dst) {
-  const int lane = threadIdx.x & 31;
-  uint4 f[TERMS];
-  load_features<TERMS>(a, b0 + 8 * j + (lane >> 2), unit * kW4Unit + 8 * (lane & 3), f);
+// has request 8 j + g, inputs 8 t .. 8 t + 7 of the unit's 32. shift: HALF, the requests'.
+template <int NT, int TERMS, bool HALF>
+__device__ __forceinline__ void stage_features(const W4Args& a, int b0, int unit, int j, const int* shift, uint4* dst) {
+  const int lane = threadIdx.x & 31, b = 8 * j + (lane >> 2);
+  float f[8];
+  load_features(a, b0 + b, unit * kW4Unit + 8 * (lane & 3), f);
+  uint32_t t[TERMS][8];
+  if constexpr (HALF) {
+    const int sh = shift[b];
+    // (in two factors: the power itself may be past float32's range)
+    const float s0 = sh == kNotFinite ? 1.f : pow2i(sh / 2), s1 = sh == kNotFinite ? 1.f : pow2i(sh - sh / 2);
 #pragma unroll
-  for (int t = 0; t < TERMS; ++t) dst[(t * NT + j) * 32 + lane] = f[t];
+    for (int i = 0; i < 8; ++i) {
+      float r = sh != kNotFinite ? f[i] * s0 * s1 : fabsf(f[i]) < INFINITY ? 0.f : f[i];
+#pragma unroll
+      for (int k = 0; k < TERMS; ++k) {
+        const __half h = __float2half_rn(r);
+        t[k][i] = __half_as_ushort(h);
+        r = sh != kNotFinite ? r - __half2float(h) : 0.f;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float r = f[i];
+      const bool finite = fabsf(f[i]) < INFINITY;
+#pragma unroll
+      for (int k = 0; k < TERMS; ++k) {
+        // truncated, 8 significant bits each: no term overflows, and three of them hold 24 bits.
+        // Infinities and NaN (whose bits may all be in the lower half) stay in the first.
+        const float h = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
+        t[k][i] = finite ? __float_as_uint(h) >> 16 : k ? 0u : f[i] != f[i] ? 0x7FC0u : __float_as_uint(f[i]) >> 16;
+        r = finite ? r - h : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k)
+    dst[(k * NT + j) * 32 + lane] = make_uint4(t[k][0] | t[k][1] << 16, t[k][2] | t[k][3] << 16, t[k][4] | t[k][5] << 16,
+                                               t[k][6] | t[k][7] << 16);
 }
 
-template <int NT, int TERMS, bool ZEROS>
-__global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + kW4Producers, 1) k_w4_project(const W4Args a, const W4Plan p) {
+// One warp's unit: 32 rows, 32 inputs.
+template <int NT, int TERMS, bool HALF>
+__device__ __forceinline__ void multiply_unit(const uint4 w4, const ZeroPoints<HALF>& z, const uint4* x,
+                                              float (&acc)[2][NT][4]) {
+  uint32_t m[4][4];
+  weights_of<HALF>(w4.x, z, 0, m[0]);
+  weights_of<HALF>(w4.y, z, 0, m[1]);
+  weights_of<HALF>(w4.z, z, 2, m[2]);
+  weights_of<HALF>(w4.w, z, 2, m[3]);
+#pragma unroll
+  for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const uint4 f = x[(term * NT + j) * 32];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        mma16<HALF>(acc[h][j], m[2 * h], f.x, f.y);
+        mma16<HALF>(acc[h][j], m[2 * h + 1], f.z, f.w);
+      }
+    }
+}
+template <int NT>
+__device__ __forceinline__ void scale_group(const uint2 s, float (&acc)[2][NT][4], float (&tot)[2][NT][4]) {
+  const float sc[4] = {bf16lo(s.x), bf16hi(s.x), bf16lo(s.y), bf16hi(s.y)};
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        tot[h][j][i] = fmaf(sc[2 * h + (i >> 1)], acc[h][j][i], tot[h][j][i]);
+        acc[h][j][i] = 0.f;
+      }
+}
+
+// n <= 4 outputs from element `at` on.
+__device__ __forceinline__ void store_outputs(const W4Args& a, long long at, const float4& y, int n) {
+  const float f[4] = {y.x, y.y, y.z, y.w};
+  if (a.out_f32) {
+    float* out = static_cast<float*>(a.out) + at;
+    if (n == 4 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
+      *reinterpret_cast<float4*>(out) = y;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) out[i] = f[i];
+  } else {
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at;
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(f[0], f[1]), hi = __floats2bfloat162_rn(f[2], f[3]);
+    if (n == 4 && (reinterpret_cast<uintptr_t>(out) & 7u) == 0) {
+      uint2 u;
+      u.x = *reinterpret_cast<const uint32_t*>(&lo);
+      u.y = *reinterpret_cast<const uint32_t*>(&hi);
+      *reinterpret_cast<uint2*>(out) = u;
+      return;
+    }
+    const __nv_bfloat16 h[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) out[i] = h[i];
+  }
+}
+
+template <int NT, int TERMS, bool HALF>
+__global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Producers), 1)
+    k_w4_project(const W4Args a, const W4Plan p) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int N = NT * 8;
   constexpr int kXBlock = 4 * TERMS * NT * 512;
   __shared__ uint64_t full[kW4MaxStages], empty[kW4MaxStages];
   __shared__ int abort_flag;
+  __shared__ int shift[N];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = p.wr * p.wk;
   const int b0 = blockIdx.y * N;
   uint8_t* ring = smem;                                                     // stages of p.stage_bytes
@@ -191,20 +321,22 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + kW4Producers, 1) k_w4
 
   if (warp > warps) {
     // ---- features of every stage
-    const int t0 = warp - warps - 1;
-    int st = 0, ph = 0;
-    for (int it = blockIdx.x; it < p.items; it += gridDim.x) {
-      deadline = globaltimer_ns() + kWaitBudgetNs;
-      for (int step = 0; step < steps; ++step) {
-        if (!dead) dead = !mbar_wait(&empty[st], ph ^ 1, deadline, &abort_flag);
-        uint4* dst = reinterpret_cast<uint4*>(ring + (size_t)st * p.stage_bytes + p.x_off);
-        const int units = min(4 * p.wk, a.lay.units - step * p.wk * 4);
-        for (int i = t0; i < units * NT; i += kW4Producers / 32) {
-          const int u = i / NT, j = i - u * NT;
-          stage_features<NT, TERMS>(a, b0, step * p.wk * 4 + u, j, dst + u * (TERMS * NT * 32));
+    if constexpr (!HALF) {
+      const int t0 = warp - warps - 1;
+      int st = 0, ph = 0;
+      for (int it = blockIdx.x; it < p.items; it += gridDim.x) {
+        deadline = globaltimer_ns() + kWaitBudgetNs;
+        for (int step = 0; step < steps; ++step) {
+          if (!dead) dead = !mbar_wait(&empty[st], ph ^ 1, deadline, &abort_flag);
+          uint4* dst = reinterpret_cast<uint4*>(ring + (size_t)st * p.stage_bytes + p.x_off);
+          const int units = min(4 * p.wk, a.lay.units - step * p.wk * 4);
+          for (int i = t0; i < units * NT; i += kW4Producers / 32) {
+            const int u = i / NT, j = i - u * NT;
+            stage_features<NT, TERMS, HALF>(a, b0, step * p.wk * 4 + u, j, nullptr, dst + u * (TERMS * NT * 32));
+          }
+          mbar_arrive(&full[st]);
+          if (++st == p.stages) st = 0, ph ^= 1;
         }
-        mbar_arrive(&full[st]);
-        if (++st == p.stages) st = 0, ph ^= 1;
       }
     }
   } else if (warp == warps) {
@@ -242,15 +374,37 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + kW4Producers, 1) k_w4
   } else {
     // ---- products
     const int wr = warp / p.wk, wk = warp - wr * p.wk, g = lane >> 2, t = lane & 3;
-    if (p.resident) {
-      for (int i = warp; i < a.lay.units * NT; i += warps) {
-        const int u = i / NT, j = i - u * NT;
-        stage_features<NT, TERMS>(a, b0, u, j, reinterpret_cast<uint4*>(xres) + u * (TERMS * NT * 32));
+    if constexpr (HALF) {
+      // the requests' largest features
+      for (int b = warp; b < N; b += warps) {
+        float m = 0.f, nan = 0.f;
+        for (int k = lane * 8; k < a.K; k += 256) {
+          float f[8];
+          load_features(a, b0 + b, k, f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            m = fmaxf(m, fabsf(f[i]));
+            nan += f[i] != f[i] ? 1.f : 0.f;
+          }
+        }
+        m = warp_max(m);
+        const bool any_nan = __any_sync(0xFFFFFFFFu, nan != 0.f);
+        if (lane == 0) shift[b] = any_nan || !(m < INFINITY) ? kNotFinite : feature_shift(m);
       }
       asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
     }
-    const int gunits = a.group / kW4Unit;
+    if (p.resident) {
+      for (int i = warp; i < a.lay.units * NT; i += warps) {
+        const int u = i / NT, j = i - u * NT;
+        stage_features<NT, TERMS, HALF>(a, b0, u, j, shift, reinterpret_cast<uint4*>(xres) + u * (TERMS * NT * 32));
+      }
+      asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+    }
+    const int gunits = a.group / kW4Unit, glog = gunits == 1 ? 0 : gunits == 2 ? 1 : 2;
+    const int wr_log = 31 - __clz(p.wr);
     int st = 0, ph = 0;
+    ZeroPoints<HALF> z;
+    z.set(0x8888u);
     for (int it = blockIdx.x; it < p.items; it += gridDim.x) {
       deadline = globaltimer_ns() + kWaitBudgetNs;
       const long long tile0 = (long long)it * p.wr;
@@ -266,60 +420,32 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + kW4Producers, 1) k_w4
         const int kb = step * p.wk + wk;
         if (kb < a.lay.blocks && tile0 + wr < a.lay.tiles) {
           const uint8_t* block = ring + (size_t)st * p.stage_bytes + (size_t)(wr * p.wk + wk) * a.lay.block_bytes;
+          const uint4* codes = reinterpret_cast<const uint4*>(block) + lane;
           const int units = min(4, a.lay.units - 4 * kb);
-          const uint4* x = p.resident ? reinterpret_cast<const uint4*>(xres) + kb * (kXBlock / 16)
-                                      : reinterpret_cast<const uint4*>(ring + (size_t)st * p.stage_bytes + p.x_off) +
-                                            wk * (kXBlock / 16);
-          const uint8_t* scales = block + units * 512;
-          const uint8_t* zeros = scales + (units + gunits - 1) / gunits * 64;
-          uint32_t base[4];
+          const uint4* x = (p.resident ? reinterpret_cast<const uint4*>(xres) + kb * (kXBlock / 16)
+                                       : reinterpret_cast<const uint4*>(ring + (size_t)st * p.stage_bytes + p.x_off) +
+                                             wk * (kXBlock / 16)) + lane;
+          const uint8_t* scales = block + units * 512 + g * 8;
+          const uint8_t* zeros = block + units * 512 + ((units + gunits - 1) >> glog) * 64 + g * 2;
+          const auto unit = [&](int u, bool last) {
+            if (a.zeros && (u & (gunits - 1)) == 0) z.set(*reinterpret_cast<const uint16_t*>(zeros + (u >> glog) * 16));
+            multiply_unit<NT, TERMS, HALF>(codes[u * 32], z, x + u * (TERMS * NT * 32), acc);
+            if (last || ((u + 1) & (gunits - 1)) == 0)
+              scale_group<NT>(*reinterpret_cast<const uint2*>(scales + (u >> glog) * 64), acc, tot);
+          };
+          if (units == 4) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) base[i] = 0x43084308u;
-          for (int u = 0; u < units; ++u) {
-            const int grp = u / gunits;
-            if (ZEROS && u == grp * gunits) {
-              const uint32_t z = reinterpret_cast<const uint16_t*>(zeros + grp * 16)[g];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) base[i] = 0x43004300u + ((z >> (4 * i)) & 15u) * 0x00010001u;
-            }
-            const uint4 w4 = reinterpret_cast<const uint4*>(block)[u * 32 + lane];
-            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-            uint32_t m[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) m[i][q] = weights_of(w[i], q, base[(i >> 1) * 2 + (q & 1)]);
-#pragma unroll
-            for (int term = 0; term < TERMS; ++term)
-#pragma unroll
-              for (int j = 0; j < NT; ++j) {
-                const uint4 f = x[((u * TERMS + term) * NT + j) * 32 + lane];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  mma_bf16(acc[h][j], m[2 * h], f.x, f.y);
-                  mma_bf16(acc[h][j], m[2 * h + 1], f.z, f.w);
-                }
-              }
-            if (u + 1 == units || u + 1 == (grp + 1) * gunits) {
-              const uint2 s = reinterpret_cast<const uint2*>(scales + grp * 64)[g];
-              const float sc[4] = {bf16lo(s.x), bf16hi(s.x), bf16lo(s.y), bf16hi(s.y)};
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    tot[h][j][i] = fmaf(sc[2 * h + (i >> 1)], acc[h][j][i], tot[h][j][i]);
-                    acc[h][j][i] = 0.f;
-                  }
-            }
+            for (int u = 0; u < 4; ++u) unit(u, u == 3);
+          } else {
+#pragma unroll 1
+            for (int u = 0; u < units; ++u) unit(u, u + 1 == units);
           }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&empty[st]);
         if (++st == p.stages) st = 0, ph ^= 1;
       }
-      // ---- the parts' sums, along the vocabulary
+      // ---- the parts' sums, along the vocabulary: 8 lanes have 32 rows of a request
       float* part = sums + (size_t)warp * N * kW4Pitch;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -329,18 +455,22 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + kW4Producers, 1) k_w4
           for (int i = 0; i < 4; ++i)
             part[(8 * j + 2 * t + (i & 1)) * kW4Pitch + h * 16 + (i >> 1) * 8 + g] = tot[h][j][i];
       asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
-      const int nb = min(N, a.B - b0);
-      for (int i = warp; i < nb * p.wr; i += warps) {
-        const int b = i / p.wr, r = i - b * p.wr;
-        const long long v = (tile0 + r) * kW4Rows + lane;
-        const float* src = sums + ((size_t)r * p.wk * N + b) * kW4Pitch + lane;
-        float y = src[0];
-        for (int k = 1; k < p.wk; ++k) y += src[(size_t)k * N * kW4Pitch];
-        if (v < a.V) {
-          const long long at = (long long)(b0 + b) * a.ld_out + v;
-          if (a.out_f32) static_cast<float*>(a.out)[at] = y;
-          else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y);
+      const int lines = min(N, a.B - b0) << wr_log;
+      for (int i = warp * 4 + (lane >> 3); i < lines; i += warps * 4) {
+        const int b = i >> wr_log, r = i & (p.wr - 1);
+        const float* src = sums + ((size_t)r * p.wk * N + b) * kW4Pitch + (lane & 7) * 4;
+        float4 y = *reinterpret_cast<const float4*>(src);
+        for (int k = 1; k < p.wk; ++k) {
+          const float4 w = *reinterpret_cast<const float4*>(src + (size_t)k * N * kW4Pitch);
+          y.x += w.x; y.y += w.y; y.z += w.z; y.w += w.w;
         }
+        if constexpr (HALF) {
+          const int sh = shift[b] == kNotFinite ? 0 : -shift[b];
+          const float s0 = pow2i(sh / 2), s1 = pow2i(sh - sh / 2);
+          y.x = y.x * s0 * s1; y.y = y.y * s0 * s1; y.z = y.z * s0 * s1; y.w = y.w * s0 * s1;
+        }
+        const long long v = (tile0 + r) * kW4Rows + (lane & 7) * 4;
+        store_outputs(a, (long long)(b0 + b) * a.ld_out + v, y, (int)min(4ll, (long long)a.V - v));
       }
       asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
     }
@@ -352,7 +482,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + kW4Producers, 1) k_w4
 // rows, in units of a warp's block of 128 inputs: its steps, what the memory takes for its
 // blocks beside the other SMs, and a start.
 template <int NT, int TERMS>
-bool plan_w4(const W4Args& a, int sms, int smem, W4Plan* best) {
+bool plan_w4(const W4Args& a, int sms, int smem, bool resident, W4Plan* best) {
   const int xblock = 4 * TERMS * NT * 512, btiles = (a.B + NT * 8 - 1) / (NT * 8);
   const int ctas = std::max(1, sms / btiles);
   double least = 1e30;
@@ -367,7 +497,8 @@ bool plan_w4(const W4Args& a, int sms, int smem, W4Plan* best) {
       p.items = (int)items;
       const int sums = wr * wk * NT * 8 * kW4Pitch * 4, codes = wr * wk * a.lay.block_bytes;
       const long long stay = (long long)a.lay.blocks * xblock;
-      p.resident = stay <= 96 * 1024 && smem - sums - stay >= 3ll * codes;
+      p.resident = resident;
+      if (resident && smem - sums - stay < 3ll * codes) continue;
       p.x_off = codes;
       p.stage_bytes = codes + (p.resident ? 0 : wk * xblock);
       const long long room = smem - sums - (p.resident ? stay : 0);
@@ -387,17 +518,27 @@ bool plan_w4(const W4Args& a, int sms, int smem, W4Plan* best) {
   return least < 1e30;
 }
 
-template <int NT, int TERMS>
-cudaError_t launch_nt(const W4Args& a, cudaStream_t s) {
-  const int sms = device_sm_count(), smem = device_max_smem_optin() - 1024;
-  W4Plan p;
-  if (sms <= 0 || !plan_w4<NT, TERMS>(a, sms, smem, &p)) return cudaErrorInvalidValue;
-  const auto k = a.zeros ? k_w4_project<NT, TERMS, true> : k_w4_project<NT, TERMS, false>;
+template <int NT, int TERMS, bool HALF>
+cudaError_t launch_plan(const W4Args& a, const W4Plan& p, int sms, cudaStream_t s) {
+  const auto k = k_w4_project<NT, TERMS, HALF>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);
   if (e != cudaSuccess) return e;
   const int btiles = (a.B + NT * 8 - 1) / (NT * 8), ctas = std::max(1, sms / btiles);
   const int threads = p.wr * p.wk * 32 + 32 + (p.resident ? 0 : kW4Producers);
   return launch_pdl(k, dim3((unsigned)std::min(p.items, ctas), (unsigned)btiles), dim3(threads), (size_t)p.smem, s, a, p);
+}
+
+template <int NT, int TERMS>
+cudaError_t launch_nt(const W4Args& a, cudaStream_t s) {
+  const int sms = device_sm_count(), smem = device_max_smem_optin() - 1024;
+  W4Plan p;
+  if (sms <= 0) return cudaErrorInvalidValue;
+  const bool stays = plan_w4<NT, TERMS>(a, sms, smem, true, &p);
+  if (!stays && !plan_w4<NT, TERMS>(a, sms, smem, false, &p)) return cudaErrorInvalidValue;
+  if constexpr (NT <= 2) {
+    if (stays) return launch_plan<NT, TERMS, true>(a, p, sms, s);
+  }
+  return launch_plan<NT, TERMS, false>(a, p, sms, s);
 }
 
 }  // namespace
