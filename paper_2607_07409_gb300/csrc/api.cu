@@ -2403,6 +2403,8 @@ int dels_row_probs(const dels_rows* x, int rows, int V, void* out, dels_dtype ou
   a.out = out;
   a.out_f32 = out_dtype == DELS_F32;
   a.ld_out = ld;
+  a.scale_lo = (float)(1.4426950408889634 / (double)x->temperature - (double)call.in.scale);
+  a.least = (float)std::max(-3e38, -300.0 / (double)call.in.scale);
   a.status = at<int>(workspace, 0);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_PROBS);

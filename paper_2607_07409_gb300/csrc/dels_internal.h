@@ -202,6 +202,8 @@ struct ProbsArgs {
   void* out;                     // [rows, V]
   int out_f32;
   long long ld_out;              // elements
+  float scale_lo;                // what in.scale leaves of log2(e) / T
+  float least;                   // distance from the largest at which a value counts no more
   int* status;
 };
 cudaError_t launch_row_probs(const ProbsArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);

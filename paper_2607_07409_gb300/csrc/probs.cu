@@ -1,5 +1,15 @@
 // Probabilities of plain or fused rows: p_v = exp(z_v - m) / sum exp(z - m), z = l / T.
-// A CTA takes a row: its largest value, its sum, then the probabilities.
+//
+// A cluster of 1 to 8 CTAs takes a row, each a slice of its columns. A slice is read once: its
+// values (as stored where they are plain, else fused, in float32) stay in shared memory,
+// so that a row costs its bytes in and its bytes out. A CTA takes its slice's largest value
+// and the sum beside it; the CTAs exchange the two, and what is left is a factor for
+// each. Rows whose slices do not fit are read three times.
+//
+// What bounds it: the bytes. An exponential is taken twice (for the sum, for the output),
+// which costs less than keeping it where the slice is held in bf16.
+#include <algorithm>
+
 #include <cuda_bf16.h>
 
 #include "row_stream.cuh"
@@ -7,55 +17,259 @@
 namespace dels {
 namespace {
 
-__device__ __forceinline__ void put(float* out, float x) { __stcs(out, x); }
-__device__ __forceinline__ void put(uint16_t* out, float x) {
-  __stcs(reinterpret_cast<unsigned short*>(out), __bfloat16_as_ushort(__float2bfloat16_rn(x)));
+// 2^(d c) for d <= 0, c = log2(e) / T given as a sum c + c_lo: d c is split into a whole
+// number and the rest, which an fma has exactly but for c's own rounding; the second fma puts
+// that right. (z = d c rounded, and c too, took up to 40 2^-24 of a value 20 below the
+// largest.) Below 2^-126: 0.
+struct Exponent {
+  float c, c_lo, least;      // least: what d is not let below, 300 / c
+  __device__ __forceinline__ float operator()(float d) const {
+    d = fmaxf(d, least);
+    const float n = fmaxf(rintf(d * c), -127.f);
+    const float f = fmaf(d, c_lo, fmaf(d, c, -n));
+    return ex2_approx(f) * __int_as_float(((int)n + 127) << 23);
+  }
+};
+
+struct SliceSum {
+  float m, s;
+  int bad;
+};
+
+__device__ __forceinline__ void held_put(float* h, int i, float x) { h[i] = x; }
+__device__ __forceinline__ void held_put(uint16_t* h, int i, float x) { h[i] = (uint16_t)(__float_as_uint(x) >> 16); }
+__device__ __forceinline__ float held_get(const float* h, int i) { return h[i]; }
+__device__ __forceinline__ float held_get(const uint16_t* h, int i) { return bf16_to_f(h[i]); }
+
+// Four values from element i of a slice; `whole`: they lie on 4 elements' boundary.
+template <typename H>
+__device__ __forceinline__ void held_get4(const H* h, int i, bool whole, float (&x)[4]) {
+  if (whole) {
+    if constexpr (sizeof(H) == 4) {
+      const float4 u = *reinterpret_cast<const float4*>(h + i);
+      x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(h + i);
+      x[0] = bf16lo(u.x); x[1] = bf16hi(u.x); x[2] = bf16lo(u.y); x[3] = bf16hi(u.y);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = held_get(h, i + j);
+  }
 }
 
-template <typename T, int F, bool VEC, typename O>
+// Four outputs from `out` on, which lies on their 16 (bf16: 8) bytes.
+__device__ __forceinline__ void put4(float* out, const float (&x)[4]) {
+  __stcs(reinterpret_cast<float4*>(out), make_float4(x[0], x[1], x[2], x[3]));
+}
+__device__ __forceinline__ void put4(__nv_bfloat16* out, const float (&x)[4]) {
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
+  __stcs(reinterpret_cast<uint2*>(out),
+         make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi)));
+}
+__device__ __forceinline__ void put1(float* out, float x) { *out = x; }
+__device__ __forceinline__ void put1(__nv_bfloat16* out, float x) { *out = __float2bfloat16_rn(x); }
+
+template <typename T, int F, bool VEC, typename O, bool HOLD>
 __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a) {
-  __shared__ float red[kStreamWarps];
-  const int tid = threadIdx.x;
-  const unsigned r = blockIdx.x;
+  using H = std::conditional_t<F == kPlain, T, float>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  H* held = reinterpret_cast<H*>(smem);
+  __shared__ float red[kStreamWarps], red_s[kStreamWarps];
+  __shared__ SliceSum slices[kMaxCluster];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const unsigned C = a.in.cluster, r = blockIdx.x / C, rank = blockIdx.x - r * C;
+  if (C > 1) cluster_arrive_relaxed();      // (the row's other CTAs have begun: waited for before they are written to)
   pdl_wait();
   if (tid == 0) pdl_trigger();
-  const FusedRow<T, F, false> row(a.in, r);
-  O* out = static_cast<O*>(a.out) + (long long)r * a.ld_out;
-  const int V = a.in.V;
-  float m = -INFINITY, nan = 0.f;
-  for (int v = tid; v < V; v += kStreamThreads) {
-    const float x = row.contracted(row.l_at(v), row.s_at(v), row.p_at(v));
-    m = fmaxf(m, x);
-    nan += x != x ? 1.f : 0.f;
-  }
+  const FusedRow<T, F, VEC> row(a.in, r);
+  const long long first = (long long)rank * a.in.slice_cols;
+  const int k0 = (int)min(first, (long long)row.end), k1 = (int)min(first + a.in.slice_cols, (long long)row.end);
+  const int items = (k1 - k0 + kStreamStep - 1) / kStreamStep;
+
+  const auto load = [&](int it, Item<T, F, VEC>& v, float (&pr)[8]) {
+    const int pos = item_pos<T, VEC>(k0, it, tid);
+    if (VEC && pos >= row.sh && pos + kHalf<T> + 4 <= k1) v.load_whole(row, pos, pr);
+    else v.load(row, pos, k1, pr);           // -inf outside
+  };
+  // f(values, first position) of every item of the thread
+  const auto each = [&](auto&& f) {
+    constexpr int U = 2;
+    for (int it = 0; it < items; it += U) {
+      Item<T, F, VEC> v[U];
+      float pr[U][8], x[8], sv[8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) load(it + u, v[u], pr[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[u].template values<true>(row, pr[u], x, sv);
+        f(x, v[u].k);
+      }
+    }
+  };
+
+  float m = -INFINITY;
+  bool nan = false;
+  each([&](float (&x)[8], int k) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) nan |= x[i] != x[i];
+    m = fmaxf(m, max8(x));
+    if constexpr (HOLD) {
+      if (VEC && k + kHalf<T> + 4 <= k1) {
+        if constexpr (sizeof(H) == 2) {
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[i] = __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632);
+          *reinterpret_cast<uint4*>(held + k - k0) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+          *reinterpret_cast<float4*>(held + k - k0) = make_float4(x[0], x[1], x[2], x[3]);
+          *reinterpret_cast<float4*>(held + k - k0 + kHalf<T>) = make_float4(x[4], x[5], x[6], x[7]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int q = elem_pos<T, VEC>(k, i);
+          if (q < k1) held_put(held, q - k0, x[i]);
+        }
+      }
+    }
+  });
   m = warp_max(m);
-  if ((tid & 31) == 0) red[tid >> 5] = m;
+  nan = __any_sync(0xFFFFFFFFu, nan);
+  if (lane == 0) red[warp] = nan ? NAN : m;
   __syncthreads();
-  for (int i = 0; i < kStreamWarps; ++i) m = fmaxf(m, red[i]);
-  float s = 0.f;
-  for (int v = tid; v < V; v += kStreamThreads) {
-    const float x = row.contracted(row.l_at(v), row.s_at(v), row.p_at(v));
-    s += ex2_approx((x - m) * a.in.scale);
+  nan = false;
+#pragma unroll
+  for (int i = 0; i < kStreamWarps; ++i) {
+    nan |= red[i] != red[i];
+    m = fmaxf(m, red[i]);
   }
-  s = block_sum(s);
-  const bool ok = block_sum(nan) == 0.f && m > -INFINITY && m < INFINITY && s > 0.f && s < INFINITY;
+  const Exponent ex{a.in.scale, a.scale_lo, a.least};
+  float s = 0.f;
+  const bool some = m > -INFINITY && m < INFINITY;
+  if (some) {
+    const auto add = [&](float (&x)[8]) {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = ex(x[i] - m);
+      s += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+    };
+    if constexpr (HOLD) {
+      const int n = k1 - k0;                 // (in fours; the ragged last one by its elements)
+      for (int i = tid * 8; i < n; i += kStreamStep) {
+        float lo[4], hi[4], x[8];
+        if (i + 8 <= n) {
+          held_get4(held, i, true, lo);
+          held_get4(held, i + 4, true, hi);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            lo[j] = i + j < n ? held_get(held, i + j) : -INFINITY;
+            hi[j] = i + 4 + j < n ? held_get(held, i + 4 + j) : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = lo[j], x[4 + j] = hi[j];
+        add(x);
+      }
+    } else {
+      each([&](float (&x)[8], int) { add(x); });
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  if (lane == 0) red_s[warp] = s;
+  __syncthreads();
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kStreamWarps; ++i) s += red_s[i];
+
+  float M = m, S = s;
+  if (C > 1) {
+    cluster_wait();
+    if (tid < C) {                            // this slice's place in every CTA of the row
+      const uint32_t at = cluster_map(smem_u32(&slices[rank]), (uint32_t)tid);
+      st_cluster_f32(at, m);
+      st_cluster_f32(at + 4, s);
+      st_cluster_f32(at + 8, __int_as_float(nan));
+    }
+    cluster_arrive();
+    cluster_wait();
+    M = -INFINITY;
+    for (unsigned i = 0; i < C; ++i) {
+      M = fmaxf(M, slices[i].m);
+      nan |= slices[i].bad != 0;
+    }
+    S = 0.f;
+    for (unsigned i = 0; i < C; ++i)
+      if (slices[i].m > -INFINITY) S += slices[i].s * ex(slices[i].m - M);
+  }
+  const bool ok = !nan && M > -INFINITY && M < INFINITY && S > 0.f && S < INFINITY;
   if (!ok && tid == 0) raise_status(a.status, DELS_STATUS_NONFINITE);
-  const float inv = ok ? 1.f / s : NAN;
-  for (int v = tid; v < V; v += kStreamThreads) {
-    const float x = row.contracted(row.l_at(v), row.s_at(v), row.p_at(v));
-    put(out + v, ex2_approx((x - m) * a.in.scale) * inv);
+  // a slice of -inf alone has no reference: any finite one gives 0
+  const float ref = some ? m : 0.f, factor = !ok ? NAN : some ? ex(m - M) / S : 0.f;
+
+  O* out = static_cast<O*>(a.out) + (long long)r * a.ld_out - row.sh;     // by position
+  const int from = max(k0, row.sh);
+  if constexpr (HOLD) {
+    // fours that lie on a boundary of the output's
+    __syncthreads();
+    const int skew = (int)((reinterpret_cast<uintptr_t>(out + from) / sizeof(O)) & 3u), start = from - skew;
+    const bool whole = ((start - k0) & 3) == 0;
+    for (int k = start + tid * 4; k < k1; k += 4 * kStreamThreads) {
+      if (k >= from && k + 4 <= k1) {
+        float x[4];
+        held_get4(held, k - k0, whole, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = ex(x[i] - ref) * factor;
+        put4(out + k, x);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (k + i >= from && k + i < k1) put1(out + k + i, ex(held_get(held, k + i - k0) - ref) * factor);
+      }
+    }
+  } else {
+    each([&](float (&x)[8], int k) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int q = elem_pos<T, VEC>(k, i);
+        if (q >= from && q < k1) put1(out + q, ex(x[i] - ref) * factor);
+      }
+    });
   }
 }
 
 }  // namespace
 
-cudaError_t launch_row_probs(const ProbsArgs& a, bool f32, bool fused, bool vec, cudaStream_t s) {
+cudaError_t launch_row_probs(const ProbsArgs& args, bool f32, bool fused, bool vec, cudaStream_t s) {
+  const int sms = device_sm_count(), most = device_max_smem_optin() - 1024;
+  if (sms <= 0 || most <= 0) return cudaErrorInvalidValue;
+  ProbsArgs a = args;
+  const int held = fused || f32 ? 4 : 2;
+  // CTAs of a row: as few as leave five slices on an SM, so that one's loads run beside another's
+  // stores, more where the rows are few
+  const auto cols = [&](int c) { return (int)(((long long)a.in.V + 7 + c - 1) / c + 63) / 64 * 64; };
+  int c = 1;
+  while (c < kMaxCluster && ((long long)cols(c) * held > 40 * 1024 ||
+                             ((long long)a.in.rows * c < 2 * sms && cols(2 * c) >= 2 * kStreamStep)))
+    c *= 2;
+  a.in.cluster = c;
+  a.in.slice_cols = c == 1 ? (a.in.V + 7 + 7) / 8 * 8 : cols(c);
+  const long long bytes = (long long)a.in.slice_cols * held;
+  const bool hold = bytes <= most;
   return dispatch_rows(a.in, f32, fused, vec, [&](auto type, auto terms, auto v) {
     using T = typename decltype(type)::type;
     constexpr int F = decltype(terms)::value;
     constexpr bool VEC = decltype(v)::value;
-    return a.out_f32 ? launch_pdl(k_row_probs<T, F, VEC, float>, dim3(a.in.rows), dim3(kStreamThreads), 0, s, a)
-                     : launch_pdl(k_row_probs<T, F, VEC, uint16_t>, dim3(a.in.rows), dim3(kStreamThreads), 0, s, a);
+    const auto k = a.out_f32 ? (hold ? k_row_probs<T, F, VEC, float, true> : k_row_probs<T, F, VEC, float, false>)
+                             : (hold ? k_row_probs<T, F, VEC, __nv_bfloat16, true>
+                                     : k_row_probs<T, F, VEC, __nv_bfloat16, false>);
+    const size_t smem = hold ? (size_t)bytes : 0;
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), smem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl_cluster(k, dim3((unsigned)a.in.rows * (unsigned)c), dim3(kStreamThreads), smem, s, c, a);
   });
 }
 

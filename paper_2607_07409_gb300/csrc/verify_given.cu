@@ -1,113 +1,299 @@
-// Speculative sampling from given probabilities and uniforms. A CTA takes a request: its
-// first warp finds the tokens kept, then all threads sum the weights that the bonus token
-// is drawn from, each a run of columns, in float64; the thread whose run has the border
-// walks it.
+// Speculative sampling from given probabilities and uniforms.
+//
+// A cluster of 1 to 8 CTAs takes a request. The first warp of each finds the tokens kept, a
+// lane a position, so that their reads wait for one another no more than once; then the row that the
+// bonus token comes from is summed, once: a warp has a run of groups of 256 columns. The
+// warps' sums meet in shared memory, the CTAs' in each other's; the warp whose run has the border
+// reads that again, out of L2, and walks it.
+//
+// Sums decide which token comes out, so they are as good as float64's: float64 itself issues
+// at 1/64 of float32's rate here, so a lane keeps a float32 sum and what its additions
+// rounded off (Knuth's two-sum), 48 bits, and only its total is float64. A difference p - q is
+// kept the same way.
 #include "dels_device.cuh"
+#include "row_stream.cuh"
 
 namespace dels {
 namespace {
 
-constexpr int kGivenThreads = 256;
+constexpr int kGivenThreads = 512, kGivenWarps = kGivenThreads / 32;
+constexpr int kGroup = 256;                // columns of a warp's step, 8 a lane
 
-__device__ __forceinline__ float given_at(const GivenRows& g, long long i) {
-  return g.f32 ? __ldg(static_cast<const float*>(g.p) + i) : bf16_to_f(__ldg(static_cast<const uint16_t*>(g.p) + i));
-}
 __device__ __forceinline__ bool is_probability(float x) { return x >= 0.f && x < INFINITY; }
 
-// What request b keeps, and what its bonus token is drawn from.
 struct Kept {
-  int a;
-  int token;           // the rejected one, or -1: all were kept
+  int a;               // tokens kept
+  int token;           // the one rejected, or -1: all were kept
   int code;            // status bits
 };
-__device__ Kept count_kept(const VerifyGivenArgs& a, int b) {
+
+template <typename P, typename Q, bool DRAFT>
+__device__ __forceinline__ Kept count_kept(const VerifyGivenArgs& a, int b) {
+  const int lane = threadIdx.x & 31;
   Kept k{0, -1, 0};
-  const int len = a.lengths ? a.lengths[b] : a.n;
-  const float last = a.uniforms[(long long)b * (a.n + 1) + a.n];
+  const float* u = a.uniforms + (long long)b * (a.n + 1);
+  const int len = a.lengths ? __ldg(a.lengths + b) : a.n;
+  const float last = __ldg(u + a.n);
   if (len < 0 || len > a.n || !(last >= 0.f && last < 1.f)) {
     k.code = DELS_STATUS_BAD_VALUE;
     return k;
   }
-  for (; k.a < len; ++k.a) {
-    const int x = a.tokens[(long long)b * a.n + k.a];
-    const float u = a.uniforms[(long long)b * (a.n + 1) + k.a];
-    if (x < 0 || x >= a.V) k.code |= DELS_STATUS_BAD_TOKEN;
-    if (!(u >= 0.f && u < 1.f)) k.code |= DELS_STATUS_BAD_VALUE;
-    if (k.code) return k;
-    const float p = given_at(a.target, b * a.target.ld_b + k.a * a.target.ld + x);
-    const float q = a.draft.p ? given_at(a.draft, b * a.draft.ld_b + k.a * a.draft.ld + x) : 1.f;
-    if (!is_probability(p) || !is_probability(q)) k.code = DELS_STATUS_NONFINITE;
-    if (k.code) return k;
-    if (!((double)u * (double)q < (double)p)) {
-      k.token = x;
+  for (int j0 = 0; j0 < len; j0 += 32) {
+    const int j = j0 + lane;
+    int token = -1, code = 0;
+    bool stop = false;
+    if (j < len) {
+      token = __ldg(a.tokens + (long long)b * a.n + j);
+      const float uj = __ldg(u + j);
+      if (token < 0 || token >= a.V) code |= DELS_STATUS_BAD_TOKEN;
+      if (!(uj >= 0.f && uj < 1.f)) code |= DELS_STATUS_BAD_VALUE;
+      if (!code) {
+        const float p = row_elem(static_cast<const P*>(a.target.p), b * a.target.ld_b + j * a.target.ld + token);
+        const float q =
+            DRAFT ? row_elem(static_cast<const Q*>(a.draft.p), b * a.draft.ld_b + j * a.draft.ld + token) : 1.f;
+        if (!is_probability(p) || !is_probability(q)) code = DELS_STATUS_NONFINITE;
+        stop = !((double)uj * (double)q < (double)p);       // (both exact)
+      }
+      stop |= code != 0;
+    }
+    const unsigned who = __ballot_sync(0xFFFFFFFFu, stop);
+    if (who) {
+      const int first = __ffs(who) - 1;
+      k.a = j0 + first;
+      k.token = __shfl_sync(0xFFFFFFFFu, token, first);
+      k.code = __shfl_sync(0xFFFFFFFFu, code, first);
       return k;
     }
   }
+  k.a = len;
   return k;
 }
 
-__global__ void __launch_bounds__(kGivenThreads) k_verify_given(const VerifyGivenArgs a) {
-  __shared__ double sums[kGivenThreads];
+// 8 elements of a row for a lane: consecutive ones, or 32 apart where the rows lie anywhere
+// (0 past the row's end).
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, int v0, int V, float (&x)[8]) {
+  const int lane = threadIdx.x & 31;
+  if (VEC && v0 + kGroup <= V) {
+    const T* at = p + v0 + lane * 8;
+    Raw8<T> w;
+#pragma unroll
+    for (int k = 0; k < Raw8<T>::W; ++k) w.w[k] = __ldg(reinterpret_cast<const uint4*>(at + 4 * k));
+    w.unpack(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int v = VEC ? v0 + lane * 8 + i : v0 + i * 32 + lane;
+      x[i] = v < V ? row_elem(p, v) : 0.f;
+    }
+  }
+}
+
+struct Sum2 {
+  float hi, lo;
+  // Adds x >= 0, and y, far below it.
+  __device__ __forceinline__ void add(float x, float y) {
+    const float t = __fadd_rn(hi, x), b = __fsub_rn(t, hi);
+    const float e = __fadd_rn(__fsub_rn(hi, __fsub_rn(t, b)), __fsub_rn(x, b));
+    hi = t;
+    lo = __fadd_rn(lo, __fadd_rn(e, y));
+  }
+};
+// max(0, p - q) as a float32 and what it rounded off (p > q >= 0: both exact, Dekker's fast two-sum).
+__device__ __forceinline__ void rest_of(float p, float q, float& w, float& e) {
+  const float d = __fsub_rn(p, q);
+  w = fmaxf(d, 0.f);
+  e = d > 0.f ? __fsub_rn(__fsub_rn(p, d), q) : 0.f;
+}
+
+struct SlicePart {
+  double sum;
+  int bad, pad;
+};
+
+template <typename P, typename Q, bool DRAFT, bool VEC>
+__global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyGivenArgs a, int cluster) {
+  __shared__ double warp_sum[kGivenWarps];
+  __shared__ int warp_bad[kGivenWarps];
+  __shared__ SlicePart parts[2][kMaxCluster];
   __shared__ Kept kept;
-  __shared__ int bad;
-  const int tid = threadIdx.x, b = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int b = blockIdx.x / cluster, rank = blockIdx.x - b * cluster;
+  if (cluster > 1) cluster_arrive_relaxed();
   pdl_wait();
-  if (tid == 0) {
-    pdl_trigger();
-    kept = count_kept(a, b);
-    bad = 0;
+  if (tid == 0) pdl_trigger();
+  if (warp == 0) {
+    const Kept k = count_kept<P, Q, DRAFT>(a, b);
+    if (lane == 0) kept = k;
   }
   __syncthreads();
   const Kept k = kept;
-  const long long p0 = b * a.target.ld_b + k.a * a.target.ld, q0 = b * a.draft.ld_b + k.a * a.draft.ld;
-  const int run = (a.V + kGivenThreads - 1) / kGivenThreads;
-  const int v0 = min(a.V, tid * run), v1 = min(a.V, v0 + run);
-  bool rest = k.token >= 0;          // from max(0, p - q)
-  const auto weight = [&](int v) {
-    const double p = given_at(a.target, p0 + v);
-    if (!rest) return p;
-    if (!a.draft.p) return v == k.token ? 0.0 : p;
-    return fmax(0.0, p - (double)given_at(a.draft, q0 + v));
-  };
+  if (cluster > 1) cluster_wait();
   int bonus = -1, code = k.code;
-  if (!code) {
-    for (int v = v0; v < v1; ++v)
-      if (!is_probability(given_at(a.target, p0 + v)) ||
-          (rest && a.draft.p && !is_probability(given_at(a.draft, q0 + v))))
-        bad = 1;
-    for (int pass = 0; pass < 2; ++pass) {
-      double s = 0.0;
-      for (int v = v0; v < v1; ++v) s += weight(v);
-      __syncthreads();
-      sums[tid] = s;
-      __syncthreads();
-      double total = 0.0, before = 0.0;
-      for (int i = 0; i < kGivenThreads; ++i) {
-        if (i == tid) before = total;
-        total += sums[i];
+  bool mine = false;
+  if (!code) {                              // (the same in every CTA of the request)
+    const P* p = static_cast<const P*>(a.target.p) + b * a.target.ld_b + k.a * a.target.ld;
+    const Q* q = DRAFT ? static_cast<const Q*>(a.draft.p) + b * a.draft.ld_b + k.a * a.draft.ld : nullptr;
+    const int groups = (a.V + kGroup - 1) / kGroup, runs = cluster * kGivenWarps, run = rank * kGivenWarps + warp;
+    const int g0 = (int)((long long)groups * run / runs), g1 = (int)((long long)groups * (run + 1) / runs);
+    // The weights of a group: from max(0, p - q), or from p.
+    const auto weights = [&](bool rest, int g, const float (&x)[8], const float (&y)[8], float (&w)[8], float (&e)[8]) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = x[i];
+        e[i] = 0.f;
+        if (DRAFT && rest) rest_of(x[i], y[i], w[i], e[i]);
       }
-      if (bad || total > 0.0 || !rest) {
-        if (bad || !(total > 0.0)) {
-          code = DELS_STATUS_NONFINITE;
-          break;
+      if (!DRAFT && rest && (unsigned)(k.token - g * kGroup) < (unsigned)kGroup) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (g * kGroup + (VEC ? lane * 8 + i : i * 32 + lane) == k.token) w[i] = 0.f;
+      }
+    };
+    bool rest = k.token >= 0;
+    for (int pass = 0;; ++pass) {
+      Sum2 s{0.f, 0.f};
+      unsigned most = 0;                    // of the bits: what is no probability is above infinity's, or it
+      const auto add = [&](int g, const float (&x)[8], const float (&y)[8]) {
+        float w[8], e[8];
+        weights(rest, g, x, y, w, e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          most = max(most, __float_as_uint(x[i] + 0.f));
+          if (DRAFT && rest) most = max(most, __float_as_uint(y[i] + 0.f));
+          s.add(w[i], e[i]);
         }
-        const double at = (double)a.uniforms[(long long)b * (a.n + 1) + a.n] * total;
-        if (before <= at && before + s > at) {
-          double c = before;
-          for (int v = v0; v < v1; ++v) {
-            const double w = weight(v);
-            c += w;
-            if (w > 0.0) bonus = v;
-            if (c > at) break;
-          }
-          a.out_bonus[b] = bonus;
+      };
+      int g = g0;
+      for (; g + 1 < g1; g += 2) {
+        float x[2][8], y[2][8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          load8<P, VEC>(p, (g + i) * kGroup, a.V, x[i]);
+          if (DRAFT && rest) load8<Q, VEC>(q, (g + i) * kGroup, a.V, y[i]);
         }
+        add(g, x[0], y[0]);
+        add(g + 1, x[1], y[1]);
+      }
+      if (g < g1) {
+        float x[8], y[8];
+        load8<P, VEC>(p, g * kGroup, a.V, x);
+        if (DRAFT && rest) load8<Q, VEC>(q, g * kGroup, a.V, y);
+        add(g, x, y);
+      }
+      double t = (double)s.hi + (double)s.lo;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
+      const int bad = __any_sync(0xFFFFFFFFu, most >= 0x7F800000u);
+      if (lane == 0) {
+        warp_sum[warp] = t;
+        warp_bad[warp] = bad;
+      }
+      __syncthreads();
+      // Every sum from here on in the columns' order, the same in every thread.
+      double own = 0.0;
+      int own_bad = 0;
+      for (int i = 0; i < kGivenWarps; ++i) {
+        own += warp_sum[i];
+        own_bad |= warp_bad[i];
+      }
+      SlicePart* part = parts[pass];
+      if (cluster > 1) {
+        if (tid < cluster) {
+          const uint32_t at = cluster_map(smem_u32(&part[rank]), (uint32_t)tid);
+          const long long bits = __double_as_longlong(own);
+          st_cluster_f32(at, __int_as_float((int)(bits & 0xFFFFFFFFll)));
+          st_cluster_f32(at + 4, __int_as_float((int)(bits >> 32)));
+          st_cluster_f32(at + 8, __int_as_float(own_bad));
+        }
+        cluster_arrive();
+        cluster_wait();
+      } else {
+        if (tid == 0) part[0] = SlicePart{own, own_bad, 0};
+        __syncthreads();
+      }
+      double total = 0.0, before = 0.0;
+      int any_bad = 0;
+      for (int i = 0; i < cluster; ++i) {
+        if (i == rank) before = total;
+        total += part[i].sum;
+        any_bad |= part[i].bad;
+      }
+      if (any_bad || !(total < INFINITY) || (!(total > 0.0) && !rest)) {
+        code = DELS_STATUS_NONFINITE;
         break;
       }
-      rest = false;
+      if (!(total > 0.0)) {                 // nothing left of p - q: from p
+        rest = false;
+        __syncthreads();                    // (the warps' sums are written again)
+        continue;
+      }
+      const double at = (double)__ldg(a.uniforms + (long long)b * (a.n + 1) + a.n) * total;
+      if (before <= at && before + own > at) {
+        // The run with the border: the first whose sums exceed it, or by roundings none: the last with weight.
+        int r = -1, last = 0;
+        double c = before, c0 = before;
+        for (int i = 0; i < kGivenWarps; ++i) {
+          if (warp_sum[i] > 0.0) last = i;
+          if (r < 0 && c + warp_sum[i] > at) {
+            r = i;
+            c0 = c;
+          }
+          c += warp_sum[i];
+        }
+        if (r < 0) {
+          r = last;
+          c0 = c - warp_sum[last];
+        }
+        if (warp == r) {
+          mine = true;
+          for (int g2 = g0; g2 < g1; ++g2) {
+            float x[8], y[8], w[8], e[8];
+            load8<P, VEC>(p, g2 * kGroup, a.V, x);
+            if (DRAFT && rest) load8<Q, VEC>(q, g2 * kGroup, a.V, y);
+            weights(rest, g2, x, y, w, e);
+            bool found = false;
+            // VEC: the lanes in order, each its 8; else 8 times the lanes in order
+            constexpr int kParts = VEC ? 1 : 8, kEach = 8 / kParts;
+#pragma unroll
+            for (int h = 0; h < kParts; ++h) {
+              if (found) continue;
+              double t2 = 0.0;
+#pragma unroll
+              for (int i = 0; i < kEach; ++i) t2 += (double)w[h * kEach + i] + (double)e[h * kEach + i];
+              double incl = t2;
+#pragma unroll
+              for (int d = 1; d < 32; d <<= 1) {
+                const double up = __shfl_up_sync(0xFFFFFFFFu, incl, d);
+                if (lane >= d) incl += up;
+              }
+              const unsigned over = __ballot_sync(0xFFFFFFFFu, c0 + incl > at);
+              const unsigned some = __ballot_sync(0xFFFFFFFFu, t2 > 0.0);
+              const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
+              if (who >= 0) {               // the border, or for now the last with weight
+                int v = -1;
+                double c2 = c0 + (incl - t2);
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                  const double w2 = (double)w[h * kEach + i] + (double)e[h * kEach + i];
+                  const bool past = c2 > at && v >= 0;
+                  c2 += w2;
+                  if (!past && w2 > 0.0) v = g2 * kGroup + (VEC ? lane * 8 + i : h * 32 + lane);
+                }
+                bonus = __shfl_sync(0xFFFFFFFFu, v, who);
+              }
+              found = over != 0;
+              c0 += __shfl_sync(0xFFFFFFFFu, incl, 31);
+            }
+            if (found) break;
+          }
+        }
+      }
+      break;
     }
   }
-  if (tid == 0) {
+  if (mine && lane == 0) a.out_bonus[b] = bonus;
+  if (rank == 0 && tid == 0) {
     a.out_accept[b] = k.a;
     if (code) {
       a.out_bonus[b] = -1;
@@ -116,10 +302,33 @@ __global__ void __launch_bounds__(kGivenThreads) k_verify_given(const VerifyGive
   }
 }
 
+template <typename P, typename Q, bool DRAFT>
+cudaError_t launch_types(const VerifyGivenArgs& a, bool vec, int cluster, cudaStream_t s) {
+  const auto k = vec ? k_verify_given<P, Q, DRAFT, true> : k_verify_given<P, Q, DRAFT, false>;
+  return launch_pdl_cluster(k, dim3((unsigned)a.B * (unsigned)cluster), dim3(kGivenThreads), 0, s, cluster, a, cluster);
+}
+
+// All rows start on 16-byte boundaries.
+bool rows_aligned(const GivenRows& g) {
+  const int es = g.f32 ? 4 : 2;
+  return (reinterpret_cast<uintptr_t>(g.p) & 15u) == 0 && g.ld * es % 16 == 0 && g.ld_b * es % 16 == 0;
+}
+
 }  // namespace
 
 cudaError_t launch_verify_given(const VerifyGivenArgs& a, cudaStream_t s) {
-  return launch_pdl(k_verify_given, dim3(a.B), dim3(kGivenThreads), 0, s, a);
+  const int sms = device_sm_count();
+  if (sms <= 0) return cudaErrorInvalidValue;
+  // as many CTAs a request as two an SM hold, at a warp's group each or nearly
+  int c = 1;
+  while (c < kMaxCluster && (long long)a.B * 2 * c <= 2 * sms && a.V >= 2 * c * 8 * kGroup) c *= 2;
+  const bool vec = rows_aligned(a.target) && (!a.draft.p || rows_aligned(a.draft));
+  const auto with_draft = [&](auto p) {
+    using P = typename decltype(p)::type;
+    if (!a.draft.p) return launch_types<P, P, false>(a, vec, c, s);
+    return a.draft.f32 ? launch_types<P, float, true>(a, vec, c, s) : launch_types<P, uint16_t, true>(a, vec, c, s);
+  };
+  return a.target.f32 ? with_draft(TypeOf<float>{}) : with_draft(TypeOf<uint16_t>{});
 }
 
 }  // namespace dels

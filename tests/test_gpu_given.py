@@ -92,7 +92,7 @@ def check(c, T=1.0, out=F32, **kw):
 @pytest.mark.parametrize("fused", [False, True])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,V", [(1, 1), (3, 2), (2, 7), (5, 255), (4, 1024), (3, 4099), (7, 32003), (300, 2050),
-                                    (2, 50257), (3, 151936)])
+                                    (2, 50257), (3, 151936), (2, 470001), (1, 1000003)])
 def test_probs(rows, V, dtype, fused):
     for T, out in [(1.0, F32), (0.7, BF16)]:
         check(Rows(rows, V, dtype, rows + V, fused, n=min(rows, 3)), T, out)
