@@ -18,16 +18,18 @@ namespace dels {
 namespace {
 
 // 2^(d c) for d <= 0, c = log2(e) / T given as a sum c + c_lo: d c is split into a whole
-// number and the rest, which an fma has exactly but for c's own rounding; the second fma puts
+// number n and the rest, which an fma has exactly but for c's own rounding; the second fma puts
 // that right. (z = d c rounded, and c too, took up to 40 2^-24 of a value 20 below the
-// largest.) Below 2^-126: 0.
+// largest.) n comes from an addition that leaves it in a float's low bits: conversions issue
+// at an eighth of its rate, as the exponential does. Below 2^-126: 0.
 struct Exponent {
-  float c, c_lo, least;      // least: what d is not let below, 300 / c
+  float c, c_lo, least;      // least: what d is not let below, -300 / c
   __device__ __forceinline__ float operator()(float d) const {
+    constexpr float kWhole = 12582912.f;                  // 1.5 2^23
     d = fmaxf(d, least);
-    const float n = fmaxf(rintf(d * c), -127.f);
+    const float t = fmaxf(fmaf(d, c, kWhole), kWhole - 126.f), n = t - kWhole;
     const float f = fmaf(d, c_lo, fmaf(d, c, -n));
-    return ex2_approx(f) * __int_as_float(((int)n + 127) << 23);
+    return ex2_approx(f) * __int_as_float((__float_as_int(t) << 23) + 0x3F800000);
   }
 };
 
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a)
   };
   // f(values, first position) of every item of the thread
   const auto each = [&](auto&& f) {
-    constexpr int U = 2;
+    constexpr int U = 4;
     for (int it = 0; it < items; it += U) {
       Item<T, F, VEC> v[U];
       float pr[U][8], x[8], sv[8];

@@ -8,8 +8,8 @@
 //
 // Sums decide which token comes out, so they are as good as float64's: float64 itself issues
 // at 1/64 of float32's rate here, so a lane keeps a float32 sum and what its additions
-// rounded off (Knuth's two-sum), 48 bits, and only its total is float64. A difference p - q is
-// kept the same way.
+// rounded off (Knuth's two-sum), 48 bits, and only totals are float64, in one warp. A
+// difference p - q is kept the same way.
 #include "dels_device.cuh"
 #include "row_stream.cuh"
 
@@ -106,16 +106,45 @@ __device__ __forceinline__ void rest_of(float p, float q, float& w, float& e) {
   e = d > 0.f ? __fsub_rn(__fsub_rn(p, d), q) : 0.f;
 }
 
+// A warp's sum, in every lane (fixed order).
+__device__ __forceinline__ Sum2 warp_sum2(Sum2 s) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    const float hi = __shfl_xor_sync(0xFFFFFFFFu, s.hi, d), lo = __shfl_xor_sync(0xFFFFFFFFu, s.lo, d);
+    s.add(hi, lo);
+  }
+  return s;
+}
+__device__ __forceinline__ double total_of(const Sum2& s) { return (double)s.hi + (double)s.lo; }
+// Sums up to and including each lane's.
+__device__ __forceinline__ double warp_scan(double x, int lanes) {
+  const int lane = threadIdx.x & 31;
+  for (int d = 1; d < lanes; d <<= 1) {
+    const double up = __shfl_up_sync(0xFFFFFFFFu, x, d);
+    if (lane >= d) x += up;
+  }
+  return x;
+}
+
 struct SlicePart {
   double sum;
   int bad, pad;
 };
+// What the first warp of a CTA finds from the sums.
+struct Border {
+  double at;           // u times the whole
+  double before;       // the sum up to the run
+  int run;             // the warp whose columns have the border, or -1
+  int again;           // nothing is left of p - q
+  int code;
+};
 
 template <typename P, typename Q, bool DRAFT, bool VEC>
 __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyGivenArgs a, int cluster) {
-  __shared__ double warp_sum[kGivenWarps];
+  __shared__ Sum2 warp_sum[kGivenWarps];
   __shared__ int warp_bad[kGivenWarps];
   __shared__ SlicePart parts[2][kMaxCluster];
+  __shared__ Border border;
   __shared__ Kept kept;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b = blockIdx.x / cluster, rank = blockIdx.x - b * cluster;
@@ -181,112 +210,129 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
         if (DRAFT && rest) load8<Q, VEC>(q, g * kGroup, a.V, y);
         add(g, x, y);
       }
-      double t = (double)s.hi + (double)s.lo;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
+      s = warp_sum2(s);
       const int bad = __any_sync(0xFFFFFFFFu, most >= 0x7F800000u);
       if (lane == 0) {
-        warp_sum[warp] = t;
+        warp_sum[warp] = s;
         warp_bad[warp] = bad;
       }
       __syncthreads();
-      // Every sum from here on in the columns' order, the same in every thread.
+      // float64 from here on, by the first warp: every warp's instruction takes 16 cycles of the SM's
       double own = 0.0;
-      int own_bad = 0;
-      for (int i = 0; i < kGivenWarps; ++i) {
-        own += warp_sum[i];
-        own_bad |= warp_bad[i];
-      }
-      SlicePart* part = parts[pass];
-      if (cluster > 1) {
-        if (tid < cluster) {
-          const uint32_t at = cluster_map(smem_u32(&part[rank]), (uint32_t)tid);
-          const long long bits = __double_as_longlong(own);
-          st_cluster_f32(at, __int_as_float((int)(bits & 0xFFFFFFFFll)));
-          st_cluster_f32(at + 4, __int_as_float((int)(bits >> 32)));
-          st_cluster_f32(at + 8, __int_as_float(own_bad));
+      if (warp == 0) {
+        own = warp_scan(lane < kGivenWarps ? total_of(warp_sum[lane]) : 0.0, kGivenWarps);
+        const int own_bad = __any_sync(0xFFFFFFFFu, lane < kGivenWarps && warp_bad[lane]);
+        const double sum = __shfl_sync(0xFFFFFFFFu, own, kGivenWarps - 1);
+        if (cluster > 1) {
+          if (lane < cluster) {
+            const uint32_t at = cluster_map(smem_u32(&parts[pass][rank]), (uint32_t)lane);
+            const long long bits = __double_as_longlong(sum);
+            st_cluster_f32(at, __int_as_float((int)(bits & 0xFFFFFFFFll)));
+            st_cluster_f32(at + 4, __int_as_float((int)(bits >> 32)));
+            st_cluster_f32(at + 8, __int_as_float(own_bad));
+          }
+        } else if (lane == 0) {
+          parts[pass][0] = SlicePart{sum, own_bad, 0};
         }
+        __syncwarp();
+      }
+      if (cluster > 1) {
         cluster_arrive();
         cluster_wait();
-      } else {
-        if (tid == 0) part[0] = SlicePart{own, own_bad, 0};
-        __syncthreads();
       }
-      double total = 0.0, before = 0.0;
-      int any_bad = 0;
-      for (int i = 0; i < cluster; ++i) {
-        if (i == rank) before = total;
-        total += part[i].sum;
-        any_bad |= part[i].bad;
+      if (warp == 0) {
+        // (every CTA of the request has the same parts, takes the same steps and finds the same one)
+        const SlicePart part = lane < cluster ? parts[pass][lane] : SlicePart{0.0, 0, 0};
+        const double upto = warp_scan(part.sum, kMaxCluster);
+        const double total = __shfl_sync(0xFFFFFFFFu, upto, kMaxCluster - 1);
+        const bool any_bad = __any_sync(0xFFFFFFFFu, part.bad != 0) || !(total < INFINITY);
+        Border f{(double)__ldg(a.uniforms + (long long)b * (a.n + 1) + a.n) * total, 0.0, -1, 0, 0};
+        if (any_bad || (!(total > 0.0) && !rest)) f.code = DELS_STATUS_NONFINITE;
+        else if (!(total > 0.0)) f.again = 1;
+        else if (__ffs(__ballot_sync(0xFFFFFFFFu, upto > f.at)) - 1 == rank) {
+          const double before = __shfl_sync(0xFFFFFFFFu, upto, max(rank - 1, 0));
+          const double c = (rank ? before : 0.0) + own;            // up to and including the lane's run
+          const unsigned over = __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && c > f.at);
+          const unsigned some =
+              __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && warp_sum[lane & (kGivenWarps - 1)].hi > 0.f);
+          // (by roundings none may exceed it: then the last with weight)
+          f.run = over ? __ffs(over) - 1 : 31 - __clz(some);
+          const double prev = __shfl_sync(0xFFFFFFFFu, c, max(f.run - 1, 0));
+          f.before = f.run ? prev : (rank ? before : 0.0);
+        }
+        if (lane == 0) border = f;
       }
-      if (any_bad || !(total < INFINITY) || (!(total > 0.0) && !rest)) {
-        code = DELS_STATUS_NONFINITE;
-        break;
-      }
-      if (!(total > 0.0)) {                 // nothing left of p - q: from p
+      __syncthreads();
+      const Border f = border;
+      if (f.again) {
         rest = false;
-        __syncthreads();                    // (the warps' sums are written again)
+        __syncthreads();                    // (the sums are written again)
         continue;
       }
-      const double at = (double)__ldg(a.uniforms + (long long)b * (a.n + 1) + a.n) * total;
-      if (before <= at && before + own > at) {
-        // The run with the border: the first whose sums exceed it, or by roundings none: the last with weight.
-        int r = -1, last = 0;
-        double c = before, c0 = before;
-        for (int i = 0; i < kGivenWarps; ++i) {
-          if (warp_sum[i] > 0.0) last = i;
-          if (r < 0 && c + warp_sum[i] > at) {
-            r = i;
-            c0 = c;
+      code = f.code;
+      if (warp == f.run) {
+        mine = true;
+        // The first group whose sums exceed it, or by roundings none: the last with weight.
+        double c0 = f.before, base = c0;
+        int at = g0;
+        for (int g2 = g0; g2 < g1; g2 += 2) {
+          float x[2][8], y[2][8];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            load8<P, VEC>(p, (g2 + i) * kGroup, g2 + i < g1 ? a.V : 0, x[i]);
+            if (DRAFT && rest) load8<Q, VEC>(q, (g2 + i) * kGroup, g2 + i < g1 ? a.V : 0, y[i]);
           }
-          c += warp_sum[i];
-        }
-        if (r < 0) {
-          r = last;
-          c0 = c - warp_sum[last];
-        }
-        if (warp == r) {
-          mine = true;
-          for (int g2 = g0; g2 < g1; ++g2) {
-            float x[8], y[8], w[8], e[8];
-            load8<P, VEC>(p, g2 * kGroup, a.V, x);
-            if (DRAFT && rest) load8<Q, VEC>(q, g2 * kGroup, a.V, y);
-            weights(rest, g2, x, y, w, e);
-            bool found = false;
-            // VEC: the lanes in order, each its 8; else 8 times the lanes in order
-            constexpr int kParts = VEC ? 1 : 8, kEach = 8 / kParts;
+          bool over = false;
 #pragma unroll
-            for (int h = 0; h < kParts; ++h) {
-              if (found) continue;
-              double t2 = 0.0;
+          for (int i = 0; i < 2; ++i) {
+            if (over) continue;
+            float w[8], e[8];
+            weights(rest, g2 + i, x[i], y[i], w, e);
+            Sum2 t{0.f, 0.f};
 #pragma unroll
-              for (int i = 0; i < kEach; ++i) t2 += (double)w[h * kEach + i] + (double)e[h * kEach + i];
-              double incl = t2;
-#pragma unroll
-              for (int d = 1; d < 32; d <<= 1) {
-                const double up = __shfl_up_sync(0xFFFFFFFFu, incl, d);
-                if (lane >= d) incl += up;
-              }
-              const unsigned over = __ballot_sync(0xFFFFFFFFu, c0 + incl > at);
-              const unsigned some = __ballot_sync(0xFFFFFFFFu, t2 > 0.0);
-              const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
-              if (who >= 0) {               // the border, or for now the last with weight
-                int v = -1;
-                double c2 = c0 + (incl - t2);
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                  const double w2 = (double)w[h * kEach + i] + (double)e[h * kEach + i];
-                  const bool past = c2 > at && v >= 0;
-                  c2 += w2;
-                  if (!past && w2 > 0.0) v = g2 * kGroup + (VEC ? lane * 8 + i : h * 32 + lane);
-                }
-                bonus = __shfl_sync(0xFFFFFFFFu, v, who);
-              }
-              found = over != 0;
-              c0 += __shfl_sync(0xFFFFFFFFu, incl, 31);
+            for (int j = 0; j < 8; ++j) t.add(w[j], e[j]);
+            t = warp_sum2(t);
+            const double upto = __shfl_sync(0xFFFFFFFFu, c0 + total_of(t), 0);
+            if (t.hi > 0.f) {
+              at = g2 + i;
+              base = c0;
+              over = upto > f.at;
             }
-            if (found) break;
+            c0 = upto;
           }
+          if (over) break;
+        }
+        float x[8], y[8], w[8], e[8];
+        load8<P, VEC>(p, at * kGroup, a.V, x);
+        if (DRAFT && rest) load8<Q, VEC>(q, at * kGroup, a.V, y);
+        weights(rest, at, x, y, w, e);
+        // VEC: the lanes in order, each its 8; else 8 times the lanes in order
+        constexpr int kParts = VEC ? 1 : 8, kEach = 8 / kParts;
+        bool found = false;
+#pragma unroll
+        for (int h = 0; h < kParts; ++h) {
+          if (found) continue;
+          double t = 0.0;
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) t += (double)w[h * kEach + i] + (double)e[h * kEach + i];
+          const double incl = warp_scan(t, 32);
+          const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > f.at);
+          const unsigned some = __ballot_sync(0xFFFFFFFFu, t > 0.0);
+          const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
+          if (who >= 0) {                 // the border, or for now the last with weight
+            int v = -1;
+            double c2 = base + (incl - t);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+              const double w2 = (double)w[h * kEach + i] + (double)e[h * kEach + i];
+              const bool past = c2 > f.at && v >= 0;
+              c2 += w2;
+              if (!past && w2 > 0.0) v = at * kGroup + (VEC ? lane * 8 + i : h * 32 + lane);
+            }
+            bonus = __shfl_sync(0xFFFFFFFFu, v, who);
+          }
+          found = over != 0;
+          base += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
       }
       break;
