@@ -29,7 +29,7 @@ int device_max_smem_optin() {
   return v;
 }
 
-cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes) {
+cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes, bool most_shared) {
   struct Entry {
     const void* kernel;
     int dev;
@@ -49,6 +49,8 @@ cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes) {
     return e;
   }
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess && most_shared)
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
   if (e == cudaSuccess) done.push_back(Entry{kernel, dev, bytes});
   return e;
 }
@@ -2403,8 +2405,9 @@ int dels_row_probs(const dels_rows* x, int rows, int V, void* out, dels_dtype ou
   a.out = out;
   a.out_f32 = out_dtype == DELS_F32;
   a.ld_out = ld;
-  a.scale_lo = (float)(1.4426950408889634 / (double)x->temperature - (double)call.in.scale);
-  a.least = (float)std::max(-3e38, -300.0 / (double)call.in.scale);
+  const double scale = 1.4426950408889634 / (double)x->temperature;
+  if ((double)a.in.scale >= scale) a.in.scale = std::nextafter(a.in.scale, 0.f);
+  a.scale_lo = std::max((float)(scale - (double)a.in.scale), 1e-37f);
   a.status = at<int>(workspace, 0);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_PROBS);

@@ -202,8 +202,7 @@ struct ProbsArgs {
   void* out;                     // [rows, V]
   int out_f32;
   long long ld_out;              // elements
-  float scale_lo;                // what in.scale leaves of log2(e) / T
-  float least;                   // distance from the largest at which a value counts no more
+  float scale_lo;                // what in.scale, rounded down here, leaves of log2(e) / T; above 0
   int* status;
 };
 cudaError_t launch_row_probs(const ProbsArgs& a, bool f32, bool fused, bool vec, cudaStream_t s);
@@ -583,7 +582,9 @@ int device_max_smem_optin();
 // Raises `kernel`'s dynamic shared-memory limit on the current device to at
 // least `bytes`, once per kernel, device and size (safe from several host
 // threads; the attribute is per device).
-cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes);
+// most_shared: the SM's memory all as shared memory (left to itself, the driver kept a
+// part of it for L1 that another CTA would have fitted in).
+cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes, bool most_shared = false);
 // G = E W^T: E [V, D] and W [O, D] bf16, G [V, O] float32, all row-major and
 // 16-byte aligned, D and O multiples of 16.
 cudaError_t launch_input_table(const uint16_t* E, const uint16_t* W, float* G, int V, int O, int D, int* status,

@@ -17,25 +17,36 @@
 namespace dels {
 namespace {
 
-// 2^(d c) for d <= 0, c = log2(e) / T given as a sum c + c_lo: d c is split into a whole
+// 2^(d c), d = x - m <= 0 (or NaN), c + c_lo = log2(e) / T, c_lo > 0: d c is split into a whole
 // number n and the rest, which an fma has exactly but for c's own rounding; the second fma puts
 // that right. (z = d c rounded, and c too, took up to 40 2^-24 of a value 20 below the
 // largest.) n comes from an addition that leaves it in a float's low bits: conversions issue
-// at an eighth of its rate, as the exponential does. Below 2^-126: 0.
+// at an eighth of its rate, as the exponential does. Below 2^-126: 0, as for d = -inf (c_lo > 0
+// keeps that from being NaN, which stays NaN). In pairs: two roundings an instruction.
 struct Exponent {
-  float c, c_lo, least;      // least: what d is not let below, -300 / c
-  __device__ __forceinline__ float operator()(float d) const {
+  float m, c, c_lo;
+  __device__ __forceinline__ f32x2 two(f32x2 x) const {
     constexpr float kWhole = 12582912.f;                  // 1.5 2^23
-    d = fmaxf(d, least);
-    const float t = fmaxf(fmaf(d, c, kWhole), kWhole - 126.f), n = t - kWhole;
-    const float f = fmaf(d, c_lo, fmaf(d, c, -n));
-    return ex2_approx(f) * __int_as_float((__float_as_int(t) << 23) + 0x3F800000);
+    const f32x2 d = add2(x, both2(-m)), c2 = both2(c);
+    float t0, t1, f0, f1;
+    split2(fma2(d, c2, both2(kWhole)), t0, t1);
+    t0 = fmaxf(t0, kWhole - 126.f);
+    t1 = fmaxf(t1, kWhole - 126.f);
+    const f32x2 minus_n = add2(both2(kWhole), pair2(-t0, -t1));
+    split2(fma2(d, both2(c_lo), fma2(d, c2, minus_n)), f0, f1);
+    const f32x2 power = pair2(__int_as_float((__float_as_int(t0) << 23) + 0x3F800000),
+                              __int_as_float((__float_as_int(t1) << 23) + 0x3F800000));
+    return mul2(pair2(ex2_approx(f0), ex2_approx(f1)), power);
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    float a, b;
+    split2(two(both2(x)), a, b);
+    return a;
   }
 };
 
 struct SliceSum {
   float m, s;
-  int bad;
 };
 
 __device__ __forceinline__ void held_put(float* h, int i, float x) { h[i] = x; }
@@ -73,7 +84,7 @@ __device__ __forceinline__ void put1(float* out, float x) { *out = x; }
 __device__ __forceinline__ void put1(__nv_bfloat16* out, float x) { *out = __float2bfloat16_rn(x); }
 
 template <typename T, int F, bool VEC, typename O, bool HOLD>
-__global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, F == kPlain ? 5 : 3) k_row_probs(const ProbsArgs a) {
   using H = std::conditional_t<F == kPlain, T, float>;
   extern __shared__ __align__(16) uint8_t smem[];
   H* held = reinterpret_cast<H*>(smem);
@@ -96,7 +107,7 @@ __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a)
   };
   // f(values, first position) of every item of the thread
   const auto each = [&](auto&& f) {
-    constexpr int U = 4;
+    constexpr int U = F == kPlain ? 4 : 2;
     for (int it = 0; it < items; it += U) {
       Item<T, F, VEC> v[U];
       float pr[U][8], x[8], sv[8];
@@ -110,11 +121,8 @@ __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a)
     }
   };
 
-  float m = -INFINITY;
-  bool nan = false;
+  float m = -INFINITY;                      // (NaN shows in the sums)
   each([&](float (&x)[8], int k) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) nan |= x[i] != x[i];
     m = fmaxf(m, max8(x));
     if constexpr (HOLD) {
       if (VEC && k + kHalf<T> + 4 <= k1) {
@@ -138,47 +146,42 @@ __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a)
     }
   });
   m = warp_max(m);
-  nan = __any_sync(0xFFFFFFFFu, nan);
-  if (lane == 0) red[warp] = nan ? NAN : m;
+  if (lane == 0) red[warp] = m;
   __syncthreads();
-  nan = false;
 #pragma unroll
-  for (int i = 0; i < kStreamWarps; ++i) {
-    nan |= red[i] != red[i];
-    m = fmaxf(m, red[i]);
-  }
-  const Exponent ex{a.in.scale, a.scale_lo, a.least};
-  float s = 0.f;
-  const bool some = m > -INFINITY && m < INFINITY;
-  if (some) {
-    const auto add = [&](float (&x)[8]) {
-      float e[8];
+  for (int i = 0; i < kStreamWarps; ++i) m = fmaxf(m, red[i]);
+  // A slice of -inf alone has no reference: any finite one gives 0, and shows a NaN in it.
+  const bool some = m > -INFINITY;
+  const float ref = some ? m : 0.f;
+  const Exponent ex{ref, a.in.scale, a.scale_lo};
+  f32x2 s2 = 0ull;
+  const auto add = [&](const float (&x)[8]) {
+    s2 = add2(s2, add2(add2(ex.two(pair2(x[0], x[1])), ex.two(pair2(x[2], x[3]))),
+                       add2(ex.two(pair2(x[4], x[5])), ex.two(pair2(x[6], x[7])))));
+  };
+  if constexpr (HOLD) {
+    const int n = k1 - k0;
+    constexpr int kApart = sizeof(H) == 4 ? 4 * kStreamThreads : 4;      // an item's fours, as in RowStream
+    for (int i = tid * (sizeof(H) == 4 ? 4 : 8); i < n; i += kStreamStep) {
+      float x[8], lo[4], hi[4];
+      if (i + kApart + 4 <= n) {
+        held_get4(held, i, true, lo);
+        held_get4(held, i + kApart, true, hi);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = ex(x[i] - m);
-      s += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-    };
-    if constexpr (HOLD) {
-      const int n = k1 - k0;                 // (in fours; the ragged last one by its elements)
-      for (int i = tid * 8; i < n; i += kStreamStep) {
-        float lo[4], hi[4], x[8];
-        if (i + 8 <= n) {
-          held_get4(held, i, true, lo);
-          held_get4(held, i + 4, true, hi);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            lo[j] = i + j < n ? held_get(held, i + j) : -INFINITY;
-            hi[j] = i + 4 + j < n ? held_get(held, i + 4 + j) : -INFINITY;
-          }
+        for (int j = 0; j < 4; ++j) {
+          lo[j] = i + j < n ? held_get(held, i + j) : -INFINITY;
+          hi[j] = i + kApart + j < n ? held_get(held, i + kApart + j) : -INFINITY;
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = lo[j], x[4 + j] = hi[j];
-        add(x);
       }
-    } else {
-      each([&](float (&x)[8], int) { add(x); });
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = lo[j], x[4 + j] = hi[j];
+      add(x);
     }
+  } else {
+    each([&](float (&x)[8], int) { add(x); });
   }
+  float s = sum2(s2);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
   if (lane == 0) red_s[warp] = s;
@@ -194,23 +197,20 @@ __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a)
       const uint32_t at = cluster_map(smem_u32(&slices[rank]), (uint32_t)tid);
       st_cluster_f32(at, m);
       st_cluster_f32(at + 4, s);
-      st_cluster_f32(at + 8, __int_as_float(nan));
     }
     cluster_arrive();
     cluster_wait();
     M = -INFINITY;
-    for (unsigned i = 0; i < C; ++i) {
-      M = fmaxf(M, slices[i].m);
-      nan |= slices[i].bad != 0;
-    }
+    for (unsigned i = 0; i < C; ++i) M = fmaxf(M, slices[i].m);
+    const Exponent to{M, a.in.scale, a.scale_lo};
     S = 0.f;
-    for (unsigned i = 0; i < C; ++i)
-      if (slices[i].m > -INFINITY) S += slices[i].s * ex(slices[i].m - M);
+    for (unsigned i = 0; i < C; ++i) S += slices[i].m > -INFINITY ? slices[i].s * to(slices[i].m) : slices[i].s;
   }
-  const bool ok = !nan && M > -INFINITY && M < INFINITY && S > 0.f && S < INFINITY;
+  const bool ok = M > -INFINITY && M < INFINITY && S > 0.f && S < INFINITY;
   if (!ok && tid == 0) raise_status(a.status, DELS_STATUS_NONFINITE);
-  // a slice of -inf alone has no reference: any finite one gives 0
-  const float ref = some ? m : 0.f, factor = !ok ? NAN : some ? ex(m - M) / S : 0.f;
+  const Exponent to{M, a.in.scale, a.scale_lo};
+  const float factor = !ok ? NAN : some ? to(m) / S : 0.f;
+  const f32x2 factor2 = both2(factor);
 
   O* out = static_cast<O*>(a.out) + (long long)r * a.ld_out - row.sh;     // by position
   const int from = max(k0, row.sh);
@@ -223,13 +223,13 @@ __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a)
       if (k >= from && k + 4 <= k1) {
         float x[4];
         held_get4(held, k - k0, whole, x);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = ex(x[i] - ref) * factor;
+        split2(mul2(ex.two(pair2(x[0], x[1])), factor2), x[0], x[1]);
+        split2(mul2(ex.two(pair2(x[2], x[3])), factor2), x[2], x[3]);
         put4(out + k, x);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (k + i >= from && k + i < k1) put1(out + k + i, ex(held_get(held, k + i - k0) - ref) * factor);
+          if (k + i >= from && k + i < k1) put1(out + k + i, ex(held_get(held, k + i - k0)) * factor);
       }
     }
   } else {
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kStreamThreads) k_row_probs(const ProbsArgs a)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int q = elem_pos<T, VEC>(k, i);
-        if (q >= from && q < k1) put1(out + q, ex(x[i] - ref) * factor);
+        if (q >= from && q < k1) put1(out + q, ex(x[i]) * factor);
       }
     });
   }
@@ -269,7 +269,7 @@ cudaError_t launch_row_probs(const ProbsArgs& args, bool f32, bool fused, bool v
                              : (hold ? k_row_probs<T, F, VEC, __nv_bfloat16, true>
                                      : k_row_probs<T, F, VEC, __nv_bfloat16, false>);
     const size_t smem = hold ? (size_t)bytes : 0;
-    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), smem);
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), smem, true);
     if (e != cudaSuccess) return e;
     return launch_pdl_cluster(k, dim3((unsigned)a.in.rows * (unsigned)c), dim3(kStreamThreads), smem, s, c, a);
   });

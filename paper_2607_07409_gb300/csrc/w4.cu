@@ -123,13 +123,21 @@ struct ZeroPoints {
     }
   }
 };
+// (w & mask) | base in one instruction: given as two constants the compiler made two of it.
+__device__ __forceinline__ uint32_t pick(uint32_t w, uint32_t mask, uint32_t base) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(base));
+  return r;
+}
 // The four registers of a word's weights: codes of nibbles q and q + 4, rows `half` and half + 1 of the lane's.
+// base: 1024 (bf16: 128) twice, in a register.
 template <bool HALF>
-__device__ __forceinline__ void weights_of(uint32_t word, const ZeroPoints<HALF>& z, int half, uint32_t (&m)[4]) {
+__device__ __forceinline__ void weights_of(uint32_t word, uint32_t base, const ZeroPoints<HALF>& z, int half,
+                                           uint32_t (&m)[4]) {
   if constexpr (HALF) {
     const uint32_t next = word >> 8;
-    const uint32_t c[4] = {(word & 0x000F000Fu) | 0x64006400u, (word & 0x00F000F0u) | 0x64006400u,
-                           (next & 0x000F000Fu) | 0x64006400u, (next & 0x00F000F0u) | 0x64006400u};
+    const uint32_t c[4] = {pick(word, 0x000F000Fu, base), pick(word, 0x00F000F0u, base), pick(next, 0x000F000Fu, base),
+                           pick(next, 0x00F000F0u, base)};
 #pragma unroll
     for (int q = 0; q < 4; q += 2) {
       asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(m[q]) : "r"(c[q]), "r"(z.low[half]));
@@ -138,7 +146,7 @@ __device__ __forceinline__ void weights_of(uint32_t word, const ZeroPoints<HALF>
   } else {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const uint32_t c = ((word >> (4 * q)) & 0x000F000Fu) | 0x43004300u;
+      const uint32_t c = pick(word >> (4 * q), 0x000F000Fu, base);
       asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(m[q]) : "r"(c), "r"(z.low[half + (q & 1)]));
     }
   }
@@ -228,22 +236,31 @@ __device__ __forceinline__ void stage_features(const W4Args& a, int b0, int unit
 
 // One warp's unit: 32 rows, 32 inputs.
 template <int NT, int TERMS, bool HALF>
-__device__ __forceinline__ void multiply_unit(const uint4 w4, const ZeroPoints<HALF>& z, const uint4* x,
+__device__ __forceinline__ void multiply_unit(const uint4 w4, uint32_t base, const ZeroPoints<HALF>& z, const uint4* x,
                                               float (&acc)[2][NT][4]) {
   uint32_t m[4][4];
-  weights_of<HALF>(w4.x, z, 0, m[0]);
-  weights_of<HALF>(w4.y, z, 0, m[1]);
-  weights_of<HALF>(w4.z, z, 2, m[2]);
-  weights_of<HALF>(w4.w, z, 2, m[3]);
+  weights_of<HALF>(w4.x, base, z, 0, m[0]);
+  weights_of<HALF>(w4.y, base, z, 0, m[1]);
+  weights_of<HALF>(w4.z, base, z, 2, m[2]);
+  weights_of<HALF>(w4.w, base, z, 2, m[3]);
+  // (a sum's two products stand four apart: one waits for the other)
+  constexpr int J = NT > 1 ? 2 : 1;
 #pragma unroll
   for (int term = 0; term < TERMS; ++term)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const uint4 f = x[(term * NT + j) * 32];
+    for (int j0 = 0; j0 < NT; j0 += J) {
+      uint4 f[J];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        mma16<HALF>(acc[h][j], m[2 * h], f.x, f.y);
-        mma16<HALF>(acc[h][j], m[2 * h + 1], f.z, f.w);
+      for (int j = 0; j < J; ++j) f[j] = x[(term * NT + j0 + j) * 32];
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        mma16<HALF>(acc[0][j0 + j], m[0], f[j].x, f[j].y);
+        mma16<HALF>(acc[1][j0 + j], m[2], f[j].x, f[j].y);
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        mma16<HALF>(acc[0][j0 + j], m[1], f[j].z, f[j].w);
+        mma16<HALF>(acc[1][j0 + j], m[3], f[j].z, f[j].w);
       }
     }
 }
@@ -405,6 +422,8 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
     int st = 0, ph = 0;
     ZeroPoints<HALF> z;
     z.set(0x8888u);
+    uint32_t base = HALF ? 0x64006400u : 0x43004300u;
+    asm("" : "+r"(base));                  // (a register, not a constant)
     for (int it = blockIdx.x; it < p.items; it += gridDim.x) {
       deadline = globaltimer_ns() + kWaitBudgetNs;
       const long long tile0 = (long long)it * p.wr;
@@ -429,7 +448,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
           const uint8_t* zeros = block + units * 512 + ((units + gunits - 1) >> glog) * 64 + g * 2;
           const auto unit = [&](int u, bool last) {
             if (a.zeros && (u & (gunits - 1)) == 0) z.set(*reinterpret_cast<const uint16_t*>(zeros + (u >> glog) * 16));
-            multiply_unit<NT, TERMS, HALF>(codes[u * 32], z, x + u * (TERMS * NT * 32), acc);
+            multiply_unit<NT, TERMS, HALF>(codes[u * 32], base, z, x + u * (TERMS * NT * 32), acc);
             if (last || ((u + 1) & (gunits - 1)) == 0)
               scale_group<NT>(*reinterpret_cast<const uint2*>(scales + (u >> glog) * 64), acc, tot);
           };
