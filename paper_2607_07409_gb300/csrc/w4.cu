@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
   bool bad = false;
   for (int kb = blockIdx.y; kb < a.lay.blocks; kb += gridDim.y) {
     const int units = min(4, a.lay.units - 4 * kb), ng = (units * kW4Unit + a.group - 1) / a.group;
-    uint8_t* block = a.packed + tile * a.lay.tile_bytes + (long long)kb * a.lay.block_bytes;
+    uint8_t* block = a.packed + w4_block_at(a.lay, tile, kb);
     if (u < units) {
       uint32_t w[4];
       for (int j = 0; j < 4; ++j) {              // word 2 (rows' half) + k-step
@@ -183,24 +183,21 @@ constexpr int kW4Producers = 96;         // threads that stage features where th
 template <int NT>
 constexpr int kW4Warps = NT <= 2 ? 16 : 8;      // warps that multiply, at most
 
-// A request's power of two: its features' largest, m, comes to 2^14 .. 2^15. 0 where there
-// is an infinity or NaN: its outputs are those of these alone, and the others count as 0.
-__device__ __forceinline__ int feature_shift(float m) {
-  return m > 0.f ? 14 - ilogbf(m) : 0;
-}
+// A request's power of two: its features' largest, of these bits, comes to 2^14 .. 2^15.
+// Where there is an infinity or NaN its outputs are those of these alone: the others count as 0.
 constexpr int kNotFinite = 1 << 20;
+__device__ __forceinline__ int feature_shift(uint32_t bits) {
+  if (bits >= 0x7F800000u) return kNotFinite;
+  return bits ? 14 - ilogbf(__uint_as_float(bits)) : 0;
+}
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }    // -126 .. 127
 
-// Fragments of a block's features: [4 units][TERMS][NT][32 lanes] of 16 bytes; lane 4 g + t
-// has request 8 j + g, inputs 8 t .. 8 t + 7 of the unit's 32. shift: HALF, the requests'.
+// Fragments of a unit's features, request 8 j + g and inputs 8 t .. 8 t + 7 of its 32 in lane
+// 4 g + t: [TERMS][NT][32 lanes] of 16 bytes. sh: HALF, the request's power.
 template <int NT, int TERMS, bool HALF>
-__device__ __forceinline__ void stage_features(const W4Args& a, int b0, int unit, int j, const int* shift, uint4* dst) {
-  const int lane = threadIdx.x & 31, b = 8 * j + (lane >> 2);
-  float f[8];
-  load_features(a, b0 + b, unit * kW4Unit + 8 * (lane & 3), f);
+__device__ __forceinline__ void put_features(const float (&f)[8], int j, int sh, uint4* dst) {
   uint32_t t[TERMS][8];
   if constexpr (HALF) {
-    const int sh = shift[b];
     // (in two factors: the power itself may be past float32's range)
     const float s0 = sh == kNotFinite ? 1.f : pow2i(sh / 2), s1 = sh == kNotFinite ? 1.f : pow2i(sh - sh / 2);
 #pragma unroll
@@ -230,8 +227,12 @@ __device__ __forceinline__ void stage_features(const W4Args& a, int b0, int unit
   }
 #pragma unroll
   for (int k = 0; k < TERMS; ++k)
-    dst[(k * NT + j) * 32 + lane] = make_uint4(t[k][0] | t[k][1] << 16, t[k][2] | t[k][3] << 16, t[k][4] | t[k][5] << 16,
-                                               t[k][6] | t[k][7] << 16);
+    dst[(k * NT + j) * 32 + (threadIdx.x & 31)] =
+        make_uint4(t[k][0] | t[k][1] << 16, t[k][2] | t[k][3] << 16, t[k][4] | t[k][5] << 16, t[k][6] | t[k][7] << 16);
+}
+__device__ __forceinline__ void load_unit(const W4Args& a, int b0, int unit, int j, float (&f)[8]) {
+  const int lane = threadIdx.x & 31;
+  load_features(a, b0 + 8 * j + (lane >> 2), unit * kW4Unit + 8 * (lane & 3), f);
 }
 
 // One warp's unit: 32 rows, 32 inputs.
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
   constexpr int kXBlock = 4 * TERMS * NT * 512;
   __shared__ uint64_t full[kW4MaxStages], empty[kW4MaxStages];
   __shared__ int abort_flag;
-  __shared__ int shift[N];
+  __shared__ uint32_t largest[N];          // HALF: bits of the requests' largest features
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = p.wr * p.wk;
   const int b0 = blockIdx.y * N;
   uint8_t* ring = smem;                                                     // stages of p.stage_bytes
@@ -329,6 +330,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
     }
     fence_mbarrier_init();
   }
+  if (HALF && threadIdx.x < N) largest[threadIdx.x] = 0;
   __syncthreads();
   pdl_wait();
   if (threadIdx.x == 0) pdl_trigger();
@@ -349,7 +351,9 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
           const int units = min(4 * p.wk, a.lay.units - step * p.wk * 4);
           for (int i = t0; i < units * NT; i += kW4Producers / 32) {
             const int u = i / NT, j = i - u * NT;
-            stage_features<NT, TERMS, HALF>(a, b0, step * p.wk * 4 + u, j, nullptr, dst + u * (TERMS * NT * 32));
+            float f[8];
+            load_unit(a, b0, step * p.wk * 4 + u, j, f);
+            put_features<NT, TERMS, HALF>(f, j, 0, dst + u * (TERMS * NT * 32));
           }
           mbar_arrive(&full[st]);
           if (++st == p.stages) st = 0, ph ^= 1;
@@ -369,13 +373,13 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
         for (int step = 0; step < steps; ++step) {
           if (!dead) dead = !mbar_wait(&empty[st], ph ^ 1, deadline, &abort_flag);
           if (dead) break;
-          const long long from = (long long)step * p.wk * a.lay.block_bytes;
-          const long long to = min(a.lay.tile_bytes, from + (long long)p.wk * a.lay.block_bytes);
-          const uint32_t bytes = (uint32_t)(to - from);
-          mbar_arrive_expect_tx(&full[st], bytes * live);
-          for (int r = 0; r < live; ++r)
-            bulk_load(ring + (size_t)st * p.stage_bytes + r * p.wk * a.lay.block_bytes,
-                      a.packed + (tile0 + r) * a.lay.tile_bytes + from, bytes, &full[st]);
+          // an input block of the live tiles is one piece
+          const int kb0 = step * p.wk, kb1 = min(a.lay.blocks, kb0 + p.wk);
+          const uint32_t whole = (uint32_t)live * a.lay.block_bytes, last = (uint32_t)live * a.lay.last_bytes;
+          mbar_arrive_expect_tx(&full[st], kb1 < a.lay.blocks ? (kb1 - kb0) * whole : (kb1 - kb0 - 1) * whole + last);
+          for (int kb = kb0; kb < kb1; ++kb)
+            bulk_load(ring + (size_t)st * p.stage_bytes + (kb - kb0) * p.wr * a.lay.block_bytes,
+                      a.packed + w4_block_at(a.lay, tile0, kb), kb + 1 < a.lay.blocks ? whole : last, &full[st]);
           ++issued;
           if (++st == p.stages) st = 0, ph ^= 1;
         }
@@ -391,29 +395,47 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
   } else {
     // ---- products
     const int wr = warp / p.wk, wk = warp - wr * p.wk, g = lane >> 2, t = lane & 3;
-    if constexpr (HALF) {
-      // the requests' largest features
-      for (int b = warp; b < N; b += warps) {
-        float m = 0.f, nan = 0.f;
-        for (int k = lane * 8; k < a.K; k += 256) {
-          float f[8];
-          load_features(a, b0 + b, k, f);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            m = fmaxf(m, fabsf(f[i]));
-            nan += f[i] != f[i] ? 1.f : 0.f;
-          }
-        }
-        m = warp_max(m);
-        const bool any_nan = __any_sync(0xFFFFFFFFu, nan != 0.f);
-        if (lane == 0) shift[b] = any_nan || !(m < INFINITY) ? kNotFinite : feature_shift(m);
-      }
-      asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
-    }
     if (p.resident) {
-      for (int i = warp; i < a.lay.units * NT; i += warps) {
-        const int u = i / NT, j = i - u * NT;
-        stage_features<NT, TERMS, HALF>(a, b0, u, j, shift, reinterpret_cast<uint4*>(xres) + u * (TERMS * NT * 32));
+      // A warp's units of features, the first ones' kept from the search for the requests' largest.
+      constexpr int kKept = 2;
+      const int tasks = a.lay.units * NT;
+      float f[kKept][8];
+#pragma unroll
+      for (int i = 0; i < kKept; ++i) {
+        const int task = warp + i * warps;
+        if (task < tasks) load_unit(a, b0, task / NT, task % NT, f[i]);
+      }
+      if constexpr (HALF) {
+        const auto look = [&](const float (&x)[8], int j) {
+          uint32_t m = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(fabsf(x[i])));      // NaN above infinity
+          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+          if (t == 0) atomicMax(&largest[8 * j + g], m);
+        };
+        for (int task = warp + kKept * warps; task < tasks; task += warps) {
+          float x[8];
+          load_unit(a, b0, task / NT, task % NT, x);
+          look(x, task % NT);
+        }
+#pragma unroll
+        for (int i = 0; i < kKept; ++i)
+          if (warp + i * warps < tasks) look(f[i], (warp + i * warps) % NT);
+        asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+      }
+      const auto place = [&](const float (&x)[8], int task) {
+        const int j = task % NT;
+        put_features<NT, TERMS, HALF>(x, j, HALF ? feature_shift(largest[8 * j + g]) : 0,
+                                      reinterpret_cast<uint4*>(xres) + (task / NT) * (TERMS * NT * 32));
+      };
+#pragma unroll
+      for (int i = 0; i < kKept; ++i)
+        if (warp + i * warps < tasks) place(f[i], warp + i * warps);
+      for (int task = warp + kKept * warps; task < tasks; task += warps) {
+        float x[8];
+        load_unit(a, b0, task / NT, task % NT, x);
+        place(x, task);
       }
       asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
     }
@@ -438,7 +460,8 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
         if (!dead) dead = !mbar_wait(&full[st], ph, deadline, &abort_flag);
         const int kb = step * p.wk + wk;
         if (kb < a.lay.blocks && tile0 + wr < a.lay.tiles) {
-          const uint8_t* block = ring + (size_t)st * p.stage_bytes + (size_t)(wr * p.wk + wk) * a.lay.block_bytes;
+          const uint8_t* block = ring + (size_t)st * p.stage_bytes + (size_t)wk * p.wr * a.lay.block_bytes +
+                                 (size_t)wr * (kb + 1 < a.lay.blocks ? a.lay.block_bytes : a.lay.last_bytes);
           const uint4* codes = reinterpret_cast<const uint4*>(block) + lane;
           const int units = min(4, a.lay.units - 4 * kb);
           const uint4* x = (p.resident ? reinterpret_cast<const uint4*>(xres) + kb * (kXBlock / 16)
@@ -484,7 +507,7 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
           y.x += w.x; y.y += w.y; y.z += w.z; y.w += w.w;
         }
         if constexpr (HALF) {
-          const int sh = shift[b] == kNotFinite ? 0 : -shift[b];
+          const int up = feature_shift(largest[b]), sh = up == kNotFinite ? 0 : -up;
           const float s0 = pow2i(sh / 2), s1 = pow2i(sh - sh / 2);
           y.x = y.x * s0 * s1; y.y = y.y * s0 * s1; y.z = y.z * s0 * s1; y.w = y.w * s0 * s1;
         }
