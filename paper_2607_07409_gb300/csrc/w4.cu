@@ -1,5 +1,6 @@
 // Products with 4-bit weights: the layout of the codes, and y = W x.
 #include <algorithm>
+#include <type_traits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -469,18 +470,25 @@ __global__ void __launch_bounds__(kW4Warps<NT> * 32 + 32 + (HALF ? 0 : kW4Produc
                                              wk * (kXBlock / 16)) + lane;
           const uint8_t* scales = block + units * 512 + g * 8;
           const uint8_t* zeros = block + units * 512 + ((units + gunits - 1) >> glog) * 64 + g * 2;
-          const auto unit = [&](int u, bool last) {
-            if (a.zeros && (u & (gunits - 1)) == 0) z.set(*reinterpret_cast<const uint16_t*>(zeros + (u >> glog) * 16));
+          const auto unit = [&](int u, int grp, bool first, bool last) {
+            if (first && a.zeros) z.set(*reinterpret_cast<const uint16_t*>(zeros + grp * 16));
             multiply_unit<NT, TERMS, HALF>(codes[u * 32], base, z, x + u * (TERMS * NT * 32), acc);
-            if (last || ((u + 1) & (gunits - 1)) == 0)
-              scale_group<NT>(*reinterpret_cast<const uint2*>(scales + (u >> glog) * 64), acc, tot);
+            if (last) scale_group<NT>(*reinterpret_cast<const uint2*>(scales + grp * 64), acc, tot);
+          };
+          // (a whole block straight on for each group size: with tests between its units 85 instructions a unit)
+          const auto whole = [&](auto group_units) {
+            constexpr int G = decltype(group_units)::value;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) unit(u, u / G, u % G == 0, u % G == G - 1);
           };
           if (units == 4) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) unit(u, u == 3);
+            if (glog == 0) whole(std::integral_constant<int, 1>{});
+            else if (glog == 1) whole(std::integral_constant<int, 2>{});
+            else whole(std::integral_constant<int, 4>{});
           } else {
 #pragma unroll 1
-            for (int u = 0; u < units; ++u) unit(u, u + 1 == units);
+            for (int u = 0; u < units; ++u)
+              unit(u, u >> glog, (u & (gunits - 1)) == 0, u + 1 == units || ((u + 1) & (gunits - 1)) == 0);
           }
         }
         __syncwarp();
