@@ -653,8 +653,10 @@ int dels_w4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros,
 /*
  * out[b, v] = sum_k w[v, k] x[b, k].  x [device] [B, K] of x_dtype, x_stride elements
  * from one row to the next (0: K); out [device] [B, V] of out_dtype, out_stride (0: V).
- * Products and sums are float32 (x to its last bit: float32 features as three exact
- * bf16 terms), each group's sum times its scale; equal calls give equal bits.
+ * Products are exact and sums float32, a group's at a time, which its scale and zero
+ * point then take: errors are those of float32 sums of scale code x and scale zero x. A
+ * request's features are held to 2^-36 of its largest one; one with infinities or NaN has
+ * NaN throughout. Equal calls give equal bits.
  * workspace >= 256 bytes. Limits: 0 <= B <= 65535; pointers aligned to their elements.
  */
 size_t dels_w4_project_workspace_bytes(const dels_w4* w, int B);

@@ -225,42 +225,26 @@ struct VerifyGivenArgs {
 cudaError_t launch_verify_given(const VerifyGivenArgs& a, cudaStream_t s);
 
 // ---- products with 4-bit weights ---------------------------------------------
-// The packed matrix: tiles of 32 rows, in bands of 16 tiles (the last one of as many as
-// there are). A band has its tiles' blocks of 128 inputs (the last one of as many whole 32s as
-// there are) one input block after another, so that what a CTA takes at a time is one
-// piece; a block has its codes, its groups' scales and zero points.
-// * codes: 512 bytes for 32 rows x 32 inputs ("unit"), 16 for each lane of a warp. Lane
-//   4 g + t has rows g + 8 i (i < 4) and inputs 8 t .. 8 t + 7, as word 2 (i / 2) + s for the
-//   inputs 8 t + 4 s .. + 3: its nibble q and q + 4 are row i % 2 = q % 2, inputs 2 (q / 2)
-//   and 2 (q / 2) + 1 of the four. A word and a mask then give the four registers of an
-//   mma.m16n8k16 operand: (w >> 4 q) & 0x000F000F is register q.
-// * scales: 64 bytes a group, bf16 of rows g, g + 8, g + 16, g + 24 for each g of 0 .. 7
-// * zero points: 16 bytes a group, four nibbles of the same rows for each g
-constexpr int kW4Rows = 32, kW4Block = 128, kW4Unit = 32, kW4Band = 16;
+// The packed matrix: tiles of 128 rows, in each its blocks of 128 inputs (K rounded up to whole
+// ones: codes and scales of 0 there), in each
+// * codes: for each 32 inputs ("unit") 16 bytes for each row, four words of 8 inputs: input
+//   2 p + h of a word in its bits 4 p + 16 h .. + 3, so that (w >> 4 p) & 0x000F000F is a pair
+// * scales: 256 bytes a group, bf16 of the rows
+// * zero points: 64 bytes a group, a nibble a row
+constexpr int kW4Rows = 128, kW4Block = 128, kW4Unit = 32, kW4UnitBytes = kW4Rows * 16;
 struct W4Layout {
-  int units, blocks;             // of 32 and 128 inputs
-  int block_bytes, last_bytes;   // of a whole block, of a tile's last one
-  long long tile_bytes;          // of 32 rows
+  int blocks;                    // of 128 inputs
+  int block_bytes;
+  long long tile_bytes;
   long long tiles;
 };
-inline __host__ __device__ int w4_part_bytes(int units, int group, int zeros) {   // of a block's first units
-  return units * 512 + (units * kW4Unit + group - 1) / group * (zeros ? 80 : 64);
-}
 inline W4Layout w4_layout(int V, int K, int group, int zeros) {
   W4Layout L;
-  L.units = (K + kW4Unit - 1) / kW4Unit;
-  L.blocks = (L.units + 3) / 4;
-  L.block_bytes = w4_part_bytes(4, group, zeros);
-  L.last_bytes = w4_part_bytes(L.units - 4 * (L.blocks - 1), group, zeros);
-  L.tile_bytes = (long long)(L.blocks - 1) * L.block_bytes + L.last_bytes;
+  L.blocks = (K + kW4Block - 1) / kW4Block;
+  L.block_bytes = 4 * kW4UnitBytes + kW4Block / group * (zeros ? 320 : 256);
+  L.tile_bytes = (long long)L.blocks * L.block_bytes;
   L.tiles = ((long long)V + kW4Rows - 1) / kW4Rows;
   return L;
-}
-// Where a tile's input block kb lies. (The tiles behind it in its band follow.)
-inline __host__ __device__ long long w4_block_at(const W4Layout& L, long long tile, int kb) {
-  const long long band = tile / kW4Band, first = band * kW4Band, left = L.tiles - first;
-  const long long tiles = left < kW4Band ? left : kW4Band;
-  return first * L.tile_bytes + kb * tiles * L.block_bytes + (tile - first) * (kb + 1 < L.blocks ? L.block_bytes : L.last_bytes);
 }
 struct W4PackArgs {
   const uint8_t* codes;

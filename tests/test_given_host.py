@@ -29,11 +29,11 @@ def ref(struct, **kw):
 # ---------------------------------------------------------------- 4-bit matrices
 
 def test_w4_bytes(dels):
-    # codes, 64 bytes of scales per group and 32 rows, 16 of zero points
-    assert dels.dels_w4_bytes(32, 128, 128, False) == 2048 + 64
-    assert dels.dels_w4_bytes(33, 128, 32, True) == 2 * (2048 + 4 * 80)
-    assert dels.dels_w4_bytes(1, 1, 64, True) == 512 + 80
-    assert dels.dels_w4_bytes(64, 1000, 64, False) == 2 * (32 * 512 + 16 * 64)
+    # for 128 rows and 128 inputs: codes, 256 bytes of scales and 64 of zero points a group
+    assert dels.dels_w4_bytes(32, 128, 128, False) == 8192 + 256
+    assert dels.dels_w4_bytes(129, 128, 32, True) == 2 * (8192 + 4 * 320)
+    assert dels.dels_w4_bytes(1, 1, 64, True) == 8192 + 2 * 320
+    assert dels.dels_w4_bytes(64, 1000, 64, False) == 8 * (8192 + 2 * 256)
     for V, K, G in [(0, 128, 32), (8, 0, 32), (8, 128, 16), (8, 128, 48), (8, 128, 256), ((1 << 27) + 1, 8, 32),
                     (8, 65537, 32), (-1, 8, 32)]:
         assert dels.dels_w4_bytes(V, K, G, False) == 0
@@ -46,8 +46,8 @@ def pack(dels, codes=64, scales=64, zeros=None, V=40, K=100, group=32, packed=40
 @pytest.mark.parametrize("code,kw", [
     (-2, dict(V=0)), (-2, dict(K=0)), (-2, dict(group=48)), (-2, dict(K=65537)),
     (-1, dict(codes=None)), (-1, dict(scales=None)), (-1, dict(packed=None)),
-    (-5, dict(ws=None)), (-5, dict(n=255)), (-5, dict(nbytes=2 * (4 * 576) - 1)),
-    (-5, dict(zeros=64, nbytes=2 * (4 * 592) - 1)),
+    (-5, dict(ws=None)), (-5, dict(n=255)), (-5, dict(nbytes=4 * 2048 + 4 * 256 - 1)),
+    (-5, dict(zeros=64, nbytes=4 * 2048 + 4 * 320 - 1)),
     (-4, dict(packed=4104)), (-4, dict(scales=65)), (-4, dict(ws=WS + 8)),
 ])
 def test_pack_refuses(dels, code, kw):

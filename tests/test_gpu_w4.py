@@ -1,10 +1,12 @@
 """Products with 4-bit weights against float64.
 
-Tolerance of an output: the products of a code and a feature (a bf16 term of it) are exact in float32; the
+Tolerance of an output: the products of a code and a feature (a term of it) are exact in float32; the
 tensor cores add 16 of them and the sum so far at a time, each off by at most 2^-24 of the
 largest in truncating and rounding it, so 17 2^-24 of the sum of all magnitudes for each 16 inputs and term of a group;
-the groups' sums take the scale's product and an addition each, and 8 more additions join their
-parts: (17 terms G / 16 + groups + 10) 2^-24 sum_k |w_k x_k| in all; bf16 half a step, 2^-8.
+a group's features are added up for its zero point in at most group + 3 additions, their product with it, the scale's
+and an addition of each group follow: with S = sum_k |scale_k| (code_k + zero_k) |x_k|,
+(17 terms G / 16 + G + groups + 10) 2^-24 S in all; bf16 half a step, 2^-8. Features are held to 2^-36 of their
+request's largest, m: 2^-36 m sum_k |scale_k| (code_k + zero_k) more.
 """
 import math
 
@@ -41,12 +43,16 @@ class Case:
         return (self.codes.double() - z) * self.scales.double()[:, of]
 
     def want(self, out):
+        of = torch.arange(self.K) // self.group
+        z = 8.0 if self.zeros is None else self.zeros.double()[:, of]
+        size = (self.codes.double() + z) * self.scales.double()[:, of].abs()
         w, x = self.weights(), self.x.double()
         y = x @ w.T
         terms = 3 if self.x.dtype is F32 else 1
-        groups = -(-self.K // self.group)
-        eps = (17 * terms * min(self.group, 32 * -(-self.K // 32)) / 16 + groups + 10) * 2.0 ** -24
-        return y, eps * (x.abs() @ w.abs().T) + (2.0 ** -8 * y.abs() if out is BF16 else 0.0) + 1e-37
+        groups, G = -(-self.K // self.group), min(self.group, 32 * -(-self.K // 32))
+        eps = (17 * terms * G / 16 + G + groups + 10) * 2.0 ** -24
+        tol = eps * (x.abs() @ size.T) + 2.0 ** -36 * x.abs().amax(-1, keepdim=True) * size.sum(-1)
+        return y, tol + (2.0 ** -8 * y.abs() if out is BF16 else 0.0) + 1e-37
 
 
 def put(x, offset=0, pitch=None):
@@ -129,8 +135,10 @@ def test_outputs_anywhere(V, offset, pitch, dtype):
         assert (big[offset + b * pitch + V:offset + (b + 1) * pitch] == -7).all()
 
 
-def test_float32_features_to_their_last_bit():
-    """Features of 24 significant bits, from the smallest to the largest: each alone against one code."""
+def test_float32_features_of_any_size():
+    """Features of 24 significant bits, from the smallest to the largest, each alone against a code of 9 beside a zero
+    point of 8: three terms' products, each sum of them off by 2^-24 of 9 x at most, 8 x taken off in one fma, and three
+    more roundings of x: 32 2^-24 x in all."""
     K = 64
     g = torch.Generator().manual_seed(1)
     m = torch.randint(1 << 23, 1 << 24, (K,), generator=g).double()
@@ -139,22 +147,22 @@ def test_float32_features_to_their_last_bit():
     x[0], x[1] = torch.finfo(F32).max, -torch.finfo(F32).max
     codes = torch.full((40, K), 9, dtype=torch.uint8)             # weight 1
     w = dels.pack_w4(codes.to(DEV), torch.ones(40, 1, dtype=BF16, device=DEV), group=64)
-    got = w.project(torch.diag(x).to(DEV)).cpu()
-    assert torch.equal(got, x[:, None].expand(K, 40))
+    got = w.project(torch.diag(x).to(DEV)).cpu().double()
+    assert ((got - x.double()[:, None]).abs() <= 32 * 2.0 ** -24 * x.double().abs()[:, None]).all()
 
 
 def test_non_finite_features_and_scales():
-    c = Case(4, 100, 200, 32, False)
-    c.codes[c.codes == 8] = 9                                     # (0 times infinity is NaN)
-    c.x[1, 7], c.x[2, 190] = INF, NAN
-    f = c.x.float()
-    for x in (c.x, f):
-        got = c.pack().project(put(x)).cpu()
-        w = c.weights()
-        assert torch.isnan(got[2]).all()
-        assert (got[1] == torch.where(w[:, 7] > 0, INF, -INF)).all()
+    """A request with an infinity or NaN has NaN throughout, the others their products; scales likewise by rows."""
+    for x in (BF16, F32):
+        c = Case(11, 100, 200, 32, False, x)
+        c.x[1, 7], c.x[2, 190], c.x[9, 0] = INF, NAN, -INF
+        got = c.pack().project(put(c.x)).cpu()
+        bad = [1, 2, 9]
+        assert torch.isnan(got[bad]).all()
+        c.x[bad] = 0
         y, tol = c.want(F32)
-        assert ((got.double() - y).abs() <= 3 * tol)[[0, 3]].all()
+        keep = [i for i in range(11) if i not in bad]
+        assert ((got.double() - y).abs() <= tol)[keep].all()
     c.scales[5, 2], c.scales[6, 0] = NAN, INF
     got = c.pack().project(put(c.x)).cpu()
     assert torch.isnan(got[0, 5]) and torch.isinf(got[0, 6]) and torch.isfinite(got[0, [4, 7]]).all()
@@ -184,8 +192,9 @@ def test_matrix_past_4_gb():
     at = torch.cat([torch.arange(64), torch.arange(V - 200, V)]).to(DEV)
     of = torch.arange(K, device=DEV) // G
     wt = (codes[at].double() - 8) * scales[at].double()[:, of]
-    want, size = x.double() @ wt.T, x.double().abs() @ wt.abs().T
-    eps = (17 * 8 + 65 + 10) * 2.0 ** -24
+    size = (codes[at].double() + 8) * scales[at].double()[:, of]
+    want, size = x.double() @ wt.T, x.double().abs() @ size.T
+    eps = (17 * 8 + 128 + 65 + 10) * 2.0 ** -24 + 2.0 ** -33
     assert ((got[:, at].double() - want).abs() <= eps * size).all()
 
 
