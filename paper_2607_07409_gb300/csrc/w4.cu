@@ -68,20 +68,18 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 // ---------------------------------------------------------------------------
 // y = W x on the tensor cores (tcgen05, the weights from tensor memory).
 //
-// What bounds few requests is the codes' stream, if nothing else is in its way: per code a
-// fraction of an instruction. fp16's numbers without an exponent are linear, so 4 bits at the
-// bottom of a half are a code times 2^-24, and where they lie one higher times 2^-20, exactly,
-// with no conversion: a word of 8 codes takes 4 masks and a shift to be four pairs of an operand.
-// The features beside the higher ones are divided by 16, and the zero point comes off a group's
-// sum: z times the sum of its features. A request's features are scaled by a power of two
-// to 2^15 at most (2^11 beside the higher codes): fp16 then holds bf16 features exactly down to
-// 2^-27 of the request's largest and what is smaller to 2^-36 of that; float32 features are
-// three fp16 terms, to the same 2^-36. A group's sum is float32 and scaled there.
-// (mma.sync with the same operands issues a quarter of a tcgen05.mma's share at most: 151936 x
-// 1024, one request, 20 us, and 151936 x 256, 64 requests, 37 us, at its rate.)
-//
-// (A request with infinities or NaN has NaN throughout: its code sums and its zero points' could not
-// be told apart.)
+// A code minus its zero point is a whole number of -15 .. 15: fp16 operands hold it, its products with
+// a feature's 11 bits are exact, and a group's sum is float32 and scaled there. fp16's 10 bits of
+// mantissa hold a code where it lies in a byte, low or high: (w & 0x000F000F) | 0x6400 is 1024 + c
+// and the high ones' 1024 + 16 c, so that a word of 8 codes takes 4 masks and a shift, and an fma a
+// pair takes the zero point off. (Without an exponent, as multiples of 2^-24, the codes need neither, but the
+// tensor cores align such numbers' products by the exponent they do not have, ten bits too far
+// up: sums were off by 8e-7 of themselves, now by 1e-7.) A request's features are scaled by a power of
+// two to 2^15 at most: fp16 then holds bf16 features exactly down to 2^-32 of the request's
+// largest and what is smaller to 2^-40 of that; float32 features are three terms, of 11 bits of a fixed
+// point each, to the same 2^-40. (A request with infinities or NaN has NaN throughout.)
+// mma.sync, with the same operands, issues at most one such product in 32 cycles of a quarter
+// SM: 151936 x 2560 for 8 requests 45 us, 151936 x 256 for 64 37 us, at that rate.
 //
 // Four warps take a tile of 128 rows, a thread a row: codes of a block of 128 inputs from
 // shared memory (bulk copies into a ring of their own, blocks ahead), operand pairs into
@@ -131,14 +129,30 @@ __device__ __forceinline__ uint64_t smem_desc_plain(uint32_t addr, uint32_t lead
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N) {
   return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
-// Operand pairs of a word of 8 codes: the codes alone.
-__device__ __forceinline__ void pairs_of(uint32_t w, uint32_t* m) {
-  const uint32_t next = w >> 8;
-  m[0] = w & 0x000F000Fu;
-  m[1] = w & 0x00F000F0u;
-  m[2] = next & 0x000F000Fu;
-  m[3] = next & 0x00F000F0u;
+// (w & mask) | base in one instruction: given as two constants the compiler made two of it.
+__device__ __forceinline__ uint32_t pick(uint32_t w, uint32_t mask, uint32_t base) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(base));
+  return r;
 }
+// Zero points as pairs_of() takes them off.
+struct ZeroPoint {
+  uint32_t low, high;      // 1024 + z and -(64 + z), twice
+  __device__ __forceinline__ explicit ZeroPoint(uint32_t z)
+      : low(0x64006400u + z * 0x00010001u), high(0xD400D400u + z * 0x00100010u) {}
+};
+// Operand pairs of a word of 8 codes. base: 0x64006400, in a register.
+__device__ __forceinline__ void pairs_of(uint32_t w, uint32_t base, const ZeroPoint& z, uint32_t* m) {
+  const uint32_t next = w >> 8;
+  const uint32_t c[4] = {pick(w, 0x000F000Fu, base), pick(w, 0x00F000F0u, base), pick(next, 0x000F000Fu, base),
+                         pick(next, 0x00F000F0u, base)};
+#pragma unroll
+  for (int q = 0; q < 4; q += 2) {
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(m[q]) : "r"(c[q]), "r"(z.low));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(m[q + 1]) : "r"(c[q + 1]), "r"(0x2C002C00u), "r"(z.high));
+  }
+}
+
 // 8 features of a row as they are stored.
 template <bool F32>
 struct Features {
@@ -181,33 +195,34 @@ __device__ __forceinline__ int feature_shift(uint32_t bits) { return bits ? 14 -
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }    // -126 .. 127
 
 // 8 features of a lane, scaled by f.x f.y (two factors: the power may be past float32's range), as TERMS
-// fp16 terms, `apart` 16-byte places from one to the next. Returns the sum of the scaled ones. (The
-// codes beside inputs 2, 3, 6, 7 are 16 times as much.)
+// fp16 terms, `apart` 16-byte places from one to the next.
 template <int TERMS>
-__device__ __forceinline__ float put_features(const float (&x)[8], const float2& f, int apart, uint4* dst) {
-  const f32x2 f0 = both2(f.x), f1 = both2(f.y), f1h = both2(f.y * 0.0625f);
-  f32x2 sum = 0ull;
+__device__ __forceinline__ void put_features(const float (&x)[8], const float2& f, int apart, uint4* dst) {
+  const f32x2 f0 = both2(f.x), f1 = both2(f.y);
   uint32_t t[TERMS][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const f32x2 y = mul2(pair2(x[2 * i], x[2 * i + 1]), f0);
-    sum = add2(sum, mul2(y, f1));
-    float r0, r1;
-    split2(mul2(y, i & 1 ? f1h : f1), r0, r1);
+    f32x2 r = mul2(mul2(pair2(x[2 * i], x[2 * i + 1]), f0), f1);
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
-      const __half2 h = __floats2half2_rn(r0, r1);
-      t[k][i] = *reinterpret_cast<const uint32_t*>(&h);
+      // of several terms each but the last is a whole multiple of its place's, 11 bits of them
+      f32x2 d = r;
+      float d0, d1;
       if (k + 1 < TERMS) {
-        r0 -= __low2float(h);
-        r1 -= __high2float(h);
+        const float place = k ? 98304.f : 201326592.f;                    // 1.5 2^(23 - 7), 1.5 2^(23 + 4)
+        d = add2(add2(r, both2(place)), both2(-place));
+        split2(d, d0, d1);
+        r = add2(r, pair2(-d0, -d1));
       }
+      split2(d, d0, d1);
+      const __half2 h = __floats2half2_rn(d0, d1);
+      t[k][i] = *reinterpret_cast<const uint32_t*>(&h);
     }
   }
 #pragma unroll
   for (int k = 0; k < TERMS; ++k) dst[k * apart] = make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
-  return sum2(sum);
 }
+
 constexpr int kW4Stages = 8;               // of a ring, at most
 
 // How a product runs: groups of four warps in a CTA, their rings, parts of K, units of an operand.
@@ -230,37 +245,27 @@ __device__ __forceinline__ bool elect_one() {
   return yes != 0;
 }
 // The products of UNITS units: operand columns from `acol`, sums from `dcol`, features from
-// the descriptor's low word `x`; GUNITS units a group. (All of it known but for three words: what
-// the compiler has to fetch from a thread's register for each product takes 60 cycles a product.)
-template <int NB, int TERMS, int UNITS, int GUNITS>
+// the descriptor's low word `x`; GUNITS units a group; ADD: to what the sums hold. (All of it known but for
+// three words: what the compiler has to fetch from a thread's register for each product takes 60
+// cycles a product.) The smallest terms first: the tensor cores cut what they add off at the last place of
+// the largest, and of the largest terms, whole multiples of one number, there is then nothing to cut.
+template <int NB, int TERMS, int UNITS, int GUNITS, bool ADD>
 __device__ __forceinline__ void issue_products(uint32_t dcol, uint32_t acol, uint32_t x, uint32_t part_units) {
   constexpr int N = NB < 16 ? 16 : NB;
   constexpr uint32_t kHigh = (NB < 16 ? 0u : 128u >> 4) | 1u << 14;      // of the descriptor
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u)
+  for (int g = 0; g < UNITS / GUNITS; ++g)
 #pragma unroll
-    for (int term = 0; term < TERMS; ++term)
+    for (int term = TERMS - 1; term >= 0; --term)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-        mma_from_tmem(dcol + u / GUNITS * N, acol + u * 16 + k * 8,
-                      (uint64_t)kHigh << 32 | (x + (term ? term * part_units * 4 * NB : 0u) + u * 4 * NB + k * 2 * NB),
-                      idesc_f16_f32(128, N), u % GUNITS || term || k);
-}
-
-// Units' products, added to what their one group's sums hold.
-template <int NB, int TERMS, int UNITS>
-__device__ __forceinline__ void add_products(uint32_t dcol, uint32_t acol, uint32_t x, uint32_t part_units) {
-  constexpr int N = NB < 16 ? 16 : NB;
-  constexpr uint32_t kHigh = (NB < 16 ? 0u : 128u >> 4) | 1u << 14;
+      for (int v = 0; v < GUNITS; ++v)
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u)
-#pragma unroll
-    for (int term = 0; term < TERMS; ++term)
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        mma_from_tmem(dcol, acol + u * 16 + k * 8,
-                      (uint64_t)kHigh << 32 | (x + (term ? term * part_units * 4 * NB : 0u) + u * 4 * NB + k * 2 * NB),
-                      idesc_f16_f32(128, N), 1);
+        for (int k = 0; k < 2; ++k) {
+          const int u = g * GUNITS + v;
+          mma_from_tmem(dcol + g * N, acol + u * 16 + k * 8,
+                        (uint64_t)kHigh << 32 | (x + (term ? term * part_units * 4 * NB : 0u) + u * 4 * NB + k * 2 * NB),
+                        idesc_f16_f32(128, N), ADD || term + 1 < TERMS || v || k);
+        }
 }
 
 template <int NB, int TERMS>
@@ -279,7 +284,6 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   const int b0 = blockIdx.y * NB;
   uint8_t* ring = smem + (size_t)grp * p.stages * p.stage_bytes;
   uint4* operand = reinterpret_cast<uint4*>(smem + (size_t)p.groups * p.stages * p.stage_bytes);
-  float* xsums = reinterpret_cast<float*>(operand + (size_t)TERMS * p.part_units * 4 * NB);     // [units of a part][NB]
   if (warp == 0) {
     tmem_alloc(&tmem_base, p.tmem_cols);
     tmem_relinquish();
@@ -363,7 +367,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   __syncthreads();
   if (tid < NB) {
     const bool finite = largest[tid] < 0x7F800000u;
-    const int up = finite ? feature_shift(largest[tid]) : 0, sh = 24 - up;
+    const int up = finite ? feature_shift(largest[tid]) : 0, sh = -up;
     scaled[tid] = make_float2(pow2i(up / 2), pow2i(up - up / 2));
     back[tid] = finite ? make_float2(pow2i(sh / 2), pow2i(sh - sh / 2)) : make_float2(NAN, NAN);
   }
@@ -376,10 +380,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       raw.unpack(x);
       const int n = 8 * (task % (NB / 8)) + (lane >> 2), u = task / (NB / 8);
       uint4* dst = operand + ((u - u0) * 4 + (lane & 3)) * NB + n;
-      float sum = put_features<TERMS>(x, scaled[n], p.part_units * 4 * NB, dst);
-      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-      if ((lane & 3) == 0) xsums[(u - u0) * NB + n] = sum;
+      put_features<TERMS>(x, scaled[n], p.part_units * 4 * NB, dst);
     };
     const int t0 = u0 * (NB / 8), t1 = u1 * (NB / 8);
     int task = t0 + warp;
@@ -395,15 +396,6 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
-    if (gunits > 1) {                       // the units' sums become their groups', in the groups' first units' places
-      for (int i = tid; i < (u1 - u0) / gunits * NB; i += warps * 32) {
-        const int s0 = i / NB * gunits, s1 = s0 + gunits;
-        float sum = xsums[s0 * NB + i % NB];
-        for (int u = s0 + 1; u < s1; ++u) sum += xsums[u * NB + i % NB];
-        xsums[s0 * NB + i % NB] = sum;
-      }
-      __syncthreads();
-    }
   };
   const bool resident = p.parts == 1;
   if (resident) stage(0, all_units, true);
@@ -421,14 +413,15 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
     __syncwarp();
   };
   int st = 0, ph = 0, dph = 0;
+  uint32_t base = 0x64006400u;
+  asm("" : "+r"(base));                   // (a register, not a constant)
   f32x2 tot[NB / 2];
   // apart in time: in step, all groups' codes wait for the ALU pipe and then all groups for their products
   __nanosleep(grp * 200);
 
-  // Sums of an operand's group i, whose features' sums are at unit `pu` of the part, scaled.
-  const auto add_sums = [&](int i, int pu, float scale, float mz) {
-    const float* xs = xsums + pu * NB;
-    const f32x2 s2 = both2(scale), mz2 = both2(mz);
+  // Sums of an operand's group i, scaled.
+  const auto add_sums = [&](int i, float scale) {
+    const f32x2 s2 = both2(scale);
     constexpr int W = NB < 16 ? 8 : 16;
 #pragma unroll
     for (int n0 = 0; n0 < NB; n0 += W) {
@@ -437,14 +430,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       else tmem_ld_x16(dcol + quadrant + i * N + n0, acc);
       tmem_ld_wait();
 #pragma unroll
-      for (int n = 0; n < W; n += 4) {
-        f32x2 y0 = pair2(acc[n], acc[n + 1]), y1 = pair2(acc[n + 2], acc[n + 3]);
-        const float4 x = *reinterpret_cast<const float4*>(xs + n0 + n);
-        y0 = fma2(mz2, pair2(x.x, x.y), y0);
-        y1 = fma2(mz2, pair2(x.z, x.w), y1);
-        tot[(n0 + n) / 2] = fma2(s2, y0, tot[(n0 + n) / 2]);
-        tot[(n0 + n) / 2 + 1] = fma2(s2, y1, tot[(n0 + n) / 2 + 1]);
-      }
+      for (int n = 0; n < W; n += 2) tot[(n0 + n) / 2] = fma2(s2, pair2(acc[n], acc[n + 1]), tot[(n0 + n) / 2]);
     }
   };
 
@@ -454,7 +440,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
     constexpr int U = decltype(step_units)::value, G = decltype(group_units)::value, NG = U > G ? U / G : 1;
     constexpr int kSteps = 4 / U;
     uint32_t m[U * 16];
-    float scale[NG], mz[NG];
+    float scale[NG];
     const auto load = [&](int i) {
       const int s0 = i % kSteps * U;
       if (s0 == 0) wait(&full[grp][st], ph);
@@ -467,15 +453,14 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         scale[g] = bf16_to_f(*reinterpret_cast<const uint16_t*>(scales + g * 256));
-        const uint32_t z = a.zeros ? zeros[g * 64] >> (4 * (row & 1)) & 15u : 8u;
-        mz[g] = 0.5f - __uint_as_float(z | 0x3F000000u);                 // -z 2^-24
-      }
+        const ZeroPoint z(a.zeros ? zeros[g * 64] >> (4 * (row & 1)) & 15u : 8u);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        pairs_of(w[u].x, m + u * 16);
-        pairs_of(w[u].y, m + u * 16 + 4);
-        pairs_of(w[u].z, m + u * 16 + 8);
-        pairs_of(w[u].w, m + u * 16 + 12);
+        for (int u = g * (U / NG); u < (g + 1) * (U / NG); ++u) {
+          pairs_of(w[u].x, base, z, m + u * 16);
+          pairs_of(w[u].y, base, z, m + u * 16 + 4);
+          pairs_of(w[u].z, base, z, m + u * 16 + 8);
+          pairs_of(w[u].w, base, z, m + u * 16 + 12);
+        }
       }
       if (s0 + U == 4 && ++st == p.stages) st = 0, ph ^= 1;
     };
@@ -484,9 +469,9 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       const int at = i % kSteps * U;
 #pragma unroll
       for (int u = 0; u < U; ++u) tmem_st_x16(acol + quadrant + u * 16, *reinterpret_cast<uint32_t(*)[16]>(m + u * 16));
-      float s_now[NG], z_now[NG];
+      float s_now[NG];
 #pragma unroll
-      for (int g = 0; g < NG; ++g) s_now[g] = scale[g], z_now[g] = mz[g];
+      for (int g = 0; g < NG; ++g) s_now[g] = scale[g];
       tmem_st_wait();
       tc_fence_before();
       asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
@@ -494,8 +479,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
         tc_fence_after();
         if (elect_one()) {
           const uint32_t x = x0 + (uint32_t)(i * U) * (4 * NB);
-          if (G > U && at > 0) add_products<NB, TERMS, U>(dcol, acol, x, p.part_units);
-          else issue_products<NB, TERMS, U, (G > U ? U : G)>(dcol, acol, x, p.part_units);
+          if (G > U && at > 0) issue_products<NB, TERMS, U, U, true>(dcol, acol, x, p.part_units);
+          else issue_products<NB, TERMS, U, (G > U ? U : G), false>(dcol, acol, x, p.part_units);
           tc_commit(&done[grp]);
         }
         __syncwarp();
@@ -510,7 +495,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       tc_fence_after();
       if (G <= U || at + U == 4) {
 #pragma unroll
-        for (int g = 0; g < NG; ++g) add_sums(g, G > U ? i * U + U - G : i * U + g * G, s_now[g], z_now[g]);
+        for (int g = 0; g < NG; ++g) add_sums(g, s_now[g]);
       }
     }
   };
@@ -582,7 +567,7 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   constexpr int N = NB < 16 ? 16 : NB;
   const int gunits = a.group / kW4Unit;
   p.stage_bytes = (a.lay.block_bytes + 127) / 128 * 128;
-  const long long unit = (long long)TERMS * 4 * NB * 16 + NB * 4, whole = 4 * a.lay.blocks * unit;
+  const long long unit = (long long)TERMS * 4 * NB * 16, whole = 4 * a.lay.blocks * unit;
   // groups of warps: no more than have tiles and leave room for the features beside two stages each, four at least
   p.groups = (int)std::min<long long>(kW4Groups<NB>, (a.lay.tiles + ctas - 1) / ctas);
   while (p.groups > 4 && room - 2ll * p.groups * p.stage_bytes < whole) --p.groups;

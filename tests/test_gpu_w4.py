@@ -1,12 +1,11 @@
 """Products with 4-bit weights against float64.
 
-Tolerance of an output: the products of a code and a feature (a term of it) are exact in float32; the
-tensor cores add 16 of them and the sum so far at a time, each off by at most 2^-24 of the
+Tolerance of an output: the products of a weight without its scale and a feature (a term of it) are exact in float32;
+the tensor cores add 16 of them and the sum so far at a time, each off by at most 2^-24 of the
 largest in truncating and rounding it, so 17 2^-24 of the sum of all magnitudes for each 16 inputs and term of a group;
-a group's features are added up for its zero point in at most group + 3 additions, their product with it, the scale's
-and an addition of each group follow: with S = sum_k |scale_k| (code_k + zero_k) |x_k|,
-(17 terms G / 16 + G + groups + 10) 2^-24 S in all; bf16 half a step, 2^-8. Features are held to 2^-36 of their
-request's largest, m: 2^-36 m sum_k |scale_k| (code_k + zero_k) more.
+the groups' sums take the scale's product and an addition each, and 8 more roundings may follow:
+(17 terms G / 16 + groups + 10) 2^-24 sum_k |w_k x_k| in all; bf16 half a step, 2^-8. Features are held to 2^-40 of
+their request's largest, m: 2^-40 m sum_k |w_k| more.
 """
 import math
 
@@ -43,15 +42,12 @@ class Case:
         return (self.codes.double() - z) * self.scales.double()[:, of]
 
     def want(self, out):
-        of = torch.arange(self.K) // self.group
-        z = 8.0 if self.zeros is None else self.zeros.double()[:, of]
-        size = (self.codes.double() + z) * self.scales.double()[:, of].abs()
         w, x = self.weights(), self.x.double()
         y = x @ w.T
         terms = 3 if self.x.dtype is F32 else 1
         groups, G = -(-self.K // self.group), min(self.group, 32 * -(-self.K // 32))
-        eps = (17 * terms * G / 16 + G + groups + 10) * 2.0 ** -24
-        tol = eps * (x.abs() @ size.T) + 2.0 ** -36 * x.abs().amax(-1, keepdim=True) * size.sum(-1)
+        eps = (17 * terms * G / 16 + groups + 10) * 2.0 ** -24
+        tol = eps * (x.abs() @ w.abs().T) + 2.0 ** -40 * x.abs().amax(-1, keepdim=True) * w.abs().sum(-1)
         return y, tol + (2.0 ** -8 * y.abs() if out is BF16 else 0.0) + 1e-37
 
 
@@ -135,20 +131,18 @@ def test_outputs_anywhere(V, offset, pitch, dtype):
         assert (big[offset + b * pitch + V:offset + (b + 1) * pitch] == -7).all()
 
 
-def test_float32_features_of_any_size():
-    """Features of 24 significant bits, from the smallest to the largest, each alone against a code of 9 beside a zero
-    point of 8: three terms' products, each sum of them off by 2^-24 of 9 x at most, 8 x taken off in one fma, and three
-    more roundings of x: 32 2^-24 x in all."""
+def test_float32_features_to_their_last_bit():
+    """Features of 24 significant bits, from the smallest to the largest, each alone against a weight of 1."""
     K = 64
     g = torch.Generator().manual_seed(1)
     m = torch.randint(1 << 23, 1 << 24, (K,), generator=g).double()
     e = torch.linspace(-120, 100, K).round()
     x = (m * 2.0 ** e).float()
     x[0], x[1] = torch.finfo(F32).max, -torch.finfo(F32).max
-    codes = torch.full((40, K), 9, dtype=torch.uint8)             # weight 1
+    codes = torch.full((40, K), 9, dtype=torch.uint8)
     w = dels.pack_w4(codes.to(DEV), torch.ones(40, 1, dtype=BF16, device=DEV), group=64)
-    got = w.project(torch.diag(x).to(DEV)).cpu().double()
-    assert ((got - x.double()[:, None]).abs() <= 32 * 2.0 ** -24 * x.double().abs()[:, None]).all()
+    got = w.project(torch.diag(x).to(DEV)).cpu()
+    assert torch.equal(got, x[:, None].expand(K, 40))
 
 
 def test_non_finite_features_and_scales():
@@ -192,9 +186,8 @@ def test_matrix_past_4_gb():
     at = torch.cat([torch.arange(64), torch.arange(V - 200, V)]).to(DEV)
     of = torch.arange(K, device=DEV) // G
     wt = (codes[at].double() - 8) * scales[at].double()[:, of]
-    size = (codes[at].double() + 8) * scales[at].double()[:, of]
-    want, size = x.double() @ wt.T, x.double().abs() @ size.T
-    eps = (17 * 8 + 128 + 65 + 10) * 2.0 ** -24 + 2.0 ** -33
+    want, size = x.double() @ wt.T, x.double().abs() @ wt.abs().T
+    eps = (17 * 8 + 65 + 10) * 2.0 ** -24 + 2.0 ** -37
     assert ((got[:, at].double() - want).abs() <= eps * size).all()
 
 
