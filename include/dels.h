@@ -87,6 +87,18 @@ typedef enum {
 } dels_head_kind;
 
 /*
+ * A matrix [V, K] of 4-bit codes with a scale for each group of `group` inputs of a
+ * row (and a zero point, or 8):  w[v, k] = scale[v, k / group] (code[v, k] - zero[v, k / group]).
+ * `data` [device] is what dels_w4_pack wrote, 16-byte aligned.
+ */
+typedef struct {
+  const void* data;
+  int V, K;
+  int group;                     /* 32, 64 or 128 */
+  int zeros;                     /* 1: zero points of its own; 0: 8 throughout */
+} dels_w4;
+
+/*
  * Local head (short-context expert) weights. All matrices are [device],
  * row-major [out, in] like a Linear layer, dtype `wdtype` (bf16 heads run the
  * matrix products on tcgen05 tensor cores; f32 heads on CUDA cores). V is the
@@ -121,6 +133,12 @@ typedef enum {
  * activations at float32 precision, passed to the tensor cores as the exact
  * three-term bf16 expansion hi + mid + lo of each value; its feature is
  * rounded to bf16 for W_vocab like the other heads'.
+ *
+ * w_vocab4, bf16 heads only: W_vocab (W_M) as a 4-bit matrix of V rows and d_rank
+ * inputs, read in place of w_vocab, which may then be NULL: the same products, with
+ * float32 accumulation, in drafting at both temperatures and in the verification
+ * of sampled blocks. (A drafter's weights change which tokens it proposes, not what the
+ * verified output follows.)
  */
 typedef struct {
   dels_head_kind kind;
@@ -135,6 +153,7 @@ typedef struct {
   const void* emb;
   const void* w[8];
   const void* w_vocab;
+  const dels_w4* w_vocab4;       /* [host], read during a call, or NULL */
 } dels_local_head;
 
 /* ---- self test of the bounded waits ------------------------------------- */
@@ -623,19 +642,7 @@ int dels_verify_given(const int32_t* tokens, const dels_probs* target, const del
                       const int32_t* lengths, int B, int n, int V, int32_t* out_accept_len, int32_t* out_bonus,
                       void* workspace, size_t workspace_bytes, dels_stream_t stream);
 
-/* ---- products with 4-bit weights ------------------------------------------ */
-
-/*
- * A matrix [V, K] of 4-bit codes with a scale for each group of `group` inputs of a
- * row (and a zero point, or 8):  w[v, k] = scale[v, k / group] (code[v, k] - zero[v, k / group]).
- * `data` [device] is what dels_w4_pack wrote, 16-byte aligned.
- */
-typedef struct {
-  const void* data;
-  int V, K;
-  int group;                     /* 32, 64 or 128 */
-  int zeros;                     /* 1: zero points of its own; 0: 8 throughout */
-} dels_w4;
+/* ---- products with 4-bit weights (dels_w4: with the local head above) ------ */
 
 /*
  * Lays a matrix out for the products, once per set of weights.

@@ -58,6 +58,15 @@ _lib = None
 _vp, _i, _f, _d, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_double, ctypes.c_size_t
 
 
+class W4(ctypes.Structure):
+    """Mirror of ``dels_w4``."""
+
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("V", ctypes.c_int), ("K", ctypes.c_int), ("group", ctypes.c_int),
+        ("zeros", ctypes.c_int),
+    ]
+
+
 class LocalHead(ctypes.Structure):
     """Mirror of ``dels_local_head``."""
 
@@ -67,6 +76,7 @@ class LocalHead(ctypes.Structure):
         ("window", ctypes.c_int), ("n_layers", ctypes.c_int), ("n_heads", ctypes.c_int),
         ("max_pos", ctypes.c_int),
         ("emb", ctypes.c_void_p), ("w", ctypes.c_void_p * 8), ("w_vocab", ctypes.c_void_p),
+        ("w_vocab4", ctypes.POINTER(W4)),
     ]
 
 
@@ -96,15 +106,6 @@ class Probs(ctypes.Structure):
     _fields_ = [
         ("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("batch_stride", ctypes.c_longlong),
         ("row_stride", ctypes.c_longlong),
-    ]
-
-
-class W4(ctypes.Structure):
-    """Mirror of ``dels_w4``."""
-
-    _fields_ = [
-        ("data", ctypes.c_void_p), ("V", ctypes.c_int), ("K", ctypes.c_int), ("group", ctypes.c_int),
-        ("zeros", ctypes.c_int),
     ]
 
 
@@ -587,14 +588,17 @@ _SLOTS = {
 
 def make_head(spec, weights: Dict[str, torch.Tensor]) -> LocalHead:
     """LocalHead for a head spec (``kind``, ``wdtype``, dims) and a dict of device weight tensors
-    (keys emb, w_vocab and the kind's slot names). The caller keeps the tensors alive."""
+    (keys emb, w_vocab and the kind's slot names; w_vocab may be a ``W4Matrix``). The caller keeps them alive."""
     h = LocalHead()
     h.kind = _KIND[spec.kind]
     h.wdtype = DELS_BF16 if spec.wdtype == "bf16" else DELS_F32
     h.d_model, h.d_hidden, h.d_rank = spec.d_model, spec.d_hidden, spec.d_rank
     h.window, h.n_layers, h.n_heads, h.max_pos = spec.window, spec.n_layers, spec.n_heads, spec.max_pos
     h.emb = _ptr(weights["emb"])
-    h.w_vocab = _ptr(weights["w_vocab"])
+    if isinstance(weights["w_vocab"], W4Matrix):
+        h.w_vocab4 = ctypes.pointer(weights["w_vocab"].struct)
+    else:
+        h.w_vocab = _ptr(weights["w_vocab"])
     for i, name in enumerate(_SLOTS[spec.kind]):
         if name in weights:
             h.w[i] = _ptr(weights[name])

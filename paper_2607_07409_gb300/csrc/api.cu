@@ -201,6 +201,7 @@ namespace {
 // ------------------------------------------------------------- tcgen05 plans
 
 struct Gemm {
+  W4Args w4{};             // packed set: a vocabulary projection with 4-bit weights, whose other terms are in a
   TcGemmArgs a{};
   CUtensorMap mA0{}, mB0{}, mA1{}, mB1{}, mL{};
   int grid = 0;
@@ -456,7 +457,52 @@ bool plan_combine(Gemm& g, int B, int V, int n, const void* X, int K, const void
   return true;
 }
 
+// A 4-bit matrix's products with bf16 (or float32) features.
+W4Args w4_args(const dels_w4& m, const void* X, int B, int* status) {
+  W4Args a{};
+  a.packed = static_cast<const uint8_t*>(m.data);
+  a.V = m.V;
+  a.K = m.K;
+  a.group = m.group;
+  a.zeros = m.zeros != 0;
+  a.lay = w4_layout(m.V, m.K, m.group, a.zeros);
+  a.x = X;
+  a.ld_x = m.K;
+  a.B = B;
+  a.status = status;
+  return a;
+}
+
+// The vocabulary projection of a bf16 head fused with the combine, from either form of its weights.
+bool plan_vocab(Gemm& g, const dels_local_head* head, int B, int V, int n, const void* X, int K, const void* longp,
+                dels_dtype ldt, const float* prior, float alpha, float beta, void* partials, int partial_ld,
+                int* status, int sms, bool pair_stages, bool sample) {
+  if (!head->w_vocab4)
+    return plan_combine(g, B, V, n, X, K, head->w_vocab, longp, ldt, prior, alpha, beta, partials, partial_ld, status,
+                        sms, pair_stages, sample);
+  W4Args& a = g.w4 = w4_args(*head->w_vocab4, X, B, status);
+  a.longp = longp;
+  a.long_f32 = ldt == DELS_F32;
+  a.ld_long = (long long)n * V;
+  a.prior = prior;
+  a.partials = partials;
+  a.partial_ld = partial_ld;
+  g.grid = w4_records(a, sms);
+  return g.grid <= partial_ld;
+}
+
 cudaError_t run(const Gemm& g, cudaStream_t s) {
+  if (g.w4.packed) {
+    W4Args w = g.w4;
+    w.longp = static_cast<const uint8_t*>(w.longp) + (size_t)g.a.j * w.V * (w.long_f32 ? 4 : 2);
+    w.alpha = g.a.alpha;
+    w.beta = g.a.beta;
+    w.j = g.a.j;
+    w.sample = g.a.sample;
+    w.seed = g.a.seed;
+    w.step = g.a.step;
+    return launch_w4_project(w, s);
+  }
   return launch_tc_gemm(g.a, &g.mA0, &g.mB0, &g.mA1, &g.mB1, &g.mL, g.grid, g.smem, s);
 }
 
@@ -702,13 +748,24 @@ cudaError_t run_rank_hh(const Gemm& gr, const Gemm* gh, cudaStream_t s) {
   return launch_tc_gemm(gr.a, &gr.mA0, &gr.mB0, &gr.mA1, &gr.mB1, &gr.mL, gr.grid, gr.smem, s, gh ? &hh : nullptr);
 }
 
+bool w4_ok(int V, int K, int group) {
+  return V >= 1 && V <= (1 << 27) && K >= 1 && K <= 65536 && (group == 32 || group == 64 || group == 128);
+}
+
 int validate_head(const dels_local_head* h, int n) {
   if (!h) return DELS_ERR_NULL_POINTER;
   if (h->wdtype != DELS_F32 && h->wdtype != DELS_BF16) return DELS_ERR_BAD_DTYPE;
   const bool bf = h->wdtype == DELS_BF16;
   auto dim_ok = [&](int d) { return d > 0 && d <= 65536 && (!bf || d % 16 == 0) && (bf || d % 4 == 0); };
-  if (!h->emb || !h->w_vocab) return DELS_ERR_NULL_POINTER;
-  if (!aligned16(h->emb) || !aligned16(h->w_vocab)) return DELS_ERR_ALIGNMENT;
+  const dels_w4* m = h->w_vocab4;
+  if (!h->emb || (!h->w_vocab && !m)) return DELS_ERR_NULL_POINTER;
+  if (m) {
+    if (!bf) return DELS_ERR_UNSUPPORTED;
+    if (!m->data) return DELS_ERR_NULL_POINTER;
+    if (!w4_ok(m->V, m->K, m->group) || m->K != h->d_rank) return DELS_ERR_BAD_SHAPE;
+    if (!aligned16(m->data)) return DELS_ERR_ALIGNMENT;
+  }
+  if (!aligned16(h->emb) || (!m && !aligned16(h->w_vocab))) return DELS_ERR_ALIGNMENT;
   for (int i = 0; i < 8; ++i)
     if (h->w[i] && !aligned16(h->w[i])) return DELS_ERR_ALIGNMENT;
   switch (h->kind) {
@@ -748,6 +805,7 @@ int validate_draft(const dels_local_head* head, const void* long_logits, dels_dt
   if (ldt != DELS_F32 && ldt != DELS_BF16) return DELS_ERR_BAD_DTYPE;
   int r = validate_head(head, n);
   if (r != DELS_OK) return r;
+  if (head->w_vocab4 && head->w_vocab4->V != V) return DELS_ERR_BAD_SHAPE;
   if (B == 0) return DELS_OK;
   if (!long_logits || !prior || !tok || !lp) return DELS_ERR_NULL_POINTER;
   if (!aligned16(long_logits) || !aligned16(prior) || !aligned16(tok) || !aligned16(lp) || (gap && !aligned16(gap)))
@@ -830,7 +888,7 @@ using namespace dels;
 
 extern "C" {
 
-int dels_version(void) { return 200; }
+int dels_version(void) { return 300; }
 
 int dels_profile_enable(int on) {
   prof::on = on != 0;
@@ -1483,14 +1541,14 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
       mb.D = D;
       mb.dest = eg;
       mb.smp.src_r = rr;
-      if (bf && persistent_enabled() && !alpha_j && !beta_j && !sm.on && B <= sms && R <= 256) {
+      if (bf && !head->w_vocab4 && persistent_enabled() && !alpha_j && !beta_j && !sm.on && B <= sms && R <= 256) {
         // one cooperative launch for the whole block
         Gemm gg, gr, gv;
         if (!plan_store(gg, B, 3 * H, eg, head->w[0], D, hb, head->w[1], H, 128, L.gru_s0, L.gru_s1, ACT_NONE,
                         gpart, nullptr, 0, status, sms) ||
             !plan_store(gr, B, R, hb, head->w[2], H, nullptr, nullptr, 0, 32, 1, 0, ACT_SILU, nullptr,
                         static_cast<uint16_t*>(rr), R, status, sms) ||
-            !plan_combine(gv, B, V, n, rr, R, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
+            !plan_vocab(gv, head, B, V, n, rr, R, long_logits, logit_dtype, log_prior, alpha, beta,
                           partials, L.partial_ld, status, sms, false, sm.on))
           return DELS_ERR_CUDA;
         PersistGruArgs P{};
@@ -1536,7 +1594,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
         }
       }
       const float* G = static_cast<const float*>(head->w[3]);
-      if (bf && G && fused_products_enabled() && !sm.on && B <= 64 && n > 1) {
+      if (bf && !head->w_vocab4 && G && fused_products_enabled() && !sm.on && B <= 64 && n > 1) {
         // Input-table path, fused variant (DELS_DRAFT_FUSED=1): two launches
         // per position —
         //   gates(j)        merge x_{j-1} from the previous position's records,
@@ -1552,7 +1610,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
                         ACT_SILU, nullptr, static_cast<uint16_t*>(rr), R, status, sms) ||
             !plan_store(gh, B, 3 * H, hb, head->w[1], H, nullptr, nullptr, 0, kHhTile, L.hh_splits, 0, ACT_NONE,
                         gpart, nullptr, 0, status, sms) ||
-            !plan_combine(gv, B, V, n, rr, R, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
+            !plan_vocab(gv, head, B, V, n, rr, R, long_logits, logit_dtype, log_prior, alpha, beta,
                           partials, L.partial_ld, status, sms, false, sm.on))
           return DELS_ERR_CUDA;
         // the rank product's K splits form one cluster per output tile
@@ -1639,7 +1697,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
         if (r != DELS_OK) return r;
         Gemm gr, gh, gv;
         if (!plan_rank_hh(gr, gh, head, L, B, hb, static_cast<uint16_t*>(rr), gpart, status) ||
-            !plan_combine(gv, B, V, n, rr, R, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
+            !plan_vocab(gv, head, B, V, n, rr, R, long_logits, logit_dtype, log_prior, alpha, beta,
                           partials, L.partial_ld, status, sms, true, sm.on))
           return DELS_ERR_CUDA;
         GatesTableArgs ga{};
@@ -1692,7 +1750,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
         if (!plan_store(gi, B, 3 * H, eg, head->w[0], D, nullptr, nullptr, 0, 128, L.ih_splits, 0, ACT_NONE, gpart,
                         nullptr, 0, status, sms) ||
             !plan_rank_hh(gr, gh, head, L, B, hb, static_cast<uint16_t*>(rr), hh_part, status) ||
-            !plan_combine(gv, B, V, n, rr, R, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
+            !plan_vocab(gv, head, B, V, n, rr, R, long_logits, logit_dtype, log_prior, alpha, beta,
                           partials, L.partial_ld, status, sms, true, sm.on))
           return DELS_ERR_CUDA;
         for (int j = 1; j < n; ++j) {
@@ -1768,7 +1826,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
             !plan_store(g2, B, Hd, h1, head->w[1], Hd, nullptr, nullptr, 0, 128, L.mlp_s2, 0, ACT_NONE, mpart,
                         nullptr, 0, status, sms))
           return DELS_ERR_CUDA;
-        if (!plan_combine(gv, B, V, n, feat, Hd, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
+        if (!plan_vocab(gv, head, B, V, n, feat, Hd, long_logits, logit_dtype, log_prior, alpha, beta,
                           partials, L.partial_ld, status, sms, true, sm.on))
           return DELS_ERR_CUDA;
         for (int j = 1; j < n; ++j) {
@@ -1856,7 +1914,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
                 plan_store_rows(go, B, T, D, ob, head->w[4], D, L.xs_o, xpart, status, sms) &&
                 plan_store_rows(g1, B, T, F, anb, head->w[5], D, L.xs_1, xpart, status, sms) &&
                 plan_store_rows(g2, B, T, D, fb, head->w[6], F, L.xs_2, xpart, status, sms) &&
-                plan_combine(gv, B, V, n, feat, D, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
+                plan_vocab(gv, head, B, V, n, feat, D, long_logits, logit_dtype, log_prior, alpha, beta,
                              partials, L.partial_ld, status, sms, true, sm.on);
       if (!ok) return DELS_ERR_CUDA;
       const int Sqkv = gqkv.g[0].a.total_splits;
@@ -1892,7 +1950,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
       r = draft_position0(long_logits, logit_dtype, B, n, V, partials, L.partial_ld, status, mb, sms, s);
       if (r != DELS_OK || n == 1) return r;
       Gemm gv;
-      if (bf && !plan_combine(gv, B, V, n, feat, R, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
+      if (bf && !plan_vocab(gv, head, B, V, n, feat, R, long_logits, logit_dtype, log_prior, alpha, beta,
                               partials, L.partial_ld, status, sms, true, sm.on))
         return DELS_ERR_CUDA;
       for (int j = 1; j < n; ++j) {
@@ -2028,8 +2086,14 @@ int dels_verify_block_sampled(const dels_local_head* head, const int32_t* draft_
   if (!workspace) return DELS_ERR_WORKSPACE;
   if (B == 0) return DELS_OK;
   if (!draft_tokens || !draft_logprob || !draft_state || !long_logits || !target_logits || !out_accept_len ||
-      !out_bonus || !head->w_vocab)
+      !out_bonus || (!head->w_vocab && !head->w_vocab4))
     return DELS_ERR_NULL_POINTER;
+  if (const dels_w4* m = head->w_vocab4) {
+    if (!bf) return DELS_ERR_UNSUPPORTED;
+    if (!m->data) return DELS_ERR_NULL_POINTER;
+    if (!w4_ok(m->V, m->K, m->group) || m->K != head->d_rank || m->V != V) return DELS_ERR_BAD_SHAPE;
+    if (!aligned16(m->data)) return DELS_ERR_ALIGNMENT;
+  }
   const size_t es_w = bf ? 2 : 4;
   if (((size_t)head->d_rank * es_w) % 16 != 0) return DELS_ERR_UNSUPPORTED;
   if (!aligned16(workspace) || !aligned16(draft_state) || !aligned16(target_logits) || !aligned16(long_logits))
@@ -2092,7 +2156,13 @@ int dels_verify_block_sampled(const dels_local_head* head, const int32_t* draft_
   a.status = status;
   { PROF(DELS_KCLASS_VERIFY); DELS_CUDA(launch_verify_accept(a, s)); }
   // 3. l_S of the rejected positions: W_vocab r (rows with no head input are zero)
-  if (bf) {
+  if (head->w_vocab4) {
+    W4Args w = w4_args(*head->w_vocab4, a.rg, B, status);
+    w.out = at<float>(workspace, L.ls);
+    w.out_f32 = 1;
+    w.ld_out = V;
+    { PROF(DELS_KCLASS_VERIFY); DELS_CUDA(launch_w4_project(w, s)); }
+  } else if (bf) {
     Gemm g;
     if (!plan_store(g, B, V, a.rg, head->w_vocab, head->d_rank, nullptr, nullptr, 0, 128, 1, 0, ACT_NONE,
                     at<float>(workspace, L.ls), nullptr, 0, status, sms))
@@ -2468,10 +2538,6 @@ int dels_verify_given(const int32_t* tokens, const dels_probs* target, const del
 
 // --------------------------------------------------- products with 4-bit weights
 
-static bool w4_ok(int V, int K, int group) {
-  return V >= 1 && V <= (1 << 27) && K >= 1 && K <= 65536 && (group == 32 || group == 64 || group == 128);
-}
-
 static int w4_matrix(const dels_w4* w) {
   if (!w || !w->data) return DELS_ERR_NULL_POINTER;
   if (!w4_ok(w->V, w->K, w->group)) return DELS_ERR_BAD_SHAPE;
@@ -2527,21 +2593,12 @@ int dels_w4_project(const dels_w4* w, const void* x, dels_dtype x_dtype, long lo
   if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(x) & (x_dtype == DELS_F32 ? 3u : 1u)) ||
       (reinterpret_cast<uintptr_t>(out) & (out_dtype == DELS_F32 ? 3u : 1u)))
     return DELS_ERR_ALIGNMENT;
-  W4Args a{};
-  a.packed = static_cast<const uint8_t*>(w->data);
-  a.V = w->V;
-  a.K = w->K;
-  a.group = w->group;
-  a.zeros = w->zeros != 0;
-  a.lay = w4_layout(w->V, w->K, w->group, a.zeros);
-  a.x = x;
+  W4Args a = w4_args(*w, x, B, at<int>(workspace, 0));
   a.x_f32 = x_dtype == DELS_F32;
   a.ld_x = ld_x;
-  a.B = B;
   a.out = out;
   a.out_f32 = out_dtype == DELS_F32;
   a.ld_out = ld_out;
-  a.status = at<int>(workspace, 0);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   PROF(DELS_KCLASS_W4);
   if (launch_w4_project(a, s) != cudaSuccess) return DELS_ERR_CUDA;

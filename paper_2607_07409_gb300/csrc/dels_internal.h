@@ -269,7 +269,19 @@ struct W4Args {
   int out_f32;
   long long ld_out;
   int* status;
+  // Fused with the combine, in place of outputs: records of l_L + alpha y - beta l_P (bf16 features).
+  const void* longp;             // position j's rows
+  int long_f32;
+  long long ld_long;
+  const float* prior;            // [V]
+  float alpha, beta;
+  int j, sample;                 // temperature 1: keys with the Gumbel variates of (seed, step)
+  unsigned long long seed, step;
+  void* partials;                // [B][partial_ld] RowAcc, a record a CTA: null for outputs
+  int partial_ld;
 };
+// Records per request of a launch that is fused with the combine.
+int w4_records(const W4Args& a, int sms);
 cudaError_t launch_w4_project(const W4Args& a, cudaStream_t s);
 
 // ---- draft merge + gather of the next local-head input ----------------------

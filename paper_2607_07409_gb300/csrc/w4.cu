@@ -268,7 +268,43 @@ __device__ __forceinline__ void issue_products(uint32_t dcol, uint32_t acol, uin
         }
 }
 
-template <int NB, int TERMS>
+// What a launch does with its products: outputs, or records of the fused rows at temperature 0 or 1.
+enum { kOutputs = 0, kRecords = 1, kKeys = 2 };
+
+// The four values that lanes 4 q .. 4 q + 3 have for one another: lane i's x[k] becomes lane k's x[i].
+__device__ __forceinline__ void exchange4(float (&x)[4]) {
+  const int lane = threadIdx.x;
+#pragma unroll
+  for (int d = 1; d < 4; d <<= 1) {
+    const bool up = lane & d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i & d) continue;
+      const float mine = up ? x[i] : x[i | d], other = __shfl_xor_sync(0xFFFFFFFFu, mine, d);
+      if (up) x[i] = other;
+      else x[i | d] = other;
+    }
+  }
+}
+
+// A warp's record of 32 rows' values l (their keys k at temperature 1) from vocabulary index v0 on, in every lane.
+__device__ __forceinline__ RowAcc warp_record(float l, float k, int v0) {
+  const int lane = threadIdx.x & 31;
+  const bool nan = __any_sync(0xFFFFFFFFu, k != k);
+  if (k != k) k = -INFINITY;
+  RowAcc r;
+  r.m = warp_max(k);
+  const int who = __ffs(__ballot_sync(0xFFFFFFFFu, k == r.m)) - 1;
+  r.idx = v0 + who;
+  r.second = warp_max(lane == who ? -INFINITY : k);
+  r.s = r.m == -INFINITY ? 0.f : ex2_approx((l - r.m) * kLog2e);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, d);
+  if (nan) r.s = NAN;
+  return r;
+}
+
+template <int NB, int TERMS, int EPI>
 __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4Args a, const W4Plan p) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int N = NB < 16 ? 16 : NB;                  // requests of an MMA: rows past NB are its first ones again
@@ -416,6 +452,10 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   uint32_t base = 0x64006400u;
   asm("" : "+r"(base));                   // (a register, not a constant)
   f32x2 tot[NB / 2];
+  constexpr int kRecs = (NB + 31) / 32;
+  RowAcc recs[kRecs];                       // of the fused rows: lane n % 32 has request n's
+#pragma unroll
+  for (int i = 0; i < kRecs; ++i) recs[i] = rowacc_init();
   // apart in time: in step, all groups' codes wait for the ALU pipe and then all groups for their products
   __nanosleep(grp * 200);
 
@@ -523,23 +563,81 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       else if (glog == 1) run(blocks, step_units, two);
       else run(blocks, step_units, four);
     }
-    // ---- outputs: a warp's 32 rows side by side
     const long long v = tile * kW4Rows + row;
-    if (live && v < a.V) {
-      const int nb = min(NB, a.B - b0);
+    const int nb = min(NB, a.B - b0);
+    if constexpr (EPI == kOutputs) {
+      // ---- outputs: a warp's 32 rows side by side
+      if (live && v < a.V) {
 #pragma unroll
-      for (int n = 0; n < NB; n += 2) {
-        float y[2];
-        split2(tot[n / 2], y[0], y[1]);
+        for (int n = 0; n < NB; n += 2) {
+          float y[2];
+          split2(tot[n / 2], y[0], y[1]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (n + i >= nb) break;
-          const float out = y[i] * back[n + i].x * back[n + i].y;
-          const long long at = (long long)(b0 + n + i) * a.ld_out + v;
-          if (a.out_f32) static_cast<float*>(a.out)[at] = out;
-          else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(out);
+          for (int i = 0; i < 2; ++i) {
+            if (n + i >= nb) break;
+            const float out = y[i] * back[n + i].x * back[n + i].y;
+            const long long at = (long long)(b0 + n + i) * a.ld_out + v;
+            if (a.out_f32) static_cast<float*>(a.out)[at] = out;
+            else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(out);
+          }
         }
       }
+    } else if (live) {
+      // ---- records of the fused rows: a warp's 32 of each request, lane n % 32 keeps request n's
+      const bool there = v < a.V;
+      const float prior = there ? __ldg(a.prior + v) : 0.f;
+      RowAcc now[kRecs];
+#pragma unroll
+      for (int n = 0; n < NB; n += 4) {
+        if (n >= nb) break;
+        float g[4] = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (EPI == kKeys) {
+          // lane i of four computes the words of the four rows for request n + i
+          uint32_t w[4];
+          philox_block(a.seed, a.step, b0 + n + (lane & 3), a.j, kStreamDraft, v >> 2, w);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) g[i] = gumbel_from_bits(w[i]);
+          exchange4(g);
+        }
+        float l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const long long at = (long long)(b0 + n + i) * a.ld_long + v;
+          l[i] = -INFINITY;
+          if (n + i < nb && there)
+            l[i] = a.long_f32 ? __ldg(static_cast<const float*>(a.longp) + at)
+                              : bf16_to_f(__ldg(static_cast<const uint16_t*>(a.longp) + at));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (n + i >= nb) break;
+          float y[2];
+          split2(tot[(n + i) / 2], y[0], y[1]);
+          const float out = y[i & 1] * back[n + i].x * back[n + i].y;
+          const float f = there ? fmaf(-a.beta, prior, fmaf(a.alpha, out, l[i])) : -INFINITY;
+          const RowAcc r = warp_record(f, EPI == kKeys ? f + g[i] : f, (int)(v - lane));
+          if (lane == ((n + i) & 31)) now[(n + i) / 32] = r;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kRecs; ++i)
+        if (lane + 32 * i < nb) recs[i] = rowacc_merge(recs[i], now[i]);
+      __syncwarp();
+    }
+  }
+  if constexpr (EPI != kOutputs) {
+    // ---- the CTA's records, through the ring's memory
+    __syncthreads();
+    RowAcc* all_recs = reinterpret_cast<RowAcc*>(smem);                  // [warps][NB]
+#pragma unroll
+    for (int i = 0; i < kRecs; ++i)
+      if (lane + 32 * i < NB) all_recs[warp * NB + lane + 32 * i] = recs[i];
+    __syncthreads();
+    if (tid < min(NB, a.B - b0)) {
+      RowAcc r = all_recs[tid];
+      for (int w = 1; w < warps; ++w) r = rowacc_merge(r, all_recs[w * NB + tid]);
+      reinterpret_cast<float4*>(a.partials)[(long long)(b0 + tid) * a.partial_ld + blockIdx.x] =
+          make_float4(r.m, r.s, r.second, __int_as_float(r.idx));
     }
   }
   if (dead) {
@@ -558,11 +656,17 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   if (warp == 0) tmem_dealloc(tmem_base, p.tmem_cols);
 }
 
-template <int NB, int TERMS>
+int w4_ctas(const W4Args& a, int NB, int sms) {
+  const int btiles = (a.B + NB - 1) / NB;
+  return (int)std::min<long long>(std::max(1, sms / btiles), a.lay.tiles);
+}
+int w4_requests(int B) { return B <= 8 ? 8 : B <= 16 ? 16 : B <= 32 ? 32 : 64; }    // of a CTA
+
+template <int NB, int TERMS, int EPI>
 cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const int sms = device_sm_count(), room = device_max_smem_optin() - 4096;
   if (sms <= 0 || room <= 0) return cudaErrorInvalidValue;
-  const int btiles = (a.B + NB - 1) / NB, ctas = (int)std::min<long long>(std::max(1, sms / btiles), a.lay.tiles);
+  const int btiles = (a.B + NB - 1) / NB, ctas = w4_ctas(a, NB, sms);
   W4Plan p{};
   constexpr int N = NB < 16 ? 16 : NB;
   const int gunits = a.group / kW4Unit;
@@ -584,7 +688,7 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   p.parts = (4 * a.lay.blocks + p.part_units - 1) / p.part_units;
   p.stages = (int)std::min<long long>(kW4Stages, (room - p.part_units * unit) / ((long long)p.groups * p.stage_bytes));
   p.smem = (int)(p.groups * p.stages * p.stage_bytes + p.part_units * unit);
-  const auto k = k_w4_project<NB, TERMS>;
+  const auto k = k_w4_project<NB, TERMS, EPI>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);
   if (e != cudaSuccess) return e;
   return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * 128), (size_t)p.smem, s, a, p);
@@ -597,15 +701,24 @@ cudaError_t launch_w4_pack(const W4PackArgs& a, cudaStream_t s) {
   return launch_pdl(k_w4_pack, grid, dim3(kPackThreads), 0, s, a);
 }
 
+int w4_records(const W4Args& a, int sms) { return w4_ctas(a, w4_requests(a.B), sms); }
+
 cudaError_t launch_w4_project(const W4Args& a, cudaStream_t s) {
-  if (a.x_f32) {
-    if (a.B <= 8) return launch_nb<8, 3>(a, s);
-    if (a.B <= 16) return launch_nb<16, 3>(a, s);
-    return a.B <= 32 ? launch_nb<32, 3>(a, s) : launch_nb<64, 3>(a, s);
-  }
-  if (a.B <= 8) return launch_nb<8, 1>(a, s);
-  if (a.B <= 16) return launch_nb<16, 1>(a, s);
-  return a.B <= 32 ? launch_nb<32, 1>(a, s) : launch_nb<64, 1>(a, s);
+  const auto launch = [&](auto terms, auto epi) {
+    constexpr int T = decltype(terms)::value, E = decltype(epi)::value;
+    switch (w4_requests(a.B)) {
+      case 8: return launch_nb<8, T, E>(a, s);
+      case 16: return launch_nb<16, T, E>(a, s);
+      case 32: return launch_nb<32, T, E>(a, s);
+      default: return launch_nb<64, T, E>(a, s);
+    }
+  };
+  using std::integral_constant;
+  if (a.partials)
+    return a.sample ? launch(integral_constant<int, 1>{}, integral_constant<int, kKeys>{})
+                    : launch(integral_constant<int, 1>{}, integral_constant<int, kRecords>{});
+  return a.x_f32 ? launch(integral_constant<int, 3>{}, integral_constant<int, kOutputs>{})
+                 : launch(integral_constant<int, 1>{}, integral_constant<int, kOutputs>{});
 }
 
 }  // namespace dels
