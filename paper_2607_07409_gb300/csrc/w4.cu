@@ -271,37 +271,68 @@ __device__ __forceinline__ void issue_products(uint32_t dcol, uint32_t acol, uin
 // What a launch does with its products: outputs, or records of the fused rows at temperature 0 or 1.
 enum { kOutputs = 0, kRecords = 1, kKeys = 2 };
 
-// The four values that lanes 4 q .. 4 q + 3 have for one another: lane i's x[k] becomes lane k's x[i].
-__device__ __forceinline__ void exchange4(float (&x)[4]) {
-  const int lane = threadIdx.x;
-#pragma unroll
-  for (int d = 1; d < 4; d <<= 1) {
-    const bool up = lane & d;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i & d) continue;
-      const float mine = up ? x[i] : x[i | d], other = __shfl_xor_sync(0xFFFFFFFFu, mine, d);
-      if (up) x[i] = other;
-      else x[i | d] = other;
-    }
-  }
+// The fused rows' records: a group of warps lays a tile's products out by requests, 32 at a time, and
+// every thread goes along as many columns of one: 8 of its products, logits and priors a step. (Each
+// warp's 32 rows of every request by shuffles, with no layout between, took 64 requests' block
+// of 16 2.4 ms.)
+template <int NB>
+constexpr int kW4Side = NB < 32 ? NB : 32;             // requests laid out at a time, and a thread's columns
+constexpr int kW4Pitch = kW4Rows + 4;
+struct RowTop {
+  float best, second, m, s;                            // m: the sum's reference
+  int idx;
+};
+
+// One product of the thread's own row: what one and two requests take, with no layout (0.59 ms a block of 16
+// where it took 0.67).
+template <bool KEYS>
+__device__ __forceinline__ void combine_one(const W4Args& a, float y, int b, long long v, RowTop& r) {
+  const long long at = b * a.ld_long + v;
+  const float l = a.long_f32 ? __ldcs(static_cast<const float*>(a.longp) + at)
+                             : bf16_to_f(__ldcs(static_cast<const uint16_t*>(a.longp) + at));
+  const float f[1] = {fmaf(-a.beta, __ldg(a.prior + v), fmaf(a.alpha, y, l))};
+  top2_push(KEYS ? f[0] + gumbel_at(a.seed, a.step, b, a.j, kStreamDraft, v) : f[0], (int)v, r.best, r.second, r.idx);
+  lse_chunk_ex2<1>(f, r.best, r.m, r.s);
 }
 
-// A warp's record of 32 rows' values l (their keys k at temperature 1) from vocabulary index v0 on, in every lane.
-__device__ __forceinline__ RowAcc warp_record(float l, float k, int v0) {
-  const int lane = threadIdx.x & 31;
-  const bool nan = __any_sync(0xFFFFFFFFu, k != k);
-  if (k != k) k = -INFINITY;
-  RowAcc r;
-  r.m = warp_max(k);
-  const int who = __ffs(__ballot_sync(0xFFFFFFFFu, k == r.m)) - 1;
-  r.idx = v0 + who;
-  r.second = warp_max(lane == who ? -INFINITY : k);
-  r.s = r.m == -INFINITY ? 0.f : ex2_approx((l - r.m) * kLog2e);
+template <int S, bool KEYS>
+__device__ __forceinline__ void combine_columns(const W4Args& a, const float* y, int b, long long v0, RowTop& r) {
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, d);
-  if (nan) r.s = NAN;
-  return r;
+  for (int c = 0; c < S; c += 8) {
+    const long long v = v0 + c;
+    if (v >= a.V) return;                              // (V is a multiple of 8)
+    const float4 y0 = *reinterpret_cast<const float4*>(y + c), y1 = *reinterpret_cast<const float4*>(y + c + 4);
+    const float4 p0 = __ldg(reinterpret_cast<const float4*>(a.prior + v));
+    const float4 p1 = __ldg(reinterpret_cast<const float4*>(a.prior + v + 4));
+    float f[8];
+    if (a.long_f32) {
+      const float4* l = reinterpret_cast<const float4*>(static_cast<const float*>(a.longp) + b * a.ld_long + v);
+      const float4 l0 = __ldcs(l), l1 = __ldcs(l + 1);
+      f[0] = l0.x; f[1] = l0.y; f[2] = l0.z; f[3] = l0.w; f[4] = l1.x; f[5] = l1.y; f[6] = l1.z; f[7] = l1.w;
+    } else {
+      const uint4 l = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.longp) + b * a.ld_long + v));
+      f[0] = bf16lo(l.x); f[1] = bf16hi(l.x); f[2] = bf16lo(l.y); f[3] = bf16hi(l.y);
+      f[4] = bf16lo(l.z); f[5] = bf16hi(l.z); f[6] = bf16lo(l.w); f[7] = bf16hi(l.w);
+    }
+    const float yy[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+    const float pp[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+    float k[8], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = f[i] = fmaf(-a.beta, pp[i], fmaf(a.alpha, yy[i], f[i]));
+    if constexpr (KEYS) {
+      float g[8];
+      gumbel8(a.seed, a.step, b, a.j, kStreamDraft, v >> 3, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) k[i] += g[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, k[i]);
+    if (top > r.second) {                              // (others change neither the largest nor the runner-up)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top2_push(k[i], (int)v + i, r.best, r.second, r.idx);
+    }
+    lse_chunk_ex2<8>(f, r.best, r.m, r.s);
+  }
 }
 
 template <int NB, int TERMS, int EPI>
@@ -452,10 +483,13 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   uint32_t base = 0x64006400u;
   asm("" : "+r"(base));                   // (a register, not a constant)
   f32x2 tot[NB / 2];
-  constexpr int kRecs = (NB + 31) / 32;
-  RowAcc recs[kRecs];                       // of the fused rows: lane n % 32 has request n's
+  constexpr int S = kW4Side<NB>;
+  float* sides = reinterpret_cast<float*>(operand + (size_t)TERMS * p.part_units * 4 * NB);      // of the records
+  const bool own_rows = EPI != kOutputs && NB == 8 && a.B <= 2;
+  constexpr int kTops = NB == 8 ? 2 : NB / S;
+  RowTop tops[kTops];                       // of requests row % S, row % S + S; of 0 and 1 where these have their own rows
 #pragma unroll
-  for (int i = 0; i < kRecs; ++i) recs[i] = rowacc_init();
+  for (int h = 0; h < kTops; ++h) tops[h] = RowTop{-INFINITY, -INFINITY, -INFINITY, 0.f, 0x7FFFFFFF};
   // apart in time: in step, all groups' codes wait for the ALU pipe and then all groups for their products
   __nanosleep(grp * 200);
 
@@ -582,60 +616,67 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
           }
         }
       }
-    } else if (live) {
-      // ---- records of the fused rows: a warp's 32 of each request, lane n % 32 keeps request n's
-      const bool there = v < a.V;
-      const float prior = there ? __ldg(a.prior + v) : 0.f;
-      RowAcc now[kRecs];
+    } else if (live && own_rows) {
+      if (v < a.V) {
 #pragma unroll
-      for (int n = 0; n < NB; n += 4) {
-        if (n >= nb) break;
-        float g[4] = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (EPI == kKeys) {
-          // lane i of four computes the words of the four rows for request n + i
-          uint32_t w[4];
-          philox_block(a.seed, a.step, b0 + n + (lane & 3), a.j, kStreamDraft, v >> 2, w);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) g[i] = gumbel_from_bits(w[i]);
-          exchange4(g);
-        }
-        float l[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const long long at = (long long)(b0 + n + i) * a.ld_long + v;
-          l[i] = -INFINITY;
-          if (n + i < nb && there)
-            l[i] = a.long_f32 ? __ldg(static_cast<const float*>(a.longp) + at)
-                              : bf16_to_f(__ldg(static_cast<const uint16_t*>(a.longp) + at));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (n + i >= nb) break;
+        for (int n = 0; n < 2; ++n) {
+          if (n >= nb) break;
           float y[2];
-          split2(tot[(n + i) / 2], y[0], y[1]);
-          const float out = y[i & 1] * back[n + i].x * back[n + i].y;
-          const float f = there ? fmaf(-a.beta, prior, fmaf(a.alpha, out, l[i])) : -INFINITY;
-          const RowAcc r = warp_record(f, EPI == kKeys ? f + g[i] : f, (int)(v - lane));
-          if (lane == ((n + i) & 31)) now[(n + i) / 32] = r;
+          split2(tot[0], y[0], y[1]);
+          combine_one<EPI == kKeys>(a, y[n] * back[n].x * back[n].y, b0 + n, v, tops[n]);
         }
       }
+    } else if (live) {
+      // ---- records of the fused rows
+      float* side = sides + (size_t)grp * S * kW4Pitch;
 #pragma unroll
-      for (int i = 0; i < kRecs; ++i)
-        if (lane + 32 * i < nb) recs[i] = rowacc_merge(recs[i], now[i]);
-      __syncwarp();
+      for (int h = 0; h < NB / S; ++h) {
+        if (h * S >= nb) break;
+#pragma unroll
+        for (int n = 0; n < S; n += 2) {
+          float y[2];
+          split2(tot[(h * S + n) / 2], y[0], y[1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float2 f = back[h * S + n + i];
+            side[(n + i) * kW4Pitch + row] = y[i] * f.x * f.y;
+          }
+        }
+        asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
+        const int n = row % S, c0 = row / S * S;
+        if (h * S + n < nb)
+          combine_columns<S, EPI == kKeys>(a, side + n * kW4Pitch + c0, b0 + h * S + n, tile * kW4Rows + c0, tops[h]);
+        asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
+      }
     }
   }
   if constexpr (EPI != kOutputs) {
-    // ---- the CTA's records, through the ring's memory
+    // ---- the CTA's records, one a thread, through the rings' memory
     __syncthreads();
-    RowAcc* all_recs = reinterpret_cast<RowAcc*>(smem);                  // [warps][NB]
+    float4* all_recs = reinterpret_cast<float4*>(smem);                  // [groups][128 / S][NB], or [warps][NB]
+    if (own_rows) {
 #pragma unroll
-    for (int i = 0; i < kRecs; ++i)
-      if (lane + 32 * i < NB) all_recs[warp * NB + lane + 32 * i] = recs[i];
+      for (int n = 0; n < 2; ++n) {
+        RowAcc r;
+        r.m = tops[n].best; r.s = tops[n].s; r.second = tops[n].second; r.idx = tops[n].idx;
+        r = rowacc_warp_reduce(r);
+        if (lane == 0) all_recs[warp * NB + n] = make_float4(r.m, r.s, r.second, __int_as_float(r.idx));
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < NB / S; ++h)
+        all_recs[(grp * (128 / S) + row / S) * NB + h * S + row % S] =
+            make_float4(tops[h].best, tops[h].s, tops[h].second, __int_as_float(tops[h].idx));
+    }
     __syncthreads();
     if (tid < min(NB, a.B - b0)) {
-      RowAcc r = all_recs[tid];
-      for (int w = 1; w < warps; ++w) r = rowacc_merge(r, all_recs[w * NB + tid]);
+      RowAcc r = rowacc_init();
+      for (int i = 0; i < (own_rows ? warps : p.groups * (128 / S)); ++i) {
+        const float4 x = all_recs[i * NB + tid];
+        RowAcc o;
+        o.m = x.x; o.s = x.y; o.second = x.z; o.idx = __float_as_int(x.w);
+        r = rowacc_merge(r, o);
+      }
       reinterpret_cast<float4*>(a.partials)[(long long)(b0 + tid) * a.partial_ld + blockIdx.x] =
           make_float4(r.m, r.s, r.second, __int_as_float(r.idx));
     }
@@ -664,7 +705,9 @@ int w4_requests(int B) { return B <= 8 ? 8 : B <= 16 ? 16 : B <= 32 ? 32 : 64; }
 
 template <int NB, int TERMS, int EPI>
 cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
-  const int sms = device_sm_count(), room = device_max_smem_optin() - 4096;
+  const int sms = device_sm_count();
+  const int side = EPI == kOutputs ? 0 : kW4Groups<NB> * kW4Side<NB> * kW4Pitch * 4;
+  const int room = device_max_smem_optin() - 4096 - side;
   if (sms <= 0 || room <= 0) return cudaErrorInvalidValue;
   const int btiles = (a.B + NB - 1) / NB, ctas = w4_ctas(a, NB, sms);
   W4Plan p{};
@@ -687,7 +730,7 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   p.part_units = (int)(std::min(whole, beside) / unit / 4 * 4);
   p.parts = (4 * a.lay.blocks + p.part_units - 1) / p.part_units;
   p.stages = (int)std::min<long long>(kW4Stages, (room - p.part_units * unit) / ((long long)p.groups * p.stage_bytes));
-  p.smem = (int)(p.groups * p.stages * p.stage_bytes + p.part_units * unit);
+  p.smem = (int)(p.groups * p.stages * p.stage_bytes + p.part_units * unit) + side;
   const auto k = k_w4_project<NB, TERMS, EPI>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);
   if (e != cudaSuccess) return e;
