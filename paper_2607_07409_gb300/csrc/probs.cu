@@ -17,26 +17,18 @@
 namespace dels {
 namespace {
 
-// 2^(d c), d = x - m <= 0 (or NaN), c + c_lo = log2(e) / T, c_lo > 0: d c is split into a whole
-// number n and the rest, which an fma has exactly but for c's own rounding; the second fma puts
-// that right. (z = d c rounded, and c too, took up to 40 2^-24 of a value 20 below the
-// largest.) n comes from an addition that leaves it in a float's low bits: conversions issue
-// at an eighth of its rate, as the exponential does. Below 2^-126: 0, as for d = -inf (c_lo > 0
-// keeps that from being NaN, which stays NaN). In pairs: two roundings an instruction.
+// 2^(d c), d = x - m <= 0 (or NaN), c + c_lo = log2(e) / T. d c takes one rounding, which differs from
+// entry to entry; c's own would be the same in all of them, and the second fma puts it right
+// (without it probabilities were off by 6e-7 of the row's norm, a library's softmax by 1.5e-7). c_lo > 0
+// keeps d = -inf from being NaN, which stays NaN. In pairs: two roundings an instruction. (d c split
+// into a whole number and the rest took three times the instructions, for a tenth of the error left.)
 struct Exponent {
   float m, c, c_lo;
   __device__ __forceinline__ f32x2 two(f32x2 x) const {
-    constexpr float kWhole = 12582912.f;                  // 1.5 2^23
-    const f32x2 d = add2(x, both2(-m)), c2 = both2(c);
-    float t0, t1, f0, f1;
-    split2(fma2(d, c2, both2(kWhole)), t0, t1);
-    t0 = fmaxf(t0, kWhole - 126.f);
-    t1 = fmaxf(t1, kWhole - 126.f);
-    const f32x2 minus_n = add2(both2(kWhole), pair2(-t0, -t1));
-    split2(fma2(d, both2(c_lo), fma2(d, c2, minus_n)), f0, f1);
-    const f32x2 power = pair2(__int_as_float((__float_as_int(t0) << 23) + 0x3F800000),
-                              __int_as_float((__float_as_int(t1) << 23) + 0x3F800000));
-    return mul2(pair2(ex2_approx(f0), ex2_approx(f1)), power);
+    const f32x2 d = add2(x, both2(-m));
+    float z0, z1;
+    split2(fma2(d, both2(c_lo), mul2(d, both2(c))), z0, z1);
+    return pair2(ex2_approx(z0), ex2_approx(z1));
   }
   __device__ __forceinline__ float operator()(float x) const {
     float a, b;
