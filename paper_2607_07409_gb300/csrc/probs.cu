@@ -114,29 +114,81 @@ __global__ void __launch_bounds__(kStreamThreads, F == kPlain ? 5 : 3) k_row_pro
   };
 
   float m = -INFINITY;                      // (NaN shows in the sums)
-  each([&](float (&x)[8], int k) {
-    m = fmaxf(m, max8(x));
-    if constexpr (HOLD) {
-      if (VEC && k + kHalf<T> + 4 <= k1) {
-        if constexpr (sizeof(H) == 2) {
-          uint32_t w[4];
+  const auto hold = [&](const float (&x)[8], int k) {
+    if (VEC && k + kHalf<T> + 4 <= k1) {
+      if constexpr (sizeof(H) == 2) {
+        uint32_t w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632);
-          *reinterpret_cast<uint4*>(held + k - k0) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-          *reinterpret_cast<float4*>(held + k - k0) = make_float4(x[0], x[1], x[2], x[3]);
-          *reinterpret_cast<float4*>(held + k - k0 + kHalf<T>) = make_float4(x[4], x[5], x[6], x[7]);
-        }
+        for (int i = 0; i < 4; ++i)
+          w[i] = __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632);
+        *reinterpret_cast<uint4*>(held + k - k0) = make_uint4(w[0], w[1], w[2], w[3]);
       } else {
+        *reinterpret_cast<float4*>(held + k - k0) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(held + k - k0 + kHalf<T>) = make_float4(x[4], x[5], x[6], x[7]);
+      }
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int q = elem_pos<T, VEC>(k, i);
-          if (q < k1) held_put(held, q - k0, x[i]);
-        }
+      for (int i = 0; i < 8; ++i) {
+        const int q = elem_pos<T, VEC>(k, i);
+        if (q < k1) held_put(held, q - k0, x[i]);
       }
     }
-  });
+  };
+  if constexpr (VEC && HOLD && F != kSome) {
+    // Whole items straight to their place, all of a thread's at once: l_L, and bf16 rows' l_S behind it, in the
+    // 32 bytes that the 8 values then take as float32. (Through registers, four items in flight: 1088
+    // plain bf16 rows 189 us.)
+    const auto whole = [&](int pos) { return pos >= row.sh && pos + kHalf<T> + 4 <= k1; };
+    for (int it = 0; it < items; ++it) {
+      const int pos = item_pos<T, VEC>(k0, it, tid);
+      if (!whole(pos)) continue;
+      const uint32_t dst = smem_u32(held + (pos - k0));
+      copy16(dst, row.L + pos);
+      if constexpr (sizeof(T) == 4) copy16(dst + 4 * kHalf<T>, row.L + pos + kHalf<T>);
+      else if constexpr (F != kPlain) copy16(dst + 16, row.S + pos);
+    }
+    copies_commit();
+    constexpr int U = F == kPlain ? 1 : 2;
+    bool waited = false;
+    for (int it = 0; it < items; it += U) {
+      Item<T, F, VEC> v[U];
+      float pr[U][8], x[8], sv[8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int pos = item_pos<T, VEC>(k0, it + u, tid);
+        if (!whole(pos)) {
+          v[u].load(row, pos, k1, pr[u]);
+          continue;
+        }
+        v[u].k = pos;
+        if constexpr (F != kPlain) {
+          if constexpr (sizeof(T) == 4) v[u].s.load(row.S + pos, kHalf<T>);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) pr[u][i] = row.p_at(elem_pos<T, VEC>(pos, i));
+        }
+      }
+      if (!waited) copies_wait<0>();
+      waited = true;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool w = whole(v[u].k);
+        if (w) {
+          const uint4* at = reinterpret_cast<const uint4*>(held + (v[u].k - k0));
+          v[u].l.w[0] = at[0];
+          if constexpr (sizeof(T) == 4) v[u].l.w[1] = *reinterpret_cast<const uint4*>(held + (v[u].k - k0) + kHalf<T>);
+          else if constexpr (F != kPlain) v[u].s.w[0] = at[1];
+        }
+        v[u].template values<true>(row, pr[u], x, sv);
+        m = fmaxf(m, max8(x));
+        if (F != kPlain || !w) hold(x, v[u].k);
+      }
+    }
+  } else {
+    each([&](float (&x)[8], int k) {
+      m = fmaxf(m, max8(x));
+      if constexpr (HOLD) hold(x, k);
+    });
+  }
   m = warp_max(m);
   if (lane == 0) red[warp] = m;
   __syncthreads();
