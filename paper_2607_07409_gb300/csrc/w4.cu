@@ -111,13 +111,40 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t at, const uint32_t (&u)[16]
       "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_ld_x16(uint32_t at, float (&r)[16]) {
+// 8, 16 or 32 sums of the thread's row, the wait for them in the same statement: nothing that uses
+// them can come before it.
+__device__ __forceinline__ void tmem_ld_now(uint32_t at, float (&r)[8]) {
   uint32_t* u = reinterpret_cast<uint32_t*>(r);
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+      : "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_now(uint32_t at, float (&r)[16]) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
       : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
         "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
-      : "r"(at));
+      : "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_now(uint32_t at, float (&r)[32]) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]),
+        "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]),
+        "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]),
+        "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(at)
+      : "memory");
 }
 // Shared-memory matrix descriptor, K-major without swizzle: 8 rows x 16 bytes are 128 bytes side by
 // side, `lead` bytes from one 8 inputs to the next, `stride` from 8 rows to the next.
@@ -490,19 +517,15 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   RowTop tops[kTops];                       // of requests row % S, row % S + S; of 0 and 1 where these have their own rows
 #pragma unroll
   for (int h = 0; h < kTops; ++h) tops[h] = RowTop{-INFINITY, -INFINITY, -INFINITY, 0.f, 0x7FFFFFFF};
-  // apart in time: in step, all groups' codes wait for the ALU pipe and then all groups for their products
-  __nanosleep(grp * 200);
 
   // Sums of an operand's group i, scaled.
   const auto add_sums = [&](int i, float scale) {
     const f32x2 s2 = both2(scale);
-    constexpr int W = NB < 16 ? 8 : 16;
+    constexpr int W = NB == 32 ? 32 : NB < 16 ? 8 : 16;      // sums at a time (more spill, with 64)
 #pragma unroll
     for (int n0 = 0; n0 < NB; n0 += W) {
       float acc[W];
-      if constexpr (W == 8) tmem_ld_32x32b_x8(dcol + quadrant + i * N + n0, acc);
-      else tmem_ld_x16(dcol + quadrant + i * N + n0, acc);
-      tmem_ld_wait();
+      tmem_ld_now(dcol + quadrant + i * N + n0, acc);
 #pragma unroll
       for (int n = 0; n < W; n += 2) tot[(n0 + n) / 2] = fma2(s2, pair2(acc[n], acc[n + 1]), tot[(n0 + n) / 2]);
     }
