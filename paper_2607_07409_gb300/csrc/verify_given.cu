@@ -4,7 +4,7 @@
 // lane a position, so that their reads wait for one another no more than once; then the row that the
 // bonus token comes from is summed, once: a warp has a run of groups of 256 columns. The
 // warps' sums meet in shared memory, the CTAs' in each other's; the warp whose run has the border
-// reads that again, out of L2, and walks it.
+// finds the part of it by sums kept on the way, reads that again, out of L2, and walks it.
 //
 // Sums decide which token comes out, so they are as good as float64's: float64 itself issues
 // at 1/64 of float32's rate here, so a lane keeps a float32 sum and what its additions
@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kGivenThreads = 512, kGivenWarps = kGivenThreads / 32;
 constexpr int kGroup = 256;                // columns of a warp's step, 8 a lane
+constexpr int kMarks = 4;                  // sums a lane keeps of its way along a run
 
 __device__ __forceinline__ bool is_probability(float x) { return x >= 0.f && x < INFINITY; }
 
@@ -141,7 +142,7 @@ struct Border {
 
 template <typename P, typename Q, bool DRAFT, bool VEC>
 __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyGivenArgs a, int cluster) {
-  __shared__ Sum2 warp_sum[kGivenWarps];
+  __shared__ Sum2 warp_sum[kGivenWarps], marks[kGivenWarps][kMarks][32];
   __shared__ int warp_bad[kGivenWarps];
   __shared__ SlicePart parts[2][kMaxCluster];
   __shared__ Border border;
@@ -193,22 +194,21 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
           s.add(w[i], e[i]);
         }
       };
-      int g = g0;
-      for (; g + 1 < g1; g += 2) {
-        float x[2][8], y[2][8];
+      for (int i = 0; i < kMarks; ++i) {    // (a run in as many parts, its sums behind each kept)
+        const int end = g0 + (int)((long long)(g1 - g0) * (i + 1) / kMarks);
+        int g = g0 + (int)((long long)(g1 - g0) * i / kMarks);
+        for (; g < end; g += 2) {
+          float x[2][8], y[2][8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          load8<P, VEC>(p, (g + i) * kGroup, a.V, x[i]);
-          if (DRAFT && rest) load8<Q, VEC>(q, (g + i) * kGroup, a.V, y[i]);
+          for (int u = 0; u < 2; ++u) {
+            if (u && g + 1 >= end) continue;
+            load8<P, VEC>(p, (g + u) * kGroup, a.V, x[u]);
+            if (DRAFT && rest) load8<Q, VEC>(q, (g + u) * kGroup, a.V, y[u]);
+          }
+          add(g, x[0], y[0]);
+          if (g + 1 < end) add(g + 1, x[1], y[1]);
         }
-        add(g, x[0], y[0]);
-        add(g + 1, x[1], y[1]);
-      }
-      if (g < g1) {
-        float x[8], y[8];
-        load8<P, VEC>(p, g * kGroup, a.V, x);
-        if (DRAFT && rest) load8<Q, VEC>(q, g * kGroup, a.V, y);
-        add(g, x, y);
+        marks[warp][i][lane] = s;
       }
       s = warp_sum2(s);
       const int bad = __any_sync(0xFFFFFFFFu, most >= 0x7F800000u);
@@ -272,62 +272,90 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
       code = f.code;
       if (warp == f.run) {
         mine = true;
-        // The first group whose sums exceed it, or by roundings none: the last with weight.
-        double c0 = f.before, base = c0;
-        int at = g0;
-        for (int g2 = g0; g2 < g1; g2 += 2) {
+        // The part of the run whose sums exceed it, by the marks, then the group; where by roundings none
+        // does, the last with weight.
+        Sum2 m[kMarks];
+#pragma unroll
+        for (int i = 0; i < kMarks; ++i) m[i] = warp_sum2(marks[warp][i][lane]);
+        double c0 = f.before;
+        int part = -1;
+#pragma unroll
+        for (int i = 0; i < kMarks; ++i) {
+          const bool some = i == 0 ? m[0].hi > 0.f : m[i].hi > m[i - 1].hi || m[i].lo > m[i - 1].lo;
+          if (!some || (part >= 0 && f.before + total_of(m[part]) > f.at)) continue;
+          part = i;
+          if (i > 0) c0 = f.before + total_of(m[i - 1]);
+        }
+        part = __shfl_sync(0xFFFFFFFFu, max(part, 0), 0);
+        c0 = __shfl_sync(0xFFFFFFFFu, c0, 0);
+        const int p0 = g0 + (int)((long long)(g1 - g0) * part / kMarks);
+        const int p1 = g0 + (int)((long long)(g1 - g0) * (part + 1) / kMarks);
+        double base = c0;
+        int at = p0;
+        float w[8], e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = e[i] = 0.f;
+        for (int g2 = p0; g2 < p1; g2 += 2) {
           float x[2][8], y[2][8];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            load8<P, VEC>(p, (g2 + i) * kGroup, g2 + i < g1 ? a.V : 0, x[i]);
-            if (DRAFT && rest) load8<Q, VEC>(q, (g2 + i) * kGroup, g2 + i < g1 ? a.V : 0, y[i]);
+            load8<P, VEC>(p, (g2 + i) * kGroup, g2 + i < p1 ? a.V : 0, x[i]);
+            if (DRAFT && rest) load8<Q, VEC>(q, (g2 + i) * kGroup, g2 + i < p1 ? a.V : 0, y[i]);
           }
           bool over = false;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if (over) continue;
-            float w[8], e[8];
-            weights(rest, g2 + i, x[i], y[i], w, e);
+            float w2[8], e2[8];
+            weights(rest, g2 + i, x[i], y[i], w2, e2);
             Sum2 t{0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t.add(w[j], e[j]);
+            for (int j = 0; j < 8; ++j) t.add(w2[j], e2[j]);
             t = warp_sum2(t);
             const double upto = __shfl_sync(0xFFFFFFFFu, c0 + total_of(t), 0);
             if (t.hi > 0.f) {
               at = g2 + i;
               base = c0;
               over = upto > f.at;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) w[j] = w2[j], e[j] = e2[j];
             }
             c0 = upto;
           }
           if (over) break;
         }
-        float x[8], y[8], w[8], e[8];
-        load8<P, VEC>(p, at * kGroup, a.V, x);
-        if (DRAFT && rest) load8<Q, VEC>(q, at * kGroup, a.V, y);
-        weights(rest, at, x, y, w, e);
-        // VEC: the lanes in order, each its 8; else 8 times the lanes in order
+        // The column. VEC: the lanes in order, each its 8; else 8 times the lanes in order.
         constexpr int kParts = VEC ? 1 : 8, kEach = 8 / kParts;
         bool found = false;
 #pragma unroll
         for (int h = 0; h < kParts; ++h) {
           if (found) continue;
-          double t = 0.0;
+          Sum2 t{0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < kEach; ++i) t += (double)w[h * kEach + i] + (double)e[h * kEach + i];
-          const double incl = warp_scan(t, 32);
+          for (int i = 0; i < kEach; ++i) t.add(w[h * kEach + i], e[h * kEach + i]);
+          Sum2 upto = t;                    // up to and including the lane's
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const float hi = __shfl_up_sync(0xFFFFFFFFu, upto.hi, d), lo = __shfl_up_sync(0xFFFFFFFFu, upto.lo, d);
+            if (lane >= d) upto.add(hi, lo);
+          }
+          const double incl = total_of(upto);
+          const double up = __shfl_up_sync(0xFFFFFFFFu, incl, 1);
           const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > f.at);
-          const unsigned some = __ballot_sync(0xFFFFFFFFu, t > 0.0);
+          const unsigned some = __ballot_sync(0xFFFFFFFFu, t.hi > 0.f);
           const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
-          if (who >= 0) {                 // the border, or for now the last with weight
+          if (who >= 0) {                   // the border, or for now the last with weight
+            const double left = f.at - (base + (lane ? up : 0.0));       // of the lane's own
+            const float left_hi = (float)left, left_lo = (float)(left - (double)left_hi);
             int v = -1;
-            double c2 = base + (incl - t);
+            bool past = false;
+            Sum2 c{0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-              const double w2 = (double)w[h * kEach + i] + (double)e[h * kEach + i];
-              const bool past = c2 > f.at && v >= 0;
-              c2 += w2;
-              if (!past && w2 > 0.0) v = at * kGroup + (VEC ? lane * 8 + i : h * 32 + lane);
+              const float w2 = w[h * kEach + i];
+              c.add(w2, e[h * kEach + i]);
+              if (!past && w2 > 0.f) v = at * kGroup + (VEC ? lane * 8 + i : h * 32 + lane);
+              past |= v >= 0 && __fadd_rn(__fsub_rn(c.hi, left_hi), __fsub_rn(c.lo, left_lo)) > 0.f;
             }
             bonus = __shfl_sync(0xFFFFFFFFu, v, who);
           }
