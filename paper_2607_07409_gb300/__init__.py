@@ -1086,7 +1086,8 @@ class W4Matrix:
     ``project``. ``pack_w4`` makes one."""
 
     def __init__(self, data: torch.Tensor, V: int, K: int, group: int, zeros: bool):
-        if data.data_ptr() % 16 or data.numel() < dels_w4_bytes(V, K, group, zeros):
+        if (not data.is_cuda or data.dtype is not torch.uint8 or not data.is_contiguous() or data.data_ptr() % 16
+                or not 0 < dels_w4_bytes(V, K, group, zeros) <= data.numel()):
             raise ValueError("data must be what dels_w4_pack wrote")
         self.data, self.V, self.K, self.group, self.zeros = data, V, K, group, zeros
         self._dev = data.get_device()

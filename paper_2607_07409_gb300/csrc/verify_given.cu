@@ -10,6 +10,10 @@
 // at 1/64 of float32's rate here, so a lane keeps a float32 sum and what its additions
 // rounded off (Knuth's two-sum), 48 bits, and only totals are float64, in one warp. A
 // difference p - q is kept the same way.
+//
+// What bounds it: latency, one part after another. 64 blocks of 16 over 151936 (78 MB, 11.5 us at a
+// copy's rate) 24 to 27 us: 2 for the tokens, 16 for the stream in two CTAs an SM (1.7 of them), 8 for the
+// sums, the exchange, the border's part and its column; one block of 8 over 32000 7.8 us.
 #include "dels_device.cuh"
 #include "row_stream.cuh"
 

@@ -89,6 +89,13 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 // (With the parts of that in warps of their own, behind mbarriers with buffers to spare, the
 // hand-overs' instructions took more than the overlap gave: 103 us against 80 at 8 requests.)
 // The features stay in shared memory; a K whose features do not fit is taken in parts.
+//
+// What bounds it: a step (four units of 32 inputs, with more than 8 requests two) goes from one of its
+// parts to the next, about 1900 cycles of instructions that wait for the one before, of which four groups
+// hide three quarters; 68 instructions a unit, 0.45 of the issue slots. 151936 x 1024 for one request
+// 20 us, x 2560 for 8 44 us (12.3 and 30.7 for the bytes at a copy's rate), 151936 x 256 for 64 24.5 us
+// (6.1), 32003 x 1000 for 5 with float32 features 12.4 us (2.7). Eight groups of half the registers spill:
+// 26.5, 55.8; their sums' registers leave 64 requests three.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
@@ -428,8 +435,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
 #pragma unroll
   for (int i = 0; i < kKept; ++i)
     if (warp + i * warps < all) load_task(warp + i * warps, kept[i]);
+  fence_proxy_async_global();
   if ((warp & 3) == 0 && lane < p.stages) {             // the first ones, a lane each
-    fence_proxy_async_global();
     const long long tile = tile0 + lane / a.lay.blocks * apart;
     const int kb = lane % a.lay.blocks;
     if (tile < a.lay.tiles) {
