@@ -89,6 +89,7 @@ typedef enum {
 /*
  * A matrix [V, K] of 4-bit codes with a scale for each group of `group` inputs of a
  * row (and a zero point, or 8):  w[v, k] = scale[v, k / group] (code[v, k] - zero[v, k / group]).
+ * Scales above 2^90 in magnitude may take sums past float32's range where the result is not.
  * `data` [device] is what dels_w4_pack wrote, 16-byte aligned.
  */
 typedef struct {

@@ -980,7 +980,19 @@ def distill_loss(short, ids, logprob, *, long=None, log_prior=None, alpha=None, 
     return _DistillLoss.apply(short, alpha, beta, long, log_prior, ids, logprob, row_weight, tail, temperature)
 
 
-# ----------------------------------------------------------------------------- probabilities, given numbers, 4-bit weights
+# ------------------------------------------------------------- probabilities, given numbers, 4-bit weights
+
+def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
+    """A tensor out of the memory of the stream that will write it: work that is still to come on the current one may
+    have been given another's by then."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = int(stream)
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
 
 class RowProbs:
     """Probabilities of [rows, V] logits, plain or fused, as float32 or bfloat16: output and a workspace for
@@ -1009,7 +1021,7 @@ class RowProbs:
             raise ValueError(f"logits must be on {self.device}")
         if out is None:
             if self._out is None:
-                self._out = torch.empty(self.rows, self.V, dtype=self.dtype, device=self.device)
+                self._out = _empty_on(stream, (self.rows, self.V), self.dtype, self.device)
             out = self._out
         shape = (self.rows, self.V)
         to = _logits(out, shape, self.dtype, self._dev, "out")
@@ -1101,13 +1113,13 @@ class W4Matrix:
     def project(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32,
                 stream=None) -> torch.Tensor:
         """[B, V] = x W^T of features [B, K] (float32 or bfloat16; rows may be strided), in a new tensor of
-        ``dtype`` or in ``out`` (float32 or bfloat16; rows may be strided; no part of ``x``)."""
+        ``dtype`` (``stream``'s own memory) or in ``out`` (of either; rows may be strided; no part of ``x``)."""
         _need_current(self._dev)
         if x.dim() != 2:
             raise ValueError(f"x must be [B, {self.K}]")
         B = x.shape[0]
         if out is None:
-            out = torch.empty(B, self.V, dtype=dtype, device=self.device)
+            out = _empty_on(stream, (B, self.V), dtype, self.device)
         xs, os_ = (B, self.K), (B, self.V)
         xp = _logits(x, xs, x.dtype, self._dev, "x")
         op = _logits(out, os_, out.dtype, self._dev, "out")
@@ -1140,6 +1152,8 @@ def pack_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Ten
     if scales is None:
         raise ValueError("a matrix needs scales")
     w = W4Matrix(data, V, K, group, zeros is not None)
+    if stream is not None:                    # what the current stream has to do to the memory taken, and to the inputs
+        torch.cuda.current_stream().synchronize()
     _check(lib().dels_w4_pack(_of(codes, torch.uint8, (V, K), dev, "codes"),
                               _of(scales, torch.bfloat16, groups, dev, "scales"),
                               _of(zeros, torch.uint8, groups, dev, "zeros"), V, K, group, data.data_ptr(), nbytes,

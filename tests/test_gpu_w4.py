@@ -263,3 +263,35 @@ def test_behind_a_kernel_on_its_stream():
         got = w.project(z)
         z.zero_()
         assert ((got.cpu().double() - y * 2.0 ** (k % 3)).abs() <= tol * 4).all()
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_another_stream_than_the_current_one(handle):
+    """Memory that the current stream has still to write, given back and taken again, and codes that it has still to
+    make: the outputs of a call on another stream are its own, and so is what is packed there."""
+    c = Case(3, 9000, 300, 64, True)
+    y, tol = c.want(F32)
+    s = torch.cuda.Stream()
+    on = s.cuda_stream if handle else s
+    w, x = c.pack(), c.x.to(DEV)
+    source = [t.to(DEV) for t in (c.codes, c.scales, c.zeros)]
+    rows = torch.randn(16, 4000, device=DEV)
+    probs = torch.softmax(rows.double(), -1)
+    torch.cuda.synchronize()
+    # torch's own memory of these sizes is free again, with the current stream's fills ahead of it
+    busy = [torch.empty(3, 9000, device=DEV), torch.empty(16, 4000, device=DEV),
+            torch.empty(w.data.numel(), dtype=torch.uint8, device=DEV)]
+    torch.cuda._sleep(50_000_000)
+    for t in busy:
+        t.fill_(7)
+    del t, busy
+    got = w.project(x, stream=on)
+    p = dels.RowProbs(16, 4000)(rows, stream=on)
+    torch.cuda.synchronize()
+    assert ((got.cpu().double() - y).abs() <= tol).all()
+    # an exponent's difference and product, 13 at most, a rounding each; the exponential, the sum and the quotient
+    assert torch.allclose(p.double(), probs, rtol=(2 * 13 + 14) * 2.0 ** -24, atol=0)
+    torch.cuda._sleep(50_000_000)
+    late = [t.clone() for t in source]
+    packed = dels.pack_w4(*late, group=64, stream=on)
+    check(c, F32, packed)
