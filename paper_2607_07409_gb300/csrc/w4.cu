@@ -382,6 +382,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   // out there, and not fetched from a thread's registers one by one)
   const int tid = threadIdx.x, lane = tid & 31, warp = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)tid >> 5);
   const int warps = p.groups * 4, grp = warp >> 2, row = tid & 127;
+  const int issuer = grp & 3;               // of a group's warps: not the same quarter of the SM in all groups
   const int b0 = blockIdx.y * NB;
   uint8_t* ring = smem + (size_t)grp * p.stages * p.stage_bytes;
   uint4* operand = reinterpret_cast<uint4*>(smem + (size_t)p.groups * p.stages * p.stage_bytes);
@@ -408,7 +409,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   const long long tile0 = (long long)grp * gridDim.x + blockIdx.x, apart = (long long)gridDim.x * p.groups;
   const long long rounds = (a.lay.tiles + apart - 1) / apart;
   const int copies = tile0 < a.lay.tiles ? (int)((a.lay.tiles - tile0 + apart - 1) / apart) * a.lay.blocks : 0;
-  int to_copy = copies - p.stages, next_kb = p.stages % a.lay.blocks, next_st = 0;            // of row 32's thread
+  int to_copy = copies - p.stages, next_kb = p.stages % a.lay.blocks, next_st = 0;            // of the thread that copies
   const uint8_t* next_block = a.packed + (tile0 + p.stages / a.lay.blocks * apart) * a.lay.tile_bytes +
                               (long long)next_kb * a.lay.block_bytes;
   const auto issue_copy = [&] {
@@ -578,8 +579,11 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       for (int g = 0; g < NG; ++g) s_now[g] = scale[g];
       tmem_st_wait();
       tc_fence_before();
-      asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
-      if ((warp & 3) == 0) {
+      // (only the warp that issues waits for the others)
+      if ((warp & 3) != issuer) {
+        asm volatile("bar.arrive %0, 128;" ::"r"(grp + 1) : "memory");
+      } else {
+        asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
         tc_fence_after();
         if (elect_one()) {
           const uint32_t x = x0 + (uint32_t)(i * U) * (4 * NB);
@@ -590,13 +594,13 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
         __syncwarp();
       }
       if (i + 1 < blocks * kSteps) load(i + 1);
-      if ((warp & 3) == 1) {
-        if (at + U == 4 && lane == 0) issue_copy();      // (the block before the one just loaded has been read)
-        __syncwarp();
-      }
       wait(&done[grp], dph);
       dph ^= 1;
       tc_fence_after();
+      if ((warp & 3) == (issuer ^ 1)) {
+        if (at + U == 4 && lane == 0) issue_copy();      // (products done: every warp has read the step's block)
+        __syncwarp();
+      }
       if (G <= U || at + U == 4) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) add_sums(g, s_now[g]);
@@ -714,7 +718,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   if (dead) {
     if (lane == 0) raise_status(a.status, DELS_STATUS_TIMEOUT);
     // a CTA that gives up has its copies and products in flight end first
-    if (row == 32) {
+    if (row == 32 * (issuer ^ 1)) {
       const uint64_t limit = globaltimer_ns() + kWaitBudgetNs / 4;
       const int issued = min(copies, copies - to_copy);
       for (int i = max(0, issued - p.stages); i < issued; ++i)
