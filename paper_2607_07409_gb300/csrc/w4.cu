@@ -271,7 +271,12 @@ struct W4Plan {
 };
 
 template <int NB>
-constexpr int kW4Groups = NB == 64 ? 3 : 4;      // (64 sums a thread: 168 registers)
+constexpr int kW4Groups = NB == 64 ? 2 : 4;
+// Halves of a group: with 64 requests eight warps take a tile, every four half of its operand and half of the
+// requests' sums. (Three groups of four warps, a thread with all 64 sums in 168 registers: 24.6 us, and 1.04 ms a
+// block of 16 where this takes 0.72; three of eight warps spill: 23.2, 0.87.)
+template <int NB>
+constexpr int kW4Halves = NB == 64 ? 2 : 1;
 
 __device__ __forceinline__ bool elect_one() {
   uint32_t yes;
@@ -310,7 +315,7 @@ enum { kOutputs = 0, kRecords = 1, kKeys = 2 };
 // warp's 32 rows of every request by shuffles, with no layout between, took 64 requests' block
 // of 16 2.4 ms.)
 template <int NB>
-constexpr int kW4Side = NB < 32 ? NB : 32;             // requests laid out at a time, and a thread's columns
+constexpr int kW4Side = NB < 32 ? NB : 32 / kW4Halves<NB>;      // requests laid out at a time, and a thread's columns
 constexpr int kW4Pitch = kW4Rows + 4;
 struct RowTop {
   float best, second, m, s;                            // m: the sum's reference
@@ -370,9 +375,10 @@ __device__ __forceinline__ void combine_columns(const W4Args& a, const float* y,
 }
 
 template <int NB, int TERMS, int EPI>
-__global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4Args a, const W4Plan p) {
+__global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_project(const W4Args a, const W4Plan p) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int N = NB < 16 ? 16 : NB;                  // requests of an MMA: rows past NB are its first ones again
+  constexpr int H = kW4Halves<NB>, kMine = NB / H;      // requests of a thread
   __shared__ uint64_t full[kW4Groups<NB>][kW4Stages], done[kW4Groups<NB>];
   __shared__ uint32_t tmem_base;
   __shared__ volatile int abort_flag;
@@ -381,7 +387,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   // (through a reduction, which leaves it in a uniform register: the products' operands are then worked
   // out there, and not fetched from a thread's registers one by one)
   const int tid = threadIdx.x, lane = tid & 31, warp = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)tid >> 5);
-  const int warps = p.groups * 4, grp = warp >> 2, row = tid & 127;
+  const int warps = p.groups * 4 * H, grp = warp / (4 * H), half = H > 1 ? warp / 4 % H : 0, row = tid & 127;
+  const int own_warp = warp % (4 * H);      // in the group
   const int issuer = grp & 3;               // of a group's warps: not the same quarter of the SM in all groups
   const int b0 = blockIdx.y * NB;
   uint8_t* ring = smem + (size_t)grp * p.stages * p.stage_bytes;
@@ -437,7 +444,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   for (int i = 0; i < kKept; ++i)
     if (warp + i * warps < all) load_task(warp + i * warps, kept[i]);
   fence_proxy_async_global();
-  if ((warp & 3) == 0 && lane < p.stages) {             // the first ones, a lane each
+  if (own_warp == 0 && lane < p.stages) {             // the first ones, a lane each
     const long long tile = tile0 + lane / a.lay.blocks * apart;
     const int kb = lane % a.lay.blocks;
     if (tile < a.lay.tiles) {
@@ -506,45 +513,44 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   const uint32_t dcol = acol + p.a_cols;
   const uint32_t quadrant = (uint32_t)(warp & 3) << 21;                // the warp's 32 lanes of tensor memory
   const uint32_t x0 = (uint32_t)smem_desc_plain(smem_u32(operand), NB * 16, 0);
-  uint64_t deadline = 0;
   bool dead = false;                        // a wait ran out: the rest runs through without waiting
   const auto wait = [&](uint64_t* bar, int parity) {
-    uint32_t polls = 0;
-    while (!mbar_try_wait(bar, (uint32_t)parity) && !dead)
-      if ((++polls & 15u) == 0 && (abort_flag || globaltimer_ns() > deadline)) abort_flag = dead = true;
+    // (the clock is read in long waits alone: a reading takes about 1000 cycles)
+    uint64_t deadline = 0;
+    for (uint32_t polls = 1; !mbar_try_wait(bar, (uint32_t)parity) && !dead; ++polls) {
+      if (polls & 255u) continue;
+      if (!deadline) deadline = globaltimer_ns() + kWaitBudgetNs;
+      else if (abort_flag || globaltimer_ns() > deadline) abort_flag = dead = true;
+    }
     __syncwarp();
   };
   int st = 0, ph = 0, dph = 0;
   uint32_t base = 0x64006400u;
   asm("" : "+r"(base));                   // (a register, not a constant)
-  f32x2 tot[NB / 2];
+  f32x2 tot[kMine / 2];
   constexpr int S = kW4Side<NB>;
   float* sides = reinterpret_cast<float*>(operand + (size_t)TERMS * p.part_units * 4 * NB);      // of the records
   const bool own_rows = EPI != kOutputs && NB == 8 && a.B <= 2;
-  constexpr int kTops = NB == 8 ? 2 : NB / S;
-  RowTop tops[kTops];                       // of requests row % S, row % S + S; of 0 and 1 where these have their own rows
+  constexpr int kTops = NB == 8 ? 2 : kMine / S;
+  RowTop tops[kTops];                       // of the half's requests row % S, row % S + S; of 0 and 1 where these have their own rows
 #pragma unroll
   for (int h = 0; h < kTops; ++h) tops[h] = RowTop{-INFINITY, -INFINITY, -INFINITY, 0.f, 0x7FFFFFFF};
 
   // Sums of an operand's group i, scaled.
   const auto add_sums = [&](int i, float scale) {
     const f32x2 s2 = both2(scale);
-    constexpr int W = NB == 32 ? 32 : NB < 16 ? 8 : 16;      // sums at a time (more spill, with 64)
+    float acc[kMine];
+    tmem_ld_now(dcol + quadrant + i * N + half * kMine, acc);
 #pragma unroll
-    for (int n0 = 0; n0 < NB; n0 += W) {
-      float acc[W];
-      tmem_ld_now(dcol + quadrant + i * N + n0, acc);
-#pragma unroll
-      for (int n = 0; n < W; n += 2) tot[(n0 + n) / 2] = fma2(s2, pair2(acc[n], acc[n + 1]), tot[(n0 + n) / 2]);
-    }
+    for (int n = 0; n < kMine; n += 2) tot[n / 2] = fma2(s2, pair2(acc[n], acc[n + 1]), tot[n / 2]);
   };
 
   // Blocks of a part, U units an operand, G a group: while a step's products run the next one's codes are
   // taken apart.
   const auto run = [&](int blocks, auto step_units, auto group_units) {
     constexpr int U = decltype(step_units)::value, G = decltype(group_units)::value, NG = U > G ? U / G : 1;
-    constexpr int kSteps = 4 / U;
-    uint32_t m[U * 16];
+    constexpr int kSteps = 4 / U, UH = U / H;            // units that a half takes apart
+    uint32_t m[UH * 16];
     float scale[NG];
     const auto load = [&](int i) {
       const int s0 = i % kSteps * U;
@@ -552,15 +558,18 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       const uint8_t* block = ring + (size_t)st * p.stage_bytes;
       const uint8_t* scales = block + 4 * kW4UnitBytes + s0 / G * 256 + row * 2;
       const uint8_t* zeros = block + 4 * kW4UnitBytes + 4 / G * 256 + s0 / G * 64 + (row >> 1);
-      uint4 w[U];
+      uint4 w[UH];
 #pragma unroll
-      for (int u = 0; u < U; ++u) w[u] = (reinterpret_cast<const uint4*>(block + s0 * kW4UnitBytes) + row)[u * kW4Rows];
+      for (int u = 0; u < UH; ++u)
+        w[u] = (reinterpret_cast<const uint4*>(block + (s0 + half * UH) * kW4UnitBytes) + row)[u * kW4Rows];
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        scale[g] = bf16_to_f(*reinterpret_cast<const uint16_t*>(scales + g * 256));
-        const ZeroPoint z(a.zeros ? zeros[g * 64] >> (4 * (row & 1)) & 15u : 8u);
+      for (int g = 0; g < NG; ++g) scale[g] = bf16_to_f(*reinterpret_cast<const uint16_t*>(scales + g * 256));
+      constexpr int NZ = (NG + H - 1) / H;               // groups of the half's units
 #pragma unroll
-        for (int u = g * (U / NG); u < (g + 1) * (U / NG); ++u) {
+      for (int g = 0; g < NZ; ++g) {
+        const ZeroPoint z(a.zeros ? zeros[(NG > 1 ? half * NZ + g : 0) * 64] >> (4 * (row & 1)) & 15u : 8u);
+#pragma unroll
+        for (int u = g * (UH / NZ); u < (g + 1) * (UH / NZ); ++u) {
           pairs_of(w[u].x, base, z, m + u * 16);
           pairs_of(w[u].y, base, z, m + u * 16 + 4);
           pairs_of(w[u].z, base, z, m + u * 16 + 8);
@@ -573,17 +582,18 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
     for (int i = 0; i < blocks * kSteps; ++i) {
       const int at = i % kSteps * U;
 #pragma unroll
-      for (int u = 0; u < U; ++u) tmem_st_x16(acol + quadrant + u * 16, *reinterpret_cast<uint32_t(*)[16]>(m + u * 16));
+      for (int u = 0; u < UH; ++u)
+        tmem_st_x16(acol + quadrant + (half * UH + u) * 16, *reinterpret_cast<uint32_t(*)[16]>(m + u * 16));
       float s_now[NG];
 #pragma unroll
       for (int g = 0; g < NG; ++g) s_now[g] = scale[g];
       tmem_st_wait();
       tc_fence_before();
       // (only the warp that issues waits for the others)
-      if ((warp & 3) != issuer) {
-        asm volatile("bar.arrive %0, 128;" ::"r"(grp + 1) : "memory");
+      if (own_warp != issuer) {
+        asm volatile("bar.arrive %0, %1;" ::"r"(grp + 1), "n"(128 * H) : "memory");
       } else {
-        asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
+        asm volatile("bar.sync %0, %1;" ::"r"(grp + 1), "n"(128 * H) : "memory");
         tc_fence_after();
         if (elect_one()) {
           const uint32_t x = x0 + (uint32_t)(i * U) * (4 * NB);
@@ -597,7 +607,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       wait(&done[grp], dph);
       dph ^= 1;
       tc_fence_after();
-      if ((warp & 3) == (issuer ^ 1)) {
+      if (own_warp == (issuer ^ 1)) {
         if (at + U == 4 && lane == 0) issue_copy();      // (products done: every warp has read the step's block)
         __syncwarp();
       }
@@ -611,9 +621,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   for (long long r = 0; r < rounds; ++r) {
     const long long tile = tile0 + r * apart;
     const bool live = tile < a.lay.tiles;   // (a group without a tile keeps to the barriers)
-    deadline = globaltimer_ns() + kWaitBudgetNs;
 #pragma unroll
-    for (int n = 0; n < NB / 2; ++n) tot[n] = 0ull;
+    for (int n = 0; n < kMine / 2; ++n) tot[n] = 0ull;
     for (int part = 0; part < p.parts; ++part) {
       const int pu0 = part * p.part_units, pu1 = min(all_units, pu0 + p.part_units);
       if (!resident) {
@@ -632,19 +641,36 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       else run(blocks, step_units, four);
     }
     const long long v = tile * kW4Rows + row;
-    const int nb = min(NB, a.B - b0);
+    const int n0 = half * kMine, nb = min(kMine, a.B - b0 - n0);        // the thread's requests
+    float* side = sides + (size_t)(grp * H + half) * S * kW4Pitch;
+    const auto together = [&] {
+      asm volatile("bar.sync %0, 128;" ::"r"((H > 1 ? kW4Groups<NB> : 0) + grp * H + half + 1) : "memory");
+    };
+    const auto lay_out = [&](int h) {       // S requests' products of the tile, h S on, by requests
+#pragma unroll
+      for (int n = 0; n < S; n += 2) {
+        float y[2];
+        split2(tot[(h * S + n) / 2], y[0], y[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 f = back[n0 + h * S + n + i];
+          side[(n + i) * kW4Pitch + row] = y[i] * f.x * f.y;
+        }
+      }
+      together();
+    };
     if constexpr (EPI == kOutputs) {
       // ---- outputs: a warp's 32 rows side by side
       if (live && v < a.V) {
 #pragma unroll
-        for (int n = 0; n < NB; n += 2) {
+        for (int n = 0; n < kMine; n += 2) {
           float y[2];
           split2(tot[n / 2], y[0], y[1]);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if (n + i >= nb) break;
-            const float out = y[i] * back[n + i].x * back[n + i].y;
-            const long long at = (long long)(b0 + n + i) * a.ld_out + v;
+            const float out = y[i] * back[n0 + n + i].x * back[n0 + n + i].y;
+            const long long at = (long long)(b0 + n0 + n + i) * a.ld_out + v;
             if (a.out_f32) static_cast<float*>(a.out)[at] = out;
             else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(out);
           }
@@ -662,25 +688,14 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       }
     } else if (live) {
       // ---- records of the fused rows
-      float* side = sides + (size_t)grp * S * kW4Pitch;
 #pragma unroll
-      for (int h = 0; h < NB / S; ++h) {
+      for (int h = 0; h < kMine / S; ++h) {
         if (h * S >= nb) break;
-#pragma unroll
-        for (int n = 0; n < S; n += 2) {
-          float y[2];
-          split2(tot[(h * S + n) / 2], y[0], y[1]);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float2 f = back[h * S + n + i];
-            side[(n + i) * kW4Pitch + row] = y[i] * f.x * f.y;
-          }
-        }
-        asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
+        lay_out(h);
         const int n = row % S, c0 = row / S * S;
         if (h * S + n < nb)
-          combine_columns<S, EPI == kKeys>(a, side + n * kW4Pitch + c0, b0 + h * S + n, tile * kW4Rows + c0, tops[h]);
-        asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory");
+          combine_columns<S, EPI == kKeys>(a, side + n * kW4Pitch + c0, b0 + n0 + h * S + n, tile * kW4Rows + c0, tops[h]);
+        together();
       }
     }
   }
@@ -698,8 +713,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
       }
     } else {
 #pragma unroll
-      for (int h = 0; h < NB / S; ++h)
-        all_recs[(grp * (128 / S) + row / S) * NB + h * S + row % S] =
+      for (int h = 0; h < kMine / S; ++h)
+        all_recs[(grp * (128 / S) + row / S) * NB + half * kMine + h * S + row % S] =
             make_float4(tops[h].best, tops[h].s, tops[h].second, __int_as_float(tops[h].idx));
     }
     __syncthreads();
@@ -718,7 +733,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128, 1) k_w4_project(const W4A
   if (dead) {
     if (lane == 0) raise_status(a.status, DELS_STATUS_TIMEOUT);
     // a CTA that gives up has its copies and products in flight end first
-    if (row == 32 * (issuer ^ 1)) {
+    if (half == 0 && row == 32 * (issuer ^ 1)) {
       const uint64_t limit = globaltimer_ns() + kWaitBudgetNs / 4;
       const int issued = min(copies, copies - to_copy);
       for (int i = max(0, issued - p.stages); i < issued; ++i)
@@ -740,7 +755,7 @@ int w4_requests(int B) { return B <= 8 ? 8 : B <= 16 ? 16 : B <= 32 ? 32 : 64; }
 template <int NB, int TERMS, int EPI>
 cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const int sms = device_sm_count();
-  const int side = EPI == kOutputs ? 0 : kW4Groups<NB> * kW4Side<NB> * kW4Pitch * 4;
+  const int side = EPI == kOutputs ? 0 : kW4Groups<NB> * kW4Halves<NB> * kW4Side<NB> * kW4Pitch * 4;
   const int room = device_max_smem_optin() - 4096 - side;
   if (sms <= 0 || room <= 0) return cudaErrorInvalidValue;
   const int btiles = (a.B + NB - 1) / NB, ctas = w4_ctas(a, NB, sms);
@@ -768,7 +783,7 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const auto k = k_w4_project<NB, TERMS, EPI>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * 128), (size_t)p.smem, s, a, p);
+  return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * 128 * kW4Halves<NB>), (size_t)p.smem, s, a, p);
 }
 
 }  // namespace

@@ -131,6 +131,22 @@ def test_outputs_anywhere(V, offset, pitch, dtype):
         assert (big[offset + b * pitch + V:offset + (b + 1) * pitch] == -7).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,V,pitch,offset", [(17, 8, 8, 0), (32, 1000, 1000, 0), (33, 1004, 1008, 8), (40, 129, 136, 0),
+                                              (64, 4096, 4096, 16), (64, 4096, 4100, 0), (65, 1003, 1003, 1),
+                                              (100, 260, 264, 0)])
+def test_outputs_of_many_requests(B, V, pitch, offset, dtype):
+    """Rows that start on 16 bytes and others; what lies between and behind them stays."""
+    c = Case(B, V, 200, 32, True)
+    big = torch.full((offset + (B + 1) * pitch,), -7.0, dtype=dtype, device=DEV)
+    out = big.as_strided((B, V), (pitch, 1), offset)
+    c.pack().project(put(c.x), out=out)
+    y, tol = c.want(dtype)
+    assert ((out.cpu().double() - y).abs() <= tol).all()
+    out.fill_(-7)
+    assert (big == -7).all()
+
+
 def test_float32_features_to_their_last_bit():
     """Features of 24 significant bits, from the smallest to the largest, each alone against a weight of 1."""
     K = 64
