@@ -271,12 +271,17 @@ struct W4Plan {
 };
 
 template <int NB>
-constexpr int kW4Groups = NB == 64 ? 2 : 4;
+constexpr int kW4Groups = NB >= 32 ? 2 : 4;
 // Halves of a group: with 64 requests eight warps take a tile, every four half of its operand and half of the
 // requests' sums. (Three groups of four warps, a thread with all 64 sums in 168 registers: 24.6 us, and 1.04 ms a
 // block of 16 where this takes 0.72; three of eight warps spill: 23.2, 0.87.)
 template <int NB>
-constexpr int kW4Halves = NB == 64 ? 2 : 1;
+constexpr int kW4Halves = NB >= 32 ? 2 : 1;
+// Threads of a group: the warps that take codes apart and add sums up and, of outputs, one that issues products and
+// copies. (Issued by one of the others: 18.8 us for one request, 38.5 for 8, 22.6 for 64, in place of 17.9, 36.0, 19.1.
+// Records need more registers than the 96 that this leaves a thread: 0.69 ms a block of 16 for 64 requests, with it 0.87.)
+template <int NB, bool APART>
+constexpr int kW4Group = 128 * kW4Halves<NB> + 32 * APART;
 
 __device__ __forceinline__ bool elect_one() {
   uint32_t yes;
@@ -375,7 +380,7 @@ __device__ __forceinline__ void combine_columns(const W4Args& a, const float* y,
 }
 
 template <int NB, int TERMS, int EPI>
-__global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_project(const W4Args a, const W4Plan p) {
+__global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>, 1) k_w4_project(const W4Args a, const W4Plan p) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int N = NB < 16 ? 16 : NB;                  // requests of an MMA: rows past NB are its first ones again
   constexpr int H = kW4Halves<NB>, kMine = NB / H;      // requests of a thread
@@ -387,9 +392,12 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
   // (through a reduction, which leaves it in a uniform register: the products' operands are then worked
   // out there, and not fetched from a thread's registers one by one)
   const int tid = threadIdx.x, lane = tid & 31, warp = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)tid >> 5);
-  const int warps = p.groups * 4 * H, grp = warp / (4 * H), half = H > 1 ? warp / 4 % H : 0, row = tid & 127;
-  const int own_warp = warp % (4 * H);      // in the group
-  const int issuer = grp & 3;               // of a group's warps: not the same quarter of the SM in all groups
+  constexpr bool kApart = EPI == kOutputs;              // the issuing warps are others than the workers, the last ones
+  const int workers = p.groups * 4 * H, warps = workers + (kApart ? p.groups : 0);
+  const bool issues = kApart && warp >= workers;
+  const int grp = issues ? warp - workers : warp / (4 * H), half = H > 1 ? warp / 4 % H : 0, row = tid & 127;
+  // else of a group's warps one issues products and the next one copies: not in the same quarter of the SM in all groups
+  const int place = warp % (4 * H), issuer = grp & 3, copier = issuer ^ 1;
   const int b0 = blockIdx.y * NB;
   uint8_t* ring = smem + (size_t)grp * p.stages * p.stage_bytes;
   uint4* operand = reinterpret_cast<uint4*>(smem + (size_t)p.groups * p.stages * p.stage_bytes);
@@ -444,7 +452,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
   for (int i = 0; i < kKept; ++i)
     if (warp + i * warps < all) load_task(warp + i * warps, kept[i]);
   fence_proxy_async_global();
-  if (own_warp == 0 && lane < p.stages) {             // the first ones, a lane each
+  if ((kApart ? issues : place == copier) && lane < p.stages) {             // the first ones, a lane each
     const long long tile = tile0 + lane / a.lay.blocks * apart;
     const int kb = lane % a.lay.blocks;
     if (tile < a.lay.tiles) {
@@ -578,6 +586,29 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
       }
       if (s0 + U == 4 && ++st == p.stages) st = 0, ph ^= 1;
     };
+    const auto issue = [&](int i) {         // (every worker has left a step's operand in its place)
+      asm volatile("bar.sync %0, %1;" ::"r"(grp + 1), "n"(kW4Group<NB, kApart>) : "memory");
+      tc_fence_after();
+      if (elect_one()) {
+        const uint32_t x = x0 + (uint32_t)(i * U) * (4 * NB);
+        if (G > U && i % kSteps > 0) issue_products<NB, TERMS, U, U, true>(dcol, acol, x, p.part_units);
+        else issue_products<NB, TERMS, U, (G > U ? U : G), false>(dcol, acol, x, p.part_units);
+        tc_commit(&done[grp]);
+      }
+      __syncwarp();
+    };
+    const auto copy_next = [&](int i) {     // (and read its block)
+      if (i % kSteps == kSteps - 1 && lane == 0) issue_copy();
+      __syncwarp();
+    };
+    if (issues) {
+      for (int i = 0; i < blocks * kSteps; ++i) {
+        issue(i);
+        copy_next(i);
+        dph ^= 1;
+      }
+      return;
+    }
     load(0);
     for (int i = 0; i < blocks * kSteps; ++i) {
       const int at = i % kSteps * U;
@@ -589,28 +620,13 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
       for (int g = 0; g < NG; ++g) s_now[g] = scale[g];
       tmem_st_wait();
       tc_fence_before();
-      // (only the warp that issues waits for the others)
-      if (own_warp != issuer) {
-        asm volatile("bar.arrive %0, %1;" ::"r"(grp + 1), "n"(128 * H) : "memory");
-      } else {
-        asm volatile("bar.sync %0, %1;" ::"r"(grp + 1), "n"(128 * H) : "memory");
-        tc_fence_after();
-        if (elect_one()) {
-          const uint32_t x = x0 + (uint32_t)(i * U) * (4 * NB);
-          if (G > U && at > 0) issue_products<NB, TERMS, U, U, true>(dcol, acol, x, p.part_units);
-          else issue_products<NB, TERMS, U, (G > U ? U : G), false>(dcol, acol, x, p.part_units);
-          tc_commit(&done[grp]);
-        }
-        __syncwarp();
-      }
+      if (!kApart && place == issuer) issue(i);
+      else asm volatile("bar.arrive %0, %1;" ::"r"(grp + 1), "n"(kW4Group<NB, kApart>) : "memory");
       if (i + 1 < blocks * kSteps) load(i + 1);
       wait(&done[grp], dph);
       dph ^= 1;
       tc_fence_after();
-      if (own_warp == (issuer ^ 1)) {
-        if (at + U == 4 && lane == 0) issue_copy();      // (products done: every warp has read the step's block)
-        __syncwarp();
-      }
+      if (!kApart && place == copier) copy_next(i);
       if (G <= U || at + U == 4) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) add_sums(g, s_now[g]);
@@ -640,11 +656,12 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
       else if (glog == 1) run(blocks, step_units, two);
       else run(blocks, step_units, four);
     }
+    if (issues) continue;
     const long long v = tile * kW4Rows + row;
     const int n0 = half * kMine, nb = min(kMine, a.B - b0 - n0);        // the thread's requests
     float* side = sides + (size_t)(grp * H + half) * S * kW4Pitch;
-    const auto together = [&] {
-      asm volatile("bar.sync %0, 128;" ::"r"((H > 1 ? kW4Groups<NB> : 0) + grp * H + half + 1) : "memory");
+    const auto together = [&] {             // (barriers of their own: the issuing warp is at the group's already)
+      asm volatile("bar.sync %0, 128;" ::"r"(kW4Groups<NB> + grp * H + half + 1) : "memory");
     };
     const auto lay_out = [&](int h) {       // S requests' products of the tile, h S on, by requests
 #pragma unroll
@@ -703,7 +720,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
     // ---- the CTA's records, one a thread, through the rings' memory
     __syncthreads();
     float4* all_recs = reinterpret_cast<float4*>(smem);                  // [groups][128 / S][NB], or [warps][NB]
-    if (own_rows) {
+    if (issues) {
+    } else if (own_rows) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         RowAcc r;
@@ -720,7 +738,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
     __syncthreads();
     if (tid < min(NB, a.B - b0)) {
       RowAcc r = rowacc_init();
-      for (int i = 0; i < (own_rows ? warps : p.groups * (128 / S)); ++i) {
+      for (int i = 0; i < (own_rows ? workers : p.groups * (128 / S)); ++i) {
         const float4 x = all_recs[i * NB + tid];
         RowAcc o;
         o.m = x.x; o.s = x.y; o.second = x.z; o.idx = __float_as_int(x.w);
@@ -730,19 +748,19 @@ __global__ void __launch_bounds__(kW4Groups<NB> * 128 * kW4Halves<NB>, 1) k_w4_p
           make_float4(r.m, r.s, r.second, __int_as_float(r.idx));
     }
   }
-  if (dead) {
-    if (lane == 0) raise_status(a.status, DELS_STATUS_TIMEOUT);
-    // a CTA that gives up has its copies and products in flight end first
-    if (half == 0 && row == 32 * (issuer ^ 1)) {
+  if (dead && lane == 0) raise_status(a.status, DELS_STATUS_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  if (abort_flag) {                         // a CTA that gives up has its copies and products in flight end first
+    if ((kApart ? issues : place == copier) && lane == 0) {
       const uint64_t limit = globaltimer_ns() + kWaitBudgetNs / 4;
       const int issued = min(copies, copies - to_copy);
       for (int i = max(0, issued - p.stages); i < issued; ++i)
         while (!mbar_try_wait(&full[grp][i % p.stages], (i / p.stages) & 1) && globaltimer_ns() < limit) {}
       while (!mbar_try_wait(&done[grp], dph ^ 1) && globaltimer_ns() < limit) {}
     }
+    __syncthreads();
   }
-  tc_fence_before();
-  __syncthreads();
   if (warp == 0) tmem_dealloc(tmem_base, p.tmem_cols);
 }
 
@@ -783,7 +801,7 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const auto k = k_w4_project<NB, TERMS, EPI>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * 128 * kW4Halves<NB>), (size_t)p.smem, s, a, p);
+  return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * kW4Group<NB, EPI == kOutputs>), (size_t)p.smem, s, a, p);
 }
 
 }  // namespace

@@ -61,7 +61,11 @@ CASES = [("gru", 1, 5, 1024, "bf16", 32, False, False), ("gru", 5, 4, 5000, "f32
          ("mlp2", 9, 4, 24008, "bf16", 64, True, False), ("xfmr", 8, 4, 4096, "f32", 128, True, False),
          ("xfmr", 17, 3, 1000, "bf16", 32, False, False), ("markov", 1, 8, 50008, "f32", 128, True, False),
          ("markov", 64, 2, 24008, "bf16", 64, False, False), ("markov", 100, 3, 2008, "f32", 32, True, False),
-         ("markov", 128, 2, 1032, "bf16", 128, False, False), ("gru", 2, 1, 1024, "bf16", 32, False, True)]
+         ("markov", 128, 2, 1032, "bf16", 128, False, False), ("gru", 2, 1, 1024, "bf16", 32, False, True),
+         # several tiles for every group of warps
+         ("markov", 5, 2, 100008, "bf16", 128, True, False), ("markov", 2, 2, 100008, "f32", 32, False, False),
+         ("gru", 12, 2, 100008, "bf16", 64, False, True), ("mlp", 20, 2, 60008, "bf16", 32, True, False),
+         ("markov", 64, 2, 60008, "f32", 64, False, False)]
 
 
 @pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}-{c[1]}-{c[3]}-{c[5]}")
