@@ -272,6 +272,9 @@ struct W4Plan {
 
 template <int NB>
 constexpr int kW4Groups = NB >= 32 ? 2 : 4;
+// Units of an operand: as many as leave registers for the sums (32 requests, 151936 x 1024: 2 33.0 us, 4 30.6).
+template <int NB>
+constexpr int kW4Step = NB == 8 || NB == 32 ? 4 : 2;
 // Halves of a group: with 64 requests eight warps take a tile, every four half of its operand and half of the
 // requests' sums. (Three groups of four warps, a thread with all 64 sums in 168 registers: 24.6 us, and 1.04 ms a
 // block of 16 where this takes 0.72; three of eight warps spill: 23.2, 0.87.)
@@ -651,7 +654,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
       const integral_constant<int, 1> one;
       const integral_constant<int, 2> two;
       const integral_constant<int, 4> four;
-      constexpr integral_constant<int, NB <= 8 ? 4 : 2> step_units;
+      constexpr integral_constant<int, kW4Step<NB>> step_units;
       if (glog == 0) run(blocks, step_units, one);
       else if (glog == 1) run(blocks, step_units, two);
       else run(blocks, step_units, four);
@@ -663,16 +666,24 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     const auto together = [&] {             // (barriers of their own: the issuing warp is at the group's already)
       asm volatile("bar.sync %0, 128;" ::"r"(kW4Groups<NB> + grp * H + half + 1) : "memory");
     };
+    // Products of 8 requests, n on. (All of them before any is stored: the compiler keeps each reading of back[]
+    // behind the stores before it, and one after another they took half of 64 requests' time.)
+    const auto products = [&](int n, float (&y)[8]) {
+      float2 f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = back[n0 + n + i];
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) split2(tot[(n + i) / 2], y[i], y[i + 1]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = y[i] * f[i].x * f[i].y;
+    };
     const auto lay_out = [&](int h) {       // S requests' products of the tile, h S on, by requests
 #pragma unroll
-      for (int n = 0; n < S; n += 2) {
-        float y[2];
-        split2(tot[(h * S + n) / 2], y[0], y[1]);
+      for (int n = 0; n < S; n += 8) {
+        float y[8];
+        products(h * S + n, y);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float2 f = back[n0 + h * S + n + i];
-          side[(n + i) * kW4Pitch + row] = y[i] * f.x * f.y;
-        }
+        for (int i = 0; i < 8; ++i) side[(n + i) * kW4Pitch + row] = y[i];
       }
       together();
     };
@@ -680,16 +691,18 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
       // ---- outputs: a warp's 32 rows side by side
       if (live && v < a.V) {
 #pragma unroll
-        for (int n = 0; n < kMine; n += 2) {
-          float y[2];
-          split2(tot[n / 2], y[0], y[1]);
+        for (int n = 0; n < kMine; n += 8) {
+          float y[8];
+          products(n, y);
+          const long long at = (long long)(b0 + n0 + n) * a.ld_out + v;
+          if (a.out_f32) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (n + i >= nb) break;
-            const float out = y[i] * back[n0 + n + i].x * back[n0 + n + i].y;
-            const long long at = (long long)(b0 + n0 + n + i) * a.ld_out + v;
-            if (a.out_f32) static_cast<float*>(a.out)[at] = out;
-            else static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(out);
+            for (int i = 0; i < 8; ++i)
+              if (n + i < nb) static_cast<float*>(a.out)[at + i * a.ld_out] = y[i];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (n + i < nb) static_cast<__nv_bfloat16*>(a.out)[at + i * a.ld_out] = __float2bfloat16_rn(y[i]);
           }
         }
       }
@@ -782,11 +795,8 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const int gunits = a.group / kW4Unit;
   p.stage_bytes = (a.lay.block_bytes + 127) / 128 * 128;
   const long long unit = (long long)TERMS * 4 * NB * 16, whole = 4 * a.lay.blocks * unit;
-  // groups of warps: no more than have tiles and leave room for the features beside two stages each, four at least
-  p.groups = (int)std::min<long long>(kW4Groups<NB>, (a.lay.tiles + ctas - 1) / ctas);
-  while (p.groups > 4 && room - 2ll * p.groups * p.stage_bytes < whole) --p.groups;
-  // an operand is of 4 units, or 2 where the registers of 4 do not fit beside those of the sums
-  constexpr int kStep = NB <= 8 ? 4 : 2;
+  p.groups = (int)std::min<long long>(kW4Groups<NB>, (a.lay.tiles + ctas - 1) / ctas);      // those that have tiles
+  constexpr int kStep = kW4Step<NB>;
   p.a_cols = 16 * kStep;
   p.d_cols = (kStep + gunits - 1) / gunits * N;
   p.groups = std::min(p.groups, 512 / (p.a_cols + p.d_cols));
@@ -801,7 +811,8 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const auto k = k_w4_project<NB, TERMS, EPI>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * kW4Group<NB, EPI == kOutputs>), (size_t)p.smem, s, a, p);
+  return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * kW4Group<NB, EPI == kOutputs>),
+                    (size_t)p.smem, s, a, p);
 }
 
 }  // namespace

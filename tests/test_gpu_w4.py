@@ -86,7 +86,8 @@ def test_w4(B, V, K, group, zeros):
 @pytest.mark.parametrize("B,V,K,group,zeros,x", [(1, 151936, 256, 64, False, BF16), (4, 50257, 1024, 128, True, BF16),
                                                  (64, 32003, 512, 32, True, F32), (5, 8000, 4096, 32, False, F32),
                                                  (64, 1500, 4096, 128, True, BF16), (1, 700, 65536, 64, True, BF16),
-                                                 (3, 129, 20000, 32, True, F32)])
+                                                 (3, 129, 20000, 32, True, F32), (64, 80000, 128, 32, True, BF16),
+                                                 (40, 100000, 64, 64, False, BF16), (20, 79992, 96, 128, True, F32)])
 def test_w4_larger(B, V, K, group, zeros, x):
     c = Case(B, V, K, group, zeros, x)
     check(c, F32)
