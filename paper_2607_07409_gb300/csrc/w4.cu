@@ -391,7 +391,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   __shared__ uint32_t tmem_base;
   __shared__ volatile int abort_flag;
   __shared__ uint32_t largest[NB];          // bits of the requests' largest features
-  __shared__ float2 scaled[NB], back[NB];   // their powers of two, in two factors, and what takes them back
+  __shared__ float2 scaled[NB];             // their powers of two, in two factors
+  __shared__ __align__(16) float back[2][NB];      // what takes them back, the same way
   // (through a reduction, which leaves it in a uniform register: the products' operands are then worked
   // out there, and not fetched from a thread's registers one by one)
   const int tid = threadIdx.x, lane = tid & 31, warp = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)tid >> 5);
@@ -489,7 +490,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     const bool finite = largest[tid] < 0x7F800000u;
     const int up = finite ? feature_shift(largest[tid]) : 0, sh = -up;
     scaled[tid] = make_float2(pow2i(up / 2), pow2i(up - up / 2));
-    back[tid] = finite ? make_float2(pow2i(sh / 2), pow2i(sh - sh / 2)) : make_float2(NAN, NAN);
+    back[0][tid] = finite ? pow2i(sh / 2) : NAN;
+    back[1][tid] = finite ? pow2i(sh - sh / 2) : NAN;
   }
   __syncthreads();
   // The features of units u0 .. u1 - 1.
@@ -669,13 +671,15 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     // Products of 8 requests, n on. (All of them before any is stored: the compiler keeps each reading of back[]
     // behind the stores before it, and one after another they took half of 64 requests' time.)
     const auto products = [&](int n, float (&y)[8]) {
-      float2 f[8];
+      float4 f[2][2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = back[n0 + n + i];
+      for (int k = 0; k < 4; ++k) f[k >> 1][k & 1] = *reinterpret_cast<const float4*>(&back[k >> 1][n0 + n + 4 * (k & 1)]);
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) split2(tot[(n + i) / 2], y[i], y[i + 1]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = y[i] * f[i].x * f[i].y;
+      for (int k = 0; k < 2; ++k) {
+        const f32x2* t = tot + n / 2 + 2 * k;
+        split2(mul2(mul2(t[0], pair2(f[0][k].x, f[0][k].y)), pair2(f[1][k].x, f[1][k].y)), y[4 * k], y[4 * k + 1]);
+        split2(mul2(mul2(t[1], pair2(f[0][k].z, f[0][k].w)), pair2(f[1][k].z, f[1][k].w)), y[4 * k + 2], y[4 * k + 3]);
+      }
     };
     const auto lay_out = [&](int h) {       // S requests' products of the tile, h S on, by requests
 #pragma unroll
@@ -695,15 +699,18 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
           float y[8];
           products(n, y);
           const long long at = (long long)(b0 + n0 + n) * a.ld_out + v;
-          if (a.out_f32) {
+          const auto put = [&](auto* out, auto value) {
+            if (n + 8 <= nb) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (n + i < nb) static_cast<float*>(a.out)[at + i * a.ld_out] = y[i];
-          } else {
+              for (int i = 0; i < 8; ++i) out[i * a.ld_out] = value(y[i]);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (n + i < nb) static_cast<__nv_bfloat16*>(a.out)[at + i * a.ld_out] = __float2bfloat16_rn(y[i]);
-          }
+              for (int i = 0; i < 8; ++i)
+                if (n + i < nb) out[i * a.ld_out] = value(y[i]);
+            }
+          };
+          if (a.out_f32) put(static_cast<float*>(a.out) + at, [](float x) { return x; });
+          else put(static_cast<__nv_bfloat16*>(a.out) + at, [](float x) { return __float2bfloat16_rn(x); });
         }
       }
     } else if (live && own_rows) {
@@ -713,7 +720,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
           if (n >= nb) break;
           float y[2];
           split2(tot[0], y[0], y[1]);
-          combine_one<EPI == kKeys>(a, y[n] * back[n].x * back[n].y, b0 + n, v, tops[n]);
+          combine_one<EPI == kKeys>(a, y[n] * back[0][n] * back[1][n], b0 + n, v, tops[n]);
         }
       }
     } else if (live) {
