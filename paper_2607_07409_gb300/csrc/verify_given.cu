@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kGivenThreads = 512, kGivenWarps = kGivenThreads / 32;
 constexpr int kGroup = 256;                // columns of a warp's step, 8 a lane
-constexpr int kMarks = 4;                  // sums a lane keeps of its way along a run
 
 __device__ __forceinline__ bool is_probability(float x) { return x >= 0.f && x < INFINITY; }
 
@@ -104,11 +103,38 @@ struct Sum2 {
     lo = __fadd_rn(lo, __fadd_rn(e, y));
   }
 };
-// max(0, p - q) as a float32 and what it rounded off (p > q >= 0: both exact, Dekker's fast two-sum).
-__device__ __forceinline__ void rest_of(float p, float q, float& w, float& e) {
-  const float d = __fsub_rn(p, q);
-  w = fmaxf(d, 0.f);
-  e = d > 0.f ? __fsub_rn(__fsub_rn(p, d), q) : 0.f;
+__device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { return fma2(b, both2(-1.f), a); }
+// Two of them in pairs of float32, two operations an instruction.
+struct Sum2Pair {
+  f32x2 hi, lo;
+  __device__ __forceinline__ f32x2 left(f32x2 x) {       // what the addition of x rounds off
+    const f32x2 t = add2(hi, x), b = sub2(t, hi);
+    const f32x2 e = add2(sub2(hi, sub2(t, b)), sub2(x, b));
+    hi = t;
+    return e;
+  }
+  __device__ __forceinline__ void add(f32x2 x) { lo = add2(lo, left(x)); }
+  __device__ __forceinline__ void add(f32x2 x, f32x2 y) { lo = add2(lo, add2(left(x), y)); }
+  __device__ __forceinline__ Sum2 both() const {
+    float h0, h1, l0, l1;
+    split2(hi, h0, h1);
+    split2(lo, l0, l1);
+    Sum2 s{h0, l0};
+    s.add(h1, l1);
+    return s;
+  }
+};
+// max(0, p - q) as float32 and what it rounded off (p > q >= 0: both exact, Dekker's fast two-sum).
+__device__ __forceinline__ void rest_of(const float* p, const float* q, float* w, float* e) {
+  const f32x2 p2 = pair2(p[0], p[1]), q2 = pair2(q[0], q[1]), d2 = sub2(p2, q2);
+  float d[2];
+  split2(d2, d[0], d[1]);
+  split2(sub2(sub2(p2, d2), q2), e[0], e[1]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    w[i] = fmaxf(d[i], 0.f);
+    e[i] = d[i] > 0.f ? e[i] : 0.f;
+  }
 }
 
 // A warp's sum, in every lane (fixed order).
@@ -146,7 +172,7 @@ struct Border {
 
 template <typename P, typename Q, bool DRAFT, bool VEC>
 __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyGivenArgs a, int cluster) {
-  __shared__ Sum2 warp_sum[kGivenWarps], marks[kGivenWarps][kMarks][32];
+  __shared__ Sum2 warp_sum[kGivenWarps];
   __shared__ int warp_bad[kGivenWarps];
   __shared__ SlicePart parts[2][kMaxCluster];
   __shared__ Border border;
@@ -168,15 +194,18 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
   if (!code) {                              // (the same in every CTA of the request)
     const P* p = static_cast<const P*>(a.target.p) + b * a.target.ld_b + k.a * a.target.ld;
     const Q* q = DRAFT ? static_cast<const Q*>(a.draft.p) + b * a.draft.ld_b + k.a * a.draft.ld : nullptr;
-    const int groups = (a.V + kGroup - 1) / kGroup, runs = cluster * kGivenWarps, run = rank * kGivenWarps + warp;
-    const int g0 = (int)((long long)groups * run / runs), g1 = (int)((long long)groups * (run + 1) / runs);
+    const int groups = (a.V + kGroup - 1) / kGroup, runs = cluster * kGivenWarps;
+    const auto first_of = [&](int w) { return (int)((long long)groups * (rank * kGivenWarps + w) / runs); };
     // The weights of a group: from max(0, p - q), or from p.
     const auto weights = [&](bool rest, int g, const float (&x)[8], const float (&y)[8], float (&w)[8], float (&e)[8]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        w[i] = x[i];
-        e[i] = 0.f;
-        if (DRAFT && rest) rest_of(x[i], y[i], w[i], e[i]);
+      for (int i = 0; i < 8; i += 2) {
+        if (DRAFT && rest) {
+          rest_of(x + i, y + i, w + i, e + i);
+        } else {
+          w[i] = x[i], w[i + 1] = x[i + 1];
+          e[i] = e[i + 1] = 0.f;
+        }
       }
       if (!DRAFT && rest && (unsigned)(k.token - g * kGroup) < (unsigned)kGroup) {
 #pragma unroll
@@ -186,35 +215,41 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
     };
     bool rest = k.token >= 0;
     for (int pass = 0;; ++pass) {
-      Sum2 s{0.f, 0.f};
+      Sum2Pair sums{0ull, 0ull};
       unsigned most = 0;                    // of the bits: what is no probability is above infinity's, or it
       const auto add = [&](int g, const float (&x)[8], const float (&y)[8]) {
+        // + 0: -0 is a probability
+        const auto look = [&](const float (&z)[8]) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            float z0, z1;
+            split2(add2(pair2(z[i], z[i + 1]), 0ull), z0, z1);
+            most = max(most, max(__float_as_uint(z0), __float_as_uint(z1)));
+          }
+        };
         float w[8], e[8];
         weights(rest, g, x, y, w, e);
+        look(x);
+        if (DRAFT && rest) look(y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          most = max(most, __float_as_uint(x[i] + 0.f));
-          if (DRAFT && rest) most = max(most, __float_as_uint(y[i] + 0.f));
-          s.add(w[i], e[i]);
+        for (int i = 0; i < 8; i += 2) {
+          if (DRAFT) sums.add(pair2(w[i], w[i + 1]), pair2(e[i], e[i + 1]));
+          else sums.add(pair2(w[i], w[i + 1]));
         }
       };
-      for (int i = 0; i < kMarks; ++i) {    // (a run in as many parts, its sums behind each kept)
-        const int end = g0 + (int)((long long)(g1 - g0) * (i + 1) / kMarks);
-        int g = g0 + (int)((long long)(g1 - g0) * i / kMarks);
-        for (; g < end; g += 2) {
-          float x[2][8], y[2][8];
+      const int g1 = first_of(warp + 1);
+      for (int g = first_of(warp); g < g1; g += 2) {
+        float x[2][8], y[2][8];
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            if (u && g + 1 >= end) continue;
-            load8<P, VEC>(p, (g + u) * kGroup, a.V, x[u]);
-            if (DRAFT && rest) load8<Q, VEC>(q, (g + u) * kGroup, a.V, y[u]);
-          }
-          add(g, x[0], y[0]);
-          if (g + 1 < end) add(g + 1, x[1], y[1]);
+        for (int u = 0; u < 2; ++u) {
+          if (u && g + 1 >= g1) continue;
+          load8<P, VEC>(p, (g + u) * kGroup, a.V, x[u]);
+          if (DRAFT && rest) load8<Q, VEC>(q, (g + u) * kGroup, a.V, y[u]);
         }
-        marks[warp][i][lane] = s;
+        add(g, x[0], y[0]);
+        if (g + 1 < g1) add(g + 1, x[1], y[1]);
       }
-      s = warp_sum2(s);
+      const Sum2 s = warp_sum2(sums.both());
       const int bad = __any_sync(0xFFFFFFFFu, most >= 0x7F800000u);
       if (lane == 0) {
         warp_sum[warp] = s;
@@ -274,97 +309,91 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
         continue;
       }
       code = f.code;
-      if (warp == f.run) {
-        mine = true;
-        // The part of the run whose sums exceed it, by the marks, then the group; where by roundings none
-        // does, the last with weight.
-        Sum2 m[kMarks];
-#pragma unroll
-        for (int i = 0; i < kMarks; ++i) m[i] = warp_sum2(marks[warp][i][lane]);
-        double c0 = f.before;
-        int part = -1;
-#pragma unroll
-        for (int i = 0; i < kMarks; ++i) {
-          const bool some = i == 0 ? m[0].hi > 0.f : m[i].hi > m[i - 1].hi || m[i].lo > m[i - 1].lo;
-          if (!some || (part >= 0 && f.before + total_of(m[part]) > f.at)) continue;
-          part = i;
-          if (i > 0) c0 = f.before + total_of(m[i - 1]);
-        }
-        part = __shfl_sync(0xFFFFFFFFu, max(part, 0), 0);
-        c0 = __shfl_sync(0xFFFFFFFFu, c0, 0);
-        const int p0 = g0 + (int)((long long)(g1 - g0) * part / kMarks);
-        const int p1 = g0 + (int)((long long)(g1 - g0) * (part + 1) / kMarks);
-        double base = c0;
-        int at = p0;
+      if (f.run >= 0) {
+        // The run in sixteen parts, a warp each, the one with the border in sixteen again, until a part is a group at
+        // most, which then lies in its warp's registers. (f.run and f.before become those of the part.)
         float w[8], e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = e[i] = 0.f;
-        for (int g2 = p0; g2 < p1; g2 += 2) {
-          float x[2][8], y[2][8];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            load8<P, VEC>(p, (g2 + i) * kGroup, g2 + i < p1 ? a.V : 0, x[i]);
-            if (DRAFT && rest) load8<Q, VEC>(q, (g2 + i) * kGroup, g2 + i < p1 ? a.V : 0, y[i]);
-          }
-          bool over = false;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (over) continue;
-            float w2[8], e2[8];
-            weights(rest, g2 + i, x[i], y[i], w2, e2);
-            Sum2 t{0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) t.add(w2[j], e2[j]);
-            t = warp_sum2(t);
-            const double upto = __shfl_sync(0xFFFFFFFFu, c0 + total_of(t), 0);
-            if (t.hi > 0.f) {
-              at = g2 + i;
-              base = c0;
-              over = upto > f.at;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) w[j] = w2[j], e[j] = e2[j];
-            }
-            c0 = upto;
-          }
-          if (over) break;
-        }
-        // The column. VEC: the lanes in order, each its 8; else 8 times the lanes in order.
-        constexpr int kParts = VEC ? 1 : 8, kEach = 8 / kParts;
-        bool found = false;
-#pragma unroll
-        for (int h = 0; h < kParts; ++h) {
-          if (found) continue;
+        int at, lo = first_of(f.run), hi = first_of(f.run + 1);
+        double base = f.before;
+        int part;
+        for (;;) {
+          const auto edge = [&](int w2) { return lo + (int)((long long)(hi - lo) * w2 / kGivenWarps); };
           Sum2 t{0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < kEach; ++i) t.add(w[h * kEach + i], e[h * kEach + i]);
-          Sum2 upto = t;                    // up to and including the lane's
+          for (int i = 0; i < 8; ++i) w[i] = e[i] = 0.f;
+          at = edge(warp);
+          for (int g = at; g < edge(warp + 1); ++g) {
+            float x[8], y[8];
+            load8<P, VEC>(p, g * kGroup, a.V, x);
+            if (DRAFT && rest) load8<Q, VEC>(q, g * kGroup, a.V, y);
+            weights(rest, g, x, y, w, e);
 #pragma unroll
-          for (int d = 1; d < 32; d <<= 1) {
-            const float hi = __shfl_up_sync(0xFFFFFFFFu, upto.hi, d), lo = __shfl_up_sync(0xFFFFFFFFu, upto.lo, d);
-            if (lane >= d) upto.add(hi, lo);
+            for (int i = 0; i < 8; ++i) t.add(w[i], e[i]);
           }
-          const double incl = total_of(upto);
-          const double up = __shfl_up_sync(0xFFFFFFFFu, incl, 1);
-          const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > f.at);
-          const unsigned some = __ballot_sync(0xFFFFFFFFu, t.hi > 0.f);
-          const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
-          if (who >= 0) {                   // the border, or for now the last with weight
-            const double left = f.at - (base + (lane ? up : 0.0));       // of the lane's own
-            const float left_hi = (float)left, left_lo = (float)(left - (double)left_hi);
-            int v = -1;
-            bool past = false;
-            Sum2 c{0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-              const float w2 = w[h * kEach + i];
-              c.add(w2, e[h * kEach + i]);
-              if (!past && w2 > 0.f) v = at * kGroup + (VEC ? lane * 8 + i : h * 32 + lane);
-              past |= v >= 0 && __fadd_rn(__fsub_rn(c.hi, left_hi), __fsub_rn(c.lo, left_lo)) > 0.f;
+          t = warp_sum2(t);
+          if (lane == 0) warp_sum[warp] = t;
+          __syncthreads();
+          if (warp == 0) {
+            const Sum2 of = warp_sum[lane & (kGivenWarps - 1)];
+            const double c = base + warp_scan(lane < kGivenWarps ? total_of(of) : 0.0, kGivenWarps);
+            const unsigned over = __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && c > f.at);
+            const unsigned some = __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && of.hi > 0.f);
+            // (by roundings none may exceed it: then the last with weight)
+            const int pick = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : 0;
+            const double prev = __shfl_sync(0xFFFFFFFFu, c, max(pick - 1, 0));
+            if (lane == 0) {
+              border.run = pick;
+              border.before = pick ? prev : base;
             }
-            bonus = __shfl_sync(0xFFFFFFFFu, v, who);
           }
-          found = over != 0;
-          base += __shfl_sync(0xFFFFFFFFu, incl, 31);
+          __syncthreads();
+          part = border.run;
+          base = border.before;
+          if (hi - lo <= kGivenWarps) break;
+          const int next = edge(part);
+          hi = edge(part + 1);
+          lo = next;
+        }
+        mine = warp == part;
+        if (mine) {
+          // The column. VEC: the lanes in order, each its 8; else 8 times the lanes in order.
+          constexpr int kParts = VEC ? 1 : 8, kEach = 8 / kParts;
+          bool found = false;
+#pragma unroll
+          for (int h = 0; h < kParts; ++h) {
+            if (found) continue;
+            Sum2 t{0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) t.add(w[h * kEach + i], e[h * kEach + i]);
+            Sum2 upto = t;                    // up to and including the lane's
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+              const float hi = __shfl_up_sync(0xFFFFFFFFu, upto.hi, d), lo = __shfl_up_sync(0xFFFFFFFFu, upto.lo, d);
+              if (lane >= d) upto.add(hi, lo);
+            }
+            const double incl = total_of(upto);
+            const double up = __shfl_up_sync(0xFFFFFFFFu, incl, 1);
+            const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > f.at);
+            const unsigned some = __ballot_sync(0xFFFFFFFFu, t.hi > 0.f);
+            const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
+            if (who >= 0) {                   // the border, or for now the last with weight
+              const double left = f.at - (base + (lane ? up : 0.0));       // of the lane's own
+              const float left_hi = (float)left, left_lo = (float)(left - (double)left_hi);
+              int v = -1;
+              bool past = false;
+              Sum2 c{0.f, 0.f};
+#pragma unroll
+              for (int i = 0; i < kEach; ++i) {
+                const float w2 = w[h * kEach + i];
+                c.add(w2, e[h * kEach + i]);
+                if (!past && w2 > 0.f) v = at * kGroup + (VEC ? lane * 8 + i : h * 32 + lane);
+                past |= v >= 0 && __fadd_rn(__fsub_rn(c.hi, left_hi), __fsub_rn(c.lo, left_lo)) > 0.f;
+              }
+              bonus = __shfl_sync(0xFFFFFFFFu, v, who);
+            }
+            found = over != 0;
+            base += __shfl_sync(0xFFFFFFFFu, incl, 31);
+          }
         }
       }
       break;
