@@ -3,17 +3,19 @@
 // A cluster of 1 to 8 CTAs takes a request. The first warp of each finds the tokens kept, a
 // lane a position, so that their reads wait for one another no more than once; then the row that the
 // bonus token comes from is summed, once: a warp has a run of groups of 256 columns. The
-// warps' sums meet in shared memory, the CTAs' in each other's; the warp whose run has the border
-// finds the part of it by sums kept on the way, reads that again, out of L2, and walks it.
+// warps' sums meet in shared memory, the CTAs' in each other's; the CTA that has the border reads
+// the run it lies in again, out of L2, a sixteenth a warp, and the warp whose group has it finds the column.
 //
 // Sums decide which token comes out, so they are as good as float64's: float64 itself issues
 // at 1/64 of float32's rate here, so a lane keeps a float32 sum and what its additions
-// rounded off (Knuth's two-sum), 48 bits, and only totals are float64, in one warp. A
+// rounded off (Knuth's two-sum), 48 bits, two such in packed pairs, and only totals are float64, in one warp. A
 // difference p - q is kept the same way.
 //
 // What bounds it: latency, one part after another. 64 blocks of 16 over 151936 (78 MB, 11.5 us at a
-// copy's rate) 24 to 27 us: 2 for the tokens, 16 for the stream in two CTAs an SM (1.7 of them), 8 for the
-// sums, the exchange, the border's part and its column; one block of 8 over 32000 7.8 us.
+// copy's rate) 18 us, 64 draws 10.6 (5.8): 2 for the tokens, the stream in two CTAs an SM (1.7 of them), 4 for
+// the sums, the exchange, the border's run and its column; one block of 8 over 32000 6.9 us. (One warp that walked the
+// border's run alone, by sums kept on the way: 24, 13.2, 7.8. The rows through a ring of asynchronous copies
+// hid the latency of blocks' reads and not what its instructions cost draws: 23.1 and 15.6 then.)
 #include "dels_device.cuh"
 #include "row_stream.cuh"
 
@@ -238,16 +240,18 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
         }
       };
       const int g1 = first_of(warp + 1);
-      for (int g = first_of(warp); g < g1; g += 2) {
-        float x[2][8], y[2][8];
+      constexpr int kAhead = 2;              // groups read at a time (four of plain rows spill: 64 draws 12.2 us for 11.0)
+      for (int g = first_of(warp); g < g1; g += kAhead) {
+        float x[kAhead][8], y[kAhead][8];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (u && g + 1 >= g1) continue;
+        for (int u = 0; u < kAhead; ++u) {
+          if (g + u >= g1) continue;
           load8<P, VEC>(p, (g + u) * kGroup, a.V, x[u]);
           if (DRAFT && rest) load8<Q, VEC>(q, (g + u) * kGroup, a.V, y[u]);
         }
-        add(g, x[0], y[0]);
-        if (g + 1 < g1) add(g + 1, x[1], y[1]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (g + u < g1) add(g + u, x[u], y[u]);
       }
       const Sum2 s = warp_sum2(sums.both());
       const int bad = __any_sync(0xFFFFFFFFu, most >= 0x7F800000u);
