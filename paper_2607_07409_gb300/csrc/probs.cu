@@ -165,8 +165,15 @@ __global__ void __launch_bounds__(kStreamThreads, F == kPlain ? 5 : 3) k_row_pro
         v[u].k = pos;
         if constexpr (F != kPlain) {
           if constexpr (sizeof(T) == 4) v[u].s.load(row.S + pos, kHalf<T>);
+          if (row.has_p() && (row.sh & 3) == 0) {      // (on its 16 bytes too: the prior starts there)
+            const float4 a4 = __ldg(reinterpret_cast<const float4*>(row.P + pos));
+            const float4 b4 = __ldg(reinterpret_cast<const float4*>(row.P + pos + kHalf<T>));
+            pr[u][0] = a4.x; pr[u][1] = a4.y; pr[u][2] = a4.z; pr[u][3] = a4.w;
+            pr[u][4] = b4.x; pr[u][5] = b4.y; pr[u][6] = b4.z; pr[u][7] = b4.w;
+          } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) pr[u][i] = row.p_at(elem_pos<T, VEC>(pos, i));
+            for (int i = 0; i < 8; ++i) pr[u][i] = row.p_at(elem_pos<T, VEC>(pos, i));
+          }
         }
       }
       if (!waited) copies_wait<0>();
