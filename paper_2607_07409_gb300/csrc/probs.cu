@@ -150,46 +150,64 @@ __global__ void __launch_bounds__(kStreamThreads, F == kPlain ? 5 : 3) k_row_pro
       else if constexpr (F != kPlain) copy16(dst + 16, row.S + pos);
     }
     copies_commit();
+    // The whole ones U at a time: what they take beside their copies is read before the copies are waited for. Those
+    // at the row's or the slice's ends one by one.
     constexpr int U = F == kPlain ? 1 : 2;
-    bool waited = false;
-    for (int it = 0; it < items; it += U) {
-      Item<T, F, VEC> v[U];
-      float pr[U][8], x[8], sv[8];
+    const int p0 = item_pos<T, VEC>(k0, 0, tid), lead = p0 >= row.sh ? 0 : 1;
+    const int past = k1 - kHalf<T> - 4 - p0 < 0 ? 0 : (k1 - kHalf<T> - 4 - p0) / kStreamStep + 1;
+    const auto beside = [&](int pos, Item<T, F, VEC>& v, float (&pr)[8]) {
+      v.k = pos;
+      if constexpr (F != kPlain) {
+        if constexpr (sizeof(T) == 4) v.s.load(row.S + pos, kHalf<T>);
+        if (row.has_p() && (row.sh & 3) == 0) {        // (on its 16 bytes too: the prior starts there)
+          const float4 a4 = __ldg(reinterpret_cast<const float4*>(row.P + pos));
+          const float4 b4 = __ldg(reinterpret_cast<const float4*>(row.P + pos + kHalf<T>));
+          pr[0] = a4.x; pr[1] = a4.y; pr[2] = a4.z; pr[3] = a4.w;
+          pr[4] = b4.x; pr[5] = b4.y; pr[6] = b4.z; pr[7] = b4.w;
+        } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int pos = item_pos<T, VEC>(k0, it + u, tid);
-        if (!whole(pos)) {
-          v[u].load(row, pos, k1, pr[u]);
-          continue;
-        }
-        v[u].k = pos;
-        if constexpr (F != kPlain) {
-          if constexpr (sizeof(T) == 4) v[u].s.load(row.S + pos, kHalf<T>);
-          if (row.has_p() && (row.sh & 3) == 0) {      // (on its 16 bytes too: the prior starts there)
-            const float4 a4 = __ldg(reinterpret_cast<const float4*>(row.P + pos));
-            const float4 b4 = __ldg(reinterpret_cast<const float4*>(row.P + pos + kHalf<T>));
-            pr[u][0] = a4.x; pr[u][1] = a4.y; pr[u][2] = a4.z; pr[u][3] = a4.w;
-            pr[u][4] = b4.x; pr[u][5] = b4.y; pr[u][6] = b4.z; pr[u][7] = b4.w;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pr[u][i] = row.p_at(elem_pos<T, VEC>(pos, i));
-          }
+          for (int i = 0; i < 8; ++i) pr[i] = row.p_at(elem_pos<T, VEC>(pos, i));
         }
       }
+    };
+    const auto take = [&](Item<T, F, VEC>& v, const float (&pr)[8]) {
+      const uint4* at = reinterpret_cast<const uint4*>(held + (v.k - k0));
+      v.l.w[0] = at[0];
+      if constexpr (sizeof(T) == 4) v.l.w[1] = *reinterpret_cast<const uint4*>(held + (v.k - k0) + kHalf<T>);
+      else if constexpr (F != kPlain) v.s.w[0] = at[1];
+      float x[8], sv[8];
+      v.template values<true>(row, pr, x, sv);
+      m = fmaxf(m, max8(x));
+      if (F != kPlain) hold(x, v.k);
+    };
+    bool waited = false;
+    int it = lead;
+    for (; it + U <= past; it += U) {
+      Item<T, F, VEC> v[U];
+      float pr[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) beside(p0 + (it + u) * kStreamStep, v[u], pr[u]);
       if (!waited) copies_wait<0>();
       waited = true;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const bool w = whole(v[u].k);
-        if (w) {
-          const uint4* at = reinterpret_cast<const uint4*>(held + (v[u].k - k0));
-          v[u].l.w[0] = at[0];
-          if constexpr (sizeof(T) == 4) v[u].l.w[1] = *reinterpret_cast<const uint4*>(held + (v[u].k - k0) + kHalf<T>);
-          else if constexpr (F != kPlain) v[u].s.w[0] = at[1];
-        }
-        v[u].template values<true>(row, pr[u], x, sv);
+      for (int u = 0; u < U; ++u) take(v[u], pr[u]);
+    }
+    if (!waited) copies_wait<0>();
+    const int left = it;
+#pragma unroll 1
+    for (it = lead ? 0 : left; it < items; it = it < lead ? left : it + 1) {
+      const int pos = p0 + it * kStreamStep;
+      if (pos >= k1) break;
+      Item<T, F, VEC> v;
+      float pr[8], x[8], sv[8];
+      if (whole(pos)) {
+        beside(pos, v, pr);
+        take(v, pr);
+      } else {
+        v.load(row, pos, k1, pr);
+        v.template values<true>(row, pr, x, sv);
         m = fmaxf(m, max8(x));
-        if (F != kPlain || !w) hold(x, v[u].k);
+        hold(x, v.k);
       }
     }
   } else {
