@@ -81,21 +81,22 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 // mma.sync, with the same operands, issues at most one such product in 32 cycles of a quarter
 // SM: 151936 x 2560 for 8 requests 45 us, 151936 x 256 for 64 37 us, at that rate.
 //
-// Four warps take a tile of 128 rows, a thread a row: codes of a block of 128 inputs from
-// shared memory (bulk copies into a ring of their own, blocks ahead), operand pairs into
+// Four warps (eight from 17 requests on) take a tile of 128 rows, a thread a row: codes of a block of 128 inputs
+// from shared memory (bulk copies into a ring of their own, blocks ahead), operand pairs into
 // tensor memory, one thread's MMAs over them with the features as the other operand,
 // the groups' sums back and scaled into the thread's registers. Up to four such groups on an SM
-// run beside one another and share nothing but the features: one's waits are the others' time.
-// (With the parts of that in warps of their own, behind mbarriers with buffers to spare, the
+// run beside one another and share nothing but the features: one's waits are the others' time. Few tiles of a
+// long K are shared by several groups, each a range of it. A group's products and copies are issued by a warp
+// of its own, which meets the others at one named barrier a step; these go on without waiting there.
+// (With every part of a step in warps of its own, behind mbarriers with buffers to spare, the
 // hand-overs' instructions took more than the overlap gave: 103 us against 80 at 8 requests.)
 // The features stay in shared memory; a K whose features do not fit is taken in parts.
 //
-// What bounds it: a step (four units of 32 inputs, with more than 8 requests two) goes from one of its
-// parts to the next, about 1900 cycles of instructions that wait for the one before, of which four groups
-// hide three quarters; 68 instructions a unit, 0.45 of the issue slots. 151936 x 1024 for one request
-// 20 us, x 2560 for 8 44 us (12.3 and 30.7 for the bytes at a copy's rate), 151936 x 256 for 64 24.5 us
-// (6.1), 32003 x 1000 for 5 with float32 features 12.4 us (2.7). Eight groups of half the registers spill:
-// 26.5, 55.8; their sums' registers leave 64 requests three.
+// What bounds it: a step (four units of 32 inputs, two with 9 to 16 requests and with more than 32) goes from one of
+// its parts to the next, 1300 cycles, most of them the instructions that take the codes apart: four warps a
+// scheduler issue about three quarters of the time. 151936 x 1024 for one request 17.9 us, x 2560 for 8 35.8 us
+// (12.3 and 30.7 for the bytes at a copy's rate), 151936 x 256 for 64 16.8 us (6.1), 32003 x 1000 for 5 with
+// float32 features 9.7 us (2.7; a start of 4 us, eight steps one after another).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
@@ -263,6 +264,7 @@ constexpr int kW4Stages = 8;               // of a ring, at most
 struct W4Plan {
   int groups;
   int stages, stage_bytes;
+  int split;           // groups that share a tile, each a range of its blocks (features resident)
   int part_units;      // a multiple of 4: the features of so many units stay (all of them, or a part at a time)
   int parts;
   int a_cols, d_cols;  // tensor memory of a group: its operand, its sums
@@ -382,8 +384,10 @@ __device__ __forceinline__ void combine_columns(const W4Args& a, const float* y,
   }
 }
 
-template <int NB, int TERMS, int EPI>
-__global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>, 1) k_w4_project(const W4Args a, const W4Plan p) {
+// SPLIT: tiles are shared by p.split groups (else its registers cost 2 to 4 %).
+template <int NB, int TERMS, int EPI, bool SPLIT>
+__global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>, 1)
+    k_w4_project(const W4Args a, const W4Plan p) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int N = NB < 16 ? 16 : NB;                  // requests of an MMA: rows past NB are its first ones again
   constexpr int H = kW4Halves<NB>, kMine = NB / H;      // requests of a thread
@@ -425,12 +429,14 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   if (tid == 0) pdl_trigger();
 
   // ---- a group's tiles: every (CTAs x groups)th, and its copies, a block each
-  const long long tile0 = (long long)grp * gridDim.x + blockIdx.x, apart = (long long)gridDim.x * p.groups;
+  const int split = SPLIT ? p.split : 1, slot = grp / split, share = grp - slot * split;
+  const int kb0 = a.lay.blocks * share / split, own_blocks = a.lay.blocks * (share + 1) / split - kb0;
+  const long long tile0 = (long long)slot * gridDim.x + blockIdx.x, apart = (long long)gridDim.x * (p.groups / split);
   const long long rounds = (a.lay.tiles + apart - 1) / apart;
-  const int copies = tile0 < a.lay.tiles ? (int)((a.lay.tiles - tile0 + apart - 1) / apart) * a.lay.blocks : 0;
-  int to_copy = copies - p.stages, next_kb = p.stages % a.lay.blocks, next_st = 0;            // of the thread that copies
-  const uint8_t* next_block = a.packed + (tile0 + p.stages / a.lay.blocks * apart) * a.lay.tile_bytes +
-                              (long long)next_kb * a.lay.block_bytes;
+  const int copies = tile0 < a.lay.tiles ? (int)((a.lay.tiles - tile0 + apart - 1) / apart) * own_blocks : 0;
+  int to_copy = copies - p.stages, next_kb = p.stages % own_blocks, next_st = 0;            // of the thread that copies
+  const uint8_t* next_block = a.packed + (tile0 + p.stages / own_blocks * apart) * a.lay.tile_bytes +
+                              (long long)(kb0 + next_kb) * a.lay.block_bytes;
   const auto issue_copy = [&] {
     if (to_copy <= 0) return;
     --to_copy;
@@ -438,9 +444,9 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     bulk_load(ring + next_st * p.stage_bytes, next_block, a.lay.block_bytes, &full[grp][next_st]);
     next_block += a.lay.block_bytes;
     if (++next_st == p.stages) next_st = 0;
-    if (++next_kb == a.lay.blocks) {
+    if (++next_kb == own_blocks) {
       next_kb = 0;
-      next_block += (apart - 1) * a.lay.tile_bytes;
+      next_block += apart * a.lay.tile_bytes - (long long)own_blocks * a.lay.block_bytes;
     }
   };
   // ---- the requests' features, read before the first copies take the memory; those of a warp's first
@@ -457,8 +463,8 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     if (warp + i * warps < all) load_task(warp + i * warps, kept[i]);
   fence_proxy_async_global();
   if ((kApart ? issues : place == copier) && lane < p.stages) {             // the first ones, a lane each
-    const long long tile = tile0 + lane / a.lay.blocks * apart;
-    const int kb = lane % a.lay.blocks;
+    const long long tile = tile0 + lane / own_blocks * apart;
+    const int kb = kb0 + lane % own_blocks;
     if (tile < a.lay.tiles) {
       mbar_arrive_expect_tx(&full[grp][lane], a.lay.block_bytes);
       bulk_load(ring + (size_t)lane * p.stage_bytes,
@@ -525,7 +531,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   const uint32_t acol = __reduce_max_sync(0xFFFFFFFFu, tmem_base) + (uint32_t)grp * (p.a_cols + p.d_cols);
   const uint32_t dcol = acol + p.a_cols;
   const uint32_t quadrant = (uint32_t)(warp & 3) << 21;                // the warp's 32 lanes of tensor memory
-  const uint32_t x0 = (uint32_t)smem_desc_plain(smem_u32(operand), NB * 16, 0);
+  const uint32_t x0 = (uint32_t)smem_desc_plain(smem_u32(operand), NB * 16, 0) + (uint32_t)(kb0 * 4) * (4 * NB);
   bool dead = false;                        // a wait ran out: the rest runs through without waiting
   const auto wait = [&](uint64_t* bar, int parity) {
     // (the clock is read in long waits alone: a reading takes about 1000 cycles)
@@ -542,7 +548,9 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   asm("" : "+r"(base));                   // (a register, not a constant)
   f32x2 tot[kMine / 2];
   constexpr int S = kW4Side<NB>;
-  float* sides = reinterpret_cast<float*>(operand + (size_t)TERMS * p.part_units * 4 * NB);      // of the records
+  // shares of tiles [slots][split - 1][NB][128]
+  float* joins = reinterpret_cast<float*>(operand + (size_t)TERMS * p.part_units * 4 * NB);
+  float* sides = joins + (SPLIT ? (size_t)(p.groups - p.groups / split) * NB * kW4Rows : 0);                 // of the records
   const bool own_rows = EPI != kOutputs && NB == 8 && a.B <= 2;
   constexpr int kTops = NB == 8 ? 2 : kMine / S;
   RowTop tops[kTops];                       // of the half's requests row % S, row % S + S; of 0 and 1 where these have their own rows
@@ -652,7 +660,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
       }
       if (!live) continue;
       using std::integral_constant;
-      const int blocks = (pu1 - pu0) / 4;
+      const int blocks = resident ? own_blocks : (pu1 - pu0) / 4;
       const integral_constant<int, 1> one;
       const integral_constant<int, 2> two;
       const integral_constant<int, 4> four;
@@ -662,6 +670,26 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
       else run(blocks, step_units, four);
     }
     if (issues) continue;
+    if (SPLIT && live) {
+      // ---- the shares of a tile, added up by its first group in their order
+      const auto all_shares = [&] {
+        asm volatile("bar.sync %0, %1;" ::"r"(kW4Groups<NB> * (1 + H) + slot + 1), "r"(split * 128 * H) : "memory");
+      };
+      float* at = joins + ((size_t)slot * (split - 1) * NB + half * kMine) * kW4Rows + row;
+      if (share) {
+        at += (size_t)(share - 1) * NB * kW4Rows;
+#pragma unroll
+        for (int n = 0; n < kMine; n += 2) split2(tot[n / 2], at[n * kW4Rows], at[(n + 1) * kW4Rows]);
+      }
+      all_shares();
+      if (!share)
+        for (int i = 1; i < split; ++i, at += (size_t)NB * kW4Rows)
+#pragma unroll
+          for (int n = 0; n < kMine; n += 2)
+            tot[n / 2] = add2(tot[n / 2], pair2(at[n * kW4Rows], at[(n + 1) * kW4Rows]));
+      all_shares();                         // (read: the next tile's may come)
+      if (share) continue;
+    }
     const long long v = tile * kW4Rows + row;
     const int n0 = half * kMine, nb = min(kMine, a.B - b0 - n0);        // the thread's requests
     float* side = sides + (size_t)(grp * H + half) * S * kW4Pitch;
@@ -794,7 +822,7 @@ template <int NB, int TERMS, int EPI>
 cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const int sms = device_sm_count();
   const int side = EPI == kOutputs ? 0 : kW4Groups<NB> * kW4Halves<NB> * kW4Side<NB> * kW4Pitch * 4;
-  const int room = device_max_smem_optin() - 4096 - side;
+  int room = device_max_smem_optin() - 4096 - side;
   if (sms <= 0 || room <= 0) return cudaErrorInvalidValue;
   const int btiles = (a.B + NB - 1) / NB, ctas = w4_ctas(a, NB, sms);
   W4Plan p{};
@@ -802,11 +830,27 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   const int gunits = a.group / kW4Unit;
   p.stage_bytes = (a.lay.block_bytes + 127) / 128 * 128;
   const long long unit = (long long)TERMS * 4 * NB * 16, whole = 4 * a.lay.blocks * unit;
-  p.groups = (int)std::min<long long>(kW4Groups<NB>, (a.lay.tiles + ctas - 1) / ctas);      // those that have tiles
+  // Groups that share a tile: as many as get through the CTA's tiles soonest, what comes with sharing (a join, and all
+  // groups' first copies at once) taken as four steps' time, a block being one step or two. 8 requests of 17789 x
+  // 4096: one group a tile 22.4 us, four 13.8; one of 10000 x 1024: 8.1, 6.9; 32003 x 1000 for 5: 9.8, two 10.1.
   constexpr int kStep = kW4Step<NB>;
+  const auto join_bytes = [](int slots, int split) { return (long long)slots * (split - 1) * NB * kW4Rows * 4; };
+  long long best = 0;
+  for (int split = 1; split <= kW4Groups<NB> && split <= a.lay.blocks; split *= 2) {
+    const int slots = (int)std::min<long long>(kW4Groups<NB> / split, (a.lay.tiles + ctas - 1) / ctas);
+    const long long rounds = (a.lay.tiles + (long long)ctas * slots - 1) / ((long long)ctas * slots);
+    const long long time = rounds * ((a.lay.blocks + split - 1) / split) + (split > 1 ? kStep : 0);
+    const long long left = room - join_bytes(slots, split) - 2ll * slots * split * p.stage_bytes;
+    if (split > 1 && (time >= best || left < whole)) continue;
+    best = time;
+    p.split = split;
+    p.groups = slots * split;
+  }
+  const int join = (int)join_bytes(p.groups / p.split, p.split);
+  room -= join;
   p.a_cols = 16 * kStep;
   p.d_cols = (kStep + gunits - 1) / gunits * N;
-  p.groups = std::min(p.groups, 512 / (p.a_cols + p.d_cols));
+  static_assert(kW4Groups<NB> * kStep * (16 + N) <= 512, "a group's operand and sums, of one unit a group of inputs");
   p.tmem_cols = 32;
   while ((int)p.tmem_cols < p.groups * (p.a_cols + p.d_cols)) p.tmem_cols *= 2;
   // the features, or of those that do not fit as many as leave two stages; what they leave is the rings'
@@ -814,8 +858,8 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   p.part_units = (int)(std::min(whole, beside) / unit / 4 * 4);
   p.parts = (4 * a.lay.blocks + p.part_units - 1) / p.part_units;
   p.stages = (int)std::min<long long>(kW4Stages, (room - p.part_units * unit) / ((long long)p.groups * p.stage_bytes));
-  p.smem = (int)(p.groups * p.stages * p.stage_bytes + p.part_units * unit) + side;
-  const auto k = k_w4_project<NB, TERMS, EPI>;
+  p.smem = (int)(p.groups * p.stages * p.stage_bytes + p.part_units * unit) + join + side;
+  const auto k = p.split > 1 ? k_w4_project<NB, TERMS, EPI, true> : k_w4_project<NB, TERMS, EPI, false>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);
   if (e != cudaSuccess) return e;
   return launch_pdl(k, dim3((unsigned)ctas, (unsigned)btiles), dim3(p.groups * kW4Group<NB, EPI == kOutputs>),

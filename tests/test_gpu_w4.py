@@ -87,7 +87,12 @@ def test_w4(B, V, K, group, zeros):
                                                  (64, 32003, 512, 32, True, F32), (5, 8000, 4096, 32, False, F32),
                                                  (64, 1500, 4096, 128, True, BF16), (1, 700, 65536, 64, True, BF16),
                                                  (3, 129, 20000, 32, True, F32), (64, 80000, 128, 32, True, BF16),
-                                                 (40, 100000, 64, 64, False, BF16), (20, 79992, 96, 128, True, F32)])
+                                                 (40, 100000, 64, 64, False, BF16), (20, 79992, 96, 128, True, F32),
+                                                 # tiles that several groups of warps share, one each and several
+                                                 (2, 1264, 4096, 64, False, F32), (1, 50257, 4096, 32, True, BF16),
+                                                 (10, 50257, 4096, 128, True, BF16), (16, 20000, 1100, 64, False, F32),
+                                                 (20, 3000, 700, 32, True, F32), (64, 1500, 1024, 64, False, BF16),
+                                                 (64, 45000, 1024, 128, True, BF16)])
 def test_w4_larger(B, V, K, group, zeros, x):
     c = Case(B, V, K, group, zeros, x)
     check(c, F32)

@@ -20,6 +20,7 @@ HEADS = {
     "mlp2": synth.HeadSpec("mlp", "bf16", 64, 96, 96, window=3, n_layers=2),
     "xfmr": synth.HeadSpec("xfmr", "bf16", 64, 256, 64, n_heads=4, max_pos=16),
     "markov": synth.HeadSpec("markov", "bf16", 0, 0, 272),
+    "wide": synth.HeadSpec("markov", "bf16", 0, 0, 1040),
 }
 
 
@@ -65,7 +66,10 @@ CASES = [("gru", 1, 5, 1024, "bf16", 32, False, False), ("gru", 5, 4, 5000, "f32
          # several tiles for every group of warps
          ("markov", 5, 2, 100008, "bf16", 128, True, False), ("markov", 2, 2, 100008, "f32", 32, False, False),
          ("gru", 12, 2, 100008, "bf16", 64, False, True), ("mlp", 20, 2, 60008, "bf16", 32, True, False),
-         ("markov", 64, 2, 60008, "f32", 64, False, False)]
+         ("markov", 64, 2, 60008, "f32", 64, False, False),
+         # tiles that several groups share
+         ("wide", 1, 3, 3008, "bf16", 64, True, False), ("wide", 7, 2, 24008, "f32", 32, False, False),
+         ("wide", 12, 2, 5000, "bf16", 128, True, False), ("wide", 40, 2, 2008, "f32", 64, False, False)]
 
 
 @pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}-{c[1]}-{c[3]}-{c[5]}")
