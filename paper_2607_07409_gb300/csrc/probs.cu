@@ -6,9 +6,9 @@
 // and the sum beside it; the CTAs exchange the two, and what is left is a factor for
 // each. Rows whose slices do not fit are read three times.
 //
-// What bounds it: the bytes of plain rows (1088 bf16 rows of 151936 to float32 161 us, 147 at a
+// What bounds it: the bytes of plain rows (1088 bf16 rows of 151936 to float32 160 us, 147 at a
 // copy's rate); of fused float32 rows three CTAs an SM, in 2.2 rounds, that load, exchange and store one
-// after another (128 rows of 151936 61 us, 34.7 at that rate). An exponential is taken twice (for the
+// after another (128 rows of 151936 59 us, 34.7 at that rate). An exponential is taken twice (for the
 // sum, for the output), which costs less than keeping it where the slice is held in bf16.
 #include <algorithm>
 
