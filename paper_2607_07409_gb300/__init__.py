@@ -680,6 +680,32 @@ def _row_stride(x: torch.Tensor, shape, what: str) -> int:
     return step
 
 
+_CODE = {torch.float32: DELS_F32, torch.bfloat16: DELS_BF16}
+
+
+def _row_args(t: torch.Tensor, shape, device: int, what: str):
+    """Device address, elements from one row to the next and dtype code of [rows, V] numbers whose rows may be
+    strided (a single row's stride may be anything)."""
+    code = _CODE.get(t.dtype)
+    if code is None or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{what} must be float32 or bfloat16 {list(shape)} on cuda:{device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+    rows, V = shape
+    step, one = t.stride()
+    if rows <= 1:
+        step = V
+    if V > 1 and one != 1:
+        raise ValueError(f"{what}: expected [rows, V] numbers whose rows are dense")
+    if step < V:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), step, code
+
+
+def _stream_on(stream, device: int) -> Optional[int]:
+    """``_stream`` of a call on a device that is the current one."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+
+
 def _of(t, dtype, shape, device: int, what) -> Optional[int]:
     """Device address of a dense tensor of this dtype and shape on this device."""
     if t is None:
@@ -729,7 +755,8 @@ def rows_of(rows: int, V: int, long=None, short=None, log_prior=None, alpha=None
         raise ValueError("expected a CUDA tensor: the library's entry points take device pointers")
     shape, dev, dtype = (rows, V), one.get_device(), one.dtype
     x = Rows()
-    x.dtype = dtype_code(dtype)
+    code = _CODE.get(dtype)
+    x.dtype = dtype_code(dtype) if code is None else code
     if long is not None:
         x.long_logits = _logits(long, shape, dtype, dev, "long")
         x.long_stride = _row_stride(long, shape, "long")
@@ -1022,11 +1049,13 @@ class RowProbs:
         if out is None:
             if self._out is None:
                 self._out = _empty_on(stream, (self.rows, self.V), self.dtype, self.device)
-            out = self._out
-        shape = (self.rows, self.V)
-        to = _logits(out, shape, self.dtype, self._dev, "out")
-        r = self._call(ctypes.byref(x), self.rows, self.V, to, self._code, _row_stride(out, shape, "out"), self._ws,
-                       self.ws_bytes, _stream(stream))
+            out, to, step = self._out, self._out.data_ptr(), self.V
+        else:
+            to, step, code = _row_args(out, (self.rows, self.V), self._dev, "out")
+            if code != self._code:
+                raise ValueError(f"out must be {self.dtype}")
+        r = self._call(ctypes.byref(x), self.rows, self.V, to, self._code, step, self._ws, self.ws_bytes,
+                       _stream_on(stream, self._dev))
         if r != DELS_OK:
             raise DelsError(r, "dels_row_probs")
         _increment_version((out,))
@@ -1038,8 +1067,10 @@ class RowProbs:
 
 def _probs_of(t: torch.Tensor, B: int, rows: int, V: int, device: int, what: str) -> Probs:
     """``dels_probs`` of a [B, rows, V] tensor (requests and rows may be strided). The caller keeps it alive."""
-    if t.shape != (B, rows, V) or t.get_device() != device:
-        raise ValueError(f"{what} must be [{B}, {rows}, {V}] on cuda:{device}, got {list(t.shape)} on {t.device}")
+    code = _CODE.get(t.dtype)
+    if code is None or t.shape != (B, rows, V) or t.get_device() != device:
+        raise ValueError(f"{what} must be float32 or bfloat16 [{B}, {rows}, {V}] on cuda:{device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
     sb, sr, one = t.stride()
     if rows == 1:
         sr = V
@@ -1047,7 +1078,7 @@ def _probs_of(t: torch.Tensor, B: int, rows: int, V: int, device: int, what: str
         sb = rows * sr
     if (V > 1 and one != 1) or sr < V or sb < (rows - 1) * sr + V:
         raise ValueError(f"{what}: expected [B, rows, V] probabilities whose rows are dense and apart")
-    return Probs(t.data_ptr(), dtype_code(t.dtype), sb, sr)
+    return Probs(t.data_ptr(), code, sb, sr)
 
 
 class BlockVerifier:
@@ -1064,6 +1095,7 @@ class BlockVerifier:
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
         self.accept_len, self.bonus = torch.empty(2, B, dtype=torch.int32, device=self.device).unbind(0)
         self._own = [t.data_ptr() for t in (self.accept_len, self.bonus, self.workspace)]
+        self._writes = (self.accept_len, self.bonus)
         self._call = lib().dels_verify_given
 
     def __call__(self, tokens, target: torch.Tensor, uniforms: torch.Tensor, *, draft=None, lengths=None, stream=None):
@@ -1083,10 +1115,10 @@ class BlockVerifier:
         acc, bonus, ws = self._own
         r = self._call(tok, ctypes.byref(p), None if q is None else ctypes.byref(q), u,
                        _of(lengths, torch.int32, (B,), dev, "lengths"), B, n, V, acc, bonus, ws, self.ws_bytes,
-                       _stream(stream))
+                       _stream_on(stream, dev))
         if r != DELS_OK:
             raise DelsError(r, "dels_verify_given")
-        _increment_version((self.accept_len, self.bonus))
+        _increment_version(self._writes)
         return self.accept_len, self.bonus
 
     def status(self, stream=None) -> int:
@@ -1108,23 +1140,24 @@ class W4Matrix:
         self.ws_bytes = dels_w4_project_workspace_bytes(self.struct, 1)
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
         self._ws = self.workspace.data_ptr()
+        self._ref = ctypes.byref(self.struct)
         self._call = lib().dels_w4_project
 
     def project(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32,
                 stream=None) -> torch.Tensor:
         """[B, V] = x W^T of features [B, K] (float32 or bfloat16; rows may be strided), in a new tensor of
         ``dtype`` (``stream``'s own memory) or in ``out`` (of either; rows may be strided; no part of ``x``)."""
-        _need_current(self._dev)
-        if x.dim() != 2:
+        dev = self._dev
+        _need_current(dev)
+        shape = x.shape
+        if len(shape) != 2:
             raise ValueError(f"x must be [B, {self.K}]")
-        B = x.shape[0]
+        B = shape[0]
         if out is None:
             out = _empty_on(stream, (B, self.V), dtype, self.device)
-        xs, os_ = (B, self.K), (B, self.V)
-        xp = _logits(x, xs, x.dtype, self._dev, "x")
-        op = _logits(out, os_, out.dtype, self._dev, "out")
-        r = self._call(ctypes.byref(self.struct), xp, dtype_code(x.dtype), _row_stride(x, xs, "x"), B, op,
-                       dtype_code(out.dtype), _row_stride(out, os_, "out"), self._ws, self.ws_bytes, _stream(stream))
+        xp, xs, xc = _row_args(x, (B, self.K), dev, "x")
+        op, os_, oc = _row_args(out, (B, self.V), dev, "out")
+        r = self._call(self._ref, xp, xc, xs, B, op, oc, os_, self._ws, self.ws_bytes, _stream_on(stream, dev))
         if r != DELS_OK:
             raise DelsError(r, "dels_w4_project")
         _increment_version((out,))
