@@ -159,6 +159,14 @@ __device__ __forceinline__ double warp_scan(double x, int lanes) {
   return x;
 }
 
+// The first lane whose sum up to and including its own is over the border, of those with weight: sums up to the same
+// column differ with the order they were taken in, and an empty lane's may be over where the one before it is not. By
+// roundings none may be over: then the last with weight (-1: none has any).
+__device__ __forceinline__ int first_over(bool over, bool weight) {
+  const unsigned some = __ballot_sync(0xFFFFFFFFu, weight), at = __ballot_sync(0xFFFFFFFFu, over) & some;
+  return at ? __ffs(at) - 1 : 31 - __clz(some);
+}
+
 struct SlicePart {
   double sum;
   int bad, pad;
@@ -292,14 +300,10 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
         Border f{(double)__ldg(a.uniforms + (long long)b * (a.n + 1) + a.n) * total, 0.0, -1, 0, 0};
         if (any_bad || (!(total > 0.0) && !rest)) f.code = DELS_STATUS_NONFINITE;
         else if (!(total > 0.0)) f.again = 1;
-        else if (__ffs(__ballot_sync(0xFFFFFFFFu, upto > f.at)) - 1 == rank) {
+        else if (first_over(upto > f.at, part.sum > 0.0) == rank) {
           const double before = __shfl_sync(0xFFFFFFFFu, upto, max(rank - 1, 0));
           const double c = (rank ? before : 0.0) + own;            // up to and including the lane's run
-          const unsigned over = __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && c > f.at);
-          const unsigned some =
-              __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && warp_sum[lane & (kGivenWarps - 1)].hi > 0.f);
-          // (by roundings none may exceed it: then the last with weight)
-          f.run = over ? __ffs(over) - 1 : 31 - __clz(some);
+          f.run = first_over(c > f.at, lane < kGivenWarps && warp_sum[lane & (kGivenWarps - 1)].hi > 0.f);
           const double prev = __shfl_sync(0xFFFFFFFFu, c, max(f.run - 1, 0));
           f.before = f.run ? prev : (rank ? before : 0.0);
         }
@@ -340,10 +344,7 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
           if (warp == 0) {
             const Sum2 of = warp_sum[lane & (kGivenWarps - 1)];
             const double c = base + warp_scan(lane < kGivenWarps ? total_of(of) : 0.0, kGivenWarps);
-            const unsigned over = __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && c > f.at);
-            const unsigned some = __ballot_sync(0xFFFFFFFFu, lane < kGivenWarps && of.hi > 0.f);
-            // (by roundings none may exceed it: then the last with weight)
-            const int pick = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : 0;
+            const int pick = max(first_over(c > f.at, lane < kGivenWarps && of.hi > 0.f), 0);
             const double prev = __shfl_sync(0xFFFFFFFFu, c, max(pick - 1, 0));
             if (lane == 0) {
               border.run = pick;
@@ -377,9 +378,8 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
             }
             const double incl = total_of(upto);
             const double up = __shfl_up_sync(0xFFFFFFFFu, incl, 1);
-            const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > f.at);
-            const unsigned some = __ballot_sync(0xFFFFFFFFu, t.hi > 0.f);
-            const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
+            const int who = first_over(base + incl > f.at, t.hi > 0.f);
+            const bool over = __any_sync(0xFFFFFFFFu, base + incl > f.at && t.hi > 0.f);
             if (who >= 0) {                   // the border, or for now the last with weight
               const double left = f.at - (base + (lane ? up : 0.0));       // of the lane's own
               const float left_hi = (float)left, left_lo = (float)(left - (double)left_hi);
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
               }
               bonus = __shfl_sync(0xFFFFFFFFu, v, who);
             }
-            found = over != 0;
+            found = over;
             base += __shfl_sync(0xFFFFFFFFu, incl, 31);
           }
         }
