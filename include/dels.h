@@ -631,8 +631,8 @@ typedef struct {
  * exact; sums are as good as float64's. Probabilities need no sum of 1. A drafted
  * token outside [0, V), a uniform outside [0, 1) or a length outside 0 .. n sets
  * DELS_STATUS_BAD_TOKEN or DELS_STATUS_BAD_VALUE; a probability that is negative, NaN
- * or infinite where it is read, or a row of p whose sum is 0
- * or above float32's range, DELS_STATUS_NONFINITE: the
+ * or infinite where it is read, a row of p whose sum is 0, or weights w whose sum is
+ * above float32's largest number, DELS_STATUS_NONFINITE: the
  * request's bonus is then -1, its length the tokens kept before that was met. What
  * lies behind the token that decides is not looked at.
  * Limits: 0 <= B <= 2^20, 0 <= n <= 1024, 1 <= V <= 2^30; pointers aligned to their

@@ -16,6 +16,8 @@
 // the sums, the exchange, the border's run and its column; one block of 8 over 32000 6.9 us. (One warp that walked the
 // border's run alone, by sums kept on the way: 24, 13.2, 7.8. The rows through a ring of asynchronous copies
 // hid the latency of blocks' reads and not what its instructions cost draws: 23.1 and 15.6 then.)
+#include <cfloat>
+
 #include "dels_device.cuh"
 #include "row_stream.cuh"
 
@@ -296,7 +298,8 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
         const SlicePart part = lane < cluster ? parts[pass][lane] : SlicePart{0.0, 0, 0};
         const double upto = warp_scan(part.sum, kMaxCluster);
         const double total = __shfl_sync(0xFFFFFFFFu, upto, kMaxCluster - 1);
-        const bool any_bad = __any_sync(0xFFFFFFFFu, part.bad != 0) || !(total < INFINITY);
+        // (a run's sum in float32 pairs is beyond them where the whole is: the same in any split)
+        const bool any_bad = __any_sync(0xFFFFFFFFu, part.bad != 0) || !(total <= (double)FLT_MAX);
         Border f{(double)__ldg(a.uniforms + (long long)b * (a.n + 1) + a.n) * total, 0.0, -1, 0, 0};
         if (any_bad || (!(total > 0.0) && !rest)) f.code = DELS_STATUS_NONFINITE;
         else if (!(total > 0.0)) f.again = 1;

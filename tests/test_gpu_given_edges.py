@@ -1,4 +1,5 @@
-"""The verification from given numbers where it can go wrong: empty columns beside a border."""
+"""The verification from given numbers where it can go wrong: empty columns beside a border, sums at
+float32's end."""
 from fractions import Fraction
 
 import pytest
@@ -10,6 +11,7 @@ pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
 F32 = torch.float32
+NONFINITE = dels.DELS_STATUS_NONFINITE
 
 
 def draw(p, u, h=None):
@@ -51,3 +53,31 @@ def test_the_border_lies_where_there_is_weight(V, step, more, u, offset):
             right.append(v)
         upto += Fraction(w)
     assert status == 0 and bonus[0] in right
+
+
+# ---------------------------------------------------------------- sums at float32's end
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("B,V", [(1, 32768), (1, 100), (40, 32768), (200, 9001)])
+def test_sums_above_float32(B, V, offset):
+    """A row whose entries are finite and whose sum is not within float32 is flagged wherever the entries lie, in any
+    batch; one that sums to float32's largest number is not."""
+    most = torch.finfo(F32).max
+    rows = []
+    for cols, values, ok in [([0, V - 1], [2e38, 2e38], False), ([5, 6], [2e38, 2e38], False),
+                             ([5, V // 2], [2e38, 2e38], False), ([0, V // 3, V - 1], [1.2e38] * 3, False),
+                             ([7], [most], True), ([7, V - 2], [most, 2.0 ** 80], False),
+                             ([3, V - 1], [2.0 ** 127, most - 2.0 ** 127], True)]:
+        rows.append((cols, values, ok))
+    for cols, values, ok in rows:
+        buf = torch.zeros(B * (V + offset), dtype=F32)
+        p = buf.as_strided((B, V), (V + offset, 1), offset) if offset else buf.view(B, V)
+        p[:, 1] = 1.0
+        p[B // 2] = 0.0
+        for c, x in zip(cols, values):
+            p[B // 2, c] = x
+        dev = buf.to(DEV)
+        p = dev.as_strided((B, V), (V + offset, 1), offset) if offset else dev.view(B, V)
+        bonus, status = draw(p, 0.25)
+        assert (bonus[B // 2], status) == ((cols[0], 0) if ok else (-1, NONFINITE)), (cols, values)
+        assert all(x == 1 for b, x in enumerate(bonus) if b != B // 2)
