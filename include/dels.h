@@ -628,7 +628,8 @@ typedef struct {
  *   uniforms [device] [B, n + 1] float32 of [0, 1);
  *   out_accept_len, out_bonus [device] [B] int32.
  * n = 0 draws a token of each row (tokens and draft are not read). Comparisons are
- * exact; sums are as good as float64's. Probabilities need no sum of 1. A drafted
+ * exact; sums are kept to 2^-32 of the whole at worst, whatever V, and as well as float64
+ * ones where roundings go both ways. Probabilities need no sum of 1. A drafted
  * token outside [0, V), a uniform outside [0, 1) or a length outside 0 .. n sets
  * DELS_STATUS_BAD_TOKEN or DELS_STATUS_BAD_VALUE; a probability that is negative, NaN
  * or infinite where it is read, a row of p whose sum is 0, or weights w whose sum is

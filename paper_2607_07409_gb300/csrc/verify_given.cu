@@ -6,10 +6,10 @@
 // warps' sums meet in shared memory, the CTAs' in each other's; the CTA that has the border reads
 // the run it lies in again, out of L2, a sixteenth a warp, and the warp whose group has it finds the column.
 //
-// Sums decide which token comes out, so they are as good as float64's: float64 itself issues
-// at 1/64 of float32's rate here, so a lane keeps a float32 sum and what its additions
-// rounded off (Knuth's two-sum), 48 bits, two such in packed pairs, and only totals are float64, in one warp. A
-// difference p - q is kept the same way.
+// Sums decide which token comes out, so float32's are not enough, and float64 itself issues
+// at 1/64 of float32's rate here: a lane keeps a float32 sum and what its additions
+// rounded off (Knuth's two-sum), 48 bits, two such in packed pairs, and only totals are float64, in one warp, of
+// a row and, where it is long, of each of its parts. A difference p - q is kept the same way.
 //
 // What bounds it: latency, one part after another. 64 blocks of 16 over 151936 (78 MB, 11.5 us at a
 // copy's rate) 18 us, 64 draws 10.6 (5.8): 2 for the tokens, the stream in two CTAs an SM (1.7 of them), 4 for
@@ -26,6 +26,10 @@ namespace {
 
 constexpr int kGivenThreads = 512, kGivenWarps = kGivenThreads / 32;
 constexpr int kGroup = 256;                // columns of a warp's step, 8 a lane
+// Groups after which a warp closes a sum and adds it up in float64: more than a warp has of a row of 262144 columns. What
+// additions rounded off is itself rounded: of 256 a sum of the lane, 2^-33 of it at worst. (Closed never, a
+// row of 2^28 weights, the first half 1.1, came out some columns off.)
+constexpr int kClose = 64;
 
 __device__ __forceinline__ bool is_probability(float x) { return x >= 0.f && x < INFINITY; }
 
@@ -182,9 +186,17 @@ struct Border {
   int code;
 };
 
-template <typename P, typename Q, bool DRAFT, bool VEC>
+// A warp's sum so far, added to *far in float64.
+__device__ __noinline__ void close_sum(double* far, f32x2 hi, f32x2 lo) {
+  const Sum2 s = warp_sum2(Sum2Pair{hi, lo}.both());
+  if ((threadIdx.x & 31) == 0) *far += total_of(s);
+}
+
+// FAR: a warp has more than kClose groups.
+template <typename P, typename Q, bool DRAFT, bool VEC, bool FAR>
 __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyGivenArgs a, int cluster) {
   __shared__ Sum2 warp_sum[kGivenWarps];
+  __shared__ double warp_far[kGivenWarps];           // what a warp's sum has been closed at, with warp_sum behind it
   __shared__ int warp_bad[kGivenWarps];
   __shared__ SlicePart parts[2][kMaxCluster];
   __shared__ Border border;
@@ -225,6 +237,14 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
           if (g * kGroup + (VEC ? lane * 8 + i : i * 32 + lane) == k.token) w[i] = 0.f;
       }
     };
+    // The sum of warp `lane`, and whether it has any weight, as the first warp reads them.
+    const auto warp_total = [&] {
+      if (lane >= kGivenWarps) return 0.0;
+      return FAR ? warp_far[lane] + total_of(warp_sum[lane]) : total_of(warp_sum[lane]);
+    };
+    const auto warp_some = [&] {
+      return lane < kGivenWarps && (warp_sum[lane].hi > 0.f || (FAR && warp_far[lane] > 0.0));
+    };
     bool rest = k.token >= 0;
     for (int pass = 0;; ++pass) {
       Sum2Pair sums{0ull, 0ull};
@@ -249,19 +269,26 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
           else sums.add(pair2(w[i], w[i + 1]));
         }
       };
+      if (FAR && lane == 0) warp_far[warp] = 0.0;
       const int g1 = first_of(warp + 1);
       constexpr int kAhead = 2;              // groups read at a time (four of plain rows spill: 64 draws 12.2 us for 11.0)
-      for (int g = first_of(warp); g < g1; g += kAhead) {
-        float x[kAhead][8], y[kAhead][8];
+      for (int g = first_of(warp);;) {
+        const int stop = FAR ? min(g + kClose, g1) : g1;
+        for (; g < stop; g += kAhead) {
+          float x[kAhead][8], y[kAhead][8];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          if (g + u >= g1) continue;
-          load8<P, VEC>(p, (g + u) * kGroup, a.V, x[u]);
-          if (DRAFT && rest) load8<Q, VEC>(q, (g + u) * kGroup, a.V, y[u]);
+          for (int u = 0; u < kAhead; ++u) {
+            if (g + u >= stop) continue;
+            load8<P, VEC>(p, (g + u) * kGroup, a.V, x[u]);
+            if (DRAFT && rest) load8<Q, VEC>(q, (g + u) * kGroup, a.V, y[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u)
+            if (g + u < stop) add(g + u, x[u], y[u]);
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-          if (g + u < g1) add(g + u, x[u], y[u]);
+        if (!FAR || g >= g1) break;
+        close_sum(&warp_far[warp], sums.hi, sums.lo);
+        sums = Sum2Pair{0ull, 0ull};
       }
       const Sum2 s = warp_sum2(sums.both());
       const int bad = __any_sync(0xFFFFFFFFu, most >= 0x7F800000u);
@@ -273,7 +300,7 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
       // float64 from here on, by the first warp: every warp's instruction takes 16 cycles of the SM's
       double own = 0.0;
       if (warp == 0) {
-        own = warp_scan(lane < kGivenWarps ? total_of(warp_sum[lane]) : 0.0, kGivenWarps);
+        own = warp_scan(warp_total(), kGivenWarps);
         const int own_bad = __any_sync(0xFFFFFFFFu, lane < kGivenWarps && warp_bad[lane]);
         const double sum = __shfl_sync(0xFFFFFFFFu, own, kGivenWarps - 1);
         if (cluster > 1) {
@@ -306,7 +333,7 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
         else if (first_over(upto > f.at, part.sum > 0.0) == rank) {
           const double before = __shfl_sync(0xFFFFFFFFu, upto, max(rank - 1, 0));
           const double c = (rank ? before : 0.0) + own;            // up to and including the lane's run
-          f.run = first_over(c > f.at, lane < kGivenWarps && warp_sum[lane & (kGivenWarps - 1)].hi > 0.f);
+          f.run = first_over(c > f.at, warp_some());
           const double prev = __shfl_sync(0xFFFFFFFFu, c, max(f.run - 1, 0));
           f.before = f.run ? prev : (rank ? before : 0.0);
         }
@@ -333,7 +360,13 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
 #pragma unroll
           for (int i = 0; i < 8; ++i) w[i] = e[i] = 0.f;
           at = edge(warp);
+          if (FAR && lane == 0) warp_far[warp] = 0.0;
           for (int g = at; g < edge(warp + 1); ++g) {
+            if (FAR && g > at && (g - at) % (kClose / 2) == 0) {
+              const Sum2 far = warp_sum2(t);
+              if (lane == 0) warp_far[warp] += total_of(far);
+              t = Sum2{0.f, 0.f};
+            }
             float x[8], y[8];
             load8<P, VEC>(p, g * kGroup, a.V, x);
             if (DRAFT && rest) load8<Q, VEC>(q, g * kGroup, a.V, y);
@@ -345,9 +378,8 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
           if (lane == 0) warp_sum[warp] = t;
           __syncthreads();
           if (warp == 0) {
-            const Sum2 of = warp_sum[lane & (kGivenWarps - 1)];
-            const double c = base + warp_scan(lane < kGivenWarps ? total_of(of) : 0.0, kGivenWarps);
-            const int pick = max(first_over(c > f.at, lane < kGivenWarps && of.hi > 0.f), 0);
+            const double c = base + warp_scan(warp_total(), kGivenWarps);
+            const int pick = max(first_over(c > f.at, warp_some()), 0);
             const double prev = __shfl_sync(0xFFFFFFFFu, c, max(pick - 1, 0));
             if (lane == 0) {
               border.run = pick;
@@ -418,7 +450,9 @@ __global__ void __launch_bounds__(kGivenThreads, 2) k_verify_given(const VerifyG
 
 template <typename P, typename Q, bool DRAFT>
 cudaError_t launch_types(const VerifyGivenArgs& a, bool vec, int cluster, cudaStream_t s) {
-  const auto k = vec ? k_verify_given<P, Q, DRAFT, true> : k_verify_given<P, Q, DRAFT, false>;
+  const bool far = (long long)a.V > (long long)kClose * kGroup * kGivenWarps * cluster;
+  const auto k = far ? (vec ? k_verify_given<P, Q, DRAFT, true, true> : k_verify_given<P, Q, DRAFT, false, true>)
+                     : (vec ? k_verify_given<P, Q, DRAFT, true, false> : k_verify_given<P, Q, DRAFT, false, false>);
   return launch_pdl_cluster(k, dim3((unsigned)a.B * (unsigned)cluster), dim3(kGivenThreads), 0, s, cluster, a, cluster);
 }
 

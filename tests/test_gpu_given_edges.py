@@ -1,5 +1,6 @@
 """The verification from given numbers where it can go wrong: empty columns beside a border, sums at
-float32's end."""
+float32's end, rows far longer than a vocabulary."""
+import math
 from fractions import Fraction
 
 import pytest
@@ -81,3 +82,26 @@ def test_sums_above_float32(B, V, offset):
         bonus, status = draw(p, 0.25)
         assert (bonus[B // 2], status) == ((cols[0], 0) if ok else (-1, NONFINITE)), (cols, values)
         assert all(x == 1 for b, x in enumerate(bonus) if b != B // 2)
+
+
+# ---------------------------------------------------------------- rows far longer than a vocabulary
+
+@pytest.mark.parametrize("V,offset", [(1 << 28, 0), ((1 << 26) + 8, 1)])
+def test_a_long_row(V, offset):
+    """Weights of a = 1.1 (as float32) in the first half, of 1 behind them: the column is floor(u total - a V / 2) + V / 2 for
+    the larger uniforms. No border of these lies within 0.05 of a weight, 2^-33 of the whole (a sum kept
+    in float32 pairs throughout has lost 2^-24 of the first half, and comes out some columns off)."""
+    a = torch.tensor(1.1, dtype=F32).item()
+    p = torch.ones(1, V + offset, dtype=F32, device=DEV)[:, offset:]
+    p[:, :V // 2] = a
+    front, total = Fraction(a) * (V // 2), (Fraction(a) + 1) * (V // 2)
+    h = dels.BlockVerifier(1, 0, V, device=DEV)
+    u = 0.53 + 0.4 * torch.rand(40, generator=torch.Generator().manual_seed(5))
+    n = 0
+    for x in u.tolist():
+        at = Fraction(x) * total - front
+        if not 0.05 < at - math.floor(at) < 0.95:
+            continue
+        assert draw(p, x, h) == ([V // 2 + math.floor(at)], 0)
+        n += 1
+    assert n > 20
