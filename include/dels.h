@@ -136,7 +136,8 @@ typedef struct {
  * rounded to bf16 for W_vocab like the other heads'.
  *
  * w_vocab4, bf16 heads only: W_vocab (W_M) as a 4-bit matrix of V rows and d_rank
- * inputs, read in place of w_vocab, which may then be NULL: the same products, with
+ * inputs, where w_vocab is NULL (a head with a w_vocab is not read past it, as by
+ * libraries of version 200 and before, whose structure ended there): the same products, with
  * float32 accumulation, in drafting at both temperatures and in the verification
  * of sampled blocks. (A drafter's weights change which tokens it proposes, not what the
  * verified output follows.)
@@ -154,7 +155,7 @@ typedef struct {
   const void* emb;
   const void* w[8];
   const void* w_vocab;
-  const dels_w4* w_vocab4;       /* [host], read during a call, or NULL */
+  const dels_w4* w_vocab4;       /* [host], read during a call where w_vocab is NULL; or NULL */
 } dels_local_head;
 
 /* ---- self test of the bounded waits ------------------------------------- */

@@ -473,14 +473,19 @@ W4Args w4_args(const dels_w4& m, const void* X, int B, int* status) {
   return a;
 }
 
+// The 4-bit vocabulary matrix of a head, or null. A head with a w_vocab is not read past it: its caller may have been
+// built when the structure ended there.
+const dels_w4* vocab4(const dels_local_head* head) { return head->w_vocab ? nullptr : head->w_vocab4; }
+
 // The vocabulary projection of a bf16 head fused with the combine, from either form of its weights.
 bool plan_vocab(Gemm& g, const dels_local_head* head, int B, int V, int n, const void* X, int K, const void* longp,
                 dels_dtype ldt, const float* prior, float alpha, float beta, void* partials, int partial_ld,
                 int* status, int sms, bool pair_stages, bool sample) {
-  if (!head->w_vocab4)
+  const dels_w4* m = vocab4(head);
+  if (!m)
     return plan_combine(g, B, V, n, X, K, head->w_vocab, longp, ldt, prior, alpha, beta, partials, partial_ld, status,
                         sms, pair_stages, sample);
-  W4Args& a = g.w4 = w4_args(*head->w_vocab4, X, B, status);
+  W4Args& a = g.w4 = w4_args(*m, X, B, status);
   a.longp = longp;
   a.long_f32 = ldt == DELS_F32;
   a.ld_long = (long long)n * V;
@@ -757,7 +762,7 @@ int validate_head(const dels_local_head* h, int n) {
   if (h->wdtype != DELS_F32 && h->wdtype != DELS_BF16) return DELS_ERR_BAD_DTYPE;
   const bool bf = h->wdtype == DELS_BF16;
   auto dim_ok = [&](int d) { return d > 0 && d <= 65536 && (!bf || d % 16 == 0) && (bf || d % 4 == 0); };
-  const dels_w4* m = h->w_vocab4;
+  const dels_w4* m = vocab4(h);
   if (!h->emb || (!h->w_vocab && !m)) return DELS_ERR_NULL_POINTER;
   if (m) {
     if (!bf) return DELS_ERR_UNSUPPORTED;
@@ -805,7 +810,7 @@ int validate_draft(const dels_local_head* head, const void* long_logits, dels_dt
   if (ldt != DELS_F32 && ldt != DELS_BF16) return DELS_ERR_BAD_DTYPE;
   int r = validate_head(head, n);
   if (r != DELS_OK) return r;
-  if (head->w_vocab4 && head->w_vocab4->V != V) return DELS_ERR_BAD_SHAPE;
+  if (vocab4(head) && vocab4(head)->V != V) return DELS_ERR_BAD_SHAPE;
   if (B == 0) return DELS_OK;
   if (!long_logits || !prior || !tok || !lp) return DELS_ERR_NULL_POINTER;
   if (!aligned16(long_logits) || !aligned16(prior) || !aligned16(tok) || !aligned16(lp) || (gap && !aligned16(gap)))
@@ -1541,7 +1546,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
       mb.D = D;
       mb.dest = eg;
       mb.smp.src_r = rr;
-      if (bf && !head->w_vocab4 && persistent_enabled() && !alpha_j && !beta_j && !sm.on && B <= sms && R <= 256) {
+      if (bf && !vocab4(head) && persistent_enabled() && !alpha_j && !beta_j && !sm.on && B <= sms && R <= 256) {
         // one cooperative launch for the whole block
         Gemm gg, gr, gv;
         if (!plan_store(gg, B, 3 * H, eg, head->w[0], D, hb, head->w[1], H, 128, L.gru_s0, L.gru_s1, ACT_NONE,
@@ -1594,7 +1599,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
         }
       }
       const float* G = static_cast<const float*>(head->w[3]);
-      if (bf && !head->w_vocab4 && G && fused_products_enabled() && !sm.on && B <= 64 && n > 1) {
+      if (bf && !vocab4(head) && G && fused_products_enabled() && !sm.on && B <= 64 && n > 1) {
         // Input-table path, fused variant (DELS_DRAFT_FUSED=1): two launches
         // per position —
         //   gates(j)        merge x_{j-1} from the previous position's records,
@@ -2088,7 +2093,7 @@ int dels_verify_block_sampled(const dels_local_head* head, const int32_t* draft_
   if (!draft_tokens || !draft_logprob || !draft_state || !long_logits || !target_logits || !out_accept_len ||
       !out_bonus || (!head->w_vocab && !head->w_vocab4))
     return DELS_ERR_NULL_POINTER;
-  if (const dels_w4* m = head->w_vocab4) {
+  if (const dels_w4* m = vocab4(head)) {
     if (!bf) return DELS_ERR_UNSUPPORTED;
     if (!m->data) return DELS_ERR_NULL_POINTER;
     if (!w4_ok(m->V, m->K, m->group) || m->K != head->d_rank || m->V != V) return DELS_ERR_BAD_SHAPE;
@@ -2156,8 +2161,8 @@ int dels_verify_block_sampled(const dels_local_head* head, const int32_t* draft_
   a.status = status;
   { PROF(DELS_KCLASS_VERIFY); DELS_CUDA(launch_verify_accept(a, s)); }
   // 3. l_S of the rejected positions: W_vocab r (rows with no head input are zero)
-  if (head->w_vocab4) {
-    W4Args w = w4_args(*head->w_vocab4, a.rg, B, status);
+  if (const dels_w4* m = vocab4(head)) {
+    W4Args w = w4_args(*m, a.rg, B, status);
     w.out = at<float>(workspace, L.ls);
     w.out_f32 = 1;
     w.ld_out = V;
