@@ -1553,7 +1553,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
                         gpart, nullptr, 0, status, sms) ||
             !plan_store(gr, B, R, hb, head->w[2], H, nullptr, nullptr, 0, 32, 1, 0, ACT_SILU, nullptr,
                         static_cast<uint16_t*>(rr), R, status, sms) ||
-            !plan_vocab(gv, head, B, V, n, rr, R, long_logits, logit_dtype, log_prior, alpha, beta,
+            !plan_combine(gv, B, V, n, rr, R, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
                           partials, L.partial_ld, status, sms, false, sm.on))
           return DELS_ERR_CUDA;
         PersistGruArgs P{};
@@ -1615,7 +1615,7 @@ int draft_block_impl(const dels_local_head* head, const void* long_logits, dels_
                         ACT_SILU, nullptr, static_cast<uint16_t*>(rr), R, status, sms) ||
             !plan_store(gh, B, 3 * H, hb, head->w[1], H, nullptr, nullptr, 0, kHhTile, L.hh_splits, 0, ACT_NONE,
                         gpart, nullptr, 0, status, sms) ||
-            !plan_vocab(gv, head, B, V, n, rr, R, long_logits, logit_dtype, log_prior, alpha, beta,
+            !plan_combine(gv, B, V, n, rr, R, head->w_vocab, long_logits, logit_dtype, log_prior, alpha, beta,
                           partials, L.partial_ld, status, sms, false, sm.on))
           return DELS_ERR_CUDA;
         // the rank product's K splits form one cluster per output tile
