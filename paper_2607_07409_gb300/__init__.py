@@ -701,11 +701,6 @@ def _row_args(t: torch.Tensor, shape, device: int, what: str):
     return t.data_ptr(), step, code
 
 
-def _stream_on(stream, device: int) -> Optional[int]:
-    """``_stream`` of a call on a device that is the current one."""
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
-
-
 def _of(t, dtype, shape, device: int, what) -> Optional[int]:
     """Device address of a dense tensor of this dtype and shape on this device."""
     if t is None:
@@ -1021,7 +1016,32 @@ def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-class RowProbs:
+class _Handle:
+    """What the handles below share. The stream that a handle is built on may still have work to do to the memory that the
+    handle is given (its workspace is zero-filled there, to begin with): the first call on each other stream waits for
+    that, on the device. (Within a capture it does not: an event of before is not known there. ``torch.cuda.graph`` has
+    waited for the device by then.)"""
+
+    def _built(self) -> None:
+        self._streams = {torch._C._cuda_getCurrentRawStream(self._dev)}
+        self._event = None
+        if not torch.cuda.is_current_stream_capturing():
+            self._event = torch.cuda.current_stream(self._dev).record_event()
+
+    def _on(self, stream) -> int:
+        """``_stream`` of a call on the handle's device, behind the handle's making."""
+        s = torch._C._cuda_getCurrentRawStream(self._dev) if stream is None else _stream(stream)
+        if s not in self._streams and self._event is not None and not torch.cuda.is_current_stream_capturing():
+            at = torch.cuda.ExternalStream(s, device=self.device) if s else torch.cuda.default_stream(self.device)
+            at.wait_event(self._event)
+            self._streams.add(s)
+        return s
+
+    def status(self, stream=None) -> int:
+        return dels_read_status(self.workspace, self._on(stream))
+
+
+class RowProbs(_Handle):
     """Probabilities of [rows, V] logits, plain or fused, as float32 or bfloat16: output and a workspace for
     repeated ``dels_row_probs`` calls."""
 
@@ -1037,6 +1057,7 @@ class RowProbs:
         self._ws = self.workspace.data_ptr()
         self._out = None
         self._call = lib().dels_row_probs
+        self._built()
 
     def __call__(self, logits: torch.Tensor, *, short=None, log_prior=None, alpha=None, beta=None,
                  temperature: float = 1.0, out=None, stream=None) -> torch.Tensor:
@@ -1055,15 +1076,11 @@ class RowProbs:
             if code != self._code:
                 raise ValueError(f"out must be {self.dtype}")
         r = self._call(ctypes.byref(x), self.rows, self.V, to, self._code, step, self._ws, self.ws_bytes,
-                       _stream_on(stream, self._dev))
+                       self._on(stream))
         if r != DELS_OK:
             raise DelsError(r, "dels_row_probs")
         _increment_version((out,))
         return out
-
-    def status(self, stream=None) -> int:
-        return dels_read_status(self.workspace, stream)
-
 
 def _probs_of(t: torch.Tensor, B: int, rows: int, V: int, device: int, what: str) -> Probs:
     """``dels_probs`` of a [B, rows, V] tensor (requests and rows may be strided). The caller keeps it alive."""
@@ -1081,7 +1098,7 @@ def _probs_of(t: torch.Tensor, B: int, rows: int, V: int, device: int, what: str
     return Probs(t.data_ptr(), code, sb, sr)
 
 
-class BlockVerifier:
+class BlockVerifier(_Handle):
     """Speculative sampling of drafted blocks from given probabilities and uniforms (``n = 0``: a token of each
     row): outputs and a workspace for repeated ``dels_verify_given`` calls."""
 
@@ -1097,6 +1114,7 @@ class BlockVerifier:
         self._own = [t.data_ptr() for t in (self.accept_len, self.bonus, self.workspace)]
         self._writes = (self.accept_len, self.bonus)
         self._call = lib().dels_verify_given
+        self._built()
 
     def __call__(self, tokens, target: torch.Tensor, uniforms: torch.Tensor, *, draft=None, lengths=None, stream=None):
         """(tokens kept of each request, the token after them), int32 [B] each, which the next call overwrites.
@@ -1115,17 +1133,13 @@ class BlockVerifier:
         acc, bonus, ws = self._own
         r = self._call(tok, ctypes.byref(p), None if q is None else ctypes.byref(q), u,
                        _of(lengths, torch.int32, (B,), dev, "lengths"), B, n, V, acc, bonus, ws, self.ws_bytes,
-                       _stream_on(stream, dev))
+                       self._on(stream))
         if r != DELS_OK:
             raise DelsError(r, "dels_verify_given")
         _increment_version(self._writes)
         return self.accept_len, self.bonus
 
-    def status(self, stream=None) -> int:
-        return dels_read_status(self.workspace, stream)
-
-
-class W4Matrix:
+class W4Matrix(_Handle):
     """A [V, K] matrix of 4-bit codes with a bf16 scale (and zero point) per group of inputs, laid out for
     ``project``. ``pack_w4`` makes one."""
 
@@ -1142,6 +1156,7 @@ class W4Matrix:
         self._ws = self.workspace.data_ptr()
         self._ref = ctypes.byref(self.struct)
         self._call = lib().dels_w4_project
+        self._built()
 
     def project(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32,
                 stream=None) -> torch.Tensor:
@@ -1157,15 +1172,11 @@ class W4Matrix:
             out = _empty_on(stream, (B, self.V), dtype, self.device)
         xp, xs, xc = _row_args(x, (B, self.K), dev, "x")
         op, os_, oc = _row_args(out, (B, self.V), dev, "out")
-        r = self._call(self._ref, xp, xc, xs, B, op, oc, os_, self._ws, self.ws_bytes, _stream_on(stream, dev))
+        r = self._call(self._ref, xp, xc, xs, B, op, oc, os_, self._ws, self.ws_bytes, self._on(stream))
         if r != DELS_OK:
             raise DelsError(r, "dels_w4_project")
         _increment_version((out,))
         return out
-
-    def status(self, stream=None) -> int:
-        return dels_read_status(self.workspace, stream)
-
 
 def pack_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, *, group: int,
             stream=None) -> W4Matrix:

@@ -1,5 +1,5 @@
 """The verification from given numbers where it can go wrong: empty columns beside a border, sums at
-float32's end, rows far longer than a vocabulary."""
+float32's end, rows far longer than a vocabulary, handles built behind unfinished work."""
 import math
 from fractions import Fraction
 
@@ -11,7 +11,8 @@ import paper_2607_07409_gb300 as dels
 pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
-F32 = torch.float32
+NAN = math.nan
+F32, BF16 = torch.float32, torch.bfloat16
 NONFINITE = dels.DELS_STATUS_NONFINITE
 
 
@@ -105,3 +106,74 @@ def test_a_long_row(V, offset):
         assert draw(p, x, h) == ([V // 2 + math.floor(at)], 0)
         n += 1
     assert n > 20
+
+
+# ---------------------------------------------------------------- handles built behind unfinished work
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_handle_built_behind_unfinished_work(handle):
+    """Built on a stream that still has to fill the memory that the handle is given, called on another one: what the
+    call writes, and the status it raises, stay."""
+    B, n, V = 64, 3, 5000
+    g = torch.Generator().manual_seed(2)
+    p = torch.softmax(torch.randn(B, n + 1, V, generator=g) * 3, -1).to(DEV)
+    tokens = p[:, :n].argmax(-1).to(torch.int32)
+    u = torch.rand(B, n + 1, generator=g).to(DEV)
+    rows = torch.randn(16, V, generator=g)
+    rows[5, 7] = NAN
+    rows = rows.to(DEV)
+    codes = torch.randint(0, 16, (500, 64), generator=g, dtype=torch.uint8).to(DEV)
+    scales = torch.ones(500, 2, dtype=BF16, device=DEV)
+    x = torch.randn(3, 64, generator=g).to(BF16).to(DEV)
+    one = dels.BlockVerifier(B, n, V, device=DEV)
+    want = [t.clone() for t in one(tokens, p, u)]
+    assert one.status() == 0
+    packed = dels.pack_w4(codes, scales, group=32)
+    y = packed.project(x).clone()
+    s = torch.cuda.Stream()
+    on = s.cuda_stream if handle else s
+    torch.cuda.synchronize()
+
+    def behind(make):
+        """make() with memory that the current stream has still to fill with other numbers."""
+        busy = [torch.empty(m, dtype=torch.uint8, device=DEV) for m in (256, 512, 1024, 256, 512) for _ in range(8)]
+        torch.cuda._sleep(100_000_000)
+        for t in busy:
+            t.fill_(1)
+        del t, busy
+        return make()
+
+    h = behind(lambda: dels.BlockVerifier(B, n, V, device=DEV))
+    acc, bonus = h(tokens, p, u, stream=on)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(acc, want[0]) and torch.equal(bonus, want[1]) and h.status() == 0
+    h = behind(lambda: dels.RowProbs(16, V, device=DEV))
+    got = h(rows, stream=on)
+    assert h.status(on) == NONFINITE
+    torch.cuda.synchronize()
+    assert torch.isnan(got[5]).all() and torch.isfinite(got[4]).all() and h.status() == 0
+    m = behind(lambda: dels.W4Matrix(packed.data, 500, 64, 32, False))
+    got = m.project(x, stream=on)
+    assert m.status(on) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(got, y) and m.status() == 0
+
+
+def test_handles_in_a_capture():
+    """Built before it and first called in it, on the capture's own stream; and built in it."""
+    g = torch.Generator().manual_seed(3)
+    x, u = torch.randn(4, 700, generator=g).to(DEV), torch.rand(4, 1, generator=g).to(DEV)
+    probs, pick = dels.RowProbs(4, 700, device=DEV), dels.BlockVerifier(4, 0, 700, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _, one = pick(None, probs(x).view(4, 1, 700), u)
+        p2, v2 = dels.RowProbs(4, 700, device=DEV), dels.BlockVerifier(4, 0, 700, device=DEV)
+        _, two = v2(None, p2(x).view(4, 1, 700), u)
+    for _ in range(2):
+        x.mul_(0.7)
+        graph.replay()
+        p = torch.softmax(x.double(), -1).cumsum(-1)
+        want = torch.searchsorted(p, u.double() * p[:, -1:], right=True).view(-1).tolist()
+        assert one.tolist() == two.tolist() == want
+    assert [h.status() for h in (probs, pick, p2, v2)] == [0] * 4
