@@ -173,6 +173,16 @@ typedef struct {
 size_t dels_selftest_timeout_bytes(void);
 int dels_selftest_timeout(void* workspace, size_t workspace_bytes, dels_stream_t stream);
 
+/*
+ * The same for the products with 4-bit weights of B requests (1 .. 128) by a [V, K] matrix in groups
+ * of 32. form 0: outputs of bf16 features; 1: of float32 ones; 2, 3: the records of a drafted position
+ * at temperature 0 and 1. stall 1: no block of the matrix is ever copied; 2: the end of the products
+ * is never reported. Limits: V a multiple of 8 up to 2^20, 1 <= K <= 65536.
+ */
+size_t dels_selftest_w4_timeout_bytes(int B, int V, int K);
+int dels_selftest_w4_timeout(int form, int stall, int B, int V, int K, void* workspace, size_t workspace_bytes,
+                             dels_stream_t stream);
+
 /* ---- self test of the Gumbel transform ---------------------------------- */
 
 /*

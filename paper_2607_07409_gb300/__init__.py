@@ -33,6 +33,7 @@ __all__ = [
     "dels_profile_enable", "dels_profile_reset", "dels_profile_read", "KCLASS",
     "dels_gru_input_table_bytes", "dels_gru_build_input_table", "gru_input_table",
     "dels_selftest_timeout_bytes", "dels_selftest_timeout", "dels_selftest_gumbel",
+    "dels_selftest_w4_timeout_bytes", "dels_selftest_w4_timeout",
     "dels_prior_workspace_bytes", "dels_prior_count", "dels_prior_log", "dels_prior_estimate", "estimate_prior",
     "make_head", "Drafter", "dtype_code",
     "Rows", "Teacher", "dels_score_workspace_bytes", "dels_score_rows",
@@ -115,6 +116,8 @@ _PROBS, _W4 = ctypes.POINTER(Probs), ctypes.POINTER(W4)
 _SIGS = {
     "dels_selftest_timeout_bytes": (_sz, []),
     "dels_selftest_timeout": (_i, [_vp, _sz, _vp]),
+    "dels_selftest_w4_timeout_bytes": (_sz, [_i, _i, _i]),
+    "dels_selftest_w4_timeout": (_i, [_i, _i, _i, _i, _i, _vp, _sz, _vp]),
     "dels_selftest_gumbel": (_i, [_vp, _vp, ctypes.c_longlong, _vp]),
     "dels_gru_input_table_bytes": (_sz, [ctypes.POINTER(LocalHead), _i]),
     "dels_gru_build_input_table": (_i, [ctypes.POINTER(LocalHead), _i, _vp, _sz, _vp, _sz, _vp]),
@@ -258,6 +261,15 @@ def dels_selftest_timeout_bytes() -> int:
 
 def dels_selftest_timeout(workspace, workspace_bytes: int, stream=None) -> int:
     return lib().dels_selftest_timeout(_ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def dels_selftest_w4_timeout_bytes(B: int, V: int, K: int) -> int:
+    return lib().dels_selftest_w4_timeout_bytes(B, V, K)
+
+
+def dels_selftest_w4_timeout(form: int, stall: int, B: int, V: int, K: int, workspace, workspace_bytes: int,
+                             stream=None) -> int:
+    return lib().dels_selftest_w4_timeout(form, stall, B, V, K, _ptr(workspace), workspace_bytes, _stream(stream))
 
 
 def dels_selftest_gumbel(bits, g, n: int, stream=None) -> int:

@@ -1399,6 +1399,69 @@ int dels_selftest_timeout(void* workspace, size_t workspace_bytes, dels_stream_t
   return DELS_OK;
 }
 
+namespace {
+
+// Parts of the 4-bit products' self test within its workspace.
+struct W4Stall {
+  size_t packed, x, out, longp, prior, partials, total;
+};
+bool w4_stall(int B, int V, int K, W4Stall* L) {
+  if (B < 1 || B > kMaxBatchTile || V < 8 || V > (1 << 20) || V % 8 || !w4_ok(V, K, 32)) return false;
+  const W4Layout m = w4_layout(V, K, 32, 0);
+  size_t at = kHeaderBytes;
+  const auto take = [&](size_t bytes) {
+    const size_t from = at;
+    at += (bytes + 255) / 256 * 256;
+    return from;
+  };
+  L->packed = take((size_t)m.tile_bytes * (size_t)m.tiles);
+  L->x = take((size_t)B * K * 4);
+  L->out = take((size_t)B * V * 4);
+  L->longp = take((size_t)B * V * 4);
+  L->prior = take((size_t)V * 4);
+  L->partials = take((size_t)B * (size_t)m.tiles * 16);          // a record a CTA, of one tile at least
+  L->total = at;
+  return true;
+}
+
+}  // namespace
+
+size_t dels_selftest_w4_timeout_bytes(int B, int V, int K) {
+  W4Stall L;
+  return w4_stall(B, V, K, &L) ? L.total : 0;
+}
+
+int dels_selftest_w4_timeout(int form, int stall, int B, int V, int K, void* workspace, size_t workspace_bytes,
+                             dels_stream_t stream) {
+  W4Stall L;
+  if (form < 0 || form > 3 || stall < 1 || stall > 2 || !w4_stall(B, V, K, &L)) return DELS_ERR_BAD_SHAPE;
+  if (!workspace || workspace_bytes < L.total) return DELS_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return DELS_ERR_ALIGNMENT;
+  const int sms = device_sm_count();
+  if (sms <= 0) return DELS_ERR_CUDA;
+  const dels_w4 m{at<uint8_t>(workspace, L.packed), V, K, 32, 0};
+  W4Args a = w4_args(m, at<uint8_t>(workspace, L.x), B, at<int>(workspace, 0));
+  a.x_f32 = form == 1;
+  a.stall = stall;
+  if (form < 2) {
+    a.out = at<float>(workspace, L.out);
+    a.out_f32 = 1;
+    a.ld_out = V;
+  } else {
+    a.longp = at<float>(workspace, L.longp);
+    a.long_f32 = 1;
+    a.ld_long = V;
+    a.prior = at<float>(workspace, L.prior);
+    a.alpha = a.beta = 0.5f;
+    a.j = 1;
+    a.sample = form == 3;
+    a.partials = at<uint8_t>(workspace, L.partials);
+    a.partial_ld = w4_records(a, sms);
+  }
+  DELS_CUDA(launch_w4_project(a, reinterpret_cast<cudaStream_t>(stream)));
+  return DELS_OK;
+}
+
 // ------------------------------------------------------- GRU input table
 
 size_t dels_gru_input_table_bytes(const dels_local_head* head, int V) {

@@ -279,6 +279,7 @@ struct W4Args {
   unsigned long long seed, step;
   void* partials;                // [B][partial_ld] RowAcc, a record a CTA: null for outputs
   int partial_ld;
+  int stall;                     // of the self test: 1 no block is copied, 2 no product's end is reported
 };
 // Records per request of a launch that is fused with the combine.
 int w4_records(const W4Args& a, int sms);

@@ -87,7 +87,8 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 // the groups' sums back and scaled into the thread's registers. Up to four such groups on an SM
 // run beside one another and share nothing but the features: one's waits are the others' time. Few tiles of a
 // long K are shared by several groups, each a range of it. A group's products and copies are issued by a warp
-// of its own, which meets the others at one named barrier a step; these go on without waiting there.
+// of its own, which meets the others at one named barrier a step; these go on without waiting there. (At an
+// mbarrier, with a time limit: 2 to 4 % more.)
 // (With every part of a step in warps of its own, behind mbarriers with buffers to spare, the
 // hand-overs' instructions took more than the overlap gave: 103 us against 80 at 8 requests.)
 // The features stay in shared memory; a K whose features do not fit is taken in parts.
@@ -270,6 +271,8 @@ struct W4Plan {
   int a_cols, d_cols;  // tensor memory of a group: its operand, its sums
   uint32_t tmem_cols;
   int smem;
+  int stall;           // of the self test: 1 no block is copied, 2 no product's end is reported
+  unsigned budget_ns;  // of a wait
 };
 
 template <int NB>
@@ -316,6 +319,14 @@ __device__ __forceinline__ void issue_products(uint32_t dcol, uint32_t acol, uin
                         idesc_f16_f32(128, N), ADD || term + 1 < TERMS || v || k);
         }
 }
+
+// Where a group waits.
+struct W4Waits {
+  uint64_t full[kW4Stages];          // a block of codes has come
+  uint64_t done;                     // a step's products are done
+  uint64_t last;                     // and all of them, where a wait has run out
+  volatile int passed;               // steps for which every warp has arrived, mod 2, as the issuing one has seen
+};
 
 // What a launch does with its products: outputs, or records of the fused rows at temperature 0 or 1.
 enum { kOutputs = 0, kRecords = 1, kKeys = 2 };
@@ -391,7 +402,12 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int N = NB < 16 ? 16 : NB;                  // requests of an MMA: rows past NB are its first ones again
   constexpr int H = kW4Halves<NB>, kMine = NB / H;      // requests of a thread
-  __shared__ uint64_t full[kW4Groups<NB>][kW4Stages], done[kW4Groups<NB>];
+  // Named barriers, behind that of __syncthreads(): each group's, of all its warps; each half's of a group, of its workers; each
+  // tile's that groups share. An id has one number of threads at a time: with a half's the same as its group's, at
+  // which the issuing warp was already waiting for the next step, a kernel faulted.
+  constexpr int kGroupBarrier = 1, kHalfBarrier = kGroupBarrier + kW4Groups<NB>, kTileBarrier = kHalfBarrier + kW4Groups<NB> * H;
+  static_assert(kTileBarrier + kW4Groups<NB> <= 16, "a CTA's named barriers");
+  __shared__ W4Waits waits[kW4Groups<NB>];
   __shared__ uint32_t tmem_base;
   __shared__ volatile int abort_flag;
   __shared__ uint32_t largest[NB];          // bits of the requests' largest features
@@ -407,6 +423,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   // else of a group's warps one issues products and the next one copies: not in the same quarter of the SM in all groups
   const int place = warp % (4 * H), issuer = grp & 3, copier = issuer ^ 1;
   const int b0 = blockIdx.y * NB;
+  W4Waits& bar = waits[grp];
   uint8_t* ring = smem + (size_t)grp * p.stages * p.stage_bytes;
   uint4* operand = reinterpret_cast<uint4*>(smem + (size_t)p.groups * p.stages * p.stage_bytes);
   if (warp == 0) {
@@ -416,8 +433,10 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   if (tid == 0) {
     abort_flag = 0;
     for (int g = 0; g < p.groups; ++g) {
-      for (int i = 0; i < p.stages; ++i) mbar_init(&full[g][i], 1);
-      mbar_init(&done[g], 1);
+      for (int i = 0; i < p.stages; ++i) mbar_init(&waits[g].full[i], 1);
+      mbar_init(&waits[g].done, 1);
+      mbar_init(&waits[g].last, 1);
+      waits[g].passed = 0;
     }
     fence_mbarrier_init();
   }
@@ -433,15 +452,15 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   const int kb0 = a.lay.blocks * share / split, own_blocks = a.lay.blocks * (share + 1) / split - kb0;
   const long long tile0 = (long long)slot * gridDim.x + blockIdx.x, apart = (long long)gridDim.x * (p.groups / split);
   const long long rounds = (a.lay.tiles + apart - 1) / apart;
-  const int copies = tile0 < a.lay.tiles ? (int)((a.lay.tiles - tile0 + apart - 1) / apart) * own_blocks : 0;
+  const int copies = p.stall != 1 && tile0 < a.lay.tiles ? (int)((a.lay.tiles - tile0 + apart - 1) / apart) * own_blocks : 0;
   int to_copy = copies - p.stages, next_kb = p.stages % own_blocks, next_st = 0;            // of the thread that copies
   const uint8_t* next_block = a.packed + (tile0 + p.stages / own_blocks * apart) * a.lay.tile_bytes +
                               (long long)(kb0 + next_kb) * a.lay.block_bytes;
   const auto issue_copy = [&] {
     if (to_copy <= 0) return;
     --to_copy;
-    mbar_arrive_expect_tx(&full[grp][next_st], a.lay.block_bytes);
-    bulk_load(ring + next_st * p.stage_bytes, next_block, a.lay.block_bytes, &full[grp][next_st]);
+    mbar_arrive_expect_tx(&bar.full[next_st], a.lay.block_bytes);
+    bulk_load(ring + next_st * p.stage_bytes, next_block, a.lay.block_bytes, &bar.full[next_st]);
     next_block += a.lay.block_bytes;
     if (++next_st == p.stages) next_st = 0;
     if (++next_kb == own_blocks) {
@@ -465,11 +484,11 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   if ((kApart ? issues : place == copier) && lane < p.stages) {             // the first ones, a lane each
     const long long tile = tile0 + lane / own_blocks * apart;
     const int kb = kb0 + lane % own_blocks;
-    if (tile < a.lay.tiles) {
-      mbar_arrive_expect_tx(&full[grp][lane], a.lay.block_bytes);
+    if (lane < copies) {
+      mbar_arrive_expect_tx(&bar.full[lane], a.lay.block_bytes);
       bulk_load(ring + (size_t)lane * p.stage_bytes,
                 a.packed + tile * a.lay.tile_bytes + (long long)kb * a.lay.block_bytes, a.lay.block_bytes,
-                &full[grp][lane]);
+                &bar.full[lane]);
     }
   }
 
@@ -533,13 +552,30 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   const uint32_t quadrant = (uint32_t)(warp & 3) << 21;                // the warp's 32 lanes of tensor memory
   const uint32_t x0 = (uint32_t)smem_desc_plain(smem_u32(operand), NB * 16, 0) + (uint32_t)(kb0 * 4) * (4 * NB);
   bool dead = false;                        // a wait ran out: the rest runs through without waiting
-  const auto wait = [&](uint64_t* bar, int parity) {
+  const auto ran_out = [&](uint32_t polls, uint64_t& deadline) {
     // (the clock is read in long waits alone: a reading takes about 1000 cycles)
+    if (polls & 255u) return;
+    if (!deadline) deadline = globaltimer_ns() + p.budget_ns;
+    else if (abort_flag || globaltimer_ns() > deadline) abort_flag = dead = true;
+  };
+  const auto wait = [&](uint64_t* at, int parity) {
     uint64_t deadline = 0;
-    for (uint32_t polls = 1; !mbar_try_wait(bar, (uint32_t)parity) && !dead; ++polls) {
-      if (polls & 255u) continue;
-      if (!deadline) deadline = globaltimer_ns() + kWaitBudgetNs;
-      else if (abort_flag || globaltimer_ns() > deadline) abort_flag = dead = true;
+    for (uint32_t polls = 1; !mbar_try_wait(at, (uint32_t)parity) && !dead; ++polls) ran_out(polls, deadline);
+    __syncwarp();
+  };
+  // A step's products, `step` its number mod 2. They are done: every warp of the group has arrived for the step, and this
+  // one may for the next. A thread that waits for them no more waits for that itself: two arrivals of a warp in one step would
+  // stand for another's, the issuing warp's among them, which would be left without partners at its last. (It comes: each
+  // warp arrives once for each step, and waits for nothing else without a limit.)
+  const auto wait_done = [&](int step) {
+    uint64_t deadline = 0;
+    for (uint32_t polls = 1; dead || !mbar_try_wait(&bar.done, (uint32_t)step); ++polls) {
+      if (dead) {
+        const uint64_t limit = globaltimer_ns() + p.budget_ns;
+        while (bar.passed == step && globaltimer_ns() < limit) {}
+        break;
+      }
+      ran_out(polls, deadline);
     }
     __syncwarp();
   };
@@ -575,7 +611,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     float scale[NG];
     const auto load = [&](int i) {
       const int s0 = i % kSteps * U;
-      if (s0 == 0) wait(&full[grp][st], ph);
+      if (s0 == 0) wait(&bar.full[st], ph);
       const uint8_t* block = ring + (size_t)st * p.stage_bytes;
       const uint8_t* scales = block + 4 * kW4UnitBytes + s0 / G * 256 + row * 2;
       const uint8_t* zeros = block + 4 * kW4UnitBytes + 4 / G * 256 + s0 / G * 64 + (row >> 1);
@@ -600,18 +636,21 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
       if (s0 + U == 4 && ++st == p.stages) st = 0, ph ^= 1;
     };
     const auto issue = [&](int i) {         // (every worker has left a step's operand in its place)
-      asm volatile("bar.sync %0, %1;" ::"r"(grp + 1), "n"(kW4Group<NB, kApart>) : "memory");
+      asm volatile("bar.sync %0, %1;" ::"r"(kGroupBarrier + grp), "n"(kW4Group<NB, kApart>) : "memory");
       tc_fence_after();
       if (elect_one()) {
         const uint32_t x = x0 + (uint32_t)(i * U) * (4 * NB);
         if (G > U && i % kSteps > 0) issue_products<NB, TERMS, U, U, true>(dcol, acol, x, p.part_units);
         else issue_products<NB, TERMS, U, (G > U ? U : G), false>(dcol, acol, x, p.part_units);
-        tc_commit(&done[grp]);
+        if (p.stall != 2) tc_commit(&bar.done);
+        bar.passed = dph ^ 1;
       }
       __syncwarp();
     };
-    const auto copy_next = [&](int i) {     // (and read its block)
-      if (i % kSteps == kSteps - 1 && lane == 0) issue_copy();
+    // (and read its block. Not once a wait has run out: its last copy may be on its way, and the next would count into
+    // that one's phase. A worker has waited for that itself.)
+    const auto copy_next = [&](int i) {
+      if (i % kSteps == kSteps - 1 && lane == 0 && !(kApart ? abort_flag != 0 : dead)) issue_copy();
       __syncwarp();
     };
     if (issues) {
@@ -634,9 +673,9 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
       tmem_st_wait();
       tc_fence_before();
       if (!kApart && place == issuer) issue(i);
-      else asm volatile("bar.arrive %0, %1;" ::"r"(grp + 1), "n"(kW4Group<NB, kApart>) : "memory");
+      else asm volatile("bar.arrive %0, %1;" ::"r"(kGroupBarrier + grp), "n"(kW4Group<NB, kApart>) : "memory");
       if (i + 1 < blocks * kSteps) load(i + 1);
-      wait(&done[grp], dph);
+      wait_done(dph);
       dph ^= 1;
       tc_fence_after();
       if (!kApart && place == copier) copy_next(i);
@@ -673,7 +712,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     if (SPLIT && live) {
       // ---- the shares of a tile, added up by its first group in their order
       const auto all_shares = [&] {
-        asm volatile("bar.sync %0, %1;" ::"r"(kW4Groups<NB> * (1 + H) + slot + 1), "r"(split * 128 * H) : "memory");
+        asm volatile("bar.sync %0, %1;" ::"r"(kTileBarrier + slot), "r"(split * 128 * H) : "memory");
       };
       float* at = joins + ((size_t)slot * (split - 1) * NB + half * kMine) * kW4Rows + row;
       if (share) {
@@ -693,9 +732,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
     const long long v = tile * kW4Rows + row;
     const int n0 = half * kMine, nb = min(kMine, a.B - b0 - n0);        // the thread's requests
     float* side = sides + (size_t)(grp * H + half) * S * kW4Pitch;
-    const auto together = [&] {             // (barriers of their own: the issuing warp is at the group's already)
-      asm volatile("bar.sync %0, 128;" ::"r"(kW4Groups<NB> + grp * H + half + 1) : "memory");
-    };
+    const auto together = [&] { asm volatile("bar.sync %0, 128;" ::"r"(kHalfBarrier + grp * H + half) : "memory"); };
     // Products of 8 requests, n on. (All of them before any is stored: the compiler keeps each reading of back[]
     // behind the stores before it, and one after another they took half of 64 requests' time.)
     const auto products = [&](int n, float (&y)[8]) {
@@ -801,11 +838,16 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   __syncthreads();
   if (abort_flag) {                         // a CTA that gives up has its copies and products in flight end first
     if ((kApart ? issues : place == copier) && lane == 0) {
-      const uint64_t limit = globaltimer_ns() + kWaitBudgetNs / 4;
+      const uint64_t limit = globaltimer_ns() + p.budget_ns / 4;
       const int issued = min(copies, copies - to_copy);
       for (int i = max(0, issued - p.stages); i < issued; ++i)
-        while (!mbar_try_wait(&full[grp][i % p.stages], (i / p.stages) & 1) && globaltimer_ns() < limit) {}
-      while (!mbar_try_wait(&done[grp], dph ^ 1) && globaltimer_ns() < limit) {}
+        while (!mbar_try_wait(&bar.full[i % p.stages], (i / p.stages) & 1) && globaltimer_ns() < limit) {}
+    }
+    __syncwarp();
+    if ((kApart ? issues : place == issuer) && elect_one()) {      // (the thread that issued them)
+      const uint64_t limit = globaltimer_ns() + p.budget_ns / 4;
+      tc_commit(&bar.last);
+      while (!mbar_try_wait(&bar.last, 0) && globaltimer_ns() < limit) {}
     }
     __syncthreads();
   }
@@ -858,6 +900,8 @@ cudaError_t launch_nb(const W4Args& a, cudaStream_t s) {
   p.part_units = (int)(std::min(whole, beside) / unit / 4 * 4);
   p.parts = (4 * a.lay.blocks + p.part_units - 1) / p.part_units;
   p.stages = (int)std::min<long long>(kW4Stages, (room - p.part_units * unit) / ((long long)p.groups * p.stage_bytes));
+  p.stall = a.stall;
+  p.budget_ns = (unsigned)(a.stall ? kWaitBudgetNs / 20 : kWaitBudgetNs);
   p.smem = (int)(p.groups * p.stages * p.stage_bytes + p.part_units * unit) + join + side;
   const auto k = p.split > 1 ? k_w4_project<NB, TERMS, EPI, true> : k_w4_project<NB, TERMS, EPI, false>;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(k), p.smem);

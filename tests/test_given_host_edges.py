@@ -1,4 +1,4 @@
-"""Host-side checks of 4-bit vocabulary matrices of local heads (no GPU needed)."""
+"""Host-side checks of 4-bit vocabulary matrices of local heads, and of the products' self test (no GPU needed)."""
 import ctypes
 import os
 import subprocess
@@ -61,3 +61,13 @@ def test_a_head_with_w_vocab_is_read_no_further(dels):
 ])
 def test_heads_with_a_4_bit_matrix(dels, code, vocab, w4):
     assert draft(dels, head(dels, vocab, **w4)) == code
+
+
+@pytest.mark.parametrize("code,args", [
+    (-2, (4, 1, 2, 128, 32, 4096, 1 << 20)), (-2, (0, 0, 2, 128, 32, 4096, 1 << 20)), (-2, (0, 3, 2, 128, 32, 4096, 1 << 20)),
+    (-2, (0, 1, 0, 128, 32, 4096, 1 << 20)), (-2, (0, 1, 129, 128, 32, 4096, 1 << 20)), (-2, (0, 1, 2, 12, 32, 4096, 1 << 20)),
+    (-2, (0, 1, 2, 128, 0, 4096, 1 << 20)), (-5, (0, 1, 2, 128, 32, None, 1 << 20)), (-5, (0, 1, 2, 128, 32, 4096, 256)),
+    (-4, (0, 1, 2, 128, 32, 4104, 1 << 20)),
+])
+def test_the_self_test_of_4_bit_products_refuses(dels, code, args):
+    assert dels.lib().dels_selftest_w4_timeout(*args, None) == code
