@@ -674,8 +674,8 @@ int dels_w4_pack(const uint8_t* codes, const void* scales, const uint8_t* zeros,
  * out[b, v] = sum_k w[v, k] x[b, k].  x [device] [B, K] of x_dtype, x_stride elements
  * from one row to the next (0: K); out [device] [B, V] of out_dtype, out_stride (0: V).
  * Products are exact, sums float32, a group's at a time before its scale. A request's
- * features are held to 2^-40 of its largest one (float32 ones as three terms); one with
- * infinities or NaN has NaN throughout. Equal calls give equal bits.
+ * features are held to 2^-40 of its largest one, float32 ones (as three terms) to 2^-35;
+ * a request with infinities or NaN has NaN throughout. Equal calls give equal bits.
  * workspace >= 256 bytes. Limits: 0 <= B <= 65535; pointers aligned to their elements.
  */
 size_t dels_w4_project_workspace_bytes(const dels_w4* w, int B);

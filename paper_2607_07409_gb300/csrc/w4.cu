@@ -75,9 +75,9 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 // pair takes the zero point off. (Without an exponent, as multiples of 2^-24, the codes need neither, but the
 // tensor cores align such numbers' products by the exponent they do not have, ten bits too far
 // up: sums were off by 8e-7 of themselves, now by 1e-7.) A request's features are scaled by a power of
-// two to 2^15 at most: fp16 then holds bf16 features exactly down to 2^-32 of the request's
-// largest and what is smaller to 2^-40 of that; float32 features are three terms, of 11 bits of a fixed
-// point each, to the same 2^-40. (A request with infinities or NaN has NaN throughout.)
+// two: bf16 ones to 2^16 at most, so that fp16 holds them exactly down to 2^-32 of the request's
+// largest and what is smaller to 2^-40 of that; float32 ones, to 2^15, are three terms, two of 12 bits of a fixed
+// point with their signs and one of 11, to 2^-35 of the largest. (A request with infinities or NaN has NaN throughout.)
 // mma.sync, with the same operands, issues at most one such product in 32 cycles of a quarter
 // SM: 151936 x 2560 for 8 requests 45 us, 151936 x 256 for 64 37 us, at that rate.
 //
@@ -226,8 +226,12 @@ struct Features {
   }
 };
 
-// A request's power of two: its features' largest, of these bits, comes to 2^14 .. 2^15.
-__device__ __forceinline__ int feature_shift(uint32_t bits) { return bits ? 14 - ilogbf(__uint_as_float(bits)) : 0; }
+// A request's power of two: its features' largest, of these bits, comes to 2^15 .. 2^16 (a bf16 number there is below fp16's
+// largest, 65504), of several terms to 2^14 .. 2^15 (the first one is rounded, up to 2^15).
+template <int TERMS>
+__device__ __forceinline__ int feature_shift(uint32_t bits) {
+  return bits ? (TERMS == 1 ? 15 : 14) - ilogbf(__uint_as_float(bits)) : 0;
+}
 __device__ __forceinline__ float pow2i(int e) { return __int_as_float((e + 127) << 23); }    // -126 .. 127
 
 // 8 features of a lane, scaled by f.x f.y (two factors: the power may be past float32's range), as TERMS
@@ -241,11 +245,12 @@ __device__ __forceinline__ void put_features(const float (&x)[8], const float2& 
     f32x2 r = mul2(mul2(pair2(x[2 * i], x[2 * i + 1]), f0), f1);
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
-      // of several terms each but the last is a whole multiple of its place's, 11 bits of them
+      // of several terms each but the last is a whole multiple of its place, 2^11 of them at most: 2^4, and 2^-8 of what
+      // is left; the last one is rounded, by 2^-21 at most
       f32x2 d = r;
       float d0, d1;
       if (k + 1 < TERMS) {
-        const float place = k ? 98304.f : 201326592.f;                    // 1.5 2^(23 - 7), 1.5 2^(23 + 4)
+        const float place = k ? 49152.f : 201326592.f;                    // 1.5 2^(23 - 8), 1.5 2^(23 + 4)
         d = add2(add2(r, both2(place)), both2(-place));
         split2(d, d0, d1);
         r = add2(r, pair2(-d0, -d1));
@@ -513,7 +518,7 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   __syncthreads();
   if (tid < NB) {
     const bool finite = largest[tid] < 0x7F800000u;
-    const int up = finite ? feature_shift(largest[tid]) : 0, sh = -up;
+    const int up = finite ? feature_shift<TERMS>(largest[tid]) : 0, sh = -up;
     scaled[tid] = make_float2(pow2i(up / 2), pow2i(up - up / 2));
     back[0][tid] = finite ? pow2i(sh / 2) : NAN;
     back[1][tid] = finite ? pow2i(sh - sh / 2) : NAN;
