@@ -77,13 +77,14 @@ __device__ __forceinline__ void put4(__nv_bfloat16* out, const float (&x)[4]) {
 __device__ __forceinline__ void put1(float* out, float x) { *out = x; }
 __device__ __forceinline__ void put1(__nv_bfloat16* out, float x) { *out = __float2bfloat16_rn(x); }
 
-// CTAs an SM (its registers): five of rows that fit, of fused float32 ones four (774 fused bf16 rows of 32000, to
-// float32: at three 67.7 us, at five 57.9; 155 of 32003 to bf16 20.5 and 16.9).
-template <typename T, int F>
-constexpr int kProbsCtas = F == kPlain || sizeof(T) == 2 ? 5 : 4;
+// CTAs an SM (its registers): five of plain rows and of fused bf16 ones that are held, of other fused ones four (774 fused
+// bf16 rows of 32000, to float32: at three 67.7 us, at five 57.9; 155 of 32003 to bf16 20.5 and 16.9. Not held, 64 of
+// 500000, float32 and bf16: at three 285 and 231 us, at four 258 and 219, where the float32 ones spill some registers; bf16 at five 256).
+template <typename T, int F, bool HOLD>
+constexpr int kProbsCtas = F == kPlain || (HOLD && sizeof(T) == 2) ? 5 : 4;
 
 template <typename T, int F, bool VEC, typename O, bool HOLD>
-__global__ void __launch_bounds__(kStreamThreads, kProbsCtas<T, F>) k_row_probs(const ProbsArgs a) {
+__global__ void __launch_bounds__(kStreamThreads, kProbsCtas<T, F, HOLD>) k_row_probs(const ProbsArgs a) {
   using H = std::conditional_t<F == kPlain, T, float>;
   extern __shared__ __align__(16) uint8_t smem[];
   H* held = reinterpret_cast<H*>(smem);
