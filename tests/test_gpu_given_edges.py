@@ -1,5 +1,6 @@
 """The verification from given numbers where it can go wrong: empty columns beside a border, sums at
-float32's end, rows far longer than a vocabulary, handles built behind unfinished work."""
+float32's end, rows far longer than a vocabulary, handles built behind unfinished work; how
+exact probabilities are."""
 import math
 from fractions import Fraction
 
@@ -177,3 +178,46 @@ def test_handles_in_a_capture():
         want = torch.searchsorted(p, u.double() * p[:, -1:], right=True).view(-1).tolist()
         assert one.tolist() == two.tolist() == want
     assert [h.status() for h in (probs, pick, p2, v2)] == [0] * 4
+
+
+# ---------------------------------------------------------------- how exact probabilities are
+
+def below(c):
+    """The float32 number at or below c."""
+    f = torch.tensor(c, dtype=F32)
+    return (f if f.item() <= c else torch.nextafter(f, torch.tensor(0.0))).item()
+
+
+def rough(lo, hi):
+    """A temperature whose log2(e) / T lies nearly a whole step above a float32 number."""
+    ts = torch.linspace(lo, hi, 4001, dtype=F32).tolist()
+    return max(ts, key=lambda t: 1 - below(math.log2(math.e) / t) / (math.log2(math.e) / t))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,T", [(1000, 1.0), (32003, 0.7), (151936, 1.0), (500009, 1.0)])
+def test_probabilities_norm(V, T, dtype):
+    """||p - softmax|| / ||softmax|| of float32 outputs. The norm is the likely entries', whose exponents are within 16 of the
+    largest: the difference and its product are rounded by 0.3 steps of 2^-20 (rms), each 2e-7 of such an entry and 1e-7 over
+    all; the exponential by 2^-23 or so, the row's own factor by three roundings, 2^-23 together: 3e-7 holds them all."""
+    g = torch.Generator().manual_seed(V)
+    x = (torch.randn(8, V, generator=g) * 3).to(dtype).to(DEV)
+    h = dels.RowProbs(8, V, device=DEV)
+    want = torch.softmax(x.double() / T, -1)
+    got = h(x, temperature=T).double()
+    assert h.status() == 0
+    assert ((got - want).norm(dim=-1) <= 3e-7 * want.norm(dim=-1)).all(), ((got - want).norm(dim=-1) / want.norm(dim=-1)).max()
+
+
+@pytest.mark.parametrize("V", [20011, 151936, 500009])
+def test_the_scale_of_all_exponents(V):
+    """A likely entry beside many that are far below and together have as much: roundings of their exponents differ and go
+    both ways, so that the likely one's probability is off by those of the row's factor, 3 2^-24, and of a sum of
+    exponentials of 2^-23, 3e-7 in all. (With log2(e) / T cut to float32 all exponents are off the same way by 12 2^-23,
+    times the others' share: 4e-7 and more.)"""
+    T = rough(0.95, 1.05)
+    x = torch.randn(4, V, generator=torch.Generator().manual_seed(V)).to(DEV)
+    x[:, 77] = math.log(V) + 0.5
+    h = dels.RowProbs(4, V, device=DEV)
+    got = h(x, temperature=T).double()[:, 77] / torch.softmax(x.double() / T, -1)[:, 77]
+    assert h.status() == 0 and ((got - 1).abs() <= 3e-7).all(), got - 1
