@@ -1055,7 +1055,8 @@ class _Handle:
 
 class RowProbs(_Handle):
     """Probabilities of [rows, V] logits, plain or fused, as float32 or bfloat16: output and a workspace for
-    repeated ``dels_row_probs`` calls."""
+    repeated ``dels_row_probs`` calls. They have no gradient: to the autograd engine they are constants, whatever the
+    logits require (``distill_loss`` is the differentiable one)."""
 
     def __init__(self, rows: int, V: int, dtype: torch.dtype = torch.float32, device=None):
         self.rows, self.V, self.dtype = rows, V, dtype
@@ -1073,8 +1074,8 @@ class RowProbs(_Handle):
 
     def __call__(self, logits: torch.Tensor, *, short=None, log_prior=None, alpha=None, beta=None,
                  temperature: float = 1.0, out=None, stream=None) -> torch.Tensor:
-        """Probabilities [rows, V]; ``out``: where they go (rows may be strided), else the handle's own tensor,
-        which its next call overwrites."""
+        """Probabilities [rows, V]; ``out``: where they go (rows may be strided; none of the inputs), else the handle's own
+        tensor, which its next call overwrites."""
         _need_current(self._dev)
         x = rows_of(self.rows, self.V, logits, short, log_prior, alpha, beta, temperature)
         if logits.get_device() != self._dev:
@@ -1153,7 +1154,8 @@ class BlockVerifier(_Handle):
 
 class W4Matrix(_Handle):
     """A [V, K] matrix of 4-bit codes with a bf16 scale (and zero point) per group of inputs, laid out for
-    ``project``. ``pack_w4`` makes one."""
+    ``project``. ``pack_w4`` makes one. Products have no gradient: to the autograd engine they are constants, whatever the
+    features require."""
 
     def __init__(self, data: torch.Tensor, V: int, K: int, group: int, zeros: bool):
         if (not data.is_cuda or data.dtype is not torch.uint8 or not data.is_contiguous() or data.data_ptr() % 16

@@ -69,8 +69,10 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 // y = W x on the tensor cores (tcgen05, the weights from tensor memory).
 //
 // A code minus its zero point is a whole number of -15 .. 15: fp16 operands hold it, its products with
-// a feature's 11 bits are exact, and a group's sum is float32 and scaled there. fp16's 10 bits of
-// mantissa hold a code where it lies in a byte, low or high: (w & 0x000F000F) | 0x6400 is 1024 + c
+// a feature's 11 bits are exact, and a group's sum is float32 and scaled there. Codes become fp16 by the
+// published way of writing a small whole number into the mantissa of a number whose last place is 1, and taking
+// that number off (Kim et al. 2022, "Who Says Elephants Can't Run"): fp16's 10 bits of mantissa hold a code
+// where it lies in a byte, low or high: (w & 0x000F000F) | 0x6400 is 1024 + c
 // and the high ones' 1024 + 16 c, so that a word of 8 codes takes 4 masks and a shift, and an fma a
 // pair takes the zero point off. (Without an exponent, as multiples of 2^-24, the codes need neither, but the
 // tensor cores align such numbers' products by the exponent they do not have, ten bits too far
@@ -93,11 +95,15 @@ __global__ void __launch_bounds__(kPackThreads) k_w4_pack(const W4PackArgs a) {
 // hand-overs' instructions took more than the overlap gave: 103 us against 80 at 8 requests.)
 // The features stay in shared memory; a K whose features do not fit is taken in parts.
 //
-// What bounds it: a step (four units of 32 inputs, two with 9 to 16 requests and with more than 32) goes from one of
-// its parts to the next, 1300 cycles, most of them the instructions that take the codes apart: four warps a
-// scheduler issue about three quarters of the time. 151936 x 1024 for one request 17.9 us, x 2560 for 8 35.8 us
-// (12.3 and 30.7 for the bytes at a copy's rate), 151936 x 256 for 64 16.8 us (6.1), 32003 x 1000 for 5 with
-// float32 features 9.7 us (2.7; a start of 4 us, eight steps one after another).
+// What bounds it: the length of a step's chain (four units of 32 inputs, two with 9 to 16 requests and with more than
+// 32): it goes from one of its parts to the next, 1300 cycles, most of them the instructions that take the codes apart. With
+// 8 requests the warps issue in two thirds of all cycles, with one and with 64 in half of them, the tensor cores
+// are busy for 9 to 15 % (ncu, cold). 151936 x 1024 for one request 17.6 us, x 2560 for 8 35.4 us
+// (12.3 and 30.7 for the bytes at a copy's rate), 151936 x 256 for 64 16.7 us (6.1), 32003 x 1000 for 5 with
+// float32 features 9.4 us (2.7; a start of 4 us, eight steps one after another, some registers spilled).
+//
+// Records of a drafted position come in the products' turn from the same warps: 64 requests and K 256 take 0.67 ms a
+// block of 16 where a bf16 matrix takes 0.45 (temperature 0; 0.77 and 0.58 at 1), one request and K 1024 0.58 for 0.88.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
