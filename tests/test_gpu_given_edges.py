@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2607_07409_gb300 as dels
+from test_gpu_given import Block
 
 pytestmark = pytest.mark.gpu
 
@@ -107,6 +108,13 @@ def test_a_long_row(V, offset):
         assert draw(p, x, h) == ([V // 2 + math.floor(at)], 0)
         n += 1
     assert n > 20
+
+
+@pytest.mark.parametrize("p,q", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, None), (BF16, None)])
+@pytest.mark.parametrize("B,n,V,offset", [(2, 2, 2200008, 0), (1, 3, 2200001, 1), (160, 1, 262403, 0)])
+def test_long_rows_of_blocks(B, n, V, offset, p, q):
+    """Blocks whose rows are closed in parts: against the definition."""
+    Block(B, n, V, B + n, p, q).check(offset=offset, pitch=V + offset)
 
 
 # ---------------------------------------------------------------- handles built behind unfinished work
