@@ -79,7 +79,8 @@ __device__ __forceinline__ void put1(__nv_bfloat16* out, float x) { *out = __flo
 
 // CTAs an SM (its registers): five of plain rows and of fused bf16 ones that are held, of other fused ones four (774 fused
 // bf16 rows of 32000, to float32: at three 67.7 us, at five 57.9; 155 of 32003 to bf16 20.5 and 16.9. Not held, 64 of
-// 500000, float32 and bf16: at three 285 and 231 us, at four 258 and 219, where the float32 ones spill some registers; bf16 at five 256).
+// 500000, float32 and bf16: at three 285 and 231 us, at four 258 and 219, where the float32 ones spill some
+// registers; bf16 at five 256).
 template <typename T, int F, bool HOLD>
 constexpr int kProbsCtas = F == kPlain || (HOLD && sizeof(T) == 2) ? 5 : 4;
 

@@ -413,10 +413,11 @@ __global__ void __launch_bounds__(kW4Groups<NB> * kW4Group<NB, EPI == kOutputs>,
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int N = NB < 16 ? 16 : NB;                  // requests of an MMA: rows past NB are its first ones again
   constexpr int H = kW4Halves<NB>, kMine = NB / H;      // requests of a thread
-  // Named barriers, behind that of __syncthreads(): each group's, of all its warps; each half's of a group, of its workers; each
-  // tile's that groups share. An id has one number of threads at a time: with a half's the same as its group's, at
+  // Named barriers, behind that of __syncthreads(): each group's, of all its warps; each half's of a group, of its
+  // workers; each tile's that groups share. An id has one number of threads at a time: with a half's the same as its group's, at
   // which the issuing warp was already waiting for the next step, a kernel faulted.
-  constexpr int kGroupBarrier = 1, kHalfBarrier = kGroupBarrier + kW4Groups<NB>, kTileBarrier = kHalfBarrier + kW4Groups<NB> * H;
+  constexpr int kGroupBarrier = 1, kHalfBarrier = kGroupBarrier + kW4Groups<NB>;
+  constexpr int kTileBarrier = kHalfBarrier + kW4Groups<NB> * H;
   static_assert(kTileBarrier + kW4Groups<NB> <= 16, "a CTA's named barriers");
   __shared__ W4Waits waits[kW4Groups<NB>];
   __shared__ uint32_t tmem_base;
